@@ -84,7 +84,26 @@ enum {
     EP_TIMER_GRAPH_BANDWIDTH = 6, /* all kernels of ep_graph_bandwidth */
     EP_TIMER_RELABEL = 7,        /* all kernels of ep_relabel_graph and ep_permute_rows */
     EP_TIMER_BALANCE = 8,        /* the kernels of ep_migrate / ep_balance other than the sort */
-    EP_TIMER_COUNT = 9
+    EP_TIMER_NORM = 9,           /* ep_rms_norm, ep_rms_norm_backward, ep_quantize_rows */
+    EP_TIMER_LINEAR = 10,        /* all kernels of ep_linear and ep_linear_backward */
+    EP_TIMER_ROUTE = 11,         /* all kernels of ep_route and ep_route_backward */
+    EP_TIMER_COUNT = 12
+};
+
+/* Element types of the partition head's operators (ep_rms_norm, ep_linear, ep_route and their gradients). */
+enum {
+    EP_F32 = 0,
+    EP_BF16 = 1,
+    EP_F16 = 2,
+    EP_E4M3 = 3 /* 8 bits: 1 sign, 4 exponent, 3 mantissa bits, largest value 448, no infinities */
+};
+
+/* Activations of ep_linear. */
+enum {
+    EP_ACT_NONE = 0,
+    EP_ACT_RELU = 1, /* max(z, 0); slope 0 at z = 0 */
+    EP_ACT_GELU = 2, /* z Phi(z), Phi the normal distribution function (the erf form) */
+    EP_ACT_SILU = 3  /* z / (1 + exp(-z)) */
 };
 
 typedef struct ep_ctx ep_ctx; /* opaque: device id, device properties, device status word, options */
@@ -344,6 +363,128 @@ int ep_cluster_and_balance(ep_ctx *ctx, const float *emb, int64_t N, int32_t d, 
                            int64_t max_degree, const uint8_t *split, const int64_t *capacities,
                            const uint32_t *rand_words, int32_t max_rounds, int32_t *assign, float *centroids,
                            int32_t *rounds_used, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* --------------------------------------------------------------------------------------------
+ * The operators of a partition head: a small network that learns, on the embeddings, to send every
+ * row to one or a few of E parts under a balance loss, and then answers for new rows one by one.
+ * (The paper clusters and migrates, Algorithm 3; it has no counterpart to these calls.  The ids of
+ * ep_route with k = 1 are an assignment as ep_partition_quality and ep_reorder take it.)
+ *
+ * Shared by all of them: matrices are row-major; rows may be 0 (nothing is read; sums over rows
+ * come out zero); base addresses need only the alignment of their element type, and the kernels use
+ * 16-byte accesses where base and width allow; sums, statistics and softmax are fp32 or wider; every
+ * output is rounded once from fp32, to nearest even.  Results are the same from run to run on
+ * the same device (no floating-point atomics).  Outputs must not overlap inputs unless said.
+ *
+ * ep_rms_norm:  h = x + residual;  out = weight * h / sqrt(mean(h^2) + eps), over each row.
+ *   x        [dev] rows x d, x_type EP_F32 / EP_BF16 / EP_F16;  1 <= d <= 16384
+ *   residual [dev] as x, or NULL (h = x)
+ *   weight   [dev] d values of weight_type (EP_F32 / EP_BF16 / EP_F16), or NULL (all ones)
+ *   out      [dev] rows x d of out_type: x_type, or EP_BF16 / EP_F16 from EP_F32, or EP_E4M3
+ *   scale    [dev] rows fp32 with EP_E4M3, else NULL: out stands for out * scale[row], scale = the row's
+ *            largest magnitude / 448 (0 for a row of zeros, whose out is 0)
+ *   hidden   [dev] out or NULL, rows x d of x_type: h (may be the same buffer as x or residual)
+ *   eps      >= 0, finite.  The norm is taken of the fp32 sum, before hidden is rounded.
+ * A row of zeros comes out as zeros, with eps = 0 too.  A row that holds a NaN comes out as NaN (scale included), one that
+ * holds an infinity as NaN there and zero elsewhere.
+ *
+ * ep_quantize_rows: the 8-bit output on its own: q = x / scale, scale as above (weights and inputs of the
+ * 8-bit form of ep_linear).
+ *
+ * ep_rms_norm_backward: with rho = 1 / sqrt(mean(h^2) + eps), a = weight * dout:
+ *   dx = rho (a - h rho^2 mean(a h)) + dhidden      (the gradient of x and, alike, of residual)
+ *   dweight = sum over rows of dout h rho
+ *   dout     [dev] rows x d of dout_type: h_type, or EP_BF16 / EP_F16 with h of EP_F32
+ *   hidden   [dev] rows x d of h_type: what the forward returned as hidden (x where it had no residual)
+ *   dhidden  [dev] rows x d of h_type or NULL: gradient that reached hidden by other ways
+ *   dx       [dev] out, rows x d of h_type (may be the same buffer as dhidden)
+ *   dweight  [dev] out or NULL, d fp32
+ */
+int ep_rms_norm(ep_ctx *ctx, const void *x, int32_t x_type, const void *residual, const void *weight,
+                int32_t weight_type, int64_t rows, int32_t d, float eps, void *out, int32_t out_type, float *scale,
+                void *hidden, void *cuda_stream);
+int ep_quantize_rows(ep_ctx *ctx, const void *x, int32_t x_type, int64_t rows, int32_t d, void *q, float *scale,
+                     void *cuda_stream);
+size_t ep_rms_norm_backward_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t d);   /* 0 = invalid shape */
+int ep_rms_norm_backward(ep_ctx *ctx, const void *dout, int32_t dout_type, const void *hidden, int32_t h_type,
+                         const void *weight, int32_t weight_type, const void *dhidden, int64_t rows, int32_t d, float eps,
+                         void *dx, float *dweight, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* --------------------------------------------------------------------------------------------
+ * ep_linear -- product with a weight matrix, with bias, activation and residual in its epilogue.
+ *
+ *   z = x W^T + bias;  out = act(z) + residual       (EP_E4M3: z = x_scale[row] w_scale[column] (x W^T) + bias)
+ *
+ *   x        [dev] rows x n_in of in_type, row i at element i * ldx (ldx >= n_in; ldw, ldr alike)
+ *   w        [dev] n_out x n_in of in_type, rows ldw apart
+ *   in_type  EP_F32, EP_BF16, EP_F16, EP_E4M3;  1 <= n_in, n_out <= 65536
+ *   x_scale  [dev] rows fp32, w_scale [dev] n_out fp32: both with EP_E4M3 (see ep_quantize_rows), else NULL
+ *   bias     [dev] n_out of bias_type (EP_F32 / EP_BF16 / EP_F16) or NULL;  act  EP_ACT_*
+ *   residual [dev] rows x n_out of out_type, rows ldr apart, or NULL
+ *   out      [dev] rows x n_out of out_type: in_type or EP_F32; EP_BF16, EP_F16 or EP_F32 from EP_E4M3
+ *   preact   [dev] out or NULL, rows x n_out of out_type: z, which the backward pass wants
+ *   aligned  (of the queries) 1 if every matrix of the call starts on a 16-byte boundary and its row stride is a
+ *            multiple of 16 bytes, else 0: unaligned ones are first copied into the workspace
+ * 16-bit and 8-bit inputs are multiplied as they are and summed in fp32.  EP_F32 inputs are written as the sum of three
+ * bf16 numbers (24 bits in all) and the six products that matter are summed: the result is as near as an fp32 product.
+ * (A row of EP_F32 that holds an infinity or a NaN comes out as NaN.)  An output of EP_F32 is summed in short runs that
+ * are added to nearest, since the tensor core truncates.
+ *
+ * ep_linear_backward:  dz = dout act'(preact);  dx = dz W;  dweight = dz^T x;  dbias = sum over rows of dz
+ *   dout     [dev] rows x n_out of dout_type: in_type or EP_F32, rows n_out apart
+ *   preact   [dev] rows x n_out of in_type, or NULL with EP_ACT_NONE
+ *   dx       [dev] out or NULL, rows x n_in of in_type;  dweight [dev] out or NULL, n_out x n_in of in_type
+ *   dbias    [dev] out or NULL, n_out fp32 (summed from dz before it is rounded);  in_type is not EP_E4M3
+ * dz is rounded to in_type before the products of 16-bit types (their operands are 16 bits).
+ */
+size_t ep_linear_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t n_in, int32_t n_out, int32_t in_type,
+                                 int32_t out_type, int32_t aligned);   /* 0 = invalid shape or types; at least 256 */
+int ep_linear(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int64_t ldw, int32_t in_type, const float *x_scale,
+              const float *w_scale, const void *bias, int32_t bias_type, int32_t act, const void *residual, int64_t ldr,
+              void *out, int32_t out_type, void *preact, int64_t rows, int32_t n_in, int32_t n_out, void *workspace,
+              size_t workspace_bytes, void *cuda_stream);
+size_t ep_linear_backward_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t n_in, int32_t n_out, int32_t in_type,
+                                          int32_t aligned);
+int ep_linear_backward(ep_ctx *ctx, const void *dout, int32_t dout_type, const void *preact, int32_t act, const void *x,
+                       int64_t ldx, const void *w, int64_t ldw, int32_t in_type, int64_t rows, int32_t n_in, int32_t n_out,
+                       void *dx, void *dweight, float *dbias, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* --------------------------------------------------------------------------------------------
+ * ep_route -- routing of rows to parts, with per-part counts and balance loss.
+ *
+ *   p = softmax(logits) over each row;  ids = the k parts of the row's largest logits in descending
+ *   order (of equal logits the lower part first);  weights = p[ids], divided by their sum if
+ *   renormalize;  counts[e] = slots that chose part e;  routed = R rows that took part;
+ *   prob[e] = mean of p[., e] over those;  loss = E sum_e counts[e] / (k R) prob[e]
+ * (the balance loss: 1 when rows and probabilities are spread evenly, up to E when all go to one part).
+ *
+ *   logits  [dev] rows x parts of `type` (EP_F32 / EP_BF16 / EP_F16);  1 <= parts <= 4096
+ *   k       1 <= k <= min(parts, 32)
+ *   valid   [dev] rows bytes or NULL: 0 = the row takes no part (it is not read)
+ *   ids     [dev] out, rows x k int32;  weights [dev] out, rows x k fp32
+ *   counts  [dev] out, parts int64;  prob [dev] out, parts fp32;  loss [dev] out, 1 fp32
+ *   routed  [dev] out, 1 int64
+ * A logit of -infinity is never chosen.  A row that is not valid, or has no logit above -infinity, takes no part:
+ * ids -1, weights 0.  A row with fewer than k logits above -infinity has ids -1 and weights 0 in the slots left over.
+ * With R = 0, prob and loss are 0.  A NaN or +infinity in a row that takes part makes its weights, prob and loss NaN;
+ * a NaN is never chosen.
+ *
+ * ep_route_backward: the gradient of logits, given those of weights and loss (counts are constants):
+ *   dp_e = dloss E counts[e] / (k R) / R  + (e = ids[i]:  dweights[i], or with renormalize
+ *          (dweights[i] - sum_j dweights[j] weights[j]) / sum_j p[ids[j]])
+ *   dlogits = p (dp - sum_e p_e dp_e);  0 in rows that take no part
+ *   logits, valid, k, renormalize, ids, counts, routed: as the forward took and returned them
+ *   dweights [dev] rows x k fp32 or NULL (zero);  dloss [dev] 1 fp32 or NULL (zero)
+ *   dlogits  [dev] out, rows x parts of `type`
+ * An id outside [-1, parts) raises EP_ERR_BAD_INDEX in the device status word and is skipped.
+ */
+size_t ep_route_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t parts);   /* 0 = invalid shape */
+int ep_route(ep_ctx *ctx, const void *logits, int32_t type, int64_t rows, int32_t parts, int32_t k, const uint8_t *valid,
+             int32_t renormalize, int32_t *ids, float *weights, int64_t *counts, float *prob, float *loss, int64_t *routed,
+             void *workspace, size_t workspace_bytes, void *cuda_stream);
+int ep_route_backward(ep_ctx *ctx, const void *logits, int32_t type, int64_t rows, int32_t parts, int32_t k,
+                      const uint8_t *valid, int32_t renormalize, const int32_t *ids, const int64_t *counts,
+                      const int64_t *routed, const float *dweights, const float *dloss, void *dlogits, void *cuda_stream);
 
 /* --------------------------------------------------------------------------------------------
  * Host-buffer variants.  Same operations and the same kernels; inputs and outputs are [host]

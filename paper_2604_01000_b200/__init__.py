@@ -15,6 +15,14 @@ from .binding import (  # noqa: F401
     ep_reorder_static,
     ep_graph_bandwidth,
     ep_kmeans_sampled,
+    ep_rms_norm,
+    ep_rms_norm_backward,
+    ep_quantize_rows,
+    ep_linear,
+    ep_linear_backward,
+    ep_route,
+    ep_route_backward,
+    RouteResult,
     library_path,
     load_library,
     EXPORTED_SYMBOLS,

@@ -23,6 +23,9 @@ EXPORTED_SYMBOLS = (
     "ep_balance_workspace_bytes", "ep_migrate", "ep_balance",
     "ep_cluster_and_balance_workspace_bytes", "ep_cluster_and_balance", "ep_selftest_wait_timeout", "ep_probe_gather",
     "ep_partition_and_reorder_host_arena_bytes", "ep_partition_and_reorder_host",
+    "ep_rms_norm", "ep_quantize_rows", "ep_rms_norm_backward_workspace_bytes", "ep_rms_norm_backward",
+    "ep_linear_workspace_bytes", "ep_linear", "ep_linear_backward_workspace_bytes", "ep_linear_backward",
+    "ep_route_workspace_bytes", "ep_route", "ep_route_backward",
 )
 
 EP_OK = 0
@@ -32,10 +35,14 @@ EP_OPT_TIMER_GROUP = 3
 EP_OPT_KMEANS_CAND_MB = 4
 EP_OPT_QUALITY_SLICE_KB = 5
 EP_OPT_KMEANS_ITERATIONS_PER_LAUNCH = 6
-TIMER_COUNT = 9
+TIMER_COUNT = 12
 TIMERS = {"kmeans_assign": 0, "kmeans_update": 1, "edge_cut": 2, "quality_prep": 3, "reorder": 4,
-          "kmeans_resolve": 5, "graph_bandwidth": 6, "relabel": 7, "balance": 8}
+          "kmeans_resolve": 5, "graph_bandwidth": 6, "relabel": 7, "balance": 8, "norm": 9, "linear": 10, "route": 11}
 KMEANS_PATHS = {"auto": 0, "simt": 1, "tensor": 2}
+# element types and activations of the partition head's operators
+TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3}
+FLOATS = (torch.float32, torch.bfloat16, torch.float16)
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 
 class EmbedPartError(RuntimeError):
@@ -154,6 +161,30 @@ def load_library() -> ctypes.CDLL:
             lib.ep_graph_bandwidth_host_arena_bytes.restype = sz
             lib.ep_graph_bandwidth_host.argtypes = [vp, vp, i32, vp, i64, vp, i64, vp, vp, vp, sz, vp]
             lib.ep_graph_bandwidth_host.restype = ctypes.c_int
+            f32 = ctypes.c_float
+            lib.ep_rms_norm.argtypes = [vp, vp, i32, vp, vp, i32, i64, i32, f32, vp, i32, vp, vp, vp]
+            lib.ep_rms_norm.restype = ctypes.c_int
+            lib.ep_quantize_rows.argtypes = [vp, vp, i32, i64, i32, vp, vp, vp]
+            lib.ep_quantize_rows.restype = ctypes.c_int
+            lib.ep_rms_norm_backward_workspace_bytes.argtypes = [vp, i64, i32]
+            lib.ep_rms_norm_backward_workspace_bytes.restype = sz
+            lib.ep_rms_norm_backward.argtypes = [vp, vp, i32, vp, i32, vp, i32, vp, i64, i32, f32, vp, vp, vp, sz, vp]
+            lib.ep_rms_norm_backward.restype = ctypes.c_int
+            lib.ep_linear_workspace_bytes.argtypes = [vp, i64, i32, i32, i32, i32, i32]
+            lib.ep_linear_workspace_bytes.restype = sz
+            lib.ep_linear.argtypes = [vp, vp, i64, vp, i64, i32, vp, vp, vp, i32, i32, vp, i64, vp, i32, vp, i64, i32, i32, vp,
+                                      sz, vp]
+            lib.ep_linear.restype = ctypes.c_int
+            lib.ep_linear_backward_workspace_bytes.argtypes = [vp, i64, i32, i32, i32, i32]
+            lib.ep_linear_backward_workspace_bytes.restype = sz
+            lib.ep_linear_backward.argtypes = [vp, vp, i32, vp, i32, vp, i64, vp, i64, i32, i64, i32, i32, vp, vp, vp, vp, sz, vp]
+            lib.ep_linear_backward.restype = ctypes.c_int
+            lib.ep_route_workspace_bytes.argtypes = [vp, i64, i32]
+            lib.ep_route_workspace_bytes.restype = sz
+            lib.ep_route.argtypes = [vp, vp, i32, i64, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+            lib.ep_route.restype = ctypes.c_int
+            lib.ep_route_backward.argtypes = [vp, vp, i32, i64, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp]
+            lib.ep_route_backward.restype = ctypes.c_int
             _lib = lib
     return _lib
 
@@ -170,6 +201,45 @@ def _check_cuda(t: torch.Tensor, dtype, name: str, device: torch.device) -> torc
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t
+
+
+def _check_matrix(t: torch.Tensor, dtypes, name: str, device: torch.device, shape=None, strided: bool = False) -> torch.Tensor:
+    """A 2-D CUDA tensor of one of `dtypes`, contiguous or (strided) with contiguous rows at any distance."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} must be a CUDA tensor on {device}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} must have dtype {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name} must have shape {tuple(shape) if shape is not None else '(rows, columns)'}, not {tuple(t.shape)}")
+    if strided:
+        if t.numel() and (t.stride(1) != 1 and t.shape[1] > 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+            raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    elif not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def _check_vector(t: Optional[torch.Tensor], dtypes, name: str, device: torch.device, n: int) -> Optional[torch.Tensor]:
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} must be a CUDA tensor on {device}")
+    if t.dtype not in dtypes or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be {n} contiguous values of {' or '.join(str(d) for d in dtypes)}")
+    return t
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _type_of(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else TYPES[t.dtype]
+
+
+def _aligned(*ts: torch.Tensor) -> bool:
+    """Whether every matrix starts on a 16-byte boundary with rows a multiple of 16 bytes apart."""
+    return all(t.data_ptr() % 16 == 0 and _row_stride(t) * t.element_size() % 16 == 0 for t in ts)
 
 
 class Context:
@@ -657,6 +727,176 @@ class Context:
             self._raise(rc)
         return out
 
+    # -- the partition head's operators --------------------------------------------------------------
+    def _scratch(self, nbytes: int, what: str) -> torch.Tensor:
+        """A workspace of this call's own, ordered by the current stream (calls on several streams may overlap)."""
+        if nbytes == 0:
+            raise EmbedPartError(1, f"shape or type out of range: {what}")
+        return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+
+    def _done(self, rc: int):
+        if rc != EP_OK:
+            self._raise(rc)
+
+    def rms_norm(self, x, weight=None, residual=None, eps: float = 1e-6, out_dtype=None):
+        """weight * h / sqrt(mean(h^2) + eps) with h = x + residual; see ep_rms_norm."""
+        x = _check_matrix(x, FLOATS, "x", self.device)
+        rows, d = x.shape
+        weight = _check_vector(weight, FLOATS, "weight", self.device, d)
+        if residual is not None:
+            residual = _check_matrix(residual, (x.dtype,), "residual", self.device, x.shape)
+        out_dtype = x.dtype if out_dtype is None else out_dtype
+        if out_dtype not in (x.dtype, torch.float8_e4m3fn) and not (x.dtype == torch.float32 and out_dtype in FLOATS):
+            raise ValueError(f"no norm from {x.dtype} to {out_dtype}")
+        out = torch.empty(rows, d, dtype=out_dtype, device=self.device)
+        scale = torch.empty(rows, dtype=torch.float32, device=self.device) if out_dtype == torch.float8_e4m3fn else None
+        hidden = torch.empty_like(x) if residual is not None else None
+        with torch.cuda.device(self.device):
+            self._done(self._lib.ep_rms_norm(self._h, _dev_ptr(x), TYPES[x.dtype], _dev_ptr(residual), _dev_ptr(weight),
+                                             _type_of(weight), rows, d, eps, _dev_ptr(out), TYPES[out_dtype], _dev_ptr(scale),
+                                             _dev_ptr(hidden), self._stream()))
+        return NormResult(out, scale, x if hidden is None else hidden)
+
+    def quantize_rows(self, x):
+        """Rows in 8 bits with a scale each: x ~ q * scale[:, None]; see ep_quantize_rows."""
+        x = _check_matrix(x, FLOATS, "x", self.device)
+        rows, d = x.shape
+        q = torch.empty(rows, d, dtype=torch.float8_e4m3fn, device=self.device)
+        scale = torch.empty(rows, dtype=torch.float32, device=self.device)
+        with torch.cuda.device(self.device):
+            self._done(self._lib.ep_quantize_rows(self._h, _dev_ptr(x), TYPES[x.dtype], rows, d, _dev_ptr(q), _dev_ptr(scale),
+                                                  self._stream()))
+        return QuantizedRows(q, scale)
+
+    def rms_norm_backward(self, dout, hidden, weight=None, eps: float = 1e-6, dhidden=None, need_dweight: bool = True):
+        """Gradients of x (and, alike, residual) and weight; hidden is the forward's; see ep_rms_norm_backward."""
+        hidden = _check_matrix(hidden, FLOATS, "hidden", self.device)
+        rows, d = hidden.shape
+        dout = _check_matrix(dout, FLOATS if hidden.dtype == torch.float32 else (hidden.dtype,), "dout", self.device, hidden.shape)
+        weight = _check_vector(weight, FLOATS, "weight", self.device, d)
+        if dhidden is not None:
+            dhidden = _check_matrix(dhidden, (hidden.dtype,), "dhidden", self.device, hidden.shape)
+        ws = self._scratch(self._lib.ep_rms_norm_backward_workspace_bytes(self._h, rows, d), f"rows={rows} d={d}")
+        dx = torch.empty_like(hidden)
+        dweight = torch.empty(d, dtype=torch.float32, device=self.device) if need_dweight else None
+        with torch.cuda.device(self.device):
+            self._done(self._lib.ep_rms_norm_backward(
+                self._h, _dev_ptr(dout), TYPES[dout.dtype], _dev_ptr(hidden), TYPES[hidden.dtype], _dev_ptr(weight),
+                _type_of(weight), _dev_ptr(dhidden), rows, d, eps, _dev_ptr(dx), _dev_ptr(dweight), _dev_ptr(ws), ws.numel(),
+                self._stream()))
+        return NormGradients(dx, dweight)
+
+    def linear(self, x, weight, bias=None, activation: str = "none", residual=None, x_scale=None, weight_scale=None,
+               out_dtype=None, preact: bool = False):
+        """act(x weight^T + bias) + residual; see ep_linear.  x, weight and residual may have strided rows."""
+        x = _check_matrix(x, tuple(TYPES), "x", self.device, strided=True)
+        rows, n_in = x.shape
+        weight = _check_matrix(weight, (x.dtype,), "weight", self.device, strided=True)
+        n_out = weight.shape[0]
+        if weight.shape[1] != n_in:
+            raise ValueError(f"weight must be n_out x {n_in}, not {tuple(weight.shape)}")
+        if activation not in ACTIVATIONS:
+            raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")
+        eight = x.dtype == torch.float8_e4m3fn
+        out_dtype = (torch.bfloat16 if eight else x.dtype) if out_dtype is None else out_dtype
+        if out_dtype not in FLOATS or not (eight or out_dtype in (x.dtype, torch.float32)):
+            raise ValueError(f"no product of {x.dtype} with output of {out_dtype}")
+        if eight != (x_scale is not None) or eight != (weight_scale is not None):
+            raise ValueError("x_scale and weight_scale go with 8-bit inputs, and with no others")
+        x_scale = _check_vector(x_scale, (torch.float32,), "x_scale", self.device, rows)
+        weight_scale = _check_vector(weight_scale, (torch.float32,), "weight_scale", self.device, n_out)
+        bias = _check_vector(bias, FLOATS, "bias", self.device, n_out)
+        if residual is not None:
+            residual = _check_matrix(residual, (out_dtype,), "residual", self.device, (rows, n_out), strided=True)
+        ws = self._scratch(self._lib.ep_linear_workspace_bytes(self._h, rows, n_in, n_out, TYPES[x.dtype], TYPES[out_dtype],
+                                                               int(_aligned(x, weight))),
+                           f"rows={rows} n_in={n_in} n_out={n_out}")
+        out = torch.empty(rows, n_out, dtype=out_dtype, device=self.device)
+        z = torch.empty_like(out) if preact else None
+        with torch.cuda.device(self.device):
+            self._done(self._lib.ep_linear(
+                self._h, _dev_ptr(x), _row_stride(x), _dev_ptr(weight), _row_stride(weight), TYPES[x.dtype], _dev_ptr(x_scale),
+                _dev_ptr(weight_scale), _dev_ptr(bias), _type_of(bias), ACTIVATIONS[activation], _dev_ptr(residual),
+                0 if residual is None else _row_stride(residual), _dev_ptr(out), TYPES[out_dtype], _dev_ptr(z), rows, n_in, n_out,
+                _dev_ptr(ws), ws.numel(), self._stream()))
+        return LinearResult(out, z)
+
+    def linear_backward(self, dout, x, weight, preact=None, activation: str = "none", need_dx: bool = True,
+                        need_dweight: bool = True, need_dbias: bool = True):
+        """Gradients of x, weight and bias (the residual's is dout itself); see ep_linear_backward."""
+        x = _check_matrix(x, FLOATS, "x", self.device, strided=True)
+        rows, n_in = x.shape
+        weight = _check_matrix(weight, (x.dtype,), "weight", self.device, strided=True)
+        n_out = weight.shape[0]
+        if weight.shape[1] != n_in:
+            raise ValueError(f"weight must be n_out x {n_in}, not {tuple(weight.shape)}")
+        if activation not in ACTIVATIONS:
+            raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")
+        dout = _check_matrix(dout, (x.dtype, torch.float32), "dout", self.device, (rows, n_out))
+        if activation != "none":
+            if preact is None:
+                raise ValueError("the gradient through an activation needs preact")
+            preact = _check_matrix(preact, (x.dtype,), "preact", self.device, (rows, n_out))
+        else:
+            preact = None
+        ws = self._scratch(self._lib.ep_linear_backward_workspace_bytes(self._h, rows, n_in, n_out, TYPES[x.dtype],
+                                                                        int(_aligned(x, weight))),
+                           f"rows={rows} n_in={n_in} n_out={n_out}")
+        dx = torch.empty(rows, n_in, dtype=x.dtype, device=self.device) if need_dx else None
+        dweight = torch.empty(n_out, n_in, dtype=x.dtype, device=self.device) if need_dweight else None
+        dbias = torch.empty(n_out, dtype=torch.float32, device=self.device) if need_dbias else None
+        with torch.cuda.device(self.device):
+            self._done(self._lib.ep_linear_backward(
+                self._h, _dev_ptr(dout), TYPES[dout.dtype], _dev_ptr(preact), ACTIVATIONS[activation], _dev_ptr(x),
+                _row_stride(x), _dev_ptr(weight), _row_stride(weight), TYPES[x.dtype], rows, n_in, n_out, _dev_ptr(dx),
+                _dev_ptr(dweight), _dev_ptr(dbias), _dev_ptr(ws), ws.numel(), self._stream()))
+        return LinearGradients(dx, dweight, dbias)
+
+    def route(self, logits, k: int = 1, valid=None, renormalize: bool = False):
+        """Rows to their k best parts, with weights, per-part counts and the balance loss; see ep_route."""
+        logits = _check_matrix(logits, FLOATS, "logits", self.device)
+        rows, parts = logits.shape
+        if not 1 <= k <= min(parts, 32):
+            raise ValueError(f"k must be in 1..{min(parts, 32)}, not {k}")
+        valid = _check_vector(valid, (torch.uint8, torch.bool), "valid", self.device, rows)
+        ws = self._scratch(self._lib.ep_route_workspace_bytes(self._h, rows, parts), f"rows={rows} parts={parts}")
+        ids = torch.empty(rows, k, dtype=torch.int32, device=self.device)
+        weights = torch.empty(rows, k, dtype=torch.float32, device=self.device)
+        counts = torch.empty(parts, dtype=torch.int64, device=self.device)
+        prob = torch.empty(parts, dtype=torch.float32, device=self.device)
+        loss = torch.empty(1, dtype=torch.float32, device=self.device)
+        routed = torch.empty(1, dtype=torch.int64, device=self.device)
+        with torch.cuda.device(self.device):
+            self._done(self._lib.ep_route(
+                self._h, _dev_ptr(logits), TYPES[logits.dtype], rows, parts, k, _dev_ptr(valid), int(renormalize), _dev_ptr(ids),
+                _dev_ptr(weights), _dev_ptr(counts), _dev_ptr(prob), _dev_ptr(loss), _dev_ptr(routed), _dev_ptr(ws), ws.numel(),
+                self._stream()))
+        return RouteResult(ids, weights, counts, prob, loss, routed)
+
+    def route_backward(self, logits, result: "RouteResult", dweights=None, dloss=None, valid=None, renormalize: bool = False):
+        """Gradient of logits from those of the weights and of the loss; logits, valid and renormalize as the forward took
+        them, result what it returned; see ep_route_backward."""
+        logits = _check_matrix(logits, FLOATS, "logits", self.device)
+        rows, parts = logits.shape
+        ids = _check_matrix(result.ids, (torch.int32,), "result.ids", self.device)
+        k = ids.shape[1]
+        if ids.shape[0] != rows or not 1 <= k <= min(parts, 32):
+            raise ValueError(f"result.ids must be {rows} x k with k in 1..{min(parts, 32)}, not {tuple(ids.shape)}")
+        counts = _check_vector(result.counts, (torch.int64,), "result.counts", self.device, parts)
+        routed = _check_vector(result.routed, (torch.int64,), "result.routed", self.device, 1)
+        if counts is None or routed is None:
+            raise ValueError("result must hold the forward's counts and routed")
+        if dweights is not None:
+            dweights = _check_matrix(dweights, (torch.float32,), "dweights", self.device, (rows, k))
+        dloss = _check_vector(dloss, (torch.float32,), "dloss", self.device, 1)
+        valid = _check_vector(valid, (torch.uint8, torch.bool), "valid", self.device, rows)
+        dlogits = torch.empty_like(logits)
+        with torch.cuda.device(self.device):
+            self._done(self._lib.ep_route_backward(
+                self._h, _dev_ptr(logits), TYPES[logits.dtype], rows, parts, k, _dev_ptr(valid), int(renormalize), _dev_ptr(ids),
+                _dev_ptr(counts), _dev_ptr(routed), _dev_ptr(dweights), _dev_ptr(dloss), _dev_ptr(dlogits), self._stream()))
+        return dlogits
+
 
 class KMeansResult(NamedTuple):
     assign: torch.Tensor                 # int32 [N]
@@ -678,6 +918,42 @@ class ReorderResult(NamedTuple):
 class BandwidthResult(NamedTuple):
     bandwidth_sum: torch.Tensor               # int64 [1]: sum of the vertex bandwidths (divide by N for the average)
     vertex_bandwidth: Optional[torch.Tensor]  # int32 [N]
+
+
+class NormResult(NamedTuple):
+    out: torch.Tensor                    # [rows, d]
+    scale: Optional[torch.Tensor]        # float32 [rows] with an 8-bit out: it stands for out * scale[:, None]
+    hidden: torch.Tensor                 # x + residual (x itself without one): what the backward pass takes
+
+
+class QuantizedRows(NamedTuple):
+    q: torch.Tensor                      # float8_e4m3fn [rows, d]
+    scale: torch.Tensor                  # float32 [rows]
+
+
+class NormGradients(NamedTuple):
+    dx: torch.Tensor                     # [rows, d]: the gradient of x and of residual
+    dweight: Optional[torch.Tensor]      # float32 [d]
+
+
+class LinearResult(NamedTuple):
+    out: torch.Tensor                    # [rows, n_out]
+    preact: Optional[torch.Tensor]       # [rows, n_out]: before the activation, what the backward pass takes
+
+
+class LinearGradients(NamedTuple):
+    dx: Optional[torch.Tensor]           # [rows, n_in]
+    dweight: Optional[torch.Tensor]      # [n_out, n_in]
+    dbias: Optional[torch.Tensor]        # float32 [n_out]
+
+
+class RouteResult(NamedTuple):
+    ids: torch.Tensor                    # int32 [rows, k], -1 = no part
+    weights: torch.Tensor                # float32 [rows, k]
+    counts: torch.Tensor                 # int64 [parts]
+    prob: torch.Tensor                   # float32 [parts]: mean probability over the routed rows
+    loss: torch.Tensor                   # float32 [1]: the balance loss
+    routed: torch.Tensor                 # int64 [1]: rows that took part
 
 
 _default: dict[int, Context] = {}
@@ -713,6 +989,43 @@ def ep_kmeans_sampled(emb, K, iters, sample_rows, init_centroids) -> KMeansResul
 def ep_graph_bandwidth(rowptr, colidx, pi, per_vertex=True) -> BandwidthResult:
     """Vertex bandwidths of the numbering pi over the CSR graph and their sum."""
     return default_context(pi.device.index).graph_bandwidth(rowptr, colidx, pi, per_vertex)
+
+
+def ep_rms_norm(x, weight=None, residual=None, eps=1e-6, out_dtype=None) -> NormResult:
+    """Root-mean-square norm of the rows of x + residual, in x's type, another float type or 8 bits with scales."""
+    return default_context(x.device.index).rms_norm(x, weight, residual, eps, out_dtype)
+
+
+def ep_rms_norm_backward(dout, hidden, weight=None, eps=1e-6, dhidden=None, need_dweight=True) -> NormGradients:
+    """Gradients of ep_rms_norm."""
+    return default_context(hidden.device.index).rms_norm_backward(dout, hidden, weight, eps, dhidden, need_dweight)
+
+
+def ep_quantize_rows(x) -> QuantizedRows:
+    """Rows in 8 bits with a scale each, as ep_linear takes them."""
+    return default_context(x.device.index).quantize_rows(x)
+
+
+def ep_linear(x, weight, bias=None, activation="none", residual=None, x_scale=None, weight_scale=None, out_dtype=None,
+              preact=False) -> LinearResult:
+    """act(x weight^T + bias) + residual."""
+    return default_context(x.device.index).linear(x, weight, bias, activation, residual, x_scale, weight_scale, out_dtype, preact)
+
+
+def ep_linear_backward(dout, x, weight, preact=None, activation="none", need_dx=True, need_dweight=True,
+                       need_dbias=True) -> LinearGradients:
+    """Gradients of ep_linear."""
+    return default_context(x.device.index).linear_backward(dout, x, weight, preact, activation, need_dx, need_dweight, need_dbias)
+
+
+def ep_route(logits, k=1, valid=None, renormalize=False) -> RouteResult:
+    """Rows to their k best parts, with weights, per-part counts and the balance loss."""
+    return default_context(logits.device.index).route(logits, k, valid, renormalize)
+
+
+def ep_route_backward(logits, result, dweights=None, dloss=None, valid=None, renormalize=False) -> torch.Tensor:
+    """Gradient of ep_route's logits."""
+    return default_context(logits.device.index).route_backward(logits, result, dweights, dloss, valid, renormalize)
 
 
 REORDER_STATIC_MAX_N = 1 << 22

@@ -168,6 +168,12 @@ int migrate_run(ep_ctx *ctx, const void *rowptr, bool rowptr64, int64_t N, int K
                 cudaStream_t stream);
 const long long *balance_state_ptr(int64_t N, int K, int64_t max_degree, void *workspace);
 
+// ---- the partition head's operators (norm.cu, route.cu, linear.cu) ---------------------------------
+inline int type_size(int type) { return type == EP_F32 ? 4 : type == EP_BF16 || type == EP_F16 ? 2 : type == EP_E4M3 ? 1 : 0; }
+inline bool float_type(int type) { return type == EP_F32 || type == EP_BF16 || type == EP_F16; }
+// out[c] = sum of parts[r][c] over r = 0..n-1, in ascending order of fixed groups of r (fp64 inside).
+int sum_partials(ep_ctx *ctx, const float *parts, int n, int cols, float *out, cudaStream_t stream);
+
 }  // namespace ep
 
 // ---- device helpers -------------------------------------------------------------------------------

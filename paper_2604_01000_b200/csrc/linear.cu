@@ -1,0 +1,1058 @@
+// Product with a weight matrix, with bias, activation and residual in its epilogue, and its backward pass.
+//
+// One tile kernel (linear_tiles) serves the forward product and both gradients: D[M, N] = sum_k A[m, k] B[n, k] with
+// either operand stored along k ("K-major") or along its own rows ("MN-major", 16-bit types), so that no operand is
+// ever transposed in memory:
+//     z  = x W^T     A = x  (K-major)     B = W (K-major)
+//     dx = dz W      A = dz (K-major)     B = W (MN-major)
+//     dW = dz^T x    A = dz (MN-major)    B = x (MN-major)
+// Beside it: a dot-product kernel for the fewest rows (serving), the kernel that makes dz and sums dbias, one that
+// copies unaligned operands or splits fp32 ones into three bf16 numbers, and one that joins the shares of a sum over k
+// that was split between blocks.
+#include "ep_common.cuh"
+#include "rows.cuh"
+#include "tc_device.cuh"
+
+#include <algorithm>
+#include <initializer_list>
+#include <mutex>
+
+using namespace eprow;
+using namespace eptc;
+
+namespace {
+
+// ---------------------------------------------------------------------------------------------- epilogue
+struct Epilogue {
+    const float *x_scale, *w_scale;   // of 8-bit inputs
+    const void *bias;
+    int bias_type, act;
+    const void *residual;
+    int64_t ldr;
+    void *out, *preact;
+    int out_type;
+    int64_t M;
+    int N;
+    bool vec;                         // out, preact, residual: 16-byte rows of whole 8-column chunks
+    float *share;                     // where a block's share of a split sum goes: [split][M][ld_share] fp32
+    int ld_share;
+};
+
+__device__ __forceinline__ float normal_cdf(float z) { return 0.5f + 0.5f * erff(z * 0.70710678f); }
+
+__device__ __forceinline__ float activate(float z, int act) {
+    if (act == EP_ACT_RELU) return z > 0.f || z != z ? z : 0.f;
+    if (act == EP_ACT_GELU) return z * normal_cdf(z);
+    if (act == EP_ACT_SILU) return z / (1.f + __expf(-z));
+    return z;
+}
+__device__ __forceinline__ float slope_of(float z, int act) {
+    if (act == EP_ACT_RELU) return z > 0.f ? 1.f : 0.f;
+    if (act == EP_ACT_GELU) return normal_cdf(z) + z * 0.39894228f * __expf(-0.5f * z * z);
+    if (act == EP_ACT_SILU) {
+        const float s = 1.f / (1.f + __expf(-z));
+        return s * (1.f + z * (1.f - s));
+    }
+    return 1.f;
+}
+
+// What a thread needs of n columns, the same for every row that it finishes.
+template <int n>
+struct Columns {
+    float bias[n], scale[n];
+    __device__ __forceinline__ void load(const Epilogue &e, int col) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            bias[i] = e.bias && col + i < e.N ? load_param(e.bias, e.bias_type, col + i) : 0.f;
+            scale[i] = e.w_scale && col + i < e.N ? __ldg(e.w_scale + col + i) : 1.f;
+        }
+    }
+};
+
+// n finished sums of one row, from column col on: scale, bias, (store z), activation, residual, store.
+template <typename O, int n>
+__device__ __forceinline__ void finish_as(const Epilogue &e, int64_t row, int col, const Columns<n> &c, float (&v)[n]) {
+    const float xs = e.x_scale ? __ldg(e.x_scale + row) : 1.f;
+#pragma unroll
+    for (int i = 0; i < n; ++i) v[i] = (e.x_scale ? v[i] * xs * c.scale[i] : v[i]) + c.bias[i];
+    const bool vec = n > 1 && e.vec;
+    if (e.preact) store_chunk(static_cast<O *>(e.preact) + row * e.N, col, e.N, vec, v);
+    if (e.act != EP_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = activate(v[i], e.act);
+    }
+    if (e.residual) {
+        float r[n];
+        load_chunk(static_cast<const O *>(e.residual) + row * e.ldr, col, e.N, vec, 0.f, r);
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] += r[i];
+    }
+    store_chunk(static_cast<O *>(e.out) + row * e.N, col, e.N, vec, v);
+}
+template <int n>
+__device__ __forceinline__ void finish(const Epilogue &e, int64_t row, int col, const Columns<n> &c, float (&v)[n]) {
+    if (e.out_type == EP_BF16)
+        finish_as<__nv_bfloat16>(e, row, col, c, v);
+    else if (e.out_type == EP_F16)
+        finish_as<__half>(e, row, col, c, v);
+    else
+        finish_as<float>(e, row, col, c, v);
+}
+
+// ---------------------------------------------------------------------------------------------- the tile kernel
+//
+// 128 x BN outputs per tile, one block per SM that goes from tile to tile: warp 8 brings k-blocks (128 bytes along k)
+// by TMA into a ring, warp 9 issues the MMAs, warps 0-7 finish a tile while the next one is being summed (two
+// accumulators in TMEM).
+//
+// PARTS == 3: fp32 operands as three bf16 numbers each, x = x1 + x2 + x3 (|x2| <= 2^-8 |x|, |x3| <= 2^-16 |x|).  Of
+// the nine products the six down to 2^-16 are summed; the other three are below 2^-24.  x1 w1 has an accumulator of
+// its own, the five small products share a second one.
+//
+// RUNS: the tensor core's fp32 sums are truncated, which costs up to an ulp of the running sum a step, always
+// downwards (measured: 4e-6 of the result after 256 steps, 2e-7 after 16).  Where the output is fp32, sums therefore
+// run over 4 k-blocks only (16 steps), and the epilogue's threads add the runs to nearest in their registers.
+constexpr int BM = 128;
+constexpr int EPI_WARPS = 8;
+constexpr int TMA_WARP = 8, MMA_WARP = 9;
+constexpr int GEMM_THREADS = 320;
+constexpr int A_BYTES = BM * 128;
+constexpr int RING_BYTES = 196608;
+constexpr int STAGING_BYTES = EPI_WARPS * 4096;   // per warp 32 rows x 32 columns of fp32
+constexpr int RUN_KB = 4;
+constexpr int MAX_STAGES = 8;
+constexpr int TMEM_COLS = 512;
+
+struct GemmShared {
+    uint64_t full[MAX_STAGES], empty[MAX_STAGES], t_full[2], t_empty[2], drain;
+    uint32_t tmem_base;
+    int abort;
+};
+constexpr size_t GEMM_SMEM = 1024 + RING_BYTES + STAGING_BYTES + sizeof(GemmShared);
+
+struct GemmShape {
+    int64_t M;
+    int N;
+    int tiles_n;
+    int64_t tiles;        // tiles of the output
+    int64_t items;        // tiles x splits
+    int kb, kb_per_split; // k-blocks of the whole sum, and of one split
+    bool a_mn, b_mn;      // operand stored along its rows
+    uint32_t idesc;
+};
+
+// The four K-steps of one k-block.
+template <bool F8>
+__device__ __forceinline__ void umma_kblock_elected(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint64_t astep,
+                                                    uint64_t bstep, uint32_t idesc, uint32_t accumulate_first) {
+    const uint64_t a1 = adesc + astep, a2 = a1 + astep, a3 = a2 + astep;
+    const uint64_t b1 = bdesc + bstep, b2 = b1 + bstep, b3 = b2 + bstep;
+    if constexpr (F8)
+        asm volatile(
+            "{\n.reg .pred pe, pa, pt;\n"
+            "elect.sync _|pe, 0xffffffff;\n"
+            "setp.ne.b32 pa, %10, 0;\nsetp.eq.b32 pt, 0, 0;\n"
+            "@pe tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %5, %9, pa;\n"
+            "@pe tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %2, %6, %9, pt;\n"
+            "@pe tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %3, %7, %9, pt;\n"
+            "@pe tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %4, %8, %9, pt;\n}"
+            ::"r"(d_tmem), "l"(adesc), "l"(a1), "l"(a2), "l"(a3), "l"(bdesc), "l"(b1), "l"(b2), "l"(b3), "r"(idesc),
+              "r"(accumulate_first)
+            : "memory");
+    else
+        asm volatile(
+            "{\n.reg .pred pe, pa, pt;\n"
+            "elect.sync _|pe, 0xffffffff;\n"
+            "setp.ne.b32 pa, %10, 0;\nsetp.eq.b32 pt, 0, 0;\n"
+            "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %5, %9, pa;\n"
+            "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], %2, %6, %9, pt;\n"
+            "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], %3, %7, %9, pt;\n"
+            "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], %4, %8, %9, pt;\n}"
+            ::"r"(d_tmem), "l"(adesc), "l"(a1), "l"(a2), "l"(a3), "l"(bdesc), "l"(b1), "l"(b2), "l"(b3), "r"(idesc),
+              "r"(accumulate_first)
+            : "memory");
+}
+
+// Shared-memory descriptor of an operand tile, 128-byte swizzle.  K-major: rows of 128 bytes along k, groups of 8 rows
+// 1024 bytes apart; a K-step is 32 bytes further along the row.  MN-major: boxes of 64 columns x 64 k, 8192 bytes
+// apart; inside a box rows of 128 bytes hold the 64 columns of one k, groups of 8 k are 1024 bytes apart, and a K-step
+// of 16 k is two groups on.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t smem, bool mn) {
+    const uint64_t lead = mn ? 8192 >> 4 : 1;
+    return (uint64_t)((smem & 0x3FFFFu) >> 4) | (lead << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+struct Item {
+    int64_t m0;
+    int n0, split, kb0, kbn;
+};
+// Tiles of one row of tiles come one after another (they share A, and B stays in the L2); splits outermost.
+__device__ __forceinline__ Item item_at(const GemmShape &g, int bn, int64_t i) {
+    Item t;
+    t.split = (int)(i / g.tiles);
+    const int64_t tile = i - (int64_t)t.split * g.tiles;
+    const int64_t tm = tile / g.tiles_n;
+    t.m0 = tm * BM;
+    t.n0 = (int)(tile - tm * g.tiles_n) * bn;
+    t.kb0 = t.split * g.kb_per_split;
+    t.kbn = min(g.kb_per_split, g.kb - t.kb0);
+    return t;
+}
+
+template <int BN, bool F8, int PARTS, bool RUNS>
+__global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_constant__ CUtensorMap map_a,
+                                                                const __grid_constant__ CUtensorMap map_b,
+                                                                const GemmShape g, const Epilogue e, int *status) {
+    constexpr int B_BYTES = BN * 128;
+    constexpr int STAGE_BYTES = PARTS * (A_BYTES + B_BYTES);
+    constexpr int STAGES = RING_BYTES / STAGE_BYTES < MAX_STAGES ? RING_BYTES / STAGE_BYTES : MAX_STAGES;
+    constexpr int ACC_COLS = BN * (PARTS == 3 ? 2 : 1);
+    constexpr int KE = F8 ? 128 : 64;   // elements of k in a k-block
+    static_assert(STAGES >= 2 && 2 * ACC_COLS <= TMEM_COLS, "ring and accumulators");
+    static_assert(PARTS == 1 || RUNS, "the split product is summed in runs");
+
+    extern __shared__ char smem_raw[];
+    char *ring = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    float *staging = reinterpret_cast<float *>(ring + RING_BYTES);
+    GemmShared *sh = reinterpret_cast<GemmShared *>(ring + RING_BYTES + STAGING_BYTES);
+    volatile int *abort_flag = &sh->abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(&sh->full[s], 1);
+            mbar_init(&sh->empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&sh->t_full[b], 1);
+            mbar_init(&sh->t_empty[b], EPI_WARPS);
+        }
+        mbar_init(&sh->drain, 1);
+        sh->abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)),
+                     "r"(TMEM_COLS)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = sh->tmem_base;
+
+    if (warp == TMA_WARP) {
+        uint32_t it = 0, s = 0, ph = 0;
+        bool ok = true;
+        const uint32_t ring_base = smem_u32(ring);
+        for (int64_t i = blockIdx.x; ok && i < g.items; i += gridDim.x) {
+            const Item t = item_at(g, BN, i);
+            for (int kb = 0; kb < t.kbn; ++kb, ++it) {
+                if (!(ok = __all_sync(FULL, mbar_wait(&sh->empty[s], ph ^ 1u, abort_flag)))) break;
+                mbar_expect_tx_elected(&sh->full[s], STAGE_BYTES);
+                const int k = (t.kb0 + kb) * KE;
+                uint32_t dst = ring_base + s * (uint32_t)STAGE_BYTES;
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p, dst += A_BYTES) {
+                    if (!g.a_mn)
+                        tma_load_3d_elected(dst, &map_a, k, (int)t.m0, p, &sh->full[s]);
+                    else {
+#pragma unroll
+                        for (int b = 0; b < BM / 64; ++b)
+                            tma_load_3d_elected(dst + b * 8192, &map_a, (int)t.m0 + 64 * b, k, p, &sh->full[s]);
+                    }
+                }
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p, dst += B_BYTES) {
+                    if (!g.b_mn)
+                        tma_load_3d_elected(dst, &map_b, k, t.n0, p, &sh->full[s]);
+                    else {
+#pragma unroll
+                        for (int b = 0; b < BN / 64; ++b)
+                            tma_load_3d_elected(dst + b * 8192, &map_b, t.n0 + 64 * b, k, p, &sh->full[s]);
+                    }
+                }
+                if (++s == (uint32_t)STAGES) {
+                    s = 0;
+                    ph ^= 1u;
+                }
+            }
+        }
+        // after an abort the loads already issued get time to land before the block leaves
+        if (lane == 0 && (!ok || *abort_flag))
+#pragma unroll 1
+            for (uint32_t j = it > (uint32_t)STAGES ? it - (uint32_t)STAGES : 0u; j < it; ++j)
+                mbar_wait_quiet(&sh->full[j % (uint32_t)STAGES], (j / (uint32_t)STAGES) & 1u, DRAIN_LIMIT_CLOCKS);
+    } else if (warp == MMA_WARP) {
+        uint32_t acc = 0, s = 0, ph = 0;
+        bool ok = true;
+        const uint32_t ring_base = smem_u32(ring);
+        const uint64_t astep = g.a_mn ? 2048 >> 4 : 32 >> 4, bstep = g.b_mn ? 2048 >> 4 : 32 >> 4;
+        for (int64_t i = blockIdx.x; ok && i < g.items; i += gridDim.x) {
+            const int kbn = item_at(g, BN, i).kbn;
+            for (int kb = 0; ok && kb < kbn; ++acc) {
+                const int run_end = RUNS ? min(kb + RUN_KB, kbn) : kbn;
+                const uint32_t buf = acc & 1u, use = (acc >> 1) & 1u;
+                if (!(ok = __all_sync(FULL, mbar_wait(&sh->t_empty[buf], use ^ 1u, abort_flag)))) break;
+                tc_fence_after();
+                const uint32_t d_tmem = tmem_base + buf * ACC_COLS;
+                for (uint32_t first = 0; kb < run_end; ++kb, first = 1) {
+                    if (!(ok = __all_sync(FULL, mbar_wait(&sh->full[s], ph, abort_flag)))) break;
+                    tc_fence_after();
+                    const uint32_t a = ring_base + s * (uint32_t)STAGE_BYTES, b = a + PARTS * A_BYTES;
+                    if constexpr (PARTS == 1) {
+                        umma_kblock_elected<F8>(d_tmem, operand_desc(a, g.a_mn), operand_desc(b, g.b_mn), astep, bstep, g.idesc,
+                                                first);
+                    } else {
+                        constexpr int pa[6] = {0, 2, 0, 1, 1, 0}, pb[6] = {0, 0, 2, 1, 0, 1};
+#pragma unroll
+                        for (int q = 0; q < 6; ++q)
+                            umma_kblock_elected<F8>(d_tmem + (q == 0 ? 0 : BN), operand_desc(a + pa[q] * A_BYTES, g.a_mn),
+                                                    operand_desc(b + pb[q] * B_BYTES, g.b_mn), astep, bstep, g.idesc,
+                                                    q <= 1 ? first : 1u);
+                    }
+                    umma_commit_elected(&sh->empty[s]);
+                    if (++s == (uint32_t)STAGES) {
+                        s = 0;
+                        ph ^= 1u;
+                    }
+                }
+                if (ok) umma_commit_elected(&sh->t_full[buf]);
+            }
+        }
+        if (__any_sync(FULL, !ok || *abort_flag)) {
+            umma_commit_elected(&sh->drain);
+            if (lane == 0) mbar_wait_quiet(&sh->drain, 0u, DRAIN_LIMIT_CLOCKS);
+        }
+    } else {
+        const int quad = warp & 3, half = warp >> 2;   // TMEM lanes 32 quad.. and the columns' half are this warp's
+        constexpr int COLS = BN / 2, CHUNKS = COLS / 32;
+        float4 *mine = reinterpret_cast<float4 *>(staging + warp * 1024);
+        uint32_t acc = 0;
+        bool ok = true;
+        // 32 columns of this warp's 32 rows, one row per lane, through shared memory (16-byte chunk c of row r lies at
+        // c ^ (r & 7)) so that neighbouring lanes finish neighbouring columns
+        auto finish_chunk = [&](const Item &t, int col, const float (&v)[32]) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                mine[lane * 8 + (c ^ (lane & 7))] = make_float4(v[c * 4], v[c * 4 + 1], v[c * 4 + 2], v[c * 4 + 3]);
+            __syncwarp();
+            const int64_t row0 = t.m0 + quad * 32;
+            if (e.share) {
+                float *to = e.share + ((int64_t)t.split * e.M + row0) * e.ld_share;
+                const int cc = lane & 7;
+#pragma unroll
+                for (int r = lane >> 3; r < 32; r += 4)
+                    if (row0 + r < e.M && col + cc * 4 < e.ld_share)
+                        *reinterpret_cast<float4 *>(to + (int64_t)r * e.ld_share + col + cc * 4) = mine[r * 8 + (cc ^ (r & 7))];
+            } else if (e.vec) {
+                const int cc = lane & 3;
+                if (col + cc * 8 < e.N) {
+                    Columns<8> c;
+                    c.load(e, col + cc * 8);
+#pragma unroll
+                    for (int r = lane >> 2; r < 32; r += 8) {
+                        if (row0 + r >= e.M) continue;
+                        const float4 a = mine[r * 8 + ((2 * cc) ^ (r & 7))], b = mine[r * 8 + ((2 * cc + 1) ^ (r & 7))];
+                        float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                        finish(e, row0 + r, col + cc * 8, c, w);
+                    }
+                }
+            } else if (col + lane < e.N) {
+                Columns<1> c;
+                c.load(e, col + lane);
+                const float *flat = reinterpret_cast<const float *>(mine);
+                for (int r = 0; r < 32 && row0 + r < e.M; ++r) {
+                    float w[1] = {flat[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)]};
+                    finish(e, row0 + r, col + lane, c, w);
+                }
+            }
+            __syncwarp();
+        };
+        for (int64_t i = blockIdx.x; ok && i < g.items; i += gridDim.x) {
+            const Item t = item_at(g, BN, i);
+            const int col0 = t.n0 + half * COLS;
+            if constexpr (RUNS) {
+                float sum[CHUNKS][32];
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) sum[c][j] = 0.f;
+                for (int kb = 0; kb < t.kbn; kb += RUN_KB, ++acc) {
+                    const uint32_t buf = acc & 1u, use = (acc >> 1) & 1u;
+                    if (!(ok = mbar_wait(&sh->t_full[buf], use, abort_flag))) break;
+                    tc_fence_after();
+                    const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + buf * ACC_COLS + half * COLS;
+#pragma unroll
+                    for (int c = 0; c < CHUNKS; ++c) {
+                        uint32_t v[32];
+                        tmem_ld32_issue(taddr + c * 32, v);
+                        if constexpr (PARTS == 3) {
+                            uint32_t w[32];
+                            tmem_ld32_issue(taddr + BN + c * 32, w);
+                            tmem_ld_wait(v);
+                            tmem_ld_wait(w);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) sum[c][j] += __uint_as_float(v[j]) + __uint_as_float(w[j]);
+                        } else {
+                            tmem_ld_wait(v);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) sum[c][j] += __uint_as_float(v[j]);
+                        }
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh->t_empty[buf]);
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int c = 0; c < CHUNKS; ++c) finish_chunk(t, col0 + c * 32, sum[c]);
+            } else {
+                const uint32_t buf = acc & 1u, use = (acc >> 1) & 1u;
+                ++acc;
+                if (!(ok = mbar_wait(&sh->t_full[buf], use, abort_flag))) break;
+                tc_fence_after();
+                const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + buf * ACC_COLS + half * COLS;
+#pragma unroll 1
+                for (int c = 0; c < CHUNKS; ++c) {
+                    uint32_t v[32];
+                    tmem_ld32_issue(taddr + c * 32, v);
+                    tmem_ld_wait(v);
+                    if (c == CHUNKS - 1) {
+                        tc_fence_before();   // every column is in registers: the accumulator is free
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sh->t_empty[buf]);
+                    }
+                    float f[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
+                    finish_chunk(t, col0 + c * 32, f);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    if (sh->abort && threadIdx.x == 0) ep_raise(status, EP_ERR_TIMEOUT);
+    if (warp == 0) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
+    }
+}
+
+// The shares of a split sum added in order, then the epilogue.  A thread finishes 8 columns of a row.
+__global__ void __launch_bounds__(256) linear_join(const float *__restrict__ shares, int splits, const Epilogue e) {
+    const int chunks = (e.N + 7) / 8;
+    const int64_t total = e.M * chunks;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t row = i / chunks;
+        const int col = (int)(i - row * chunks) * 8;
+        const float *from = shares + row * e.ld_share + col;
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int s = 0; s < splits; ++s, from += e.M * e.ld_share) {
+            const float4 a = *reinterpret_cast<const float4 *>(from), b = *reinterpret_cast<const float4 *>(from + 4);
+            v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w;
+            v[4] += b.x, v[5] += b.y, v[6] += b.z, v[7] += b.w;
+        }
+        Columns<8> c;
+        c.load(e, col);
+        finish(e, row, col, c, v);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- few rows
+// A warp computes one column of ROWS rows: its lanes share out the row of W in 16-byte chunks, which are read once; x
+// comes from the L1.  Sums are fp32 multiply-adds to nearest, so all types are exact to fp32 here.
+template <typename T, int ROWS>
+__global__ void __launch_bounds__(256) linear_few_rows(const T *__restrict__ x, int64_t ldx, const T *__restrict__ w, int64_t ldw,
+                                                       int n_in, const Epilogue e, bool vec) {
+    constexpr int N = 16 / (int)sizeof(T);
+    const int lane = threadIdx.x & 31;
+    const int col = (int)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (col >= e.N) return;
+    float sum[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) sum[r] = 0.f;
+    const T *wr = w + col * ldw;
+#pragma unroll 4
+    for (int c = lane * N; c < n_in; c += 32 * N) {
+        float a[N];
+        load_chunk(wr, c, n_in, vec, 0.f, a);
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            if (r < e.M) {
+                float b[N];
+                load_chunk(x + r * ldx, c, n_in, vec, 0.f, b);
+#pragma unroll
+                for (int i = 0; i < N; ++i) sum[r] = fmaf(a[i], b[i], sum[r]);
+            }
+        }
+    }
+    float v[1] = {0.f};
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) sum[r] += __shfl_xor_sync(FULL, sum[r], o);
+        if (lane == r) v[0] = sum[r];
+    }
+    if (lane < ROWS && lane < e.M) {
+        Columns<1> c;
+        c.load(e, col);
+        finish(e, lane, col, c, v);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- operands
+// x = x1 + x2 + x3, each the bf16 nearest to what is left (x1 by truncation: it never overflows to infinity).
+__device__ __forceinline__ void split3(float x, __nv_bfloat16 (&p)[3]) {
+    const float a = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+    p[0] = __float2bfloat16_rn(a);
+    const float r = x - a;
+    p[1] = __float2bfloat16_rn(r);
+    p[2] = __float2bfloat16_rn(r - __bfloat162float(p[1]));
+}
+
+// Copies rows of `cols` elements, `ld` apart, to rows ld_to apart (a multiple of 16 bytes; the tail is zero).
+// PARTS == 3: fp32 to three bf16 matrices, part_stride elements apart.
+template <typename T, typename O, int PARTS>
+__global__ void __launch_bounds__(256) pack_rows(const T *__restrict__ from, int64_t ld, int64_t rows, int cols, O *__restrict__ to,
+                                                 int ld_to, int64_t part_stride, bool vec) {
+    const int chunks = ld_to / 8;
+    const int64_t total = rows * chunks;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t row = i / chunks;
+        const int col = (int)(i - row * chunks) * 8;
+        if constexpr (PARTS == 3) {
+            float v[8];
+            load_chunk(from + row * ld, col, cols, vec, 0.f, v);
+            __nv_bfloat16 p[8][3];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) split3(v[q], p[q]);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                alignas(16) __nv_bfloat16 o[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) o[q] = p[q][k];
+                *reinterpret_cast<uint4 *>(to + k * part_stride + row * ld_to + col) = *reinterpret_cast<const uint4 *>(o);
+            }
+        } else {
+            alignas(16) O o[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) o[q] = col + q < cols ? from[row * ld + col + q] : O{};
+            using R = typename Raw<8 * (int)sizeof(O)>::type;
+            *reinterpret_cast<R *>(to + row * ld_to + col) = *reinterpret_cast<const R *>(o);
+        }
+    }
+}
+
+// dz = dout act'(z), written for the products (16 bits as they are, fp32 as three bf16 parts; rows ld_to apart, zero
+// beyond N), and the sums of its columns over this block's rows: part[blockIdx.y][N].
+constexpr int DZ_CHUNKS = 16, DZ_ROWS = 16;   // a block covers 128 columns, 16 rows at a time
+template <typename T, typename D, int PARTS>
+__global__ void __launch_bounds__(DZ_CHUNKS *DZ_ROWS) linear_dz(const D *__restrict__ dout, const T *__restrict__ z, int act,
+                                                                int64_t rows, int n_out, void *to_raw, int ld_to,
+                                                                int64_t part_stride, float *__restrict__ part, int64_t slab,
+                                                                bool vec) {
+    __shared__ float fold[DZ_ROWS][DZ_CHUNKS * 8];
+    const int cx = threadIdx.x % DZ_CHUNKS, r0 = threadIdx.x / DZ_CHUNKS;
+    const int col = (blockIdx.x * DZ_CHUNKS + cx) * 8;
+    const int64_t begin = (int64_t)blockIdx.y * slab, end = min(rows, begin + slab);
+    float sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+    if (col < ld_to)
+        for (int64_t row = begin + r0; row < end; row += DZ_ROWS) {
+            float v[8];
+            load_chunk(dout + row * n_out, col, n_out, vec, 0.f, v);
+            if (act != EP_ACT_NONE) {
+                float zz[8];
+                load_chunk(z + row * n_out, col, n_out, vec, 0.f, zz);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= slope_of(zz[i], act);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += col + i < n_out ? v[i] : 0.f;
+            if (to_raw) {
+                if constexpr (PARTS == 3) {
+                    __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(to_raw) + row * ld_to + col;
+                    __nv_bfloat16 p[8][3];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) split3(v[q], p[q]);
+#pragma unroll
+                    for (int k = 0; k < 3; ++k) {
+                        alignas(16) __nv_bfloat16 o[8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) o[q] = p[q][k];
+                        *reinterpret_cast<uint4 *>(to + k * part_stride) = *reinterpret_cast<const uint4 *>(o);
+                    }
+                } else {
+                    store_chunk(static_cast<T *>(to_raw) + row * ld_to, col, ld_to, true, v);
+                }
+            }
+        }
+    if (!part) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) fold[r0][cx * 8 + i] = sum[i];
+    __syncthreads();
+    for (int c = threadIdx.x; c < DZ_CHUNKS * 8; c += DZ_CHUNKS * DZ_ROWS) {
+        const int to = blockIdx.x * DZ_CHUNKS * 8 + c;
+        if (to >= n_out) continue;
+        float t = 0.f;
+#pragma unroll
+        for (int q = 0; q < DZ_ROWS; ++q) t += fold[q][c];
+        part[(size_t)blockIdx.y * n_out + to] = t;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- host side
+constexpr int MAX_WIDTH = 65536;
+constexpr int FEW_ROWS = 8;
+constexpr int PACK_BLOCKS_PER_SM = 8;
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn() {
+    static EncodeTiledFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiledFn>(p);
+    });
+    return fn;
+}
+
+// An operand as the tile kernel reads it: `parts` matrices [rows][cols], rows ld elements apart.
+struct Operand {
+    const void *base;
+    int type;             // EP_BF16, EP_F16 or EP_E4M3
+    int64_t rows;
+    int cols;
+    int64_t ld;
+    int parts;
+    int64_t part_stride;
+};
+
+// A tile of the operand is 128 bytes of k (K-major) or 64 of its columns x 64 k (MN-major) by box_rows rows.
+bool encode_operand(CUtensorMap *map, const Operand &o, bool mn, int box_rows) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t size = (cuuint64_t)ep::type_size(o.type);
+    const cuuint64_t dims[3] = {(cuuint64_t)o.cols, (cuuint64_t)o.rows, (cuuint64_t)o.parts};
+    const cuuint64_t strides[2] = {(cuuint64_t)o.ld * size, (cuuint64_t)(o.parts > 1 ? o.part_stride : o.ld * o.rows) * size};
+    const cuuint32_t box[3] = {(cuuint32_t)(128 / size), (cuuint32_t)(mn ? 64 : box_rows), 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUtensorMapDataType type = o.type == EP_BF16  ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                     : o.type == EP_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                        : CU_TENSOR_MAP_DATA_TYPE_UINT8;
+    return fn(map, type, 3, const_cast<void *>(o.base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+struct GemmPlan {
+    int bn, splits;
+    bool runs;
+    int ld_share;
+    GemmShape shape;
+    size_t share_bytes(int64_t M) const { return splits > 1 ? sizeof(float) * (size_t)splits * (size_t)M * (size_t)ld_share : 0; }
+};
+
+// Tile width and split of the sum.  A block's time for a tile is about its columns plus a constant (the A tile, the
+// pipeline's start), so the width with the least waves x (columns + 32) is taken.  When all tiles fit one wave with
+// blocks to spare, the sum over k is split between them, into shares of at least 4 k-blocks.
+GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, int parts, bool fp32_out) {
+    GemmPlan p{};
+    p.runs = fp32_out;
+    const int ke = type == EP_E4M3 ? 128 : 64;
+    p.shape.M = M;
+    p.shape.N = N;
+    p.shape.kb = (int)ep::ceil_div(K, ke);
+    int64_t best = 0;
+    for (int bn : {256, 128, 64}) {
+        if (p.runs && bn != 128) continue;
+        const int64_t tiles = ep::ceil_div(M, BM) * ep::ceil_div(N, bn);
+        const int64_t cost = ep::ceil_div(tiles, ctx->sm_count) * (bn + 32);
+        if (!p.bn || cost < best) {
+            best = cost;
+            p.bn = bn;
+        }
+    }
+    p.shape.tiles_n = (int)ep::ceil_div(N, p.bn);
+    p.shape.tiles = ep::ceil_div(M, BM) * p.shape.tiles_n;
+    int64_t splits = std::max<int64_t>(1, std::min<int64_t>(ctx->sm_count / p.shape.tiles, p.shape.kb / 4));
+    int per = (int)ep::ceil_div(p.shape.kb, splits);
+    if (p.runs) per = (int)round_up(per, RUN_KB);
+    p.splits = (int)ep::ceil_div(p.shape.kb, per);
+    p.shape.kb_per_split = per;
+    p.shape.items = p.shape.tiles * p.splits;
+    p.ld_share = (int)round_up(N, 8);
+    return p;
+}
+
+template <int BN, bool F8, int PARTS, bool RUNS>
+int launch_tiles(ep_ctx *ctx, const GemmPlan &p, const CUtensorMap &ma, const CUtensorMap &mb, const Epilogue &e,
+                 cudaStream_t stream) {
+    auto kernel = linear_tiles<BN, F8, PARTS, RUNS>;
+    EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)GEMM_SMEM));
+    const int grid = (int)std::min<int64_t>(p.shape.items, ctx->sm_count);
+    kernel<<<grid, GEMM_THREADS, GEMM_SMEM, stream>>>(ma, mb, p.shape, e, ctx->d_status);
+    EP_CUDA(ctx, cudaGetLastError());
+    return EP_OK;
+}
+
+// D = A B^T by tiles, with the epilogue; `share` is room for the shares of a split sum.  Adds to *kernels.
+int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand &b, bool b_mn, Epilogue e, float *share,
+             cudaStream_t stream, int *kernels) {
+    const bool f8 = a.type == EP_E4M3;
+    const uint32_t fmt = a.type == EP_BF16 ? 1u : 0u;   // f16 and e4m3 are both format 0 of their kinds
+    p.shape.a_mn = a_mn;
+    p.shape.b_mn = b_mn;
+    p.shape.idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+                    ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
+    CUtensorMap ma, mb;
+    if (!encode_operand(&ma, a, a_mn, BM) || !encode_operand(&mb, b, b_mn, p.bn))
+        return ep::fail(ctx, EP_ERR_CUDA, "cuTensorMapEncodeTiled failed for a product of %lld x %d", (long long)e.M, e.N);
+    e.share = p.splits > 1 ? share : nullptr;
+    e.ld_share = p.ld_share;
+    int rc;
+    if (a.parts == 3)
+        rc = launch_tiles<128, false, 3, true>(ctx, p, ma, mb, e, stream);
+    else if (f8)
+        rc = p.runs        ? launch_tiles<128, true, 1, true>(ctx, p, ma, mb, e, stream)
+             : p.bn == 256 ? launch_tiles<256, true, 1, false>(ctx, p, ma, mb, e, stream)
+             : p.bn == 128 ? launch_tiles<128, true, 1, false>(ctx, p, ma, mb, e, stream)
+                           : launch_tiles<64, true, 1, false>(ctx, p, ma, mb, e, stream);
+    else
+        rc = p.runs        ? launch_tiles<128, false, 1, true>(ctx, p, ma, mb, e, stream)
+             : p.bn == 256 ? launch_tiles<256, false, 1, false>(ctx, p, ma, mb, e, stream)
+             : p.bn == 128 ? launch_tiles<128, false, 1, false>(ctx, p, ma, mb, e, stream)
+                           : launch_tiles<64, false, 1, false>(ctx, p, ma, mb, e, stream);
+    if (rc != EP_OK) return rc;
+    ++*kernels;
+    if (p.splits > 1) {
+        const int64_t threads = e.M * ((e.N + 7) / 8);
+        const int grid = (int)std::min<int64_t>(ep::ceil_div(threads, 256), (int64_t)ctx->sm_count * PACK_BLOCKS_PER_SM);
+        linear_join<<<grid, 256, 0, stream>>>(share, p.splits, e);
+        EP_CUDA(ctx, cudaGetLastError());
+        ++*kernels;
+    }
+    return EP_OK;
+}
+
+bool tma_ready(const void *p, int64_t ld, int type) { return ep::aligned(p, 16) && ld * ep::type_size(type) % 16 == 0; }
+
+// The copy of an operand that TMA can read: fp32 always (three bf16 parts), others when unaligned.
+struct Packed {
+    int ld, parts, type;
+    int64_t part_stride;
+    size_t bytes;
+};
+Packed packed_form(int64_t rows, int cols, int type) {
+    Packed p;
+    p.parts = type == EP_F32 ? 3 : 1;
+    p.type = type == EP_F32 ? EP_BF16 : type;
+    p.ld = (int)round_up(cols, type == EP_E4M3 ? 16 : 8);
+    p.part_stride = rows * p.ld;
+    p.bytes = (size_t)p.parts * (size_t)p.part_stride * (size_t)ep::type_size(p.type);
+    return p;
+}
+
+// `base` as an operand, copied to `room` first where it has to be (needs_copy).
+int make_operand(ep_ctx *ctx, const void *base, int64_t ld, int64_t rows, int cols, int type, bool needs_copy, void *room,
+                 cudaStream_t stream, Operand *out, int *kernels) {
+    if (!needs_copy) {
+        *out = Operand{base, type, rows, cols, ld, 1, 0};
+        return EP_OK;
+    }
+    const Packed p = packed_form(rows, cols, type);
+    const int64_t threads = rows * (p.ld / 8);
+    const int grid = (int)std::min<int64_t>(ep::ceil_div(threads, 256), (int64_t)ctx->sm_count * PACK_BLOCKS_PER_SM);
+    const bool vec = ep::aligned(base, 16) && ld * ep::type_size(type) % 16 == 0 && cols % 8 == 0;
+    if (type == EP_F32)
+        pack_rows<float, __nv_bfloat16, 3><<<grid, 256, 0, stream>>>(static_cast<const float *>(base), ld, rows, cols,
+                                                                     static_cast<__nv_bfloat16 *>(room), p.ld, p.part_stride, vec);
+    else if (type == EP_E4M3)
+        pack_rows<uint8_t, uint8_t, 1><<<grid, 256, 0, stream>>>(static_cast<const uint8_t *>(base), ld, rows, cols,
+                                                                 static_cast<uint8_t *>(room), p.ld, p.part_stride, vec);
+    else
+        pack_rows<uint16_t, uint16_t, 1><<<grid, 256, 0, stream>>>(static_cast<const uint16_t *>(base), ld, rows, cols,
+                                                                   static_cast<uint16_t *>(room), p.ld, p.part_stride, vec);
+    EP_CUDA(ctx, cudaGetLastError());
+    ++*kernels;
+    *out = Operand{room, p.type, rows, cols, p.ld, p.parts, p.part_stride};
+    return EP_OK;
+}
+
+bool linear_shape_ok(int64_t rows, int n_in, int n_out) {
+    return rows >= 0 && rows < (1ll << 31) && n_in >= 1 && n_in <= MAX_WIDTH && n_out >= 1 && n_out <= MAX_WIDTH;
+}
+bool linear_types_ok(int in_type, int out_type) {
+    if (in_type == EP_E4M3) return ep::float_type(out_type);
+    return ep::float_type(in_type) && (out_type == in_type || out_type == EP_F32);
+}
+
+struct LinearWorkspace {
+    void *x, *w;
+    float *share;
+    GemmPlan plan;
+    size_t bytes;
+};
+LinearWorkspace linear_workspace(const ep_ctx *ctx, int64_t rows, int n_in, int n_out, int in_type, int out_type, bool aligned,
+                                 void *base) {
+    ep::Arena a(base);
+    LinearWorkspace w{};
+    if (rows > FEW_ROWS) {
+        const bool copy = in_type == EP_F32 || !aligned;
+        if (copy) {
+            w.x = a.take<char>(packed_form(rows, n_in, in_type).bytes);
+            w.w = a.take<char>(packed_form(n_out, n_in, in_type).bytes);
+        }
+        w.plan = plan_gemm(ctx, rows, n_out, n_in, in_type, in_type == EP_F32 ? 3 : 1, out_type == EP_F32);
+        w.share = a.take<float>(w.plan.share_bytes(rows) / sizeof(float));
+    }
+    w.bytes = std::max<size_t>(a.used, 256);
+    return w;
+}
+
+struct BackwardWorkspace {
+    void *dz, *x, *w;
+    float *dbias_parts, *share;
+    GemmPlan dx, dw;
+    Packed dz_form;
+    int slabs;
+    int64_t slab;
+    size_t bytes;
+};
+BackwardWorkspace backward_workspace(const ep_ctx *ctx, int64_t rows, int n_in, int n_out, int in_type, bool aligned, void *base) {
+    ep::Arena a(base);
+    BackwardWorkspace w{};
+    const bool copy = in_type == EP_F32 || !aligned;
+    w.dz_form = packed_form(rows, n_out, in_type);
+    w.dz = a.take<char>(w.dz_form.bytes);
+    if (copy) {
+        w.x = a.take<char>(packed_form(rows, n_in, in_type).bytes);
+        w.w = a.take<char>(packed_form(n_out, n_in, in_type).bytes);
+    }
+    const int across = (int)ep::ceil_div(w.dz_form.ld, DZ_CHUNKS * 8);
+    const int64_t want = std::max<int64_t>(1, (int64_t)ctx->sm_count * 8 / across);
+    w.slab = round_up(ep::ceil_div(std::max<int64_t>(rows, 1), want), DZ_ROWS);
+    w.slabs = (int)std::max<int64_t>(1, ep::ceil_div(rows, w.slab));
+    w.dbias_parts = a.take<float>((size_t)w.slabs * n_out);
+    const int parts = in_type == EP_F32 ? 3 : 1;
+    w.dx = plan_gemm(ctx, std::max<int64_t>(rows, 1), n_in, n_out, in_type, parts, in_type == EP_F32);
+    w.dw = plan_gemm(ctx, n_out, n_in, std::max<int64_t>(rows, 1), in_type, parts, in_type == EP_F32);
+    w.share = a.take<float>(std::max(w.dx.share_bytes(rows), w.dw.share_bytes(n_out)) / sizeof(float));
+    w.bytes = std::max<size_t>(a.used, 256);
+    return w;
+}
+
+template <int ROWS>
+int launch_few_rows(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int64_t ldw, int in_type, int n_in, const Epilogue &e,
+                    bool vec, cudaStream_t stream) {
+    const int grid = (int)ep::ceil_div(e.N, 8);
+    if (in_type == EP_F32)
+        linear_few_rows<float, ROWS><<<grid, 256, 0, stream>>>((const float *)x, ldx, (const float *)w, ldw, n_in, e, vec);
+    else if (in_type == EP_BF16)
+        linear_few_rows<__nv_bfloat16, ROWS><<<grid, 256, 0, stream>>>((const __nv_bfloat16 *)x, ldx, (const __nv_bfloat16 *)w, ldw,
+                                                                       n_in, e, vec);
+    else if (in_type == EP_F16)
+        linear_few_rows<__half, ROWS><<<grid, 256, 0, stream>>>((const __half *)x, ldx, (const __half *)w, ldw, n_in, e, vec);
+    else
+        linear_few_rows<e4m3, ROWS><<<grid, 256, 0, stream>>>((const e4m3 *)x, ldx, (const e4m3 *)w, ldw, n_in, e, vec);
+    EP_CUDA(ctx, cudaGetLastError());
+    return EP_OK;
+}
+
+template <typename T, typename D, int PARTS>
+void launch_dz(const BackwardWorkspace &w, const void *dout, const void *z, int act, int64_t rows, int n_out, bool write, bool sum,
+               bool vec, cudaStream_t stream) {
+    const dim3 grid((unsigned)ep::ceil_div(w.dz_form.ld, DZ_CHUNKS * 8), (unsigned)w.slabs);
+    linear_dz<T, D, PARTS><<<grid, DZ_CHUNKS * DZ_ROWS, 0, stream>>>((const D *)dout, (const T *)z, act, rows, n_out,
+                                                                     write ? w.dz : nullptr, w.dz_form.ld, w.dz_form.part_stride,
+                                                                     sum ? w.dbias_parts : nullptr, w.slab, vec);
+}
+
+int linear_run(ep_ctx *ctx, const LinearWorkspace &ws, const void *x, int64_t ldx, const void *w, int64_t ldw, int in_type,
+               int64_t rows, int n_in, int n_out, bool aligned, const Epilogue &e, cudaStream_t stream, int *kernels) {
+    if (rows <= FEW_ROWS) {
+        const int n = 16 / ep::type_size(in_type);
+        const bool vec = aligned && n_in % n == 0;
+        ++*kernels;
+        if (rows == 1) return launch_few_rows<1>(ctx, x, ldx, w, ldw, in_type, n_in, e, vec, stream);
+        if (rows == 2) return launch_few_rows<2>(ctx, x, ldx, w, ldw, in_type, n_in, e, vec, stream);
+        if (rows <= 4) return launch_few_rows<4>(ctx, x, ldx, w, ldw, in_type, n_in, e, vec, stream);
+        return launch_few_rows<8>(ctx, x, ldx, w, ldw, in_type, n_in, e, vec, stream);
+    }
+    const bool copy = in_type == EP_F32 || !aligned;
+    Operand a, b;
+    int rc = make_operand(ctx, x, ldx, rows, n_in, in_type, copy, ws.x, stream, &a, kernels);
+    if (rc == EP_OK) rc = make_operand(ctx, w, ldw, n_out, n_in, in_type, copy, ws.w, stream, &b, kernels);
+    if (rc == EP_OK) rc = run_gemm(ctx, ws.plan, a, false, b, false, e, ws.share, stream, kernels);
+    return rc;
+}
+
+int linear_backward_run(ep_ctx *ctx, const BackwardWorkspace &ws, const void *dout, int dout_type, const void *preact, int act,
+                        const void *x, int64_t ldx, const void *w, int64_t ldw, int in_type, int64_t rows, int n_in, int n_out,
+                        bool aligned, void *dx, void *dweight, float *dbias, cudaStream_t stream, int *kernels) {
+    const bool copy = in_type == EP_F32 || !aligned;
+    const bool direct = act == EP_ACT_NONE && dout_type == in_type && !copy && tma_ready(dout, n_out, in_type);
+    const bool write = !direct && (dx || dweight);
+    if (write || dbias) {
+        const bool vec = n_out % 8 == 0 && ep::aligned(dout, 16) && ep::aligned(preact, 16);
+        if (in_type == EP_F32)
+            launch_dz<float, float, 3>(ws, dout, preact, act, rows, n_out, write, dbias, vec, stream);
+        else if (in_type == EP_BF16 && dout_type == EP_BF16)
+            launch_dz<__nv_bfloat16, __nv_bfloat16, 1>(ws, dout, preact, act, rows, n_out, write, dbias, vec, stream);
+        else if (in_type == EP_BF16)
+            launch_dz<__nv_bfloat16, float, 1>(ws, dout, preact, act, rows, n_out, write, dbias, vec, stream);
+        else if (dout_type == EP_F16)
+            launch_dz<__half, __half, 1>(ws, dout, preact, act, rows, n_out, write, dbias, vec, stream);
+        else
+            launch_dz<__half, float, 1>(ws, dout, preact, act, rows, n_out, write, dbias, vec, stream);
+        EP_CUDA(ctx, cudaGetLastError());
+        ++*kernels;
+        if (dbias) {
+            const int rc = ep::sum_partials(ctx, ws.dbias_parts, ws.slabs, n_out, dbias, stream);
+            if (rc != EP_OK) return rc;
+            ++*kernels;
+        }
+    }
+    Operand dz;
+    if (direct)
+        dz = Operand{dout, in_type, rows, n_out, n_out, 1, 0};
+    else
+        dz = Operand{ws.dz, ws.dz_form.type, rows, n_out, ws.dz_form.ld, ws.dz_form.parts, ws.dz_form.part_stride};
+    Epilogue e{};
+    e.out_type = in_type;
+    e.bias_type = EP_F32;
+    if (dx) {
+        Operand b;
+        int rc = make_operand(ctx, w, ldw, n_out, n_in, in_type, copy, ws.w, stream, &b, kernels);
+        e.out = dx;
+        e.M = rows;
+        e.N = n_in;
+        e.vec = n_in % 8 == 0 && ep::aligned(dx, 16);
+        if (rc == EP_OK) rc = run_gemm(ctx, ws.dx, dz, false, b, true, e, ws.share, stream, kernels);
+        if (rc != EP_OK) return rc;
+    }
+    if (dweight) {
+        Operand b;
+        int rc = make_operand(ctx, x, ldx, rows, n_in, in_type, copy, ws.x, stream, &b, kernels);
+        e.out = dweight;
+        e.M = n_out;
+        e.N = n_in;
+        e.vec = n_in % 8 == 0 && ep::aligned(dweight, 16);
+        if (rc == EP_OK) rc = run_gemm(ctx, ws.dw, dz, true, b, true, e, ws.share, stream, kernels);
+        if (rc != EP_OK) return rc;
+    }
+    return EP_OK;
+}
+
+}  // namespace
+
+using namespace ep;
+
+namespace {
+bool type_aligned(const void *p, int type) { return !p || aligned(p, (size_t)type_size(type)); }
+}  // namespace
+
+extern "C" {
+
+size_t ep_linear_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t n_in, int32_t n_out, int32_t in_type,
+                                 int32_t out_type, int32_t is_aligned) {
+    if (!ctx || !linear_shape_ok(rows, n_in, n_out) || !linear_types_ok(in_type, out_type)) return 0;
+    return linear_workspace(ctx, rows, n_in, n_out, in_type, out_type, is_aligned != 0, nullptr).bytes;
+}
+
+int ep_linear(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int64_t ldw, int32_t in_type, const float *x_scale,
+              const float *w_scale, const void *bias, int32_t bias_type, int32_t act, const void *residual, int64_t ldr,
+              void *out, int32_t out_type, void *preact, int64_t rows, int32_t n_in, int32_t n_out, void *workspace,
+              size_t workspace_bytes, void *cuda_stream) {
+    if (!ctx) return EP_ERR_INVALID_ARG;
+    if (!linear_shape_ok(rows, n_in, n_out))
+        return fail(ctx, EP_ERR_INVALID_ARG, "rows %lld, n_in %d or n_out %d out of range", (long long)rows, n_in, n_out);
+    if (!linear_types_ok(in_type, out_type) || (bias && !float_type(bias_type)))
+        return fail(ctx, EP_ERR_INVALID_ARG, "no product of type %d with output of type %d", in_type, out_type);
+    if (act < EP_ACT_NONE || act > EP_ACT_SILU) return fail(ctx, EP_ERR_INVALID_ARG, "unknown activation %d", act);
+    if (ldx < n_in || ldw < n_in || (residual && ldr < n_out)) return fail(ctx, EP_ERR_INVALID_ARG, "a row stride is shorter than its row");
+    if (rows == 0) return EP_OK;
+    if ((in_type == EP_E4M3) != (x_scale != nullptr) || (in_type == EP_E4M3) != (w_scale != nullptr))
+        return fail(ctx, EP_ERR_INVALID_ARG, "scales go with 8-bit inputs, and with no others");
+    if (!x || !w || !out || !type_aligned(x, in_type) || !type_aligned(w, in_type) || !type_aligned(out, out_type) ||
+        !type_aligned(preact, out_type) || !type_aligned(residual, out_type) || !type_aligned(bias, bias ? bias_type : EP_E4M3) ||
+        !aligned(x_scale, 4) || !aligned(w_scale, 4))
+        return fail(ctx, EP_ERR_INVALID_ARG, "null or misaligned pointer");
+    const bool ready = tma_ready(x, ldx, in_type) && tma_ready(w, ldw, in_type);
+    const LinearWorkspace ws = linear_workspace(ctx, rows, n_in, n_out, in_type, out_type, ready, workspace);
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < ws.bytes)
+        return fail(ctx, EP_ERR_WORKSPACE, "workspace too small or misaligned");
+    Epilogue e{};
+    e.x_scale = x_scale;
+    e.w_scale = w_scale;
+    e.bias = bias;
+    e.bias_type = bias_type;
+    e.act = act;
+    e.residual = residual;
+    e.ldr = ldr;
+    e.out = out;
+    e.preact = preact;
+    e.out_type = out_type;
+    e.M = rows;
+    e.N = n_out;
+    e.vec = n_out % 8 == 0 && aligned(out, 16) && aligned(preact, 16) && aligned(residual, 16) &&
+            (!residual || ldr * type_size(out_type) % 16 == 0);
+    DeviceGuard guard(ctx->device);
+    Timed tm(ctx, static_cast<cudaStream_t>(cuda_stream), EP_TIMER_LINEAR);
+    int kernels = 0;
+    const int rc = linear_run(ctx, ws, x, ldx, w, ldw, in_type, rows, n_in, n_out, ready, e, static_cast<cudaStream_t>(cuda_stream),
+                              &kernels);
+    tm.end(kernels);
+    return rc;
+}
+
+size_t ep_linear_backward_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t n_in, int32_t n_out, int32_t in_type,
+                                          int32_t is_aligned) {
+    if (!ctx || !linear_shape_ok(rows, n_in, n_out) || !float_type(in_type)) return 0;
+    return backward_workspace(ctx, rows, n_in, n_out, in_type, is_aligned != 0, nullptr).bytes;
+}
+
+int ep_linear_backward(ep_ctx *ctx, const void *dout, int32_t dout_type, const void *preact, int32_t act, const void *x,
+                       int64_t ldx, const void *w, int64_t ldw, int32_t in_type, int64_t rows, int32_t n_in, int32_t n_out,
+                       void *dx, void *dweight, float *dbias, void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    if (!ctx) return EP_ERR_INVALID_ARG;
+    if (!linear_shape_ok(rows, n_in, n_out))
+        return fail(ctx, EP_ERR_INVALID_ARG, "rows %lld, n_in %d or n_out %d out of range", (long long)rows, n_in, n_out);
+    if (!float_type(in_type) || !(dout_type == in_type || dout_type == EP_F32))
+        return fail(ctx, EP_ERR_INVALID_ARG, "no gradient of type %d for a product of type %d", dout_type, in_type);
+    if (act < EP_ACT_NONE || act > EP_ACT_SILU) return fail(ctx, EP_ERR_INVALID_ARG, "unknown activation %d", act);
+    if (ldx < n_in || ldw < n_in) return fail(ctx, EP_ERR_INVALID_ARG, "a row stride is shorter than its row");
+    if (!type_aligned(dweight, in_type) || !aligned(dbias, 4)) return fail(ctx, EP_ERR_INVALID_ARG, "misaligned pointer");
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    DeviceGuard guard(ctx->device);
+    if (rows == 0) {
+        if (dweight) EP_CUDA(ctx, cudaMemsetAsync(dweight, 0, (size_t)n_out * n_in * type_size(in_type), stream));
+        if (dbias) EP_CUDA(ctx, cudaMemsetAsync(dbias, 0, sizeof(float) * (size_t)n_out, stream));
+        return EP_OK;
+    }
+    if (!dout || (dweight && !x) || (dx && !w) || (act != EP_ACT_NONE && !preact) || !type_aligned(dout, dout_type) ||
+        !type_aligned(preact, in_type) || !type_aligned(x, in_type) || !type_aligned(w, in_type) || !type_aligned(dx, in_type))
+        return fail(ctx, EP_ERR_INVALID_ARG, "null or misaligned pointer");
+    const bool ready = tma_ready(x, ldx, in_type) && tma_ready(w, ldw, in_type);
+    const BackwardWorkspace ws = backward_workspace(ctx, rows, n_in, n_out, in_type, ready, workspace);
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < ws.bytes)
+        return fail(ctx, EP_ERR_WORKSPACE, "workspace too small or misaligned");
+    Timed tm(ctx, stream, EP_TIMER_LINEAR);
+    int kernels = 0;
+    const int rc = linear_backward_run(ctx, ws, dout, dout_type, preact, act, x, ldx, w, ldw, in_type, rows, n_in, n_out, ready, dx,
+                                       dweight, dbias, stream, &kernels);
+    tm.end(kernels);
+    return rc;
+}
+
+}  // extern "C"

@@ -1,0 +1,470 @@
+// Root-mean-square norm with the residual's addition and an optional 8-bit output, its backward pass, and the 8-bit
+// output on its own.
+//
+// One pass over the data: a row stays in the registers of the L threads that share it, between the sum that gives its
+// scale and the product with it, so every input is read once and every output written once.  All of these kernels are
+// bound by HBM bandwidth for many rows and by launch latency for few.
+#include "ep_common.cuh"
+#include "rows.cuh"
+
+#include <algorithm>
+
+using namespace eprow;
+
+namespace {
+
+// Rows of up to V * L chunks of 16 bytes of the input type; thread `lane` of a row holds chunks lane, lane + L, ...
+// (neighbouring threads read neighbouring chunks).  L <= 32: a block of 256 threads has 256 / L rows at a time.
+// L > 32: the block is L threads and has one.
+template <int L>
+constexpr int block_threads() { return L > 32 ? L : 256; }
+
+constexpr float E4M3_TOP = 448.f;
+
+// rho = 1 / sqrt(mean(h^2) + eps) of a row.  Where the fp32 squares leave the range that is safe for their sum (a row of
+// magnitudes below 1e-15 or above 1e18, or of zeros) they are taken of the row times a power of two instead; all
+// threads that reduce together take that turn together.  A row of zeros with eps = 0 has rho = 0, so that it stays zero.
+template <int L, int V, int N>
+__device__ __forceinline__ float row_rho(const float (&h)[V][N], int d, float eps, float *slots, int &turn) {
+    float ss = 0.f;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) ss = fmaf(h[j][i], h[j][i], ss);
+    const float mean = reduce_row<L, OpSum>(ss, slots, turn) / (float)d;
+    float rho = rsqrtf(mean + eps);
+    const bool rare = !(mean + eps > 1e-30f && mean < 1e36f);
+    if (__any_sync(FULL, rare)) {
+        float top = 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(h[j][i]));
+        top = reduce_row<L, OpMaxNumber>(top, slots, turn);
+        // (with eps > 0 magnitudes below 2^-87 do not count beside it; 2^60 keeps eps s^2 finite)
+        const int up = min(max(-ilogbf(fmaxf(top, 1.17549435e-38f)), -100), eps > 0.f ? 60 : 126);
+        const float s = scalbnf(1.f, up);
+        ss = 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) ss = fmaf(h[j][i] * s, h[j][i] * s, ss);
+        const float scaled = reduce_row<L, OpSum>(ss, slots, turn) / (float)d + eps * s * s;
+        if (rare && scaled == 0.f)
+            rho = 0.f;
+        else if (rare)
+            rho = scaled == scaled ? fminf(s * rsqrtf(scaled), 3.4e38f) : scaled;
+    }
+    return rho;
+}
+
+// NORM: the norm; otherwise the rows are only brought to 8 bits.
+template <typename T, typename O, int L, int V, bool NORM>
+__global__ void __launch_bounds__(block_threads<L>()) norm_rows(const T *x, const T *residual, const void *weight,
+                                                                int weight_type, int64_t rows, int d, float eps, O *out,
+                                                                float *scale, T *hidden, bool vec) {
+    constexpr int N = 16 / (int)sizeof(T);
+    constexpr int GROUPS = block_threads<L>() / L;
+    __shared__ float slots[L > 32 ? 64 : 1];
+    int turn = 0;
+    const int lane = threadIdx.x % L, group = threadIdx.x / L;
+    float g[V][N];
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = (j * L + lane) * N + i;
+            g[j][i] = NORM && weight && c < d ? load_param(weight, weight_type, c) : 1.f;
+        }
+    // the loop is the same for all threads of a warp (they reduce together); rows past the end are empty
+    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += (int64_t)gridDim.x * GROUPS) {
+        const int64_t row = first + group;
+        const int width = row < rows ? d : 0;
+        const int64_t at = row < rows ? row * d : 0;
+        float h[V][N];
+#pragma unroll
+        for (int j = 0; j < V; ++j) load_chunk(x + at, (j * L + lane) * N, width, vec, 0.f, h[j]);
+        if (NORM && residual) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float r[N];
+                load_chunk(residual + at, (j * L + lane) * N, width, vec, 0.f, r);
+#pragma unroll
+                for (int i = 0; i < N; ++i) h[j][i] += r[i];
+            }
+        }
+        if (NORM && hidden) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) store_chunk(hidden + at, (j * L + lane) * N, width, vec, h[j]);
+        }
+        if (NORM) {
+            const float rho = row_rho<L>(h, d, eps, slots, turn);
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+#pragma unroll
+                for (int i = 0; i < N; ++i) h[j][i] = h[j][i] * rho * g[j][i];
+        }
+        if constexpr (sizeof(O) == 1) {
+            float top = 0.f;
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+#pragma unroll
+                for (int i = 0; i < N; ++i) top = OpMax::apply(top, fabsf(h[j][i]));
+            const float s = reduce_row<L, OpMax>(top, slots, turn) / E4M3_TOP;
+            // a scale below the smallest normal number has no finite reciprocal worth multiplying by: divide there
+            const bool tiny = s < 1.17549435e-38f;
+            const float inverse = s > 0.f || s != s ? 1.f / s : 0.f;
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+#pragma unroll
+                for (int i = 0; i < N; ++i) h[j][i] = tiny && s > 0.f ? h[j][i] / s : h[j][i] * inverse;
+            if (lane == 0 && row < rows) scale[row] = s;
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) store_chunk(out + at, (j * L + lane) * N, width, vec, h[j]);
+    }
+}
+
+// dx of every row; the block's share of dweight goes to part[blockIdx.x][d] (or to dweight itself when it is alone).
+template <typename T, typename D, int L, int V>
+__global__ void __launch_bounds__(block_threads<L>()) norm_rows_backward(const D *dout, const T *hidden, const void *weight,
+                                                                         int weight_type, const T *dhidden, int64_t rows,
+                                                                         int d, float eps, T *dx, float *part, bool vec) {
+    constexpr int N = 16 / (int)sizeof(T);
+    constexpr int GROUPS = block_threads<L>() / L;
+    __shared__ float slots[L > 32 ? 64 : 1];
+    extern __shared__ float fold[];   // [GROUPS][V * L * N] where GROUPS > 1
+    int turn = 0;
+    const int lane = threadIdx.x % L, group = threadIdx.x / L;
+    float g[V][N], dg[V][N];
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = (j * L + lane) * N + i;
+            g[j][i] = weight && c < d ? load_param(weight, weight_type, c) : 1.f;
+            dg[j][i] = 0.f;
+        }
+    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += (int64_t)gridDim.x * GROUPS) {
+        const int64_t row = first + group;
+        const int width = row < rows ? d : 0;
+        const int64_t at = row < rows ? row * d : 0;
+        float h[V][N], y[V][N];
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            load_chunk(hidden + at, (j * L + lane) * N, width, vec, 0.f, h[j]);
+            load_chunk(dout + at, (j * L + lane) * N, width, vec, 0.f, y[j]);
+        }
+        float ah = 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) ah = fmaf(y[j][i] * g[j][i], h[j][i], ah);
+        const float rho = row_rho<L>(h, d, eps, slots, turn);
+        const float back = rho * (reduce_row<L, OpSum>(ah, slots, turn) / (float)d);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float o[N];
+            if (dhidden)
+                load_chunk(dhidden + at, (j * L + lane) * N, width, vec, 0.f, o);
+            else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) o[i] = 0.f;
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float unit = h[j][i] * rho;
+                o[i] += rho * (y[j][i] * g[j][i] - unit * back);
+                dg[j][i] = fmaf(y[j][i], unit, dg[j][i]);
+            }
+            store_chunk(dx + at, (j * L + lane) * N, width, vec, o);
+        }
+    }
+    if (!part) return;
+    float *to = part + (size_t)blockIdx.x * d;
+    if constexpr (GROUPS == 1) {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int c = (j * L + lane) * N + i;
+                if (c < d) to[c] = dg[j][i];
+            }
+    } else {
+        constexpr int WIDE = V * L * N;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) fold[group * WIDE + (j * L + lane) * N + i] = dg[j][i];
+        __syncthreads();
+        for (int c = threadIdx.x; c < d; c += blockDim.x) {
+            float s = 0.f;
+#pragma unroll 4
+            for (int q = 0; q < GROUPS; ++q) s += fold[q * WIDE + c];
+            to[c] = s;
+        }
+    }
+}
+
+// A block sums 32 columns: 32 x 8 threads, thread (c, r) the rows r, r + 8, ... in fp64; then the eight in order.
+__global__ void __launch_bounds__(256) fold_partials(const float *__restrict__ parts, int n, int cols, float *__restrict__ out) {
+    __shared__ double s[8][32];
+    const int lane = threadIdx.x & 31, r0 = threadIdx.x >> 5;
+    const int c = blockIdx.x * 32 + lane;
+    double t = 0.0;
+    if (c < cols)
+#pragma unroll 4
+        for (int r = r0; r < n; r += 8) t += (double)parts[(size_t)r * cols + c];
+    s[r0][lane] = t;
+    __syncthreads();
+    if (r0 == 0 && c < cols) {
+#pragma unroll
+        for (int q = 1; q < 8; ++q) t += s[q][lane];
+        out[c] = (float)t;
+    }
+}
+
+constexpr int MAX_D = 16384;
+constexpr int BLOCKS_PER_SM = 8;
+
+// The fewest threads and chunks per thread that hold a row of `chunks` 16-byte chunks; F<L, V>() runs the launch.
+template <typename F>
+int with_layout(int64_t chunks, F f) {
+    if (chunks <= 8) return f.template run<8, 1>();
+    if (chunks <= 16) return f.template run<16, 1>();
+    if (chunks <= 32) return f.template run<32, 1>();
+    if (chunks <= 64) return f.template run<32, 2>();
+    if (chunks <= 128) return f.template run<32, 4>();
+    if (chunks <= 256) return f.template run<256, 1>();
+    if (chunks <= 512) return f.template run<256, 2>();
+    if (chunks <= 1024) return f.template run<256, 4>();
+    if (chunks <= 2048) return f.template run<512, 4>();
+    return f.template run<512, 8>();
+}
+
+template <int L>
+int grid_for(const ep_ctx *ctx, int64_t rows) {
+    constexpr int groups = block_threads<L>() / L;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(rows, groups), (int64_t)ctx->sm_count * BLOCKS_PER_SM));
+}
+
+struct NormArgs {
+    ep_ctx *ctx;
+    const void *x, *residual, *weight;
+    int weight_type;
+    int64_t rows;
+    int d;
+    float eps;
+    void *out;
+    float *scale;
+    void *hidden;
+    bool vec;
+    cudaStream_t stream;
+};
+
+template <typename T, typename O, bool NORM>
+struct NormLaunch {
+    const NormArgs &a;
+    template <int L, int V>
+    int run() const {
+        if constexpr (V * L * (16 / (int)sizeof(T)) > MAX_D) {
+            return ep::fail(a.ctx, EP_ERR_UNSUPPORTED, "rows of %d columns are not supported", a.d);
+        } else {
+            norm_rows<T, O, L, V, NORM><<<grid_for<L>(a.ctx, a.rows), block_threads<L>(), 0, a.stream>>>(
+                (const T *)a.x, (const T *)a.residual, a.weight, a.weight_type, a.rows, a.d, a.eps, (O *)a.out, a.scale,
+                (T *)a.hidden, a.vec);
+            EP_CUDA(a.ctx, cudaGetLastError());
+            return EP_OK;
+        }
+    }
+};
+
+template <typename T, typename O, bool NORM>
+int launch_norm(const NormArgs &a) {
+    return with_layout(ep::ceil_div(a.d, 16 / (int)sizeof(T)), NormLaunch<T, O, NORM>{a});
+}
+
+template <typename T>
+int launch_norm_out(const NormArgs &a, int out_type) {
+    if constexpr (sizeof(T) == 4) {
+        if (out_type == EP_BF16) return launch_norm<T, __nv_bfloat16, true>(a);
+        if (out_type == EP_F16) return launch_norm<T, __half, true>(a);
+    }
+    if (out_type == EP_E4M3) return launch_norm<T, e4m3, true>(a);
+    return launch_norm<T, T, true>(a);
+}
+
+struct BackArgs {
+    ep_ctx *ctx;
+    const void *dout, *hidden, *weight;
+    int weight_type;
+    const void *dhidden;
+    int64_t rows;
+    int d;
+    float eps;
+    void *dx;
+    float *dweight, *parts;
+    bool vec;
+    cudaStream_t stream;
+    int kernels;
+};
+
+template <typename T, typename D>
+struct BackLaunch {
+    BackArgs &a;
+    template <int L, int V>
+    int run() const {
+        if constexpr (V * L * (16 / (int)sizeof(T)) > MAX_D) {
+            return ep::fail(a.ctx, EP_ERR_UNSUPPORTED, "rows of %d columns are not supported", a.d);
+        } else {
+            constexpr int threads = block_threads<L>();
+            constexpr size_t smem = threads == L ? 0 : sizeof(float) * (threads / L) * V * L * (16 / sizeof(T));
+            const int grid = grid_for<L>(a.ctx, a.rows);
+            float *part = !a.dweight ? nullptr : grid == 1 ? a.dweight : a.parts;
+            norm_rows_backward<T, D, L, V><<<grid, threads, smem, a.stream>>>(
+                (const D *)a.dout, (const T *)a.hidden, a.weight, a.weight_type, (const T *)a.dhidden, a.rows, a.d, a.eps,
+                (T *)a.dx, part, a.vec);
+            EP_CUDA(a.ctx, cudaGetLastError());
+            a.kernels = 1;
+            if (part && grid > 1) {
+                a.kernels = 2;
+                return ep::sum_partials(a.ctx, a.parts, grid, a.d, a.dweight, a.stream);
+            }
+            return EP_OK;
+        }
+    }
+};
+
+template <typename T, typename D>
+int launch_backward(BackArgs &a) {
+    return with_layout(ep::ceil_div(a.d, 16 / (int)sizeof(T)), BackLaunch<T, D>{a});
+}
+
+}  // namespace
+
+namespace ep {
+
+int sum_partials(ep_ctx *ctx, const float *parts, int n, int cols, float *out, cudaStream_t stream) {
+    fold_partials<<<(unsigned)ceil_div(cols, 32), 256, 0, stream>>>(parts, n, cols, out);
+    EP_CUDA(ctx, cudaGetLastError());
+    return EP_OK;
+}
+
+}  // namespace ep
+
+using namespace ep;
+
+namespace {
+
+bool norm_shape_ok(int64_t rows, int d) { return rows >= 0 && rows < (1ll << 31) && d >= 1 && d <= MAX_D; }
+bool element_aligned(const void *p, int type) { return !p || aligned(p, (size_t)type_size(type)); }
+bool all16(std::initializer_list<const void *> ps) {
+    for (const void *p : ps)
+        if (!aligned(p, 16)) return false;
+    return true;
+}
+
+int norm_call(ep_ctx *ctx, bool norm, const void *x, int x_type, const void *residual, const void *weight, int weight_type,
+              int64_t rows, int d, float eps, void *out, int out_type, float *scale, void *hidden, cudaStream_t stream) {
+    NormArgs a{ctx, x, residual, weight, weight_type, rows, d, eps, out, scale, hidden, false, stream};
+    a.vec = d % (16 / type_size(x_type)) == 0 && all16({x, residual, out, hidden});
+    DeviceGuard guard(ctx->device);
+    Timed tm(ctx, stream, EP_TIMER_NORM);
+    int rc;
+    if (!norm)
+        rc = x_type == EP_F32    ? launch_norm<float, e4m3, false>(a)
+             : x_type == EP_BF16 ? launch_norm<__nv_bfloat16, e4m3, false>(a)
+                                 : launch_norm<__half, e4m3, false>(a);
+    else
+        rc = x_type == EP_F32    ? launch_norm_out<float>(a, out_type)
+             : x_type == EP_BF16 ? launch_norm_out<__nv_bfloat16>(a, out_type)
+                                 : launch_norm_out<__half>(a, out_type);
+    tm.end(rc == EP_OK ? 1 : 0);
+    return rc;
+}
+
+}  // namespace
+
+extern "C" {
+
+int ep_rms_norm(ep_ctx *ctx, const void *x, int32_t x_type, const void *residual, const void *weight,
+                int32_t weight_type, int64_t rows, int32_t d, float eps, void *out, int32_t out_type, float *scale,
+                void *hidden, void *cuda_stream) {
+    if (!ctx) return EP_ERR_INVALID_ARG;
+    if (!norm_shape_ok(rows, d)) return fail(ctx, EP_ERR_INVALID_ARG, "rows %lld or d %d out of range", (long long)rows, d);
+    if (!float_type(x_type) || (weight && !float_type(weight_type)) ||
+        !(out_type == x_type || out_type == EP_E4M3 || (x_type == EP_F32 && float_type(out_type))))
+        return fail(ctx, EP_ERR_INVALID_ARG, "no norm from type %d to type %d", x_type, out_type);
+    if (!(eps >= 0.f) || eps > 3e38f) return fail(ctx, EP_ERR_INVALID_ARG, "eps must be finite and not negative");
+    if (rows == 0) return EP_OK;
+    if ((out_type == EP_E4M3) != (scale != nullptr))
+        return fail(ctx, EP_ERR_INVALID_ARG, "scale goes with an 8-bit output, and with no other");
+    if (!x || !out || !element_aligned(x, x_type) || !element_aligned(residual, x_type) || !element_aligned(out, out_type) ||
+        !element_aligned(hidden, x_type) || !element_aligned(weight, weight ? weight_type : EP_E4M3) || !aligned(scale, 4))
+        return fail(ctx, EP_ERR_INVALID_ARG, "null or misaligned pointer");
+    return norm_call(ctx, true, x, x_type, residual, weight, weight_type, rows, d, eps, out, out_type, scale, hidden,
+                     static_cast<cudaStream_t>(cuda_stream));
+}
+
+int ep_quantize_rows(ep_ctx *ctx, const void *x, int32_t x_type, int64_t rows, int32_t d, void *q, float *scale,
+                     void *cuda_stream) {
+    if (!ctx) return EP_ERR_INVALID_ARG;
+    if (!norm_shape_ok(rows, d)) return fail(ctx, EP_ERR_INVALID_ARG, "rows %lld or d %d out of range", (long long)rows, d);
+    if (!float_type(x_type)) return fail(ctx, EP_ERR_INVALID_ARG, "rows of type %d cannot be brought to 8 bits", x_type);
+    if (rows == 0) return EP_OK;
+    if (!x || !q || !scale || !element_aligned(x, x_type) || !aligned(scale, 4))
+        return fail(ctx, EP_ERR_INVALID_ARG, "null or misaligned pointer");
+    return norm_call(ctx, false, x, x_type, nullptr, nullptr, EP_F32, rows, d, 0.f, q, EP_E4M3, scale, nullptr,
+                     static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t ep_rms_norm_backward_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t d) {
+    if (!ctx || !norm_shape_ok(rows, d)) return 0;
+    Arena a(nullptr);
+    a.take<float>((size_t)ctx->sm_count * BLOCKS_PER_SM * d);
+    return a.used;
+}
+
+int ep_rms_norm_backward(ep_ctx *ctx, const void *dout, int32_t dout_type, const void *hidden, int32_t h_type,
+                         const void *weight, int32_t weight_type, const void *dhidden, int64_t rows, int32_t d, float eps,
+                         void *dx, float *dweight, void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    if (!ctx) return EP_ERR_INVALID_ARG;
+    if (!norm_shape_ok(rows, d)) return fail(ctx, EP_ERR_INVALID_ARG, "rows %lld or d %d out of range", (long long)rows, d);
+    if (!float_type(h_type) || (weight && !float_type(weight_type)) ||
+        !(dout_type == h_type || (h_type == EP_F32 && float_type(dout_type))))
+        return fail(ctx, EP_ERR_INVALID_ARG, "no norm gradient from type %d to type %d", dout_type, h_type);
+    if (!(eps >= 0.f) || eps > 3e38f) return fail(ctx, EP_ERR_INVALID_ARG, "eps must be finite and not negative");
+    if (!aligned(dweight, 4)) return fail(ctx, EP_ERR_INVALID_ARG, "misaligned pointer");
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    DeviceGuard guard(ctx->device);
+    if (rows == 0) {
+        if (dweight) EP_CUDA(ctx, cudaMemsetAsync(dweight, 0, sizeof(float) * (size_t)d, stream));
+        return EP_OK;
+    }
+    if (!dout || !hidden || !dx || !element_aligned(dout, dout_type) || !element_aligned(hidden, h_type) ||
+        !element_aligned(dhidden, h_type) || !element_aligned(dx, h_type) ||
+        !element_aligned(weight, weight ? weight_type : EP_E4M3))
+        return fail(ctx, EP_ERR_INVALID_ARG, "null or misaligned pointer");
+    if (dweight && (!workspace || !aligned(workspace, 256) ||
+                    workspace_bytes < ep_rms_norm_backward_workspace_bytes(ctx, rows, d)))
+        return fail(ctx, EP_ERR_WORKSPACE, "workspace too small or misaligned");
+    BackArgs a{ctx, dout, hidden, weight, weight_type, dhidden, rows, d, eps, dx, dweight, static_cast<float *>(workspace),
+               false, stream, 0};
+    a.vec = d % (16 / type_size(h_type)) == 0 && all16({dout, hidden, dhidden, dx});
+    Timed tm(ctx, stream, EP_TIMER_NORM);
+    int rc;
+    if (h_type == EP_BF16)
+        rc = launch_backward<__nv_bfloat16, __nv_bfloat16>(a);
+    else if (h_type == EP_F16)
+        rc = launch_backward<__half, __half>(a);
+    else if (dout_type == EP_BF16)
+        rc = launch_backward<float, __nv_bfloat16>(a);
+    else if (dout_type == EP_F16)
+        rc = launch_backward<float, __half>(a);
+    else
+        rc = launch_backward<float, float>(a);
+    tm.end(rc == EP_OK ? a.kernels : 0);
+    return rc;
+}
+
+}  // extern "C"

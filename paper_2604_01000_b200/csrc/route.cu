@@ -1,0 +1,534 @@
+// Routing of rows to parts: softmax, the k largest, counts per part and the balance loss in one pass over the logits;
+// and its gradient, again in one pass.
+//
+// A row stays in the registers of the L threads that share it.  A thread holds the same columns of every row that it
+// meets, so the sums over rows (of the probabilities) stay in its registers too until the block ends; counts are
+// integers in shared memory.  Blocks leave their sums in the workspace and a second, small kernel adds them in a fixed
+// order.  One block (few rows) needs neither: it writes the results itself.
+#include "ep_common.cuh"
+#include "rows.cuh"
+
+#include <algorithm>
+
+using namespace eprow;
+
+namespace {
+
+constexpr int MAX_PARTS = 4096;
+constexpr int MAX_K = 32;
+constexpr int BLOCKS_PER_SM = 4;
+constexpr int THREADS = 256;
+
+// The better of two (logit, column) pairs: the larger logit, of equal ones the lower column.
+__device__ __forceinline__ void keep_better(float &v, int &c, float ov, int oc) {
+    const bool take = ov > v || (ov == v && oc < c);
+    v = take ? ov : v;
+    c = take ? oc : c;
+}
+
+// The best pair over the L threads of a row.  L > 32: the whole block, by shared memory (2 x 8 pairs used in turn).
+template <int L>
+__device__ __forceinline__ void best_of_row(float &v, int &c, float *slot_v, int *slot_c, int &turn) {
+    constexpr int W = L < 32 ? L : 32;
+#pragma unroll
+    for (int o = W / 2; o >= 1; o >>= 1) {
+        const float ov = __shfl_xor_sync(FULL, v, o);
+        const int oc = __shfl_xor_sync(FULL, c, o);
+        keep_better(v, c, ov, oc);
+    }
+    if constexpr (L > 32) {
+        float *sv = slot_v + turn * 8;
+        int *sc = slot_c + turn * 8;
+        turn ^= 1;
+        if ((threadIdx.x & 31) == 0) {
+            sv[threadIdx.x >> 5] = v;
+            sc[threadIdx.x >> 5] = c;
+        }
+        __syncthreads();
+        v = sv[0];
+        c = sc[0];
+#pragma unroll
+        for (int w = 1; w < L / 32; ++w) keep_better(v, c, sv[w], sc[w]);
+    }
+}
+
+struct Finish {   // what the last step needs to turn sums into results
+    int parts, k;
+    int64_t *counts, *routed;
+    float *prob, *loss;
+};
+
+// prob, loss and routed from the sums over all rows: one block.  counts[] and prob[] (as sums) are already there.
+__device__ void finish_block(const Finish &f, int64_t rows_routed, double *red) {
+    const double rows = rows_routed > 0 ? (double)rows_routed : 1.0;
+    double t = 0.0;
+    for (int e = threadIdx.x; e < f.parts; e += blockDim.x) {
+        const float p = (float)((double)f.prob[e] / rows);
+        f.prob[e] = p;
+        t += (double)f.counts[e] * (double)p;
+    }
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) t += __shfl_xor_sync(FULL, t, o);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = t;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        t = red[0];
+        for (int w = 1; w < (int)(blockDim.x >> 5); ++w) t += red[w];
+        *f.loss = (float)(t * (double)f.parts / ((double)f.k * rows));
+        *f.routed = rows_routed;
+    }
+}
+
+template <typename T, int L, int V>
+__global__ void __launch_bounds__(THREADS) route_rows(const T *__restrict__ logits, int64_t rows, int parts, int k,
+                                                      const uint8_t *__restrict__ valid, bool renormalize,
+                                                      int32_t *__restrict__ ids, float *weights,
+                                                      float *__restrict__ part_prob, int *__restrict__ part_count, Finish fin,
+                                                      bool vec) {
+    constexpr int N = 16 / (int)sizeof(T);
+    constexpr int GROUPS = THREADS / L;
+    constexpr int WIDE = V * L * N;
+    __shared__ float slots[L > 32 ? 64 : 1];
+    __shared__ float slot_v[L > 32 ? 16 : 1];
+    __shared__ int slot_c[L > 32 ? 16 : 1];
+    __shared__ double red[8];
+    extern __shared__ int hist[];   // counts of [parts + 1] (the last: rows that take part), then the fold of the sums
+    int turn = 0, turn_best = 0;
+    const int lane = threadIdx.x % L, group = threadIdx.x / L;
+    for (int e = threadIdx.x; e <= parts; e += THREADS) hist[e] = 0;
+    __syncthreads();
+    float sum_p[V][N];
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum_p[j][i] = 0.f;
+
+    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += (int64_t)gridDim.x * GROUPS) {
+        const int64_t row = first + group;
+        const bool mine = row < rows;
+        const bool read = mine && (!valid || valid[row]);
+        const int width = read ? parts : 0;
+        const T *from = logits + (read ? row * parts : 0);
+        float l[V][N];
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            load_chunk(from, (j * L + lane) * N, width, vec, -INFINITY, l[j]);
+#pragma unroll
+            for (int i = 0; i < N; ++i) top = fmaxf(top, l[j][i]);
+        }
+        top = reduce_row<L, OpMaxNumber>(top, slots, turn);
+        const bool part = top > -INFINITY;   // false for a row of NaN and -infinity alone, too
+        float s = 0.f;
+        float e[V][N];
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                e[j][i] = part ? __expf(l[j][i] - top) : 0.f;
+                s += e[j][i];
+            }
+        s = reduce_row<L, OpSum>(s, slots, turn);
+        const float inverse = part ? 1.f / s : 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum_p[j][i] = fmaf(e[j][i], inverse, sum_p[j][i]);
+        if (lane == 0 && part) atomicAdd(&hist[parts], 1);
+
+        // the k largest, one after the other: each thread offers the best of its columns that is left
+        float chosen_sum = 0.f, my_w = 0.f;
+        for (int r = 0; r < k; ++r) {
+            float v = -INFINITY;
+            int c = MAX_PARTS;
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (l[j][i] > v) {
+                        v = l[j][i];
+                        c = (j * L + lane) * N + i;
+                    }
+            best_of_row<L>(v, c, slot_v, slot_c, turn_best);
+            const bool got = v > -INFINITY;
+            const float w = got ? __expf(v - top) * inverse : 0.f;
+            chosen_sum += w;
+            if (lane == r % L) {
+                if (mine) {
+                    ids[row * k + r] = got ? c : -1;
+                    if (!renormalize || r >= L) weights[row * k + r] = w;
+                }
+                if (r < L) my_w = w;
+                if (got) atomicAdd(&hist[c], 1);
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if ((j * L + lane) * N + i == c) l[j][i] = -INFINITY;
+        }
+        if (renormalize && mine) {
+            const float scale = part ? 1.f / chosen_sum : 0.f;
+            if (lane < k) weights[row * k + lane] = my_w * scale;
+            for (int r = lane + L; r < k; r += L) weights[row * k + r] *= scale;   // this thread's own earlier stores
+        }
+    }
+
+    // the block's sums: over its groups in order, then to the workspace or, alone, to the results
+    __syncthreads();
+    float *fold = reinterpret_cast<float *>(hist + ((parts + 1 + 3) & ~3));
+    const bool alone = gridDim.x == 1;
+    float *prob_to = alone ? fin.prob : part_prob + (size_t)blockIdx.x * parts;
+    if constexpr (GROUPS > 1) {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) fold[group * WIDE + (j * L + lane) * N + i] = sum_p[j][i];
+        __syncthreads();
+        for (int c = threadIdx.x; c < parts; c += THREADS) {
+            float t = 0.f;
+#pragma unroll 4
+            for (int q = 0; q < GROUPS; ++q) t += fold[q * WIDE + c];
+            prob_to[c] = t;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int c = (j * L + lane) * N + i;
+                if (c < parts) prob_to[c] = sum_p[j][i];
+            }
+    }
+    if (alone) {
+        for (int c = threadIdx.x; c < parts; c += THREADS) fin.counts[c] = hist[c];
+        __syncthreads();
+        finish_block(fin, hist[parts], red);
+    } else {
+        int *count_to = part_count + (size_t)blockIdx.x * (parts + 1);
+        for (int c = threadIdx.x; c <= parts; c += THREADS) count_to[c] = hist[c];
+    }
+}
+
+// counts[c] and prob[c] (still a sum) over the blocks' shares; column `parts` is the number of rows that took part.
+__global__ void __launch_bounds__(256) route_fold(const float *__restrict__ part_prob, const int *__restrict__ part_count, int n,
+                                                  Finish f) {
+    __shared__ double sp[8][32];
+    __shared__ long long sc[8][32];
+    const int lane = threadIdx.x & 31, r0 = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    double p = 0.0;
+    long long m = 0;
+#pragma unroll 4
+    for (int r = r0; r < n; r += 8) {
+        if (c < f.parts) p += (double)part_prob[(size_t)r * f.parts + c];
+        if (c <= f.parts) m += part_count[(size_t)r * (f.parts + 1) + c];
+    }
+    sp[r0][lane] = p;
+    sc[r0][lane] = m;
+    __syncthreads();
+    if (r0 == 0) {
+#pragma unroll
+        for (int q = 1; q < 8; ++q) {
+            p += sp[q][lane];
+            m += sc[q][lane];
+        }
+        if (c < f.parts) {
+            f.prob[c] = (float)p;
+            f.counts[c] = m;
+        } else if (c == f.parts)
+            *f.routed = m;
+    }
+}
+
+__global__ void __launch_bounds__(1024) route_finish(Finish f) {
+    __shared__ double red[32];
+    finish_block(f, *f.routed, red);
+}
+
+template <typename T, int L, int V>
+__global__ void __launch_bounds__(THREADS) route_rows_backward(const T *__restrict__ logits, int64_t rows, int parts, int k,
+                                                               const uint8_t *__restrict__ valid, bool renormalize,
+                                                               const int32_t *__restrict__ ids,
+                                                               const int64_t *__restrict__ counts,
+                                                               const int64_t *__restrict__ routed,
+                                                               const float *__restrict__ dweights,
+                                                               const float *__restrict__ dloss, T *__restrict__ dlogits,
+                                                               int *status, bool vec) {
+    constexpr int N = 16 / (int)sizeof(T);
+    constexpr int GROUPS = THREADS / L;
+    __shared__ float slots[L > 32 ? 64 : 1];
+    int turn = 0;
+    const int lane = threadIdx.x % L, group = threadIdx.x / L;
+    float slope[V][N];   // d loss / d p of this thread's columns, the same for every row
+    {
+        const double r = (double)max((long long)*routed, 1ll);
+        const float unit = dloss ? (float)((double)*dloss * (double)parts / ((double)k * r * r)) : 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int c = (j * L + lane) * N + i;
+                slope[j][i] = dloss && c < parts ? unit * (float)counts[c] : 0.f;
+            }
+    }
+    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += (int64_t)gridDim.x * GROUPS) {
+        const int64_t row = first + group;
+        const bool mine = row < rows;
+        const bool read = mine && (!valid || valid[row]);
+        const T *from = logits + (read ? row * parts : 0);
+        float p[V][N];
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            load_chunk(from, (j * L + lane) * N, read ? parts : 0, vec, -INFINITY, p[j]);
+#pragma unroll
+            for (int i = 0; i < N; ++i) top = fmaxf(top, p[j][i]);
+        }
+        top = reduce_row<L, OpMaxNumber>(top, slots, turn);
+        const bool part = top > -INFINITY;
+        float s = 0.f, dot = 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                p[j][i] = part ? __expf(p[j][i] - top) : 0.f;
+                s += p[j][i];
+                dot = fmaf(p[j][i], slope[j][i], dot);
+            }
+        s = reduce_row<L, OpSum>(s, slots, turn);
+        dot = reduce_row<L, OpSum>(dot, slots, turn);
+        const float inverse = part ? 1.f / s : 0.f;
+        dot *= inverse;
+        // the slots: every thread of the row goes over all of them (the reads are broadcasts)
+        const bool weighted = dweights && part;
+        float chosen = 0.f, pulled = 0.f;   // sum of p, and of dweights p, over the slots
+        if (weighted)
+            for (int q = 0; q < k; ++q) {
+                const int id = ids[row * k + q];
+                if (id < 0 || id >= parts) {
+                    if (id != -1 && lane == 0) ep_raise(status, EP_ERR_BAD_INDEX);
+                    continue;
+                }
+                const float w = __expf(to_f32(from[id]) - top) * inverse;
+                chosen += w;
+                pulled = fmaf(dweights[row * k + q], w, pulled);
+            }
+        // with renormalised weights the slots' own terms of sum_e p_e dp_e cancel
+        const float back = renormalize ? dot : dot + pulled;
+        const float mean = renormalize && weighted ? pulled / chosen : 0.f;
+        const float per = renormalize && weighted ? 1.f / chosen : 1.f;
+        float extra[V][N];
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) extra[j][i] = slope[j][i];
+        if (weighted)
+            for (int q = 0; q < k; ++q) {
+                const int id = ids[row * k + q];
+                if (id < 0 || id >= parts || (id / N) % L != lane) continue;
+                const float dp = (dweights[row * k + q] - mean) * per;
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        if ((j * L + lane) * N + i == id) extra[j][i] += dp;
+            }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float o[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) o[i] = part ? p[j][i] * inverse * (extra[j][i] - back) : 0.f;
+            store_chunk(dlogits + (mine ? row * parts : 0), (j * L + lane) * N, mine ? parts : 0, vec, o);
+        }
+    }
+}
+
+// The fewest threads and chunks per thread that hold a row of `chunks` 16-byte chunks.
+template <typename F>
+int with_layout(int64_t chunks, F f) {
+    if (chunks <= 1) return f.template run<1, 1>();
+    if (chunks <= 2) return f.template run<2, 1>();
+    if (chunks <= 4) return f.template run<4, 1>();
+    if (chunks <= 8) return f.template run<8, 1>();
+    if (chunks <= 16) return f.template run<16, 1>();
+    if (chunks <= 32) return f.template run<32, 1>();
+    if (chunks <= 64) return f.template run<32, 2>();
+    if (chunks <= 128) return f.template run<32, 4>();
+    if (chunks <= 256) return f.template run<256, 1>();
+    if (chunks <= 512) return f.template run<256, 2>();
+    return f.template run<256, 4>();
+}
+
+int grid_for(const ep_ctx *ctx, int64_t rows, int groups) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(rows, groups), (int64_t)ctx->sm_count * BLOCKS_PER_SM));
+}
+
+struct RouteArgs {
+    ep_ctx *ctx;
+    const void *logits;
+    int64_t rows;
+    int parts, k;
+    const uint8_t *valid;
+    bool renormalize;
+    int32_t *ids;
+    float *weights;
+    float *part_prob;
+    int *part_count;
+    Finish fin;
+    bool vec;
+    cudaStream_t stream;
+    int kernels;
+};
+
+template <typename T>
+struct RouteLaunch {
+    RouteArgs &a;
+    template <int L, int V>
+    int run() const {
+        constexpr int n = 16 / (int)sizeof(T);
+        if constexpr (V > 1 && V * L / 2 * n >= MAX_PARTS) {   // a narrower layout holds every row
+            return ep::fail(a.ctx, EP_ERR_UNSUPPORTED, "%d parts are not supported", a.parts);
+        } else {
+            constexpr int groups = THREADS / L;
+            const size_t smem = sizeof(int) * (size_t)((a.parts + 1 + 3) & ~3) + (groups > 1 ? sizeof(float) * groups * V * L * n : 0);
+            const int grid = grid_for(a.ctx, a.rows, groups);
+            route_rows<T, L, V><<<grid, THREADS, smem, a.stream>>>((const T *)a.logits, a.rows, a.parts, a.k, a.valid,
+                                                                   a.renormalize, a.ids, a.weights, a.part_prob, a.part_count,
+                                                                   a.fin, a.vec);
+            EP_CUDA(a.ctx, cudaGetLastError());
+            a.kernels = 1;
+            if (grid > 1) {
+                route_fold<<<a.parts / 32 + 1, 256, 0, a.stream>>>(a.part_prob, a.part_count, grid, a.fin);
+                EP_CUDA(a.ctx, cudaGetLastError());
+                route_finish<<<1, 1024, 0, a.stream>>>(a.fin);
+                EP_CUDA(a.ctx, cudaGetLastError());
+                a.kernels = 3;
+            }
+            return EP_OK;
+        }
+    }
+};
+
+struct RouteBackArgs {
+    ep_ctx *ctx;
+    const void *logits;
+    int64_t rows;
+    int parts, k;
+    const uint8_t *valid;
+    bool renormalize;
+    const int32_t *ids;
+    const int64_t *counts, *routed;
+    const float *dweights, *dloss;
+    void *dlogits;
+    bool vec;
+    cudaStream_t stream;
+};
+
+template <typename T>
+struct RouteBackLaunch {
+    const RouteBackArgs &a;
+    template <int L, int V>
+    int run() const {
+        if constexpr (V > 1 && V * L / 2 * (16 / (int)sizeof(T)) >= MAX_PARTS) {   // a narrower layout holds every row
+            return ep::fail(a.ctx, EP_ERR_UNSUPPORTED, "%d parts are not supported", a.parts);
+        } else {
+            route_rows_backward<T, L, V><<<grid_for(a.ctx, a.rows, THREADS / L), THREADS, 0, a.stream>>>(
+                (const T *)a.logits, a.rows, a.parts, a.k, a.valid, a.renormalize, a.ids, a.counts, a.routed, a.dweights, a.dloss,
+                (T *)a.dlogits, a.ctx->d_status, a.vec);
+            EP_CUDA(a.ctx, cudaGetLastError());
+            return EP_OK;
+        }
+    }
+};
+
+bool route_shape_ok(int64_t rows, int parts) { return rows >= 0 && rows < (1ll << 31) && parts >= 1 && parts <= MAX_PARTS; }
+
+struct RouteWorkspace {
+    float *prob;
+    int *count;
+    size_t bytes;
+};
+
+RouteWorkspace route_workspace(const ep_ctx *ctx, int parts, void *p) {
+    ep::Arena a(p);
+    RouteWorkspace w{};
+    const size_t blocks = (size_t)ctx->sm_count * BLOCKS_PER_SM;
+    w.prob = a.take<float>(blocks * parts);
+    w.count = a.take<int>(blocks * (parts + 1));
+    w.bytes = a.used;
+    return w;
+}
+
+}  // namespace
+
+using namespace ep;
+
+extern "C" {
+
+size_t ep_route_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t parts) {
+    if (!ctx || !route_shape_ok(rows, parts)) return 0;
+    return route_workspace(ctx, parts, nullptr).bytes;
+}
+
+int ep_route(ep_ctx *ctx, const void *logits, int32_t type, int64_t rows, int32_t parts, int32_t k, const uint8_t *valid,
+             int32_t renormalize, int32_t *ids, float *weights, int64_t *counts, float *prob, float *loss, int64_t *routed,
+             void *workspace, size_t workspace_bytes, void *cuda_stream) {
+    if (!ctx) return EP_ERR_INVALID_ARG;
+    if (!route_shape_ok(rows, parts))
+        return fail(ctx, EP_ERR_INVALID_ARG, "rows %lld or parts %d out of range", (long long)rows, parts);
+    if (k < 1 || k > std::min(parts, MAX_K)) return fail(ctx, EP_ERR_INVALID_ARG, "k %d out of range for %d parts", k, parts);
+    if (!float_type(type)) return fail(ctx, EP_ERR_INVALID_ARG, "logits of type %d are not supported", type);
+    if (!counts || !prob || !loss || !routed || !aligned(counts, 8) || !aligned(prob, 4) || !aligned(loss, 4) || !aligned(routed, 8))
+        return fail(ctx, EP_ERR_INVALID_ARG, "null or misaligned pointer");
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    DeviceGuard guard(ctx->device);
+    if (rows == 0) {
+        EP_CUDA(ctx, cudaMemsetAsync(counts, 0, sizeof(int64_t) * (size_t)parts, stream));
+        EP_CUDA(ctx, cudaMemsetAsync(prob, 0, sizeof(float) * (size_t)parts, stream));
+        EP_CUDA(ctx, cudaMemsetAsync(loss, 0, sizeof(float), stream));
+        EP_CUDA(ctx, cudaMemsetAsync(routed, 0, sizeof(int64_t), stream));
+        return EP_OK;
+    }
+    if (!logits || !ids || !weights || !aligned(logits, type_size(type)) || !aligned(ids, 4) || !aligned(weights, 4))
+        return fail(ctx, EP_ERR_INVALID_ARG, "null or misaligned pointer");
+    const RouteWorkspace w = route_workspace(ctx, parts, workspace);
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < w.bytes)
+        return fail(ctx, EP_ERR_WORKSPACE, "workspace too small or misaligned");
+    RouteArgs a{ctx, logits, rows, parts, k, valid, renormalize != 0, ids, weights, w.prob, w.count,
+                Finish{parts, k, counts, routed, prob, loss}, parts % (16 / type_size(type)) == 0 && aligned(logits, 16), stream, 0};
+    Timed tm(ctx, stream, EP_TIMER_ROUTE);
+    const int64_t chunks = ceil_div(parts, 16 / type_size(type));
+    const int rc = type == EP_F32    ? with_layout(chunks, RouteLaunch<float>{a})
+                   : type == EP_BF16 ? with_layout(chunks, RouteLaunch<__nv_bfloat16>{a})
+                                     : with_layout(chunks, RouteLaunch<__half>{a});
+    tm.end(a.kernels);
+    return rc;
+}
+
+int ep_route_backward(ep_ctx *ctx, const void *logits, int32_t type, int64_t rows, int32_t parts, int32_t k,
+                      const uint8_t *valid, int32_t renormalize, const int32_t *ids, const int64_t *counts,
+                      const int64_t *routed, const float *dweights, const float *dloss, void *dlogits, void *cuda_stream) {
+    if (!ctx) return EP_ERR_INVALID_ARG;
+    if (!route_shape_ok(rows, parts))
+        return fail(ctx, EP_ERR_INVALID_ARG, "rows %lld or parts %d out of range", (long long)rows, parts);
+    if (k < 1 || k > std::min(parts, MAX_K)) return fail(ctx, EP_ERR_INVALID_ARG, "k %d out of range for %d parts", k, parts);
+    if (!float_type(type)) return fail(ctx, EP_ERR_INVALID_ARG, "logits of type %d are not supported", type);
+    if (rows == 0) return EP_OK;
+    if (!logits || !ids || !counts || !routed || !dlogits || !aligned(logits, type_size(type)) || !aligned(ids, 4) ||
+        !aligned(counts, 8) || !aligned(routed, 8) || !aligned(dweights, 4) || !aligned(dloss, 4) ||
+        !aligned(dlogits, type_size(type)))
+        return fail(ctx, EP_ERR_INVALID_ARG, "null or misaligned pointer");
+    RouteBackArgs a{ctx, logits, rows, parts, k, valid, renormalize != 0, ids, counts, routed, dweights, dloss, dlogits,
+                    parts % (16 / type_size(type)) == 0 && aligned(logits, 16) && aligned(dlogits, 16),
+                    static_cast<cudaStream_t>(cuda_stream)};
+    DeviceGuard guard(ctx->device);
+    Timed tm(ctx, a.stream, EP_TIMER_ROUTE);
+    const int64_t chunks = ceil_div(parts, 16 / type_size(type));
+    const int rc = type == EP_F32    ? with_layout(chunks, RouteBackLaunch<float>{a})
+                   : type == EP_BF16 ? with_layout(chunks, RouteBackLaunch<__nv_bfloat16>{a})
+                                     : with_layout(chunks, RouteBackLaunch<__half>{a});
+    tm.end(rc == EP_OK ? 1 : 0);
+    return rc;
+}
+
+}  // extern "C"

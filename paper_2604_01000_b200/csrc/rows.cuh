@@ -1,0 +1,146 @@
+// Device helpers of the row-wise kernels (norm.cu, route.cu) and of the products' epilogues (linear.cu): element
+// types, accesses of 16-byte chunks, and sums and maxima over the threads that share a row.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <math_constants.h>
+#include <stdint.h>
+
+#include "embedpart.h"
+
+namespace eprow {
+
+constexpr unsigned FULL = 0xffffffffu;
+
+struct e4m3 {
+    uint8_t bits;
+};
+
+__device__ __forceinline__ float to_f32(float v) { return v; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+__device__ __forceinline__ float to_f32(e4m3 v) {
+    return __half2float(__half(__nv_cvt_fp8_to_halfraw(v.bits, __NV_E4M3)));
+}
+
+// Every rounding is to nearest, ties to even; e4m3 saturates at 448 (its callers scale to that range first).
+template <typename T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+template <>
+__device__ __forceinline__ e4m3 from_f32<e4m3>(float v) {
+    e4m3 r;
+    r.bits = __nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3);
+    return r;
+}
+
+// One vector parameter (a norm's weight, a product's bias) of type EP_F32, EP_BF16 or EP_F16.
+__device__ __forceinline__ float load_param(const void *p, int type, int64_t i) {
+    if (type == EP_F32) return __ldg(static_cast<const float *>(p) + i);
+    if (type == EP_BF16) return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
+    return __half2float(static_cast<const __half *>(p)[i]);
+}
+
+template <int BYTES>
+struct Raw;
+template <>
+struct Raw<1> { using type = uint8_t; };
+template <>
+struct Raw<2> { using type = uint16_t; };
+template <>
+struct Raw<4> { using type = uint32_t; };
+template <>
+struct Raw<8> { using type = uint2; };
+template <>
+struct Raw<16> { using type = uint4; };
+template <>
+struct Raw<32> { using type = uint4; };
+
+// N consecutive elements at column `col` of a row of `width` elements.  vec: the row starts on a boundary of the
+// whole access and width is a multiple of N, so the chunk is one access, all of it inside the row or none of it.
+// Elements past the row's end read as `fill`.
+template <int N, typename T>
+__device__ __forceinline__ void load_chunk(const T *row, int col, int width, bool vec, float fill, float (&v)[N]) {
+    if (vec) {
+        if (col < width) {
+            alignas(16) T e[N];
+            constexpr int B = N * (int)sizeof(T);
+            using R = typename Raw<B>::type;
+            constexpr int PIECES = B > 16 ? B / 16 : 1;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) reinterpret_cast<R *>(e)[i] = reinterpret_cast<const R *>(row + col)[i];
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = to_f32(e[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = fill;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = col + i < width ? to_f32(row[col + i]) : fill;
+    }
+}
+
+template <int N, typename T>
+__device__ __forceinline__ void store_chunk(T *row, int col, int width, bool vec, const float (&v)[N]) {
+    if (vec) {
+        if (col < width) {
+            alignas(16) T e[N];
+            constexpr int B = N * (int)sizeof(T);
+            using R = typename Raw<B>::type;
+            constexpr int PIECES = B > 16 ? B / 16 : 1;
+#pragma unroll
+            for (int i = 0; i < N; ++i) e[i] = from_f32<T>(v[i]);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) reinterpret_cast<R *>(row + col)[i] = reinterpret_cast<const R *>(e)[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (col + i < width) row[col + i] = from_f32<T>(v[i]);
+    }
+}
+
+// ---- sums and maxima over the L threads of a row -------------------------------------------------
+// L <= 32: neighbouring lanes of one warp (all 32 lanes of the warp call together).  L > 32: the whole block; `slots`
+// is then shared memory of 2 x 32 floats used in turn (`turn` flips with every call), one barrier per call.
+struct OpSum {
+    static __device__ __forceinline__ float apply(float a, float b) { return a + b; }
+    static constexpr float none = 0.f;
+};
+struct OpMax {   // NaN if either is: a row that holds one has no largest magnitude to scale by
+    static __device__ __forceinline__ float apply(float a, float b) { return (a > b || a != a) ? a : b; }
+    static constexpr float none = -INFINITY;
+};
+struct OpMaxNumber {   // NaN only if both are
+    static __device__ __forceinline__ float apply(float a, float b) { return fmaxf(a, b); }
+    static constexpr float none = -INFINITY;
+};
+
+template <int L, typename Op>
+__device__ __forceinline__ float reduce_row(float v, float *slots, int &turn) {
+    constexpr int W = L < 32 ? L : 32;
+#pragma unroll
+    for (int o = W / 2; o >= 1; o >>= 1) v = Op::apply(v, __shfl_xor_sync(FULL, v, o));
+    if constexpr (L > 32) {
+        float *s = slots + turn * 32;
+        turn ^= 1;
+        if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
+        __syncthreads();
+        float t = (threadIdx.x & 31) < L / 32 ? s[threadIdx.x & 31] : Op::none;
+#pragma unroll
+        for (int o = L / 64; o >= 1; o >>= 1) t = Op::apply(t, __shfl_xor_sync(FULL, t, o));
+        v = __shfl_sync(FULL, t, 0);
+    }
+    return v;
+}
+
+}  // namespace eprow
