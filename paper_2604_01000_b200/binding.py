@@ -205,28 +205,38 @@ def _check_cuda(t: torch.Tensor, dtype, name: str, device: torch.device) -> torc
 
 def _check_matrix(t: torch.Tensor, dtypes, name: str, device: torch.device, shape=None, strided: bool = False) -> torch.Tensor:
     """A 2-D CUDA tensor of one of `dtypes`, contiguous or (strided) with contiguous rows at any distance."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
+    if not isinstance(t, torch.Tensor) or t.get_device() != device.index:
         raise ValueError(f"{name} must be a CUDA tensor on {device}")
     if t.dtype not in dtypes:
         raise ValueError(f"{name} must have dtype {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
         raise ValueError(f"{name} must have shape {tuple(shape) if shape is not None else '(rows, columns)'}, not {tuple(t.shape)}")
-    if strided:
+    if not t.is_contiguous():
+        if not strided:
+            raise ValueError(f"{name} must be contiguous")
         if t.numel() and (t.stride(1) != 1 and t.shape[1] > 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]):
             raise ValueError(f"{name} must have contiguous rows that do not overlap")
-    elif not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
     return t
 
 
 def _check_vector(t: Optional[torch.Tensor], dtypes, name: str, device: torch.device, n: int) -> Optional[torch.Tensor]:
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
+    if not isinstance(t, torch.Tensor) or t.get_device() != device.index:
         raise ValueError(f"{name} must be a CUDA tensor on {device}")
     if t.dtype not in dtypes or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must be {n} contiguous values of {' or '.join(str(d) for d in dtypes)}")
     return t
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _context_of(t) -> "Context":
+    """The default context of a tensor's device (of the current one for anything else: the call then refuses it)."""
+    idx = t.get_device() if isinstance(t, torch.Tensor) else -1
+    return _default.get(idx) or default_context(idx if idx >= 0 else None)
 
 
 def _row_stride(t: torch.Tensor) -> int:
@@ -734,6 +744,9 @@ class Context:
             raise EmbedPartError(1, f"shape or type out of range: {what}")
         return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
 
+    def _raw_stream(self) -> int:
+        return torch._C._cuda_getCurrentRawStream(self.device.index)
+
     def _done(self, rc: int):
         if rc != EP_OK:
             self._raise(rc)
@@ -751,10 +764,9 @@ class Context:
         out = torch.empty(rows, d, dtype=out_dtype, device=self.device)
         scale = torch.empty(rows, dtype=torch.float32, device=self.device) if out_dtype == torch.float8_e4m3fn else None
         hidden = torch.empty_like(x) if residual is not None else None
-        with torch.cuda.device(self.device):
-            self._done(self._lib.ep_rms_norm(self._h, _dev_ptr(x), TYPES[x.dtype], _dev_ptr(residual), _dev_ptr(weight),
-                                             _type_of(weight), rows, d, eps, _dev_ptr(out), TYPES[out_dtype], _dev_ptr(scale),
-                                             _dev_ptr(hidden), self._stream()))
+        self._done(self._lib.ep_rms_norm(self._h, _ptr(x), TYPES[x.dtype], _ptr(residual), _ptr(weight),
+                                         _type_of(weight), rows, d, eps, _ptr(out), TYPES[out_dtype], _ptr(scale),
+                                         _ptr(hidden), self._raw_stream()))
         return NormResult(out, scale, x if hidden is None else hidden)
 
     def quantize_rows(self, x):
@@ -763,9 +775,8 @@ class Context:
         rows, d = x.shape
         q = torch.empty(rows, d, dtype=torch.float8_e4m3fn, device=self.device)
         scale = torch.empty(rows, dtype=torch.float32, device=self.device)
-        with torch.cuda.device(self.device):
-            self._done(self._lib.ep_quantize_rows(self._h, _dev_ptr(x), TYPES[x.dtype], rows, d, _dev_ptr(q), _dev_ptr(scale),
-                                                  self._stream()))
+        self._done(self._lib.ep_quantize_rows(self._h, _ptr(x), TYPES[x.dtype], rows, d, _ptr(q), _ptr(scale),
+                                              self._raw_stream()))
         return QuantizedRows(q, scale)
 
     def rms_norm_backward(self, dout, hidden, weight=None, eps: float = 1e-6, dhidden=None, need_dweight: bool = True):
@@ -779,11 +790,10 @@ class Context:
         ws = self._scratch(self._lib.ep_rms_norm_backward_workspace_bytes(self._h, rows, d), f"rows={rows} d={d}")
         dx = torch.empty_like(hidden)
         dweight = torch.empty(d, dtype=torch.float32, device=self.device) if need_dweight else None
-        with torch.cuda.device(self.device):
-            self._done(self._lib.ep_rms_norm_backward(
-                self._h, _dev_ptr(dout), TYPES[dout.dtype], _dev_ptr(hidden), TYPES[hidden.dtype], _dev_ptr(weight),
-                _type_of(weight), _dev_ptr(dhidden), rows, d, eps, _dev_ptr(dx), _dev_ptr(dweight), _dev_ptr(ws), ws.numel(),
-                self._stream()))
+        self._done(self._lib.ep_rms_norm_backward(
+            self._h, _ptr(dout), TYPES[dout.dtype], _ptr(hidden), TYPES[hidden.dtype], _ptr(weight),
+            _type_of(weight), _ptr(dhidden), rows, d, eps, _ptr(dx), _ptr(dweight), _ptr(ws), ws.numel(),
+            self._raw_stream()))
         return NormGradients(dx, dweight)
 
     def linear(self, x, weight, bias=None, activation: str = "none", residual=None, x_scale=None, weight_scale=None,
@@ -813,12 +823,11 @@ class Context:
                            f"rows={rows} n_in={n_in} n_out={n_out}")
         out = torch.empty(rows, n_out, dtype=out_dtype, device=self.device)
         z = torch.empty_like(out) if preact else None
-        with torch.cuda.device(self.device):
-            self._done(self._lib.ep_linear(
-                self._h, _dev_ptr(x), _row_stride(x), _dev_ptr(weight), _row_stride(weight), TYPES[x.dtype], _dev_ptr(x_scale),
-                _dev_ptr(weight_scale), _dev_ptr(bias), _type_of(bias), ACTIVATIONS[activation], _dev_ptr(residual),
-                0 if residual is None else _row_stride(residual), _dev_ptr(out), TYPES[out_dtype], _dev_ptr(z), rows, n_in, n_out,
-                _dev_ptr(ws), ws.numel(), self._stream()))
+        self._done(self._lib.ep_linear(
+            self._h, _ptr(x), _row_stride(x), _ptr(weight), _row_stride(weight), TYPES[x.dtype], _ptr(x_scale),
+            _ptr(weight_scale), _ptr(bias), _type_of(bias), ACTIVATIONS[activation], _ptr(residual),
+            0 if residual is None else _row_stride(residual), _ptr(out), TYPES[out_dtype], _ptr(z), rows, n_in, n_out,
+            _ptr(ws), ws.numel(), self._raw_stream()))
         return LinearResult(out, z)
 
     def linear_backward(self, dout, x, weight, preact=None, activation: str = "none", need_dx: bool = True,
@@ -845,11 +854,10 @@ class Context:
         dx = torch.empty(rows, n_in, dtype=x.dtype, device=self.device) if need_dx else None
         dweight = torch.empty(n_out, n_in, dtype=x.dtype, device=self.device) if need_dweight else None
         dbias = torch.empty(n_out, dtype=torch.float32, device=self.device) if need_dbias else None
-        with torch.cuda.device(self.device):
-            self._done(self._lib.ep_linear_backward(
-                self._h, _dev_ptr(dout), TYPES[dout.dtype], _dev_ptr(preact), ACTIVATIONS[activation], _dev_ptr(x),
-                _row_stride(x), _dev_ptr(weight), _row_stride(weight), TYPES[x.dtype], rows, n_in, n_out, _dev_ptr(dx),
-                _dev_ptr(dweight), _dev_ptr(dbias), _dev_ptr(ws), ws.numel(), self._stream()))
+        self._done(self._lib.ep_linear_backward(
+            self._h, _ptr(dout), TYPES[dout.dtype], _ptr(preact), ACTIVATIONS[activation], _ptr(x),
+            _row_stride(x), _ptr(weight), _row_stride(weight), TYPES[x.dtype], rows, n_in, n_out, _ptr(dx),
+            _ptr(dweight), _ptr(dbias), _ptr(ws), ws.numel(), self._raw_stream()))
         return LinearGradients(dx, dweight, dbias)
 
     def route(self, logits, k: int = 1, valid=None, renormalize: bool = False):
@@ -866,11 +874,10 @@ class Context:
         prob = torch.empty(parts, dtype=torch.float32, device=self.device)
         loss = torch.empty(1, dtype=torch.float32, device=self.device)
         routed = torch.empty(1, dtype=torch.int64, device=self.device)
-        with torch.cuda.device(self.device):
-            self._done(self._lib.ep_route(
-                self._h, _dev_ptr(logits), TYPES[logits.dtype], rows, parts, k, _dev_ptr(valid), int(renormalize), _dev_ptr(ids),
-                _dev_ptr(weights), _dev_ptr(counts), _dev_ptr(prob), _dev_ptr(loss), _dev_ptr(routed), _dev_ptr(ws), ws.numel(),
-                self._stream()))
+        self._done(self._lib.ep_route(
+            self._h, _ptr(logits), TYPES[logits.dtype], rows, parts, k, _ptr(valid), int(renormalize), _ptr(ids),
+            _ptr(weights), _ptr(counts), _ptr(prob), _ptr(loss), _ptr(routed), _ptr(ws), ws.numel(),
+            self._raw_stream()))
         return RouteResult(ids, weights, counts, prob, loss, routed)
 
     def route_backward(self, logits, result: "RouteResult", dweights=None, dloss=None, valid=None, renormalize: bool = False):
@@ -891,10 +898,9 @@ class Context:
         dloss = _check_vector(dloss, (torch.float32,), "dloss", self.device, 1)
         valid = _check_vector(valid, (torch.uint8, torch.bool), "valid", self.device, rows)
         dlogits = torch.empty_like(logits)
-        with torch.cuda.device(self.device):
-            self._done(self._lib.ep_route_backward(
-                self._h, _dev_ptr(logits), TYPES[logits.dtype], rows, parts, k, _dev_ptr(valid), int(renormalize), _dev_ptr(ids),
-                _dev_ptr(counts), _dev_ptr(routed), _dev_ptr(dweights), _dev_ptr(dloss), _dev_ptr(dlogits), self._stream()))
+        self._done(self._lib.ep_route_backward(
+            self._h, _ptr(logits), TYPES[logits.dtype], rows, parts, k, _ptr(valid), int(renormalize), _ptr(ids),
+            _ptr(counts), _ptr(routed), _ptr(dweights), _ptr(dloss), _ptr(dlogits), self._raw_stream()))
         return dlogits
 
 
@@ -993,39 +999,39 @@ def ep_graph_bandwidth(rowptr, colidx, pi, per_vertex=True) -> BandwidthResult:
 
 def ep_rms_norm(x, weight=None, residual=None, eps=1e-6, out_dtype=None) -> NormResult:
     """Root-mean-square norm of the rows of x + residual, in x's type, another float type or 8 bits with scales."""
-    return default_context(x.device.index).rms_norm(x, weight, residual, eps, out_dtype)
+    return _context_of(x).rms_norm(x, weight, residual, eps, out_dtype)
 
 
 def ep_rms_norm_backward(dout, hidden, weight=None, eps=1e-6, dhidden=None, need_dweight=True) -> NormGradients:
     """Gradients of ep_rms_norm."""
-    return default_context(hidden.device.index).rms_norm_backward(dout, hidden, weight, eps, dhidden, need_dweight)
+    return _context_of(hidden).rms_norm_backward(dout, hidden, weight, eps, dhidden, need_dweight)
 
 
 def ep_quantize_rows(x) -> QuantizedRows:
     """Rows in 8 bits with a scale each, as ep_linear takes them."""
-    return default_context(x.device.index).quantize_rows(x)
+    return _context_of(x).quantize_rows(x)
 
 
 def ep_linear(x, weight, bias=None, activation="none", residual=None, x_scale=None, weight_scale=None, out_dtype=None,
               preact=False) -> LinearResult:
     """act(x weight^T + bias) + residual."""
-    return default_context(x.device.index).linear(x, weight, bias, activation, residual, x_scale, weight_scale, out_dtype, preact)
+    return _context_of(x).linear(x, weight, bias, activation, residual, x_scale, weight_scale, out_dtype, preact)
 
 
 def ep_linear_backward(dout, x, weight, preact=None, activation="none", need_dx=True, need_dweight=True,
                        need_dbias=True) -> LinearGradients:
     """Gradients of ep_linear."""
-    return default_context(x.device.index).linear_backward(dout, x, weight, preact, activation, need_dx, need_dweight, need_dbias)
+    return _context_of(x).linear_backward(dout, x, weight, preact, activation, need_dx, need_dweight, need_dbias)
 
 
 def ep_route(logits, k=1, valid=None, renormalize=False) -> RouteResult:
     """Rows to their k best parts, with weights, per-part counts and the balance loss."""
-    return default_context(logits.device.index).route(logits, k, valid, renormalize)
+    return _context_of(logits).route(logits, k, valid, renormalize)
 
 
 def ep_route_backward(logits, result, dweights=None, dloss=None, valid=None, renormalize=False) -> torch.Tensor:
     """Gradient of ep_route's logits."""
-    return default_context(logits.device.index).route_backward(logits, result, dweights, dloss, valid, renormalize)
+    return _context_of(logits).route_backward(logits, result, dweights, dloss, valid, renormalize)
 
 
 REORDER_STATIC_MAX_N = 1 << 22

@@ -33,27 +33,65 @@ struct Epilogue {
     int out_type;
     int64_t M;
     int N;
-    bool vec;                         // out, preact, residual: 16-byte rows of whole 8-column chunks
+    bool vec;                         // out, preact, residual, bias, scales: 16-byte rows of whole 8-column chunks
     float *share;                     // where a block's share of a split sum goes: [split][M][ld_share] fp32
     int ld_share;
 };
 
-__device__ __forceinline__ float normal_cdf(float z) { return 0.5f + 0.5f * erff(z * 0.70710678f); }
-
-__device__ __forceinline__ float activate(float z, int act) {
-    if (act == EP_ACT_RELU) return z > 0.f || z != z ? z : 0.f;
-    if (act == EP_ACT_GELU) return z * normal_cdf(z);
-    if (act == EP_ACT_SILU) return z / (1.f + __expf(-z));
-    return z;
+// The upper tail of the normal distribution at |z|, over exp(-z^2 / 2): a polynomial in t = 1 / (1 + 0.33 |z|), fitted
+// (weighted least squares, reweighted towards the largest error) to 2.2e-9 of the tail itself; fp32 rounding makes that
+// 6e-8.  The gradient needs the same exponential, and where the slope of z Phi(z) crosses zero the exponential is a common
+// factor of the terms that cancel.
+__device__ __forceinline__ float normal_tail(float z) {
+    const float t = __fdividef(1.f, fmaf(0.33f, fabsf(z), 1.f));
+    float q = fmaf(0.0436886735f, t, -0.211661354f);
+    q = fmaf(q, t, 0.313509107f);
+    q = fmaf(q, t, -0.0706691593f);
+    q = fmaf(q, t, 0.170115322f);
+    q = fmaf(q, t, 0.122831702f);
+    q = fmaf(q, t, 0.132185712f);
+    return q * t;
 }
-__device__ __forceinline__ float slope_of(float z, int act) {
-    if (act == EP_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-    if (act == EP_ACT_GELU) return normal_cdf(z) + z * 0.39894228f * __expf(-0.5f * z * z);
-    if (act == EP_ACT_SILU) {
-        const float s = 1.f / (1.f + __expf(-z));
-        return s * (1.f + z * (1.f - s));
+__device__ __forceinline__ float gelu(float z) {
+    const float tail = normal_tail(z) * __expf(-0.5f * z * z);
+    return z * (z >= 0.f ? 1.f - tail : tail);
+}
+__device__ __forceinline__ float gelu_slope(float z) {
+    const float bell = __expf(-0.5f * z * z);
+    const float q = fmaf(fabsf(z), -0.39894228f, normal_tail(z));
+    return z >= 0.f ? fmaf(-q, bell, 1.f) : q * bell;
+}
+
+// act(z) of n values; the switch is outside the loops, and taken by all threads alike.
+template <int n>
+__device__ __forceinline__ void activate(float (&v)[n], int act) {
+    if (act == EP_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = v[i] > 0.f || v[i] != v[i] ? v[i] : 0.f;
+    } else if (act == EP_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = gelu(v[i]);
+    } else if (act == EP_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = __fdividef(v[i], 1.f + __expf(fminf(-v[i], 80.f)));
     }
-    return 1.f;
+}
+// v *= act'(z)
+template <int n>
+__device__ __forceinline__ void times_slope(float (&v)[n], const float (&z)[n], int act) {
+    if (act == EP_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = z[i] > 0.f ? v[i] : 0.f;
+    } else if (act == EP_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] *= gelu_slope(z[i]);
+    } else if (act == EP_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float s = __fdividef(1.f, 1.f + __expf(fminf(-z[i], 80.f)));
+            v[i] *= s * fmaf(z[i], 1.f - s, 1.f);
+        }
+    }
 }
 
 // What a thread needs of n columns, the same for every row that it finishes.
@@ -63,40 +101,50 @@ struct Columns {
     __device__ __forceinline__ void load(const Epilogue &e, int col) {
 #pragma unroll
         for (int i = 0; i < n; ++i) {
-            bias[i] = e.bias && col + i < e.N ? load_param(e.bias, e.bias_type, col + i) : 0.f;
-            scale[i] = e.w_scale && col + i < e.N ? __ldg(e.w_scale + col + i) : 1.f;
+            bias[i] = 0.f;
+            scale[i] = 1.f;
         }
+        if (e.bias) {   // (vec is only set where the bias is aligned too)
+            if (e.bias_type == EP_F32)
+                load_chunk(static_cast<const float *>(e.bias), col, e.N, n > 1 && e.vec, 0.f, bias);
+            else if (e.bias_type == EP_BF16)
+                load_chunk(static_cast<const __nv_bfloat16 *>(e.bias), col, e.N, n > 1 && e.vec, 0.f, bias);
+            else
+                load_chunk(static_cast<const __half *>(e.bias), col, e.N, n > 1 && e.vec, 0.f, bias);
+        }
+        if (e.w_scale) load_chunk(e.w_scale, col, e.N, n > 1 && e.vec, 1.f, scale);
     }
 };
 
-// n finished sums of one row, from column col on: scale, bias, (store z), activation, residual, store.
+// n finished sums of one row, from column col on: scale, bias, (store z), activation, residual, store.  `r` holds the
+// residual, where there is one.
 template <typename O, int n>
-__device__ __forceinline__ void finish_as(const Epilogue &e, int64_t row, int col, const Columns<n> &c, float (&v)[n]) {
-    const float xs = e.x_scale ? __ldg(e.x_scale + row) : 1.f;
+__device__ __forceinline__ void finish(const Epilogue &e, int64_t row, int col, const Columns<n> &c, float (&v)[n],
+                                       const float (&r)[n]) {
+    if (e.x_scale) {
+        const float xs = __ldg(e.x_scale + row);
 #pragma unroll
-    for (int i = 0; i < n; ++i) v[i] = (e.x_scale ? v[i] * xs * c.scale[i] : v[i]) + c.bias[i];
+        for (int i = 0; i < n; ++i) v[i] *= xs * c.scale[i];
+    }
+#pragma unroll
+    for (int i = 0; i < n; ++i) v[i] += c.bias[i];
     const bool vec = n > 1 && e.vec;
     if (e.preact) store_chunk(static_cast<O *>(e.preact) + row * e.N, col, e.N, vec, v);
-    if (e.act != EP_ACT_NONE) {
-#pragma unroll
-        for (int i = 0; i < n; ++i) v[i] = activate(v[i], e.act);
-    }
+    activate(v, e.act);
     if (e.residual) {
-        float r[n];
-        load_chunk(static_cast<const O *>(e.residual) + row * e.ldr, col, e.N, vec, 0.f, r);
 #pragma unroll
         for (int i = 0; i < n; ++i) v[i] += r[i];
     }
     store_chunk(static_cast<O *>(e.out) + row * e.N, col, e.N, vec, v);
 }
-template <int n>
-__device__ __forceinline__ void finish(const Epilogue &e, int64_t row, int col, const Columns<n> &c, float (&v)[n]) {
-    if (e.out_type == EP_BF16)
-        finish_as<__nv_bfloat16>(e, row, col, c, v);
-    else if (e.out_type == EP_F16)
-        finish_as<__half>(e, row, col, c, v);
-    else
-        finish_as<float>(e, row, col, c, v);
+template <typename O, int n>
+__device__ __forceinline__ void load_residual(const Epilogue &e, int64_t row, int col, float (&r)[n]) {
+    if (e.residual)
+        load_chunk(static_cast<const O *>(e.residual) + row * e.ldr, col, e.N, n > 1 && e.vec, 0.f, r);
+    else {
+#pragma unroll
+        for (int i = 0; i < n; ++i) r[i] = 0.f;
+    }
 }
 
 // ---------------------------------------------------------------------------------------------- the tile kernel
@@ -199,7 +247,7 @@ __device__ __forceinline__ Item item_at(const GemmShape &g, int bn, int64_t i) {
     return t;
 }
 
-template <int BN, bool F8, int PARTS, bool RUNS>
+template <int BN, bool F8, int PARTS, bool RUNS, typename O>
 __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_constant__ CUtensorMap map_a,
                                                                 const __grid_constant__ CUtensorMap map_b,
                                                                 const GemmShape g, const Epilogue e, int *status) {
@@ -333,10 +381,10 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
         bool ok = true;
         // 32 columns of this warp's 32 rows, one row per lane, through shared memory (16-byte chunk c of row r lies at
         // c ^ (r & 7)) so that neighbouring lanes finish neighbouring columns
-        auto finish_chunk = [&](const Item &t, int col, const float (&v)[32]) {
+        auto finish_chunk = [&](const Item &t, int col, const Columns<8> &c, const float (&v)[32]) {
 #pragma unroll
-            for (int c = 0; c < 8; ++c)
-                mine[lane * 8 + (c ^ (lane & 7))] = make_float4(v[c * 4], v[c * 4 + 1], v[c * 4 + 2], v[c * 4 + 3]);
+            for (int q = 0; q < 8; ++q)
+                mine[lane * 8 + (q ^ (lane & 7))] = make_float4(v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
             __syncwarp();
             const int64_t row0 = t.m0 + quad * 32;
             if (e.share) {
@@ -349,26 +397,36 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
             } else if (e.vec) {
                 const int cc = lane & 3;
                 if (col + cc * 8 < e.N) {
-                    Columns<8> c;
-                    c.load(e, col + cc * 8);
-#pragma unroll
+                    // two rows at a time: the code stays small enough for the instruction cache (with all four
+                    // unrolled and the type chosen at run time, waiting for instructions was the largest stall)
+#pragma unroll 2
                     for (int r = lane >> 2; r < 32; r += 8) {
-                        if (row0 + r >= e.M) continue;
+                        if (row0 + r >= e.M) break;
+                        float add[8];
+                        load_residual<O>(e, row0 + r, col + cc * 8, add);
                         const float4 a = mine[r * 8 + ((2 * cc) ^ (r & 7))], b = mine[r * 8 + ((2 * cc + 1) ^ (r & 7))];
                         float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-                        finish(e, row0 + r, col + cc * 8, c, w);
+                        finish<O>(e, row0 + r, col + cc * 8, c, w, add);
                     }
                 }
             } else if (col + lane < e.N) {
-                Columns<1> c;
-                c.load(e, col + lane);
+                Columns<1> c1;
+                c1.load(e, col + lane);
                 const float *flat = reinterpret_cast<const float *>(mine);
+#pragma unroll 1
                 for (int r = 0; r < 32 && row0 + r < e.M; ++r) {
-                    float w[1] = {flat[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)]};
-                    finish(e, row0 + r, col + lane, c, w);
+                    float w[1] = {flat[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)]}, add[1];
+                    load_residual<O>(e, row0 + r, col + lane, add);
+                    finish<O>(e, row0 + r, col + lane, c1, w, add);
                 }
             }
             __syncwarp();
+        };
+        // bias and scales of this thread's columns of a chunk, fetched before the sums are waited for
+        auto columns = [&](int col) {
+            Columns<8> c;
+            if (!e.share && e.vec) c.load(e, col + (lane & 3) * 8);
+            return c;
         };
         for (int64_t i = blockIdx.x; ok && i < g.items; i += gridDim.x) {
             const Item t = item_at(g, BN, i);
@@ -407,10 +465,11 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                 }
                 if (!ok) break;
 #pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) finish_chunk(t, col0 + c * 32, sum[c]);
+                for (int c = 0; c < CHUNKS; ++c) finish_chunk(t, col0 + c * 32, columns(col0 + c * 32), sum[c]);
             } else {
                 const uint32_t buf = acc & 1u, use = (acc >> 1) & 1u;
                 ++acc;
+                Columns<8> cols = columns(col0);
                 if (!(ok = mbar_wait(&sh->t_full[buf], use, abort_flag))) break;
                 tc_fence_after();
                 const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + buf * ACC_COLS + half * COLS;
@@ -427,7 +486,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                     float f[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
-                    finish_chunk(t, col0 + c * 32, f);
+                    finish_chunk(t, col0 + c * 32, cols, f);
+                    if (c + 1 < CHUNKS) cols = columns(col0 + (c + 1) * 32);
                 }
             }
         }
@@ -441,6 +501,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
 }
 
 // The shares of a split sum added in order, then the epilogue.  A thread finishes 8 columns of a row.
+template <typename O>
 __global__ void __launch_bounds__(256) linear_join(const float *__restrict__ shares, int splits, const Epilogue e) {
     const int chunks = (e.N + 7) / 8;
     const int64_t total = e.M * chunks;
@@ -457,7 +518,9 @@ __global__ void __launch_bounds__(256) linear_join(const float *__restrict__ sha
         }
         Columns<8> c;
         c.load(e, col);
-        finish(e, row, col, c, v);
+        float add[8];
+        load_residual<O>(e, row, col, add);
+        finish<O>(e, row, col, c, v, add);
     }
 }
 
@@ -499,7 +562,17 @@ __global__ void __launch_bounds__(256) linear_few_rows(const T *__restrict__ x, 
     if (lane < ROWS && lane < e.M) {
         Columns<1> c;
         c.load(e, col);
-        finish(e, lane, col, c, v);
+        float add[1];
+        if (e.out_type == EP_BF16) {
+            load_residual<__nv_bfloat16>(e, lane, col, add);
+            finish<__nv_bfloat16>(e, lane, col, c, v, add);
+        } else if (e.out_type == EP_F16) {
+            load_residual<__half>(e, lane, col, add);
+            finish<__half>(e, lane, col, c, v, add);
+        } else {
+            load_residual<float>(e, lane, col, add);
+            finish<float>(e, lane, col, c, v, add);
+        }
     }
 }
 
@@ -568,8 +641,7 @@ __global__ void __launch_bounds__(DZ_CHUNKS *DZ_ROWS) linear_dz(const D *__restr
             if (act != EP_ACT_NONE) {
                 float zz[8];
                 load_chunk(z + row * n_out, col, n_out, vec, 0.f, zz);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] *= slope_of(zz[i], act);
+                times_slope(v, zz, act);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += col + i < n_out ? v[i] : 0.f;
@@ -695,10 +767,10 @@ GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, int
     return p;
 }
 
-template <int BN, bool F8, int PARTS, bool RUNS>
+template <int BN, bool F8, int PARTS, bool RUNS, typename O>
 int launch_tiles(ep_ctx *ctx, const GemmPlan &p, const CUtensorMap &ma, const CUtensorMap &mb, const Epilogue &e,
                  cudaStream_t stream) {
-    auto kernel = linear_tiles<BN, F8, PARTS, RUNS>;
+    auto kernel = linear_tiles<BN, F8, PARTS, RUNS, O>;
     EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)GEMM_SMEM));
     const int grid = (int)std::min<int64_t>(p.shape.items, ctx->sm_count);
     kernel<<<grid, GEMM_THREADS, GEMM_SMEM, stream>>>(ma, mb, p.shape, e, ctx->d_status);
@@ -706,10 +778,23 @@ int launch_tiles(ep_ctx *ctx, const GemmPlan &p, const CUtensorMap &ma, const CU
     return EP_OK;
 }
 
+// (the type of the output is fp32 exactly where sums are kept in runs)
+template <bool F8, typename O>
+int launch_width(ep_ctx *ctx, const GemmPlan &p, const CUtensorMap &ma, const CUtensorMap &mb, const Epilogue &e, cudaStream_t stream) {
+    return p.bn == 256   ? launch_tiles<256, F8, 1, false, O>(ctx, p, ma, mb, e, stream)
+           : p.bn == 128 ? launch_tiles<128, F8, 1, false, O>(ctx, p, ma, mb, e, stream)
+                         : launch_tiles<64, F8, 1, false, O>(ctx, p, ma, mb, e, stream);
+}
+template <bool F8>
+int launch_type(ep_ctx *ctx, const GemmPlan &p, const CUtensorMap &ma, const CUtensorMap &mb, const Epilogue &e, cudaStream_t stream) {
+    return p.runs                   ? launch_tiles<128, F8, 1, true, float>(ctx, p, ma, mb, e, stream)
+           : e.out_type == EP_BF16 ? launch_width<F8, __nv_bfloat16>(ctx, p, ma, mb, e, stream)
+                                    : launch_width<F8, __half>(ctx, p, ma, mb, e, stream);
+}
+
 // D = A B^T by tiles, with the epilogue; `share` is room for the shares of a split sum.  Adds to *kernels.
 int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand &b, bool b_mn, Epilogue e, float *share,
              cudaStream_t stream, int *kernels) {
-    const bool f8 = a.type == EP_E4M3;
     const uint32_t fmt = a.type == EP_BF16 ? 1u : 0u;   // f16 and e4m3 are both format 0 of their kinds
     p.shape.a_mn = a_mn;
     p.shape.b_mn = b_mn;
@@ -720,25 +805,20 @@ int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand
         return ep::fail(ctx, EP_ERR_CUDA, "cuTensorMapEncodeTiled failed for a product of %lld x %d", (long long)e.M, e.N);
     e.share = p.splits > 1 ? share : nullptr;
     e.ld_share = p.ld_share;
-    int rc;
-    if (a.parts == 3)
-        rc = launch_tiles<128, false, 3, true>(ctx, p, ma, mb, e, stream);
-    else if (f8)
-        rc = p.runs        ? launch_tiles<128, true, 1, true>(ctx, p, ma, mb, e, stream)
-             : p.bn == 256 ? launch_tiles<256, true, 1, false>(ctx, p, ma, mb, e, stream)
-             : p.bn == 128 ? launch_tiles<128, true, 1, false>(ctx, p, ma, mb, e, stream)
-                           : launch_tiles<64, true, 1, false>(ctx, p, ma, mb, e, stream);
-    else
-        rc = p.runs        ? launch_tiles<128, false, 1, true>(ctx, p, ma, mb, e, stream)
-             : p.bn == 256 ? launch_tiles<256, false, 1, false>(ctx, p, ma, mb, e, stream)
-             : p.bn == 128 ? launch_tiles<128, false, 1, false>(ctx, p, ma, mb, e, stream)
-                           : launch_tiles<64, false, 1, false>(ctx, p, ma, mb, e, stream);
+    const int rc = a.parts == 3          ? launch_tiles<128, false, 3, true, float>(ctx, p, ma, mb, e, stream)
+                   : a.type == EP_E4M3 ? launch_type<true>(ctx, p, ma, mb, e, stream)
+                                         : launch_type<false>(ctx, p, ma, mb, e, stream);
     if (rc != EP_OK) return rc;
     ++*kernels;
     if (p.splits > 1) {
         const int64_t threads = e.M * ((e.N + 7) / 8);
         const int grid = (int)std::min<int64_t>(ep::ceil_div(threads, 256), (int64_t)ctx->sm_count * PACK_BLOCKS_PER_SM);
-        linear_join<<<grid, 256, 0, stream>>>(share, p.splits, e);
+        if (e.out_type == EP_BF16)
+            linear_join<__nv_bfloat16><<<grid, 256, 0, stream>>>(share, p.splits, e);
+        else if (e.out_type == EP_F16)
+            linear_join<__half><<<grid, 256, 0, stream>>>(share, p.splits, e);
+        else
+            linear_join<float><<<grid, 256, 0, stream>>>(share, p.splits, e);
         EP_CUDA(ctx, cudaGetLastError());
         ++*kernels;
     }
@@ -1005,7 +1085,8 @@ int ep_linear(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int64_t ld
     e.out_type = out_type;
     e.M = rows;
     e.N = n_out;
-    e.vec = n_out % 8 == 0 && aligned(out, 16) && aligned(preact, 16) && aligned(residual, 16) &&
+    e.vec = n_out % 8 == 0 && aligned(out, 16) && aligned(preact, 16) && aligned(residual, 16) && aligned(bias, 16) &&
+            aligned(w_scale, 16) &&
             (!residual || ldr * type_size(out_type) % 16 == 0);
     DeviceGuard guard(ctx->device);
     Timed tm(ctx, static_cast<cudaStream_t>(cuda_stream), EP_TIMER_LINEAR);
