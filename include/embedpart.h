@@ -473,7 +473,8 @@ int ep_linear_backward(ep_ctx *ctx, const void *dout, int32_t dout_type, const v
  *   dp_e = dloss E counts[e] / (k R) / R  + (e = ids[i]:  dweights[i], or with renormalize
  *          (dweights[i] - sum_j dweights[j] weights[j]) / sum_j p[ids[j]])
  *   dlogits = p (dp - sum_e p_e dp_e);  0 in rows that take no part
- *   logits, valid, k, renormalize, ids, counts, routed: as the forward took and returned them
+ *   logits, valid, k, renormalize, ids, counts, routed: as the forward took and returned them (a row's ids other than -1
+ *            are distinct)
  *   dweights [dev] rows x k fp32 or NULL (zero);  dloss [dev] 1 fp32 or NULL (zero)
  *   dlogits  [dev] out, rows x parts of `type`
  * An id outside [-1, parts) raises EP_ERR_BAD_INDEX in the device status word and is skipped.
