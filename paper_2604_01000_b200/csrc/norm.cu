@@ -13,9 +13,7 @@ using namespace eprow;
 
 namespace {
 
-// Rows of up to V * L chunks of 16 bytes of the input type; thread `lane` of a row holds chunks lane, lane + L, ...
-// (neighbouring threads read neighbouring chunks).  L <= 32: a block of 256 threads has 256 / L rows at a time.
-// L > 32: the block is L threads and has one.
+// L <= 32: a block of 256 threads has 256 / L rows at a time.  L > 32: the block is L threads and has one.
 template <int L>
 constexpr int block_threads() { return L > 32 ? L : 256; }
 
@@ -31,7 +29,8 @@ __device__ __forceinline__ float row_rho(const float (&h)[V][N], int d, float ep
     for (int j = 0; j < V; ++j)
 #pragma unroll
         for (int i = 0; i < N; ++i) ss = fmaf(h[j][i], h[j][i], ss);
-    const float mean = reduce_row<L, OpSum>(ss, slots, turn) / (float)d;
+    const float per_column = 1.f / (float)d;
+    const float mean = reduce_row<L, OpSum>(ss, slots, turn) * per_column;
     float rho = rsqrtf(mean + eps);
     const bool rare = !(mean + eps > 1e-30f && mean < 1e36f);
     if (__any_sync(FULL, rare)) {
@@ -49,7 +48,7 @@ __device__ __forceinline__ float row_rho(const float (&h)[V][N], int d, float ep
         for (int j = 0; j < V; ++j)
 #pragma unroll
             for (int i = 0; i < N; ++i) ss = fmaf(h[j][i] * s, h[j][i] * s, ss);
-        const float scaled = reduce_row<L, OpSum>(ss, slots, turn) / (float)d + eps * s * s;
+        const float scaled = reduce_row<L, OpSum>(ss, slots, turn) * per_column + eps * s * s;
         if (rare && scaled == 0.f)
             rho = 0.f;
         else if (rare)
@@ -59,11 +58,11 @@ __device__ __forceinline__ float row_rho(const float (&h)[V][N], int d, float ep
 }
 
 // NORM: the norm; otherwise the rows are only brought to 8 bits.
-template <typename T, typename O, int L, int V, bool NORM>
-__global__ void __launch_bounds__(block_threads<L>()) norm_rows(const T *x, const T *residual, const void *weight,
-                                                                int weight_type, int64_t rows, int d, float eps, O *out,
-                                                                float *scale, T *hidden, bool vec) {
-    constexpr int N = 16 / (int)sizeof(T);
+template <typename T, typename O, typename Lay, bool NORM>
+__global__ void __launch_bounds__(block_threads<Lay::L>()) norm_rows(const T *x, const T *residual, const void *weight,
+                                                                     int weight_type, int64_t rows, int d, float eps, O *out,
+                                                                     float *scale, T *hidden) {
+    constexpr int L = Lay::L, V = Lay::V, N = Lay::N;
     constexpr int GROUPS = block_threads<L>() / L;
     __shared__ float slots[L > 32 ? 64 : 1];
     int turn = 0;
@@ -73,30 +72,24 @@ __global__ void __launch_bounds__(block_threads<L>()) norm_rows(const T *x, cons
     for (int j = 0; j < V; ++j)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int c = (j * L + lane) * N + i;
+            const int c = Lay::col(lane, j, i);
             g[j][i] = NORM && weight && c < d ? load_param(weight, weight_type, c) : 1.f;
         }
     // the loop is the same for all threads of a warp (they reduce together); rows past the end are empty
     for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += (int64_t)gridDim.x * GROUPS) {
-        const int64_t row = first + group;
-        const int width = row < rows ? d : 0;
-        const int64_t at = row < rows ? row * d : 0;
+        const int64_t row = first + group, at = row * d;
+        const bool mine = row < rows;
         float h[V][N];
-#pragma unroll
-        for (int j = 0; j < V; ++j) load_chunk(x + at, (j * L + lane) * N, width, vec, 0.f, h[j]);
+        Lay::load_if(mine, x + at, lane, d, 0.f, h);
         if (NORM && residual) {
+            float r[V][N];
+            Lay::load_if(mine, residual + at, lane, d, 0.f, r);
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                float r[N];
-                load_chunk(residual + at, (j * L + lane) * N, width, vec, 0.f, r);
+            for (int j = 0; j < V; ++j)
 #pragma unroll
-                for (int i = 0; i < N; ++i) h[j][i] += r[i];
-            }
+                for (int i = 0; i < N; ++i) h[j][i] += r[j][i];
         }
-        if (NORM && hidden) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) store_chunk(hidden + at, (j * L + lane) * N, width, vec, h[j]);
-        }
+        if (NORM && hidden && mine) Lay::store(hidden + at, lane, d, h);
         if (NORM) {
             const float rho = row_rho<L>(h, d, eps, slots, turn);
 #pragma unroll
@@ -118,67 +111,56 @@ __global__ void __launch_bounds__(block_threads<L>()) norm_rows(const T *x, cons
             for (int j = 0; j < V; ++j)
 #pragma unroll
                 for (int i = 0; i < N; ++i) h[j][i] = tiny && s > 0.f ? h[j][i] / s : h[j][i] * inverse;
-            if (lane == 0 && row < rows) scale[row] = s;
+            if (lane == 0 && mine) scale[row] = s;
         }
-#pragma unroll
-        for (int j = 0; j < V; ++j) store_chunk(out + at, (j * L + lane) * N, width, vec, h[j]);
+        if (mine) Lay::store(out + at, lane, d, h);
     }
 }
 
 // dx of every row; the block's share of dweight goes to part[blockIdx.x][d] (or to dweight itself when it is alone).
-template <typename T, typename D, int L, int V>
-__global__ void __launch_bounds__(block_threads<L>()) norm_rows_backward(const D *dout, const T *hidden, const void *weight,
-                                                                         int weight_type, const T *dhidden, int64_t rows,
-                                                                         int d, float eps, T *dx, float *part, bool vec) {
-    constexpr int N = 16 / (int)sizeof(T);
+template <typename T, typename D, typename Lay>
+__global__ void __launch_bounds__(block_threads<Lay::L>()) norm_rows_backward(const D *dout, const T *hidden, const void *weight,
+                                                                              int weight_type, const T *dhidden, int64_t rows,
+                                                                              int d, float eps, T *dx, float *part) {
+    constexpr int L = Lay::L, V = Lay::V, N = Lay::N;
     constexpr int GROUPS = block_threads<L>() / L;
     __shared__ float slots[L > 32 ? 64 : 1];
     extern __shared__ float fold[];   // [GROUPS][V * L * N] where GROUPS > 1
     int turn = 0;
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
+    const float per_column = 1.f / (float)d;
     float g[V][N], dg[V][N];
 #pragma unroll
     for (int j = 0; j < V; ++j)
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int c = (j * L + lane) * N + i;
+            const int c = Lay::col(lane, j, i);
             g[j][i] = weight && c < d ? load_param(weight, weight_type, c) : 1.f;
             dg[j][i] = 0.f;
         }
     for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += (int64_t)gridDim.x * GROUPS) {
-        const int64_t row = first + group;
-        const int width = row < rows ? d : 0;
-        const int64_t at = row < rows ? row * d : 0;
-        float h[V][N], y[V][N];
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            load_chunk(hidden + at, (j * L + lane) * N, width, vec, 0.f, h[j]);
-            load_chunk(dout + at, (j * L + lane) * N, width, vec, 0.f, y[j]);
-        }
+        const int64_t row = first + group, at = row * d;
+        const bool mine = row < rows;
+        float h[V][N], y[V][N], o[V][N];   // all three on their way before the first sum
+        Lay::load_if(mine, hidden + at, lane, d, 0.f, h);
+        Lay::load_if(mine, dout + at, lane, d, 0.f, y);
+        Lay::load_if(mine && dhidden, dhidden + at, lane, d, 0.f, o);
         float ah = 0.f;
 #pragma unroll
         for (int j = 0; j < V; ++j)
 #pragma unroll
             for (int i = 0; i < N; ++i) ah = fmaf(y[j][i] * g[j][i], h[j][i], ah);
         const float rho = row_rho<L>(h, d, eps, slots, turn);
-        const float back = rho * (reduce_row<L, OpSum>(ah, slots, turn) / (float)d);
+        const float back = rho * (reduce_row<L, OpSum>(ah, slots, turn) * per_column);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            float o[N];
-            if (dhidden)
-                load_chunk(dhidden + at, (j * L + lane) * N, width, vec, 0.f, o);
-            else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) o[i] = 0.f;
-            }
+        for (int j = 0; j < V; ++j)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float unit = h[j][i] * rho;
-                o[i] += rho * (y[j][i] * g[j][i] - unit * back);
+                o[j][i] = fmaf(rho, y[j][i] * g[j][i] - unit * back, o[j][i]);
                 dg[j][i] = fmaf(y[j][i], unit, dg[j][i]);
             }
-            store_chunk(dx + at, (j * L + lane) * N, width, vec, o);
-        }
+        if (mine) Lay::store(dx + at, lane, d, o);
     }
     if (!part) return;
     float *to = part + (size_t)blockIdx.x * d;
@@ -186,66 +168,48 @@ __global__ void __launch_bounds__(block_threads<L>()) norm_rows_backward(const D
 #pragma unroll
         for (int j = 0; j < V; ++j)
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int c = (j * L + lane) * N + i;
-                if (c < d) to[c] = dg[j][i];
-            }
+            for (int i = 0; i < N; ++i)
+                if (Lay::col(lane, j, i) < d) to[Lay::col(lane, j, i)] = dg[j][i];
     } else {
-        constexpr int WIDE = V * L * N;
 #pragma unroll
         for (int j = 0; j < V; ++j)
 #pragma unroll
-            for (int i = 0; i < N; ++i) fold[group * WIDE + (j * L + lane) * N + i] = dg[j][i];
+            for (int i = 0; i < N; ++i) fold[group * Lay::WIDE + Lay::col(lane, j, i)] = dg[j][i];
         __syncthreads();
         for (int c = threadIdx.x; c < d; c += blockDim.x) {
             float s = 0.f;
 #pragma unroll 4
-            for (int q = 0; q < GROUPS; ++q) s += fold[q * WIDE + c];
+            for (int q = 0; q < GROUPS; ++q) s += fold[q * Lay::WIDE + c];
             to[c] = s;
         }
     }
 }
 
-// A block sums 32 columns: 32 x 8 threads, thread (c, r) the rows r, r + 8, ... in fp64; then the eight in order.
-__global__ void __launch_bounds__(256) fold_partials(const float *__restrict__ parts, int n, int cols, float *__restrict__ out) {
-    __shared__ double s[8][32];
+// A block sums 32 columns: 32 x 32 threads, thread (c, r) the rows r, r + 32, ... in fp64; then the 32 in order.
+__global__ void __launch_bounds__(1024) fold_partials(const float *__restrict__ parts, int n, int cols, float *__restrict__ out) {
+    __shared__ double s[32][32];
     const int lane = threadIdx.x & 31, r0 = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;
     double t = 0.0;
     if (c < cols)
-#pragma unroll 4
-        for (int r = r0; r < n; r += 8) t += (double)parts[(size_t)r * cols + c];
+#pragma unroll 8
+        for (int r = r0; r < n; r += 32) t += (double)parts[(size_t)r * cols + c];
     s[r0][lane] = t;
     __syncthreads();
     if (r0 == 0 && c < cols) {
-#pragma unroll
-        for (int q = 1; q < 8; ++q) t += s[q][lane];
+#pragma unroll 8
+        for (int q = 1; q < 32; ++q) t += s[q][lane];
         out[c] = (float)t;
     }
 }
 
 constexpr int MAX_D = 16384;
-constexpr int BLOCKS_PER_SM = 8;
-
-// The fewest threads and chunks per thread that hold a row of `chunks` 16-byte chunks; F<L, V>() runs the launch.
-template <typename F>
-int with_layout(int64_t chunks, F f) {
-    if (chunks <= 8) return f.template run<8, 1>();
-    if (chunks <= 16) return f.template run<16, 1>();
-    if (chunks <= 32) return f.template run<32, 1>();
-    if (chunks <= 64) return f.template run<32, 2>();
-    if (chunks <= 128) return f.template run<32, 4>();
-    if (chunks <= 256) return f.template run<256, 1>();
-    if (chunks <= 512) return f.template run<256, 2>();
-    if (chunks <= 1024) return f.template run<256, 4>();
-    if (chunks <= 2048) return f.template run<512, 4>();
-    return f.template run<512, 8>();
-}
+constexpr int FORWARD_BLOCKS_PER_SM = 8, BACKWARD_BLOCKS_PER_SM = 4;   // about what their registers let stay resident
 
 template <int L>
-int grid_for(const ep_ctx *ctx, int64_t rows) {
+int grid_for(const ep_ctx *ctx, int64_t rows, int per_sm) {
     constexpr int groups = block_threads<L>() / L;
-    return (int)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(rows, groups), (int64_t)ctx->sm_count * BLOCKS_PER_SM));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(rows, groups), (int64_t)ctx->sm_count * per_sm));
 }
 
 struct NormArgs {
@@ -264,24 +228,20 @@ struct NormArgs {
 
 template <typename T, typename O, bool NORM>
 struct NormLaunch {
+    static constexpr int MAX_WIDTH = MAX_D;
     const NormArgs &a;
-    template <int L, int V>
+    template <typename Lay>
     int run() const {
-        if constexpr (V * L * (16 / (int)sizeof(T)) > MAX_D) {
-            return ep::fail(a.ctx, EP_ERR_UNSUPPORTED, "rows of %d columns are not supported", a.d);
-        } else {
-            norm_rows<T, O, L, V, NORM><<<grid_for<L>(a.ctx, a.rows), block_threads<L>(), 0, a.stream>>>(
-                (const T *)a.x, (const T *)a.residual, a.weight, a.weight_type, a.rows, a.d, a.eps, (O *)a.out, a.scale,
-                (T *)a.hidden, a.vec);
-            EP_CUDA(a.ctx, cudaGetLastError());
-            return EP_OK;
-        }
+        norm_rows<T, O, Lay, NORM><<<grid_for<Lay::L>(a.ctx, a.rows, FORWARD_BLOCKS_PER_SM), block_threads<Lay::L>(), 0, a.stream>>>(
+            (const T *)a.x, (const T *)a.residual, a.weight, a.weight_type, a.rows, a.d, a.eps, (O *)a.out, a.scale, (T *)a.hidden);
+        EP_CUDA(a.ctx, cudaGetLastError());
+        return EP_OK;
     }
 };
 
 template <typename T, typename O, bool NORM>
 int launch_norm(const NormArgs &a) {
-    return with_layout(ep::ceil_div(a.d, 16 / (int)sizeof(T)), NormLaunch<T, O, NORM>{a});
+    return with_layout<T>(a.d, a.vec, NormLaunch<T, O, NORM>{a});
 }
 
 template <typename T>
@@ -311,33 +271,30 @@ struct BackArgs {
 
 template <typename T, typename D>
 struct BackLaunch {
+    static constexpr int MAX_WIDTH = MAX_D;
     BackArgs &a;
-    template <int L, int V>
+    template <typename Lay>
     int run() const {
-        if constexpr (V * L * (16 / (int)sizeof(T)) > MAX_D) {
-            return ep::fail(a.ctx, EP_ERR_UNSUPPORTED, "rows of %d columns are not supported", a.d);
-        } else {
-            constexpr int threads = block_threads<L>();
-            constexpr size_t smem = threads == L ? 0 : sizeof(float) * (threads / L) * V * L * (16 / sizeof(T));
-            const int grid = grid_for<L>(a.ctx, a.rows);
-            float *part = !a.dweight ? nullptr : grid == 1 ? a.dweight : a.parts;
-            norm_rows_backward<T, D, L, V><<<grid, threads, smem, a.stream>>>(
-                (const D *)a.dout, (const T *)a.hidden, a.weight, a.weight_type, (const T *)a.dhidden, a.rows, a.d, a.eps,
-                (T *)a.dx, part, a.vec);
-            EP_CUDA(a.ctx, cudaGetLastError());
-            a.kernels = 1;
-            if (part && grid > 1) {
-                a.kernels = 2;
-                return ep::sum_partials(a.ctx, a.parts, grid, a.d, a.dweight, a.stream);
-            }
-            return EP_OK;
+        constexpr int threads = block_threads<Lay::L>();
+        constexpr size_t smem = threads == Lay::L ? 0 : sizeof(float) * (threads / Lay::L) * Lay::WIDE;
+        const int grid = grid_for<Lay::L>(a.ctx, a.rows, BACKWARD_BLOCKS_PER_SM);
+        float *part = !a.dweight ? nullptr : grid == 1 ? a.dweight : a.parts;
+        norm_rows_backward<T, D, Lay><<<grid, threads, smem, a.stream>>>((const D *)a.dout, (const T *)a.hidden, a.weight,
+                                                                         a.weight_type, (const T *)a.dhidden, a.rows, a.d, a.eps,
+                                                                         (T *)a.dx, part);
+        EP_CUDA(a.ctx, cudaGetLastError());
+        a.kernels = 1;
+        if (part && grid > 1) {
+            a.kernels = 2;
+            return ep::sum_partials(a.ctx, a.parts, grid, a.d, a.dweight, a.stream);
         }
+        return EP_OK;
     }
 };
 
 template <typename T, typename D>
 int launch_backward(BackArgs &a) {
-    return with_layout(ep::ceil_div(a.d, 16 / (int)sizeof(T)), BackLaunch<T, D>{a});
+    return with_layout<T>(a.d, a.vec, BackLaunch<T, D>{a});
 }
 
 }  // namespace
@@ -345,7 +302,7 @@ int launch_backward(BackArgs &a) {
 namespace ep {
 
 int sum_partials(ep_ctx *ctx, const float *parts, int n, int cols, float *out, cudaStream_t stream) {
-    fold_partials<<<(unsigned)ceil_div(cols, 32), 256, 0, stream>>>(parts, n, cols, out);
+    fold_partials<<<(unsigned)ceil_div(cols, 32), 1024, 0, stream>>>(parts, n, cols, out);
     EP_CUDA(ctx, cudaGetLastError());
     return EP_OK;
 }
@@ -421,7 +378,7 @@ int ep_quantize_rows(ep_ctx *ctx, const void *x, int32_t x_type, int64_t rows, i
 size_t ep_rms_norm_backward_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t d) {
     if (!ctx || !norm_shape_ok(rows, d)) return 0;
     Arena a(nullptr);
-    a.take<float>((size_t)ctx->sm_count * BLOCKS_PER_SM * d);
+    a.take<float>((size_t)ctx->sm_count * BACKWARD_BLOCKS_PER_SM * d);
     return a.used;
 }
 

@@ -16,41 +16,8 @@ namespace {
 
 constexpr int MAX_PARTS = 4096;
 constexpr int MAX_K = 32;
-constexpr int BLOCKS_PER_SM = 6;
+constexpr int BLOCKS_PER_SM = 4;   // what their registers let stay resident
 constexpr int THREADS = 256;
-
-// How a row lies over the L threads that share it, V * N columns to each.  VEC: chunks of N columns (16 bytes) dealt out
-// in turn; rows start on 16-byte boundaries and hold whole chunks.  Otherwise single columns dealt out in turn, so that
-// neighbouring lanes read neighbouring elements wherever the row starts.
-template <typename T, int L, int V, int N, bool VEC>
-struct Layout {
-    static __device__ __forceinline__ int col(int lane, int j, int i) {
-        return VEC ? (j * L + lane) * N + i : (j * N + i) * L + lane;
-    }
-    static __device__ __forceinline__ void load(const T *row, int lane, int width, float fill, float (&v)[V][N]) {
-        if constexpr (VEC) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) load_chunk(row, col(lane, j, 0), width, true, fill, v[j]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-#pragma unroll
-                for (int i = 0; i < N; ++i) v[j][i] = col(lane, j, i) < width ? to_f32(row[col(lane, j, i)]) : fill;
-        }
-    }
-    static __device__ __forceinline__ void store(T *row, int lane, int width, const float (&v)[V][N]) {
-        if constexpr (VEC) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) store_chunk(row, col(lane, j, 0), width, true, v[j]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (col(lane, j, i) < width) row[col(lane, j, i)] = from_f32<T>(v[j][i]);
-        }
-    }
-};
 
 // The better of two (logit, column) pairs: the larger logit, of equal ones the lower column.
 __device__ __forceinline__ void keep_better(float &v, int &c, float ov, int oc) {
@@ -124,15 +91,14 @@ __device__ void finish_block(const Finish &f, int64_t rows_routed, double *red) 
     }
 }
 
-template <typename T, int L, int V, int N, bool VEC>
+template <typename T, typename Lay>
 __global__ void __launch_bounds__(THREADS) route_rows(const T *__restrict__ logits, int64_t rows, int parts, int k,
                                                       const uint8_t *__restrict__ valid, bool renormalize,
                                                       int32_t *__restrict__ ids, float *weights,
                                                       float *__restrict__ part_prob, int *__restrict__ part_count,
                                                       unsigned *ticket, Finish fin) {
-    using Lay = Layout<T, L, V, N, VEC>;
+    constexpr int L = Lay::L, V = Lay::V, N = Lay::N, WIDE = Lay::WIDE;
     constexpr int GROUPS = THREADS / L;
-    constexpr int WIDE = V * L * N;
     __shared__ float slots[L > 32 ? 64 : 1];
     __shared__ float slot_v[L > 32 ? 16 : 1];
     __shared__ int slot_c[L > 32 ? 16 : 1];
@@ -155,7 +121,7 @@ __global__ void __launch_bounds__(THREADS) route_rows(const T *__restrict__ logi
         const bool mine = row < rows;
         const bool read = mine && (!valid || valid[row]);
         float l[V][N];
-        Lay::load(logits + (read ? row * parts : 0), lane, read ? parts : 0, -INFINITY, l);
+        Lay::load_if(read, logits + row * parts, lane, parts, -INFINITY, l);
         float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < V; ++j)
@@ -163,17 +129,18 @@ __global__ void __launch_bounds__(THREADS) route_rows(const T *__restrict__ logi
             for (int i = 0; i < N; ++i) top = fmaxf(top, l[j][i]);
         top = reduce_row<L, OpMaxNumber>(top, slots, turn);
         const bool part = top > -INFINITY;   // false for a row of NaN and -infinity alone, too
+        const float shift = part ? top : 0.f;   // (-infinity - 0: the exponentials of a row left out are zero)
         float s = 0.f;
         float e[V][N];
 #pragma unroll
         for (int j = 0; j < V; ++j)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                e[j][i] = part ? __expf(l[j][i] - top) : 0.f;
+                e[j][i] = __expf(l[j][i] - shift);
                 s += e[j][i];
             }
         s = reduce_row<L, OpSum>(s, slots, turn);
-        const float inverse = part ? 1.f / s : 0.f;
+        const float inverse = part ? __fdividef(1.f, s) : 0.f;
 #pragma unroll
         for (int j = 0; j < V; ++j)
 #pragma unroll
@@ -224,7 +191,7 @@ __global__ void __launch_bounds__(THREADS) route_rows(const T *__restrict__ logi
             }
         }
         if (renormalize && mine) {
-            const float scale = part ? 1.f / chosen_sum : 0.f;
+            const float scale = part ? __fdividef(1.f, chosen_sum) : 0.f;
             if (lane < k) weights[row * k + lane] = my_w * scale;
             for (int r = lane + L; r < k; r += L) weights[row * k + r] *= scale;   // this thread's own earlier stores
         }
@@ -267,16 +234,16 @@ __global__ void __launch_bounds__(THREADS) route_rows(const T *__restrict__ logi
 
 // counts[c] and prob[c] over the blocks' shares; column `parts` is the number of rows that took part.  The block that
 // finishes last (the ticket tells) turns the sums into the results.
-__global__ void __launch_bounds__(256) route_fold(const float *__restrict__ part_prob, const int *__restrict__ part_count, int n,
+__global__ void __launch_bounds__(1024) route_fold(const float *__restrict__ part_prob, const int *__restrict__ part_count, int n,
                                                   unsigned *ticket, Finish f) {
-    __shared__ double sp[8][32];
-    __shared__ long long sc[8][32];
+    __shared__ double sp[32][32];
+    __shared__ long long sc[32][32];
     __shared__ bool last;
     const int lane = threadIdx.x & 31, r0 = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     double p = 0.0;
     long long m = 0;
-#pragma unroll 4
-    for (int r = r0; r < n; r += 8) {
+#pragma unroll 8
+    for (int r = r0; r < n; r += 32) {
         if (c < f.parts) p += (double)part_prob[(size_t)r * f.parts + c];
         if (c <= f.parts) m += part_count[(size_t)r * (f.parts + 1) + c];
     }
@@ -284,8 +251,8 @@ __global__ void __launch_bounds__(256) route_fold(const float *__restrict__ part
     sc[r0][lane] = m;
     __syncthreads();
     if (r0 == 0) {
-#pragma unroll
-        for (int q = 1; q < 8; ++q) {
+#pragma unroll 8
+        for (int q = 1; q < 32; ++q) {
             p += sp[q][lane];
             m += sc[q][lane];
         }
@@ -304,7 +271,7 @@ __global__ void __launch_bounds__(256) route_fold(const float *__restrict__ part
     finish_block(f, *(volatile int64_t *)f.routed, &sp[0][0]);
 }
 
-template <typename T, int L, int V, int N, bool VEC>
+template <typename T, typename Lay>
 __global__ void __launch_bounds__(THREADS) route_rows_backward(const T *__restrict__ logits, int64_t rows, int parts, int k,
                                                                const uint8_t *__restrict__ valid, bool renormalize,
                                                                const int32_t *__restrict__ ids,
@@ -313,7 +280,7 @@ __global__ void __launch_bounds__(THREADS) route_rows_backward(const T *__restri
                                                                const float *__restrict__ dweights,
                                                                const float *__restrict__ dloss, T *__restrict__ dlogits,
                                                                int *status) {
-    using Lay = Layout<T, L, V, N, VEC>;
+    constexpr int L = Lay::L, V = Lay::V, N = Lay::N;
     constexpr int GROUPS = THREADS / L;
     __shared__ float slots[L > 32 ? 64 : 1];
     int turn = 0;
@@ -335,9 +302,9 @@ __global__ void __launch_bounds__(THREADS) route_rows_backward(const T *__restri
         const int64_t row = first + group;
         const bool mine = row < rows;
         const bool read = mine && (!valid || valid[row]);
-        const T *from = logits + (read ? row * parts : 0);
+        const T *from = logits + row * parts;
         float p[V][N];
-        Lay::load(from, lane, read ? parts : 0, -INFINITY, p);
+        Lay::load_if(read, from, lane, parts, -INFINITY, p);
         float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < V; ++j)
@@ -345,21 +312,23 @@ __global__ void __launch_bounds__(THREADS) route_rows_backward(const T *__restri
             for (int i = 0; i < N; ++i) top = fmaxf(top, p[j][i]);
         top = reduce_row<L, OpMaxNumber>(top, slots, turn);
         const bool part = top > -INFINITY;
+        const float shift = part ? top : 0.f;
         float s = 0.f, dot = 0.f;
 #pragma unroll
         for (int j = 0; j < V; ++j)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                p[j][i] = part ? __expf(p[j][i] - top) : 0.f;
+                p[j][i] = __expf(p[j][i] - shift);
                 s += p[j][i];
                 dot = fmaf(p[j][i], slope[j][i], dot);
             }
         s = reduce_row<L, OpSum>(s, slots, turn);
         dot = reduce_row<L, OpSum>(dot, slots, turn);
-        const float inverse = part ? 1.f / s : 0.f;
+        const float inverse = part ? __fdividef(1.f, s) : 0.f;
         dot *= inverse;
-        // the slots, shared out over the row's threads: sum of p and of dweights p
-        float chosen = 0.f, pulled = 0.f;
+        // the slots, shared out over the row's threads: sum of p and of dweights p.  A thread keeps its first slot.
+        float chosen = 0.f, pulled = 0.f, first_w = 0.f, first_dw = 0.f;
+        int first_id = -1;
         if (dweights) {
             if (part)
                 for (int q = lane; q < k; q += L) {
@@ -368,9 +337,14 @@ __global__ void __launch_bounds__(THREADS) route_rows_backward(const T *__restri
                         if (id != -1) ep_raise(status, EP_ERR_BAD_INDEX);
                         continue;
                     }
-                    const float w = __expf(to_f32(from[id]) - top) * inverse;
+                    const float w = __expf(to_f32(from[id]) - top) * inverse, dw = dweights[row * k + q];
                     chosen += w;
-                    pulled = fmaf(dweights[row * k + q], w, pulled);
+                    pulled = fmaf(dw, w, pulled);
+                    if (q == lane) {
+                        first_id = id;
+                        first_w = w;
+                        first_dw = dw;
+                    }
                 }
             chosen = reduce_row<L, OpSum>(chosen, slots, turn);
             pulled = reduce_row<L, OpSum>(pulled, slots, turn);
@@ -380,9 +354,9 @@ __global__ void __launch_bounds__(THREADS) route_rows_backward(const T *__restri
 #pragma unroll
         for (int j = 0; j < V; ++j)
 #pragma unroll
-            for (int i = 0; i < N; ++i) p[j][i] = part ? p[j][i] * inverse * (slope[j][i] - back) : 0.f;
-        T *to = dlogits + (mine ? row * parts : 0);
-        Lay::store(to, lane, mine ? parts : 0, p);
+            for (int i = 0; i < N; ++i) p[j][i] *= inverse * (slope[j][i] - back);
+        T *to = dlogits + row * parts;
+        if (mine) Lay::store(to, lane, parts, p);
         if (!dweights) continue;
         // the chosen columns once more, with their slots' terms: over what the row's threads have just stored
         if constexpr (L > 32)
@@ -391,61 +365,17 @@ __global__ void __launch_bounds__(THREADS) route_rows_backward(const T *__restri
             __syncwarp();
         if (part) {
             const float mean = renormalize ? pulled / chosen : 0.f, per = renormalize ? 1.f / chosen : 1.f;
-            for (int q = lane; q < k; q += L) {
-                const int id = ids[row * k + q];
-                if (id < 0 || id >= parts) continue;
-                const float w = __expf(to_f32(from[id]) - top) * inverse;
+            auto again = [&](int id, float w, float dw) {
                 const float own = dloss ? unit * (float)counts[id] : 0.f;
-                to[id] = from_f32<T>(w * (own + (dweights[row * k + q] - mean) * per - back));
+                to[id] = from_f32<T>(w * (own + (dw - mean) * per - back));
+            };
+            if (first_id >= 0) again(first_id, first_w, first_dw);
+            for (int q = lane + L; q < k; q += L) {
+                const int id = ids[row * k + q];
+                if (id >= 0 && id < parts) again(id, __expf(to_f32(from[id]) - top) * inverse, dweights[row * k + q]);
             }
         }
     }
-}
-
-// About 16 columns per thread: fewer steps of the sums across threads, and still enough loads in flight (2449029 rows
-// of 32 fp32 logits: 8 threads of 4 columns 218 us, 2 threads of 16 columns 80 us).  Rows that 16-byte accesses do not
-// fit (the second list) take more threads, so that a warp's accesses stay close together.
-template <typename T, typename F>
-int with_layout(int parts, bool vec, F f) {
-    constexpr int N = 16 / (int)sizeof(T);
-    const int chunks = (parts + N - 1) / N;
-    if (vec) {
-        if constexpr (sizeof(T) == 4) {
-            if (chunks <= 1) return f.template run<1, 1, N, true>();
-            if (chunks <= 4) return f.template run<1, 4, N, true>();
-            if (chunks <= 8) return f.template run<2, 4, N, true>();
-            if (chunks <= 16) return f.template run<4, 4, N, true>();
-            if (chunks <= 32) return f.template run<8, 4, N, true>();
-            if (chunks <= 64) return f.template run<16, 4, N, true>();
-            if (chunks <= 128) return f.template run<32, 4, N, true>();
-            if (chunks <= 256) return f.template run<32, 8, N, true>();
-            if (chunks <= 512) return f.template run<256, 2, N, true>();
-            return f.template run<256, 4, N, true>();
-        } else {
-            if (chunks <= 1) return f.template run<1, 1, N, true>();
-            if (chunks <= 2) return f.template run<1, 2, N, true>();
-            if (chunks <= 4) return f.template run<2, 2, N, true>();
-            if (chunks <= 8) return f.template run<4, 2, N, true>();
-            if (chunks <= 16) return f.template run<8, 2, N, true>();
-            if (chunks <= 32) return f.template run<16, 2, N, true>();
-            if (chunks <= 64) return f.template run<32, 2, N, true>();
-            if (chunks <= 128) return f.template run<32, 4, N, true>();
-            if (chunks <= 256) return f.template run<256, 1, N, true>();
-            return f.template run<256, 2, N, true>();
-        }
-    }
-    if (parts <= 4) return f.template run<1, 1, 4, false>();
-    if (parts <= 16) return f.template run<4, 1, 4, false>();
-    if (parts <= 32) return f.template run<8, 1, 4, false>();
-    if (parts <= 64) return f.template run<16, 1, 4, false>();
-    if (parts <= 128) return f.template run<32, 1, 4, false>();
-    if (parts <= 256) return f.template run<32, 2, 4, false>();
-    if (parts <= 384) return f.template run<32, 3, 4, false>();
-    if (parts <= 512) return f.template run<32, 4, 4, false>();
-    if (parts <= 768) return f.template run<32, 6, 4, false>();
-    if (parts <= 1024) return f.template run<32, 8, 4, false>();
-    if (parts <= 2048) return f.template run<256, 2, 4, false>();
-    return f.template run<256, 4, 4, false>();
 }
 
 int grid_for(const ep_ctx *ctx, int64_t rows, int groups) {
@@ -471,19 +401,20 @@ struct RouteArgs {
 
 template <typename T>
 struct RouteLaunch {
+    static constexpr int MAX_WIDTH = MAX_PARTS;
     RouteArgs &a;
-    template <int L, int V, int N, bool VEC>
+    template <typename Lay>
     int run() const {
-        constexpr int groups = THREADS / L;
-        const size_t smem = sizeof(int) * (size_t)((a.parts + 1 + 3) & ~3) + (groups > 1 ? sizeof(float) * groups * V * L * N : 0);
+        constexpr int groups = THREADS / Lay::L;
+        const size_t smem = sizeof(int) * (size_t)((a.parts + 1 + 3) & ~3) + (groups > 1 ? sizeof(float) * groups * Lay::WIDE : 0);
         const int grid = grid_for(a.ctx, a.rows, groups);
-        route_rows<T, L, V, N, VEC><<<grid, THREADS, smem, a.stream>>>((const T *)a.logits, a.rows, a.parts, a.k, a.valid,
+        route_rows<T, Lay><<<grid, THREADS, smem, a.stream>>>((const T *)a.logits, a.rows, a.parts, a.k, a.valid,
                                                                        a.renormalize, a.ids, a.weights, a.part_prob, a.part_count,
                                                                        a.ticket, a.fin);
         EP_CUDA(a.ctx, cudaGetLastError());
         a.kernels = 1;
         if (grid > 1) {
-            route_fold<<<a.parts / 32 + 1, 256, 0, a.stream>>>(a.part_prob, a.part_count, grid, a.ticket, a.fin);
+            route_fold<<<a.parts / 32 + 1, 1024, 0, a.stream>>>(a.part_prob, a.part_count, grid, a.ticket, a.fin);
             EP_CUDA(a.ctx, cudaGetLastError());
             a.kernels = 2;
         }
@@ -507,10 +438,11 @@ struct RouteBackArgs {
 
 template <typename T>
 struct RouteBackLaunch {
+    static constexpr int MAX_WIDTH = MAX_PARTS;
     const RouteBackArgs &a;
-    template <int L, int V, int N, bool VEC>
+    template <typename Lay>
     int run() const {
-        route_rows_backward<T, L, V, N, VEC><<<grid_for(a.ctx, a.rows, THREADS / L), THREADS, 0, a.stream>>>(
+        route_rows_backward<T, Lay><<<grid_for(a.ctx, a.rows, THREADS / Lay::L), THREADS, 0, a.stream>>>(
             (const T *)a.logits, a.rows, a.parts, a.k, a.valid, a.renormalize, a.ids, a.counts, a.routed, a.dweights, a.dloss,
             (T *)a.dlogits, a.ctx->d_status);
         EP_CUDA(a.ctx, cudaGetLastError());

@@ -143,4 +143,124 @@ __device__ __forceinline__ float reduce_row(float v, float *slots, int &turn) {
     return v;
 }
 
+// ---- how a row lies over the L threads that share it ------------------------------------------------
+// V x N columns to each thread.  VEC: chunks of N columns (16 bytes of the input type) dealt out in turn; every row
+// starts on a 16-byte boundary and holds whole chunks.  Otherwise single columns dealt out in turn, so that neighbouring
+// lanes access neighbouring elements wherever the row starts.  Rows have more than LOW columns: what lies below is not
+// checked against the row's end.
+template <int L_, int V_, int N_, bool VEC_, int LOW_>
+struct Layout {
+    static constexpr int L = L_, V = V_, N = N_, WIDE = L_ * V_ * N_;
+    static constexpr bool VEC = VEC_;
+    static __device__ __forceinline__ int col(int lane, int j, int i) {
+        return VEC ? (j * L + lane) * N + i : (j * N + i) * L + lane;
+    }
+    static __device__ __forceinline__ bool inside(int lane, int j, int i, int width) {
+        return (VEC ? (j + 1) * L * N : (j * N + i + 1) * L) <= LOW_ || col(lane, j, i) < width;
+    }
+    template <typename T>
+    static __device__ __forceinline__ void load(const T *row, int lane, int width, float fill, float (&v)[V_][N_]) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if constexpr (VEC) {
+                if (inside(lane, j, 0, width))
+                    load_chunk(row, col(lane, j, 0), 1 << 30, true, fill, v[j]);
+                else {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) v[j][i] = fill;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[j][i] = inside(lane, j, i, width) ? to_f32(row[col(lane, j, i)]) : fill;
+            }
+        }
+    }
+    template <typename T>
+    static __device__ __forceinline__ void store(T *row, int lane, int width, const float (&v)[V_][N_]) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if constexpr (VEC) {
+                if (inside(lane, j, 0, width)) store_chunk(row, col(lane, j, 0), 1 << 30, true, v[j]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (inside(lane, j, i, width)) row[col(lane, j, i)] = from_f32<T>(v[j][i]);
+            }
+        }
+    }
+    // A row that is not there (or is not to be read) is all `fill`.
+    template <typename T>
+    static __device__ __forceinline__ void load_if(bool there, const T *row, int lane, int width, float fill, float (&v)[V_][N_]) {
+        if (there)
+            load(row, lane, width, fill, v);
+        else
+            set(fill, v);
+    }
+    static __device__ __forceinline__ void set(float fill, float (&v)[V_][N_]) {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[j][i] = fill;
+    }
+};
+
+// Calls f.run<Layout>() with the layout for rows of `width` elements of T.  About 16 columns per thread: fewer steps of
+// the sums across threads than with one chunk each, and as many loads in flight.
+template <typename T, typename F>
+int with_layout(int width, bool vec, F f) {
+    constexpr int N = 16 / (int)sizeof(T);
+    if (vec) {
+        if constexpr (sizeof(T) == 4) {
+            if (width <= 4) return f.template run<Layout<1, 1, N, true, 0>>();
+            if (width <= 16) return f.template run<Layout<1, 4, N, true, 4>>();
+            if (width <= 32) return f.template run<Layout<2, 4, N, true, 16>>();
+            if (width <= 64) return f.template run<Layout<4, 4, N, true, 32>>();
+            if (width <= 128) return f.template run<Layout<8, 4, N, true, 64>>();
+            if (width <= 256) return f.template run<Layout<16, 4, N, true, 128>>();
+            if (width <= 512) return f.template run<Layout<32, 4, N, true, 256>>();
+            if (width <= 1024) return f.template run<Layout<32, 8, N, true, 512>>();
+            if (width <= 2048) return f.template run<Layout<256, 2, N, true, 1024>>();
+            if (width <= 4096) return f.template run<Layout<256, 4, N, true, 2048>>();
+            if constexpr (F::MAX_WIDTH > 4096) {
+                if (width <= 8192) return f.template run<Layout<512, 4, N, true, 4096>>();
+                return f.template run<Layout<512, 8, N, true, 8192>>();
+            }
+        } else {
+            if (width <= 8) return f.template run<Layout<1, 1, N, true, 0>>();
+            if (width <= 16) return f.template run<Layout<1, 2, N, true, 8>>();
+            if (width <= 32) return f.template run<Layout<2, 2, N, true, 16>>();
+            if (width <= 64) return f.template run<Layout<4, 2, N, true, 32>>();
+            if (width <= 128) return f.template run<Layout<8, 2, N, true, 64>>();
+            if (width <= 256) return f.template run<Layout<16, 2, N, true, 128>>();
+            if (width <= 512) return f.template run<Layout<32, 2, N, true, 256>>();
+            if (width <= 1024) return f.template run<Layout<32, 4, N, true, 512>>();
+            if (width <= 2048) return f.template run<Layout<256, 1, N, true, 1024>>();
+            if (width <= 4096) return f.template run<Layout<256, 2, N, true, 2048>>();
+            if constexpr (F::MAX_WIDTH > 4096) {
+                if (width <= 8192) return f.template run<Layout<256, 4, N, true, 4096>>();
+                return f.template run<Layout<512, 4, N, true, 8192>>();
+            }
+        }
+        return 0;
+    }
+    if (width <= 4) return f.template run<Layout<1, 1, 4, false, 0>>();
+    if (width <= 16) return f.template run<Layout<2, 2, 4, false, 4>>();
+    if (width <= 32) return f.template run<Layout<4, 2, 4, false, 16>>();
+    if (width <= 64) return f.template run<Layout<8, 2, 4, false, 32>>();
+    if (width <= 128) return f.template run<Layout<8, 4, 4, false, 64>>();
+    if (width <= 192) return f.template run<Layout<16, 3, 4, false, 128>>();
+    if (width <= 256) return f.template run<Layout<16, 4, 4, false, 192>>();
+    if (width <= 320) return f.template run<Layout<16, 5, 4, false, 256>>();
+    if (width <= 512) return f.template run<Layout<32, 4, 4, false, 320>>();
+    if (width <= 768) return f.template run<Layout<32, 6, 4, false, 512>>();
+    if (width <= 1024) return f.template run<Layout<32, 8, 4, false, 768>>();
+    if (width <= 2048) return f.template run<Layout<256, 2, 4, false, 1024>>();
+    if (width <= 4096) return f.template run<Layout<256, 4, 4, false, 2048>>();
+    if constexpr (F::MAX_WIDTH > 4096) {
+        if (width <= 8192) return f.template run<Layout<512, 4, 4, false, 4096>>();
+        return f.template run<Layout<512, 8, 4, false, 8192>>();
+    }
+    return 0;
+}
+
 }  // namespace eprow
