@@ -19,35 +19,24 @@ constexpr int block_threads() { return L > 32 ? L : 256; }
 
 constexpr float E4M3_TOP = 448.f;
 
-// rho = 1 / sqrt(mean(h^2) + eps) of a row.  Where the fp32 squares leave the range that is safe for their sum (a row of
-// magnitudes below 1e-15 or above 1e18, or of zeros) they are taken of the row times a power of two instead; all
-// threads that reduce together take that turn together.  A row of zeros with eps = 0 has rho = 0, so that it stays zero.
-template <int L, int V, int N>
-__device__ __forceinline__ float row_rho(const float (&h)[V][N], int d, float eps, float *slots, int &turn) {
-    float ss = 0.f;
-#pragma unroll
-    for (int j = 0; j < V; ++j)
-#pragma unroll
-        for (int i = 0; i < N; ++i) ss = fmaf(h[j][i], h[j][i], ss);
-    const float per_column = 1.f / (float)d;
+// rho = 1 / sqrt(mean(h^2) + eps) of a row, from this thread's share `ss` of the sum of squares.  Where the fp32 squares
+// leave the range that is safe for their sum (a row of magnitudes below 1e-15 or above 1e18, or of zeros) they are taken
+// of the row times a power of two instead; all threads that reduce together take that turn together.  A row of zeros
+// with eps = 0 has rho = 0, so that it stays zero.  each(f) calls f with every h of this thread.
+template <int L, typename Each>
+__device__ __forceinline__ float row_rho(float ss, float per_column, float eps, float *slots, int &turn, Each each) {
     const float mean = reduce_row<L, OpSum>(ss, slots, turn) * per_column;
     float rho = rsqrtf(mean + eps);
     const bool rare = !(mean + eps > 1e-30f && mean < 1e36f);
     if (__any_sync(FULL, rare)) {
         float top = 0.f;
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-#pragma unroll
-            for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(h[j][i]));
+        each([&](float h) { top = fmaxf(top, fabsf(h)); });
         top = reduce_row<L, OpMaxNumber>(top, slots, turn);
         // (with eps > 0 magnitudes below 2^-87 do not count beside it; 2^60 keeps eps s^2 finite)
         const int up = min(max(-ilogbf(fmaxf(top, 1.17549435e-38f)), -100), eps > 0.f ? 60 : 126);
         const float s = scalbnf(1.f, up);
         ss = 0.f;
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-#pragma unroll
-            for (int i = 0; i < N; ++i) ss = fmaf(h[j][i] * s, h[j][i] * s, ss);
+        each([&](float h) { ss = fmaf(h * s, h * s, ss); });
         const float scaled = reduce_row<L, OpSum>(ss, slots, turn) * per_column + eps * s * s;
         if (rare && scaled == 0.f)
             rho = 0.f;
@@ -91,7 +80,15 @@ __global__ void __launch_bounds__(block_threads<Lay::L>()) norm_rows(const T *x,
         }
         if (NORM && hidden && mine) Lay::store(hidden + at, lane, d, h);
         if (NORM) {
-            const float rho = row_rho<L>(h, d, eps, slots, turn);
+            float ss = 0.f;
+            auto each = [&](auto f) {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) f(h[j][i]);
+            };
+            each([&](float v) { ss = fmaf(v, v, ss); });
+            const float rho = row_rho<L>(ss, 1.f / (float)d, eps, slots, turn, each);
 #pragma unroll
             for (int j = 0; j < V; ++j)
 #pragma unroll
@@ -117,18 +114,28 @@ __global__ void __launch_bounds__(block_threads<Lay::L>()) norm_rows(const T *x,
     }
 }
 
+// How many rows a thread's copies run ahead of it, plus one.  Three rows of three inputs keep 50 to 150 KB in flight per
+// SM whatever the registers allow (without the copies: 2449029 x 128 bf16 in 605 us, half of the memory's rate).  1: rows
+// too wide for it, or not in 16-byte chunks, are read straight into registers.
+template <typename Lay>
+constexpr int stages() { return !Lay::VEC || block_threads<Lay::L>() > 256 || Lay::V > 4 ? 1 : Lay::V > 2 ? 2 : 3; }
+template <typename T, typename D, typename Lay>
+constexpr size_t ring_bytes() { return stages<Lay>() == 1 ? 0 : (size_t)stages<Lay>() * 3 * Lay::V * block_threads<Lay::L>() * 16; }
+
 // dx of every row; the block's share of dweight goes to part[blockIdx.x][d] (or to dweight itself when it is alone).
 template <typename T, typename D, typename Lay>
 __global__ void __launch_bounds__(block_threads<Lay::L>()) norm_rows_backward(const D *dout, const T *hidden, const void *weight,
                                                                               int weight_type, const T *dhidden, int64_t rows,
                                                                               int d, float eps, T *dx, float *part) {
-    constexpr int L = Lay::L, V = Lay::V, N = Lay::N;
-    constexpr int GROUPS = block_threads<L>() / L;
+    constexpr int L = Lay::L, V = Lay::V, N = Lay::N, S = stages<Lay>();
+    constexpr int THREADS = block_threads<L>(), GROUPS = THREADS / L;
     __shared__ float slots[L > 32 ? 64 : 1];
-    extern __shared__ float fold[];   // [GROUPS][V * L * N] where GROUPS > 1
+    extern __shared__ uint4 ring[];                        // [S][3][V][THREADS]
+    float *fold = reinterpret_cast<float *>(ring);         // then [GROUPS][V * L * N] where GROUPS > 1
     int turn = 0;
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
     const float per_column = 1.f / (float)d;
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
     float g[V][N], dg[V][N];
 #pragma unroll
     for (int j = 0; j < V; ++j)
@@ -138,29 +145,90 @@ __global__ void __launch_bounds__(block_threads<Lay::L>()) norm_rows_backward(co
             g[j][i] = weight && c < d ? load_param(weight, weight_type, c) : 1.f;
             dg[j][i] = 0.f;
         }
-    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += (int64_t)gridDim.x * GROUPS) {
-        const int64_t row = first + group, at = row * d;
+    auto fetch = [&](int64_t row, int s) {
+        uint4 *to = ring + (size_t)s * 3 * V * THREADS + threadIdx.x;
+        if (row < rows) {
+            copy_row<Lay>(to, THREADS, hidden + row * d, lane, d);
+            copy_row<Lay>(to + V * THREADS, THREADS, dout + row * d, lane, d);
+            if (dhidden) copy_row<Lay>(to + 2 * V * THREADS, THREADS, dhidden + row * d, lane, d);
+        }
+        copies_end_group();
+    };
+    // the gradient of one row, from its chunks: called the same by all threads of a warp
+    auto work = [&](int64_t row, auto hj, auto yj, auto oj) {
         const bool mine = row < rows;
-        float h[V][N], y[V][N], o[V][N];   // all three on their way before the first sum
-        Lay::load_if(mine, hidden + at, lane, d, 0.f, h);
-        Lay::load_if(mine, dout + at, lane, d, 0.f, y);
-        Lay::load_if(mine && dhidden, dhidden + at, lane, d, 0.f, o);
-        float ah = 0.f;
+        float ss = 0.f, ah = 0.f;
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-#pragma unroll
-            for (int i = 0; i < N; ++i) ah = fmaf(y[j][i] * g[j][i], h[j][i], ah);
-        const float rho = row_rho<L>(h, d, eps, slots, turn);
-        const float back = rho * (reduce_row<L, OpSum>(ah, slots, turn) * per_column);
-#pragma unroll
-        for (int j = 0; j < V; ++j)
+        for (int j = 0; j < V; ++j) {
+            float h[N], y[N];
+            hj(j, h);
+            yj(j, y);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float unit = h[j][i] * rho;
-                o[j][i] = fmaf(rho, y[j][i] * g[j][i] - unit * back, o[j][i]);
-                dg[j][i] = fmaf(y[j][i], unit, dg[j][i]);
+                ss = fmaf(h[i], h[i], ss);
+                ah = fmaf(y[i] * g[j][i], h[i], ah);
             }
-        if (mine) Lay::store(dx + at, lane, d, o);
+        }
+        const float rho = row_rho<L>(ss, per_column, eps, slots, turn, [&](auto f) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                float h[N];
+                hj(j, h);
+#pragma unroll
+                for (int i = 0; i < N; ++i) f(h[i]);
+            }
+        });
+        const float back = rho * (reduce_row<L, OpSum>(ah, slots, turn) * per_column);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float h[N], y[N], o[N];
+            hj(j, h);
+            yj(j, y);
+            oj(j, o);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float unit = h[i] * rho;
+                o[i] = fmaf(rho, y[i] * g[j][i] - unit * back, o[i]);
+                dg[j][i] = fmaf(y[i], unit, dg[j][i]);
+            }
+            if (mine) Lay::store_part(dx + row * d, lane, j, d, o);
+        }
+    };
+    if constexpr (S > 1) {
+        int64_t ahead = (int64_t)blockIdx.x * GROUPS + group;
+#pragma unroll
+        for (int s = 0; s < S - 1; ++s, ahead += step) fetch(ahead, s);
+        int s = 0;
+        for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += step, ahead += step) {
+            fetch(ahead, s == 0 ? S - 1 : s - 1);   // into the slots of the row before
+            copies_wait<S - 1>();
+            const uint4 *from = ring + (size_t)s * 3 * V * THREADS + threadIdx.x;
+            const int64_t row = first + group;
+            const bool mine = row < rows;
+            work(
+                row, [&](int j, float(&v)[N]) { copied_chunk<Lay, T>(from, THREADS, mine, lane, j, d, 0.f, v); },
+                [&](int j, float(&v)[N]) { copied_chunk<Lay, D>(from + V * THREADS, THREADS, mine, lane, j, d, 0.f, v); },
+                [&](int j, float(&v)[N]) { copied_chunk<Lay, T>(from + 2 * V * THREADS, THREADS, mine && dhidden, lane, j, d, 0.f, v); });
+            s = s + 1 == S ? 0 : s + 1;
+        }
+        copies_wait<0>();
+        __syncthreads();   // the ring becomes the fold
+    } else {
+        for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += step) {
+            const int64_t row = first + group, at = row * d;
+            const bool mine = row < rows;
+            float h[V][N], y[V][N], o[V][N];
+            Lay::load_if(mine, hidden + at, lane, d, 0.f, h);
+            Lay::load_if(mine, dout + at, lane, d, 0.f, y);
+            Lay::load_if(mine && dhidden, dhidden + at, lane, d, 0.f, o);
+            auto held = [](const float(&a)[V][N]) {
+                return [&a](int j, float(&v)[N]) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) v[i] = a[j][i];
+                };
+            };
+            work(row, held(h), held(y), held(o));
+        }
     }
     if (!part) return;
     float *to = part + (size_t)blockIdx.x * d;
@@ -185,9 +253,9 @@ __global__ void __launch_bounds__(block_threads<Lay::L>()) norm_rows_backward(co
     }
 }
 
-// A block sums 32 columns: 32 x 32 threads, thread (c, r) the rows r, r + 32, ... in fp64; then the 32 in order.
+// A block sums 32 columns: 32 x 32 threads, thread (c, r) the rows r, r + 32, ... in fp64; then a warp per column.
 __global__ void __launch_bounds__(1024) fold_partials(const float *__restrict__ parts, int n, int cols, float *__restrict__ out) {
-    __shared__ double s[32][32];
+    __shared__ double s[32][33];
     const int lane = threadIdx.x & 31, r0 = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;
     double t = 0.0;
@@ -196,11 +264,10 @@ __global__ void __launch_bounds__(1024) fold_partials(const float *__restrict__ 
         for (int r = r0; r < n; r += 32) t += (double)parts[(size_t)r * cols + c];
     s[r0][lane] = t;
     __syncthreads();
-    if (r0 == 0 && c < cols) {
-#pragma unroll 8
-        for (int q = 1; q < 32; ++q) t += s[q][lane];
-        out[c] = (float)t;
-    }
+    t = s[lane][r0];   // a warp per column now
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) t += __shfl_xor_sync(FULL, t, o);
+    if (lane == 0 && blockIdx.x * 32 + r0 < cols) out[blockIdx.x * 32 + r0] = (float)t;
 }
 
 constexpr int MAX_D = 16384;
@@ -276,9 +343,12 @@ struct BackLaunch {
     template <typename Lay>
     int run() const {
         constexpr int threads = block_threads<Lay::L>();
-        constexpr size_t smem = threads == Lay::L ? 0 : sizeof(float) * (threads / Lay::L) * Lay::WIDE;
+        constexpr size_t fold = threads == Lay::L ? 0 : sizeof(float) * (threads / Lay::L) * Lay::WIDE;
+        constexpr size_t smem = std::max(fold, ring_bytes<T, D, Lay>());
         const int grid = grid_for<Lay::L>(a.ctx, a.rows, BACKWARD_BLOCKS_PER_SM);
         float *part = !a.dweight ? nullptr : grid == 1 ? a.dweight : a.parts;
+        if (smem > 48 * 1024)
+            EP_CUDA(a.ctx, cudaFuncSetAttribute(norm_rows_backward<T, D, Lay>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
         norm_rows_backward<T, D, Lay><<<grid, threads, smem, a.stream>>>((const D *)a.dout, (const T *)a.hidden, a.weight,
                                                                          a.weight_type, (const T *)a.dhidden, a.rows, a.d, a.eps,
                                                                          (T *)a.dx, part);

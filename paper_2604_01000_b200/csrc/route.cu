@@ -91,19 +91,26 @@ __device__ void finish_block(const Finish &f, int64_t rows_routed, double *red) 
     }
 }
 
+// Rows in flight per thread (see the ring in rows.cuh); 1: read straight into registers.
+template <typename Lay>
+constexpr int stages() { return !Lay::VEC ? 1 : 3; }
+template <typename Lay>
+constexpr size_t ring_bytes() { return stages<Lay>() == 1 ? 0 : (size_t)stages<Lay>() * Lay::V * THREADS * 16; }
+
 template <typename T, typename Lay>
 __global__ void __launch_bounds__(THREADS) route_rows(const T *__restrict__ logits, int64_t rows, int parts, int k,
                                                       const uint8_t *__restrict__ valid, bool renormalize,
                                                       int32_t *__restrict__ ids, float *weights,
                                                       float *__restrict__ part_prob, int *__restrict__ part_count,
-                                                      unsigned *ticket, Finish fin) {
+                                                      unsigned *ticket, Finish fin, int hist_at) {
     constexpr int L = Lay::L, V = Lay::V, N = Lay::N, WIDE = Lay::WIDE;
     constexpr int GROUPS = THREADS / L;
     __shared__ float slots[L > 32 ? 64 : 1];
     __shared__ float slot_v[L > 32 ? 16 : 1];
     __shared__ int slot_c[L > 32 ? 16 : 1];
     __shared__ double red[8];
-    extern __shared__ int hist[];   // counts of [parts + 1] (the last: rows that take part), then the fold of the sums
+    extern __shared__ uint4 ring[];   // [S][V][THREADS] chunks on their way, later the fold of the sums; then counts
+    int *hist = reinterpret_cast<int *>(reinterpret_cast<char *>(ring) + hist_at);   // of [parts + 1] (the last: rows that take part)
     int turn = 0, turn_best = 0;
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
     if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;   // of route_fold, which runs after this kernel
@@ -115,13 +122,35 @@ __global__ void __launch_bounds__(THREADS) route_rows(const T *__restrict__ logi
 #pragma unroll
         for (int i = 0; i < N; ++i) sum_p[j][i] = 0.f;
     int took_part = 0;
+    constexpr int S = stages<Lay>();
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    auto fetch = [&](int64_t row, int s) {
+        if (row < rows && (!valid || valid[row]))
+            copy_row<Lay>(ring + (size_t)s * V * THREADS + threadIdx.x, THREADS, logits + row * parts, lane, parts);
+        copies_end_group();
+    };
+    int64_t ahead = (int64_t)blockIdx.x * GROUPS + group;
+    int stage = 0;
+    if constexpr (S > 1) {
+#pragma unroll
+        for (int s = 0; s < S - 1; ++s, ahead += step) fetch(ahead, s);
+    }
 
-    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += (int64_t)gridDim.x * GROUPS) {
+    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += step, ahead += step) {
         const int64_t row = first + group;
         const bool mine = row < rows;
         const bool read = mine && (!valid || valid[row]);
         float l[V][N];
-        Lay::load_if(read, logits + row * parts, lane, parts, -INFINITY, l);
+        if constexpr (S > 1) {
+            fetch(ahead, stage == 0 ? S - 1 : stage - 1);   // into the slots of the row before
+            copies_wait<S - 1>();
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                copied_chunk<Lay, T>(ring + (size_t)stage * V * THREADS + threadIdx.x, THREADS, read, lane, j, parts, -INFINITY, l[j]);
+            stage = stage + 1 == S ? 0 : stage + 1;
+        } else {
+            Lay::load_if(read, logits + row * parts, lane, parts, -INFINITY, l);
+        }
         float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < V; ++j)
@@ -198,9 +227,10 @@ __global__ void __launch_bounds__(THREADS) route_rows(const T *__restrict__ logi
     }
 
     // the block's sums: over its groups in order, then to the workspace or, alone, to the results
+    if constexpr (S > 1) copies_wait<0>();
     if (took_part) atomicAdd(&hist[parts], took_part);
     __syncthreads();
-    float *fold = reinterpret_cast<float *>(hist + ((parts + 1 + 3) & ~3));
+    float *fold = reinterpret_cast<float *>(ring);   // (every thread is past its last copy)
     const bool alone = gridDim.x == 1;
     float *prob_to = alone ? fin.prob : part_prob + (size_t)blockIdx.x * parts;
     if constexpr (GROUPS > 1) {
@@ -236,8 +266,8 @@ __global__ void __launch_bounds__(THREADS) route_rows(const T *__restrict__ logi
 // finishes last (the ticket tells) turns the sums into the results.
 __global__ void __launch_bounds__(1024) route_fold(const float *__restrict__ part_prob, const int *__restrict__ part_count, int n,
                                                   unsigned *ticket, Finish f) {
-    __shared__ double sp[32][32];
-    __shared__ long long sc[32][32];
+    __shared__ double sp[32][33];
+    __shared__ long long sc[32][33];
     __shared__ bool last;
     const int lane = threadIdx.x & 31, r0 = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     double p = 0.0;
@@ -250,16 +280,19 @@ __global__ void __launch_bounds__(1024) route_fold(const float *__restrict__ par
     sp[r0][lane] = p;
     sc[r0][lane] = m;
     __syncthreads();
-    if (r0 == 0) {
-#pragma unroll 8
-        for (int q = 1; q < 32; ++q) {
-            p += sp[q][lane];
-            m += sc[q][lane];
-        }
-        if (c < f.parts) {
-            f.prob[c] = (float)p;
-            f.counts[c] = m;
-        } else if (c == f.parts)
+    p = sp[lane][r0];   // a warp per column now
+    m = sc[lane][r0];
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) {
+        p += __shfl_xor_sync(FULL, p, o);
+        m += __shfl_xor_sync(FULL, m, o);
+    }
+    const int mine = blockIdx.x * 32 + r0;
+    if (lane == 0) {
+        if (mine < f.parts) {
+            f.prob[mine] = (float)p;
+            f.counts[mine] = m;
+        } else if (mine == f.parts)
             *f.routed = m;
         __threadfence();
     }
@@ -406,11 +439,14 @@ struct RouteLaunch {
     template <typename Lay>
     int run() const {
         constexpr int groups = THREADS / Lay::L;
-        const size_t smem = sizeof(int) * (size_t)((a.parts + 1 + 3) & ~3) + (groups > 1 ? sizeof(float) * groups * Lay::WIDE : 0);
+        constexpr size_t hist_at = std::max(ring_bytes<Lay>(), groups > 1 ? sizeof(float) * groups * Lay::WIDE : 0);
+        const size_t smem = hist_at + sizeof(int) * (size_t)(a.parts + 1);
         const int grid = grid_for(a.ctx, a.rows, groups);
+        if (smem > 48 * 1024)
+            EP_CUDA(a.ctx, cudaFuncSetAttribute(route_rows<T, Lay>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
         route_rows<T, Lay><<<grid, THREADS, smem, a.stream>>>((const T *)a.logits, a.rows, a.parts, a.k, a.valid,
                                                                        a.renormalize, a.ids, a.weights, a.part_prob, a.part_count,
-                                                                       a.ticket, a.fin);
+                                                                       a.ticket, a.fin, (int)hist_at);
         EP_CUDA(a.ctx, cudaGetLastError());
         a.kernels = 1;
         if (grid > 1) {

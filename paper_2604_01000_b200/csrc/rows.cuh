@@ -178,14 +178,16 @@ struct Layout {
     template <typename T>
     static __device__ __forceinline__ void store(T *row, int lane, int width, const float (&v)[V_][N_]) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            if constexpr (VEC) {
-                if (inside(lane, j, 0, width)) store_chunk(row, col(lane, j, 0), 1 << 30, true, v[j]);
-            } else {
+        for (int j = 0; j < V; ++j) store_part(row, lane, j, width, v[j]);
+    }
+    template <typename T>
+    static __device__ __forceinline__ void store_part(T *row, int lane, int j, int width, const float (&v)[N_]) {
+        if constexpr (VEC) {
+            if (inside(lane, j, 0, width)) store_chunk(row, col(lane, j, 0), 1 << 30, true, v);
+        } else {
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (inside(lane, j, i, width)) row[col(lane, j, i)] = from_f32<T>(v[j][i]);
-            }
+            for (int i = 0; i < N; ++i)
+                if (inside(lane, j, i, width)) row[col(lane, j, i)] = from_f32<T>(v[i]);
         }
     }
     // A row that is not there (or is not to be read) is all `fill`.
@@ -203,6 +205,41 @@ struct Layout {
             for (int i = 0; i < N; ++i) v[j][i] = fill;
     }
 };
+
+// ---- rows on their way to shared memory ---------------------------------------------------------------
+// A thread's own chunks of a row (VEC layouts), copied asynchronously several rows ahead: each thread reads back only
+// what it copied itself, so nothing has to be synchronised, and the bytes in flight do not cost registers.  `slots` is
+// this thread's first 16-byte slot, slots of one chunk index lie `threads` apart.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void *to, const void *from) {
+    const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to);
+    if constexpr (BYTES == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(from) : "memory");
+    else
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(from), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copies_end_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int PENDING>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
+
+template <typename Lay, typename T>
+__device__ __forceinline__ void copy_row(uint4 *slots, int threads, const T *row, int lane, int width) {
+#pragma unroll
+    for (int j = 0; j < Lay::V; ++j)
+        if (Lay::inside(lane, j, 0, width))
+            copy_async<Lay::N * (int)sizeof(T)>(slots + j * threads, row + Lay::col(lane, j, 0));
+}
+// Chunk j of a row copied by copy_row; `fill` where the row has no such chunk.
+template <typename Lay, typename T>
+__device__ __forceinline__ void copied_chunk(const uint4 *slots, int threads, bool there, int lane, int j, int width, float fill,
+                                             float (&v)[Lay::N]) {
+    if (there && Lay::inside(lane, j, 0, width))
+        load_chunk(reinterpret_cast<const T *>(slots + j * threads), 0, 1 << 30, true, fill, v);
+    else {
+#pragma unroll
+        for (int i = 0; i < Lay::N; ++i) v[i] = fill;
+    }
+}
 
 // Calls f.run<Layout>() with the layout for rows of `width` elements of T.  About 16 columns per thread: fewer steps of
 // the sums across threads than with one chunk each, and as many loads in flight.
