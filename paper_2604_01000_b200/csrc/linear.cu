@@ -34,6 +34,7 @@ struct Epilogue {
     int64_t M;
     int N;
     bool vec;                         // out, preact, residual, bias, scales: 16-byte rows of whole 8-column chunks
+    bool tma;                         // out and preact can be written by TMA, residual, bias and scales read by 16 bytes
     float *share;                     // where a block's share of a split sum goes: [split][M][ld_share] fp32
     int ld_share;
 };
@@ -147,6 +148,73 @@ __device__ __forceinline__ void load_residual(const Epilogue &e, int64_t row, in
     }
 }
 
+// ---------------------------------------------------------------------------------------------- a chunk of the output
+// 32 columns of a warp's 32 rows, one row per lane, are finished in registers and leave through shared memory by TMA,
+// which writes whole lines and cuts off what lies outside the matrix.  (Finished from shared memory in a coalesced
+// order instead, addresses, bounds and types made 18 instructions per element, and the epilogue took longer than the
+// sums and the memory both: 169343 x 128 -> 512 in 137 us.)
+template <typename O>
+struct ChunkStore {
+    static constexpr int G = 16 / (int)sizeof(O);             // columns of a 16-byte piece
+    static constexpr int ROW = 32 * (int)sizeof(O);           // bytes of a row of the chunk: 64 or 128
+    static constexpr int BYTES = 32 * ROW;                    // 2 or 4 KB of the warp's 4 KB
+    static constexpr int SLOTS = 4096 / BYTES;
+    // Where piece c of row r lies: as the swizzle of a TMA box of 64- or 128-byte rows has it (no two lanes that
+    // access a piece each together meet in a bank).
+    static __device__ __forceinline__ int at(int r, int c) { return r * ROW + ((sizeof(O) == 2 ? c ^ ((r >> 1) & 3) : c ^ (r & 7)) << 4); }
+};
+
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, const void *src, int x, int y, int z) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(map), "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// Until at most PENDING of this thread's stores still read shared memory.
+template <int PENDING>
+__device__ __forceinline__ void tma_stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PENDING) : "memory"); }
+
+// One lane's 32 columns into `slot` and out to (x, y, z).  The slot has been free since before `ready` stores.
+template <typename O, int READY>
+__device__ __forceinline__ void store_by_tma(const CUtensorMap *map, char *slot, int lane, int x, int y, int z, const float (&v)[32]) {
+    using C = ChunkStore<O>;
+    if (lane == 0) tma_stores_read<READY>();
+    __syncwarp();
+#pragma unroll
+    for (int c = 0; c < 32 / C::G; ++c) {
+        float w[C::G];
+#pragma unroll
+        for (int i = 0; i < C::G; ++i) w[i] = v[c * C::G + i];
+        store_chunk(reinterpret_cast<O *>(slot + C::at(lane, c)), 0, 1 << 30, true, w);
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    if (lane == 0) tma_store_3d(map, slot, x, y, z);
+}
+
+// v += p[col ..]  or  v *= s p[col ..]: 32 parameters, the same for all lanes.
+template <int G, bool SCALE>
+__device__ __forceinline__ void with_parameters(const void *p, int type, int col, int n, float s, float (&v)[32]) {
+#pragma unroll
+    for (int c = 0; c < 32; c += G) {
+        if (col + c >= n) break;
+        float w[G];
+        if (type == EP_F32)
+            load_chunk(static_cast<const float *>(p) + col, c, 1 << 30, true, 0.f, w);
+        else if (type == EP_BF16)
+            load_chunk(static_cast<const __nv_bfloat16 *>(p) + col, c, 1 << 30, true, 0.f, w);
+        else
+            load_chunk(static_cast<const __half *>(p) + col, c, 1 << 30, true, 0.f, w);
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            if constexpr (SCALE)
+                v[c + i] *= s * w[i];
+            else
+                v[c + i] += w[i];
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------------------------- the tile kernel
 //
 // 128 x BN outputs per tile, one block per SM that goes from tile to tile: warp 8 brings k-blocks (128 bytes along k)
@@ -250,6 +318,8 @@ __device__ __forceinline__ Item item_at(const GemmShape &g, int bn, int64_t i) {
 template <int BN, bool F8, int PARTS, bool RUNS, typename O>
 __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_constant__ CUtensorMap map_a,
                                                                 const __grid_constant__ CUtensorMap map_b,
+                                                                const __grid_constant__ CUtensorMap map_out,
+                                                                const __grid_constant__ CUtensorMap map_z,
                                                                 const GemmShape g, const Epilogue e, int *status) {
     constexpr int B_BYTES = BN * 128;
     constexpr int STAGE_BYTES = PARTS * (A_BYTES + B_BYTES);
@@ -377,60 +447,89 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
         const int quad = warp & 3, half = warp >> 2;   // TMEM lanes 32 quad.. and the columns' half are this warp's
         constexpr int COLS = BN / 2, CHUNKS = COLS / 32;
         float4 *mine = reinterpret_cast<float4 *>(staging + warp * 1024);
+        char *bytes = reinterpret_cast<char *>(mine);
         uint32_t acc = 0;
         bool ok = true;
-        // 32 columns of this warp's 32 rows, one row per lane, through shared memory (16-byte chunk c of row r lies at
-        // c ^ (r & 7)) so that neighbouring lanes finish neighbouring columns
-        auto finish_chunk = [&](const Item &t, int col, const Columns<8> &c, const float (&v)[32]) {
+        using C = ChunkStore<O>;
+        // the residual's chunk, copied ahead into the last slot (which is then not used for stores)
+        char *landing = bytes + (C::SLOTS - 1) * C::BYTES;
+        auto fetch_residual = [&](const Item &t, int col) {
+            constexpr int PER_ROW = 32 / C::G;
+            const int c = lane % PER_ROW;
 #pragma unroll
-            for (int q = 0; q < 8; ++q)
-                mine[lane * 8 + (q ^ (lane & 7))] = make_float4(v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
-            __syncwarp();
-            const int64_t row0 = t.m0 + quad * 32;
+            for (int r = lane / PER_ROW; r < 32; r += 32 / PER_ROW) {
+                const int64_t row = t.m0 + quad * 32 + r;
+                if (row < e.M && col + c * C::G < e.N)
+                    copy_async<16>(landing + C::at(r, c), static_cast<const O *>(e.residual) + row * e.ldr + col + c * C::G);
+            }
+            copies_end_group();
+        };
+        const bool ahead = e.tma && !e.share && e.residual && C::SLOTS > 1;
+        int turn = 0;
+        // One lane's 32 finished sums from column col on.  next: the column of the residual to copy after this one, or -1.
+        auto finish_chunk = [&](const Item &t, int col, int next, float (&v)[32]) {
+            const int64_t row0 = t.m0 + quad * 32, row = row0 + lane;
+            if (row0 >= e.M || col >= e.N) return;
             if (e.share) {
-                float *to = e.share + ((int64_t)t.split * e.M + row0) * e.ld_share;
-                const int cc = lane & 7;
+                store_by_tma<float, 0>(&map_out, bytes, lane, col, (int)row0, t.split, v);
+            } else if (e.tma) {
+                if (e.x_scale) with_parameters<C::G, true>(e.w_scale, EP_F32, col, e.N, row < e.M ? __ldg(e.x_scale + row) : 0.f, v);
+                if (e.bias) with_parameters<C::G, false>(e.bias, e.bias_type, col, e.N, 0.f, v);
+                // slots taken in turn; with a residual the last one is the residual's (where there are two)
+                auto put = [&](const CUtensorMap *map) {
+                    if (C::SLOTS == 1 || ahead)
+                        store_by_tma<O, 0>(map, bytes, lane, col, (int)row0, 0, v);
+                    else {
+                        store_by_tma<O, C::SLOTS - 1>(map, bytes + turn * C::BYTES, lane, col, (int)row0, 0, v);
+                        turn ^= 1;
+                    }
+                };
+                if (e.preact) put(&map_z);
+                activate(v, e.act);
+                if (e.residual) {
+                    if (!ahead) {
+                        if (lane == 0) tma_stores_read<0>();
+                        __syncwarp();
+                        fetch_residual(t, col);
+                    }
+                    copies_wait<0>();
+                    __syncwarp();
 #pragma unroll
-                for (int r = lane >> 3; r < 32; r += 4)
-                    if (row0 + r < e.M && col + cc * 4 < e.ld_share)
-                        *reinterpret_cast<float4 *>(to + (int64_t)r * e.ld_share + col + cc * 4) = mine[r * 8 + (cc ^ (r & 7))];
-            } else if (e.vec) {
-                const int cc = lane & 3;
-                if (col + cc * 8 < e.N) {
-                    // two rows at a time: the code stays small enough for the instruction cache (with all four
-                    // unrolled and the type chosen at run time, waiting for instructions was the largest stall)
-#pragma unroll 2
-                    for (int r = lane >> 2; r < 32; r += 8) {
-                        if (row0 + r >= e.M) break;
-                        float add[8];
-                        load_residual<O>(e, row0 + r, col + cc * 8, add);
-                        const float4 a = mine[r * 8 + ((2 * cc) ^ (r & 7))], b = mine[r * 8 + ((2 * cc + 1) ^ (r & 7))];
-                        float w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-                        finish<O>(e, row0 + r, col + cc * 8, c, w, add);
+                    for (int c = 0; c < 32 / C::G; ++c) {
+                        float w[C::G];
+                        load_chunk(reinterpret_cast<const O *>(landing + C::at(lane, c)), 0, 1 << 30, true, 0.f, w);
+#pragma unroll
+                        for (int i = 0; i < C::G; ++i) v[c * C::G + i] += w[i];
+                    }
+                    __syncwarp();
+                    if (ahead && next >= 0 && next < e.N) fetch_residual(t, next);
+                }
+                put(&map_out);
+            } else {
+                // rows that TMA cannot write: through shared memory (16-byte piece c of row r lies at c ^ (r & 7)), so
+                // that neighbouring lanes finish neighbouring columns
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                    mine[lane * 8 + (q ^ (lane & 7))] = make_float4(v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
+                __syncwarp();
+                if (col + lane < e.N) {
+                    Columns<1> c1;
+                    c1.load(e, col + lane);
+                    const float *flat = reinterpret_cast<const float *>(mine);
+#pragma unroll 1
+                    for (int r = 0; r < 32 && row0 + r < e.M; ++r) {
+                        float w[1] = {flat[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)]}, add[1];
+                        load_residual<O>(e, row0 + r, col + lane, add);
+                        finish<O>(e, row0 + r, col + lane, c1, w, add);
                     }
                 }
-            } else if (col + lane < e.N) {
-                Columns<1> c1;
-                c1.load(e, col + lane);
-                const float *flat = reinterpret_cast<const float *>(mine);
-#pragma unroll 1
-                for (int r = 0; r < 32 && row0 + r < e.M; ++r) {
-                    float w[1] = {flat[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)]}, add[1];
-                    load_residual<O>(e, row0 + r, col + lane, add);
-                    finish<O>(e, row0 + r, col + lane, c1, w, add);
-                }
+                __syncwarp();
             }
-            __syncwarp();
-        };
-        // bias and scales of this thread's columns of a chunk, fetched before the sums are waited for
-        auto columns = [&](int col) {
-            Columns<8> c;
-            if (!e.share && e.vec) c.load(e, col + (lane & 3) * 8);
-            return c;
         };
         for (int64_t i = blockIdx.x; ok && i < g.items; i += gridDim.x) {
             const Item t = item_at(g, BN, i);
             const int col0 = t.n0 + half * COLS;
+            if (ahead && col0 < e.N) fetch_residual(t, col0);   // while the sums are on their way
             if constexpr (RUNS) {
                 float sum[CHUNKS][32];
 #pragma unroll
@@ -465,11 +564,10 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                 }
                 if (!ok) break;
 #pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) finish_chunk(t, col0 + c * 32, columns(col0 + c * 32), sum[c]);
+                for (int c = 0; c < CHUNKS; ++c) finish_chunk(t, col0 + c * 32, c + 1 < CHUNKS ? col0 + (c + 1) * 32 : -1, sum[c]);
             } else {
                 const uint32_t buf = acc & 1u, use = (acc >> 1) & 1u;
                 ++acc;
-                Columns<8> cols = columns(col0);
                 if (!(ok = mbar_wait(&sh->t_full[buf], use, abort_flag))) break;
                 tc_fence_after();
                 const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + buf * ACC_COLS + half * COLS;
@@ -486,11 +584,12 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                     float f[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
-                    finish_chunk(t, col0 + c * 32, cols, f);
-                    if (c + 1 < CHUNKS) cols = columns(col0 + (c + 1) * 32);
+                    finish_chunk(t, col0 + c * 32, c + 1 < CHUNKS ? col0 + (c + 1) * 32 : -1, f);
                 }
             }
         }
+        copies_wait<0>();
+        if (lane == 0) tma_stores_read<0>();   // before the block gives its shared memory back
     }
     __syncthreads();
     if (sh->abort && threadIdx.x == 0) ep_raise(status, EP_ERR_TIMEOUT);
@@ -727,6 +826,23 @@ bool encode_operand(CUtensorMap *map, const Operand &o, bool mn, int box_rows) {
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
+// A matrix [depth][rows][cols] as a warp of the tile kernel writes it: boxes of 32 columns x 32 rows.
+bool encode_result(CUtensorMap *map, void *base, int type, int64_t depth, int64_t rows, int cols, int64_t ld) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t size = (cuuint64_t)ep::type_size(type);
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)depth};
+    const cuuint64_t strides[2] = {(cuuint64_t)ld * size, (cuuint64_t)(ld * rows) * size};
+    const cuuint32_t box[3] = {32, 32, 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUtensorMapDataType t = type == EP_BF16  ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                  : type == EP_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
+                                                   : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+    return fn(map, t, 3, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              size == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 struct GemmPlan {
     int bn, splits;
     bool runs;
@@ -767,29 +883,33 @@ GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, int
     return p;
 }
 
+struct Maps {
+    CUtensorMap a, b, out, z;   // out: of the shares, where the sum is split
+};
+
 template <int BN, bool F8, int PARTS, bool RUNS, typename O>
-int launch_tiles(ep_ctx *ctx, const GemmPlan &p, const CUtensorMap &ma, const CUtensorMap &mb, const Epilogue &e,
+int launch_tiles(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &e,
                  cudaStream_t stream) {
     auto kernel = linear_tiles<BN, F8, PARTS, RUNS, O>;
     EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)GEMM_SMEM));
     const int grid = (int)std::min<int64_t>(p.shape.items, ctx->sm_count);
-    kernel<<<grid, GEMM_THREADS, GEMM_SMEM, stream>>>(ma, mb, p.shape, e, ctx->d_status);
+    kernel<<<grid, GEMM_THREADS, GEMM_SMEM, stream>>>(m.a, m.b, m.out, m.z, p.shape, e, ctx->d_status);
     EP_CUDA(ctx, cudaGetLastError());
     return EP_OK;
 }
 
 // (the type of the output is fp32 exactly where sums are kept in runs)
 template <bool F8, typename O>
-int launch_width(ep_ctx *ctx, const GemmPlan &p, const CUtensorMap &ma, const CUtensorMap &mb, const Epilogue &e, cudaStream_t stream) {
-    return p.bn == 256   ? launch_tiles<256, F8, 1, false, O>(ctx, p, ma, mb, e, stream)
-           : p.bn == 128 ? launch_tiles<128, F8, 1, false, O>(ctx, p, ma, mb, e, stream)
-                         : launch_tiles<64, F8, 1, false, O>(ctx, p, ma, mb, e, stream);
+int launch_width(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &e, cudaStream_t stream) {
+    return p.bn == 256   ? launch_tiles<256, F8, 1, false, O>(ctx, p, m, e, stream)
+           : p.bn == 128 ? launch_tiles<128, F8, 1, false, O>(ctx, p, m, e, stream)
+                         : launch_tiles<64, F8, 1, false, O>(ctx, p, m, e, stream);
 }
 template <bool F8>
-int launch_type(ep_ctx *ctx, const GemmPlan &p, const CUtensorMap &ma, const CUtensorMap &mb, const Epilogue &e, cudaStream_t stream) {
-    return p.runs                   ? launch_tiles<128, F8, 1, true, float>(ctx, p, ma, mb, e, stream)
-           : e.out_type == EP_BF16 ? launch_width<F8, __nv_bfloat16>(ctx, p, ma, mb, e, stream)
-                                    : launch_width<F8, __half>(ctx, p, ma, mb, e, stream);
+int launch_type(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &e, cudaStream_t stream) {
+    return p.runs                   ? launch_tiles<128, F8, 1, true, float>(ctx, p, m, e, stream)
+           : e.out_type == EP_BF16 ? launch_width<F8, __nv_bfloat16>(ctx, p, m, e, stream)
+                                    : launch_width<F8, __half>(ctx, p, m, e, stream);
 }
 
 // D = A B^T by tiles, with the epilogue; `share` is room for the shares of a split sum.  Adds to *kernels.
@@ -800,14 +920,19 @@ int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand
     p.shape.b_mn = b_mn;
     p.shape.idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
                     ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
-    CUtensorMap ma, mb;
-    if (!encode_operand(&ma, a, a_mn, BM) || !encode_operand(&mb, b, b_mn, p.bn))
-        return ep::fail(ctx, EP_ERR_CUDA, "cuTensorMapEncodeTiled failed for a product of %lld x %d", (long long)e.M, e.N);
     e.share = p.splits > 1 ? share : nullptr;
     e.ld_share = p.ld_share;
-    const int rc = a.parts == 3          ? launch_tiles<128, false, 3, true, float>(ctx, p, ma, mb, e, stream)
-                   : a.type == EP_E4M3 ? launch_type<true>(ctx, p, ma, mb, e, stream)
-                                         : launch_type<false>(ctx, p, ma, mb, e, stream);
+    Maps m{};
+    bool ok = encode_operand(&m.a, a, a_mn, BM) && encode_operand(&m.b, b, b_mn, p.bn);
+    if (e.share)
+        ok = ok && encode_result(&m.out, share, EP_F32, p.splits, e.M, p.ld_share, p.ld_share);
+    else if (e.tma)
+        ok = ok && encode_result(&m.out, e.out, e.out_type, 1, e.M, e.N, e.N) &&
+             (!e.preact || encode_result(&m.z, e.preact, e.out_type, 1, e.M, e.N, e.N));
+    if (!ok) return ep::fail(ctx, EP_ERR_CUDA, "cuTensorMapEncodeTiled failed for a product of %lld x %d", (long long)e.M, e.N);
+    const int rc = a.parts == 3          ? launch_tiles<128, false, 3, true, float>(ctx, p, m, e, stream)
+                   : a.type == EP_E4M3 ? launch_type<true>(ctx, p, m, e, stream)
+                                         : launch_type<false>(ctx, p, m, e, stream);
     if (rc != EP_OK) return rc;
     ++*kernels;
     if (p.splits > 1) {
@@ -1018,6 +1143,7 @@ int linear_backward_run(ep_ctx *ctx, const BackwardWorkspace &ws, const void *do
         e.M = rows;
         e.N = n_in;
         e.vec = n_in % 8 == 0 && ep::aligned(dx, 16);
+        e.tma = tma_ready(dx, n_in, in_type);
         if (rc == EP_OK) rc = run_gemm(ctx, ws.dx, dz, false, b, true, e, ws.share, stream, kernels);
         if (rc != EP_OK) return rc;
     }
@@ -1028,6 +1154,7 @@ int linear_backward_run(ep_ctx *ctx, const BackwardWorkspace &ws, const void *do
         e.M = n_out;
         e.N = n_in;
         e.vec = n_in % 8 == 0 && ep::aligned(dweight, 16);
+        e.tma = tma_ready(dweight, n_in, in_type);
         if (rc == EP_OK) rc = run_gemm(ctx, ws.dw, dz, true, b, true, e, ws.share, stream, kernels);
         if (rc != EP_OK) return rc;
     }
@@ -1088,6 +1215,8 @@ int ep_linear(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int64_t ld
     e.vec = n_out % 8 == 0 && aligned(out, 16) && aligned(preact, 16) && aligned(residual, 16) && aligned(bias, 16) &&
             aligned(w_scale, 16) &&
             (!residual || ldr * type_size(out_type) % 16 == 0);
+    e.tma = tma_ready(out, n_out, out_type) && tma_ready(preact, n_out, out_type) && aligned(bias, 16) && aligned(w_scale, 16) &&
+            (!residual || tma_ready(residual, ldr, out_type));
     DeviceGuard guard(ctx->device);
     Timed tm(ctx, static_cast<cudaStream_t>(cuda_stream), EP_TIMER_LINEAR);
     int kernels = 0;
