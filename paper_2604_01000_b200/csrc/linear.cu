@@ -34,7 +34,7 @@ struct Epilogue {
     int64_t M;
     int N;
     bool vec;                         // out, preact, residual, bias, scales: 16-byte rows of whole 8-column chunks
-    bool tma;                         // out and preact can be written by TMA, residual, bias and scales read by 16 bytes
+    bool tma;                         // out and preact can be written by TMA, the residual read by 16 bytes
     float *share;                     // where a block's share of a split sum goes: [split][M][ld_share] fp32
     int ld_share;
 };
@@ -192,29 +192,6 @@ __device__ __forceinline__ void store_by_tma(const CUtensorMap *map, char *slot,
     if (lane == 0) tma_store_3d(map, slot, x, y, z);
 }
 
-// v += p[col ..]  or  v *= s p[col ..]: 32 parameters, the same for all lanes.
-template <int G, bool SCALE>
-__device__ __forceinline__ void with_parameters(const void *p, int type, int col, int n, float s, float (&v)[32]) {
-#pragma unroll
-    for (int c = 0; c < 32; c += G) {
-        if (col + c >= n) break;
-        float w[G];
-        if (type == EP_F32)
-            load_chunk(static_cast<const float *>(p) + col, c, 1 << 30, true, 0.f, w);
-        else if (type == EP_BF16)
-            load_chunk(static_cast<const __nv_bfloat16 *>(p) + col, c, 1 << 30, true, 0.f, w);
-        else
-            load_chunk(static_cast<const __half *>(p) + col, c, 1 << 30, true, 0.f, w);
-#pragma unroll
-        for (int i = 0; i < G; ++i) {
-            if constexpr (SCALE)
-                v[c + i] *= s * w[i];
-            else
-                v[c + i] += w[i];
-        }
-    }
-}
-
 // ---------------------------------------------------------------------------------------------- the tile kernel
 //
 // 128 x BN outputs per tile, one block per SM that goes from tile to tile: warp 8 brings k-blocks (128 bytes along k)
@@ -244,7 +221,9 @@ struct GemmShared {
     uint32_t tmem_base;
     int abort;
 };
-constexpr size_t GEMM_SMEM = 1024 + RING_BYTES + STAGING_BYTES + sizeof(GemmShared);
+constexpr int BIAS_BYTES = EPI_WARPS * 128;       // per warp the bias of a chunk's 32 columns
+constexpr size_t GEMM_SMEM = 1024 + RING_BYTES + STAGING_BYTES + BIAS_BYTES + sizeof(GemmShared);
+static_assert(GEMM_SMEM <= 227 * 1024, "shared memory of a block");
 
 struct GemmShape {
     int64_t M;
@@ -332,7 +311,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
     extern __shared__ char smem_raw[];
     char *ring = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     float *staging = reinterpret_cast<float *>(ring + RING_BYTES);
-    GemmShared *sh = reinterpret_cast<GemmShared *>(ring + RING_BYTES + STAGING_BYTES);
+    GemmShared *sh = reinterpret_cast<GemmShared *>(ring + RING_BYTES + STAGING_BYTES + BIAS_BYTES);
     volatile int *abort_flag = &sh->abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -467,14 +446,40 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
         const bool ahead = e.tma && !e.share && e.residual && C::SLOTS > 1;
         int turn = 0;
         // One lane's 32 finished sums from column col on.  next: the column of the residual to copy after this one, or -1.
-        auto finish_chunk = [&](const Item &t, int col, int next, float (&v)[32]) {
+        // Bias and scale of a chunk's columns, one per lane, fetched before the sums are waited for.
+        struct Lane {
+            float bias, scale;
+        };
+        auto fetch_lane = [&](int col) {
+            Lane p{0.f, 1.f};
+            if (e.tma && !e.share && col + lane < e.N) {
+                if (e.bias) p.bias = load_param(e.bias, e.bias_type, col + lane);
+                if (e.w_scale) p.scale = __ldg(e.w_scale + col + lane);
+            }
+            return p;
+        };
+        float *chunk_bias = reinterpret_cast<float *>(ring + RING_BYTES + STAGING_BYTES) + warp * 32;
+        auto finish_chunk = [&](const Item &t, int col, int next, const Lane &p, float (&v)[32]) {
             const int64_t row0 = t.m0 + quad * 32, row = row0 + lane;
             if (row0 >= e.M || col >= e.N) return;
             if (e.share) {
                 store_by_tma<float, 0>(&map_out, bytes, lane, col, (int)row0, t.split, v);
             } else if (e.tma) {
-                if (e.x_scale) with_parameters<C::G, true>(e.w_scale, EP_F32, col, e.N, row < e.M ? __ldg(e.x_scale + row) : 0.f, v);
-                if (e.bias) with_parameters<C::G, false>(e.bias, e.bias_type, col, e.N, 0.f, v);
+                if (e.x_scale) {
+                    const float xs = row < e.M ? __ldg(e.x_scale + row) : 0.f;
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] *= xs * __shfl_sync(FULL, p.scale, j);
+                }
+                if (e.bias) {
+                    chunk_bias[lane] = p.bias;
+                    __syncwarp();
+#pragma unroll
+                    for (int j = 0; j < 32; j += 4) {
+                        const float4 b = *reinterpret_cast<const float4 *>(chunk_bias + j);
+                        v[j] += b.x, v[j + 1] += b.y, v[j + 2] += b.z, v[j + 3] += b.w;
+                    }
+                    __syncwarp();
+                }
                 // slots taken in turn; with a residual the last one is the residual's (where there are two)
                 auto put = [&](const CUtensorMap *map) {
                     if (C::SLOTS == 1 || ahead)
@@ -530,6 +535,9 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
             const Item t = item_at(g, BN, i);
             const int col0 = t.n0 + half * COLS;
             if (ahead && col0 < e.N) fetch_residual(t, col0);   // while the sums are on their way
+            Lane lanes[CHUNKS];
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) lanes[c] = fetch_lane(col0 + c * 32);
             if constexpr (RUNS) {
                 float sum[CHUNKS][32];
 #pragma unroll
@@ -564,7 +572,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                 }
                 if (!ok) break;
 #pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) finish_chunk(t, col0 + c * 32, c + 1 < CHUNKS ? col0 + (c + 1) * 32 : -1, sum[c]);
+                for (int c = 0; c < CHUNKS; ++c) finish_chunk(t, col0 + c * 32, c + 1 < CHUNKS ? col0 + (c + 1) * 32 : -1, lanes[c], sum[c]);
             } else {
                 const uint32_t buf = acc & 1u, use = (acc >> 1) & 1u;
                 ++acc;
@@ -573,6 +581,10 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                 const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + buf * ACC_COLS + half * COLS;
 #pragma unroll 1
                 for (int c = 0; c < CHUNKS; ++c) {
+                    Lane now = lanes[0];
+#pragma unroll
+                    for (int q = 1; q < CHUNKS; ++q)
+                        if (q == c) now = lanes[q];
                     uint32_t v[32];
                     tmem_ld32_issue(taddr + c * 32, v);
                     tmem_ld_wait(v);
@@ -584,7 +596,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                     float f[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
-                    finish_chunk(t, col0 + c * 32, c + 1 < CHUNKS ? col0 + (c + 1) * 32 : -1, f);
+                    finish_chunk(t, col0 + c * 32, c + 1 < CHUNKS ? col0 + (c + 1) * 32 : -1, now, f);
                 }
             }
         }
@@ -1215,7 +1227,7 @@ int ep_linear(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int64_t ld
     e.vec = n_out % 8 == 0 && aligned(out, 16) && aligned(preact, 16) && aligned(residual, 16) && aligned(bias, 16) &&
             aligned(w_scale, 16) &&
             (!residual || ldr * type_size(out_type) % 16 == 0);
-    e.tma = tma_ready(out, n_out, out_type) && tma_ready(preact, n_out, out_type) && aligned(bias, 16) && aligned(w_scale, 16) &&
+    e.tma = tma_ready(out, n_out, out_type) && tma_ready(preact, n_out, out_type) &&
             (!residual || tma_ready(residual, ldr, out_type));
     DeviceGuard guard(ctx->device);
     Timed tm(ctx, static_cast<cudaStream_t>(cuda_stream), EP_TIMER_LINEAR);
