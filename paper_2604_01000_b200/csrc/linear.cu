@@ -68,7 +68,7 @@ template <int n>
 __device__ __forceinline__ void activate(float (&v)[n], int act) {
     if (act == EP_ACT_RELU) {
 #pragma unroll
-        for (int i = 0; i < n; ++i) v[i] = v[i] > 0.f || v[i] != v[i] ? v[i] : 0.f;
+        for (int i = 0; i < n; ++i) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v[i]));   // (a NaN stays one)
     } else if (act == EP_ACT_GELU) {
 #pragma unroll
         for (int i = 0; i < n; ++i) v[i] = gelu(v[i]);
@@ -153,12 +153,12 @@ __device__ __forceinline__ void load_residual(const Epilogue &e, int64_t row, in
 // which writes whole lines and cuts off what lies outside the matrix.  (Finished from shared memory in a coalesced
 // order instead, addresses, bounds and types made 18 instructions per element, and the epilogue took longer than the
 // sums and the memory both: 169343 x 128 -> 512 in 137 us.)
-template <typename O>
+template <typename O, int ROOM = 4096>
 struct ChunkStore {
     static constexpr int G = 16 / (int)sizeof(O);             // columns of a 16-byte piece
     static constexpr int ROW = 32 * (int)sizeof(O);           // bytes of a row of the chunk: 64 or 128
-    static constexpr int BYTES = 32 * ROW;                    // 2 or 4 KB of the warp's 4 KB
-    static constexpr int SLOTS = 4096 / BYTES;
+    static constexpr int BYTES = 32 * ROW;                    // 2 or 4 KB of the warp's ROOM
+    static constexpr int SLOTS = ROOM / BYTES;
     // Where piece c of row r lies: as the swizzle of a TMA box of 64- or 128-byte rows has it (no two lanes that
     // access a piece each together meet in a bank).
     static __device__ __forceinline__ int at(int r, int c) { return r * ROW + ((sizeof(O) == 2 ? c ^ ((r >> 1) & 3) : c ^ (r & 7)) << 4); }
@@ -205,25 +205,41 @@ __device__ __forceinline__ void store_by_tma(const CUtensorMap *map, char *slot,
 // RUNS: the tensor core's fp32 sums are truncated, which costs up to an ulp of the running sum a step, always
 // downwards (measured: 4e-6 of the result after 256 steps, 2e-7 after 16).  Where the output is fp32, sums therefore
 // run over 4 k-blocks only (16 steps), and the epilogue's threads add the runs to nearest in their registers.
-constexpr int BM = 128;
+//
+// PAIR: two blocks of a cluster (one TPC's two SMs) work on one tile of 256 x BN.  Either keeps 128 rows of A and half of
+// B in its shared memory and 128 rows of the sums in its TMEM; the first one's MMA warp issues for both.  A block then
+// loads half as much of B for the same product: a 128 x 256 tile alone needs 96 bytes a clock from the L2 at full rate.
+constexpr int BM = 128;               // rows of a block
 constexpr int EPI_WARPS = 8;
 constexpr int TMA_WARP = 8, MMA_WARP = 9;
 constexpr int GEMM_THREADS = 320;
 constexpr int A_BYTES = BM * 128;
-constexpr int RING_BYTES = 196608;
-constexpr int STAGING_BYTES = EPI_WARPS * 4096;   // per warp 32 rows x 32 columns of fp32
 constexpr int RUN_KB = 4;
 constexpr int MAX_STAGES = 8;
 constexpr int TMEM_COLS = 512;
+constexpr int BIAS_BYTES = EPI_WARPS * 128;   // per warp the bias of a chunk's 32 columns
 
 struct GemmShared {
     uint64_t full[MAX_STAGES], empty[MAX_STAGES], t_full[2], t_empty[2], drain;
     uint32_t tmem_base;
     int abort;
 };
-constexpr int BIAS_BYTES = EPI_WARPS * 128;       // per warp the bias of a chunk's 32 columns
-constexpr size_t GEMM_SMEM = 1024 + RING_BYTES + STAGING_BYTES + BIAS_BYTES + sizeof(GemmShared);
-static_assert(GEMM_SMEM <= 227 * 1024, "shared memory of a block");
+
+// The shared memory of a block: ring of operand stages, then per epilogue warp room for chunks on their way out.
+template <int BN, int PARTS, bool PAIR>
+struct TileMemory {
+    static constexpr int B_ROWS = PAIR ? BN / 2 : BN;
+    static constexpr int B_BYTES = B_ROWS * 128;
+    static constexpr int STAGE_BYTES = PARTS * (A_BYTES + B_BYTES);
+    static constexpr int WARP_STAGING = PAIR ? 8192 : 4096;
+    static constexpr int STAGING_BYTES = EPI_WARPS * WARP_STAGING;
+    static constexpr int REST = 1024 + STAGING_BYTES + BIAS_BYTES + (int)sizeof(GemmShared);
+    static constexpr int FIT = (227 * 1024 - REST) / STAGE_BYTES;
+    static constexpr int STAGES = FIT < MAX_STAGES ? FIT : MAX_STAGES;
+    static constexpr int RING_BYTES = STAGES * STAGE_BYTES;
+    static constexpr size_t TOTAL = (size_t)REST + RING_BYTES;
+    static_assert(STAGES >= 2 && TOTAL <= 227 * 1024, "shared memory of a block");
+};
 
 struct GemmShape {
     int64_t M;
@@ -237,35 +253,76 @@ struct GemmShape {
 };
 
 // The four K-steps of one k-block.
-template <bool F8>
+#define EP_UMMA_KBLOCK(GROUP, KIND)                                                                                        \
+    asm volatile("{\n.reg .pred pe, pa, pt;\n"                                                                             \
+                 "elect.sync _|pe, 0xffffffff;\n"                                                                          \
+                 "setp.ne.b32 pa, %10, 0;\nsetp.eq.b32 pt, 0, 0;\n"                                                        \
+                 "@pe tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %1, %5, %9, pa;\n"                             \
+                 "@pe tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %2, %6, %9, pt;\n"                             \
+                 "@pe tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %3, %7, %9, pt;\n"                             \
+                 "@pe tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], %4, %8, %9, pt;\n}" ::"r"(d_tmem),             \
+                 "l"(adesc), "l"(a1), "l"(a2), "l"(a3), "l"(bdesc), "l"(b1), "l"(b2), "l"(b3), "r"(idesc),                 \
+                 "r"(accumulate_first)                                                                                     \
+                 : "memory")
+template <bool F8, bool PAIR>
 __device__ __forceinline__ void umma_kblock_elected(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint64_t astep,
                                                     uint64_t bstep, uint32_t idesc, uint32_t accumulate_first) {
     const uint64_t a1 = adesc + astep, a2 = a1 + astep, a3 = a2 + astep;
     const uint64_t b1 = bdesc + bstep, b2 = b1 + bstep, b3 = b2 + bstep;
-    if constexpr (F8)
-        asm volatile(
-            "{\n.reg .pred pe, pa, pt;\n"
-            "elect.sync _|pe, 0xffffffff;\n"
-            "setp.ne.b32 pa, %10, 0;\nsetp.eq.b32 pt, 0, 0;\n"
-            "@pe tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %5, %9, pa;\n"
-            "@pe tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %2, %6, %9, pt;\n"
-            "@pe tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %3, %7, %9, pt;\n"
-            "@pe tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %4, %8, %9, pt;\n}"
-            ::"r"(d_tmem), "l"(adesc), "l"(a1), "l"(a2), "l"(a3), "l"(bdesc), "l"(b1), "l"(b2), "l"(b3), "r"(idesc),
-              "r"(accumulate_first)
-            : "memory");
+    if constexpr (F8 && PAIR)
+        EP_UMMA_KBLOCK("2", "f8f6f4");
+    else if constexpr (F8)
+        EP_UMMA_KBLOCK("1", "f8f6f4");
+    else if constexpr (PAIR)
+        EP_UMMA_KBLOCK("2", "f16");
     else
-        asm volatile(
-            "{\n.reg .pred pe, pa, pt;\n"
-            "elect.sync _|pe, 0xffffffff;\n"
-            "setp.ne.b32 pa, %10, 0;\nsetp.eq.b32 pt, 0, 0;\n"
-            "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %5, %9, pa;\n"
-            "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], %2, %6, %9, pt;\n"
-            "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], %3, %7, %9, pt;\n"
-            "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], %4, %8, %9, pt;\n}"
-            ::"r"(d_tmem), "l"(adesc), "l"(a1), "l"(a2), "l"(a3), "l"(bdesc), "l"(b1), "l"(b2), "l"(b3), "r"(idesc),
-              "r"(accumulate_first)
-            : "memory");
+        EP_UMMA_KBLOCK("1", "f16");
+}
+#undef EP_UMMA_KBLOCK
+
+// Forms for a pair of blocks.  The barrier's address may be the other block's (shared::cluster).
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void cluster_meet() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
+template <bool PAIR>
+__device__ __forceinline__ void load_tile_elected(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+    if constexpr (PAIR)
+        asm volatile("{\n.reg .pred pe;\nelect.sync _|pe, 0xffffffff;\n"
+                     "@pe cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], "
+                     "[%1, {%2, %3, %4}], [%5];\n}" ::"r"(dst),
+                     "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                     : "memory");
+    else
+        asm volatile("{\n.reg .pred pe;\nelect.sync _|pe, 0xffffffff;\n"
+                     "@pe cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], "
+                     "[%1, {%2, %3, %4}], [%5];\n}" ::"r"(dst),
+                     "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                     : "memory");
+}
+// One arrival at the barrier, of both blocks where there are two, when all MMAs issued so far are done.
+template <bool PAIR>
+__device__ __forceinline__ void commit_elected(uint64_t *bar) {
+    if constexpr (PAIR)
+        asm volatile("{\n.reg .pred pe;\nelect.sync _|pe, 0xffffffff;\n"
+                     "@pe tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n}" ::"r"(
+                         smem_u32(bar)),
+                     "h"((uint16_t)3)
+                     : "memory");
+    else
+        umma_commit_elected(bar);
 }
 
 // Shared-memory descriptor of an operand tile, 128-byte swizzle.  K-major: rows of 128 bytes along k, groups of 8 rows
@@ -282,36 +339,39 @@ struct Item {
     int n0, split, kb0, kbn;
 };
 // Tiles of one row of tiles come one after another (they share A, and B stays in the L2); splits outermost.
-__device__ __forceinline__ Item item_at(const GemmShape &g, int bn, int64_t i) {
+__device__ __forceinline__ Item item_at(const GemmShape &g, int bm, int bn, int64_t i) {
     Item t;
     t.split = (int)(i / g.tiles);
     const int64_t tile = i - (int64_t)t.split * g.tiles;
     const int64_t tm = tile / g.tiles_n;
-    t.m0 = tm * BM;
+    t.m0 = tm * bm;
     t.n0 = (int)(tile - tm * g.tiles_n) * bn;
     t.kb0 = t.split * g.kb_per_split;
     t.kbn = min(g.kb_per_split, g.kb - t.kb0);
     return t;
 }
 
-template <int BN, bool F8, int PARTS, bool RUNS, typename O>
+template <int BN, bool F8, int PARTS, bool RUNS, bool PAIR, typename O>
 __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_constant__ CUtensorMap map_a,
                                                                 const __grid_constant__ CUtensorMap map_b,
                                                                 const __grid_constant__ CUtensorMap map_out,
                                                                 const __grid_constant__ CUtensorMap map_z,
                                                                 const GemmShape g, const Epilogue e, int *status) {
-    constexpr int B_BYTES = BN * 128;
-    constexpr int STAGE_BYTES = PARTS * (A_BYTES + B_BYTES);
-    constexpr int STAGES = RING_BYTES / STAGE_BYTES < MAX_STAGES ? RING_BYTES / STAGE_BYTES : MAX_STAGES;
+    using Mem = TileMemory<BN, PARTS, PAIR>;
+    constexpr int B_BYTES = Mem::B_BYTES, STAGE_BYTES = Mem::STAGE_BYTES, STAGES = Mem::STAGES;
     constexpr int ACC_COLS = BN * (PARTS == 3 ? 2 : 1);
     constexpr int KE = F8 ? 128 : 64;   // elements of k in a k-block
-    static_assert(STAGES >= 2 && 2 * ACC_COLS <= TMEM_COLS, "ring and accumulators");
+    constexpr int TILE_M = PAIR ? 2 * BM : BM;
+    static_assert(2 * ACC_COLS <= TMEM_COLS, "accumulators");
     static_assert(PARTS == 1 || RUNS, "the split product is summed in runs");
 
     extern __shared__ char smem_raw[];
     char *ring = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    float *staging = reinterpret_cast<float *>(ring + RING_BYTES);
-    GemmShared *sh = reinterpret_cast<GemmShared *>(ring + RING_BYTES + STAGING_BYTES + BIAS_BYTES);
+    char *staging = ring + Mem::RING_BYTES;
+    char *biases = staging + Mem::STAGING_BYTES;
+    GemmShared *sh = reinterpret_cast<GemmShared *>(biases + BIAS_BYTES);
+    const uint32_t rank = PAIR ? cluster_rank() : 0;     // rank 0 issues the MMAs
+    const int64_t worker = PAIR ? blockIdx.x >> 1 : blockIdx.x, workers = PAIR ? gridDim.x >> 1 : gridDim.x;
     volatile int *abort_flag = &sh->abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -322,20 +382,28 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&sh->t_full[b], 1);
-            mbar_init(&sh->t_empty[b], EPI_WARPS);
+            mbar_init(&sh->t_empty[b], PAIR ? 2 * EPI_WARPS : EPI_WARPS);   // (of both blocks, at the first one's)
         }
         mbar_init(&sh->drain, 1);
         sh->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)),
-                     "r"(TMEM_COLS)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if constexpr (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)),
+                         "r"(TMEM_COLS)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)),
+                         "r"(TMEM_COLS)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
     tc_fence_before();
     __syncthreads();
+    if constexpr (PAIR) cluster_meet();   // the other block's barriers are ready
     tc_fence_after();
     const uint32_t tmem_base = sh->tmem_base;
 
@@ -343,31 +411,33 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
         uint32_t it = 0, s = 0, ph = 0;
         bool ok = true;
         const uint32_t ring_base = smem_u32(ring);
-        for (int64_t i = blockIdx.x; ok && i < g.items; i += gridDim.x) {
-            const Item t = item_at(g, BN, i);
+        for (int64_t i = worker; ok && i < g.items; i += workers) {
+            const Item t = item_at(g, TILE_M, BN, i);
+            const int m = (int)t.m0 + (int)rank * BM, n = t.n0 + (int)rank * Mem::B_ROWS;   // this block's rows of A and of B
             for (int kb = 0; kb < t.kbn; ++kb, ++it) {
                 if (!(ok = __all_sync(FULL, mbar_wait(&sh->empty[s], ph ^ 1u, abort_flag)))) break;
-                mbar_expect_tx_elected(&sh->full[s], STAGE_BYTES);
+                if (rank == 0) mbar_expect_tx_elected(&sh->full[s], (PAIR ? 2 : 1) * STAGE_BYTES);
+                const uint32_t bar = PAIR ? in_block(smem_u32(&sh->full[s]), 0) : smem_u32(&sh->full[s]);
                 const int k = (t.kb0 + kb) * KE;
                 uint32_t dst = ring_base + s * (uint32_t)STAGE_BYTES;
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p, dst += A_BYTES) {
                     if (!g.a_mn)
-                        tma_load_3d_elected(dst, &map_a, k, (int)t.m0, p, &sh->full[s]);
+                        load_tile_elected<PAIR>(dst, &map_a, k, m, p, bar);
                     else {
 #pragma unroll
                         for (int b = 0; b < BM / 64; ++b)
-                            tma_load_3d_elected(dst + b * 8192, &map_a, (int)t.m0 + 64 * b, k, p, &sh->full[s]);
+                            load_tile_elected<PAIR>(dst + b * 8192, &map_a, m + 64 * b, k, p, bar);
                     }
                 }
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p, dst += B_BYTES) {
                     if (!g.b_mn)
-                        tma_load_3d_elected(dst, &map_b, k, t.n0, p, &sh->full[s]);
+                        load_tile_elected<PAIR>(dst, &map_b, k, n, p, bar);
                     else {
 #pragma unroll
-                        for (int b = 0; b < BN / 64; ++b)
-                            tma_load_3d_elected(dst + b * 8192, &map_b, t.n0 + 64 * b, k, p, &sh->full[s]);
+                        for (int b = 0; b < Mem::B_ROWS / 64; ++b)
+                            load_tile_elected<PAIR>(dst + b * 8192, &map_b, n + 64 * b, k, p, bar);
                     }
                 }
                 if (++s == (uint32_t)STAGES) {
@@ -376,8 +446,9 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                 }
             }
         }
-        // after an abort the loads already issued get time to land before the block leaves
-        if (lane == 0 && (!ok || *abort_flag))
+        // after an abort the loads already issued get time to land before the block leaves (those of a pair all count at
+        // the first block's barriers, and neither leaves before the other)
+        if (rank == 0 && lane == 0 && (!ok || *abort_flag))
 #pragma unroll 1
             for (uint32_t j = it > (uint32_t)STAGES ? it - (uint32_t)STAGES : 0u; j < it; ++j)
                 mbar_wait_quiet(&sh->full[j % (uint32_t)STAGES], (j / (uint32_t)STAGES) & 1u, DRAIN_LIMIT_CLOCKS);
@@ -386,8 +457,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
         bool ok = true;
         const uint32_t ring_base = smem_u32(ring);
         const uint64_t astep = g.a_mn ? 2048 >> 4 : 32 >> 4, bstep = g.b_mn ? 2048 >> 4 : 32 >> 4;
-        for (int64_t i = blockIdx.x; ok && i < g.items; i += gridDim.x) {
-            const int kbn = item_at(g, BN, i).kbn;
+        for (int64_t i = worker; rank == 0 && ok && i < g.items; i += workers) {
+            const int kbn = item_at(g, TILE_M, BN, i).kbn;
             for (int kb = 0; ok && kb < kbn; ++acc) {
                 const int run_end = RUNS ? min(kb + RUN_KB, kbn) : kbn;
                 const uint32_t buf = acc & 1u, use = (acc >> 1) & 1u;
@@ -399,37 +470,49 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                     tc_fence_after();
                     const uint32_t a = ring_base + s * (uint32_t)STAGE_BYTES, b = a + PARTS * A_BYTES;
                     if constexpr (PARTS == 1) {
-                        umma_kblock_elected<F8>(d_tmem, operand_desc(a, g.a_mn), operand_desc(b, g.b_mn), astep, bstep, g.idesc,
+                        umma_kblock_elected<F8, PAIR>(d_tmem, operand_desc(a, g.a_mn), operand_desc(b, g.b_mn), astep, bstep, g.idesc,
                                                 first);
                     } else {
                         constexpr int pa[6] = {0, 2, 0, 1, 1, 0}, pb[6] = {0, 0, 2, 1, 0, 1};
 #pragma unroll
                         for (int q = 0; q < 6; ++q)
-                            umma_kblock_elected<F8>(d_tmem + (q == 0 ? 0 : BN), operand_desc(a + pa[q] * A_BYTES, g.a_mn),
+                            umma_kblock_elected<F8, PAIR>(d_tmem + (q == 0 ? 0 : BN), operand_desc(a + pa[q] * A_BYTES, g.a_mn),
                                                     operand_desc(b + pb[q] * B_BYTES, g.b_mn), astep, bstep, g.idesc,
                                                     q <= 1 ? first : 1u);
                     }
-                    umma_commit_elected(&sh->empty[s]);
+                    commit_elected<PAIR>(&sh->empty[s]);
                     if (++s == (uint32_t)STAGES) {
                         s = 0;
                         ph ^= 1u;
                     }
                 }
-                if (ok) umma_commit_elected(&sh->t_full[buf]);
+                if (ok) commit_elected<PAIR>(&sh->t_full[buf]);
             }
         }
-        if (__any_sync(FULL, !ok || *abort_flag)) {
-            umma_commit_elected(&sh->drain);
+        if (rank == 0 && __any_sync(FULL, !ok || *abort_flag)) {
+            commit_elected<PAIR>(&sh->drain);
             if (lane == 0) mbar_wait_quiet(&sh->drain, 0u, DRAIN_LIMIT_CLOCKS);
         }
     } else {
         const int quad = warp & 3, half = warp >> 2;   // TMEM lanes 32 quad.. and the columns' half are this warp's
         constexpr int COLS = BN / 2, CHUNKS = COLS / 32;
-        float4 *mine = reinterpret_cast<float4 *>(staging + warp * 1024);
-        char *bytes = reinterpret_cast<char *>(mine);
+        char *bytes = staging + warp * Mem::WARP_STAGING;
+        float4 *mine = reinterpret_cast<float4 *>(bytes);
+        const int m_off = (int)rank * BM + quad * 32;   // this warp's rows in the tile
+        const uint32_t t_empty = PAIR ? in_block(smem_u32(&sh->t_empty[0]), 0) : smem_u32(&sh->t_empty[0]);
+        auto give_back = [&](uint32_t buf) {   // the accumulator, once every column of it is in registers
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (PAIR)
+                    arrive_at(t_empty + buf * 8);
+                else
+                    mbar_arrive(&sh->t_empty[buf]);
+            }
+        };
         uint32_t acc = 0;
         bool ok = true;
-        using C = ChunkStore<O>;
+        using C = ChunkStore<O, Mem::WARP_STAGING>;
         // the residual's chunk, copied ahead into the last slot (which is then not used for stores)
         char *landing = bytes + (C::SLOTS - 1) * C::BYTES;
         auto fetch_residual = [&](const Item &t, int col) {
@@ -437,7 +520,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
             const int c = lane % PER_ROW;
 #pragma unroll
             for (int r = lane / PER_ROW; r < 32; r += 32 / PER_ROW) {
-                const int64_t row = t.m0 + quad * 32 + r;
+                const int64_t row = t.m0 + m_off + r;
                 if (row < e.M && col + c * C::G < e.N)
                     copy_async<16>(landing + C::at(r, c), static_cast<const O *>(e.residual) + row * e.ldr + col + c * C::G);
             }
@@ -458,12 +541,14 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
             }
             return p;
         };
-        float *chunk_bias = reinterpret_cast<float *>(ring + RING_BYTES + STAGING_BYTES) + warp * 32;
+        float *chunk_bias = reinterpret_cast<float *>(biases) + warp * 32;
         auto finish_chunk = [&](const Item &t, int col, int next, const Lane &p, float (&v)[32]) {
-            const int64_t row0 = t.m0 + quad * 32, row = row0 + lane;
+            const int64_t row0 = t.m0 + m_off, row = row0 + lane;
             if (row0 >= e.M || col >= e.N) return;
             if (e.share) {
-                store_by_tma<float, 0>(&map_out, bytes, lane, col, (int)row0, t.split, v);
+                constexpr int SLOTS = ChunkStore<float, Mem::WARP_STAGING>::SLOTS;
+                store_by_tma<float, SLOTS - 1>(&map_out, bytes + turn * 4096, lane, col, (int)row0, t.split, v);
+                turn = turn + 1 == SLOTS ? 0 : turn + 1;
             } else if (e.tma) {
                 if (e.x_scale) {
                     const float xs = row < e.M ? __ldg(e.x_scale + row) : 0.f;
@@ -480,13 +565,15 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                     }
                     __syncwarp();
                 }
-                // slots taken in turn; with a residual the last one is the residual's (where there are two)
+                // slots taken in turn; with a residual the last one is the residual's (where there is more than one)
                 auto put = [&](const CUtensorMap *map) {
-                    if (C::SLOTS == 1 || ahead)
-                        store_by_tma<O, 0>(map, bytes, lane, col, (int)row0, 0, v);
-                    else {
+                    if (ahead) {
+                        constexpr int FREE = C::SLOTS > 1 ? C::SLOTS - 1 : 1;
+                        store_by_tma<O, FREE - 1>(map, bytes + turn * C::BYTES, lane, col, (int)row0, 0, v);
+                        turn = turn + 1 == FREE ? 0 : turn + 1;
+                    } else {
                         store_by_tma<O, C::SLOTS - 1>(map, bytes + turn * C::BYTES, lane, col, (int)row0, 0, v);
-                        turn ^= 1;
+                        turn = turn + 1 == C::SLOTS ? 0 : turn + 1;
                     }
                 };
                 if (e.preact) put(&map_z);
@@ -531,8 +618,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                 __syncwarp();
             }
         };
-        for (int64_t i = blockIdx.x; ok && i < g.items; i += gridDim.x) {
-            const Item t = item_at(g, BN, i);
+        for (int64_t i = worker; ok && i < g.items; i += workers) {
+            const Item t = item_at(g, TILE_M, BN, i);
             const int col0 = t.n0 + half * COLS;
             if (ahead && col0 < e.N) fetch_residual(t, col0);   // while the sums are on their way
             Lane lanes[CHUNKS];
@@ -566,9 +653,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                             for (int j = 0; j < 32; ++j) sum[c][j] += __uint_as_float(v[j]);
                         }
                     }
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh->t_empty[buf]);
+                    give_back(buf);
                 }
                 if (!ok) break;
 #pragma unroll
@@ -588,11 +673,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                     uint32_t v[32];
                     tmem_ld32_issue(taddr + c * 32, v);
                     tmem_ld_wait(v);
-                    if (c == CHUNKS - 1) {
-                        tc_fence_before();   // every column is in registers: the accumulator is free
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&sh->t_empty[buf]);
-                    }
+                    if (c == CHUNKS - 1) give_back(buf);
                     float f[32];
 #pragma unroll
                     for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
@@ -604,10 +685,14 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
         if (lane == 0) tma_stores_read<0>();   // before the block gives its shared memory back
     }
     __syncthreads();
+    if constexpr (PAIR) cluster_meet();   // neither block leaves while the other may still signal it
     if (sh->abort && threadIdx.x == 0) ep_raise(status, EP_ERR_TIMEOUT);
     if (warp == 0) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
+        if constexpr (PAIR)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
     }
 }
 
@@ -857,16 +942,17 @@ bool encode_result(CUtensorMap *map, void *base, int type, int64_t depth, int64_
 
 struct GemmPlan {
     int bn, splits;
-    bool runs;
+    bool runs, pair;
     int ld_share;
     GemmShape shape;
     size_t share_bytes(int64_t M) const { return splits > 1 ? sizeof(float) * (size_t)splits * (size_t)M * (size_t)ld_share : 0; }
 };
 
-// Tile width and split of the sum.  A block's time for a tile is about its columns plus a constant (the A tile, the
-// pipeline's start), so the width with the least waves x (columns + 32) is taken.  When all tiles fit one wave with
-// blocks to spare, the sum over k is split between them, into shares of at least 4 k-blocks.
-GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, int parts, bool fp32_out) {
+// Tile and split of the sum.  A block's time for a tile is about its columns plus a constant (the A tile, the
+// pipeline's start), so of the widths, alone and in pairs, the one with the least waves x (columns + 32) is taken; a pair
+// counts 7/8, for the operand bytes that it saves.  When all tiles fit one wave with blocks to spare, the sum over k is
+// split between them, into shares of at least 4 k-blocks.
+GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, bool fp32_out) {
     GemmPlan p{};
     p.runs = fp32_out;
     const int ke = type == EP_E4M3 ? 128 : 64;
@@ -874,18 +960,22 @@ GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, int
     p.shape.N = N;
     p.shape.kb = (int)ep::ceil_div(K, ke);
     int64_t best = 0;
-    for (int bn : {256, 128, 64}) {
-        if (p.runs && bn != 128) continue;
-        const int64_t tiles = ep::ceil_div(M, BM) * ep::ceil_div(N, bn);
-        const int64_t cost = ep::ceil_div(tiles, ctx->sm_count) * (bn + 32);
-        if (!p.bn || cost < best) {
-            best = cost;
-            p.bn = bn;
+    for (int pair = 0; pair <= 1; ++pair)
+        for (int bn : {256, 128, 64}) {
+            if (bn == (pair ? 64 : 256) || (p.runs && bn != 128)) continue;
+            const int64_t tiles = ep::ceil_div(M, pair ? 2 * BM : BM) * ep::ceil_div(N, bn);
+            const int64_t waves = ep::ceil_div(tiles, pair ? ctx->sm_count / 2 : ctx->sm_count);
+            const int64_t cost = waves * (bn + 32) * (pair ? 7 : 8);
+            if (!p.bn || cost < best) {
+                best = cost;
+                p.bn = bn;
+                p.pair = pair;
+            }
         }
-    }
     p.shape.tiles_n = (int)ep::ceil_div(N, p.bn);
-    p.shape.tiles = ep::ceil_div(M, BM) * p.shape.tiles_n;
-    int64_t splits = std::max<int64_t>(1, std::min<int64_t>(ctx->sm_count / p.shape.tiles, p.shape.kb / 4));
+    p.shape.tiles = ep::ceil_div(M, p.pair ? 2 * BM : BM) * p.shape.tiles_n;
+    const int workers = p.pair ? ctx->sm_count / 2 : ctx->sm_count;
+    int64_t splits = std::max<int64_t>(1, std::min<int64_t>(workers / p.shape.tiles, p.shape.kb / 4));
     int per = (int)ep::ceil_div(p.shape.kb, splits);
     if (p.runs) per = (int)round_up(per, RUN_KB);
     p.splits = (int)ep::ceil_div(p.shape.kb, per);
@@ -899,29 +989,41 @@ struct Maps {
     CUtensorMap a, b, out, z;   // out: of the shares, where the sum is split
 };
 
-template <int BN, bool F8, int PARTS, bool RUNS, typename O>
-int launch_tiles(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &e,
-                 cudaStream_t stream) {
-    auto kernel = linear_tiles<BN, F8, PARTS, RUNS, O>;
-    EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)GEMM_SMEM));
-    const int grid = (int)std::min<int64_t>(p.shape.items, ctx->sm_count);
-    kernel<<<grid, GEMM_THREADS, GEMM_SMEM, stream>>>(m.a, m.b, m.out, m.z, p.shape, e, ctx->d_status);
-    EP_CUDA(ctx, cudaGetLastError());
+template <int BN, bool F8, int PARTS, bool RUNS, bool PAIR, typename O>
+int launch_tiles(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &e, cudaStream_t stream) {
+    auto kernel = linear_tiles<BN, F8, PARTS, RUNS, PAIR, O>;
+    constexpr size_t smem = TileMemory<BN, PARTS, PAIR>::TOTAL;
+    EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    const int64_t workers = std::min<int64_t>(p.shape.items, PAIR ? ctx->sm_count / 2 : ctx->sm_count);
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(PAIR ? 2 * workers : workers));
+    cfg.blockDim = dim3(GEMM_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim = {2, 1, 1};
+    cfg.attrs = &attr;
+    cfg.numAttrs = PAIR ? 1 : 0;
+    EP_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, m.a, m.b, m.out, m.z, p.shape, e, ctx->d_status));
     return EP_OK;
 }
 
 // (the type of the output is fp32 exactly where sums are kept in runs)
 template <bool F8, typename O>
 int launch_width(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &e, cudaStream_t stream) {
-    return p.bn == 256   ? launch_tiles<256, F8, 1, false, O>(ctx, p, m, e, stream)
-           : p.bn == 128 ? launch_tiles<128, F8, 1, false, O>(ctx, p, m, e, stream)
-                         : launch_tiles<64, F8, 1, false, O>(ctx, p, m, e, stream);
+    if (p.pair)
+        return p.bn == 256 ? launch_tiles<256, F8, 1, false, true, O>(ctx, p, m, e, stream)
+                           : launch_tiles<128, F8, 1, false, true, O>(ctx, p, m, e, stream);
+    return p.bn == 128 ? launch_tiles<128, F8, 1, false, false, O>(ctx, p, m, e, stream)
+                       : launch_tiles<64, F8, 1, false, false, O>(ctx, p, m, e, stream);
 }
 template <bool F8>
 int launch_type(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &e, cudaStream_t stream) {
-    return p.runs                   ? launch_tiles<128, F8, 1, true, float>(ctx, p, m, e, stream)
-           : e.out_type == EP_BF16 ? launch_width<F8, __nv_bfloat16>(ctx, p, m, e, stream)
-                                    : launch_width<F8, __half>(ctx, p, m, e, stream);
+    if (p.runs)
+        return p.pair ? launch_tiles<128, F8, 1, true, true, float>(ctx, p, m, e, stream)
+                      : launch_tiles<128, F8, 1, true, false, float>(ctx, p, m, e, stream);
+    return e.out_type == EP_BF16 ? launch_width<F8, __nv_bfloat16>(ctx, p, m, e, stream) : launch_width<F8, __half>(ctx, p, m, e, stream);
 }
 
 // D = A B^T by tiles, with the epilogue; `share` is room for the shares of a split sum.  Adds to *kernels.
@@ -931,20 +1033,23 @@ int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand
     p.shape.a_mn = a_mn;
     p.shape.b_mn = b_mn;
     p.shape.idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
-                    ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
+                    ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)((p.pair ? 2 * BM : BM) >> 4) << 24);
     e.share = p.splits > 1 ? share : nullptr;
     e.ld_share = p.ld_share;
     Maps m{};
-    bool ok = encode_operand(&m.a, a, a_mn, BM) && encode_operand(&m.b, b, b_mn, p.bn);
+    bool ok = encode_operand(&m.a, a, a_mn, BM) && encode_operand(&m.b, b, b_mn, p.pair ? p.bn / 2 : p.bn);
     if (e.share)
         ok = ok && encode_result(&m.out, share, EP_F32, p.splits, e.M, p.ld_share, p.ld_share);
     else if (e.tma)
         ok = ok && encode_result(&m.out, e.out, e.out_type, 1, e.M, e.N, e.N) &&
              (!e.preact || encode_result(&m.z, e.preact, e.out_type, 1, e.M, e.N, e.N));
     if (!ok) return ep::fail(ctx, EP_ERR_CUDA, "cuTensorMapEncodeTiled failed for a product of %lld x %d", (long long)e.M, e.N);
-    const int rc = a.parts == 3          ? launch_tiles<128, false, 3, true, float>(ctx, p, m, e, stream)
-                   : a.type == EP_E4M3 ? launch_type<true>(ctx, p, m, e, stream)
-                                         : launch_type<false>(ctx, p, m, e, stream);
+    int rc;
+    if (a.parts == 3)
+        rc = p.pair ? launch_tiles<128, false, 3, true, true, float>(ctx, p, m, e, stream)
+                    : launch_tiles<128, false, 3, true, false, float>(ctx, p, m, e, stream);
+    else
+        rc = a.type == EP_E4M3 ? launch_type<true>(ctx, p, m, e, stream) : launch_type<false>(ctx, p, m, e, stream);
     if (rc != EP_OK) return rc;
     ++*kernels;
     if (p.splits > 1) {
@@ -1030,7 +1135,7 @@ LinearWorkspace linear_workspace(const ep_ctx *ctx, int64_t rows, int n_in, int 
             w.x = a.take<char>(packed_form(rows, n_in, in_type).bytes);
             w.w = a.take<char>(packed_form(n_out, n_in, in_type).bytes);
         }
-        w.plan = plan_gemm(ctx, rows, n_out, n_in, in_type, in_type == EP_F32 ? 3 : 1, out_type == EP_F32);
+        w.plan = plan_gemm(ctx, rows, n_out, n_in, in_type, out_type == EP_F32);
         w.share = a.take<float>(w.plan.share_bytes(rows) / sizeof(float));
     }
     w.bytes = std::max<size_t>(a.used, 256);
@@ -1061,9 +1166,8 @@ BackwardWorkspace backward_workspace(const ep_ctx *ctx, int64_t rows, int n_in, 
     w.slab = round_up(ep::ceil_div(std::max<int64_t>(rows, 1), want), DZ_ROWS);
     w.slabs = (int)std::max<int64_t>(1, ep::ceil_div(rows, w.slab));
     w.dbias_parts = a.take<float>((size_t)w.slabs * n_out);
-    const int parts = in_type == EP_F32 ? 3 : 1;
-    w.dx = plan_gemm(ctx, std::max<int64_t>(rows, 1), n_in, n_out, in_type, parts, in_type == EP_F32);
-    w.dw = plan_gemm(ctx, n_out, n_in, std::max<int64_t>(rows, 1), in_type, parts, in_type == EP_F32);
+    w.dx = plan_gemm(ctx, std::max<int64_t>(rows, 1), n_in, n_out, in_type, in_type == EP_F32);
+    w.dw = plan_gemm(ctx, n_out, n_in, std::max<int64_t>(rows, 1), in_type, in_type == EP_F32);
     w.share = a.take<float>(std::max(w.dx.share_bytes(rows), w.dw.share_bytes(n_out)) / sizeof(float));
     w.bytes = std::max<size_t>(a.used, 256);
     return w;
