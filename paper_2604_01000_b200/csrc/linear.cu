@@ -149,47 +149,60 @@ __device__ __forceinline__ void load_residual(const Epilogue &e, int64_t row, in
 }
 
 // ---------------------------------------------------------------------------------------------- a chunk of the output
-// 32 columns of a warp's 32 rows, one row per lane, are finished in registers and leave through shared memory by TMA,
+// A warp's 32 rows of a few columns, one row per lane, are finished in registers and leave through shared memory by TMA,
 // which writes whole lines and cuts off what lies outside the matrix.  (Finished from shared memory in a coalesced
 // order instead, addresses, bounds and types made 18 instructions per element, and the epilogue took longer than the
-// sums and the memory both: 169343 x 128 -> 512 in 137 us.)
-template <typename O, int ROOM = 4096>
+// sums and the memory both: 169343 x 128 -> 512 in 137 us.)  Boxes have rows of 128 bytes where the tile allows: TMA
+// takes them row by row, and rows of 64 bytes cost as much.
+constexpr int SLOT_BYTES = 4096;   // a warp has two slots of this size
+template <typename O, int COLS>
 struct ChunkStore {
-    static constexpr int G = 16 / (int)sizeof(O);             // columns of a 16-byte piece
-    static constexpr int ROW = 32 * (int)sizeof(O);           // bytes of a row of the chunk: 64 or 128
-    static constexpr int BYTES = 32 * ROW;                    // 2 or 4 KB of the warp's ROOM
-    static constexpr int SLOTS = ROOM / BYTES;
+    static constexpr int G = 16 / (int)sizeof(O);                                   // columns of a 16-byte piece
+    static constexpr int WIDTH = 128 / (int)sizeof(O) < COLS ? 128 / (int)sizeof(O) : COLS;
+    static constexpr int ROW = WIDTH * (int)sizeof(O);                              // bytes of a row of the box: 64 or 128
     // Where piece c of row r lies: as the swizzle of a TMA box of 64- or 128-byte rows has it (no two lanes that
     // access a piece each together meet in a bank).
-    static __device__ __forceinline__ int at(int r, int c) { return r * ROW + ((sizeof(O) == 2 ? c ^ ((r >> 1) & 3) : c ^ (r & 7)) << 4); }
+    static __device__ __forceinline__ int at(int r, int c) { return r * ROW + ((ROW == 64 ? c ^ ((r >> 1) & 3) : c ^ (r & 7)) << 4); }
+    // 32 of a lane's columns, from piece c0 on
+    static __device__ __forceinline__ void write(char *slot, int lane, int c0, const float (&v)[32]) {
+#pragma unroll
+        for (int c = 0; c < 32 / G; ++c) {
+            float w[G];
+#pragma unroll
+            for (int i = 0; i < G; ++i) w[i] = v[c * G + i];
+            store_chunk(reinterpret_cast<O *>(slot + at(lane, c0 + c)), 0, 1 << 30, true, w);
+        }
+    }
+    static __device__ __forceinline__ void add(const char *slot, int lane, int c0, float (&v)[32]) {
+#pragma unroll
+        for (int c = 0; c < 32 / G; ++c) {
+            float w[G];
+            load_chunk(reinterpret_cast<const O *>(slot + at(lane, c0 + c)), 0, 1 << 30, true, 0.f, w);
+#pragma unroll
+            for (int i = 0; i < G; ++i) v[c * G + i] += w[i];
+        }
+    }
 };
 
-__device__ __forceinline__ void tma_store_3d(const CUtensorMap *map, const void *src, int x, int y, int z) {
-    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
-                 ::"l"(map), "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z)
+// Called by the whole warp; the elected lane (always the same one) issues.
+__device__ __forceinline__ void tma_store_3d_elected(const CUtensorMap *map, const void *src, int x, int y, int z) {
+    asm volatile("{\n.reg .pred pe;\nelect.sync _|pe, 0xffffffff;\n"
+                 "@pe cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];\n"
+                 "@pe cp.async.bulk.commit_group;\n}" ::"l"(map),
+                 "r"(smem_u32(src)), "r"(x), "r"(y), "r"(z)
                  : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
-// Until at most PENDING of this thread's stores still read shared memory.
+// Until at most PENDING of the warp's stores still read shared memory; all lanes may then write there.  (Only the elected
+// lane has any to wait for.)
 template <int PENDING>
-__device__ __forceinline__ void tma_stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PENDING) : "memory"); }
-
-// One lane's 32 columns into `slot` and out to (x, y, z).  The slot has been free since before `ready` stores.
-template <typename O, int READY>
-__device__ __forceinline__ void store_by_tma(const CUtensorMap *map, char *slot, int lane, int x, int y, int z, const float (&v)[32]) {
-    using C = ChunkStore<O>;
-    if (lane == 0) tma_stores_read<READY>();
+__device__ __forceinline__ void stores_read() {
+    asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(PENDING) : "memory");
     __syncwarp();
-#pragma unroll
-    for (int c = 0; c < 32 / C::G; ++c) {
-        float w[C::G];
-#pragma unroll
-        for (int i = 0; i < C::G; ++i) w[i] = v[c * C::G + i];
-        store_chunk(reinterpret_cast<O *>(slot + C::at(lane, c)), 0, 1 << 30, true, w);
-    }
+}
+// What the lanes have written becomes visible to the stores that are issued next.
+__device__ __forceinline__ void before_stores() {
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
-    if (lane == 0) tma_store_3d(map, slot, x, y, z);
 }
 
 // ---------------------------------------------------------------------------------------------- the tile kernel
@@ -217,7 +230,6 @@ constexpr int A_BYTES = BM * 128;
 constexpr int RUN_KB = 4;
 constexpr int MAX_STAGES = 8;
 constexpr int TMEM_COLS = 512;
-constexpr int BIAS_BYTES = EPI_WARPS * 128;   // per warp the bias of a chunk's 32 columns
 
 struct GemmShared {
     uint64_t full[MAX_STAGES], empty[MAX_STAGES], t_full[2], t_empty[2], drain;
@@ -231,9 +243,9 @@ struct TileMemory {
     static constexpr int B_ROWS = PAIR ? BN / 2 : BN;
     static constexpr int B_BYTES = B_ROWS * 128;
     static constexpr int STAGE_BYTES = PARTS * (A_BYTES + B_BYTES);
-    static constexpr int WARP_STAGING = PAIR ? 8192 : 4096;
+    static constexpr int WARP_STAGING = 2 * SLOT_BYTES;
     static constexpr int STAGING_BYTES = EPI_WARPS * WARP_STAGING;
-    static constexpr int REST = 1024 + STAGING_BYTES + BIAS_BYTES + (int)sizeof(GemmShared);
+    static constexpr int REST = 1024 + STAGING_BYTES + (int)sizeof(GemmShared);
     static constexpr int FIT = (227 * 1024 - REST) / STAGE_BYTES;
     static constexpr int STAGES = FIT < MAX_STAGES ? FIT : MAX_STAGES;
     static constexpr int RING_BYTES = STAGES * STAGE_BYTES;
@@ -244,10 +256,11 @@ struct TileMemory {
 struct GemmShape {
     int64_t M;
     int N;
-    int tiles_n;
+    int tiles_n, tiles_m;
+    int step_m, step_n;   // one worker's way from tile to tile: tiles of M and of N
     int64_t tiles;        // tiles of the output
     int64_t items;        // tiles x splits
-    int kb, kb_per_split; // k-blocks of the whole sum, and of one split
+    int splits, kb, kb_per_split;   // k-blocks of the whole sum, and of one split
     bool a_mn, b_mn;      // operand stored along its rows
     uint32_t idesc;
 };
@@ -294,8 +307,10 @@ __device__ __forceinline__ uint32_t in_block(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void cluster_meet() {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// (relaxed: nothing but the reading of TMEM goes before it, which tcgen05's own fence and wait order; with release an
+// arrival at the other block took 1500 clocks)
 __device__ __forceinline__ void arrive_at(uint32_t cluster_addr) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 template <bool PAIR>
 __device__ __forceinline__ void load_tile_elected(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
@@ -334,22 +349,36 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t smem, bool mn) {
     return (uint64_t)((smem & 0x3FFFFu) >> 4) | (lead << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
-struct Item {
-    int64_t m0;
-    int n0, split, kb0, kbn;
+// One worker's tiles: first, first + workers, ...  Tiles of one row of tiles come one after another (they share A, and B
+// stays in the L2); splits outermost.  Only the first is found by division.
+template <int TILE_M, int TILE_N>
+struct Items {
+    const GemmShape &g;
+    int tm, tn, split;
+    __device__ __forceinline__ Items(const GemmShape &shape, int64_t first) : g(shape) {
+        split = (int)(first / g.tiles);
+        const int64_t tile = first - (int64_t)split * g.tiles;
+        tm = (int)(tile / g.tiles_n);
+        tn = (int)(tile - (int64_t)tm * g.tiles_n);
+    }
+    __device__ __forceinline__ bool more() const { return split < g.splits; }
+    __device__ __forceinline__ void next() {
+        tm += g.step_m;
+        tn += g.step_n;
+        if (tn >= g.tiles_n) {
+            tn -= g.tiles_n;
+            ++tm;
+        }
+        while (tm >= g.tiles_m) {
+            tm -= g.tiles_m;
+            ++split;
+        }
+    }
+    __device__ __forceinline__ int m0() const { return tm * TILE_M; }
+    __device__ __forceinline__ int n0() const { return tn * TILE_N; }
+    __device__ __forceinline__ int kb0() const { return split * g.kb_per_split; }
+    __device__ __forceinline__ int kbn() const { return min(g.kb_per_split, g.kb - kb0()); }
 };
-// Tiles of one row of tiles come one after another (they share A, and B stays in the L2); splits outermost.
-__device__ __forceinline__ Item item_at(const GemmShape &g, int bm, int bn, int64_t i) {
-    Item t;
-    t.split = (int)(i / g.tiles);
-    const int64_t tile = i - (int64_t)t.split * g.tiles;
-    const int64_t tm = tile / g.tiles_n;
-    t.m0 = tm * bm;
-    t.n0 = (int)(tile - tm * g.tiles_n) * bn;
-    t.kb0 = t.split * g.kb_per_split;
-    t.kbn = min(g.kb_per_split, g.kb - t.kb0);
-    return t;
-}
 
 template <int BN, bool F8, int PARTS, bool RUNS, bool PAIR, typename O>
 __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_constant__ CUtensorMap map_a,
@@ -368,10 +397,10 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
     extern __shared__ char smem_raw[];
     char *ring = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     char *staging = ring + Mem::RING_BYTES;
-    char *biases = staging + Mem::STAGING_BYTES;
-    GemmShared *sh = reinterpret_cast<GemmShared *>(biases + BIAS_BYTES);
+    GemmShared *sh = reinterpret_cast<GemmShared *>(staging + Mem::STAGING_BYTES);
     const uint32_t rank = PAIR ? cluster_rank() : 0;     // rank 0 issues the MMAs
-    const int64_t worker = PAIR ? blockIdx.x >> 1 : blockIdx.x, workers = PAIR ? gridDim.x >> 1 : gridDim.x;
+    const int64_t worker = PAIR ? blockIdx.x >> 1 : blockIdx.x;
+    using Walk = Items<TILE_M, BN>;
     volatile int *abort_flag = &sh->abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -411,14 +440,14 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
         uint32_t it = 0, s = 0, ph = 0;
         bool ok = true;
         const uint32_t ring_base = smem_u32(ring);
-        for (int64_t i = worker; ok && i < g.items; i += workers) {
-            const Item t = item_at(g, TILE_M, BN, i);
-            const int m = (int)t.m0 + (int)rank * BM, n = t.n0 + (int)rank * Mem::B_ROWS;   // this block's rows of A and of B
-            for (int kb = 0; kb < t.kbn; ++kb, ++it) {
+        for (Walk t(g, worker); ok && t.more(); t.next()) {
+            const int m = t.m0() + (int)rank * BM, n = t.n0() + (int)rank * Mem::B_ROWS;   // this block's rows of A and of B
+            const int kb0 = t.kb0(), kbn = t.kbn();
+            for (int kb = 0; kb < kbn; ++kb, ++it) {
                 if (!(ok = __all_sync(FULL, mbar_wait(&sh->empty[s], ph ^ 1u, abort_flag)))) break;
                 if (rank == 0) mbar_expect_tx_elected(&sh->full[s], (PAIR ? 2 : 1) * STAGE_BYTES);
                 const uint32_t bar = PAIR ? in_block(smem_u32(&sh->full[s]), 0) : smem_u32(&sh->full[s]);
-                const int k = (t.kb0 + kb) * KE;
+                const int k = (kb0 + kb) * KE;
                 uint32_t dst = ring_base + s * (uint32_t)STAGE_BYTES;
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p, dst += A_BYTES) {
@@ -457,8 +486,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
         bool ok = true;
         const uint32_t ring_base = smem_u32(ring);
         const uint64_t astep = g.a_mn ? 2048 >> 4 : 32 >> 4, bstep = g.b_mn ? 2048 >> 4 : 32 >> 4;
-        for (int64_t i = worker; rank == 0 && ok && i < g.items; i += workers) {
-            const int kbn = item_at(g, TILE_M, BN, i).kbn;
+        for (Walk t(g, worker); rank == 0 && ok && t.more(); t.next()) {
+            const int kbn = t.kbn();
             for (int kb = 0; ok && kb < kbn; ++acc) {
                 const int run_end = RUNS ? min(kb + RUN_KB, kbn) : kbn;
                 const uint32_t buf = acc & 1u, use = (acc >> 1) & 1u;
@@ -495,9 +524,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
         }
     } else {
         const int quad = warp & 3, half = warp >> 2;   // TMEM lanes 32 quad.. and the columns' half are this warp's
-        constexpr int COLS = BN / 2, CHUNKS = COLS / 32;
-        char *bytes = staging + warp * Mem::WARP_STAGING;
-        float4 *mine = reinterpret_cast<float4 *>(bytes);
+        constexpr int COLS = BN / 2;
+        char *slots = staging + warp * Mem::WARP_STAGING;
         const int m_off = (int)rank * BM + quad * 32;   // this warp's rows in the tile
         const uint32_t t_empty = PAIR ? in_block(smem_u32(&sh->t_empty[0]), 0) : smem_u32(&sh->t_empty[0]);
         auto give_back = [&](uint32_t buf) {   // the accumulator, once every column of it is in registers
@@ -512,126 +540,144 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
         };
         uint32_t acc = 0;
         bool ok = true;
-        using C = ChunkStore<O, Mem::WARP_STAGING>;
-        // the residual's chunk, copied ahead into the last slot (which is then not used for stores)
-        char *landing = bytes + (C::SLOTS - 1) * C::BYTES;
-        auto fetch_residual = [&](const Item &t, int col) {
-            constexpr int PER_ROW = 32 / C::G;
+        using C = ChunkStore<O, COLS>;
+        constexpr int SUBS = C::WIDTH / 32;            // a chunk is one or two times 32 columns
+        constexpr int CHUNKS = COLS / C::WIDTH;
+        const bool by_tma = e.tma && !e.share, with_z = e.preact != nullptr;
+        // The residual's chunk is copied ahead into the slot that the chunk will leave from, and added in place.  z takes
+        // the other slot; without z the two take turns.
+        auto fetch_residual = [&](int64_t row0, int col, char *slot) {
+            constexpr int PER_ROW = C::WIDTH / C::G;
             const int c = lane % PER_ROW;
 #pragma unroll
             for (int r = lane / PER_ROW; r < 32; r += 32 / PER_ROW) {
-                const int64_t row = t.m0 + m_off + r;
+                const int64_t row = row0 + r;
                 if (row < e.M && col + c * C::G < e.N)
-                    copy_async<16>(landing + C::at(r, c), static_cast<const O *>(e.residual) + row * e.ldr + col + c * C::G);
+                    copy_async<16>(slot + C::at(r, c), static_cast<const O *>(e.residual) + row * e.ldr + col + c * C::G);
             }
             copies_end_group();
         };
-        const bool ahead = e.tma && !e.share && e.residual && C::SLOTS > 1;
-        int turn = 0;
-        // One lane's 32 finished sums from column col on.  next: the column of the residual to copy after this one, or -1.
         // Bias and scale of a chunk's columns, one per lane, fetched before the sums are waited for.
         struct Lane {
-            float bias, scale;
+            float bias[SUBS], scale[SUBS];
         };
         auto fetch_lane = [&](int col) {
-            Lane p{0.f, 1.f};
-            if (e.tma && !e.share && col + lane < e.N) {
-                if (e.bias) p.bias = load_param(e.bias, e.bias_type, col + lane);
-                if (e.w_scale) p.scale = __ldg(e.w_scale + col + lane);
+            Lane p;
+#pragma unroll
+            for (int q = 0; q < SUBS; ++q) {
+                const int c = col + q * 32 + lane;
+                p.bias[q] = by_tma && e.bias && c < e.N ? load_param(e.bias, e.bias_type, c) : 0.f;
+                p.scale[q] = by_tma && e.w_scale && c < e.N ? __ldg(e.w_scale + c) : 1.f;
             }
             return p;
         };
-        float *chunk_bias = reinterpret_cast<float *>(biases) + warp * 32;
-        auto finish_chunk = [&](const Item &t, int col, int next, const Lane &p, float (&v)[32]) {
-            const int64_t row0 = t.m0 + m_off, row = row0 + lane;
+        int turn = 0;   // slot of the next chunk
+        // One lane's finished sums from column col on.  next: the column of the chunk after this one in the tile, or -1.
+        auto finish_chunk = [&](int split, int64_t row0, int col, int next, const Lane &p, float (&v)[SUBS][32]) {
+            const int64_t row = row0 + lane;
             if (row0 >= e.M || col >= e.N) return;
             if (e.share) {
-                constexpr int SLOTS = ChunkStore<float, Mem::WARP_STAGING>::SLOTS;
-                store_by_tma<float, SLOTS - 1>(&map_out, bytes + turn * 4096, lane, col, (int)row0, t.split, v);
-                turn = turn + 1 == SLOTS ? 0 : turn + 1;
-            } else if (e.tma) {
-                if (e.x_scale) {
-                    const float xs = row < e.M ? __ldg(e.x_scale + row) : 0.f;
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] *= xs * __shfl_sync(FULL, p.scale, j);
+                for (int q = 0; q < SUBS; ++q) {
+                    if (col + q * 32 >= e.N) break;
+                    stores_read<1>();
+                    ChunkStore<float, 32>::write(slots + turn * SLOT_BYTES, lane, 0, v[q]);
+                    before_stores();
+                    tma_store_3d_elected(&map_out, slots + turn * SLOT_BYTES, col + q * 32, (int)row0, split);
+                    turn ^= 1;
                 }
-                if (e.bias) {
-                    chunk_bias[lane] = p.bias;
-                    __syncwarp();
-#pragma unroll
-                    for (int j = 0; j < 32; j += 4) {
-                        const float4 b = *reinterpret_cast<const float4 *>(chunk_bias + j);
-                        v[j] += b.x, v[j + 1] += b.y, v[j + 2] += b.z, v[j + 3] += b.w;
-                    }
-                    __syncwarp();
-                }
-                // slots taken in turn; with a residual the last one is the residual's (where there is more than one)
-                auto put = [&](const CUtensorMap *map) {
-                    if (ahead) {
-                        constexpr int FREE = C::SLOTS > 1 ? C::SLOTS - 1 : 1;
-                        store_by_tma<O, FREE - 1>(map, bytes + turn * C::BYTES, lane, col, (int)row0, 0, v);
-                        turn = turn + 1 == FREE ? 0 : turn + 1;
-                    } else {
-                        store_by_tma<O, C::SLOTS - 1>(map, bytes + turn * C::BYTES, lane, col, (int)row0, 0, v);
-                        turn = turn + 1 == C::SLOTS ? 0 : turn + 1;
-                    }
-                };
-                if (e.preact) put(&map_z);
-                activate(v, e.act);
+            } else if (by_tma) {
+                char *out_slot = slots + (with_z ? SLOT_BYTES : turn * SLOT_BYTES);
                 if (e.residual) {
-                    if (!ahead) {
-                        if (lane == 0) tma_stores_read<0>();
-                        __syncwarp();
-                        fetch_residual(t, col);
-                    }
                     copies_wait<0>();
-                    __syncwarp();
-#pragma unroll
-                    for (int c = 0; c < 32 / C::G; ++c) {
-                        float w[C::G];
-                        load_chunk(reinterpret_cast<const O *>(landing + C::at(lane, c)), 0, 1 << 30, true, 0.f, w);
-#pragma unroll
-                        for (int i = 0; i < C::G; ++i) v[c * C::G + i] += w[i];
+                    if (with_z)
+                        stores_read<0>();   // (out_slot's own store was waited for before the copy)
+                    else {
+                        if (next >= 0 && next < e.N) {
+                            stores_read<0>();
+                            fetch_residual(row0, next, slots + (turn ^ 1) * SLOT_BYTES);
+                        } else
+                            __syncwarp();
                     }
-                    __syncwarp();
-                    if (ahead && next >= 0 && next < e.N) fetch_residual(t, next);
+                } else if (with_z)
+                    stores_read<0>();
+                else
+                    stores_read<1>();
+                const float xs = e.x_scale && row < e.M ? __ldg(e.x_scale + row) : 0.f;
+#pragma unroll
+                for (int q = 0; q < SUBS; ++q) {
+                    if (e.x_scale) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[q][j] *= xs * __shfl_sync(FULL, p.scale[q], j);
+                    }
+                    if (e.bias) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[q][j] += __shfl_sync(FULL, p.bias[q], j);
+                    }
+                    if (with_z) C::write(slots, lane, q * (32 / C::G), v[q]);
+                    activate(v[q], e.act);
+                    if (e.residual) C::add(out_slot, lane, q * (32 / C::G), v[q]);
+                    C::write(out_slot, lane, q * (32 / C::G), v[q]);
                 }
-                put(&map_out);
+                before_stores();
+                if (with_z) tma_store_3d_elected(&map_z, slots, col, (int)row0, 0);
+                tma_store_3d_elected(&map_out, out_slot, col, (int)row0, 0);
+                if (with_z) {
+                    if (e.residual && next >= 0 && next < e.N) {
+                        stores_read<0>();
+                        fetch_residual(row0, next, out_slot);
+                    }
+                } else
+                    turn ^= 1;
             } else {
                 // rows that TMA cannot write: through shared memory (16-byte piece c of row r lies at c ^ (r & 7)), so
                 // that neighbouring lanes finish neighbouring columns
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    mine[lane * 8 + (q ^ (lane & 7))] = make_float4(v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
-                __syncwarp();
-                if (col + lane < e.N) {
-                    Columns<1> c1;
-                    c1.load(e, col + lane);
-                    const float *flat = reinterpret_cast<const float *>(mine);
+                float4 *mine = reinterpret_cast<float4 *>(slots);
 #pragma unroll 1
-                    for (int r = 0; r < 32 && row0 + r < e.M; ++r) {
-                        float w[1] = {flat[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)]}, add[1];
-                        load_residual<O>(e, row0 + r, col + lane, add);
-                        finish<O>(e, row0 + r, col + lane, c1, w, add);
+                for (int q = 0; q < SUBS; ++q) {
+                    const int at = col + q * 32;
+                    float w32[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) w32[j] = SUBS > 1 && q == 1 ? v[SUBS - 1][j] : v[0][j];
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        mine[lane * 8 + (c ^ (lane & 7))] = make_float4(w32[c * 4], w32[c * 4 + 1], w32[c * 4 + 2], w32[c * 4 + 3]);
+                    __syncwarp();
+                    if (at + lane < e.N) {
+                        Columns<1> c1;
+                        c1.load(e, at + lane);
+                        const float *flat = reinterpret_cast<const float *>(mine);
+#pragma unroll 1
+                        for (int r = 0; r < 32 && row0 + r < e.M; ++r) {
+                            float w[1] = {flat[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)]}, add[1];
+                            load_residual<O>(e, row0 + r, at + lane, add);
+                            finish<O>(e, row0 + r, at + lane, c1, w, add);
+                        }
                     }
+                    __syncwarp();
                 }
-                __syncwarp();
             }
         };
-        for (int64_t i = worker; ok && i < g.items; i += workers) {
-            const Item t = item_at(g, TILE_M, BN, i);
-            const int col0 = t.n0 + half * COLS;
-            if (ahead && col0 < e.N) fetch_residual(t, col0);   // while the sums are on their way
+        for (Walk t(g, worker); ok && t.more(); t.next()) {
+            const int col0 = t.n0() + half * COLS;
+            const int64_t row0 = (int64_t)t.m0() + m_off;   // (below 2^31 where there are rows)
+            auto next_of = [&](int c) { return c + 1 < CHUNKS ? col0 + (c + 1) * C::WIDTH : -1; };
+            if (by_tma && e.residual && col0 < e.N && row0 < e.M) {   // while the sums are on their way
+                stores_read<0>();
+                fetch_residual(row0, col0, slots + (with_z ? SLOT_BYTES : turn * SLOT_BYTES));
+            }
             Lane lanes[CHUNKS];
 #pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) lanes[c] = fetch_lane(col0 + c * 32);
+            for (int c = 0; c < CHUNKS; ++c) lanes[c] = fetch_lane(col0 + c * C::WIDTH);
             if constexpr (RUNS) {
-                float sum[CHUNKS][32];
+                const int kbn = t.kbn();
+                static_assert(SUBS == 1, "sums in runs are of fp32 outputs");
+                float sum[CHUNKS][1][32];
 #pragma unroll
                 for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) sum[c][j] = 0.f;
-                for (int kb = 0; kb < t.kbn; kb += RUN_KB, ++acc) {
+                    for (int j = 0; j < 32; ++j) sum[c][0][j] = 0.f;
+                for (int kb = 0; kb < kbn; kb += RUN_KB, ++acc) {
                     const uint32_t buf = acc & 1u, use = (acc >> 1) & 1u;
                     if (!(ok = mbar_wait(&sh->t_full[buf], use, abort_flag))) break;
                     tc_fence_after();
@@ -646,18 +692,18 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                             tmem_ld_wait(v);
                             tmem_ld_wait(w);
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) sum[c][j] += __uint_as_float(v[j]) + __uint_as_float(w[j]);
+                            for (int j = 0; j < 32; ++j) sum[c][0][j] += __uint_as_float(v[j]) + __uint_as_float(w[j]);
                         } else {
                             tmem_ld_wait(v);
 #pragma unroll
-                            for (int j = 0; j < 32; ++j) sum[c][j] += __uint_as_float(v[j]);
+                            for (int j = 0; j < 32; ++j) sum[c][0][j] += __uint_as_float(v[j]);
                         }
                     }
                     give_back(buf);
                 }
                 if (!ok) break;
 #pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) finish_chunk(t, col0 + c * 32, c + 1 < CHUNKS ? col0 + (c + 1) * 32 : -1, lanes[c], sum[c]);
+                for (int c = 0; c < CHUNKS; ++c) finish_chunk(t.split, row0, col0 + c * 32, next_of(c), lanes[c], sum[c]);
             } else {
                 const uint32_t buf = acc & 1u, use = (acc >> 1) & 1u;
                 ++acc;
@@ -670,19 +716,23 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
 #pragma unroll
                     for (int q = 1; q < CHUNKS; ++q)
                         if (q == c) now = lanes[q];
-                    uint32_t v[32];
-                    tmem_ld32_issue(taddr + c * 32, v);
-                    tmem_ld_wait(v);
-                    if (c == CHUNKS - 1) give_back(buf);
-                    float f[32];
+                    uint32_t v[SUBS][32];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]);
-                    finish_chunk(t, col0 + c * 32, c + 1 < CHUNKS ? col0 + (c + 1) * 32 : -1, now, f);
+                    for (int q = 0; q < SUBS; ++q) tmem_ld32_issue(taddr + c * C::WIDTH + q * 32, v[q]);
+#pragma unroll
+                    for (int q = 0; q < SUBS; ++q) tmem_ld_wait(v[q]);
+                    if (c == CHUNKS - 1) give_back(buf);
+                    float f[SUBS][32];
+#pragma unroll
+                    for (int q = 0; q < SUBS; ++q)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) f[q][j] = __uint_as_float(v[q][j]);
+                    finish_chunk(t.split, row0, col0 + c * C::WIDTH, next_of(c), now, f);
                 }
             }
         }
         copies_wait<0>();
-        if (lane == 0) tma_stores_read<0>();   // before the block gives its shared memory back
+        stores_read<0>();   // before the block gives its shared memory back
     }
     __syncthreads();
     if constexpr (PAIR) cluster_meet();   // neither block leaves while the other may still signal it
@@ -923,25 +973,27 @@ bool encode_operand(CUtensorMap *map, const Operand &o, bool mn, int box_rows) {
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
-// A matrix [depth][rows][cols] as a warp of the tile kernel writes it: boxes of 32 columns x 32 rows.
-bool encode_result(CUtensorMap *map, void *base, int type, int64_t depth, int64_t rows, int cols, int64_t ld) {
+// A matrix [depth][rows][cols] as a warp of the tile kernel writes it: boxes of 32 rows of 128 bytes
+// (64 bytes where a warp has only 32 columns of 16 bits).
+bool encode_result(CUtensorMap *map, void *base, int type, int64_t depth, int64_t rows, int cols, int64_t ld, int bn) {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return false;
     const cuuint64_t size = (cuuint64_t)ep::type_size(type);
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)depth};
     const cuuint64_t strides[2] = {(cuuint64_t)ld * size, (cuuint64_t)(ld * rows) * size};
-    const cuuint32_t box[3] = {32, 32, 1};
+    const cuuint32_t width = (cuuint32_t)std::min<int64_t>(128 / (int64_t)size, bn / 2);
+    const cuuint32_t box[3] = {width, 32, 1};
     const cuuint32_t estr[3] = {1, 1, 1};
     const CUtensorMapDataType t = type == EP_BF16  ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                   : type == EP_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16
                                                    : CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
     return fn(map, t, 3, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              size == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+              width * size == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 struct GemmPlan {
-    int bn, splits;
+    int bn, splits, workers;
     bool runs, pair;
     int ld_share;
     GemmShape shape;
@@ -962,7 +1014,7 @@ GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, boo
     int64_t best = 0;
     for (int pair = 0; pair <= 1; ++pair)
         for (int bn : {256, 128, 64}) {
-            if (bn == (pair ? 64 : 256) || (p.runs && bn != 128)) continue;
+            if (bn == (pair ? 64 : 256) || (p.runs && bn != (type == EP_F32 && !pair ? 64 : 128))) continue;
             const int64_t tiles = ep::ceil_div(M, pair ? 2 * BM : BM) * ep::ceil_div(N, bn);
             const int64_t waves = ep::ceil_div(tiles, pair ? ctx->sm_count / 2 : ctx->sm_count);
             const int64_t cost = waves * (bn + 32) * (pair ? 7 : 8);
@@ -973,14 +1025,19 @@ GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, boo
             }
         }
     p.shape.tiles_n = (int)ep::ceil_div(N, p.bn);
-    p.shape.tiles = ep::ceil_div(M, p.pair ? 2 * BM : BM) * p.shape.tiles_n;
+    p.shape.tiles_m = (int)ep::ceil_div(M, p.pair ? 2 * BM : BM);
+    p.shape.tiles = (int64_t)p.shape.tiles_m * p.shape.tiles_n;
     const int workers = p.pair ? ctx->sm_count / 2 : ctx->sm_count;
     int64_t splits = std::max<int64_t>(1, std::min<int64_t>(workers / p.shape.tiles, p.shape.kb / 4));
     int per = (int)ep::ceil_div(p.shape.kb, splits);
     if (p.runs) per = (int)round_up(per, RUN_KB);
     p.splits = (int)ep::ceil_div(p.shape.kb, per);
     p.shape.kb_per_split = per;
+    p.shape.splits = p.splits;
     p.shape.items = p.shape.tiles * p.splits;
+    p.workers = (int)std::min<int64_t>(p.shape.items, workers);
+    p.shape.step_m = p.workers / p.shape.tiles_n;
+    p.shape.step_n = p.workers % p.shape.tiles_n;
     p.ld_share = (int)round_up(N, 8);
     return p;
 }
@@ -994,9 +1051,8 @@ int launch_tiles(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &
     auto kernel = linear_tiles<BN, F8, PARTS, RUNS, PAIR, O>;
     constexpr size_t smem = TileMemory<BN, PARTS, PAIR>::TOTAL;
     EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    const int64_t workers = std::min<int64_t>(p.shape.items, PAIR ? ctx->sm_count / 2 : ctx->sm_count);
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(PAIR ? 2 * workers : workers));
+    cfg.gridDim = dim3((unsigned)(PAIR ? 2 * p.workers : p.workers));
     cfg.blockDim = dim3(GEMM_THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
@@ -1039,15 +1095,15 @@ int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand
     Maps m{};
     bool ok = encode_operand(&m.a, a, a_mn, BM) && encode_operand(&m.b, b, b_mn, p.pair ? p.bn / 2 : p.bn);
     if (e.share)
-        ok = ok && encode_result(&m.out, share, EP_F32, p.splits, e.M, p.ld_share, p.ld_share);
+        ok = ok && encode_result(&m.out, share, EP_F32, p.splits, e.M, p.ld_share, p.ld_share, p.bn);
     else if (e.tma)
-        ok = ok && encode_result(&m.out, e.out, e.out_type, 1, e.M, e.N, e.N) &&
-             (!e.preact || encode_result(&m.z, e.preact, e.out_type, 1, e.M, e.N, e.N));
+        ok = ok && encode_result(&m.out, e.out, e.out_type, 1, e.M, e.N, e.N, p.bn) &&
+             (!e.preact || encode_result(&m.z, e.preact, e.out_type, 1, e.M, e.N, e.N, p.bn));
     if (!ok) return ep::fail(ctx, EP_ERR_CUDA, "cuTensorMapEncodeTiled failed for a product of %lld x %d", (long long)e.M, e.N);
     int rc;
     if (a.parts == 3)
         rc = p.pair ? launch_tiles<128, false, 3, true, true, float>(ctx, p, m, e, stream)
-                    : launch_tiles<128, false, 3, true, false, float>(ctx, p, m, e, stream);
+                    : launch_tiles<64, false, 3, true, false, float>(ctx, p, m, e, stream);
     else
         rc = a.type == EP_E4M3 ? launch_type<true>(ctx, p, m, e, stream) : launch_type<false>(ctx, p, m, e, stream);
     if (rc != EP_OK) return rc;
