@@ -44,7 +44,7 @@ struct Epilogue {
 // 6e-8.  The gradient needs the same exponential, and where the slope of z Phi(z) crosses zero the exponential is a common
 // factor of the terms that cancel.
 __device__ __forceinline__ float normal_tail(float z) {
-    const float t = __fdividef(1.f, fmaf(0.33f, fabsf(z), 1.f));
+    const float t = reciprocal_fast(fmaf(0.33f, fabsf(z), 1.f));
     float q = fmaf(0.0436886735f, t, -0.211661354f);
     q = fmaf(q, t, 0.313509107f);
     q = fmaf(q, t, -0.0706691593f);
@@ -54,11 +54,11 @@ __device__ __forceinline__ float normal_tail(float z) {
     return q * t;
 }
 __device__ __forceinline__ float gelu(float z) {
-    const float tail = normal_tail(z) * __expf(-0.5f * z * z);
+    const float tail = normal_tail(z) * exp2_fast(z * z * (-0.5f * 1.44269504f));
     return z * (z >= 0.f ? 1.f - tail : tail);
 }
 __device__ __forceinline__ float gelu_slope(float z) {
-    const float bell = __expf(-0.5f * z * z);
+    const float bell = exp2_fast(z * z * (-0.5f * 1.44269504f));
     const float q = fmaf(fabsf(z), -0.39894228f, normal_tail(z));
     return z >= 0.f ? fmaf(-q, bell, 1.f) : q * bell;
 }
@@ -74,7 +74,7 @@ __device__ __forceinline__ void activate(float (&v)[n], int act) {
         for (int i = 0; i < n; ++i) v[i] = gelu(v[i]);
     } else if (act == EP_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < n; ++i) v[i] = __fdividef(v[i], 1.f + __expf(fminf(-v[i], 80.f)));
+        for (int i = 0; i < n; ++i) v[i] *= reciprocal_fast(1.f + exp_fast(fminf(-v[i], 80.f)));
     }
 }
 // v *= act'(z)
@@ -89,7 +89,7 @@ __device__ __forceinline__ void times_slope(float (&v)[n], const float (&z)[n], 
     } else if (act == EP_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < n; ++i) {
-            const float s = __fdividef(1.f, 1.f + __expf(fminf(-z[i], 80.f)));
+            const float s = reciprocal_fast(1.f + exp_fast(fminf(-z[i], 80.f)));
             v[i] *= s * fmaf(z[i], 1.f - s, 1.f);
         }
     }
@@ -890,7 +890,7 @@ __global__ void __launch_bounds__(DZ_CHUNKS *DZ_ROWS) linear_dz(const D *__restr
                 times_slope(v, zz, act);
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += col + i < n_out ? v[i] : 0.f;
+            for (int i = 0; i < 8; ++i) sum[i] += v[i];   // (zero past the row's end: dout reads as zero there)
             if (to_raw) {
                 if constexpr (PARTS == 3) {
                     __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(to_raw) + row * ld_to + col;
@@ -1000,46 +1000,52 @@ struct GemmPlan {
     size_t share_bytes(int64_t M) const { return splits > 1 ? sizeof(float) * (size_t)splits * (size_t)M * (size_t)ld_share : 0; }
 };
 
-// Tile and split of the sum.  A block's time for a tile is about its columns plus a constant (the A tile, the
-// pipeline's start), so of the widths, alone and in pairs, the one with the least waves x (columns + 32) is taken; a pair
-// counts 7/8, for the operand bytes that it saves.  When all tiles fit one wave with blocks to spare, the sum over k is
-// split between them, into shares of at least 4 k-blocks.
+// Tile and split of the sum, by the clocks that a launch would take.  A k-block costs the longer of its MMAs (128 x bn x
+// 64 products at 4096 a clock and SM) and its operands' bytes (64 a clock and SM from the L2); a tile's end 20 clocks a
+// column and 1000 more; the join of a split sum 5000 and its shares' bytes (3400 a clock).  The sum is only split while
+// the tiles leave workers idle, into shares of at least 4 k-blocks.  (With the largest tile that fills one wave instead,
+// the weights' gradient of 232965 x 256 x 256 went by tiles of 64 columns that read each operand up to four times.)
 GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, bool fp32_out) {
-    GemmPlan p{};
-    p.runs = fp32_out;
-    const int ke = type == EP_E4M3 ? 128 : 64;
-    p.shape.M = M;
-    p.shape.N = N;
-    p.shape.kb = (int)ep::ceil_div(K, ke);
-    int64_t best = 0;
+    const int ke = type == EP_E4M3 ? 128 : 64, parts = type == EP_F32 ? 3 : 1;
+    const int kb = (int)ep::ceil_div(K, ke);
+    GemmPlan best{};
+    double best_cost = 0.0;
     for (int pair = 0; pair <= 1; ++pair)
         for (int bn : {256, 128, 64}) {
-            if (bn == (pair ? 64 : 256) || (p.runs && bn != (type == EP_F32 && !pair ? 64 : 128))) continue;
-            const int64_t tiles = ep::ceil_div(M, pair ? 2 * BM : BM) * ep::ceil_div(N, bn);
-            const int64_t waves = ep::ceil_div(tiles, pair ? ctx->sm_count / 2 : ctx->sm_count);
-            const int64_t cost = waves * (bn + 32) * (pair ? 7 : 8);
-            if (!p.bn || cost < best) {
-                best = cost;
-                p.bn = bn;
-                p.pair = pair;
+            if (bn == (pair ? 64 : 256) || (fp32_out && bn != (parts == 3 && !pair ? 64 : 128))) continue;
+            GemmPlan p{};
+            p.runs = fp32_out;
+            p.pair = pair;
+            p.bn = bn;
+            p.shape.M = M;
+            p.shape.N = N;
+            p.shape.kb = kb;
+            p.shape.tiles_n = (int)ep::ceil_div(N, bn);
+            p.shape.tiles_m = (int)ep::ceil_div(M, pair ? 2 * BM : BM);
+            p.shape.tiles = (int64_t)p.shape.tiles_m * p.shape.tiles_n;
+            const int workers = pair ? ctx->sm_count / 2 : ctx->sm_count;
+            const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(workers / p.shape.tiles, kb / 4));
+            int per = (int)ep::ceil_div(kb, splits);
+            if (p.runs) per = (int)round_up(per, RUN_KB);
+            p.splits = (int)ep::ceil_div(kb, per);
+            p.shape.splits = p.splits;
+            p.shape.kb_per_split = per;
+            p.shape.items = p.shape.tiles * p.splits;
+            p.workers = (int)std::min<int64_t>(p.shape.items, workers);
+            p.shape.step_m = p.workers / p.shape.tiles_n;
+            p.shape.step_n = p.workers % p.shape.tiles_n;
+            p.ld_share = (int)round_up(N, 8);
+            const double mma = (parts == 3 ? 6 : 1) * 2.0 * bn;
+            const double load = parts * (16384.0 + 128.0 * (pair ? bn / 2 : bn)) / 64.0;
+            const double item = per * std::max(mma, load) + 20.0 * bn + 1000.0;
+            const double cost = ep::ceil_div(p.shape.items, p.workers) * item +
+                                (p.splits > 1 ? 5000.0 + p.share_bytes(M) / 3400.0 : 0.0);
+            if (!best.bn || cost < best_cost) {
+                best_cost = cost;
+                best = p;
             }
         }
-    p.shape.tiles_n = (int)ep::ceil_div(N, p.bn);
-    p.shape.tiles_m = (int)ep::ceil_div(M, p.pair ? 2 * BM : BM);
-    p.shape.tiles = (int64_t)p.shape.tiles_m * p.shape.tiles_n;
-    const int workers = p.pair ? ctx->sm_count / 2 : ctx->sm_count;
-    int64_t splits = std::max<int64_t>(1, std::min<int64_t>(workers / p.shape.tiles, p.shape.kb / 4));
-    int per = (int)ep::ceil_div(p.shape.kb, splits);
-    if (p.runs) per = (int)round_up(per, RUN_KB);
-    p.splits = (int)ep::ceil_div(p.shape.kb, per);
-    p.shape.kb_per_split = per;
-    p.shape.splits = p.splits;
-    p.shape.items = p.shape.tiles * p.splits;
-    p.workers = (int)std::min<int64_t>(p.shape.items, workers);
-    p.shape.step_m = p.workers / p.shape.tiles_n;
-    p.shape.step_n = p.workers % p.shape.tiles_n;
-    p.ld_share = (int)round_up(N, 8);
-    return p;
+    return best;
 }
 
 struct Maps {
@@ -1168,7 +1174,7 @@ int make_operand(ep_ctx *ctx, const void *base, int64_t ld, int64_t rows, int co
 }
 
 bool linear_shape_ok(int64_t rows, int n_in, int n_out) {
-    return rows >= 0 && rows < (1ll << 31) && n_in >= 1 && n_in <= MAX_WIDTH && n_out >= 1 && n_out <= MAX_WIDTH;
+    return rows >= 0 && rows <= (1ll << 31) - 256 && n_in >= 1 && n_in <= MAX_WIDTH && n_out >= 1 && n_out <= MAX_WIDTH;
 }
 bool linear_types_ok(int in_type, int out_type) {
     if (in_type == EP_E4M3) return ep::float_type(out_type);

@@ -165,11 +165,11 @@ __global__ void __launch_bounds__(THREADS) route_rows(const T *__restrict__ logi
         for (int j = 0; j < V; ++j)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                e[j][i] = __expf(l[j][i] - shift);
+                e[j][i] = exp_fast(l[j][i] - shift);
                 s += e[j][i];
             }
         s = reduce_row<L, OpSum>(s, slots, turn);
-        const float inverse = part ? __fdividef(1.f, s) : 0.f;
+        const float inverse = part ? reciprocal_fast(s) : 0.f;
 #pragma unroll
         for (int j = 0; j < V; ++j)
 #pragma unroll
@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(THREADS) route_rows(const T *__restrict__ logi
             }
             best_of_row<L>(v, c, slot_v, slot_c, turn_best);
             const bool got = v > -INFINITY;
-            const float w = got ? __expf(v - top) * inverse : 0.f;
+            const float w = got ? exp_fast(v - top) * inverse : 0.f;
             chosen_sum += w;
             if (lane == r % L) {
                 if (mine) {
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(THREADS) route_rows(const T *__restrict__ logi
             }
         }
         if (renormalize && mine) {
-            const float scale = part ? __fdividef(1.f, chosen_sum) : 0.f;
+            const float scale = part ? reciprocal_fast(chosen_sum) : 0.f;
             if (lane < k) weights[row * k + lane] = my_w * scale;
             for (int r = lane + L; r < k; r += L) weights[row * k + r] *= scale;   // this thread's own earlier stores
         }
@@ -351,13 +351,13 @@ __global__ void __launch_bounds__(THREADS) route_rows_backward(const T *__restri
         for (int j = 0; j < V; ++j)
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                p[j][i] = __expf(p[j][i] - shift);
+                p[j][i] = exp_fast(p[j][i] - shift);
                 s += p[j][i];
                 dot = fmaf(p[j][i], slope[j][i], dot);
             }
         s = reduce_row<L, OpSum>(s, slots, turn);
         dot = reduce_row<L, OpSum>(dot, slots, turn);
-        const float inverse = part ? __fdividef(1.f, s) : 0.f;
+        const float inverse = part ? reciprocal_fast(s) : 0.f;
         dot *= inverse;
         // the slots, shared out over the row's threads: sum of p and of dweights p.  A thread keeps its first slot.
         float chosen = 0.f, pulled = 0.f, first_w = 0.f, first_dw = 0.f;
@@ -370,7 +370,7 @@ __global__ void __launch_bounds__(THREADS) route_rows_backward(const T *__restri
                         if (id != -1) ep_raise(status, EP_ERR_BAD_INDEX);
                         continue;
                     }
-                    const float w = __expf(to_f32(from[id]) - top) * inverse, dw = dweights[row * k + q];
+                    const float w = exp_fast(to_f32(from[id]) - top) * inverse, dw = dweights[row * k + q];
                     chosen += w;
                     pulled = fmaf(dw, w, pulled);
                     if (q == lane) {
@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(THREADS) route_rows_backward(const T *__restri
             if (first_id >= 0) again(first_id, first_w, first_dw);
             for (int q = lane + L; q < k; q += L) {
                 const int id = ids[row * k + q];
-                if (id >= 0 && id < parts) again(id, __expf(to_f32(from[id]) - top) * inverse, dweights[row * k + q]);
+                if (id >= 0 && id < parts) again(id, exp_fast(to_f32(from[id]) - top) * inverse, dweights[row * k + q]);
             }
         }
     }

@@ -15,6 +15,20 @@ namespace eprow {
 
 constexpr unsigned FULL = 0xffffffffu;
 
+// 2^x, e^x and 1 / x by the special function unit: within a few units of 2^-22 of themselves (times |x| 2^-24 more for
+// e^x), results below 2^-126 are zero.
+__device__ __forceinline__ float exp2_fast(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float exp_fast(float x) { return exp2_fast(x * 1.44269504f); }
+__device__ __forceinline__ float reciprocal_fast(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 struct e4m3 {
     uint8_t bits;
 };
