@@ -53,14 +53,69 @@ __device__ __forceinline__ float normal_tail(float z) {
     q = fmaf(q, t, 0.132185712f);
     return q * t;
 }
-__device__ __forceinline__ float gelu(float z) {
-    const float tail = normal_tail(z) * exp2_fast(z * z * (-0.5f * 1.44269504f));
-    return z * (z >= 0.f ? 1.f - tail : tail);
-}
 __device__ __forceinline__ float gelu_slope(float z) {
     const float bell = exp2_fast(z * z * (-0.5f * 1.44269504f));
     const float q = fmaf(fabsf(z), -0.39894228f, normal_tail(z));
     return z >= 0.f ? fmaf(-q, bell, 1.f) : q * bell;
+}
+
+// Two floats that go through one instruction (the fp32 pipe takes pairs): GELU costs half as much issue time so.
+struct Pair {
+    unsigned long long v;
+    __device__ __forceinline__ Pair() {}
+    __device__ __forceinline__ Pair(float lo, float hi) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi)); }
+    __device__ __forceinline__ explicit Pair(float both) : Pair(both, both) {}
+    __device__ __forceinline__ void get(float &lo, float &hi) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+};
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+// For z = (z0, z1): the bell exp(-z^2 / 2), |z| and the polynomial above.
+__device__ __forceinline__ void normal_parts(float z0, float z1, Pair &bell, Pair &size, Pair &tail) {
+    const Pair z(z0, z1);
+    size = Pair(fabsf(z0), fabsf(z1));
+    float a, b;
+    fma2(size, Pair(0.33f), Pair(1.f)).get(a, b);
+    const Pair t(reciprocal_fast(a), reciprocal_fast(b));
+    Pair q = fma2(t, Pair(0.0436886735f), Pair(-0.211661354f));
+    q = fma2(q, t, Pair(0.313509107f));
+    q = fma2(q, t, Pair(-0.0706691593f));
+    q = fma2(q, t, Pair(0.170115322f));
+    q = fma2(q, t, Pair(0.122831702f));
+    q = fma2(q, t, Pair(0.132185712f));
+    tail = mul2(q, t);
+    mul2(mul2(z, z), Pair(-0.5f * 1.44269504f)).get(a, b);
+    bell = Pair(exp2_fast(a), exp2_fast(b));
+}
+// 1/2 + sign(z) (1/2 - m) for both: Phi(z) and the slope of z Phi(z) from what they are below zero.
+__device__ __forceinline__ Pair from_lower(float z0, float z1, Pair m_minus_half) {
+    float a, b;
+    m_minus_half.get(a, b);
+    return add2(Pair(0.5f), Pair(copysignf(a, z0), copysignf(b, z1)));
+}
+__device__ __forceinline__ void gelu2(float &v0, float &v1) {
+    Pair bell, size, tail;
+    normal_parts(v0, v1, bell, size, tail);
+    mul2(Pair(v0, v1), from_lower(v0, v1, fma2(tail, mul2(bell, Pair(-1.f)), Pair(0.5f)))).get(v0, v1);
+}
+// v *= slope of GELU at z (to 6e-8 of 1: for operands that are rounded to 16 bits afterwards)
+__device__ __forceinline__ void times_gelu_slope2(float &v0, float &v1, float z0, float z1) {
+    Pair bell, size, tail;
+    normal_parts(z0, z1, bell, size, tail);
+    const Pair q = fma2(size, Pair(0.39894228f), mul2(tail, Pair(-1.f)));   // (minus the lower value, over the bell)
+    mul2(Pair(v0, v1), from_lower(z0, z1, fma2(q, bell, Pair(0.5f)))).get(v0, v1);
 }
 
 // act(z) of n values; the switch is outside the loops, and taken by all threads alike.
@@ -71,21 +126,31 @@ __device__ __forceinline__ void activate(float (&v)[n], int act) {
         for (int i = 0; i < n; ++i) asm("max.NaN.f32 %0, %0, 0f00000000;" : "+f"(v[i]));   // (a NaN stays one)
     } else if (act == EP_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < n; ++i) v[i] = gelu(v[i]);
+        for (int i = 0; i + 1 < n; i += 2) gelu2(v[i], v[i + 1]);
+        if constexpr (n % 2 == 1) {
+            float none = 0.f;
+            gelu2(v[n - 1], none);
+        }
     } else if (act == EP_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < n; ++i) v[i] *= reciprocal_fast(1.f + exp_fast(fminf(-v[i], 80.f)));
     }
 }
-// v *= act'(z)
-template <int n>
+// v *= act'(z).  EXACT: where the product stays fp32.
+template <bool EXACT, int n>
 __device__ __forceinline__ void times_slope(float (&v)[n], const float (&z)[n], int act) {
     if (act == EP_ACT_RELU) {
 #pragma unroll
         for (int i = 0; i < n; ++i) v[i] = z[i] > 0.f ? v[i] : 0.f;
     } else if (act == EP_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < n; ++i) v[i] *= gelu_slope(z[i]);
+        for (int i = 0; i < n; i += 2) {
+            if constexpr (EXACT) {
+                v[i] *= gelu_slope(z[i]);
+                v[i + 1] *= gelu_slope(z[i + 1]);
+            } else
+                times_gelu_slope2(v[i], v[i + 1], z[i], z[i + 1]);
+        }
     } else if (act == EP_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < n; ++i) {
@@ -648,11 +713,14 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                         c1.load(e, at + lane);
                         const float *flat = reinterpret_cast<const float *>(mine);
 #pragma unroll 1
-                        for (int r = 0; r < 32 && row0 + r < e.M; ++r) {
-                            float w[1] = {flat[r * 32 + (((lane >> 2) ^ (r & 7)) << 2) + (lane & 3)]}, add[1];
-                            load_residual<O>(e, row0 + r, at + lane, add);
-                            finish<O>(e, row0 + r, at + lane, c1, w, add);
-                        }
+                        for (int r8 = 0; r8 < 32; r8 += 8)
+#pragma unroll
+                            for (int r = 0; r < 8; ++r) {
+                                if (row0 + r8 + r >= e.M) break;
+                                float w[1] = {flat[(r8 + r) * 32 + (((lane >> 2) ^ r) << 2) + (lane & 3)]}, add[1];
+                                load_residual<O>(e, row0 + r8 + r, at + lane, add);
+                                finish<O>(e, row0 + r8 + r, at + lane, c1, w, add);
+                            }
                     }
                     __syncwarp();
                 }
@@ -746,28 +814,40 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
     }
 }
 
-// The shares of a split sum added in order, then the epilogue.  A thread finishes 8 columns of a row.
+// The shares of a split sum, then the epilogue: 32 chunks of 8 columns a block, 8 threads to each, which add the shares
+// s, s + 8, ... in order; then the eight in order.
+__host__ __device__ constexpr int join_chunks() { return 32; }
 template <typename O>
 __global__ void __launch_bounds__(256) linear_join(const float *__restrict__ shares, int splits, const Epilogue e) {
+    __shared__ float part[8][join_chunks()][9];
     const int chunks = (e.N + 7) / 8;
-    const int64_t total = e.M * chunks;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
-        const int64_t row = i / chunks;
-        const int col = (int)(i - row * chunks) * 8;
-        const float *from = shares + row * e.ld_share + col;
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    const int64_t total = e.M * chunks, i = (int64_t)blockIdx.x * join_chunks() + (threadIdx.x & 31);
+    const int s0 = threadIdx.x >> 5;
+    const int64_t row = i / chunks;
+    const int col = (int)(i - row * chunks) * 8;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (i < total) {
+        const float *from = shares + ((int64_t)s0 * e.M + row) * e.ld_share + col;
 #pragma unroll 4
-        for (int s = 0; s < splits; ++s, from += e.M * e.ld_share) {
+        for (int s = s0; s < splits; s += 8, from += 8 * e.M * e.ld_share) {
             const float4 a = *reinterpret_cast<const float4 *>(from), b = *reinterpret_cast<const float4 *>(from + 4);
             v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w;
             v[4] += b.x, v[5] += b.y, v[6] += b.z, v[7] += b.w;
         }
-        Columns<8> c;
-        c.load(e, col);
-        float add[8];
-        load_residual<O>(e, row, col, add);
-        finish<O>(e, row, col, c, v, add);
     }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) part[s0][threadIdx.x & 31][q] = v[q];
+    __syncthreads();
+    if (s0 > 0 || i >= total) return;
+#pragma unroll
+    for (int s = 1; s < 8; ++s)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] += part[s][threadIdx.x][q];
+    Columns<8> c;
+    c.load(e, col);
+    float add[8];
+    load_residual<O>(e, row, col, add);
+    finish<O>(e, row, col, c, v, add);
 }
 
 // ---------------------------------------------------------------------------------------------- few rows
@@ -832,19 +912,28 @@ __device__ __forceinline__ void split3(float x, __nv_bfloat16 (&p)[3]) {
     p[2] = __float2bfloat16_rn(r - __bfloat162float(p[1]));
 }
 
-// Copies rows of `cols` elements, `ld` apart, to rows ld_to apart (a multiple of 16 bytes; the tail is zero).
-// PARTS == 3: fp32 to three bf16 matrices, part_stride elements apart.
+// Copies matrices, rows of `cols` elements `ld` apart, to rows ld_to apart (a multiple of 16 bytes; the tail is zero).
+// PARTS == 3: fp32 to three bf16 matrices, part_stride elements apart.  blockIdx.y chooses one of two matrices.
+struct PackJob {
+    const void *from;
+    void *to;
+    int64_t ld, rows, part_stride;
+    int cols, ld_to;
+    bool vec;
+};
 template <typename T, typename O, int PARTS>
-__global__ void __launch_bounds__(256) pack_rows(const T *__restrict__ from, int64_t ld, int64_t rows, int cols, O *__restrict__ to,
-                                                 int ld_to, int64_t part_stride, bool vec) {
-    const int chunks = ld_to / 8;
-    const int64_t total = rows * chunks;
+__global__ void __launch_bounds__(256) pack_rows(const PackJob first, const PackJob second) {
+    const PackJob &j = blockIdx.y ? second : first;
+    const T *from = static_cast<const T *>(j.from);
+    O *to = static_cast<O *>(j.to);
+    const int chunks = j.ld_to / 8;
+    const int64_t total = j.rows * chunks;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
         const int64_t row = i / chunks;
         const int col = (int)(i - row * chunks) * 8;
         if constexpr (PARTS == 3) {
             float v[8];
-            load_chunk(from + row * ld, col, cols, vec, 0.f, v);
+            load_chunk(from + row * j.ld, col, j.cols, j.vec, 0.f, v);
             __nv_bfloat16 p[8][3];
 #pragma unroll
             for (int q = 0; q < 8; ++q) split3(v[q], p[q]);
@@ -853,14 +942,14 @@ __global__ void __launch_bounds__(256) pack_rows(const T *__restrict__ from, int
                 alignas(16) __nv_bfloat16 o[8];
 #pragma unroll
                 for (int q = 0; q < 8; ++q) o[q] = p[q][k];
-                *reinterpret_cast<uint4 *>(to + k * part_stride + row * ld_to + col) = *reinterpret_cast<const uint4 *>(o);
+                *reinterpret_cast<uint4 *>(to + k * j.part_stride + row * j.ld_to + col) = *reinterpret_cast<const uint4 *>(o);
             }
         } else {
             alignas(16) O o[8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) o[q] = col + q < cols ? from[row * ld + col + q] : O{};
+            for (int q = 0; q < 8; ++q) o[q] = col + q < j.cols ? from[row * j.ld + col + q] : O{};
             using R = typename Raw<8 * (int)sizeof(O)>::type;
-            *reinterpret_cast<R *>(to + row * ld_to + col) = *reinterpret_cast<const R *>(o);
+            *reinterpret_cast<R *>(to + row * j.ld_to + col) = *reinterpret_cast<const R *>(o);
         }
     }
 }
@@ -868,52 +957,96 @@ __global__ void __launch_bounds__(256) pack_rows(const T *__restrict__ from, int
 // dz = dout act'(z), written for the products (16 bits as they are, fp32 as three bf16 parts; rows ld_to apart, zero
 // beyond N), and the sums of its columns over this block's rows: part[blockIdx.y][N].
 constexpr int DZ_CHUNKS = 16, DZ_ROWS = 16;   // a block covers 128 columns, 16 rows at a time
+constexpr int DZ_THREADS = DZ_CHUNKS * DZ_ROWS;
+constexpr int DZ_STAGES = 4;                  // rows in flight per thread and one more (see the ring in rows.cuh)
+template <typename T, typename D>
+constexpr int dz_pieces() { return (8 * (int)(sizeof(T) + sizeof(D))) / 16; }   // 16-byte pieces of 8 elements of dout and z
 template <typename T, typename D, int PARTS>
-__global__ void __launch_bounds__(DZ_CHUNKS *DZ_ROWS) linear_dz(const D *__restrict__ dout, const T *__restrict__ z, int act,
-                                                                int64_t rows, int n_out, void *to_raw, int ld_to,
-                                                                int64_t part_stride, float *__restrict__ part, int64_t slab,
-                                                                bool vec) {
+__global__ void __launch_bounds__(DZ_THREADS) linear_dz(const D *__restrict__ dout, const T *__restrict__ z, int act, int64_t rows,
+                                                        int n_out, void *to_raw, int ld_to, int64_t part_stride,
+                                                        float *__restrict__ part, int64_t slab, bool vec) {
+    constexpr int D_PIECES = 8 * (int)sizeof(D) / 16, Z_PIECES = 8 * (int)sizeof(T) / 16;
     __shared__ float fold[DZ_ROWS][DZ_CHUNKS * 8];
+    extern __shared__ uint4 ring[];   // [DZ_STAGES][D_PIECES + Z_PIECES][DZ_THREADS], where vec
     const int cx = threadIdx.x % DZ_CHUNKS, r0 = threadIdx.x / DZ_CHUNKS;
     const int col = (blockIdx.x * DZ_CHUNKS + cx) * 8;
     const int64_t begin = (int64_t)blockIdx.y * slab, end = min(rows, begin + slab);
     float sum[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.f;
-    if (col < ld_to)
-        for (int64_t row = begin + r0; row < end; row += DZ_ROWS) {
-            float v[8];
-            load_chunk(dout + row * n_out, col, n_out, vec, 0.f, v);
-            if (act != EP_ACT_NONE) {
-                float zz[8];
-                load_chunk(z + row * n_out, col, n_out, vec, 0.f, zz);
-                times_slope(v, zz, act);
+    auto work = [&](int64_t row, float(&v)[8], const float(&zz)[8]) {
+        if (act != EP_ACT_NONE) times_slope<PARTS == 3>(v, zz, act);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += v[i];   // (zero past the row's end: dout reads as zero there)
+        if (!to_raw) return;
+        if constexpr (PARTS == 3) {
+            __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(to_raw) + row * ld_to + col;
+            __nv_bfloat16 p[8][3];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) split3(v[q], p[q]);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                alignas(16) __nv_bfloat16 o[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) o[q] = p[q][k];
+                *reinterpret_cast<uint4 *>(to + k * part_stride) = *reinterpret_cast<const uint4 *>(o);
             }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += v[i];   // (zero past the row's end: dout reads as zero there)
-            if (to_raw) {
-                if constexpr (PARTS == 3) {
-                    __nv_bfloat16 *to = static_cast<__nv_bfloat16 *>(to_raw) + row * ld_to + col;
-                    __nv_bfloat16 p[8][3];
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) split3(v[q], p[q]);
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) {
-                        alignas(16) __nv_bfloat16 o[8];
-#pragma unroll
-                        for (int q = 0; q < 8; ++q) o[q] = p[q][k];
-                        *reinterpret_cast<uint4 *>(to + k * part_stride) = *reinterpret_cast<const uint4 *>(o);
-                    }
-                } else {
-                    store_chunk(static_cast<T *>(to_raw) + row * ld_to, col, ld_to, true, v);
-                }
-            }
+        } else {
+            store_chunk(static_cast<T *>(to_raw) + row * ld_to, col, ld_to, true, v);
         }
+    };
+    if (vec) {
+        auto slot = [&](int s) { return ring + (size_t)s * (D_PIECES + Z_PIECES) * DZ_THREADS + threadIdx.x; };
+        auto fetch = [&](int64_t row, int s) {
+            if (row < end && col < n_out) {
+                uint4 *to = slot(s);
+#pragma unroll
+                for (int p = 0; p < D_PIECES; ++p) copy_async<16>(to + p * DZ_THREADS, reinterpret_cast<const uint4 *>(dout + row * n_out + col) + p);
+                if (act != EP_ACT_NONE)
+#pragma unroll
+                    for (int p = 0; p < Z_PIECES; ++p)
+                        copy_async<16>(to + (D_PIECES + p) * DZ_THREADS, reinterpret_cast<const uint4 *>(z + row * n_out + col) + p);
+            }
+            copies_end_group();
+        };
+        int64_t ahead = begin + r0;
+#pragma unroll
+        for (int s = 0; s < DZ_STAGES - 1; ++s, ahead += DZ_ROWS) fetch(ahead, s);
+        int s = 0;
+        for (int64_t row = begin + r0; row < end; row += DZ_ROWS, ahead += DZ_ROWS) {
+            fetch(ahead, s == 0 ? DZ_STAGES - 1 : s - 1);   // into the slots of the row before
+            copies_wait<DZ_STAGES - 1>();
+            if (col < n_out) {   // (whole chunks: rows of ld_to and of n_out elements end at the same one)
+                float v[8], zz[8];
+                const uint4 *from = slot(s);
+                auto held = [&](auto type, int at, float(&to)[8]) {
+                    using E = decltype(type);
+                    alignas(16) E e[8];
+#pragma unroll
+                    for (int p = 0; p < 8 * (int)sizeof(E) / 16; ++p) reinterpret_cast<uint4 *>(e)[p] = from[(at + p) * DZ_THREADS];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) to[i] = to_f32(e[i]);
+                };
+                held(D{}, 0, v);
+                if (act != EP_ACT_NONE) held(T{}, D_PIECES, zz);
+                work(row, v, zz);
+            }
+            s = s + 1 == DZ_STAGES ? 0 : s + 1;
+        }
+        copies_wait<0>();
+    } else if (col < ld_to) {
+        for (int64_t row = begin + r0; row < end; row += DZ_ROWS) {
+            float v[8], zz[8];
+            load_chunk(dout + row * n_out, col, n_out, false, 0.f, v);
+            if (act != EP_ACT_NONE) load_chunk(z + row * n_out, col, n_out, false, 0.f, zz);
+            work(row, v, zz);
+        }
+    }
     if (!part) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) fold[r0][cx * 8 + i] = sum[i];
     __syncthreads();
-    for (int c = threadIdx.x; c < DZ_CHUNKS * 8; c += DZ_CHUNKS * DZ_ROWS) {
+    for (int c = threadIdx.x; c < DZ_CHUNKS * 8; c += DZ_THREADS) {
         const int to = blockIdx.x * DZ_CHUNKS * 8 + c;
         if (to >= n_out) continue;
         float t = 0.f;
@@ -1115,8 +1248,8 @@ int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand
     if (rc != EP_OK) return rc;
     ++*kernels;
     if (p.splits > 1) {
-        const int64_t threads = e.M * ((e.N + 7) / 8);
-        const int grid = (int)std::min<int64_t>(ep::ceil_div(threads, 256), (int64_t)ctx->sm_count * PACK_BLOCKS_PER_SM);
+        // (a split sum has at most as many tiles as there are SMs: the grid is far below its limit)
+        const unsigned grid = (unsigned)ep::ceil_div(e.M * ((e.N + 7) / 8), join_chunks());
         if (e.out_type == EP_BF16)
             linear_join<__nv_bfloat16><<<grid, 256, 0, stream>>>(share, p.splits, e);
         else if (e.out_type == EP_F16)
@@ -1147,29 +1280,38 @@ Packed packed_form(int64_t rows, int cols, int type) {
     return p;
 }
 
-// `base` as an operand, copied to `room` first where it has to be (needs_copy).
-int make_operand(ep_ctx *ctx, const void *base, int64_t ld, int64_t rows, int cols, int type, bool needs_copy, void *room,
-                 cudaStream_t stream, Operand *out, int *kernels) {
-    if (!needs_copy) {
-        *out = Operand{base, type, rows, cols, ld, 1, 0};
-        return EP_OK;
-    }
-    const Packed p = packed_form(rows, cols, type);
-    const int64_t threads = rows * (p.ld / 8);
-    const int grid = (int)std::min<int64_t>(ep::ceil_div(threads, 256), (int64_t)ctx->sm_count * PACK_BLOCKS_PER_SM);
-    const bool vec = ep::aligned(base, 16) && ld * ep::type_size(type) % 16 == 0 && cols % 8 == 0;
+struct Matrix {
+    const void *base;   // NULL: not wanted
+    int64_t ld, rows;
+    int cols;
+    void *room;         // for its copy
+};
+// Two matrices as operands, copied first (in one launch) where they have to be.
+int make_operands(ep_ctx *ctx, const Matrix &first, const Matrix &second, int type, bool needs_copy, cudaStream_t stream,
+                  Operand *a, Operand *b, int *kernels) {
+    auto operand = [&](const Matrix &m) {
+        if (!needs_copy) return Operand{m.base, type, m.rows, m.cols, m.ld, 1, 0};
+        const Packed p = packed_form(m.rows, m.cols, type);
+        return Operand{m.room, p.type, m.rows, m.cols, p.ld, p.parts, p.part_stride};
+    };
+    *a = operand(first);
+    *b = operand(second);
+    if (!needs_copy) return EP_OK;
+    auto job = [&](const Matrix &m) {
+        const Packed p = packed_form(m.rows, m.cols, type);
+        return PackJob{m.base, m.room, m.ld, m.base ? m.rows : 0, p.part_stride, m.cols, p.ld, tma_ready(m.base, m.ld, type) && m.cols % 8 == 0};
+    };
+    const PackJob x = job(first), w = job(second);
+    const int64_t threads = std::max(x.rows * (x.ld_to / 8), w.rows * (w.ld_to / 8));
+    const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(threads, 256), (int64_t)ctx->sm_count * PACK_BLOCKS_PER_SM)), 2);
     if (type == EP_F32)
-        pack_rows<float, __nv_bfloat16, 3><<<grid, 256, 0, stream>>>(static_cast<const float *>(base), ld, rows, cols,
-                                                                     static_cast<__nv_bfloat16 *>(room), p.ld, p.part_stride, vec);
+        pack_rows<float, __nv_bfloat16, 3><<<grid, 256, 0, stream>>>(x, w);
     else if (type == EP_E4M3)
-        pack_rows<uint8_t, uint8_t, 1><<<grid, 256, 0, stream>>>(static_cast<const uint8_t *>(base), ld, rows, cols,
-                                                                 static_cast<uint8_t *>(room), p.ld, p.part_stride, vec);
+        pack_rows<uint8_t, uint8_t, 1><<<grid, 256, 0, stream>>>(x, w);
     else
-        pack_rows<uint16_t, uint16_t, 1><<<grid, 256, 0, stream>>>(static_cast<const uint16_t *>(base), ld, rows, cols,
-                                                                   static_cast<uint16_t *>(room), p.ld, p.part_stride, vec);
+        pack_rows<uint16_t, uint16_t, 1><<<grid, 256, 0, stream>>>(x, w);
     EP_CUDA(ctx, cudaGetLastError());
     ++*kernels;
-    *out = Operand{room, p.type, rows, cols, p.ld, p.parts, p.part_stride};
     return EP_OK;
 }
 
@@ -1256,7 +1398,10 @@ template <typename T, typename D, int PARTS>
 void launch_dz(const BackwardWorkspace &w, const void *dout, const void *z, int act, int64_t rows, int n_out, bool write, bool sum,
                bool vec, cudaStream_t stream) {
     const dim3 grid((unsigned)ep::ceil_div(w.dz_form.ld, DZ_CHUNKS * 8), (unsigned)w.slabs);
-    linear_dz<T, D, PARTS><<<grid, DZ_CHUNKS * DZ_ROWS, 0, stream>>>((const D *)dout, (const T *)z, act, rows, n_out,
+    const size_t smem = vec ? (size_t)DZ_STAGES * dz_pieces<T, D>() * DZ_THREADS * 16 : 0;
+    cudaFuncSetAttribute(linear_dz<T, D, PARTS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                         DZ_STAGES * dz_pieces<T, D>() * DZ_THREADS * 16);
+    linear_dz<T, D, PARTS><<<grid, DZ_THREADS, smem, stream>>>((const D *)dout, (const T *)z, act, rows, n_out,
                                                                      write ? w.dz : nullptr, w.dz_form.ld, w.dz_form.part_stride,
                                                                      sum ? w.dbias_parts : nullptr, w.slab, vec);
 }
@@ -1274,8 +1419,8 @@ int linear_run(ep_ctx *ctx, const LinearWorkspace &ws, const void *x, int64_t ld
     }
     const bool copy = in_type == EP_F32 || !aligned;
     Operand a, b;
-    int rc = make_operand(ctx, x, ldx, rows, n_in, in_type, copy, ws.x, stream, &a, kernels);
-    if (rc == EP_OK) rc = make_operand(ctx, w, ldw, n_out, n_in, in_type, copy, ws.w, stream, &b, kernels);
+    int rc = make_operands(ctx, Matrix{x, ldx, rows, n_in, ws.x}, Matrix{w, ldw, n_out, n_in, ws.w}, in_type, copy, stream, &a, &b,
+                           kernels);
     if (rc == EP_OK) rc = run_gemm(ctx, ws.plan, a, false, b, false, e, ws.share, stream, kernels);
     return rc;
 }
@@ -1301,8 +1446,8 @@ int linear_backward_run(ep_ctx *ctx, const BackwardWorkspace &ws, const void *do
         EP_CUDA(ctx, cudaGetLastError());
         ++*kernels;
         if (dbias) {
-            const int rc = ep::sum_partials(ctx, ws.dbias_parts, ws.slabs, n_out, dbias, stream);
-            if (rc != EP_OK) return rc;
+            const int rc_sum = ep::sum_partials(ctx, ws.dbias_parts, ws.slabs, n_out, dbias, stream);
+            if (rc_sum != EP_OK) return rc_sum;
             ++*kernels;
         }
     }
@@ -1314,26 +1459,28 @@ int linear_backward_run(ep_ctx *ctx, const BackwardWorkspace &ws, const void *do
     Epilogue e{};
     e.out_type = in_type;
     e.bias_type = EP_F32;
+    Operand xs{}, wt{};
+    int rc = EP_OK;
+    if (dx || dweight)
+        rc = make_operands(ctx, Matrix{dweight ? x : nullptr, ldx, rows, n_in, ws.x}, Matrix{dx ? w : nullptr, ldw, n_out, n_in, ws.w},
+                           in_type, copy, stream, &xs, &wt, kernels);
+    if (rc != EP_OK) return rc;
     if (dx) {
-        Operand b;
-        int rc = make_operand(ctx, w, ldw, n_out, n_in, in_type, copy, ws.w, stream, &b, kernels);
         e.out = dx;
         e.M = rows;
         e.N = n_in;
         e.vec = n_in % 8 == 0 && ep::aligned(dx, 16);
         e.tma = tma_ready(dx, n_in, in_type);
-        if (rc == EP_OK) rc = run_gemm(ctx, ws.dx, dz, false, b, true, e, ws.share, stream, kernels);
+        rc = run_gemm(ctx, ws.dx, dz, false, wt, true, e, ws.share, stream, kernels);
         if (rc != EP_OK) return rc;
     }
     if (dweight) {
-        Operand b;
-        int rc = make_operand(ctx, x, ldx, rows, n_in, in_type, copy, ws.x, stream, &b, kernels);
         e.out = dweight;
         e.M = n_out;
         e.N = n_in;
         e.vec = n_in % 8 == 0 && ep::aligned(dweight, 16);
         e.tma = tma_ready(dweight, n_in, in_type);
-        if (rc == EP_OK) rc = run_gemm(ctx, ws.dw, dz, true, b, true, e, ws.share, stream, kernels);
+        rc = run_gemm(ctx, ws.dw, dz, true, xs, true, e, ws.share, stream, kernels);
         if (rc != EP_OK) return rc;
     }
     return EP_OK;
