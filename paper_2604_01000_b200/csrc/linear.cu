@@ -59,29 +59,6 @@ __device__ __forceinline__ float gelu_slope(float z) {
     return z >= 0.f ? fmaf(-q, bell, 1.f) : q * bell;
 }
 
-// Two floats that go through one instruction (the fp32 pipe takes pairs): GELU costs half as much issue time so.
-struct Pair {
-    unsigned long long v;
-    __device__ __forceinline__ Pair() {}
-    __device__ __forceinline__ Pair(float lo, float hi) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi)); }
-    __device__ __forceinline__ explicit Pair(float both) : Pair(both, both) {}
-    __device__ __forceinline__ void get(float &lo, float &hi) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-};
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
-    Pair r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
-__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
-    Pair r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ Pair add2(Pair a, Pair b) {
-    Pair r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
 // For z = (z0, z1): the bell exp(-z^2 / 2), |z| and the polynomial above.
 __device__ __forceinline__ void normal_parts(float z0, float z1, Pair &bell, Pair &size, Pair &tail) {
     const Pair z(z0, z1);

@@ -16,7 +16,7 @@ namespace {
 
 constexpr int MAX_PARTS = 4096;
 constexpr int MAX_K = 32;
-constexpr int BLOCKS_PER_SM = 4;   // what their registers let stay resident
+constexpr int BLOCKS_PER_SM = 3;   // what their registers let stay resident
 constexpr int THREADS = 256;
 
 // The better of two (logit, column) pairs: the larger logit, of equal ones the lower column.
@@ -64,6 +64,25 @@ __device__ __forceinline__ void best_of_row(float &v, int &c, float *slot_v, int
     }
 }
 
+// e = exp(l - shift) of a thread's columns, and their sum.
+template <int V, int N>
+__device__ __forceinline__ float exponentials(const float (&l)[V][N], float shift, float (&e)[V][N]) {
+    Pair sum(0.f);
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            float a, b;
+            mul2(add2(Pair(l[j][i], l[j][i + 1]), Pair(-shift)), Pair(1.44269504f)).get(a, b);
+            e[j][i] = exp2_fast(a);
+            e[j][i + 1] = exp2_fast(b);
+            sum = add2(sum, Pair(e[j][i], e[j][i + 1]));
+        }
+    float lo, hi;
+    sum.get(lo, hi);
+    return lo + hi;
+}
+
 struct Finish {   // what the last step needs to turn sums into results
     int parts, k;
     int64_t *counts, *routed;
@@ -98,7 +117,7 @@ template <typename Lay>
 constexpr size_t ring_bytes() { return stages<Lay>() == 1 ? 0 : (size_t)stages<Lay>() * Lay::V * THREADS * 16; }
 
 template <typename T, typename Lay>
-__global__ void __launch_bounds__(THREADS) route_rows(const T *__restrict__ logits, int64_t rows, int parts, int k,
+__global__ void __launch_bounds__(THREADS, 3) route_rows(const T *__restrict__ logits, int64_t rows, int parts, int k,
                                                       const uint8_t *__restrict__ valid, bool renormalize,
                                                       int32_t *__restrict__ ids, float *weights,
                                                       float *__restrict__ part_prob, int *__restrict__ part_count,
@@ -159,21 +178,15 @@ __global__ void __launch_bounds__(THREADS) route_rows(const T *__restrict__ logi
         top = reduce_row<L, OpMaxNumber>(top, slots, turn);
         const bool part = top > -INFINITY;   // false for a row of NaN and -infinity alone, too
         const float shift = part ? top : 0.f;   // (-infinity - 0: the exponentials of a row left out are zero)
-        float s = 0.f;
         float e[V][N];
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                e[j][i] = exp_fast(l[j][i] - shift);
-                s += e[j][i];
-            }
+        float s = exponentials(l, shift, e);
         s = reduce_row<L, OpSum>(s, slots, turn);
         const float inverse = part ? reciprocal_fast(s) : 0.f;
 #pragma unroll
         for (int j = 0; j < V; ++j)
 #pragma unroll
-            for (int i = 0; i < N; ++i) sum_p[j][i] = fmaf(e[j][i], inverse, sum_p[j][i]);
+            for (int i = 0; i < N; i += 2)
+                fma2(Pair(e[j][i], e[j][i + 1]), Pair(inverse), Pair(sum_p[j][i], sum_p[j][i + 1])).get(sum_p[j][i], sum_p[j][i + 1]);
         took_part += part && lane == 0;
 
         // the k largest, one after the other: each thread offers the best of its columns that is left (the first is
@@ -305,7 +318,7 @@ __global__ void __launch_bounds__(1024) route_fold(const float *__restrict__ par
 }
 
 template <typename T, typename Lay>
-__global__ void __launch_bounds__(THREADS) route_rows_backward(const T *__restrict__ logits, int64_t rows, int parts, int k,
+__global__ void __launch_bounds__(THREADS, 3) route_rows_backward(const T *__restrict__ logits, int64_t rows, int parts, int k,
                                                                const uint8_t *__restrict__ valid, bool renormalize,
                                                                const int32_t *__restrict__ ids,
                                                                const int64_t *__restrict__ counts,
@@ -346,15 +359,17 @@ __global__ void __launch_bounds__(THREADS) route_rows_backward(const T *__restri
         top = reduce_row<L, OpMaxNumber>(top, slots, turn);
         const bool part = top > -INFINITY;
         const float shift = part ? top : 0.f;
-        float s = 0.f, dot = 0.f;
+        float s = exponentials(p, shift, p), dot;
+        {
+            Pair both(0.f);
 #pragma unroll
-        for (int j = 0; j < V; ++j)
+            for (int j = 0; j < V; ++j)
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                p[j][i] = exp_fast(p[j][i] - shift);
-                s += p[j][i];
-                dot = fmaf(p[j][i], slope[j][i], dot);
-            }
+                for (int i = 0; i < N; i += 2) both = fma2(Pair(p[j][i], p[j][i + 1]), Pair(slope[j][i], slope[j][i + 1]), both);
+            float odd;
+            both.get(dot, odd);
+            dot += odd;
+        }
         s = reduce_row<L, OpSum>(s, slots, turn);
         dot = reduce_row<L, OpSum>(dot, slots, turn);
         const float inverse = part ? reciprocal_fast(s) : 0.f;
@@ -387,7 +402,9 @@ __global__ void __launch_bounds__(THREADS) route_rows_backward(const T *__restri
 #pragma unroll
         for (int j = 0; j < V; ++j)
 #pragma unroll
-            for (int i = 0; i < N; ++i) p[j][i] *= inverse * (slope[j][i] - back);
+            for (int i = 0; i < N; i += 2)
+                mul2(mul2(Pair(p[j][i], p[j][i + 1]), Pair(inverse)), add2(Pair(slope[j][i], slope[j][i + 1]), Pair(-back)))
+                    .get(p[j][i], p[j][i + 1]);
         T *to = dlogits + row * parts;
         if (mine) Lay::store(to, lane, parts, p);
         if (!dweights) continue;
