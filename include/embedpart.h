@@ -460,7 +460,7 @@ int ep_linear_backward(ep_ctx *ctx, const void *dout, int32_t dout_type, const v
  *
  *   logits  [dev] rows x parts of `type` (EP_F32 / EP_BF16 / EP_F16);  1 <= parts <= 4096
  *   k       1 <= k <= min(parts, 32)
- *   valid   [dev] rows bytes or NULL: 0 = the row takes no part (it is not read)
+ *   valid   [dev] rows bytes or NULL: 0 = the row takes no part (whatever its logits hold)
  *   ids     [dev] out, rows x k int32;  weights [dev] out, rows x k fp32
  *   counts  [dev] out, parts int64;  prob [dev] out, parts fp32;  loss [dev] out, 1 fp32
  *   routed  [dev] out, 1 int64

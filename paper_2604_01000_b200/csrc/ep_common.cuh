@@ -168,6 +168,24 @@ int migrate_run(ep_ctx *ctx, const void *rowptr, bool rowptr64, int64_t N, int K
                 cudaStream_t stream);
 const long long *balance_state_ptr(int64_t N, int K, int64_t max_degree, void *workspace);
 
+// Launches a kernel that may start while the launch before it on the stream still runs.  The kernel calls
+// ep_wait_for_launch_before() before it touches memory; the one before may call ep_let_next_launch_start() as soon as its
+// own blocks are all running.  What overlaps is the start of the one with the end of the other (2 to 3 us a launch).
+template <typename... P, typename... A>
+cudaError_t launch_early(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, A... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 // ---- the partition head's operators (norm.cu, route.cu, linear.cu) ---------------------------------
 inline int type_size(int type) { return type == EP_F32 ? 4 : type == EP_BF16 || type == EP_F16 ? 2 : type == EP_E4M3 ? 1 : 0; }
 inline bool float_type(int type) { return type == EP_F32 || type == EP_BF16 || type == EP_F16; }
@@ -178,6 +196,10 @@ int sum_partials(ep_ctx *ctx, const float *parts, int n, int cols, float *out, c
 
 // ---- device helpers -------------------------------------------------------------------------------
 __device__ __forceinline__ void ep_raise(int *status, int code) { atomicMax(status, code); }
+
+// See ep::launch_early.  The wait returns when every launch before this one has ended and its memory is visible.
+__device__ __forceinline__ void ep_wait_for_launch_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void ep_let_next_launch_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // The bounds-checked build (-DEP_DEBUG: `EP_DEBUG=1 python -m paper_2604_01000_b200.build`, library
 // libembedpart_debug.so): an index the kernels compute themselves (a scatter destination, a slot of a list, a row

@@ -476,6 +476,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
     __syncthreads();
     if constexpr (PAIR) cluster_meet();   // the other block's barriers are ready
     tc_fence_after();
+    ep_wait_for_launch_before();          // (everything up to here needs no memory of the launch before)
+    ep_let_next_launch_start();
     const uint32_t tmem_base = sh->tmem_base;
 
     if (warp == TMA_WARP) {
@@ -802,6 +804,7 @@ __global__ void __launch_bounds__(256) linear_join(const float *__restrict__ sha
     const int s0 = threadIdx.x >> 5;
     const int64_t row = i / chunks;
     const int col = (int)(i - row * chunks) * 8;
+    ep_wait_for_launch_before();
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (i < total) {
         const float *from = shares + ((int64_t)s0 * e.M + row) * e.ld_share + col;
@@ -903,6 +906,7 @@ __global__ void __launch_bounds__(256) pack_rows(const PackJob first, const Pack
     const PackJob &j = blockIdx.y ? second : first;
     const T *from = static_cast<const T *>(j.from);
     O *to = static_cast<O *>(j.to);
+    ep_let_next_launch_start();
     const int chunks = j.ld_to / 8;
     const int64_t total = j.rows * chunks;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
@@ -948,6 +952,7 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz(const D *__restrict__ do
     const int cx = threadIdx.x % DZ_CHUNKS, r0 = threadIdx.x / DZ_CHUNKS;
     const int col = (blockIdx.x * DZ_CHUNKS + cx) * 8;
     const int64_t begin = (int64_t)blockIdx.y * slab, end = min(rows, begin + slab);
+    ep_let_next_launch_start();
     float sum[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.f;
@@ -1172,11 +1177,14 @@ int launch_tiles(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &
     cfg.blockDim = dim3(GEMM_THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr{};
-    attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim = {2, 1, 1};
-    cfg.attrs = &attr;
-    cfg.numAttrs = PAIR ? 1 : 0;
+    cudaLaunchAttribute attrs[2] = {};
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = 2;
+    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+    cfg.attrs = attrs;
+    cfg.numAttrs = PAIR ? 2 : 1;
+    attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attrs[0].val.programmaticStreamSerializationAllowed = 1;
     EP_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, m.a, m.b, m.out, m.z, p.shape, e, ctx->d_status));
     return EP_OK;
 }
@@ -1228,12 +1236,11 @@ int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand
         // (a split sum has at most as many tiles as there are SMs: the grid is far below its limit)
         const unsigned grid = (unsigned)ep::ceil_div(e.M * ((e.N + 7) / 8), join_chunks());
         if (e.out_type == EP_BF16)
-            linear_join<__nv_bfloat16><<<grid, 256, 0, stream>>>(share, p.splits, e);
+            EP_CUDA(ctx, ep::launch_early(linear_join<__nv_bfloat16>, dim3(grid), dim3(256), 0, stream, (const float *)share, p.splits, e));
         else if (e.out_type == EP_F16)
-            linear_join<__half><<<grid, 256, 0, stream>>>(share, p.splits, e);
+            EP_CUDA(ctx, ep::launch_early(linear_join<__half>, dim3(grid), dim3(256), 0, stream, (const float *)share, p.splits, e));
         else
-            linear_join<float><<<grid, 256, 0, stream>>>(share, p.splits, e);
-        EP_CUDA(ctx, cudaGetLastError());
+            EP_CUDA(ctx, ep::launch_early(linear_join<float>, dim3(grid), dim3(256), 0, stream, (const float *)share, p.splits, e));
         ++*kernels;
     }
     return EP_OK;

@@ -132,6 +132,7 @@ __global__ void __launch_bounds__(block_threads<Lay::L>()) norm_rows_backward(co
     __shared__ float slots[L > 32 ? 64 : 1];
     extern __shared__ uint4 ring[];                        // [S][3][V][THREADS]
     float *fold = reinterpret_cast<float *>(ring);         // then [GROUPS][V * L * N] where GROUPS > 1
+    ep_let_next_launch_start();
     int turn = 0;
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
     const float per_column = 1.f / (float)d;
@@ -258,6 +259,7 @@ __global__ void __launch_bounds__(1024) fold_partials(const float *__restrict__ 
     __shared__ double s[32][33];
     const int lane = threadIdx.x & 31, r0 = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;
+    ep_wait_for_launch_before();
     double t = 0.0;
     if (c < cols)
 #pragma unroll 8
@@ -347,7 +349,7 @@ struct BackLaunch {
         constexpr size_t smem = std::max(fold, ring_bytes<T, D, Lay>());
         const int grid = grid_for<Lay::L>(a.ctx, a.rows, BACKWARD_BLOCKS_PER_SM);
         float *part = !a.dweight ? nullptr : grid == 1 ? a.dweight : a.parts;
-        if (smem > 48 * 1024)
+        if (smem > 40 * 1024)   // (static shared memory counts too)
             EP_CUDA(a.ctx, cudaFuncSetAttribute(norm_rows_backward<T, D, Lay>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
         norm_rows_backward<T, D, Lay><<<grid, threads, smem, a.stream>>>((const D *)a.dout, (const T *)a.hidden, a.weight,
                                                                          a.weight_type, (const T *)a.dhidden, a.rows, a.d, a.eps,
@@ -372,8 +374,7 @@ int launch_backward(BackArgs &a) {
 namespace ep {
 
 int sum_partials(ep_ctx *ctx, const float *parts, int n, int cols, float *out, cudaStream_t stream) {
-    fold_partials<<<(unsigned)ceil_div(cols, 32), 1024, 0, stream>>>(parts, n, cols, out);
-    EP_CUDA(ctx, cudaGetLastError());
+    EP_CUDA(ctx, launch_early(fold_partials, dim3((unsigned)ceil_div(cols, 32)), dim3(1024), 0, stream, parts, n, cols, out));
     return EP_OK;
 }
 

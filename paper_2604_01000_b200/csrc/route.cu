@@ -110,29 +110,24 @@ __device__ void finish_block(const Finish &f, int64_t rows_routed, double *red) 
     }
 }
 
-// Rows in flight per thread (see the ring in rows.cuh); 1: read straight into registers.
-template <typename Lay>
-constexpr int stages() { return !Lay::VEC ? 1 : 3; }
-template <typename Lay>
-constexpr size_t ring_bytes() { return stages<Lay>() == 1 ? 0 : (size_t)stages<Lay>() * Lay::V * THREADS * 16; }
-
 template <typename T, typename Lay>
 __global__ void __launch_bounds__(THREADS, 3) route_rows(const T *__restrict__ logits, int64_t rows, int parts, int k,
                                                       const uint8_t *__restrict__ valid, bool renormalize,
                                                       int32_t *__restrict__ ids, float *weights,
                                                       float *__restrict__ part_prob, int *__restrict__ part_count,
-                                                      unsigned *ticket, Finish fin, int hist_at) {
+                                                      unsigned *ticket, Finish fin, int hist_at, bool spans) {
     constexpr int L = Lay::L, V = Lay::V, N = Lay::N, WIDE = Lay::WIDE;
     constexpr int GROUPS = THREADS / L;
     __shared__ float slots[L > 32 ? 64 : 1];
     __shared__ float slot_v[L > 32 ? 16 : 1];
     __shared__ int slot_c[L > 32 ? 16 : 1];
     __shared__ double red[8];
-    extern __shared__ uint4 ring[];   // [S][V][THREADS] chunks on their way, later the fold of the sums; then counts
+    extern __shared__ uint4 ring[];   // rows on their way, later the fold of the sums; then counts
     int *hist = reinterpret_cast<int *>(reinterpret_cast<char *>(ring) + hist_at);   // of [parts + 1] (the last: rows that take part)
     int turn = 0, turn_best = 0;
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
-    if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;   // of route_fold, which runs after this kernel
+    ep_let_next_launch_start();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;   // of route_fold, which goes on after this kernel
     for (int e = threadIdx.x; e <= parts; e += THREADS) hist[e] = 0;
     __syncthreads();
     float sum_p[V][N];
@@ -141,35 +136,15 @@ __global__ void __launch_bounds__(THREADS, 3) route_rows(const T *__restrict__ l
 #pragma unroll
         for (int i = 0; i < N; ++i) sum_p[j][i] = 0.f;
     int took_part = 0;
-    constexpr int S = stages<Lay>();
     const int64_t step = (int64_t)gridDim.x * GROUPS;
-    auto fetch = [&](int64_t row, int s) {
-        if (row < rows && (!valid || valid[row]))
-            copy_row<Lay>(ring + (size_t)s * V * THREADS + threadIdx.x, THREADS, logits + row * parts, lane, parts);
-        copies_end_group();
-    };
-    int64_t ahead = (int64_t)blockIdx.x * GROUPS + group;
-    int stage = 0;
-    if constexpr (S > 1) {
-#pragma unroll
-        for (int s = 0; s < S - 1; ++s, ahead += step) fetch(ahead, s);
-    }
+    RowStream<T, Lay, THREADS> stream(reinterpret_cast<char *>(ring), logits, rows, parts, lane, group, spans);
+    stream.begin((int64_t)blockIdx.x * GROUPS, step);
 
-    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += step, ahead += step) {
+    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += step) {
         const int64_t row = first + group;
         const bool mine = row < rows;
-        const bool read = mine && (!valid || valid[row]);
         float l[V][N];
-        if constexpr (S > 1) {
-            fetch(ahead, stage == 0 ? S - 1 : stage - 1);   // into the slots of the row before
-            copies_wait<S - 1>();
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                copied_chunk<Lay, T>(ring + (size_t)stage * V * THREADS + threadIdx.x, THREADS, read, lane, j, parts, -INFINITY, l[j]);
-            stage = stage + 1 == S ? 0 : stage + 1;
-        } else {
-            Lay::load_if(read, logits + row * parts, lane, parts, -INFINITY, l);
-        }
+        stream.next(first, step, mine && (!valid || valid[row]), -INFINITY, l);
         float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < V; ++j)
@@ -240,7 +215,7 @@ __global__ void __launch_bounds__(THREADS, 3) route_rows(const T *__restrict__ l
     }
 
     // the block's sums: over its groups in order, then to the workspace or, alone, to the results
-    if constexpr (S > 1) copies_wait<0>();
+    stream.end();
     if (took_part) atomicAdd(&hist[parts], took_part);
     __syncthreads();
     float *fold = reinterpret_cast<float *>(ring);   // (every thread is past its last copy)
@@ -283,6 +258,7 @@ __global__ void __launch_bounds__(1024) route_fold(const float *__restrict__ par
     __shared__ long long sc[32][33];
     __shared__ bool last;
     const int lane = threadIdx.x & 31, r0 = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    ep_wait_for_launch_before();
     double p = 0.0;
     long long m = 0;
 #pragma unroll 8
@@ -325,7 +301,7 @@ __global__ void __launch_bounds__(THREADS, 3) route_rows_backward(const T *__res
                                                                const int64_t *__restrict__ routed,
                                                                const float *__restrict__ dweights,
                                                                const float *__restrict__ dloss, T *__restrict__ dlogits,
-                                                               int *status) {
+                                                               int *status, bool spans) {
     constexpr int L = Lay::L, V = Lay::V, N = Lay::N;
     constexpr int GROUPS = THREADS / L;
     __shared__ float slots[L > 32 ? 64 : 1];
@@ -344,13 +320,32 @@ __global__ void __launch_bounds__(THREADS, 3) route_rows_backward(const T *__res
             const int c = Lay::col(lane, j, i);
             slope[j][i] = dloss && c < parts ? unit * (float)counts[c] : 0.f;
         }
-    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += (int64_t)gridDim.x * GROUPS) {
+    extern __shared__ uint4 ring[];
+    const int64_t step = (int64_t)gridDim.x * GROUPS;
+    RowStream<T, Lay, THREADS> stream(reinterpret_cast<char *>(ring), logits, rows, parts, lane, group, spans);
+    stream.begin((int64_t)blockIdx.x * GROUPS, step);
+    // what the next row needs besides its logits, a step ahead: whether it takes part, and this thread's first slot
+    struct Ahead {
+        bool read;
+        int id;
+        float dw;
+    };
+    auto look = [&](int64_t row) {
+        Ahead a{row < rows && (!valid || valid[row]), -1, 0.f};
+        if (dweights && row < rows && lane < k) {
+            a.id = ids[row * k + lane];
+            a.dw = dweights[row * k + lane];
+        }
+        return a;
+    };
+    Ahead ahead = look((int64_t)blockIdx.x * GROUPS + group);
+    for (int64_t first = (int64_t)blockIdx.x * GROUPS; first < rows; first += step) {
         const int64_t row = first + group;
         const bool mine = row < rows;
-        const bool read = mine && (!valid || valid[row]);
-        const T *from = logits + row * parts;
+        const Ahead now = ahead;
+        ahead = look(row + step);
         float p[V][N];
-        Lay::load_if(read, from, lane, parts, -INFINITY, p);
+        stream.next(first, step, now.read, -INFINITY, p);
         float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < V; ++j)
@@ -375,25 +370,25 @@ __global__ void __launch_bounds__(THREADS, 3) route_rows_backward(const T *__res
         const float inverse = part ? reciprocal_fast(s) : 0.f;
         dot *= inverse;
         // the slots, shared out over the row's threads: sum of p and of dweights p.  A thread keeps its first slot.
-        float chosen = 0.f, pulled = 0.f, first_w = 0.f, first_dw = 0.f;
+        float chosen = 0.f, pulled = 0.f, first_w = 0.f;
         int first_id = -1;
         if (dweights) {
-            if (part)
-                for (int q = lane; q < k; q += L) {
-                    const int id = ids[row * k + q];
-                    if (id < 0 || id >= parts) {
-                        if (id != -1) ep_raise(status, EP_ERR_BAD_INDEX);
-                        continue;
-                    }
-                    const float w = exp_fast(to_f32(from[id]) - top) * inverse, dw = dweights[row * k + q];
-                    chosen += w;
-                    pulled = fmaf(dw, w, pulled);
-                    if (q == lane) {
-                        first_id = id;
-                        first_w = w;
-                        first_dw = dw;
-                    }
+            if constexpr (L <= 32) __syncwarp();   // (wider rows have met at a sum)
+            auto slot = [&](int id, float dw) {
+                if (id < 0 || id >= parts) {
+                    if (id != -1) ep_raise(status, EP_ERR_BAD_INDEX);
+                    return 0.f;
                 }
+                const float w = exp_fast(stream.element(first, id) - top) * inverse;
+                chosen += w;
+                pulled = fmaf(dw, w, pulled);
+                return w;
+            };
+            if (part) {
+                first_w = slot(now.id, now.dw);
+                first_id = now.id < parts ? now.id : -1;
+                for (int q = lane + L; q < k; q += L) slot(ids[row * k + q], dweights[row * k + q]);
+            }
             chosen = reduce_row<L, OpSum>(chosen, slots, turn);
             pulled = reduce_row<L, OpSum>(pulled, slots, turn);
         }
@@ -419,13 +414,18 @@ __global__ void __launch_bounds__(THREADS, 3) route_rows_backward(const T *__res
                 const float own = dloss ? unit * (float)counts[id] : 0.f;
                 to[id] = from_f32<T>(w * (own + (dw - mean) * per - back));
             };
-            if (first_id >= 0) again(first_id, first_w, first_dw);
+            if (first_id >= 0) again(first_id, first_w, now.dw);
             for (int q = lane + L; q < k; q += L) {
                 const int id = ids[row * k + q];
-                if (id >= 0 && id < parts) again(id, exp_fast(to_f32(from[id]) - top) * inverse, dweights[row * k + q]);
+                if (id >= 0 && id < parts) again(id, exp_fast(stream.element(first, id) - top) * inverse, dweights[row * k + q]);
             }
         }
+        if constexpr (L > 32)   // the row's logits are no longer read
+            __syncthreads();
+        else
+            __syncwarp();
     }
+    stream.end();
 }
 
 int grid_for(const ep_ctx *ctx, int64_t rows, int groups) {
@@ -456,19 +456,20 @@ struct RouteLaunch {
     template <typename Lay>
     int run() const {
         constexpr int groups = THREADS / Lay::L;
-        constexpr size_t hist_at = std::max(ring_bytes<Lay>(), groups > 1 ? sizeof(float) * groups * Lay::WIDE : 0);
+        const size_t hist_at = std::max((size_t)RowStream<T, Lay, THREADS>::ring_bytes(a.parts),
+                                        groups > 1 ? sizeof(float) * groups * Lay::WIDE : 0);
         const size_t smem = hist_at + sizeof(int) * (size_t)(a.parts + 1);
         const int grid = grid_for(a.ctx, a.rows, groups);
-        if (smem > 48 * 1024)
+        if (smem > 40 * 1024)   // (static shared memory counts too)
             EP_CUDA(a.ctx, cudaFuncSetAttribute(route_rows<T, Lay>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
         route_rows<T, Lay><<<grid, THREADS, smem, a.stream>>>((const T *)a.logits, a.rows, a.parts, a.k, a.valid,
                                                                        a.renormalize, a.ids, a.weights, a.part_prob, a.part_count,
-                                                                       a.ticket, a.fin, (int)hist_at);
+                                                                       a.ticket, a.fin, (int)hist_at, ep::aligned(a.logits, 16));
         EP_CUDA(a.ctx, cudaGetLastError());
         a.kernels = 1;
         if (grid > 1) {
-            route_fold<<<a.parts / 32 + 1, 1024, 0, a.stream>>>(a.part_prob, a.part_count, grid, a.ticket, a.fin);
-            EP_CUDA(a.ctx, cudaGetLastError());
+            EP_CUDA(a.ctx, ep::launch_early(route_fold, dim3(a.parts / 32 + 1), dim3(1024), 0, a.stream, (const float *)a.part_prob,
+                                            (const int *)a.part_count, grid, a.ticket, a.fin));
             a.kernels = 2;
         }
         return EP_OK;
@@ -495,9 +496,12 @@ struct RouteBackLaunch {
     const RouteBackArgs &a;
     template <typename Lay>
     int run() const {
-        route_rows_backward<T, Lay><<<grid_for(a.ctx, a.rows, THREADS / Lay::L), THREADS, 0, a.stream>>>(
+        const int smem = RowStream<T, Lay, THREADS>::ring_bytes(a.parts);
+        if (smem > 40 * 1024)   // (static shared memory counts too)
+            EP_CUDA(a.ctx, cudaFuncSetAttribute(route_rows_backward<T, Lay>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        route_rows_backward<T, Lay><<<grid_for(a.ctx, a.rows, THREADS / Lay::L), THREADS, smem, a.stream>>>(
             (const T *)a.logits, a.rows, a.parts, a.k, a.valid, a.renormalize, a.ids, a.counts, a.routed, a.dweights, a.dloss,
-            (T *)a.dlogits, a.ctx->d_status);
+            (T *)a.dlogits, a.ctx->d_status, ep::aligned(a.logits, 16));
         EP_CUDA(a.ctx, cudaGetLastError());
         return EP_OK;
     }

@@ -278,6 +278,99 @@ __device__ __forceinline__ void copied_chunk(const uint4 *slots, int threads, bo
     }
 }
 
+// `bytes` (up to 16) of 16, the rest zero.
+__device__ __forceinline__ void copy_async_some(void *to, const void *from, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(bytes)
+                 : "memory");
+}
+
+// One input of a kernel that goes over its rows in steps of a whole grid, THREADS / L rows a block: rows on their way to
+// shared memory S - 1 steps ahead.  VEC layouts as above.  Other layouts of up to 32 threads a row: a warp copies
+// the 16-byte pieces that its rows lie in, whatever their alignment, and its threads pick their elements (the input
+// itself has to start on a 16-byte boundary: `on`).  What is left reads straight into registers.
+template <typename T, typename Lay, int THREADS>
+struct RowStream {
+    static constexpr bool SPAN = !Lay::VEC && Lay::L <= 32;
+    static constexpr int S = Lay::VEC || SPAN ? 3 : 1;
+    static __host__ __device__ constexpr int span_bytes(int width) { return ((32 / Lay::L) * width * (int)sizeof(T) + 30) / 16 * 16; }
+    static __host__ __device__ constexpr int ring_bytes(int width) {
+        return Lay::VEC ? S * Lay::V * THREADS * 16 : SPAN ? S * (THREADS / 32) * span_bytes(width) : 0;
+    }
+    const T *base;
+    int64_t rows;
+    int width, lane, group, stage;
+    bool on;
+    char *mine, *shown;   // VEC: this thread's first slot; otherwise this warp's first span; and that of the row of next()
+
+    __device__ __forceinline__ RowStream(char *ring, const T *input, int64_t n, int w, int lane_, int group_, bool spans)
+        : base(input), rows(n), width(w), lane(lane_), group(group_), stage(0), on(Lay::VEC || (SPAN && spans)) {
+        mine = Lay::VEC ? ring + threadIdx.x * 16 : ring + (threadIdx.x >> 5) * span_bytes(w);
+    }
+    __device__ __forceinline__ char *at(int s) const {
+        return mine + s * (Lay::VEC ? Lay::V * THREADS * 16 : (THREADS / 32) * span_bytes(width));
+    }
+    // Starts the copy of the step whose first row (of the block) is `first` into stage s.
+    __device__ __forceinline__ void fetch(int64_t first, int s) {
+        if constexpr (Lay::VEC) {
+            if (first + group < rows) copy_row<Lay>(reinterpret_cast<uint4 *>(at(s)), THREADS, base + (first + group) * width, lane, width);
+            copies_end_group();
+        } else if constexpr (SPAN) {
+            if (!on) return;
+            const int64_t row = first + (group & ~(32 / Lay::L - 1));
+            if (row < rows) {
+                const int64_t start = row * width * (int64_t)sizeof(T), from = start & ~int64_t(15);
+                const int length = (int)min(rows - row, (int64_t)(32 / Lay::L)) * width * (int)sizeof(T) + (int)(start - from);
+                const bool last = rows - row <= 32 / Lay::L;   // the last piece must not reach past the input
+                const char *src = reinterpret_cast<const char *>(base) + from;
+                char *dst = at(s);
+                for (int p = (threadIdx.x & 31) * 16; p < length; p += 512)
+                    copy_async_some(dst + p, src + p, last ? min(length - p, 16) : 16);
+            }
+            copies_end_group();
+        }
+    }
+    __device__ __forceinline__ void begin(int64_t first, int64_t step) {
+#pragma unroll
+        for (int s = 0; s < S - 1; ++s) fetch(first + s * step, s);
+    }
+    // The row of this step: there = it is to be read.  Called by all threads of a warp.
+    __device__ __forceinline__ void next(int64_t first, int64_t step, bool there, float fill, float (&v)[Lay::V][Lay::N]) {
+        const int64_t row = first + group;
+        if (on) {
+            if constexpr (SPAN) __syncwarp();   // every lane has read what the next copy overwrites
+            fetch(first + (S - 1) * step, stage == 0 ? S - 1 : stage - 1);
+            copies_wait<S - 1>();
+            if constexpr (Lay::VEC) {
+#pragma unroll
+                for (int j = 0; j < Lay::V; ++j)
+                    copied_chunk<Lay, T>(reinterpret_cast<const uint4 *>(at(stage)), THREADS, there, lane, j, width, fill, v[j]);
+            } else {
+                __syncwarp();
+                const int64_t first_row = first + (group & ~(32 / Lay::L - 1));
+                const int shift = (int)(first_row * width * (int64_t)sizeof(T) & 15);
+                Lay::load_if(there, reinterpret_cast<const T *>(at(stage) + shift) + (int)(row - first_row) * width, lane, width, fill, v);
+            }
+            shown = at(stage);
+            stage = stage + 1 == S ? 0 : stage + 1;
+        } else {
+            Lay::load_if(there, base + row * width, lane, width, fill, v);
+        }
+    }
+    // Element c of the row that next() has delivered (after the threads of the row have met).
+    __device__ __forceinline__ float element(int64_t first, int c) const {
+        if (!on) return to_f32(base[(first + group) * width + c]);
+        if constexpr (Lay::VEC) {
+            const int q = c / Lay::N;
+            return to_f32(reinterpret_cast<const T *>(shown + ((q / Lay::L) * THREADS + q % Lay::L - lane) * 16)[c % Lay::N]);
+        } else {
+            const int64_t first_row = first + (group & ~(32 / Lay::L - 1));
+            const int shift = (int)(first_row * width * (int64_t)sizeof(T) & 15);
+            return to_f32(reinterpret_cast<const T *>(shown + shift)[(int)(first + group - first_row) * width + c]);
+        }
+    }
+    __device__ __forceinline__ void end() const { copies_wait<0>(); }
+};
+
 // Calls f.run<Layout>() with the layout for rows of `width` elements of T.  About 16 columns per thread: fewer steps of
 // the sums across threads than with one chunk each, and as many loads in flight.
 template <typename T, typename F>
