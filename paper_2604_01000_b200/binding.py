@@ -2,6 +2,8 @@
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import os
 import threading
 from typing import NamedTuple, Optional
@@ -39,10 +41,6 @@ TIMER_COUNT = 12
 TIMERS = {"kmeans_assign": 0, "kmeans_update": 1, "edge_cut": 2, "quality_prep": 3, "reorder": 4,
           "kmeans_resolve": 5, "graph_bandwidth": 6, "relabel": 7, "balance": 8, "norm": 9, "linear": 10, "route": 11}
 KMEANS_PATHS = {"auto": 0, "simt": 1, "tensor": 2}
-# element types and activations of the partition head's operators
-TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3}
-FLOATS = (torch.float32, torch.bfloat16, torch.float16)
-ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 
 class EmbedPartError(RuntimeError):
@@ -189,6 +187,35 @@ def load_library() -> ctypes.CDLL:
     return _lib
 
 
+_head = None
+_HEAD_CALLS = ("ep_rms_norm", "ep_quantize_rows", "ep_rms_norm_backward_workspace_bytes", "ep_rms_norm_backward",
+               "ep_linear_workspace_bytes", "ep_linear", "ep_linear_backward_workspace_bytes", "ep_linear_backward",
+               "ep_route_workspace_bytes", "ep_route", "ep_route_backward")
+
+
+def _raise_status(ctx: int, status: int, what: str = ""):
+    lib = load_library()
+    msg, detail = lib.ep_status_string(status).decode(), what or lib.ep_last_error(ctx).decode()
+    raise EmbedPartError(status, f"{msg}: {detail}" if detail else msg)
+
+
+def _load_head():
+    """The compiled marshalling of the partition head's operators (_head.so), bound to the loaded library."""
+    global _head
+    lib = load_library()
+    with _lib_lock:
+        if _head is None:
+            path = os.path.join(_PKG, "_head.so")
+            if not os.path.exists(path):
+                raise FileNotFoundError(f"{path} is missing: build it with `python -m paper_2604_01000_b200.build`")
+            loader = importlib.machinery.ExtensionFileLoader("_head", path)
+            module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_head", loader))
+            loader.exec_module(module)
+            module.bind({n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in _HEAD_CALLS}, _raise_status)
+            _head = module
+    return _head
+
+
 def _dev_ptr(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
@@ -201,36 +228,6 @@ def _check_cuda(t: torch.Tensor, dtype, name: str, device: torch.device) -> torc
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t
-
-
-def _check_matrix(t: torch.Tensor, dtypes, name: str, device: torch.device, shape=None, strided: bool = False) -> torch.Tensor:
-    """A 2-D CUDA tensor of one of `dtypes`, contiguous or (strided) with contiguous rows at any distance."""
-    if not isinstance(t, torch.Tensor) or t.get_device() != device.index:
-        raise ValueError(f"{name} must be a CUDA tensor on {device}")
-    if t.dtype not in dtypes:
-        raise ValueError(f"{name} must have dtype {' or '.join(str(d) for d in dtypes)}, not {t.dtype}")
-    if t.dim() != 2 or (shape is not None and t.shape != shape):
-        raise ValueError(f"{name} must have shape {tuple(shape) if shape is not None else '(rows, columns)'}, not {tuple(t.shape)}")
-    if not t.is_contiguous():
-        if not strided:
-            raise ValueError(f"{name} must be contiguous")
-        if t.numel() and (t.stride(1) != 1 and t.shape[1] > 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-            raise ValueError(f"{name} must have contiguous rows that do not overlap")
-    return t
-
-
-def _check_vector(t: Optional[torch.Tensor], dtypes, name: str, device: torch.device, n: int) -> Optional[torch.Tensor]:
-    if t is None:
-        return None
-    if not isinstance(t, torch.Tensor) or t.get_device() != device.index:
-        raise ValueError(f"{name} must be a CUDA tensor on {device}")
-    if t.dtype not in dtypes or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name} must be {n} contiguous values of {' or '.join(str(d) for d in dtypes)}")
-    return t
-
-
-def _ptr(t: Optional[torch.Tensor]):
-    return None if t is None else t.data_ptr()
 
 
 def _context_of(t) -> "Context":
@@ -265,12 +262,15 @@ class Context:
         if rc != EP_OK:
             raise EmbedPartError(rc, self._lib.ep_status_string(rc).decode())
         self._h = h
+        self._address = h.value
+        self._head = _load_head()
         self._ws: Optional[torch.Tensor] = None
 
     def close(self):
         if getattr(self, "_h", None):
             self._lib.ep_destroy(self._h)
             self._h = None
+            self._address = 0
 
     def __del__(self):  # pragma: no cover
         try:
@@ -737,171 +737,46 @@ class Context:
             self._raise(rc)
         return out
 
-    # -- the partition head's operators --------------------------------------------------------------
-    def _scratch(self, nbytes: int, what: str) -> torch.Tensor:
-        """A workspace of this call's own, ordered by the current stream (calls on several streams may overlap)."""
-        if nbytes == 0:
-            raise EmbedPartError(1, f"shape or type out of range: {what}")
-        return torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-
-    def _raw_stream(self) -> int:
-        return torch._C._cuda_getCurrentRawStream(self.device.index)
-
-    def _done(self, rc: int):
-        if rc != EP_OK:
-            self._raise(rc)
-
-    def rms_norm(self, x, weight=None, residual=None, eps: float = 1e-6, out_dtype=None):
+    # -- the partition head's operators (checked, allocated and called in _head.so) ------------------
+    # Matrices are contiguous CUDA tensors on this device (x, weight and residual of linear may have strided rows); a
+    # wrong type, shape or device raises ValueError, what the library refuses EmbedPartError.  Each call's workspace is
+    # its own, ordered by the current stream, so calls on several streams may overlap.
+    def rms_norm(self, x, weight=None, residual=None, eps: float = 1e-6, out_dtype=None) -> "NormResult":
         """weight * h / sqrt(mean(h^2) + eps) with h = x + residual; see ep_rms_norm."""
-        x = _check_matrix(x, FLOATS, "x", self.device)
-        rows, d = x.shape
-        weight = _check_vector(weight, FLOATS, "weight", self.device, d)
-        if residual is not None:
-            residual = _check_matrix(residual, (x.dtype,), "residual", self.device, x.shape)
-        out_dtype = x.dtype if out_dtype is None else out_dtype
-        if out_dtype not in (x.dtype, torch.float8_e4m3fn) and not (x.dtype == torch.float32 and out_dtype in FLOATS):
-            raise ValueError(f"no norm from {x.dtype} to {out_dtype}")
-        out = torch.empty(rows, d, dtype=out_dtype, device=self.device)
-        scale = torch.empty(rows, dtype=torch.float32, device=self.device) if out_dtype == torch.float8_e4m3fn else None
-        hidden = torch.empty_like(x) if residual is not None else None
-        self._done(self._lib.ep_rms_norm(self._h, _ptr(x), TYPES[x.dtype], _ptr(residual), _ptr(weight),
-                                         _type_of(weight), rows, d, eps, _ptr(out), TYPES[out_dtype], _ptr(scale),
-                                         _ptr(hidden), self._raw_stream()))
-        return NormResult(out, scale, x if hidden is None else hidden)
+        return NormResult(*self._head.rms_norm(self._address, self.device.index, x, weight, residual, eps, out_dtype))
 
-    def quantize_rows(self, x):
+    def quantize_rows(self, x) -> "QuantizedRows":
         """Rows in 8 bits with a scale each: x ~ q * scale[:, None]; see ep_quantize_rows."""
-        x = _check_matrix(x, FLOATS, "x", self.device)
-        rows, d = x.shape
-        q = torch.empty(rows, d, dtype=torch.float8_e4m3fn, device=self.device)
-        scale = torch.empty(rows, dtype=torch.float32, device=self.device)
-        self._done(self._lib.ep_quantize_rows(self._h, _ptr(x), TYPES[x.dtype], rows, d, _ptr(q), _ptr(scale),
-                                              self._raw_stream()))
-        return QuantizedRows(q, scale)
+        return QuantizedRows(*self._head.quantize_rows(self._address, self.device.index, x))
 
-    def rms_norm_backward(self, dout, hidden, weight=None, eps: float = 1e-6, dhidden=None, need_dweight: bool = True):
+    def rms_norm_backward(self, dout, hidden, weight=None, eps: float = 1e-6, dhidden=None,
+                          need_dweight: bool = True) -> "NormGradients":
         """Gradients of x (and, alike, residual) and weight; hidden is the forward's; see ep_rms_norm_backward."""
-        hidden = _check_matrix(hidden, FLOATS, "hidden", self.device)
-        rows, d = hidden.shape
-        dout = _check_matrix(dout, FLOATS if hidden.dtype == torch.float32 else (hidden.dtype,), "dout", self.device, hidden.shape)
-        weight = _check_vector(weight, FLOATS, "weight", self.device, d)
-        if dhidden is not None:
-            dhidden = _check_matrix(dhidden, (hidden.dtype,), "dhidden", self.device, hidden.shape)
-        ws = self._scratch(self._lib.ep_rms_norm_backward_workspace_bytes(self._h, rows, d), f"rows={rows} d={d}")
-        dx = torch.empty_like(hidden)
-        dweight = torch.empty(d, dtype=torch.float32, device=self.device) if need_dweight else None
-        self._done(self._lib.ep_rms_norm_backward(
-            self._h, _ptr(dout), TYPES[dout.dtype], _ptr(hidden), TYPES[hidden.dtype], _ptr(weight),
-            _type_of(weight), _ptr(dhidden), rows, d, eps, _ptr(dx), _ptr(dweight), _ptr(ws), ws.numel(),
-            self._raw_stream()))
-        return NormGradients(dx, dweight)
+        return NormGradients(*self._head.rms_norm_backward(self._address, self.device.index, dout, hidden, weight, eps, dhidden,
+                                                           need_dweight))
 
     def linear(self, x, weight, bias=None, activation: str = "none", residual=None, x_scale=None, weight_scale=None,
-               out_dtype=None, preact: bool = False):
-        """act(x weight^T + bias) + residual; see ep_linear.  x, weight and residual may have strided rows."""
-        x = _check_matrix(x, tuple(TYPES), "x", self.device, strided=True)
-        rows, n_in = x.shape
-        weight = _check_matrix(weight, (x.dtype,), "weight", self.device, strided=True)
-        n_out = weight.shape[0]
-        if weight.shape[1] != n_in:
-            raise ValueError(f"weight must be n_out x {n_in}, not {tuple(weight.shape)}")
-        if activation not in ACTIVATIONS:
-            raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")
-        eight = x.dtype == torch.float8_e4m3fn
-        out_dtype = (torch.bfloat16 if eight else x.dtype) if out_dtype is None else out_dtype
-        if out_dtype not in FLOATS or not (eight or out_dtype in (x.dtype, torch.float32)):
-            raise ValueError(f"no product of {x.dtype} with output of {out_dtype}")
-        if eight != (x_scale is not None) or eight != (weight_scale is not None):
-            raise ValueError("x_scale and weight_scale go with 8-bit inputs, and with no others")
-        x_scale = _check_vector(x_scale, (torch.float32,), "x_scale", self.device, rows)
-        weight_scale = _check_vector(weight_scale, (torch.float32,), "weight_scale", self.device, n_out)
-        bias = _check_vector(bias, FLOATS, "bias", self.device, n_out)
-        if residual is not None:
-            residual = _check_matrix(residual, (out_dtype,), "residual", self.device, (rows, n_out), strided=True)
-        ws = self._scratch(self._lib.ep_linear_workspace_bytes(self._h, rows, n_in, n_out, TYPES[x.dtype], TYPES[out_dtype],
-                                                               int(_aligned(x, weight))),
-                           f"rows={rows} n_in={n_in} n_out={n_out}")
-        out = torch.empty(rows, n_out, dtype=out_dtype, device=self.device)
-        z = torch.empty_like(out) if preact else None
-        self._done(self._lib.ep_linear(
-            self._h, _ptr(x), _row_stride(x), _ptr(weight), _row_stride(weight), TYPES[x.dtype], _ptr(x_scale),
-            _ptr(weight_scale), _ptr(bias), _type_of(bias), ACTIVATIONS[activation], _ptr(residual),
-            0 if residual is None else _row_stride(residual), _ptr(out), TYPES[out_dtype], _ptr(z), rows, n_in, n_out,
-            _ptr(ws), ws.numel(), self._raw_stream()))
-        return LinearResult(out, z)
+               out_dtype=None, preact: bool = False) -> "LinearResult":
+        """act(x weight^T + bias) + residual; see ep_linear."""
+        return LinearResult(*self._head.linear(self._address, self.device.index, x, weight, bias, activation, residual, x_scale,
+                                               weight_scale, out_dtype, preact))
 
     def linear_backward(self, dout, x, weight, preact=None, activation: str = "none", need_dx: bool = True,
-                        need_dweight: bool = True, need_dbias: bool = True):
+                        need_dweight: bool = True, need_dbias: bool = True) -> "LinearGradients":
         """Gradients of x, weight and bias (the residual's is dout itself); see ep_linear_backward."""
-        x = _check_matrix(x, FLOATS, "x", self.device, strided=True)
-        rows, n_in = x.shape
-        weight = _check_matrix(weight, (x.dtype,), "weight", self.device, strided=True)
-        n_out = weight.shape[0]
-        if weight.shape[1] != n_in:
-            raise ValueError(f"weight must be n_out x {n_in}, not {tuple(weight.shape)}")
-        if activation not in ACTIVATIONS:
-            raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}")
-        dout = _check_matrix(dout, (x.dtype, torch.float32), "dout", self.device, (rows, n_out))
-        if activation != "none":
-            if preact is None:
-                raise ValueError("the gradient through an activation needs preact")
-            preact = _check_matrix(preact, (x.dtype,), "preact", self.device, (rows, n_out))
-        else:
-            preact = None
-        ws = self._scratch(self._lib.ep_linear_backward_workspace_bytes(self._h, rows, n_in, n_out, TYPES[x.dtype],
-                                                                        int(_aligned(x, weight))),
-                           f"rows={rows} n_in={n_in} n_out={n_out}")
-        dx = torch.empty(rows, n_in, dtype=x.dtype, device=self.device) if need_dx else None
-        dweight = torch.empty(n_out, n_in, dtype=x.dtype, device=self.device) if need_dweight else None
-        dbias = torch.empty(n_out, dtype=torch.float32, device=self.device) if need_dbias else None
-        self._done(self._lib.ep_linear_backward(
-            self._h, _ptr(dout), TYPES[dout.dtype], _ptr(preact), ACTIVATIONS[activation], _ptr(x),
-            _row_stride(x), _ptr(weight), _row_stride(weight), TYPES[x.dtype], rows, n_in, n_out, _ptr(dx),
-            _ptr(dweight), _ptr(dbias), _ptr(ws), ws.numel(), self._raw_stream()))
-        return LinearGradients(dx, dweight, dbias)
+        return LinearGradients(*self._head.linear_backward(self._address, self.device.index, dout, x, weight, preact, activation,
+                                                           need_dx, need_dweight, need_dbias))
 
-    def route(self, logits, k: int = 1, valid=None, renormalize: bool = False):
+    def route(self, logits, k: int = 1, valid=None, renormalize: bool = False) -> "RouteResult":
         """Rows to their k best parts, with weights, per-part counts and the balance loss; see ep_route."""
-        logits = _check_matrix(logits, FLOATS, "logits", self.device)
-        rows, parts = logits.shape
-        if not 1 <= k <= min(parts, 32):
-            raise ValueError(f"k must be in 1..{min(parts, 32)}, not {k}")
-        valid = _check_vector(valid, (torch.uint8, torch.bool), "valid", self.device, rows)
-        ws = self._scratch(self._lib.ep_route_workspace_bytes(self._h, rows, parts), f"rows={rows} parts={parts}")
-        ids = torch.empty(rows, k, dtype=torch.int32, device=self.device)
-        weights = torch.empty(rows, k, dtype=torch.float32, device=self.device)
-        counts = torch.empty(parts, dtype=torch.int64, device=self.device)
-        prob = torch.empty(parts, dtype=torch.float32, device=self.device)
-        loss = torch.empty(1, dtype=torch.float32, device=self.device)
-        routed = torch.empty(1, dtype=torch.int64, device=self.device)
-        self._done(self._lib.ep_route(
-            self._h, _ptr(logits), TYPES[logits.dtype], rows, parts, k, _ptr(valid), int(renormalize), _ptr(ids),
-            _ptr(weights), _ptr(counts), _ptr(prob), _ptr(loss), _ptr(routed), _ptr(ws), ws.numel(),
-            self._raw_stream()))
-        return RouteResult(ids, weights, counts, prob, loss, routed)
+        return RouteResult(*self._head.route(self._address, self.device.index, logits, k, valid, renormalize))
 
-    def route_backward(self, logits, result: "RouteResult", dweights=None, dloss=None, valid=None, renormalize: bool = False):
+    def route_backward(self, logits, result: "RouteResult", dweights=None, dloss=None, valid=None,
+                       renormalize: bool = False) -> torch.Tensor:
         """Gradient of logits from those of the weights and of the loss; logits, valid and renormalize as the forward took
         them, result what it returned; see ep_route_backward."""
-        logits = _check_matrix(logits, FLOATS, "logits", self.device)
-        rows, parts = logits.shape
-        ids = _check_matrix(result.ids, (torch.int32,), "result.ids", self.device)
-        k = ids.shape[1]
-        if ids.shape[0] != rows or not 1 <= k <= min(parts, 32):
-            raise ValueError(f"result.ids must be {rows} x k with k in 1..{min(parts, 32)}, not {tuple(ids.shape)}")
-        counts = _check_vector(result.counts, (torch.int64,), "result.counts", self.device, parts)
-        routed = _check_vector(result.routed, (torch.int64,), "result.routed", self.device, 1)
-        if counts is None or routed is None:
-            raise ValueError("result must hold the forward's counts and routed")
-        if dweights is not None:
-            dweights = _check_matrix(dweights, (torch.float32,), "dweights", self.device, (rows, k))
-        dloss = _check_vector(dloss, (torch.float32,), "dloss", self.device, 1)
-        valid = _check_vector(valid, (torch.uint8, torch.bool), "valid", self.device, rows)
-        dlogits = torch.empty_like(logits)
-        self._done(self._lib.ep_route_backward(
-            self._h, _ptr(logits), TYPES[logits.dtype], rows, parts, k, _ptr(valid), int(renormalize), _ptr(ids),
-            _ptr(counts), _ptr(routed), _ptr(dweights), _ptr(dloss), _ptr(dlogits), self._raw_stream()))
-        return dlogits
+        return self._head.route_backward(self._address, self.device.index, logits, result.ids, result.counts, result.routed,
+                                         dweights, dloss, valid, renormalize)
 
 
 class KMeansResult(NamedTuple):

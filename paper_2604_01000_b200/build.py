@@ -1,4 +1,4 @@
-"""Builds libembedpart.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Builds libembedpart.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _head.so beside it."""
 from __future__ import annotations
 
 import os
@@ -18,6 +18,26 @@ NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "--expt-relaxed-constexpr", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
 ]
+
+
+HEAD = os.path.join(PKG, "_head.so")                      # tensor marshalling of the partition head's operators
+
+
+def head_commands():
+    """(compile, link) of _head.so: host code against torch's own headers and libraries."""
+    import sysconfig
+    import torch
+    base = os.path.dirname(torch.__file__)
+    lib = os.path.join(base, "lib")
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    obj = os.path.join(OBJ, "head_binding.o")
+    inc = [x for d in [os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"), os.path.join(cuda, "include"), sysconfig.get_paths()["include"],
+                       os.path.join(ROOT, "include")] for x in ("-isystem", d)]
+    cxx = os.environ.get("CXX", "g++")
+    return ([cxx, "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+             *inc, "-c", os.path.join(CSRC, "head_binding.cpp"), "-o", obj],
+            [cxx, "-shared", obj, "-L", lib, "-Wl,-rpath," + lib, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch",
+             "-ltorch_python", "-o"])
 
 
 def sources():
@@ -50,10 +70,15 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
                 cmd.insert(1, "-Xptxas=-v")
             jobs.append(cmd)
 
+    head_src = os.path.join(CSRC, "head_binding.cpp")
+    head_new = not debug and (force or not os.path.exists(HEAD) or os.path.getmtime(HEAD) < max(os.path.getmtime(head_src), hdr))
+    if head_new:
+        jobs.append(head_commands()[0])
+
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)
         if r.returncode != 0:
-            raise RuntimeError("nvcc failed: %s\n%s\n%s" % (" ".join(cmd), r.stdout, r.stderr))
+            raise RuntimeError("compiler failed: %s\n%s\n%s" % (" ".join(cmd), r.stdout, r.stderr))
         return r.stderr
 
     with ThreadPoolExecutor(max_workers=max(1, min(8, len(jobs)))) as ex:
@@ -65,6 +90,10 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
         run([nvcc, "-shared", "-gencode", "arch=compute_100a,code=sm_100a", "-o", tmp, *objs, "-lcudart_static",
              "-ldl", "-lrt", "-lpthread"])
         os.replace(tmp, LIB)
+    if head_new:
+        tmp = HEAD + ".tmp.%d" % os.getpid()
+        run([*head_commands()[1], tmp])
+        os.replace(tmp, HEAD)
     return LIB
 
 
