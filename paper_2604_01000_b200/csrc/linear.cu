@@ -831,30 +831,33 @@ __global__ void __launch_bounds__(256) linear_join(const float *__restrict__ sha
 }
 
 // ---------------------------------------------------------------------------------------------- few rows
-// A warp computes one column of ROWS rows: its lanes share out the row of W in 16-byte chunks, which are read once; x
-// comes from the L1.  Sums are fp32 multiply-adds to nearest, so all types are exact to fp32 here.
-template <typename T, int ROWS>
+// Dot products: `share` warps of a block (1, 2, 4 or 8 of its 8) to one column of ROWS rows.  Their lanes share out the row
+// of W, in 16-byte chunks (VEC) or, where it is not aligned for that, element by element next to one another; W is read
+// once, x comes from the L1.  Sums are fp32 multiply-adds to nearest, so all types are exact to fp32 here.
+template <typename T, int ROWS, bool VEC>
 __global__ void __launch_bounds__(256) linear_few_rows(const T *__restrict__ x, int64_t ldx, const T *__restrict__ w, int64_t ldw,
-                                                       int n_in, const Epilogue e, bool vec) {
-    constexpr int N = 16 / (int)sizeof(T);
-    const int lane = threadIdx.x & 31;
-    const int col = (int)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (col >= e.N) return;
+                                                       int n_in, const Epilogue e, int share) {
+    constexpr int N = VEC ? 16 / (int)sizeof(T) : 1;
+    __shared__ float part[8][ROWS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int col = (int)blockIdx.x * (8 / share) + warp / share, mine = warp % share;
     float sum[ROWS];
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) sum[r] = 0.f;
-    const T *wr = w + col * ldw;
+    if (col < e.N) {
+        const T *wr = w + col * ldw;
 #pragma unroll 4
-    for (int c = lane * N; c < n_in; c += 32 * N) {
-        float a[N];
-        load_chunk(wr, c, n_in, vec, 0.f, a);
+        for (int c = (mine * 32 + lane) * N; c < n_in; c += share * 32 * N) {
+            float a[N];
+            load_chunk(wr, c, n_in, VEC, 0.f, a);
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r) {
-            if (r < e.M) {
-                float b[N];
-                load_chunk(x + r * ldx, c, n_in, vec, 0.f, b);
+            for (int r = 0; r < ROWS; ++r) {
+                if (r < e.M) {
+                    float b[N];
+                    load_chunk(x + r * ldx, c, n_in, VEC, 0.f, b);
 #pragma unroll
-                for (int i = 0; i < N; ++i) sum[r] = fmaf(a[i], b[i], sum[r]);
+                    for (int i = 0; i < N; ++i) sum[r] = fmaf(a[i], b[i], sum[r]);
+                }
             }
         }
     }
@@ -865,7 +868,13 @@ __global__ void __launch_bounds__(256) linear_few_rows(const T *__restrict__ x, 
         for (int o = 16; o >= 1; o >>= 1) sum[r] += __shfl_xor_sync(FULL, sum[r], o);
         if (lane == r) v[0] = sum[r];
     }
-    if (lane < ROWS && lane < e.M) {
+    if (share > 1) {
+        if (lane < ROWS) part[warp][lane] = v[0];
+        __syncthreads();
+        if (mine == 0 && lane < ROWS)
+            for (int s = 1; s < share; ++s) v[0] += part[warp + s][lane];
+    }
+    if (col < e.N && mine == 0 && lane < ROWS && lane < e.M) {
         Columns<1> c;
         c.load(e, col);
         float add[1];
@@ -1040,7 +1049,14 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz(const D *__restrict__ do
 
 // ---------------------------------------------------------------------------------------------- host side
 constexpr int MAX_WIDTH = 65536;
+// Whether the dot products serve rows x n_in -> n_out, and not the tiles.  They go by the CUDA cores, about 4 products a
+// picosecond: up to 2^24 products they are the faster ones (1024 x 1024 bf16: 8 rows in 4.8 us against 6.0; 4096 x 4096:
+// 1 row 6.9 against 10.0, 2 rows 12.3 against 10.0).  fp32 operands would first have to be split (4096 x 4096: 8 rows
+// 40 us against 65), so there they serve every call of up to 8 rows.
 constexpr int FEW_ROWS = 8;
+bool few_rows(int64_t rows, int n_in, int n_out, int type) {
+    return rows <= FEW_ROWS && (type == EP_F32 || rows * n_in * n_out <= (1ll << 24));
+}
 constexpr int PACK_BLOCKS_PER_SM = 8;
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -1317,7 +1333,7 @@ LinearWorkspace linear_workspace(const ep_ctx *ctx, int64_t rows, int n_in, int 
                                  void *base) {
     ep::Arena a(base);
     LinearWorkspace w{};
-    if (rows > FEW_ROWS) {
+    if (!few_rows(rows, n_in, n_out, in_type)) {
         const bool copy = in_type == EP_F32 || !aligned;
         if (copy) {
             w.x = a.take<char>(packed_form(rows, n_in, in_type).bytes);
@@ -1361,21 +1377,28 @@ BackwardWorkspace backward_workspace(const ep_ctx *ctx, int64_t rows, int n_in, 
     return w;
 }
 
+// As many warps to a column as the columns leave idle (about 2 blocks an SM), and no more than have a chunk each.
+template <int ROWS, typename T>
+int launch_few_rows_of(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int64_t ldw, int n_in, const Epilogue &e, bool vec,
+                       cudaStream_t stream) {
+    const int per_pass = 32 * (vec ? 16 / (int)sizeof(T) : 1);
+    int share = 1;
+    while (share < 8 && (int64_t)e.N * share * 2 <= (int64_t)ctx->sm_count * 16 && n_in > share * per_pass) share *= 2;
+    const int grid = (int)ep::ceil_div(e.N, 8 / share);
+    if (vec)
+        linear_few_rows<T, ROWS, true><<<grid, 256, 0, stream>>>((const T *)x, ldx, (const T *)w, ldw, n_in, e, share);
+    else
+        linear_few_rows<T, ROWS, false><<<grid, 256, 0, stream>>>((const T *)x, ldx, (const T *)w, ldw, n_in, e, share);
+    EP_CUDA(ctx, cudaGetLastError());
+    return EP_OK;
+}
 template <int ROWS>
 int launch_few_rows(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int64_t ldw, int in_type, int n_in, const Epilogue &e,
                     bool vec, cudaStream_t stream) {
-    const int grid = (int)ep::ceil_div(e.N, 8);
-    if (in_type == EP_F32)
-        linear_few_rows<float, ROWS><<<grid, 256, 0, stream>>>((const float *)x, ldx, (const float *)w, ldw, n_in, e, vec);
-    else if (in_type == EP_BF16)
-        linear_few_rows<__nv_bfloat16, ROWS><<<grid, 256, 0, stream>>>((const __nv_bfloat16 *)x, ldx, (const __nv_bfloat16 *)w, ldw,
-                                                                       n_in, e, vec);
-    else if (in_type == EP_F16)
-        linear_few_rows<__half, ROWS><<<grid, 256, 0, stream>>>((const __half *)x, ldx, (const __half *)w, ldw, n_in, e, vec);
-    else
-        linear_few_rows<e4m3, ROWS><<<grid, 256, 0, stream>>>((const e4m3 *)x, ldx, (const e4m3 *)w, ldw, n_in, e, vec);
-    EP_CUDA(ctx, cudaGetLastError());
-    return EP_OK;
+    if (in_type == EP_F32) return launch_few_rows_of<ROWS, float>(ctx, x, ldx, w, ldw, n_in, e, vec, stream);
+    if (in_type == EP_BF16) return launch_few_rows_of<ROWS, __nv_bfloat16>(ctx, x, ldx, w, ldw, n_in, e, vec, stream);
+    if (in_type == EP_F16) return launch_few_rows_of<ROWS, __half>(ctx, x, ldx, w, ldw, n_in, e, vec, stream);
+    return launch_few_rows_of<ROWS, e4m3>(ctx, x, ldx, w, ldw, n_in, e, vec, stream);
 }
 
 template <typename T, typename D, int PARTS>
@@ -1392,7 +1415,7 @@ void launch_dz(const BackwardWorkspace &w, const void *dout, const void *z, int 
 
 int linear_run(ep_ctx *ctx, const LinearWorkspace &ws, const void *x, int64_t ldx, const void *w, int64_t ldw, int in_type,
                int64_t rows, int n_in, int n_out, bool aligned, const Epilogue &e, cudaStream_t stream, int *kernels) {
-    if (rows <= FEW_ROWS) {
+    if (few_rows(rows, n_in, n_out, in_type)) {
         const int n = 16 / ep::type_size(in_type);
         const bool vec = aligned && n_in % n == 0;
         ++*kernels;
