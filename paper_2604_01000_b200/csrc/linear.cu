@@ -247,6 +247,64 @@ __device__ __forceinline__ void before_stores() {
     __syncwarp();
 }
 
+// Rows that TMA cannot write: a warp's 32 x 32 sums from shared memory (rows LOOSE floats apart), a column to each lane so
+// that neighbouring lanes write neighbouring elements.  What counts here is the number of instructions: the block has
+// two such warps a scheduler, and each takes about five clocks an instruction (with addresses and bounds worked out for
+// every row, 10000 x 65 fp32 took 5.5 us a chunk).
+constexpr int LOOSE = 33;
+template <typename O>
+struct LooseRows {
+    O *out, *z;
+    const O *residual;
+    const float *x_scale;
+    int64_t ldr;
+    int ldo, rows, act;
+    float bias, scale;
+    const float *sums;
+};
+template <typename O>
+__device__ __noinline__ void finish_rows(LooseRows<O> w) {
+    const bool plain = !w.z && !w.residual && !w.x_scale && w.act == EP_ACT_NONE;
+#pragma unroll 1
+    for (int r0 = 0; r0 < w.rows; r0 += 8, w.out += 8ll * w.ldo, w.sums += 8 * LOOSE) {
+        float v[8], add[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] = w.sums[r * LOOSE];
+        const bool whole = r0 + 8 <= w.rows;
+        if (!plain) {
+            if (w.x_scale) {
+#pragma unroll
+                for (int r = 0; r < 8; ++r) v[r] *= r0 + r < w.rows ? w.x_scale[r0 + r] * w.scale : 0.f;
+            }
+#pragma unroll
+            for (int r = 0; r < 8; ++r) add[r] = w.residual && r0 + r < w.rows ? to_f32(w.residual[r * w.ldr]) : 0.f;
+        }
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] += w.bias;
+        if (!plain) {
+            if (w.z) {
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r0 + r < w.rows) w.z[(int64_t)r * w.ldo] = from_f32<O>(v[r]);
+                w.z += 8ll * w.ldo;
+            }
+            activate(v, w.act);
+#pragma unroll
+            for (int r = 0; r < 8; ++r) v[r] += add[r];
+            if (w.residual) w.residual += 8 * w.ldr;
+        }
+        O *to = w.out;
+        if (whole) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r, to += w.ldo) *to = from_f32<O>(v[r]);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 8; ++r, to += w.ldo)
+                if (r0 + r < w.rows) *to = from_f32<O>(v[r]);
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------------------------- the tile kernel
 //
 // 128 x BN outputs per tile, one block per SM that goes from tile to tile: warp 8 brings k-blocks (128 bytes along k)
@@ -304,7 +362,7 @@ struct GemmShape {
     int64_t items;        // tiles x splits
     int splits, kb, kb_per_split;   // k-blocks of the whole sum, and of one split
     bool a_mn, b_mn;      // operand stored along its rows
-    uint32_t idesc;
+    uint32_t idesc;       // without the number of columns
 };
 
 // The four K-steps of one k-block.
@@ -418,6 +476,8 @@ struct Items {
     }
     __device__ __forceinline__ int m0() const { return tm * TILE_M; }
     __device__ __forceinline__ int n0() const { return tn * TILE_N; }
+    // Columns that the MMAs compute: the last tile's are cut to what the matrix has, in steps of 16.
+    __device__ __forceinline__ int columns() const { return min(TILE_N, (g.N - n0() + 15) & ~15); }
     __device__ __forceinline__ int kb0() const { return split * g.kb_per_split; }
     __device__ __forceinline__ int kbn() const { return min(g.kb_per_split, g.kb - kb0()); }
 };
@@ -485,7 +545,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
         bool ok = true;
         const uint32_t ring_base = smem_u32(ring);
         for (Walk t(g, worker); ok && t.more(); t.next()) {
-            const int m = t.m0() + (int)rank * BM, n = t.n0() + (int)rank * Mem::B_ROWS;   // this block's rows of A and of B
+            const int m = t.m0() + (int)rank * BM, n = t.n0() + (int)rank * (t.columns() / 2);   // this block's rows of A and of B
             const int kb0 = t.kb0(), kbn = t.kbn();
             for (int kb = 0; kb < kbn; ++kb, ++it) {
                 if (!(ok = __all_sync(FULL, mbar_wait(&sh->empty[s], ph ^ 1u, abort_flag)))) break;
@@ -532,6 +592,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
         const uint64_t astep = g.a_mn ? 2048 >> 4 : 32 >> 4, bstep = g.b_mn ? 2048 >> 4 : 32 >> 4;
         for (Walk t(g, worker); rank == 0 && ok && t.more(); t.next()) {
             const int kbn = t.kbn();
+            const uint32_t idesc = g.idesc | (uint32_t)(t.columns() >> 3) << 17;
             for (int kb = 0; ok && kb < kbn; ++acc) {
                 const int run_end = RUNS ? min(kb + RUN_KB, kbn) : kbn;
                 const uint32_t buf = acc & 1u, use = (acc >> 1) & 1u;
@@ -543,14 +604,14 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                     tc_fence_after();
                     const uint32_t a = ring_base + s * (uint32_t)STAGE_BYTES, b = a + PARTS * A_BYTES;
                     if constexpr (PARTS == 1) {
-                        umma_kblock_elected<F8, PAIR>(d_tmem, operand_desc(a, g.a_mn), operand_desc(b, g.b_mn), astep, bstep, g.idesc,
+                        umma_kblock_elected<F8, PAIR>(d_tmem, operand_desc(a, g.a_mn), operand_desc(b, g.b_mn), astep, bstep, idesc,
                                                 first);
                     } else {
                         constexpr int pa[6] = {0, 2, 0, 1, 1, 0}, pb[6] = {0, 0, 2, 1, 0, 1};
 #pragma unroll
                         for (int q = 0; q < 6; ++q)
                             umma_kblock_elected<F8, PAIR>(d_tmem + (q == 0 ? 0 : BN), operand_desc(a + pa[q] * A_BYTES, g.a_mn),
-                                                    operand_desc(b + pb[q] * B_BYTES, g.b_mn), astep, bstep, g.idesc,
+                                                    operand_desc(b + pb[q] * B_BYTES, g.b_mn), astep, bstep, idesc,
                                                     q <= 1 ? first : 1u);
                     }
                     commit_elected<PAIR>(&sh->empty[s]);
@@ -674,32 +735,24 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                 } else
                     turn ^= 1;
             } else {
-                // rows that TMA cannot write: through shared memory (16-byte piece c of row r lies at c ^ (r & 7)), so
-                // that neighbouring lanes finish neighbouring columns
-                float4 *mine = reinterpret_cast<float4 *>(slots);
-#pragma unroll 1
+                float *mine = reinterpret_cast<float *>(slots);
+#pragma unroll
                 for (int q = 0; q < SUBS; ++q) {
                     const int at = col + q * 32;
-                    float w32[32];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) w32[j] = SUBS > 1 && q == 1 ? v[SUBS - 1][j] : v[0][j];
-#pragma unroll
-                    for (int c = 0; c < 8; ++c)
-                        mine[lane * 8 + (c ^ (lane & 7))] = make_float4(w32[c * 4], w32[c * 4 + 1], w32[c * 4 + 2], w32[c * 4 + 3]);
+                    for (int j = 0; j < 32; ++j) mine[lane * LOOSE + j] = v[q][j];
                     __syncwarp();
                     if (at + lane < e.N) {
-                        Columns<1> c1;
-                        c1.load(e, at + lane);
-                        const float *flat = reinterpret_cast<const float *>(mine);
-#pragma unroll 1
-                        for (int r8 = 0; r8 < 32; r8 += 8)
-#pragma unroll
-                            for (int r = 0; r < 8; ++r) {
-                                if (row0 + r8 + r >= e.M) break;
-                                float w[1] = {flat[(r8 + r) * 32 + (((lane >> 2) ^ r) << 2) + (lane & 3)]}, add[1];
-                                load_residual<O>(e, row0 + r8 + r, at + lane, add);
-                                finish<O>(e, row0 + r8 + r, at + lane, c1, w, add);
-                            }
+                        LooseRows<O> w{static_cast<O *>(e.out) + row0 * e.N + at + lane, nullptr, nullptr, nullptr, e.ldr, e.N,
+                                       (int)min(e.M - row0, (int64_t)32), e.act, 0.f, 1.f, mine + lane};
+                        if (e.preact) w.z = static_cast<O *>(e.preact) + row0 * e.N + at + lane;
+                        if (e.residual) w.residual = static_cast<const O *>(e.residual) + row0 * e.ldr + at + lane;
+                        if (e.bias) w.bias = load_param(e.bias, e.bias_type, at + lane);
+                        if (e.x_scale) {
+                            w.x_scale = e.x_scale + row0;
+                            w.scale = __ldg(e.w_scale + at + lane);
+                        }
+                        finish_rows<O>(w);
                     }
                     __syncwarp();
                 }
@@ -808,11 +861,20 @@ __global__ void __launch_bounds__(256) linear_join(const float *__restrict__ sha
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (i < total) {
         const float *from = shares + ((int64_t)s0 * e.M + row) * e.ld_share + col;
-#pragma unroll 4
-        for (int s = s0; s < splits; s += 8, from += 8 * e.M * e.ld_share) {
-            const float4 a = *reinterpret_cast<const float4 *>(from), b = *reinterpret_cast<const float4 *>(from + 4);
-            v[0] += a.x, v[1] += a.y, v[2] += a.z, v[3] += a.w;
-            v[4] += b.x, v[5] += b.y, v[6] += b.z, v[7] += b.w;
+        const int64_t apart = 8 * e.M * e.ld_share;
+        for (int s = s0; s < splits; s += 8 * 5, from += 5 * apart) {   // five shares at a time, none alone at the end
+            float4 a[5], b[5];
+#pragma unroll
+            for (int q = 0; q < 5; ++q) {
+                const bool there = s + 8 * q < splits;
+                a[q] = there ? *reinterpret_cast<const float4 *>(from + q * apart) : make_float4(0.f, 0.f, 0.f, 0.f);
+                b[q] = there ? *reinterpret_cast<const float4 *>(from + q * apart + 4) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int q = 0; q < 5; ++q) {
+                v[0] += a[q].x, v[1] += a[q].y, v[2] += a[q].z, v[3] += a[q].w;
+                v[4] += b[q].x, v[5] += b[q].y, v[6] += b[q].z, v[7] += b[q].w;
+            }
         }
     }
 #pragma unroll
@@ -1229,7 +1291,7 @@ int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand
     p.shape.a_mn = a_mn;
     p.shape.b_mn = b_mn;
     p.shape.idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
-                    ((uint32_t)(p.bn >> 3) << 17) | ((uint32_t)((p.pair ? 2 * BM : BM) >> 4) << 24);
+                    ((uint32_t)((p.pair ? 2 * BM : BM) >> 4) << 24);
     e.share = p.splits > 1 ? share : nullptr;
     e.ld_share = p.ld_share;
     Maps m{};

@@ -262,8 +262,13 @@ __global__ void __launch_bounds__(1024) fold_partials(const float *__restrict__ 
     ep_wait_for_launch_before();
     double t = 0.0;
     if (c < cols)
-#pragma unroll 8
-        for (int r = r0; r < n; r += 32) t += (double)parts[(size_t)r * cols + c];
+        for (int r = r0; r < n; r += 32 * 16) {   // 16 loads at a time, none of them alone at the end
+            float v[16];
+#pragma unroll
+            for (int q = 0; q < 16; ++q) v[q] = r + 32 * q < n ? parts[(size_t)(r + 32 * q) * cols + c] : 0.f;
+#pragma unroll
+            for (int q = 0; q < 16; ++q) t += (double)v[q];
+        }
     s[r0][lane] = t;
     __syncthreads();
     t = s[lane][r0];   // a warp per column now

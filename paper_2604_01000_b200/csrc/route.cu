@@ -261,11 +261,22 @@ __global__ void __launch_bounds__(1024) route_fold(const float *__restrict__ par
     ep_wait_for_launch_before();
     double p = 0.0;
     long long m = 0;
-#pragma unroll 8
-    for (int r = r0; r < n; r += 32) {
-        if (c < f.parts) p += (double)part_prob[(size_t)r * f.parts + c];
-        if (c <= f.parts) m += part_count[(size_t)r * (f.parts + 1) + c];
-    }
+    if (c <= f.parts)
+        for (int r = r0; r < n; r += 32 * 8) {   // 8 loads of each at a time, none of them alone at the end
+            float v[8];
+            int u[8];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const bool there = r + 32 * q < n;
+                v[q] = there && c < f.parts ? part_prob[(size_t)(r + 32 * q) * f.parts + c] : 0.f;
+                u[q] = there ? part_count[(size_t)(r + 32 * q) * (f.parts + 1) + c] : 0;
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                p += (double)v[q];
+                m += u[q];
+            }
+        }
     sp[r0][lane] = p;
     sc[r0][lane] = m;
     __syncthreads();
@@ -277,6 +288,30 @@ __global__ void __launch_bounds__(1024) route_fold(const float *__restrict__ par
         m += __shfl_xor_sync(FULL, m, o);
     }
     const int mine = blockIdx.x * 32 + r0;
+    __syncthreads();
+    if (lane == 0) {   // sums of the block's columns to the first row
+        sp[0][r0] = p;
+        sc[0][r0] = m;
+    }
+    if (gridDim.x == 1) {   // (up to 31 parts: no other block to wait for)
+        __syncthreads();
+        if (r0 > 0) return;
+        const double rows = (double)max(sc[0][f.parts], 1ll);
+        double t = 0.0;
+        if (lane < f.parts) {
+            const float mean = (float)(sp[0][lane] / rows);
+            f.prob[lane] = mean;
+            f.counts[lane] = sc[0][lane];
+            t = (double)sc[0][lane] * (double)mean;
+        }
+#pragma unroll
+        for (int o = 16; o >= 1; o >>= 1) t += __shfl_xor_sync(FULL, t, o);
+        if (lane == 0) {
+            *f.loss = (float)(t * (double)f.parts / ((double)f.k * rows));
+            *f.routed = sc[0][f.parts];
+        }
+        return;
+    }
     if (lane == 0) {
         if (mine < f.parts) {
             f.prob[mine] = (float)p;
