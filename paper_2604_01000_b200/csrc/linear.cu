@@ -848,10 +848,40 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
 
 // The shares of a split sum, then the epilogue: 32 chunks of 8 columns a block, 8 threads to each, which add the shares
 // s, s + 8, ... in order; then the eight in order.
+// Blocks past those fold the partial sums of dbias, where there are any: 8 columns a block, 32 threads to each (one launch
+// less for a backward pass).
+struct BiasFold {
+    const float *parts;   // [slabs][n_out]; NULL: none
+    int slabs, n_out;
+    float *dbias;
+};
 __host__ __device__ constexpr int join_chunks() { return 32; }
 template <typename O>
-__global__ void __launch_bounds__(256) linear_join(const float *__restrict__ shares, int splits, const Epilogue e) {
-    __shared__ float part[8][join_chunks()][9];
+__global__ void __launch_bounds__(256) linear_join(const float *__restrict__ shares, int splits, const Epilogue e, int join_blocks,
+                                                   const BiasFold bias) {
+    __shared__ __align__(16) float part[8][join_chunks()][9];
+    if ((int)blockIdx.x >= join_blocks) {
+        const int c = ((int)blockIdx.x - join_blocks) * 8 + (threadIdx.x & 7), r0 = threadIdx.x >> 3;
+        double *sums = reinterpret_cast<double *>(part);   // [32][8]
+        ep_wait_for_launch_before();
+        double t = 0.0;
+        if (c < bias.n_out)
+            for (int r = r0; r < bias.slabs; r += 32 * 16) {
+                float v[16];
+#pragma unroll
+                for (int q = 0; q < 16; ++q) v[q] = r + 32 * q < bias.slabs ? bias.parts[(size_t)(r + 32 * q) * bias.n_out + c] : 0.f;
+#pragma unroll
+                for (int q = 0; q < 16; ++q) t += (double)v[q];
+            }
+        sums[threadIdx.x] = t;
+        __syncthreads();
+        if (threadIdx.x < 8 && c < bias.n_out) {
+#pragma unroll
+            for (int q = 1; q < 32; ++q) t += sums[q * 8 + threadIdx.x];
+            bias.dbias[c] = (float)t;
+        }
+        return;
+    }
     const int chunks = (e.N + 7) / 8;
     const int64_t total = e.M * chunks, i = (int64_t)blockIdx.x * join_chunks() + (threadIdx.x & 31);
     const int s0 = threadIdx.x >> 5;
@@ -1285,8 +1315,9 @@ int launch_type(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &e
 }
 
 // D = A B^T by tiles, with the epilogue; `share` is room for the shares of a split sum.  Adds to *kernels.
+// bias: sums to fold in the joining launch; without one (*folded stays false) that is left to the caller.
 int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand &b, bool b_mn, Epilogue e, float *share,
-             cudaStream_t stream, int *kernels) {
+             cudaStream_t stream, int *kernels, const BiasFold &bias = BiasFold{}, bool *folded = nullptr) {
     const uint32_t fmt = a.type == EP_BF16 ? 1u : 0u;   // f16 and e4m3 are both format 0 of their kinds
     p.shape.a_mn = a_mn;
     p.shape.b_mn = b_mn;
@@ -1312,13 +1343,15 @@ int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand
     ++*kernels;
     if (p.splits > 1) {
         // (a split sum has at most as many tiles as there are SMs: the grid is far below its limit)
-        const unsigned grid = (unsigned)ep::ceil_div(e.M * ((e.N + 7) / 8), join_chunks());
+        const int blocks = (int)ep::ceil_div(e.M * ((e.N + 7) / 8), join_chunks());
+        const unsigned grid = (unsigned)(blocks + (bias.parts ? ep::ceil_div(bias.n_out, 8) : 0));
+        if (folded) *folded = bias.parts != nullptr;
         if (e.out_type == EP_BF16)
-            EP_CUDA(ctx, ep::launch_early(linear_join<__nv_bfloat16>, dim3(grid), dim3(256), 0, stream, (const float *)share, p.splits, e));
+            EP_CUDA(ctx, ep::launch_early(linear_join<__nv_bfloat16>, dim3(grid), dim3(256), 0, stream, (const float *)share, p.splits, e, blocks, bias));
         else if (e.out_type == EP_F16)
-            EP_CUDA(ctx, ep::launch_early(linear_join<__half>, dim3(grid), dim3(256), 0, stream, (const float *)share, p.splits, e));
+            EP_CUDA(ctx, ep::launch_early(linear_join<__half>, dim3(grid), dim3(256), 0, stream, (const float *)share, p.splits, e, blocks, bias));
         else
-            EP_CUDA(ctx, ep::launch_early(linear_join<float>, dim3(grid), dim3(256), 0, stream, (const float *)share, p.splits, e));
+            EP_CUDA(ctx, ep::launch_early(linear_join<float>, dim3(grid), dim3(256), 0, stream, (const float *)share, p.splits, e, blocks, bias));
         ++*kernels;
     }
     return EP_OK;
@@ -1428,8 +1461,8 @@ BackwardWorkspace backward_workspace(const ep_ctx *ctx, int64_t rows, int n_in, 
         w.w = a.take<char>(packed_form(n_out, n_in, in_type).bytes);
     }
     const int across = (int)ep::ceil_div(w.dz_form.ld, DZ_CHUNKS * 8);
-    const int64_t want = std::max<int64_t>(1, (int64_t)ctx->sm_count * 8 / across);
-    w.slab = round_up(ep::ceil_div(std::max<int64_t>(rows, 1), want), DZ_ROWS);
+    const int64_t want = std::max<int64_t>(1, (int64_t)ctx->sm_count * 4 / across);   // about what stays resident
+    w.slab = std::max<int64_t>(round_up(ep::ceil_div(std::max<int64_t>(rows, 1), want), DZ_ROWS), 2 * DZ_ROWS);
     w.slabs = (int)std::max<int64_t>(1, ep::ceil_div(rows, w.slab));
     w.dbias_parts = a.take<float>((size_t)w.slabs * n_out);
     w.dx = plan_gemm(ctx, std::max<int64_t>(rows, 1), n_in, n_out, in_type, in_type == EP_F32);
@@ -1514,11 +1547,6 @@ int linear_backward_run(ep_ctx *ctx, const BackwardWorkspace &ws, const void *do
             launch_dz<__half, float, 1>(ws, dout, preact, act, rows, n_out, write, dbias, vec, stream);
         EP_CUDA(ctx, cudaGetLastError());
         ++*kernels;
-        if (dbias) {
-            const int rc_sum = ep::sum_partials(ctx, ws.dbias_parts, ws.slabs, n_out, dbias, stream);
-            if (rc_sum != EP_OK) return rc_sum;
-            ++*kernels;
-        }
     }
     Operand dz;
     if (direct)
@@ -1530,6 +1558,7 @@ int linear_backward_run(ep_ctx *ctx, const BackwardWorkspace &ws, const void *do
     e.bias_type = EP_F32;
     Operand xs{}, wt{};
     int rc = EP_OK;
+    bool folded = false;
     if (dx || dweight)
         rc = make_operands(ctx, Matrix{dweight ? x : nullptr, ldx, rows, n_in, ws.x}, Matrix{dx ? w : nullptr, ldw, n_out, n_in, ws.w},
                            in_type, copy, stream, &xs, &wt, kernels);
@@ -1549,8 +1578,14 @@ int linear_backward_run(ep_ctx *ctx, const BackwardWorkspace &ws, const void *do
         e.N = n_in;
         e.vec = n_in % 8 == 0 && ep::aligned(dweight, 16);
         e.tma = tma_ready(dweight, n_in, in_type);
-        rc = run_gemm(ctx, ws.dw, dz, true, xs, true, e, ws.share, stream, kernels);
+        rc = run_gemm(ctx, ws.dw, dz, true, xs, true, e, ws.share, stream, kernels,
+                      dbias ? BiasFold{ws.dbias_parts, ws.slabs, n_out, dbias} : BiasFold{}, &folded);
         if (rc != EP_OK) return rc;
+    }
+    if (dbias && !folded) {
+        rc = ep::sum_partials(ctx, ws.dbias_parts, ws.slabs, n_out, dbias, stream);
+        if (rc != EP_OK) return rc;
+        ++*kernels;
     }
     return EP_OK;
 }
