@@ -1000,25 +1000,25 @@ struct PackJob {
     void *to;
     int64_t ld, rows, part_stride;
     int cols, ld_to;
-    bool vec;
 };
 template <typename T, typename O, int PARTS>
 __global__ void __launch_bounds__(256) pack_rows(const PackJob first, const PackJob second) {
     const PackJob &j = blockIdx.y ? second : first;
-    const T *from = static_cast<const T *>(j.from);
+    const T *from = static_cast<const T *>(j.from), *end = from + (j.rows - 1) * j.ld + j.cols;
     O *to = static_cast<O *>(j.to);
     ep_let_next_launch_start();
-    const int chunks = j.ld_to / 8;
+    constexpr int N = PARTS == 3 ? 8 : 16 / (int)sizeof(O);   // elements of a thread: 16 bytes of each output
+    const int chunks = j.ld_to / N;
     const int64_t total = j.rows * chunks;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += (int64_t)gridDim.x * blockDim.x) {
         const int64_t row = i / chunks;
-        const int col = (int)(i - row * chunks) * 8;
+        const int col = (int)(i - row * chunks) * N;
+        T e[N];
+        load_elements_anywhere(from + row * j.ld + col, j.cols - col, from, end, e);
         if constexpr (PARTS == 3) {
-            float v[8];
-            load_chunk(from + row * j.ld, col, j.cols, j.vec, 0.f, v);
             __nv_bfloat16 p[8][3];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) split3(v[q], p[q]);
+            for (int q = 0; q < 8; ++q) split3(e[q], p[q]);
 #pragma unroll
             for (int k = 0; k < 3; ++k) {
                 alignas(16) __nv_bfloat16 o[8];
@@ -1027,11 +1027,10 @@ __global__ void __launch_bounds__(256) pack_rows(const PackJob first, const Pack
                 *reinterpret_cast<uint4 *>(to + k * j.part_stride + row * j.ld_to + col) = *reinterpret_cast<const uint4 *>(o);
             }
         } else {
-            alignas(16) O o[8];
+            alignas(16) O o[N];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) o[q] = col + q < j.cols ? from[row * j.ld + col + q] : O{};
-            using R = typename Raw<8 * (int)sizeof(O)>::type;
-            *reinterpret_cast<R *>(to + row * j.ld_to + col) = *reinterpret_cast<const R *>(o);
+            for (int q = 0; q < N; ++q) o[q] = e[q];
+            *reinterpret_cast<uint4 *>(to + row * j.ld_to + col) = *reinterpret_cast<const uint4 *>(o);
         }
     }
 }
@@ -1120,8 +1119,16 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz(const D *__restrict__ do
     } else if (col < ld_to) {
         for (int64_t row = begin + r0; row < end; row += DZ_ROWS) {
             float v[8], zz[8];
-            load_chunk(dout + row * n_out, col, n_out, false, 0.f, v);
-            if (act != EP_ACT_NONE) load_chunk(z + row * n_out, col, n_out, false, 0.f, zz);
+            D d[8];
+            load_elements_anywhere(dout + row * n_out + col, n_out - col, dout, dout + rows * n_out, d);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = to_f32(d[i]);
+            if (act != EP_ACT_NONE) {
+                T q[8];
+                load_elements_anywhere(z + row * n_out + col, n_out - col, z, z + rows * n_out, q);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) zz[i] = to_f32(q[i]);
+            }
             work(row, v, zz);
         }
     }
@@ -1394,7 +1401,7 @@ int make_operands(ep_ctx *ctx, const Matrix &first, const Matrix &second, int ty
     if (!needs_copy) return EP_OK;
     auto job = [&](const Matrix &m) {
         const Packed p = packed_form(m.rows, m.cols, type);
-        return PackJob{m.base, m.room, m.ld, m.base ? m.rows : 0, p.part_stride, m.cols, p.ld, tma_ready(m.base, m.ld, type) && m.cols % 8 == 0};
+        return PackJob{m.base, m.room, m.ld, m.base ? m.rows : 0, p.part_stride, m.cols, p.ld};
     };
     const PackJob x = job(first), w = job(second);
     const int64_t threads = std::max(x.rows * (x.ld_to / 8), w.rows * (w.ld_to / 8));

@@ -208,9 +208,10 @@ __global__ void __launch_bounds__(THREADS, 3) route_rows(const T *__restrict__ l
             }
         }
         if (renormalize && mine) {
-            const float scale = part ? reciprocal_fast(chosen_sum) : 0.f;
-            if (lane < k) weights[row * k + lane] = my_w * scale;
-            for (int r = lane + L; r < k; r += L) weights[row * k + r] *= scale;   // this thread's own earlier stores
+            // (divided, not multiplied by a reciprocal: the weight of a row's only slot is exactly 1)
+            if (lane < k) weights[row * k + lane] = part ? my_w / chosen_sum : 0.f;
+            for (int r = lane + L; r < k; r += L)   // this thread's own earlier stores
+                weights[row * k + r] = part ? weights[row * k + r] / chosen_sum : 0.f;
         }
     }
 
@@ -404,27 +405,41 @@ __global__ void __launch_bounds__(THREADS, 3) route_rows_backward(const T *__res
         dot = reduce_row<L, OpSum>(dot, slots, turn);
         const float inverse = part ? reciprocal_fast(s) : 0.f;
         dot *= inverse;
-        // the slots, shared out over the row's threads: sum of p and of dweights p.  A thread keeps its first slot.
+        // The slots, shared out over the row's threads; a thread keeps its first.  Renormalised: the sum of their p, then
+        // the mean of dweights by p / sum (in this order: where a row's weights are constants, what reaches them cancels
+        // exactly); otherwise the sum of dweights p.
         float chosen = 0.f, pulled = 0.f, first_w = 0.f;
         int first_id = -1;
         if (dweights) {
             if constexpr (L <= 32) __syncwarp();   // (wider rows have met at a sum)
-            auto slot = [&](int id, float dw) {
+            auto slot = [&](int id) {
                 if (id < 0 || id >= parts) {
                     if (id != -1) ep_raise(status, EP_ERR_BAD_INDEX);
                     return 0.f;
                 }
-                const float w = exp_fast(stream.element(first, id) - top) * inverse;
-                chosen += w;
-                pulled = fmaf(dw, w, pulled);
-                return w;
+                return exp_fast(stream.element(first, id) - top) * inverse;
+            };
+            auto slots_after_first = [&](auto f) {
+                for (int q = lane + L; q < k; q += L) f(slot(ids[row * k + q]), dweights[row * k + q]);
             };
             if (part) {
-                first_w = slot(now.id, now.dw);
+                first_w = slot(now.id);
                 first_id = now.id < parts ? now.id : -1;
-                for (int q = lane + L; q < k; q += L) slot(ids[row * k + q], dweights[row * k + q]);
+                if (renormalize) {
+                    chosen = first_w;
+                    slots_after_first([&](float w, float) { chosen += w; });
+                } else {
+                    pulled = now.dw * first_w;
+                    slots_after_first([&](float w, float dw) { pulled = fmaf(dw, w, pulled); });
+                }
             }
-            chosen = reduce_row<L, OpSum>(chosen, slots, turn);
+            if (renormalize) {
+                chosen = reduce_row<L, OpSum>(chosen, slots, turn);
+                if (part && chosen > 0.f) {
+                    pulled = now.dw * (first_w / chosen);
+                    slots_after_first([&](float w, float dw) { pulled = fmaf(dw, w / chosen, pulled); });
+                }
+            }
             pulled = reduce_row<L, OpSum>(pulled, slots, turn);
         }
         // with renormalised weights the slots' own terms of sum_e p_e dp_e cancel
@@ -444,7 +459,7 @@ __global__ void __launch_bounds__(THREADS, 3) route_rows_backward(const T *__res
         else
             __syncwarp();
         if (part) {
-            const float mean = renormalize ? pulled / chosen : 0.f, per = renormalize ? 1.f / chosen : 1.f;
+            const float mean = renormalize ? pulled : 0.f, per = renormalize ? 1.f / chosen : 1.f;
             auto again = [&](int id, float w, float dw) {
                 const float own = dloss ? unit * (float)counts[id] : 0.f;
                 to[id] = from_f32<T>(w * (own + (dw - mean) * per - back));

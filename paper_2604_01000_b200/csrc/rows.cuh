@@ -146,6 +146,47 @@ __device__ __forceinline__ void store_chunk(T *row, int col, int width, bool vec
     }
 }
 
+// WORDS consecutive 32-bit words from any byte address on, by 16-byte accesses and shifts.  The accesses reach up to 15
+// bytes to either side: the caller has made sure that [p & ~15, + 4 WORDS + 16) belongs to the matrix.
+template <int WORDS>
+__device__ __forceinline__ void load_words_anywhere(const void *p, uint32_t (&out)[WORDS]) {
+    const uintptr_t b = reinterpret_cast<uintptr_t>(p);
+    const uint4 *from = reinterpret_cast<const uint4 *>(b & ~uintptr_t(15));
+    uint32_t w[WORDS + 4];
+#pragma unroll
+    for (int q = 0; q < WORDS / 4 + 1; ++q) {
+        const uint4 v = from[q];
+        w[4 * q] = v.x, w[4 * q + 1] = v.y, w[4 * q + 2] = v.z, w[4 * q + 3] = v.w;
+    }
+    const bool one = b & 4, two = b & 8;
+#pragma unroll
+    for (int i = 0; i < WORDS + 3; ++i) w[i] = one ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < WORDS + 1; ++i) w[i] = two ? w[i + 2] : w[i];
+    const unsigned bits = (unsigned)(b & 3) * 8;
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) out[i] = __funnelshift_r(w[i], w[i + 1], bits);
+}
+// N elements of a row from p on, of which the first `inside` (at least 1) belong to it; the others come out as zero bits.
+// begin, end: the matrix.
+template <int N, typename T>
+__device__ __forceinline__ void load_elements_anywhere(const T *p, int inside, const T *begin, const T *end, T (&e)[N]) {
+    constexpr int BYTES = N * (int)sizeof(T);
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p) & ~uintptr_t(15);
+    if (a >= reinterpret_cast<uintptr_t>(begin) && a + BYTES + 16 <= reinterpret_cast<uintptr_t>(end)) {
+        union {
+            uint32_t w[BYTES / 4];
+            T t[N];
+        } u;
+        load_words_anywhere(p, u.w);
+#pragma unroll
+        for (int i = 0; i < N; ++i) e[i] = i < inside ? u.t[i] : T{};
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) e[i] = i < inside ? p[i] : T{};
+    }
+}
+
 // ---- sums and maxima over the L threads of a row -------------------------------------------------
 // L <= 32: neighbouring lanes of one warp (all 32 lanes of the warp call together).  L > 32: the whole block; `slots`
 // is then shared memory of 2 x 32 floats used in turn (`turn` flips with every call), one barrier per call.

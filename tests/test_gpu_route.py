@@ -181,6 +181,16 @@ def test_gradient_against_differences():
         assert abs(float((grad.double() * v.double()).sum()) - diff) <= 2e-3 * float(grad.norm()) * float(v.norm())
 
 
+@pytest.mark.parametrize("parts", [1, 5, 40, 700, 2000])
+def test_a_single_renormalised_weight_is_one_and_has_no_gradient(parts):
+    for dtype in (F32, BF16):
+        l = make(50, parts, dtype, 15)
+        r = ep().ep_route(l, 1, None, True)
+        assert bool((r.weights == 1).all())
+        dw = torch.randn(50, 1, device="cuda")
+        assert not bool(ep().ep_route_backward(l, r, dw, None, None, True).any())
+
+
 def test_balance_loss_of_even_and_of_one_sided_routing():
     even = torch.full((64, 8), -4.0, device="cuda")
     even[torch.arange(64), torch.arange(64) % 8] = 4.0
