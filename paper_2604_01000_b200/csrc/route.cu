@@ -16,8 +16,9 @@ namespace {
 
 constexpr int MAX_PARTS = 4096;
 constexpr int MAX_K = 32;
-constexpr int BLOCKS_PER_SM = 3;   // what their registers let stay resident
 constexpr int THREADS = 256;
+// Blocks that stay resident (2449029 rows of 32: 75 us; with 4 to an SM, and 64 registers a thread, 80).
+constexpr int BLOCKS_PER_SM = 3;
 
 // The better of two (logit, column) pairs: the larger logit, of equal ones the lower column.
 __device__ __forceinline__ void keep_better(float &v, int &c, float ov, int oc) {
@@ -111,7 +112,7 @@ __device__ void finish_block(const Finish &f, int64_t rows_routed, double *red) 
 }
 
 template <typename T, typename Lay>
-__global__ void __launch_bounds__(THREADS, 3) route_rows(const T *__restrict__ logits, int64_t rows, int parts, int k,
+__global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) route_rows(const T *__restrict__ logits, int64_t rows, int parts, int k,
                                                       const uint8_t *__restrict__ valid, bool renormalize,
                                                       int32_t *__restrict__ ids, float *weights,
                                                       float *__restrict__ part_prob, int *__restrict__ part_count,
@@ -153,20 +154,12 @@ __global__ void __launch_bounds__(THREADS, 3) route_rows(const T *__restrict__ l
         top = reduce_row<L, OpMaxNumber>(top, slots, turn);
         const bool part = top > -INFINITY;   // false for a row of NaN and -infinity alone, too
         const float shift = part ? top : 0.f;   // (-infinity - 0: the exponentials of a row left out are zero)
-        float e[V][N];
-        float s = exponentials(l, shift, e);
-        s = reduce_row<L, OpSum>(s, slots, turn);
-        const float inverse = part ? reciprocal_fast(s) : 0.f;
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-#pragma unroll
-            for (int i = 0; i < N; i += 2)
-                fma2(Pair(e[j][i], e[j][i + 1]), Pair(inverse), Pair(sum_p[j][i], sum_p[j][i + 1])).get(sum_p[j][i], sum_p[j][i + 1]);
         took_part += part && lane == 0;
 
-        // the k largest, one after the other: each thread offers the best of its columns that is left (the first is
-        // the lowest column that holds the maximum just found)
-        float chosen_sum = 0.f, my_w = 0.f;
+        // the k largest, one after the other, while the logits are still there: each thread offers the best of its columns
+        // that is not taken (the first is the lowest column that holds the maximum just found)
+        uint32_t taken = 0;
+        float chosen = 0.f, mine_exp = 0.f;   // the sum of the slots' exponentials, and that of this thread's first slot
         for (int r = 0; r < k; ++r) {
             float v = r == 0 ? top : -INFINITY;
             int c = MAX_PARTS;
@@ -182,21 +175,21 @@ __global__ void __launch_bounds__(THREADS, 3) route_rows(const T *__restrict__ l
                 for (int j = 0; j < V; ++j)
 #pragma unroll
                     for (int i = 0; i < N; ++i)
-                        if (l[j][i] > v) {
+                        if (l[j][i] > v && !(taken >> (j * N + i) & 1)) {
                             v = l[j][i];
                             c = Lay::col(lane, j, i);
                         }
             }
             best_of_row<L>(v, c, slot_v, slot_c, turn_best);
             const bool got = v > -INFINITY;
-            const float w = got ? exp_fast(v - top) * inverse : 0.f;
-            chosen_sum += w;
+            const float ex = got ? exp_fast(v - top) : 0.f;
+            chosen += ex;
             if (lane == r % L) {
                 if (mine) {
                     ids[row * k + r] = got ? c : -1;
-                    if (!renormalize || r >= L) weights[row * k + r] = w;
+                    if (r >= L) weights[row * k + r] = ex;   // finished below, by this thread
                 }
-                if (r < L) my_w = w;
+                if (r < L) mine_exp = ex;
                 if (got) atomicAdd(&hist[c], 1);
             }
             if (r + 1 < k) {
@@ -204,14 +197,25 @@ __global__ void __launch_bounds__(THREADS, 3) route_rows(const T *__restrict__ l
                 for (int j = 0; j < V; ++j)
 #pragma unroll
                     for (int i = 0; i < N; ++i)
-                        if (Lay::col(lane, j, i) == c) l[j][i] = -INFINITY;
+                        if (Lay::col(lane, j, i) == c) taken |= 1u << (j * N + i);
             }
         }
-        if (renormalize && mine) {
-            // (divided, not multiplied by a reciprocal: the weight of a row's only slot is exactly 1)
-            if (lane < k) weights[row * k + lane] = part ? my_w / chosen_sum : 0.f;
-            for (int r = lane + L; r < k; r += L)   // this thread's own earlier stores
-                weights[row * k + r] = part ? weights[row * k + r] / chosen_sum : 0.f;
+        static_assert(V * N <= 32, "a bit of `taken` for every column of a thread");
+
+        const float s = reduce_row<L, OpSum>(exponentials(l, shift, l), slots, turn);
+        const float inverse = part ? reciprocal_fast(s) : 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int i = 0; i < N; i += 2)
+                fma2(Pair(l[j][i], l[j][i + 1]), Pair(inverse), Pair(sum_p[j][i], sum_p[j][i + 1])).get(sum_p[j][i], sum_p[j][i + 1]);
+        if (mine) {
+            // over all columns or, renormalised, over the chosen ones (divided, not multiplied by a reciprocal: the weight
+            // of a row's only slot is exactly 1).  A NaN or +infinity in the row makes both sums' quotients NaN.
+            const float nan_too = s != s ? s : 0.f;
+            auto weight = [&](float ex) { return renormalize ? (part ? ex / chosen + nan_too : 0.f) : ex * inverse; };
+            if (lane < k) weights[row * k + lane] = weight(mine_exp);
+            for (int r = lane + L; r < k; r += L) weights[row * k + r] = weight(weights[row * k + r]);
         }
     }
 
@@ -330,7 +334,7 @@ __global__ void __launch_bounds__(1024) route_fold(const float *__restrict__ par
 }
 
 template <typename T, typename Lay>
-__global__ void __launch_bounds__(THREADS, 3) route_rows_backward(const T *__restrict__ logits, int64_t rows, int parts, int k,
+__global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) route_rows_backward(const T *__restrict__ logits, int64_t rows, int parts, int k,
                                                                const uint8_t *__restrict__ valid, bool renormalize,
                                                                const int32_t *__restrict__ ids,
                                                                const int64_t *__restrict__ counts,
@@ -478,8 +482,9 @@ __global__ void __launch_bounds__(THREADS, 3) route_rows_backward(const T *__res
     stream.end();
 }
 
-int grid_for(const ep_ctx *ctx, int64_t rows, int groups) {
-    return (int)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(rows, groups), (int64_t)ctx->sm_count * BLOCKS_PER_SM));
+template <typename Lay>
+int grid_for(const ep_ctx *ctx, int64_t rows) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(rows, THREADS / Lay::L), (int64_t)ctx->sm_count * BLOCKS_PER_SM));
 }
 
 struct RouteArgs {
@@ -509,7 +514,7 @@ struct RouteLaunch {
         const size_t hist_at = std::max((size_t)RowStream<T, Lay, THREADS>::ring_bytes(a.parts),
                                         groups > 1 ? sizeof(float) * groups * Lay::WIDE : 0);
         const size_t smem = hist_at + sizeof(int) * (size_t)(a.parts + 1);
-        const int grid = grid_for(a.ctx, a.rows, groups);
+        const int grid = grid_for<Lay>(a.ctx, a.rows);
         if (smem > 40 * 1024)   // (static shared memory counts too)
             EP_CUDA(a.ctx, cudaFuncSetAttribute(route_rows<T, Lay>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
         route_rows<T, Lay><<<grid, THREADS, smem, a.stream>>>((const T *)a.logits, a.rows, a.parts, a.k, a.valid,
@@ -549,7 +554,7 @@ struct RouteBackLaunch {
         const int smem = RowStream<T, Lay, THREADS>::ring_bytes(a.parts);
         if (smem > 40 * 1024)   // (static shared memory counts too)
             EP_CUDA(a.ctx, cudaFuncSetAttribute(route_rows_backward<T, Lay>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-        route_rows_backward<T, Lay><<<grid_for(a.ctx, a.rows, THREADS / Lay::L), THREADS, smem, a.stream>>>(
+        route_rows_backward<T, Lay><<<grid_for<Lay>(a.ctx, a.rows), THREADS, smem, a.stream>>>(
             (const T *)a.logits, a.rows, a.parts, a.k, a.valid, a.renormalize, a.ids, a.counts, a.routed, a.dweights, a.dloss,
             (T *)a.dlogits, a.ctx->d_status, ep::aligned(a.logits, 16));
         EP_CUDA(a.ctx, cudaGetLastError());
