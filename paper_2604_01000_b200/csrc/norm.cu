@@ -1,9 +1,11 @@
 // Root-mean-square norm with the residual's addition and an optional 8-bit output, its backward pass, and the 8-bit
 // output on its own.
 //
-// One pass over the data: a row stays in the registers of the L threads that share it, between the sum that gives its
-// scale and the product with it, so every input is read once and every output written once.  All of these kernels are
-// bound by HBM bandwidth for many rows and by launch latency for few.
+// One pass over the data: a row stays with the L threads that share it (in registers, in the backward pass in shared
+// memory), between the sum that gives its scale and the product with it, so every input is read once and every output
+// written once.  All of these kernels are bound by HBM bandwidth for many rows and by launch latency for few.  Measured
+// (of 6464 GB/s, a plain copy): 169343 x 128 fp32 with residual to bf16 50 us, 6.1 TB/s; backward of 2449029 x 128 bf16
+// 422 us, 5.9 TB/s; one row of 1024 to 8 bits 4 us.
 #include "ep_common.cuh"
 #include "rows.cuh"
 

@@ -3,7 +3,7 @@
 Bounds.  With S = sum |x| |w| of an output, the tensor core adds 16 products (32 of 8-bit inputs) a step and truncates:
 at most 2^-22 S a step (2^-23 of the running sum, and the same again for aligning a step's products), so (n_in / 16 + 4)
 2^-22 S where sums run through, 32 2^-22 S where they are kept in runs (fp32 outputs).  Three bf16 parts leave out
-products below 3 2^-24 S.  The epilogue's fp32 work is within 2^-20 of its terms, and one rounding ends it.
+products below 2^-22 S together.  The epilogue's fp32 work is within 2^-20 of its terms, and one rounding ends it.
 """
 import math
 
