@@ -366,8 +366,9 @@ struct GemmShape {
     int step_m, step_n;   // one worker's way from tile to tile: tiles of M and of N
     int64_t tiles;        // tiles of the output
     int64_t items;        // tiles x splits
-    int splits, kb, kb_per_split;   // k-blocks of the whole sum, and of one split
+    int splits, kb;       // shares of the sum; k-blocks of all of it (share s takes k-blocks s, s + splits, ...)
     bool a_mn, b_mn;      // operand stored along its rows
+    bool backwards;       // the last row of tiles first: where A has just been written, its end is still in the L2
     uint32_t idesc;       // without the number of columns
 };
 
@@ -480,12 +481,11 @@ struct Items {
             ++split;
         }
     }
-    __device__ __forceinline__ int m0() const { return tm * TILE_M; }
+    __device__ __forceinline__ int m0() const { return (g.backwards ? g.tiles_m - 1 - tm : tm) * TILE_M; }
     __device__ __forceinline__ int n0() const { return tn * TILE_N; }
     // Columns that the MMAs compute: the last tile's are cut to what the matrix has, in steps of 16.
     __device__ __forceinline__ int columns() const { return min(TILE_N, (g.N - n0() + 15) & ~15); }
-    __device__ __forceinline__ int kb0() const { return split * g.kb_per_split; }
-    __device__ __forceinline__ int kbn() const { return min(g.kb_per_split, g.kb - kb0()); }
+    __device__ __forceinline__ int kbn() const { return (g.kb - split + g.splits - 1) / g.splits; }
 };
 
 template <int BN, bool F8, int PARTS, bool RUNS, bool PAIR, typename O>
@@ -552,12 +552,12 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
         const uint32_t ring_base = smem_u32(ring);
         for (Walk t(g, worker); ok && t.more(); t.next()) {
             const int m = t.m0() + (int)rank * BM, n = t.n0() + (int)rank * (t.columns() / 2);   // this block's rows of A and of B
-            const int kb0 = t.kb0(), kbn = t.kbn();
+            const int kbn = t.kbn();
             for (int kb = 0; kb < kbn; ++kb, ++it) {
                 if (!(ok = __all_sync(FULL, mbar_wait(&sh->empty[s], ph ^ 1u, abort_flag)))) break;
                 if (rank == 0) mbar_expect_tx_elected(&sh->full[s], (PAIR ? 2 : 1) * STAGE_BYTES);
                 const uint32_t bar = PAIR ? in_block(smem_u32(&sh->full[s]), 0) : smem_u32(&sh->full[s]);
-                const int k = (kb0 + kb) * KE;
+                const int k = (t.split + kb * g.splits) * KE;
                 uint32_t dst = ring_base + s * (uint32_t)STAGE_BYTES;
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p, dst += A_BYTES) {
@@ -1053,13 +1053,14 @@ constexpr int dz_pieces() { return (8 * (int)(sizeof(T) + sizeof(D))) / 16; }   
 template <typename T, typename D, int PARTS>
 __global__ void __launch_bounds__(DZ_THREADS) linear_dz(const D *__restrict__ dout, const T *__restrict__ z, int act, int64_t rows,
                                                         int n_out, void *to_raw, int ld_to, int64_t part_stride,
-                                                        float *__restrict__ part, int64_t slab, bool vec) {
+                                                        float *__restrict__ part, bool vec) {
     constexpr int D_PIECES = 8 * (int)sizeof(D) / 16, Z_PIECES = 8 * (int)sizeof(T) / 16;
     __shared__ float fold[DZ_ROWS][DZ_CHUNKS * 8];
     extern __shared__ uint4 ring[];   // [DZ_STAGES][D_PIECES + Z_PIECES][DZ_THREADS], where vec
     const int cx = threadIdx.x % DZ_CHUNKS, r0 = threadIdx.x / DZ_CHUNKS;
     const int col = (blockIdx.x * DZ_CHUNKS + cx) * 8;
-    const int64_t begin = (int64_t)blockIdx.y * slab, end = min(rows, begin + slab);
+    // all blocks go over the rows side by side, so that what is written last lies together (see GemmShape::backwards)
+    const int64_t begin = (int64_t)blockIdx.y * DZ_ROWS, step = (int64_t)gridDim.y * DZ_ROWS;
     ep_let_next_launch_start();
     float sum[8];
 #pragma unroll
@@ -1088,7 +1089,7 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz(const D *__restrict__ do
     if (vec) {
         auto slot = [&](int s) { return ring + (size_t)s * (D_PIECES + Z_PIECES) * DZ_THREADS + threadIdx.x; };
         auto fetch = [&](int64_t row, int s) {
-            if (row < end && col < n_out) {
+            if (row < rows && col < n_out) {
                 uint4 *to = slot(s);
 #pragma unroll
                 for (int p = 0; p < D_PIECES; ++p) copy_async<16>(to + p * DZ_THREADS, reinterpret_cast<const uint4 *>(dout + row * n_out + col) + p);
@@ -1101,9 +1102,9 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz(const D *__restrict__ do
         };
         int64_t ahead = begin + r0;
 #pragma unroll
-        for (int s = 0; s < DZ_STAGES - 1; ++s, ahead += DZ_ROWS) fetch(ahead, s);
+        for (int s = 0; s < DZ_STAGES - 1; ++s, ahead += step) fetch(ahead, s);
         int s = 0;
-        for (int64_t row = begin + r0; row < end; row += DZ_ROWS, ahead += DZ_ROWS) {
+        for (int64_t row = begin + r0; row < rows; row += step, ahead += step) {
             fetch(ahead, s == 0 ? DZ_STAGES - 1 : s - 1);   // into the slots of the row before
             copies_wait<DZ_STAGES - 1>();
             if (col < n_out) {   // (whole chunks: rows of ld_to and of n_out elements end at the same one)
@@ -1125,7 +1126,7 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz(const D *__restrict__ do
         }
         copies_wait<0>();
     } else if (col < ld_to) {
-        for (int64_t row = begin + r0; row < end; row += DZ_ROWS) {
+        for (int64_t row = begin + r0; row < rows; row += step) {
             float v[8], zz[8];
             D d[8];
             load_elements_anywhere(dout + row * n_out + col, n_out - col, dout, dout + rows * n_out, d);
@@ -1262,12 +1263,9 @@ GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, boo
             p.shape.tiles_m = (int)ep::ceil_div(M, pair ? 2 * BM : BM);
             p.shape.tiles = (int64_t)p.shape.tiles_m * p.shape.tiles_n;
             const int workers = pair ? ctx->sm_count / 2 : ctx->sm_count;
-            const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(workers / p.shape.tiles, kb / 4));
-            int per = (int)ep::ceil_div(kb, splits);
-            if (p.runs) per = (int)round_up(per, RUN_KB);
-            p.splits = (int)ep::ceil_div(kb, per);
+            p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(workers / p.shape.tiles, kb / 4));
+            const int per = (int)ep::ceil_div(kb, p.splits);
             p.shape.splits = p.splits;
-            p.shape.kb_per_split = per;
             p.shape.items = p.shape.tiles * p.splits;
             p.workers = (int)std::min<int64_t>(p.shape.items, workers);
             p.shape.step_m = p.workers / p.shape.tiles_n;
@@ -1461,8 +1459,7 @@ struct BackwardWorkspace {
     float *dbias_parts, *share;
     GemmPlan dx, dw;
     Packed dz_form;
-    int slabs;
-    int64_t slab;
+    int slabs;   // blocks that share out the rows in linear_dz
     size_t bytes;
 };
 BackwardWorkspace backward_workspace(const ep_ctx *ctx, int64_t rows, int n_in, int n_out, int in_type, bool aligned, void *base) {
@@ -1477,8 +1474,7 @@ BackwardWorkspace backward_workspace(const ep_ctx *ctx, int64_t rows, int n_in, 
     }
     const int across = (int)ep::ceil_div(w.dz_form.ld, DZ_CHUNKS * 8);
     const int64_t want = std::max<int64_t>(1, (int64_t)ctx->sm_count * 4 / across);   // about what stays resident
-    w.slab = std::max<int64_t>(round_up(ep::ceil_div(std::max<int64_t>(rows, 1), want), DZ_ROWS), 2 * DZ_ROWS);
-    w.slabs = (int)std::max<int64_t>(1, ep::ceil_div(rows, w.slab));
+    w.slabs = (int)std::max<int64_t>(1, std::min<int64_t>(want, ep::ceil_div(rows, 2 * DZ_ROWS)));
     w.dbias_parts = a.take<float>((size_t)w.slabs * n_out);
     w.dx = plan_gemm(ctx, std::max<int64_t>(rows, 1), n_in, n_out, in_type, in_type == EP_F32);
     w.dw = plan_gemm(ctx, n_out, n_in, std::max<int64_t>(rows, 1), in_type, in_type == EP_F32);
@@ -1520,7 +1516,7 @@ void launch_dz(const BackwardWorkspace &w, const void *dout, const void *z, int 
                          DZ_STAGES * dz_pieces<T, D>() * DZ_THREADS * 16);
     linear_dz<T, D, PARTS><<<grid, DZ_THREADS, smem, stream>>>((const D *)dout, (const T *)z, act, rows, n_out,
                                                                      write ? w.dz : nullptr, w.dz_form.ld, w.dz_form.part_stride,
-                                                                     sum ? w.dbias_parts : nullptr, w.slab, vec);
+                                                                     sum ? w.dbias_parts : nullptr, vec);
 }
 
 int linear_run(ep_ctx *ctx, const LinearWorkspace &ws, const void *x, int64_t ldx, const void *w, int64_t ldw, int in_type,
@@ -1584,7 +1580,9 @@ int linear_backward_run(ep_ctx *ctx, const BackwardWorkspace &ws, const void *do
         e.N = n_in;
         e.vec = n_in % 8 == 0 && ep::aligned(dx, 16);
         e.tma = tma_ready(dx, n_in, in_type);
-        rc = run_gemm(ctx, ws.dx, dz, false, wt, true, e, ws.share, stream, kernels);
+        GemmPlan back = ws.dx;
+        back.shape.backwards = true;
+        rc = run_gemm(ctx, back, dz, false, wt, true, e, ws.share, stream, kernels);
         if (rc != EP_OK) return rc;
     }
     if (dweight) {

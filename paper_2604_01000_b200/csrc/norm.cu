@@ -283,8 +283,9 @@ constexpr int MAX_D = 16384;
 constexpr int FORWARD_BLOCKS_PER_SM = 8, BACKWARD_BLOCKS_PER_SM = 4;   // about what their registers let stay resident
 
 template <int L>
-int grid_for(const ep_ctx *ctx, int64_t rows, int per_sm) {
+int grid_for(const ep_ctx *ctx, int64_t rows, int per_sm, int alone = 1) {
     constexpr int groups = block_threads<L>() / L;
+    if (rows <= (int64_t)groups * alone) return 1;
     return (int)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(rows, groups), (int64_t)ctx->sm_count * per_sm));
 }
 
@@ -354,7 +355,8 @@ struct BackLaunch {
         constexpr int threads = block_threads<Lay::L>();
         constexpr size_t fold = threads == Lay::L ? 0 : sizeof(float) * (threads / Lay::L) * Lay::WIDE;
         constexpr size_t smem = std::max(fold, ring_bytes<T, D, Lay>());
-        const int grid = grid_for<Lay::L>(a.ctx, a.rows, BACKWARD_BLOCKS_PER_SM);
+        // (two rounds of one block are quicker than two blocks and the fold after them: 128 x 64 fp32 in 3.9 us against 4.5)
+        const int grid = grid_for<Lay::L>(a.ctx, a.rows, BACKWARD_BLOCKS_PER_SM, a.dweight ? 2 : 1);
         float *part = !a.dweight ? nullptr : grid == 1 ? a.dweight : a.parts;
         if (smem > 40 * 1024)   // (static shared memory counts too)
             EP_CUDA(a.ctx, cudaFuncSetAttribute(norm_rows_backward<T, D, Lay>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));

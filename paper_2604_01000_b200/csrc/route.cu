@@ -518,7 +518,8 @@ struct RouteLaunch {
         const size_t hist_at = std::max((size_t)RowStream<T, Lay, THREADS>::ring_bytes(a.parts),
                                         groups > 1 ? sizeof(float) * groups * Lay::WIDE : 0);
         const size_t smem = hist_at + sizeof(int) * (size_t)(a.parts + 1);
-        const int grid = grid_for<Lay>(a.ctx, a.rows);
+        // (two rounds of one block are quicker than two blocks and the fold after them: 128 x 64 fp32 in 5.0 us against 7.3)
+        const int grid = a.rows <= 2 * groups ? 1 : grid_for<Lay>(a.ctx, a.rows);
         if (smem > 40 * 1024)   // (static shared memory counts too)
             EP_CUDA(a.ctx, cudaFuncSetAttribute(route_rows<T, Lay>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
         route_rows<T, Lay><<<grid, THREADS, smem, a.stream>>>((const T *)a.logits, a.rows, a.parts, a.k, a.valid,
