@@ -11,10 +11,9 @@
 // that was split between blocks.
 //
 // Measured: 8192 x 4096 x 4096 fp16 195 us, 1410 TFLOP/s (tensor pipe 90 % busy; cuBLAS alone reaches 1669 in short bursts);
-// 2000 x 4096 x 4096 in 8 bits 31 us, 2150 TFLOP/s (1.7 waves of tiles, so 2); 169343 x 128 -> 512 bf16 with z kept 73 us,
-// 5.3 TB/s of 6.5 (the epilogue's two warps a scheduler, then memory); backward of 232965 x 256 x 256 bf16 through GELU
-// 158 us: dz 60, dx 47, dW 46 and its join 7, against 74 us for reading and writing everything once; one row of 1024 x 1024
-// 3 us.
+// 2000 x 4096 x 4096 in 8 bits 31 us, 2150 TFLOP/s (1.7 waves of tiles, so 2); 169343 x 128 -> 512 bf16 41 us, 5.3 TB/s of
+// 6.5, with z kept 75 us, 5.2 TB/s; backward of 232965 x 256 x 256 bf16 through GELU 153 us: dz 60, dx 44, dW 46 and its
+// join 7, against 74 us for reading and writing everything once; one row of 1024 x 1024 3 us.
 #include "ep_common.cuh"
 #include "rows.cuh"
 #include "tc_device.cuh"
@@ -202,7 +201,7 @@ __device__ __forceinline__ void load_residual(const Epilogue &e, int64_t row, in
 // order instead, addresses, bounds and types made 18 instructions per element, and the epilogue took longer than the
 // sums and the memory both: 169343 x 128 -> 512 in 137 us.)  Boxes have rows of 128 bytes where the tile allows: TMA
 // takes them row by row, and rows of 64 bytes cost as much.
-constexpr int SLOT_BYTES = 4096;   // a warp has two slots of this size
+constexpr int SLOT_BYTES = 4096;   // a warp's room in shared memory: one such chunk
 template <typename O, int COLS>
 struct ChunkStore {
     static constexpr int G = 16 / (int)sizeof(O);                                   // columns of a 16-byte piece
@@ -253,11 +252,10 @@ __device__ __forceinline__ void before_stores() {
     __syncwarp();
 }
 
-// Rows that TMA cannot write: a warp's 32 x 32 sums from shared memory (rows LOOSE floats apart), a column to each lane so
-// that neighbouring lanes write neighbouring elements.  What counts here is the number of instructions: the block has
-// two such warps a scheduler, and each takes about five clocks an instruction (with addresses and bounds worked out for
-// every row, 10000 x 65 fp32 took 5.5 us a chunk).
-constexpr int LOOSE = 33;
+// Rows that TMA cannot write: a warp's 32 x 32 sums from shared memory (element j of row r at 32 r + (j + r) % 32, which
+// keeps lanes in different banks both ways), a column to each lane so that neighbouring lanes write neighbouring elements.
+// What counts here is the number of instructions: each takes a warp about five clocks (with addresses and bounds worked
+// out for every row, 10000 x 65 fp32 took 5.5 us a chunk).
 template <typename O>
 struct LooseRows {
     O *out, *z;
@@ -270,51 +268,57 @@ struct LooseRows {
 };
 template <typename O>
 __device__ __noinline__ void finish_rows(LooseRows<O> w) {
+    const int lane = threadIdx.x & 31;
     const bool plain = !w.z && !w.residual && !w.x_scale && w.act == EP_ACT_NONE;
 #pragma unroll 1
-    for (int r0 = 0; r0 < w.rows; r0 += 8, w.out += 8ll * w.ldo, w.sums += 8 * LOOSE) {
-        float v[8], add[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) v[r] = w.sums[r * LOOSE];
+    for (int r0 = 0; r0 < w.rows; r0 += 8, w.sums += 8 * 32) {
         const bool whole = r0 + 8 <= w.rows;
-        if (!plain) {
+        float v[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) v[r] = w.sums[r * 32 + ((lane + r0 + r) & 31)];
+        if (plain) {
+#pragma unroll
+            for (int r = 0; r < 8; ++r) v[r] += w.bias;
+        } else {
+            float add[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) add[r] = 0.f;
+            if (w.residual) {
+#pragma unroll
+                for (int r = 0; r < 8; ++r, w.residual += w.ldr)
+                    if (whole || r0 + r < w.rows) add[r] = to_f32(*w.residual);
+            }
             if (w.x_scale) {
 #pragma unroll
-                for (int r = 0; r < 8; ++r) v[r] *= r0 + r < w.rows ? w.x_scale[r0 + r] * w.scale : 0.f;
+                for (int r = 0; r < 8; ++r)
+                    if (whole || r0 + r < w.rows) v[r] *= w.x_scale[r0 + r] * w.scale;
             }
 #pragma unroll
-            for (int r = 0; r < 8; ++r) add[r] = w.residual && r0 + r < w.rows ? to_f32(w.residual[r * w.ldr]) : 0.f;
-        }
-#pragma unroll
-        for (int r = 0; r < 8; ++r) v[r] += w.bias;
-        if (!plain) {
+            for (int r = 0; r < 8; ++r) v[r] += w.bias;
             if (w.z) {
 #pragma unroll
-                for (int r = 0; r < 8; ++r)
-                    if (r0 + r < w.rows) w.z[(int64_t)r * w.ldo] = from_f32<O>(v[r]);
-                w.z += 8ll * w.ldo;
+                for (int r = 0; r < 8; ++r, w.z += w.ldo)
+                    if (whole || r0 + r < w.rows) *w.z = from_f32<O>(v[r]);
             }
             activate(v, w.act);
 #pragma unroll
             for (int r = 0; r < 8; ++r) v[r] += add[r];
-            if (w.residual) w.residual += 8 * w.ldr;
         }
-        O *to = w.out;
         if (whole) {
 #pragma unroll
-            for (int r = 0; r < 8; ++r, to += w.ldo) *to = from_f32<O>(v[r]);
+            for (int r = 0; r < 8; ++r, w.out += w.ldo) *w.out = from_f32<O>(v[r]);
         } else {
 #pragma unroll
-            for (int r = 0; r < 8; ++r, to += w.ldo)
-                if (r0 + r < w.rows) *to = from_f32<O>(v[r]);
+            for (int r = 0; r < 8; ++r, w.out += w.ldo)
+                if (r0 + r < w.rows) *w.out = from_f32<O>(v[r]);
         }
     }
 }
 
 // ---------------------------------------------------------------------------------------------- the tile kernel
 //
-// 128 x BN outputs per tile, one block per SM that goes from tile to tile: warp 8 brings k-blocks (128 bytes along k)
-// by TMA into a ring, warp 9 issues the MMAs, warps 0-7 finish a tile while the next one is being summed (two
+// 128 x BN outputs per tile, one block per SM that goes from tile to tile: one warp brings k-blocks (128 bytes along k)
+// by TMA into a ring, the last one issues the MMAs, the others finish a tile while the next one is being summed (two
 // accumulators in TMEM).
 //
 // PARTS == 3: fp32 operands as three bf16 numbers each, x = x1 + x2 + x3 (|x2| < 2^-7 |x|, |x3| <= 2^-16 |x|).  Of the
@@ -329,9 +333,6 @@ __device__ __noinline__ void finish_rows(LooseRows<O> w) {
 // B in its shared memory and 128 rows of the sums in its TMEM; the first one's MMA warp issues for both.  A block then
 // loads half as much of B for the same product: a 128 x 256 tile alone needs 96 bytes a clock from the L2 at full rate.
 constexpr int BM = 128;               // rows of a block
-constexpr int EPI_WARPS = 8;
-constexpr int TMA_WARP = 8, MMA_WARP = 9;
-constexpr int GEMM_THREADS = 320;
 constexpr int A_BYTES = BM * 128;
 constexpr int RUN_KB = 4;
 constexpr int MAX_STAGES = 8;
@@ -344,13 +345,17 @@ struct GemmShared {
 };
 
 // The shared memory of a block: ring of operand stages, then per epilogue warp room for chunks on their way out.
+// The epilogue's instructions follow one another closely (sum, bias, activation, store), so it takes warps to fill a
+// scheduler: 16 where every one of them still has 32 columns (169343 x 128 -> 512 bf16: 41 us against 51 with 8, through
+// GELU and with a residual 95 against 137).
 template <int BN, int PARTS, bool PAIR>
 struct TileMemory {
+    static constexpr int EPI_WARPS = BN >= 128 ? 16 : 8;
+    static constexpr int THREADS = 32 * (EPI_WARPS + 2);
     static constexpr int B_ROWS = PAIR ? BN / 2 : BN;
     static constexpr int B_BYTES = B_ROWS * 128;
     static constexpr int STAGE_BYTES = PARTS * (A_BYTES + B_BYTES);
-    static constexpr int WARP_STAGING = 2 * SLOT_BYTES;
-    static constexpr int STAGING_BYTES = EPI_WARPS * WARP_STAGING;
+    static constexpr int STAGING_BYTES = EPI_WARPS * SLOT_BYTES;
     static constexpr int REST = 1024 + STAGING_BYTES + (int)sizeof(GemmShared);
     static constexpr int FIT = (227 * 1024 - REST) / STAGE_BYTES;
     static constexpr int STAGES = FIT < MAX_STAGES ? FIT : MAX_STAGES;
@@ -489,13 +494,14 @@ struct Items {
 };
 
 template <int BN, bool F8, int PARTS, bool RUNS, bool PAIR, typename O>
-__global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_constant__ CUtensorMap map_a,
+__global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linear_tiles(const __grid_constant__ CUtensorMap map_a,
                                                                 const __grid_constant__ CUtensorMap map_b,
                                                                 const __grid_constant__ CUtensorMap map_out,
                                                                 const __grid_constant__ CUtensorMap map_z,
                                                                 const GemmShape g, const Epilogue e, int *status) {
     using Mem = TileMemory<BN, PARTS, PAIR>;
     constexpr int B_BYTES = Mem::B_BYTES, STAGE_BYTES = Mem::STAGE_BYTES, STAGES = Mem::STAGES;
+    constexpr int EPI_WARPS = Mem::EPI_WARPS, TMA_WARP = EPI_WARPS;
     constexpr int ACC_COLS = BN * (PARTS == 3 ? 2 : 1);
     constexpr int KE = F8 ? 128 : 64;   // elements of k in a k-block
     constexpr int TILE_M = PAIR ? 2 * BM : BM;
@@ -591,7 +597,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
 #pragma unroll 1
             for (uint32_t j = it > (uint32_t)STAGES ? it - (uint32_t)STAGES : 0u; j < it; ++j)
                 mbar_wait_quiet(&sh->full[j % (uint32_t)STAGES], (j / (uint32_t)STAGES) & 1u, DRAIN_LIMIT_CLOCKS);
-    } else if (warp == MMA_WARP) {
+    } else if (warp == TMA_WARP + 1) {
         uint32_t acc = 0, s = 0, ph = 0;
         bool ok = true;
         const uint32_t ring_base = smem_u32(ring);
@@ -634,9 +640,12 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
             if (lane == 0) mbar_wait_quiet(&sh->drain, 0u, DRAIN_LIMIT_CLOCKS);
         }
     } else {
-        const int quad = warp & 3, half = warp >> 2;   // TMEM lanes 32 quad.. and the columns' half are this warp's
-        constexpr int COLS = BN / 2;
-        char *slots = staging + warp * Mem::WARP_STAGING;
+        const int quad = warp & 3, piece = warp >> 2;   // TMEM lanes 32 quad.. and a piece of the columns are this warp's
+        constexpr int COLS = BN * 4 / EPI_WARPS;
+        using C = ChunkStore<O, COLS>;
+        constexpr int SUBS = COLS / 32;
+        static_assert(C::WIDTH == COLS, "a warp's columns leave as one box");
+        char *slot = staging + warp * SLOT_BYTES;
         const int m_off = (int)rank * BM + quad * 32;   // this warp's rows in the tile
         const uint32_t t_empty = PAIR ? in_block(smem_u32(&sh->t_empty[0]), 0) : smem_u32(&sh->t_empty[0]);
         auto give_back = [&](uint32_t buf) {   // the accumulator, once every column of it is in registers
@@ -651,13 +660,9 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
         };
         uint32_t acc = 0;
         bool ok = true;
-        using C = ChunkStore<O, COLS>;
-        constexpr int SUBS = C::WIDTH / 32;            // a chunk is one or two times 32 columns
-        constexpr int CHUNKS = COLS / C::WIDTH;
         const bool by_tma = e.tma && !e.share, with_z = e.preact != nullptr;
-        // The residual's chunk is copied ahead into the slot that the chunk will leave from, and added in place.  z takes
-        // the other slot; without z the two take turns.
-        auto fetch_residual = [&](int64_t row0, int col, char *slot) {
+        // The residual is copied into the slot that the result will leave from, and added in place.
+        auto fetch_residual = [&](int64_t row0, int col) {
             constexpr int PER_ROW = C::WIDTH / C::G;
             const int c = lane % PER_ROW;
 #pragma unroll
@@ -668,89 +673,149 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
             }
             copies_end_group();
         };
-        // Bias and scale of a chunk's columns, one per lane, fetched before the sums are waited for.
-        struct Lane {
+        for (Walk t(g, worker); ok && t.more(); t.next()) {
+            const int col = t.n0() + piece * COLS;
+            const int64_t row0 = (int64_t)t.m0() + m_off;   // (below 2^31 where there are rows)
+            const bool mine = row0 < e.M && col < e.N;
+            // while the sums are on their way: the residual, and bias and scale of this warp's columns, one to a lane
+            if (by_tma && e.residual && !with_z && mine) {
+                stores_read<0>();
+                fetch_residual(row0, col);
+            }
             float bias[SUBS], scale[SUBS];
-        };
-        auto fetch_lane = [&](int col) {
-            Lane p;
 #pragma unroll
             for (int q = 0; q < SUBS; ++q) {
                 const int c = col + q * 32 + lane;
-                p.bias[q] = by_tma && e.bias && c < e.N ? load_param(e.bias, e.bias_type, c) : 0.f;
-                p.scale[q] = by_tma && e.w_scale && c < e.N ? __ldg(e.w_scale + c) : 1.f;
+                bias[q] = by_tma && e.bias && c < e.N ? load_param(e.bias, e.bias_type, c) : 0.f;
+                scale[q] = by_tma && e.w_scale && c < e.N ? __ldg(e.w_scale + c) : 1.f;
             }
-            return p;
-        };
-        int turn = 0;   // slot of the next chunk
-        // One lane's finished sums from column col on.  next: the column of the chunk after this one in the tile, or -1.
-        auto finish_chunk = [&](int split, int64_t row0, int col, int next, const Lane &p, float (&v)[SUBS][32]) {
-            const int64_t row = row0 + lane;
-            if (row0 >= e.M || col >= e.N) return;
-            if (e.share) {
+            // The sums, 32 columns at a time: in runs they are in registers, otherwise they are read from TMEM where they are
+            // needed (twice where z is stored too: cheaper than keeping them).
+            float run[RUNS ? 32 : 1];
+            uint32_t buf = 0, taddr = 0;
+            if constexpr (RUNS) {
+                static_assert(SUBS == 1, "sums in runs are of fp32 outputs");
+                const int kbn = t.kbn();
 #pragma unroll
-                for (int q = 0; q < SUBS; ++q) {
-                    if (col + q * 32 >= e.N) break;
-                    stores_read<1>();
-                    ChunkStore<float, 32>::write(slots + turn * SLOT_BYTES, lane, 0, v[q]);
-                    before_stores();
-                    tma_store_3d_elected(&map_out, slots + turn * SLOT_BYTES, col + q * 32, (int)row0, split);
-                    turn ^= 1;
-                }
-            } else if (by_tma) {
-                char *out_slot = slots + (with_z ? SLOT_BYTES : turn * SLOT_BYTES);
-                if (e.residual) {
-                    copies_wait<0>();
-                    if (with_z)
-                        stores_read<0>();   // (out_slot's own store was waited for before the copy)
-                    else {
-                        if (next >= 0 && next < e.N) {
-                            stores_read<0>();
-                            fetch_residual(row0, next, slots + (turn ^ 1) * SLOT_BYTES);
-                        } else
-                            __syncwarp();
+                for (int j = 0; j < 32; ++j) run[j] = 0.f;
+                for (int kb = 0; kb < kbn; kb += RUN_KB, ++acc) {
+                    buf = acc & 1u;
+                    if (!(ok = mbar_wait(&sh->t_full[buf], (acc >> 1) & 1u, abort_flag))) break;
+                    tc_fence_after();
+                    taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + buf * ACC_COLS + piece * COLS;
+                    uint32_t a[32];
+                    tmem_ld32_issue(taddr, a);
+                    tmem_ld_wait(a);
+                    if constexpr (PARTS == 3) {
+                        uint32_t w[32];
+                        tmem_ld32_issue(taddr + BN, w);
+                        tmem_ld_wait(w);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) run[j] += __uint_as_float(a[j]) + __uint_as_float(w[j]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) run[j] += __uint_as_float(a[j]);
                     }
-                } else if (with_z)
-                    stores_read<0>();
-                else
-                    stores_read<1>();
-                const float xs = e.x_scale && row < e.M ? __ldg(e.x_scale + row) : 0.f;
+                    give_back(buf);
+                }
+                if (!ok) break;
+            } else {
+                buf = acc & 1u;
+                if (!(ok = mbar_wait(&sh->t_full[buf], (acc >> 1) & 1u, abort_flag))) break;
+                ++acc;
+                tc_fence_after();
+                taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + buf * ACC_COLS + piece * COLS;
+            }
+            auto sums = [&](int q, float(&v)[32]) {
+                if constexpr (RUNS) {
 #pragma unroll
-                for (int q = 0; q < SUBS; ++q) {
+                    for (int j = 0; j < 32; ++j) v[j] = run[j];
+                } else {
+                    uint32_t a[32];
+                    tmem_ld32_issue(taddr + q * 32, a);
+                    tmem_ld_wait(a);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(a[j]);
+                }
+            };
+            auto all_read = [&] {
+                if constexpr (!RUNS) give_back(buf);
+            };
+            if (!mine) {
+                all_read();
+                continue;
+            }
+            if (e.share) {
+#pragma unroll 1
+                for (int q = 0; q < SUBS && col + q * 32 < e.N; ++q) {
+                    float v[32];
+                    sums(q, v);
+                    stores_read<0>();
+                    ChunkStore<float, 32>::write(slot, lane, 0, v);
+                    before_stores();
+                    tma_store_3d_elected(&map_out, slot, col + q * 32, (int)row0, t.split);
+                }
+                all_read();
+            } else if (by_tma) {
+                const float xs = e.x_scale && row0 + lane < e.M ? __ldg(e.x_scale + row0 + lane) : 0.f;
+                auto biased = [&](int q, float(&v)[32]) {
+                    sums(q, v);
+                    const float s = SUBS > 1 && q == 1 ? scale[SUBS - 1] : scale[0], b = SUBS > 1 && q == 1 ? bias[SUBS - 1] : bias[0];
                     if (e.x_scale) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[q][j] *= xs * __shfl_sync(FULL, p.scale[q], j);
+                        for (int j = 0; j < 32; ++j) v[j] *= xs * __shfl_sync(FULL, s, j);
                     }
                     if (e.bias) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[q][j] += __shfl_sync(FULL, p.bias[q], j);
+                        for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(FULL, b, j);
                     }
-                    if (with_z) C::write(slots, lane, q * (32 / C::G), v[q]);
-                    activate(v[q], e.act);
-                    if (e.residual) C::add(out_slot, lane, q * (32 / C::G), v[q]);
-                    C::write(out_slot, lane, q * (32 / C::G), v[q]);
-                }
-                before_stores();
-                if (with_z) tma_store_3d_elected(&map_z, slots, col, (int)row0, 0);
-                tma_store_3d_elected(&map_out, out_slot, col, (int)row0, 0);
-                if (with_z) {
-                    if (e.residual && next >= 0 && next < e.N) {
+                };
+                if (with_z) {   // z leaves first, from the same slot
+                    stores_read<0>();
+#pragma unroll 1
+                    for (int q = 0; q < SUBS; ++q) {
+                        float v[32];
+                        biased(q, v);
+                        C::write(slot, lane, q * (32 / C::G), v);
+                    }
+                    before_stores();
+                    tma_store_3d_elected(&map_z, slot, col, (int)row0, 0);
+                    if (e.residual) {
                         stores_read<0>();
-                        fetch_residual(row0, next, out_slot);
+                        fetch_residual(row0, col);
                     }
-                } else
-                    turn ^= 1;
+                }
+#pragma unroll 1
+                for (int q = 0; q < SUBS; ++q) {
+                    float v[32];
+                    biased(q, v);
+                    activate(v, e.act);
+                    if (q == 0) {   // only now does the slot have to be free, or the residual there
+                        if (e.residual) {
+                            copies_wait<0>();
+                            __syncwarp();
+                        } else
+                            stores_read<0>();
+                    }
+                    if (e.residual) C::add(slot, lane, q * (32 / C::G), v);
+                    C::write(slot, lane, q * (32 / C::G), v);
+                }
+                all_read();
+                before_stores();
+                tma_store_3d_elected(&map_out, slot, col, (int)row0, 0);
             } else {
-                float *mine = reinterpret_cast<float *>(slots);
-#pragma unroll
+                float *loose = reinterpret_cast<float *>(slot);
+#pragma unroll 1
                 for (int q = 0; q < SUBS; ++q) {
                     const int at = col + q * 32;
+                    float v[32];
+                    sums(q, v);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) mine[lane * LOOSE + j] = v[q][j];
+                    for (int j = 0; j < 32; ++j) loose[lane * 32 + ((j + lane) & 31)] = v[j];
                     __syncwarp();
                     if (at + lane < e.N) {
                         LooseRows<O> w{static_cast<O *>(e.out) + row0 * e.N + at + lane, nullptr, nullptr, nullptr, e.ldr, e.N,
-                                       (int)min(e.M - row0, (int64_t)32), e.act, 0.f, 1.f, mine + lane};
+                                       (int)min(e.M - row0, (int64_t)32), e.act, 0.f, 1.f, loose};
                         if (e.preact) w.z = static_cast<O *>(e.preact) + row0 * e.N + at + lane;
                         if (e.residual) w.residual = static_cast<const O *>(e.residual) + row0 * e.ldr + at + lane;
                         if (e.bias) w.bias = load_param(e.bias, e.bias_type, at + lane);
@@ -762,79 +827,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) linear_tiles(const __grid_con
                     }
                     __syncwarp();
                 }
-            }
-        };
-        for (Walk t(g, worker); ok && t.more(); t.next()) {
-            const int col0 = t.n0() + half * COLS;
-            const int64_t row0 = (int64_t)t.m0() + m_off;   // (below 2^31 where there are rows)
-            auto next_of = [&](int c) { return c + 1 < CHUNKS ? col0 + (c + 1) * C::WIDTH : -1; };
-            if (by_tma && e.residual && col0 < e.N && row0 < e.M) {   // while the sums are on their way
-                stores_read<0>();
-                fetch_residual(row0, col0, slots + (with_z ? SLOT_BYTES : turn * SLOT_BYTES));
-            }
-            Lane lanes[CHUNKS];
-#pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) lanes[c] = fetch_lane(col0 + c * C::WIDTH);
-            if constexpr (RUNS) {
-                const int kbn = t.kbn();
-                static_assert(SUBS == 1, "sums in runs are of fp32 outputs");
-                float sum[CHUNKS][1][32];
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) sum[c][0][j] = 0.f;
-                for (int kb = 0; kb < kbn; kb += RUN_KB, ++acc) {
-                    const uint32_t buf = acc & 1u, use = (acc >> 1) & 1u;
-                    if (!(ok = mbar_wait(&sh->t_full[buf], use, abort_flag))) break;
-                    tc_fence_after();
-                    const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + buf * ACC_COLS + half * COLS;
-#pragma unroll
-                    for (int c = 0; c < CHUNKS; ++c) {
-                        uint32_t v[32];
-                        tmem_ld32_issue(taddr + c * 32, v);
-                        if constexpr (PARTS == 3) {
-                            uint32_t w[32];
-                            tmem_ld32_issue(taddr + BN + c * 32, w);
-                            tmem_ld_wait(v);
-                            tmem_ld_wait(w);
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) sum[c][0][j] += __uint_as_float(v[j]) + __uint_as_float(w[j]);
-                        } else {
-                            tmem_ld_wait(v);
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) sum[c][0][j] += __uint_as_float(v[j]);
-                        }
-                    }
-                    give_back(buf);
-                }
-                if (!ok) break;
-#pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) finish_chunk(t.split, row0, col0 + c * 32, next_of(c), lanes[c], sum[c]);
-            } else {
-                const uint32_t buf = acc & 1u, use = (acc >> 1) & 1u;
-                ++acc;
-                if (!(ok = mbar_wait(&sh->t_full[buf], use, abort_flag))) break;
-                tc_fence_after();
-                const uint32_t taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + buf * ACC_COLS + half * COLS;
-#pragma unroll 1
-                for (int c = 0; c < CHUNKS; ++c) {
-                    Lane now = lanes[0];
-#pragma unroll
-                    for (int q = 1; q < CHUNKS; ++q)
-                        if (q == c) now = lanes[q];
-                    uint32_t v[SUBS][32];
-#pragma unroll
-                    for (int q = 0; q < SUBS; ++q) tmem_ld32_issue(taddr + c * C::WIDTH + q * 32, v[q]);
-#pragma unroll
-                    for (int q = 0; q < SUBS; ++q) tmem_ld_wait(v[q]);
-                    if (c == CHUNKS - 1) give_back(buf);
-                    float f[SUBS][32];
-#pragma unroll
-                    for (int q = 0; q < SUBS; ++q)
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) f[q][j] = __uint_as_float(v[q][j]);
-                    finish_chunk(t.split, row0, col0 + c * C::WIDTH, next_of(c), now, f);
-                }
+                all_read();
             }
         }
         copies_wait<0>();
@@ -1220,7 +1213,7 @@ bool encode_result(CUtensorMap *map, void *base, int type, int64_t depth, int64_
     const cuuint64_t size = (cuuint64_t)ep::type_size(type);
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)depth};
     const cuuint64_t strides[2] = {(cuuint64_t)ld * size, (cuuint64_t)(ld * rows) * size};
-    const cuuint32_t width = (cuuint32_t)std::min<int64_t>(128 / (int64_t)size, bn / 2);
+    const cuuint32_t width = (cuuint32_t)std::min<int64_t>(128 / (int64_t)size, bn == 256 ? 64 : 32);
     const cuuint32_t box[3] = {width, 32, 1};
     const cuuint32_t estr[3] = {1, 1, 1};
     const CUtensorMapDataType t = type == EP_BF16  ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
@@ -1295,7 +1288,7 @@ int launch_tiles(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &
     EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(PAIR ? 2 * p.workers : p.workers));
-    cfg.blockDim = dim3(GEMM_THREADS);
+    cfg.blockDim = dim3(TileMemory<BN, PARTS, PAIR>::THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attrs[2] = {};

@@ -36,36 +36,21 @@ __device__ __forceinline__ uint32_t ordered(float v) {
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 
-// The best pair over the L threads of a row.  L > 32: the whole block, by shared memory (2 x 8 pairs used in turn).
+// The best pair over L neighbouring lanes.
 template <int L>
-__device__ __forceinline__ void best_of_row(float &v, int &c, float *slot_v, int *slot_c, int &turn) {
+__device__ __forceinline__ void best_of_lanes(float &v, int &c) {
     if constexpr (L == 32) {
         const uint32_t key = ordered(v), top = __reduce_max_sync(FULL, key);
         c = (int)__reduce_min_sync(FULL, key == top ? (uint32_t)c : 0x7fffffffu);
         const uint32_t b = top ^ (top & 0x80000000u ? 0x80000000u : 0xffffffffu);
         v = __uint_as_float(b);
     } else {
-        constexpr int W = L < 32 ? L : 32;
 #pragma unroll
-        for (int o = W / 2; o >= 1; o >>= 1) {
+        for (int o = L / 2; o >= 1; o >>= 1) {
             const float ov = __shfl_xor_sync(FULL, v, o);
             const int oc = __shfl_xor_sync(FULL, c, o);
             keep_better(v, c, ov, oc);
         }
-    }
-    if constexpr (L > 32) {
-        float *sv = slot_v + turn * 8;
-        int *sc = slot_c + turn * 8;
-        turn ^= 1;
-        if ((threadIdx.x & 31) == 0) {
-            sv[threadIdx.x >> 5] = v;
-            sc[threadIdx.x >> 5] = c;
-        }
-        __syncthreads();
-        v = sv[0];
-        c = sc[0];
-#pragma unroll
-        for (int w = 1; w < L / 32; ++w) keep_better(v, c, sv[w], sc[w]);
     }
 }
 
@@ -124,12 +109,13 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) route_rows(const T *__
     constexpr int L = Lay::L, V = Lay::V, N = Lay::N, WIDE = Lay::WIDE;
     constexpr int GROUPS = THREADS / L;
     __shared__ float slots[L > 32 ? 64 : 1];
-    __shared__ float slot_v[L > 32 ? 16 : 1];
-    __shared__ int slot_c[L > 32 ? 16 : 1];
+    constexpr int WARPS = THREADS / 32;
+    __shared__ float warp_v[L > 32 ? 2 * WARPS : 1];   // rows that a whole block shares: each warp's best, two slots in turn
+    __shared__ int warp_c[L > 32 ? 2 * WARPS : 1];
     __shared__ double red[8];
     extern __shared__ uint4 ring[];   // rows on their way, later the fold of the sums; then counts
     int *hist = reinterpret_cast<int *>(reinterpret_cast<char *>(ring) + hist_at);   // of [parts + 1] (the last: rows that take part)
-    int turn = 0, turn_best = 0;
+    int turn = 0;
     const int lane = threadIdx.x % L, group = threadIdx.x / L;
     ep_let_next_launch_start();
     if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;   // of route_fold, which goes on after this kernel
@@ -163,28 +149,51 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) route_rows(const T *__
         // the k largest, one after the other, while the logits are still there: each thread offers the best of its columns
         // that is not taken (the first is the lowest column that holds the maximum just found)
         uint32_t taken = 0;
+        auto best_left = [&](float &v, int &c) {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (l[j][i] > v && !(taken >> (j * N + i) & 1)) {
+                        v = l[j][i];
+                        c = Lay::col(lane, j, i);
+                    }
+        };
         float chosen = 0.f, mine_exp = 0.f;   // the sum of the slots' exponentials, and that of this thread's first slot
+        // a wide row's threads keep the best that each of them has left: only the warp whose own was taken looks again
+        float best_v = -INFINITY;
+        int best_c = MAX_PARTS;
+        if constexpr (L > 32) best_left(best_v, best_c);
         for (int r = 0; r < k; ++r) {
             float v = r == 0 ? top : -INFINITY;
             int c = MAX_PARTS;
-            if (r == 0) {
+            if constexpr (L > 32) {
+                v = best_v;
+                c = best_c;
+                best_of_lanes<32>(v, c);
+                float *sv = warp_v + (r & 1) * WARPS;
+                int *sc = warp_c + (r & 1) * WARPS;
+                if ((threadIdx.x & 31) == 0) {
+                    sv[threadIdx.x >> 5] = v;
+                    sc[threadIdx.x >> 5] = c;
+                }
+                __syncthreads();
+                v = sv[0];
+                c = sc[0];
+#pragma unroll
+                for (int w = 1; w < WARPS; ++w) keep_better(v, c, sv[w], sc[w]);
+            } else if (r == 0) {
 #pragma unroll
                 for (int j = V - 1; j >= 0; --j)
 #pragma unroll
                     for (int i = N - 1; i >= 0; --i)
                         if (l[j][i] == top) c = Lay::col(lane, j, i);
                 if (c == MAX_PARTS) v = -INFINITY;
+                best_of_lanes<L>(v, c);
             } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-#pragma unroll
-                    for (int i = 0; i < N; ++i)
-                        if (l[j][i] > v && !(taken >> (j * N + i) & 1)) {
-                            v = l[j][i];
-                            c = Lay::col(lane, j, i);
-                        }
+                best_left(v, c);
+                best_of_lanes<L>(v, c);
             }
-            best_of_row<L>(v, c, slot_v, slot_c, turn_best);
             const bool got = v > -INFINITY;
             const float ex = got ? exp_fast(v - top) : 0.f;
             chosen += ex;
@@ -196,12 +205,13 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) route_rows(const T *__
                 if (r < L) mine_exp = ex;
                 if (got) atomicAdd(&hist[c], 1);
             }
-            if (r + 1 < k) {
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-#pragma unroll
-                    for (int i = 0; i < N; ++i)
-                        if (Lay::col(lane, j, i) == c) taken |= 1u << (j * N + i);
+            if (got && r + 1 < k && Lay::owner(c) == lane) {
+                taken |= 1u << Lay::index(c);
+                if constexpr (L > 32) {
+                    best_v = -INFINITY;
+                    best_c = MAX_PARTS;
+                    best_left(best_v, best_c);
+                }
             }
         }
         static_assert(V * N <= 32, "a bit of `taken` for every column of a thread");

@@ -233,6 +233,10 @@ struct Layout {
     static __device__ __forceinline__ int col(int lane, int j, int i) {
         return VEC ? (j * L + lane) * N + i : (j * N + i) * L + lane;
     }
+    // The thread that holds column c, and the column's place j * N + i there (any c; a place past the thread's own for
+    // columns past the layout).
+    static __device__ __forceinline__ int owner(int c) { return VEC ? c / N % L : c % L; }
+    static __device__ __forceinline__ int index(int c) { return VEC ? c / N / L * N + c % N : c / L; }
     static __device__ __forceinline__ bool inside(int lane, int j, int i, int width) {
         return (VEC ? (j + 1) * L * N : (j * N + i + 1) * L) <= LOW_ || col(lane, j, i) < width;
     }
