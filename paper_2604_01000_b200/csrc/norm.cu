@@ -103,13 +103,18 @@ __global__ void __launch_bounds__(block_threads<Lay::L>()) norm_rows(const T *x,
 #pragma unroll
                 for (int i = 0; i < N; ++i) top = OpMax::apply(top, fabsf(h[j][i]));
             const float s = reduce_row<L, OpMax>(top, slots, turn) / E4M3_TOP;
-            // a scale below the smallest normal number has no finite reciprocal worth multiplying by: divide there
-            const bool tiny = s < 1.17549435e-38f;
-            const float inverse = s > 0.f || s != s ? 1.f / s : 0.f;
+            if (s > 0.f && s < 1.17549435e-38f) {   // no finite reciprocal worth multiplying by: divide
 #pragma unroll
-            for (int j = 0; j < V; ++j)
+                for (int j = 0; j < V; ++j)
 #pragma unroll
-                for (int i = 0; i < N; ++i) h[j][i] = tiny && s > 0.f ? h[j][i] / s : h[j][i] * inverse;
+                    for (int i = 0; i < N; ++i) h[j][i] = h[j][i] / s;
+            } else {
+                const float inverse = s == 0.f ? 0.f : 1.f / s;
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) h[j][i] *= inverse;
+            }
             if (lane == 0 && mine) scale[row] = s;
         }
         if (mine) Lay::store(out + at, lane, d, h);

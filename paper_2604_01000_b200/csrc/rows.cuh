@@ -79,6 +79,11 @@ __device__ __forceinline__ e4m3 from_f32<e4m3>(float v) {
     return r;
 }
 
+// Two floats to two e4m3 (a in the low byte).
+__device__ __forceinline__ uint16_t to_e4m3_pair(float a, float b) {
+    return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+}
+
 // One vector parameter (a norm's weight, a product's bias) of type EP_F32, EP_BF16 or EP_F16.
 __device__ __forceinline__ float load_param(const void *p, int type, int64_t i) {
     if (type == EP_F32) return __ldg(static_cast<const float *>(p) + i);
@@ -134,8 +139,13 @@ __device__ __forceinline__ void store_chunk(T *row, int col, int width, bool vec
             constexpr int B = N * (int)sizeof(T);
             using R = typename Raw<B>::type;
             constexpr int PIECES = B > 16 ? B / 16 : 1;
+            if constexpr (sizeof(T) == 1 && N % 2 == 0) {   // (8 bits are converted two at a time)
 #pragma unroll
-            for (int i = 0; i < N; ++i) e[i] = from_f32<T>(v[i]);
+                for (int i = 0; i < N; i += 2) reinterpret_cast<uint16_t *>(e)[i / 2] = to_e4m3_pair(v[i], v[i + 1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) e[i] = from_f32<T>(v[i]);
+            }
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) reinterpret_cast<R *>(row + col)[i] = reinterpret_cast<const R *>(e)[i];
         }
@@ -195,7 +205,11 @@ struct OpSum {
     static constexpr float none = 0.f;
 };
 struct OpMax {   // NaN if either is: a row that holds one has no largest magnitude to scale by
-    static __device__ __forceinline__ float apply(float a, float b) { return (a > b || a != a) ? a : b; }
+    static __device__ __forceinline__ float apply(float a, float b) {
+        float r;
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+        return r;
+    }
     static constexpr float none = -INFINITY;
 };
 struct OpMaxNumber {   // NaN only if both are
@@ -266,6 +280,13 @@ struct Layout {
     static __device__ __forceinline__ void store_part(T *row, int lane, int j, int width, const float (&v)[N_]) {
         if constexpr (VEC) {
             if (inside(lane, j, 0, width)) store_chunk(row, col(lane, j, 0), 1 << 30, true, v);
+        } else if constexpr (sizeof(T) == 1) {
+#pragma unroll
+            for (int i = 0; i < N; i += 2) {
+                const uint16_t two = to_e4m3_pair(v[i], v[i + 1]);
+                if (inside(lane, j, i, width)) row[col(lane, j, i)].bits = (uint8_t)two;
+                if (inside(lane, j, i + 1, width)) row[col(lane, j, i + 1)].bits = (uint8_t)(two >> 8);
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i)
@@ -459,12 +480,15 @@ int with_layout(int width, bool vec, F f) {
     if (width <= 4) return f.template run<Layout<1, 1, 4, false, 0>>();
     if (width <= 16) return f.template run<Layout<2, 2, 4, false, 4>>();
     if (width <= 32) return f.template run<Layout<4, 2, 4, false, 16>>();
-    if (width <= 64) return f.template run<Layout<8, 2, 4, false, 32>>();
-    if (width <= 128) return f.template run<Layout<8, 4, 4, false, 64>>();
+    if (width <= 48) return f.template run<Layout<4, 3, 4, false, 32>>();
+    if (width <= 64) return f.template run<Layout<8, 2, 4, false, 48>>();
+    if (width <= 96) return f.template run<Layout<8, 3, 4, false, 64>>();
+    if (width <= 128) return f.template run<Layout<8, 4, 4, false, 96>>();
     if (width <= 192) return f.template run<Layout<16, 3, 4, false, 128>>();
     if (width <= 256) return f.template run<Layout<16, 4, 4, false, 192>>();
     if (width <= 320) return f.template run<Layout<16, 5, 4, false, 256>>();
-    if (width <= 512) return f.template run<Layout<32, 4, 4, false, 320>>();
+    if (width <= 384) return f.template run<Layout<32, 3, 4, false, 320>>();
+    if (width <= 512) return f.template run<Layout<32, 4, 4, false, 384>>();
     if (width <= 768) return f.template run<Layout<32, 6, 4, false, 512>>();
     if (width <= 1024) return f.template run<Layout<32, 8, 4, false, 768>>();
     if (width <= 2048) return f.template run<Layout<256, 2, 4, false, 1024>>();
