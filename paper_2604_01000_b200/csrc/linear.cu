@@ -10,9 +10,9 @@
 // copies unaligned operands or splits fp32 ones into three bf16 numbers, and one that joins the shares of a sum over k
 // that was split between blocks.
 //
-// Measured: 8192 x 4096 x 4096 fp16 195 us, 1410 TFLOP/s (tensor pipe 90 % busy; cuBLAS alone reaches 1669 in short bursts);
+// Measured: 8192 x 4096 x 4096 fp16 193 us, 1430 TFLOP/s (tensor pipe 90 % busy; cuBLAS alone reaches 1669 in short bursts);
 // 2000 x 4096 x 4096 in 8 bits 31 us, 2150 TFLOP/s (1.7 waves of tiles, so 2); 169343 x 128 -> 512 bf16 41 us, 5.3 TB/s of
-// 6.5, with z kept 75 us, 5.2 TB/s; backward of 232965 x 256 x 256 bf16 through GELU 153 us: dz 60, dx 44, dW 46 and its
+// 6.5, with z kept 76 us, 5.2 TB/s; backward of 232965 x 256 x 256 bf16 through GELU 152 us: dz 60, dx 44, dW 46 and its
 // join 7, against 74 us for reading and writing everything once; one row of 1024 x 1024 3 us.
 #include "ep_common.cuh"
 #include "rows.cuh"
@@ -831,7 +831,8 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
             }
         }
         copies_wait<0>();
-        stores_read<0>();   // before the block gives its shared memory back
+        // what has been stored is written before the block ends: the launch that follows may already be waiting for it
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncthreads();
     if constexpr (PAIR) cluster_meet();   // neither block leaves while the other may still signal it

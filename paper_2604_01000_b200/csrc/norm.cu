@@ -5,7 +5,7 @@
 // memory), between the sum that gives its scale and the product with it, so every input is read once and every output
 // written once.  All of these kernels are bound by HBM bandwidth for many rows and by launch latency for few.  Measured
 // (of 6464 GB/s, a plain copy): 169343 x 128 fp32 with residual to bf16 50 us, 6.1 TB/s; backward of 2449029 x 128 bf16
-// 422 us, 5.9 TB/s; one row of 1024 to 8 bits 4 us.
+// 425 us, 5.9 TB/s; one row of 1024 to 8 bits 4 us.
 #include "ep_common.cuh"
 #include "rows.cuh"
 
