@@ -417,7 +417,7 @@ int ep_rms_norm_backward(ep_ctx *ctx, const void *dout, int32_t dout_type, const
  *
  *   x        [dev] rows x n_in of in_type, row i at element i * ldx (ldx >= n_in; ldw, ldr alike)
  *   w        [dev] n_out x n_in of in_type, rows ldw apart
- *   in_type  EP_F32, EP_BF16, EP_F16, EP_E4M3;  1 <= n_in, n_out <= 65536
+ *   in_type  EP_F32, EP_BF16, EP_F16, EP_E4M3;  1 <= n_in, n_out <= 65536;  0 <= rows <= 2^31 - 256
  *   x_scale  [dev] rows fp32, w_scale [dev] n_out fp32: both with EP_E4M3 (see ep_quantize_rows), else NULL
  *   bias     [dev] n_out of bias_type (EP_F32 / EP_BF16 / EP_F16) or NULL;  act  EP_ACT_*
  *   residual [dev] rows x n_out of out_type, rows ldr apart, or NULL

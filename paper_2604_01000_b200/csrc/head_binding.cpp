@@ -70,6 +70,7 @@ struct Device {
     void *stream() const { return c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)index).stream(); }
     Tensor empty(at::IntArrayRef size, ScalarType t) const { return at::detail::empty_cuda(size, t, device, std::nullopt); }
 
+    static constexpr int64_t most = INT32_MAX;
     void on(const Tensor &t, const char *name) const {
         if (!t.defined() || !t.is_cuda() || t.get_device() != index)
             refuse(std::string(name) + " must be a CUDA tensor on cuda:" + std::to_string(index));
@@ -80,6 +81,7 @@ struct Device {
         if (t.dim() != 2 || (rows >= 0 && t.size(0) != rows) || (cols >= 0 && t.size(1) != cols))
             refuse(std::string(name) + " must have shape (" + (rows >= 0 ? std::to_string(rows) : "rows") + ", " +
                    (cols >= 0 ? std::to_string(cols) : "columns") + "), not " + shape_of(t));
+        if (t.size(1) > most) refuse(std::string(name) + " is too wide");   // (the C ABI counts columns in 32 bits)
         if (t.is_contiguous()) return;
         if (!strided) refuse(std::string(name) + " must be contiguous");
         if (t.numel() && ((t.stride(1) != 1 && t.size(1) > 1) || (t.size(0) > 1 && t.stride(0) < t.size(1))))
@@ -188,6 +190,7 @@ std::tuple<Tensor, Maybe> linear(int64_t ctx, int index, const Tensor &x, const 
     d.matrix(weight, "weight", -1, n_in, true);
     need(weight.scalar_type() == t, "weight must have x's dtype");
     const int64_t n_out = weight.size(0);
+    need(n_out <= Device::most, "weight has too many rows");
     const int a = activation(act);
     const bool eight = t == at::kFloat8_e4m3fn;
     const ScalarType o = out_dtype.value_or(eight ? at::kBFloat16 : t);
@@ -223,6 +226,7 @@ std::tuple<Maybe, Maybe, Maybe> linear_backward(int64_t ctx, int index, const Te
     d.matrix(weight, "weight", -1, n_in, true);
     need(weight.scalar_type() == t, "weight must have x's dtype");
     const int64_t n_out = weight.size(0);
+    need(n_out <= Device::most, "weight has too many rows");
     const int a = activation(act);
     d.matrix(dout, "dout", rows, n_out);
     need(dout.scalar_type() == t || dout.scalar_type() == at::kFloat, "dout must have x's dtype or float32");
