@@ -560,7 +560,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
             const int m = t.m0() + (int)rank * BM, n = t.n0() + (int)rank * (t.columns() / 2);   // this block's rows of A and of B
             const int kbn = t.kbn();
             for (int kb = 0; kb < kbn; ++kb, ++it) {
-                if (!(ok = __all_sync(FULL, mbar_wait(&sh->empty[s], ph ^ 1u, abort_flag)))) break;
+                if (!(ok = mbar_wait_warp(&sh->empty[s], ph ^ 1u, abort_flag))) break;
                 if (rank == 0) mbar_expect_tx_elected(&sh->full[s], (PAIR ? 2 : 1) * STAGE_BYTES);
                 const uint32_t bar = PAIR ? in_block(smem_u32(&sh->full[s]), 0) : smem_u32(&sh->full[s]);
                 const int k = (t.split + kb * g.splits) * KE;
@@ -608,11 +608,11 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
             for (int kb = 0; ok && kb < kbn; ++acc) {
                 const int run_end = RUNS ? min(kb + RUN_KB, kbn) : kbn;
                 const uint32_t buf = acc & 1u, use = (acc >> 1) & 1u;
-                if (!(ok = __all_sync(FULL, mbar_wait(&sh->t_empty[buf], use ^ 1u, abort_flag)))) break;
+                if (!(ok = mbar_wait_warp(&sh->t_empty[buf], use ^ 1u, abort_flag))) break;
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + buf * ACC_COLS;
                 for (uint32_t first = 0; kb < run_end; ++kb, first = 1) {
-                    if (!(ok = __all_sync(FULL, mbar_wait(&sh->full[s], ph, abort_flag)))) break;
+                    if (!(ok = mbar_wait_warp(&sh->full[s], ph, abort_flag))) break;
                     tc_fence_after();
                     const uint32_t a = ring_base + s * (uint32_t)STAGE_BYTES, b = a + PARTS * A_BYTES;
                     if constexpr (PARTS == 1) {
@@ -700,7 +700,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
                 for (int j = 0; j < 32; ++j) run[j] = 0.f;
                 for (int kb = 0; kb < kbn; kb += RUN_KB, ++acc) {
                     buf = acc & 1u;
-                    if (!(ok = mbar_wait(&sh->t_full[buf], (acc >> 1) & 1u, abort_flag))) break;
+                    if (!(ok = mbar_wait_warp(&sh->t_full[buf], (acc >> 1) & 1u, abort_flag))) break;
                     tc_fence_after();
                     taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + buf * ACC_COLS + piece * COLS;
                     uint32_t a[32];
@@ -721,7 +721,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
                 if (!ok) break;
             } else {
                 buf = acc & 1u;
-                if (!(ok = mbar_wait(&sh->t_full[buf], (acc >> 1) & 1u, abort_flag))) break;
+                if (!(ok = mbar_wait_warp(&sh->t_full[buf], (acc >> 1) & 1u, abort_flag))) break;
                 ++acc;
                 tc_fence_after();
                 taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + buf * ACC_COLS + piece * COLS;

@@ -53,6 +53,14 @@ __device__ __forceinline__ bool mbar_wait(uint64_t *bar, uint32_t parity, volati
     }
 }
 
+// The wait of a whole warp (all 32 lanes call together): one answer for every lane.  By itself each lane has its own,
+// from its own look at the barrier, the abort flag and the clock, and lanes that differ would part before instructions
+// that the whole warp has to reach together (TMEM loads, shuffles, barriers): those that went on would wait for ever.
+__device__ __forceinline__ bool mbar_wait_warp(uint64_t *bar, uint32_t parity, volatile int *abort_flag,
+                                               long long limit = WAIT_LIMIT_CLOCKS) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, limit));
+}
+
 // The same wait without the abort flag, for a block that is already on its way out after an abort: it gives the
 // copies and MMAs the block has in flight `limit` clocks to finish (their completion is what flips the phase), so
 // that nothing of its own still writes to its shared memory or TMEM when it releases them.

@@ -41,3 +41,14 @@ def test_an_expired_wait_is_reported_and_the_context_stays_usable():
             ctx.selftest_wait_timeout(10 ** 10)                # a limit of seconds is refused on the host
     finally:
         ctx.close()
+
+
+def test_a_warp_waits_as_a_whole():
+    # lanes that see their barrier complete do not go on without those that gave up (bit 2: any lane of the third warp)
+    import paper_2604_01000_b200 as ep
+    ctx = ep.Context(0)
+    try:
+        assert int(ctx.selftest_wait_timeout(100_000)[2]) & 4 == 0
+        assert ctx.poll_status() == 5
+    finally:
+        ctx.close()
