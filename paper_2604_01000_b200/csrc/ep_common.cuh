@@ -169,7 +169,8 @@ int migrate_run(ep_ctx *ctx, const void *rowptr, bool rowptr64, int64_t N, int K
 const long long *balance_state_ptr(int64_t N, int K, int64_t max_degree, void *workspace);
 
 // Launches a kernel that may start while the launch before it on the stream still runs.  The kernel calls
-// ep_wait_for_launch_before() before it touches memory; the one before may call ep_let_next_launch_start() as soon as its
+// ep_wait_for_launch_before() before it touches memory, and takes its pointers without __restrict__ (which, like __ldg,
+// would let the compiler move loads ahead of that wait); the one before may call ep_let_next_launch_start() as soon as its
 // own blocks are all running.  What overlaps is the start of the one with the end of the other (2 to 3 us a launch).
 template <typename... P, typename... A>
 cudaError_t launch_early(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, A... args) {

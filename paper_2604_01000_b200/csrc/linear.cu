@@ -170,7 +170,7 @@ template <typename O, int n>
 __device__ __forceinline__ void finish(const Epilogue &e, int64_t row, int col, const Columns<n> &c, float (&v)[n],
                                        const float (&r)[n]) {
     if (e.x_scale) {
-        const float xs = __ldg(e.x_scale + row);
+        const float xs = e.x_scale[row];
 #pragma unroll
         for (int i = 0; i < n; ++i) v[i] *= xs * c.scale[i];
     }
@@ -687,7 +687,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
             for (int q = 0; q < SUBS; ++q) {
                 const int c = col + q * 32 + lane;
                 bias[q] = by_tma && e.bias && c < e.N ? load_param(e.bias, e.bias_type, c) : 0.f;
-                scale[q] = by_tma && e.w_scale && c < e.N ? __ldg(e.w_scale + c) : 1.f;
+                scale[q] = by_tma && e.w_scale && c < e.N ? e.w_scale[c] : 1.f;
             }
             // The sums, 32 columns at a time: in runs they are in registers, otherwise they are read from TMEM where they are
             // needed (twice where z is stored too: cheaper than keeping them).
@@ -757,7 +757,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
                 }
                 all_read();
             } else if (by_tma) {
-                const float xs = e.x_scale && row0 + lane < e.M ? __ldg(e.x_scale + row0 + lane) : 0.f;
+                const float xs = e.x_scale && row0 + lane < e.M ? e.x_scale[row0 + lane] : 0.f;
                 auto biased = [&](int q, float(&v)[32]) {
                     sums(q, v);
                     const float s = SUBS > 1 && q == 1 ? scale[SUBS - 1] : scale[0], b = SUBS > 1 && q == 1 ? bias[SUBS - 1] : bias[0];
@@ -821,7 +821,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
                         if (e.bias) w.bias = load_param(e.bias, e.bias_type, at + lane);
                         if (e.x_scale) {
                             w.x_scale = e.x_scale + row0;
-                            w.scale = __ldg(e.w_scale + at + lane);
+                            w.scale = e.w_scale[at + lane];
                         }
                         finish_rows<O>(w);
                     }
@@ -857,7 +857,7 @@ struct BiasFold {
 };
 __host__ __device__ constexpr int join_chunks() { return 32; }
 template <typename O>
-__global__ void __launch_bounds__(256) linear_join(const float *__restrict__ shares, int splits, const Epilogue e, int join_blocks,
+__global__ void __launch_bounds__(256) linear_join(const float *shares, int splits, const Epilogue e, int join_blocks,
                                                    const BiasFold bias) {
     __shared__ __align__(16) float part[8][join_chunks()][9];
     if ((int)blockIdx.x >= join_blocks) {

@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(block_threads<Lay::L>()) norm_rows_backward(co
 }
 
 // A block sums 32 columns: 32 x 32 threads, thread (c, r) the rows r, r + 32, ... in fp64; then a warp per column.
-__global__ void __launch_bounds__(1024) fold_partials(const float *__restrict__ parts, int n, int cols, float *__restrict__ out) {
+__global__ void __launch_bounds__(1024) fold_partials(const float *parts, int n, int cols, float *out) {
     __shared__ double s[32][33];
     const int lane = threadIdx.x & 31, r0 = threadIdx.x >> 5;
     const int c = blockIdx.x * 32 + lane;

@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) route_rows(const T *__
 
 // counts[c] and prob[c] over the blocks' shares; column `parts` is the number of rows that took part.  The block that
 // finishes last (the ticket tells) turns the sums into the results.
-__global__ void __launch_bounds__(1024) route_fold(const float *__restrict__ part_prob, const int *__restrict__ part_count, int n,
+__global__ void __launch_bounds__(1024) route_fold(const float *part_prob, const int *part_count, int n,
                                                   unsigned *ticket, Finish f) {
     __shared__ double sp[32][33];
     __shared__ long long sc[32][33];

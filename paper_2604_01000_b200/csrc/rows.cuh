@@ -86,7 +86,7 @@ __device__ __forceinline__ uint16_t to_e4m3_pair(float a, float b) {
 
 // One vector parameter (a norm's weight, a product's bias) of type EP_F32, EP_BF16 or EP_F16.
 __device__ __forceinline__ float load_param(const void *p, int type, int64_t i) {
-    if (type == EP_F32) return __ldg(static_cast<const float *>(p) + i);
+    if (type == EP_F32) return static_cast<const float *>(p)[i];
     if (type == EP_BF16) return __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
     return __half2float(static_cast<const __half *>(p)[i]);
 }
