@@ -44,60 +44,47 @@ struct Epilogue {
     int ld_share;
 };
 
-// The upper tail of the normal distribution at |z|, over exp(-z^2 / 2): a polynomial in t = 1 / (1 + 0.33 |z|), fitted
-// (weighted least squares, reweighted towards the largest error) to 2.2e-9 of the tail itself; fp32 rounding makes that
-// 6e-8.  The gradient needs the same exponential, and where the slope of z Phi(z) crosses zero the exponential is a common
-// factor of the terms that cancel.
-__device__ __forceinline__ float normal_tail(float z) {
-    const float t = reciprocal_fast(fmaf(0.33f, fabsf(z), 1.f));
-    float q = fmaf(0.0436886735f, t, -0.211661354f);
-    q = fmaf(q, t, 0.313509107f);
-    q = fmaf(q, t, -0.0706691593f);
-    q = fmaf(q, t, 0.170115322f);
-    q = fmaf(q, t, 0.122831702f);
-    q = fmaf(q, t, 0.132185712f);
-    return q * t;
-}
-__device__ __forceinline__ float gelu_slope(float z) {
-    const float bell = exp2_fast(z * z * (-0.5f * 1.44269504f));
-    const float q = fmaf(fabsf(z), -0.39894228f, normal_tail(z));
-    return z >= 0.f ? fmaf(-q, bell, 1.f) : q * bell;
-}
-
-// For z = (z0, z1): the bell exp(-z^2 / 2), |z| and the polynomial above.
+// The upper tail of the normal distribution at |z|, over exp(-z^2 / 2): a polynomial in t = 1 / (1 + 0.35 |z|), fitted
+// (weighted least squares, reweighted towards the largest error) to 1.1e-7 (1 + z^2) of the tail itself up to |z| = 14,
+// where fp32 loses as much by rounding the exponential's argument.  The gradient needs the same exponential, and where the
+// slope of z Phi(z) crosses zero the exponential is a common factor of the terms that cancel.
+// For z = (z0, z1): the bell exp(-z^2 / 2), |z| and that tail.
 __device__ __forceinline__ void normal_parts(float z0, float z1, Pair &bell, Pair &size, Pair &tail) {
     const Pair z(z0, z1);
     size = Pair(fabsf(z0), fabsf(z1));
     float a, b;
-    fma2(size, Pair(0.33f), Pair(1.f)).get(a, b);
+    fma2(size, Pair(0.35f), Pair(1.f)).get(a, b);
     const Pair t(reciprocal_fast(a), reciprocal_fast(b));
-    Pair q = fma2(t, Pair(0.0436886735f), Pair(-0.211661354f));
-    q = fma2(q, t, Pair(0.313509107f));
-    q = fma2(q, t, Pair(-0.0706691593f));
-    q = fma2(q, t, Pair(0.170115322f));
-    q = fma2(q, t, Pair(0.122831702f));
-    q = fma2(q, t, Pair(0.132185712f));
+    Pair q = fma2(t, Pair(0.0452263094f), Pair(-0.186698169f));
+    q = fma2(q, t, Pair(0.214374468f));
+    q = fma2(q, t, Pair(0.00660444144f));
+    q = fma2(q, t, Pair(0.143951952f));
+    q = fma2(q, t, Pair(0.136762664f));
+    q = fma2(q, t, Pair(0.139778391f));
     tail = mul2(q, t);
     mul2(mul2(z, z), Pair(-0.5f * 1.44269504f)).get(a, b);
     bell = Pair(exp2_fast(a), exp2_fast(b));
 }
-// 1/2 + sign(z) (1/2 - m) for both: Phi(z) and the slope of z Phi(z) from what they are below zero.
-__device__ __forceinline__ Pair from_lower(float z0, float z1, Pair m_minus_half) {
-    float a, b;
-    m_minus_half.get(a, b);
-    return add2(Pair(0.5f), Pair(copysignf(a, z0), copysignf(b, z1)));
+// q bell below zero, 1 - q bell above: Phi(z) and the slope of z Phi(z) from what they are at -|z|.  Chosen, not computed
+// from one another: 1 - (1 - m) would leave nothing of a small m.
+__device__ __forceinline__ Pair either_side(float z0, float z1, Pair q, Pair bell) {
+    float low0, low1, high0, high1;
+    const Pair m = mul2(q, bell);
+    m.get(low0, low1);
+    fma2(m, Pair(-1.f), Pair(1.f)).get(high0, high1);
+    return Pair(z0 >= 0.f ? high0 : low0, z1 >= 0.f ? high1 : low1);
 }
 __device__ __forceinline__ void gelu2(float &v0, float &v1) {
     Pair bell, size, tail;
     normal_parts(v0, v1, bell, size, tail);
-    mul2(Pair(v0, v1), from_lower(v0, v1, fma2(tail, mul2(bell, Pair(-1.f)), Pair(0.5f)))).get(v0, v1);
+    mul2(Pair(v0, v1), either_side(v0, v1, tail, bell)).get(v0, v1);
 }
-// v *= slope of GELU at z (to 6e-8 of 1: for operands that are rounded to 16 bits afterwards)
+// v *= slope of GELU at z
 __device__ __forceinline__ void times_gelu_slope2(float &v0, float &v1, float z0, float z1) {
     Pair bell, size, tail;
     normal_parts(z0, z1, bell, size, tail);
-    const Pair q = fma2(size, Pair(0.39894228f), mul2(tail, Pair(-1.f)));   // (minus the lower value, over the bell)
-    mul2(Pair(v0, v1), from_lower(z0, z1, fma2(q, bell, Pair(0.5f)))).get(v0, v1);
+    const Pair q = fma2(size, Pair(-0.39894228f), tail);
+    mul2(Pair(v0, v1), either_side(z0, z1, q, bell)).get(v0, v1);
 }
 
 // act(z) of n values; the switch is outside the loops, and taken by all threads alike.
@@ -118,21 +105,15 @@ __device__ __forceinline__ void activate(float (&v)[n], int act) {
         for (int i = 0; i < n; ++i) v[i] *= reciprocal_fast(1.f + exp_fast(fminf(-v[i], 80.f)));
     }
 }
-// v *= act'(z).  EXACT: where the product stays fp32.
-template <bool EXACT, int n>
+// v *= act'(z)
+template <int n>
 __device__ __forceinline__ void times_slope(float (&v)[n], const float (&z)[n], int act) {
     if (act == EP_ACT_RELU) {
 #pragma unroll
         for (int i = 0; i < n; ++i) v[i] = z[i] > 0.f ? v[i] : 0.f;
     } else if (act == EP_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < n; i += 2) {
-            if constexpr (EXACT) {
-                v[i] *= gelu_slope(z[i]);
-                v[i + 1] *= gelu_slope(z[i + 1]);
-            } else
-                times_gelu_slope2(v[i], v[i + 1], z[i], z[i + 1]);
-        }
+        for (int i = 0; i < n; i += 2) times_gelu_slope2(v[i], v[i + 1], z[i], z[i + 1]);
     } else if (act == EP_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < n; ++i) {
@@ -1060,7 +1041,7 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz(const D *__restrict__ do
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.f;
     auto work = [&](int64_t row, float(&v)[8], const float(&zz)[8]) {
-        if (act != EP_ACT_NONE) times_slope<PARTS == 3>(v, zz, act);
+        if (act != EP_ACT_NONE) times_slope(v, zz, act);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] += v[i];   // (zero past the row's end: dout reads as zero there)
         if (!to_raw) return;
