@@ -102,7 +102,7 @@ __device__ __forceinline__ void activate(float (&v)[n], int act) {
         }
     } else if (act == EP_ACT_SILU) {
 #pragma unroll
-        for (int i = 0; i < n; ++i) v[i] *= reciprocal_fast(1.f + exp_fast(fminf(-v[i], 80.f)));
+        for (int i = 0; i < n; ++i) v[i] *= reciprocal_fast(1.f + exp_fast(-v[i]));   // (1 / infinity: far below zero the sigmoid is 0)
     }
 }
 // v *= act'(z)
@@ -117,7 +117,7 @@ __device__ __forceinline__ void times_slope(float (&v)[n], const float (&z)[n], 
     } else if (act == EP_ACT_SILU) {
 #pragma unroll
         for (int i = 0; i < n; ++i) {
-            const float s = reciprocal_fast(1.f + exp_fast(fminf(-z[i], 80.f)));
+            const float s = reciprocal_fast(1.f + exp_fast(-z[i]));
             v[i] *= s * fmaf(z[i], 1.f - s, 1.f);
         }
     }

@@ -46,3 +46,22 @@ def test_gelu_slope_keeps_its_lower_tail():
     want = ref.slope(zd, "gelu")
     terms = 0.5 * torch.special.erfc(-zd / math.sqrt(2)) + zd.abs() * torch.exp(-zd * zd / 2) / math.sqrt(2 * math.pi)
     ref.within(dx, want, terms * 2.0 ** -20 * (zd * zd + 4) + 1.01 * ref.UNIT[BF16] * want.abs() + 12 * 2.0 ** -126, "slope")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [5, 200])
+def test_silu_far_below_zero(dtype, rows):
+    z = torch.tensor([-1e38, -3e30, -1e9, -1e4, -200.0, -100.0, -90.0, -87.0, -80.0, -60.0, -10.0, -1.0, 0.0, 5.0, 90.0, 1e38],
+                     device="cuda").to(dtype)
+    got, zd = through(z, "silu", rows, dtype), z.double()
+    want = ref.act(zd, "silu")
+    bound = want.abs() * (2.0 ** -20 * (zd.abs().clamp(max=200) + 4) + 1.01 * ref.UNIT[dtype]) + 200 * 2.0 ** -126
+    ref.within(got, want.expand(rows, -1), bound.expand(rows, -1), "silu")
+    low = through(torch.full((8,), -math.inf, device="cuda", dtype=dtype), "silu", rows, dtype)
+    assert bool((torch.isnan(low) | (low == 0)).all())   # (the formula's own: -infinity / infinity; its limit is 0)
+    r = ep().ep_linear_backward(torch.ones(20, 16, device="cuda"), torch.ones(20, 8, device="cuda"), torch.ones(16, 8, device="cuda"),
+                                z.float().repeat(20, 1), "silu")
+    slope = ref.slope(zd, "silu")
+    slope[:6] = torch.exp(zd[:6]) * (1 + zd[:6])         # (the reference's product is 0 times infinity there)
+    slope[0], slope[15] = 0.0, 1.0
+    ref.within(r.dbias, 20 * slope, 20 * (slope.abs() * 2.0 ** -18 * (zd.abs().clamp(max=200) + 4) + 200 * 2.0 ** -126), "slope")
