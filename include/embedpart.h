@@ -428,7 +428,8 @@ int ep_rms_norm_backward(ep_ctx *ctx, const void *dout, int32_t dout_type, const
  *            multiple of 16 bytes, else 0: unaligned ones are first copied into the workspace
  * 16-bit and 8-bit inputs are multiplied as they are and summed in fp32.  EP_F32 inputs are written as the sum of three
  * bf16 numbers (24 bits in all) and the six products that matter are summed: the result is as near as an fp32 product.
- * (A row of EP_F32 that holds an infinity or a NaN comes out as NaN.)  An output of EP_F32 is summed in short runs that
+ * (A row of x or of w of EP_F32 that holds an infinity or a NaN makes its row or column of the output NaN, however many
+ * rows there are.)  An output of EP_F32 is summed in short runs that
  * are added to nearest, since the tensor core truncates.
  *
  * ep_linear_backward:  dz = dout act'(preact);  dx = dz W;  dweight = dz^T x;  dbias = sum over rows of dz

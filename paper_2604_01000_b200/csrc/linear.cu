@@ -947,6 +947,17 @@ __global__ void __launch_bounds__(256) linear_few_rows(const T *__restrict__ x, 
         if (mine == 0 && lane < ROWS)
             for (int s = 1; s < share; ++s) v[0] += part[warp + s][lane];
     }
+    if constexpr (sizeof(T) == 4) {
+        // The tiles split fp32 numbers, and an infinity splits into NaN: so it does here.  A sum is only infinite where an
+        // operand is, or where it overflows, which stays an infinity.
+        if (col < e.N && mine == 0)
+            for (unsigned left = __ballot_sync(FULL, lane < ROWS && lane < e.M && isinf(v[0])); left; left &= left - 1) {
+                const int r = __ffs(left) - 1;
+                bool infinite = false;
+                for (int c = lane; c < n_in; c += 32) infinite |= isinf(x[r * ldx + c]) || isinf(w[col * ldw + c]);
+                if (__any_sync(FULL, infinite) && lane == r) v[0] = CUDART_NAN_F;
+            }
+    }
     if (col < e.N && mine == 0 && lane < ROWS && lane < e.M) {
         Columns<1> c;
         c.load(e, col);

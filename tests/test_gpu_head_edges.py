@@ -65,3 +65,25 @@ def test_silu_far_below_zero(dtype, rows):
     slope[:6] = torch.exp(zd[:6]) * (1 + zd[:6])         # (the reference's product is 0 times infinity there)
     slope[0], slope[15] = 0.0, 1.0
     ref.within(r.dbias, 20 * slope, 20 * (slope.abs() * 2.0 ** -18 * (zd.abs().clamp(max=200) + 4) + 200 * 2.0 ** -126), "slope")
+
+
+@pytest.mark.parametrize("rows", [1, 3, 8, 40])
+@pytest.mark.parametrize("n_in,n_out", [(96, 64), (33, 7), (2048, 5)])
+def test_an_infinity_in_fp32_is_nan_whatever_the_number_of_rows(rows, n_in, n_out):
+    g = torch.Generator(device="cuda").manual_seed(50)
+    x, w = torch.randn(rows, n_in, generator=g, device="cuda"), torch.randn(n_out, n_in, generator=g, device="cuda") * 0.1
+    clean = ep().ep_linear(x, w).out
+    for bad in (math.inf, -math.inf, math.nan):
+        a, b = x.clone(), w.clone()
+        a[rows - 1, n_in - 1] = bad
+        out = ep().ep_linear(a, w).out
+        assert bool(torch.isnan(out[rows - 1]).all()) and torch.equal(out[:rows - 1], clean[:rows - 1])
+        b[2, 1] = bad
+        out = ep().ep_linear(x, b).out
+        keep = [c for c in range(n_out) if c != 2]
+        assert bool(torch.isnan(out[:, 2]).all()) and torch.equal(out[:, keep], clean[:, keep])
+
+
+def test_a_sum_that_overflows_is_an_infinity():
+    x, w = torch.full((2, 40), 1e20, device="cuda"), torch.full((9, 40), 1e20, device="cuda")
+    assert bool(torch.isposinf(ep().ep_linear(x, w).out).all()) and bool(torch.isneginf(ep().ep_linear(-x, w).out).all())
