@@ -437,7 +437,9 @@ int ep_rms_norm_backward(ep_ctx *ctx, const void *dout, int32_t dout_type, const
  *   preact   [dev] rows x n_out of in_type, or NULL with EP_ACT_NONE
  *   dx       [dev] out or NULL, rows x n_in of in_type;  dweight [dev] out or NULL, n_out x n_in of in_type
  *   dbias    [dev] out or NULL, n_out fp32 (summed from dz before it is rounded);  in_type is not EP_E4M3
- * dz is rounded to in_type before the products of 16-bit types (their operands are 16 bits).
+ * dz is rounded to in_type before the products of 16-bit types (their operands are 16 bits; dx and dweight are off by about 1.4
+ * times the error that rounding them alone would leave).  For EP_F16 dz is scaled first, by the power of two that brings the
+ * largest finite |dout| to 2^14, and the sums scaled back: elements below 2^-39 of that largest are lost, whatever its size.
  */
 size_t ep_linear_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t n_in, int32_t n_out, int32_t in_type,
                                  int32_t out_type, int32_t aligned);   /* 0 = invalid shape or types; at least 256 */

@@ -21,6 +21,7 @@
 #include <algorithm>
 #include <initializer_list>
 #include <mutex>
+#include <type_traits>
 
 using namespace eprow;
 using namespace eptc;
@@ -40,6 +41,7 @@ struct Epilogue {
     int N;
     bool vec;                         // out, preact, residual, bias, scales: 16-byte rows of whole 8-column chunks
     bool tma;                         // out and preact can be written by TMA, the residual read by 16 bytes
+    const float *factor;              // of fp16 results: what the sums are multiplied by first (one value), or NULL
     float *share;                     // where a block's share of a split sum goes: [split][M][ld_share] fp32
     int ld_share;
 };
@@ -150,6 +152,13 @@ struct Columns {
 template <typename O, int n>
 __device__ __forceinline__ void finish(const Epilogue &e, int64_t row, int col, const Columns<n> &c, float (&v)[n],
                                        const float (&r)[n]) {
+    if constexpr (std::is_same_v<O, __half>) {
+        if (e.factor) {
+            const float f = *e.factor;
+#pragma unroll
+            for (int i = 0; i < n; ++i) v[i] *= f;
+        }
+    }
     if (e.x_scale) {
         const float xs = e.x_scale[row];
 #pragma unroll
@@ -642,6 +651,8 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
         uint32_t acc = 0;
         bool ok = true;
         const bool by_tma = e.tma && !e.share, with_z = e.preact != nullptr;
+        const bool scaled = std::is_same_v<O, __half> && e.factor && !e.share;   // (shares are joined first)
+        const float factor = scaled ? *e.factor : 1.f;
         // The residual is copied into the slot that the result will leave from, and added in place.
         auto fetch_residual = [&](int64_t row0, int col) {
             constexpr int PER_ROW = C::WIDTH / C::G;
@@ -741,6 +752,10 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
                 const float xs = e.x_scale && row0 + lane < e.M ? e.x_scale[row0 + lane] : 0.f;
                 auto biased = [&](int q, float(&v)[32]) {
                     sums(q, v);
+                    if (scaled) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] *= factor;
+                    }
                     const float s = SUBS > 1 && q == 1 ? scale[SUBS - 1] : scale[0], b = SUBS > 1 && q == 1 ? bias[SUBS - 1] : bias[0];
                     if (e.x_scale) {
 #pragma unroll
@@ -792,7 +807,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
                     float v[32];
                     sums(q, v);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) loose[lane * 32 + ((j + lane) & 31)] = v[j];
+                    for (int j = 0; j < 32; ++j) loose[lane * 32 + ((j + lane) & 31)] = scaled ? v[j] * factor : v[j];
                     __syncwarp();
                     if (at + lane < e.N) {
                         LooseRows<O> w{static_cast<O *>(e.out) + row0 * e.N + at + lane, nullptr, nullptr, nullptr, e.ldr, e.N,
@@ -1028,6 +1043,55 @@ __global__ void __launch_bounds__(256) pack_rows(const PackJob first, const Pack
     }
 }
 
+// fp16 holds nothing below 2^-25 and nothing above 65504, where a mean loss over many rows, or a loss scale, puts whole
+// gradients.  So dz that has to be rounded to fp16 is first multiplied by the power of two that brings the largest finite
+// |dout| to [2^14, 2^15) (the slopes are below 1.13), and the products' sums by its inverse: elements down to 2^-28 of that
+// largest keep fp16's 11 bits, what is lost of smaller ones is below 2^-39 of it.  dout is read once more for it (232965 x 256
+// fp16: 24 us of 179).  Each block leaves its largest; the blocks of linear_dz take the largest of those.
+constexpr int PEAK_BLOCKS_PER_SM = 4;
+template <typename D>
+__global__ void __launch_bounds__(256) linear_peaks(const D *__restrict__ dout, int64_t total, float *__restrict__ peaks) {
+    __shared__ float tops[8];
+    constexpr int N = 16 / (int)sizeof(D), Q = 4;   // Q 16-byte chunks in flight
+    float top = 0.f;
+    auto look = [&](D v) {
+        const float size = fabsf(to_f32(v));
+        top = fmaxf(top, size < INFINITY ? size : 0.f);
+    };
+    // the elements before the first 16-byte boundary and after the last whole chunk are the last block's
+    const int64_t before = min((int64_t)((16 - (reinterpret_cast<uintptr_t>(dout) & 15)) & 15) / (int)sizeof(D), total);
+    const int64_t chunks = (total - before) / N, step = (int64_t)gridDim.x * 256;
+    const uint4 *from = reinterpret_cast<const uint4 *>(dout + before);
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < chunks; i += Q * step) {
+        alignas(16) D e[Q][N];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) *reinterpret_cast<uint4 *>(e[q]) = i + q * step < chunks ? from[i + q * step] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+#pragma unroll
+            for (int c = 0; c < N; ++c) look(e[q][c]);
+    }
+    if (blockIdx.x == gridDim.x - 1) {
+        if (threadIdx.x < before) look(dout[threadIdx.x]);
+        const int64_t rest = before + chunks * N + threadIdx.x;
+        if (rest < total) look(dout[rest]);
+    }
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
+    if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+#pragma unroll
+        for (int w = 1; w < 8; ++w) top = fmaxf(top, tops[w]);
+        peaks[blockIdx.x] = top;
+    }
+}
+struct Peaks {   // NULL: dz is written as it is
+    float *each;
+    int n;
+    float *factor;   // out: the inverse of the power of two
+};
+
 // dz = dout act'(z), written for the products (16 bits as they are, fp32 as three bf16 parts; rows ld_to apart, zero
 // beyond N), and the sums of its columns over this block's rows: part[blockIdx.y][N].  232965 x 256 bf16 through GELU:
 // 60 us, 6.0 TB/s, with instruction issue close behind (23 an element).
@@ -1039,7 +1103,7 @@ constexpr int dz_pieces() { return (8 * (int)(sizeof(T) + sizeof(D))) / 16; }   
 template <typename T, typename D, int PARTS>
 __global__ void __launch_bounds__(DZ_THREADS) linear_dz(const D *__restrict__ dout, const T *__restrict__ z, int act, int64_t rows,
                                                         int n_out, void *to_raw, int ld_to, int64_t part_stride,
-                                                        float *__restrict__ part, bool vec) {
+                                                        float *__restrict__ part, bool vec, const Peaks peaks) {
     constexpr int D_PIECES = 8 * (int)sizeof(D) / 16, Z_PIECES = 8 * (int)sizeof(T) / 16;
     __shared__ float fold[DZ_ROWS][DZ_CHUNKS * 8];
     extern __shared__ uint4 ring[];   // [DZ_STAGES][D_PIECES + Z_PIECES][DZ_THREADS], where vec
@@ -1048,6 +1112,23 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz(const D *__restrict__ do
     // all blocks go over the rows side by side, so that what is written last lies together (see GemmShape::backwards)
     const int64_t begin = (int64_t)blockIdx.y * DZ_ROWS, step = (int64_t)gridDim.y * DZ_ROWS;
     ep_let_next_launch_start();
+    float scale = 1.f;
+    if constexpr (std::is_same_v<T, __half>) {
+        if (peaks.each) {
+            float top = 0.f;
+            for (int i = threadIdx.x; i < peaks.n; i += DZ_THREADS) top = fmaxf(top, peaks.each[i]);
+#pragma unroll
+            for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
+            if ((threadIdx.x & 31) == 0) fold[0][threadIdx.x >> 5] = top;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < DZ_THREADS / 32; ++w) top = fmaxf(top, fold[0][w]);
+            __syncthreads();   // (fold is used again)
+            const int up = top > 0.f ? min(14 - ilogbf(top), 126) : 0;
+            scale = scalbnf(1.f, up);
+            if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *peaks.factor = scalbnf(1.f, -up);
+        }
+    }
     float sum[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.f;
@@ -1069,6 +1150,10 @@ __global__ void __launch_bounds__(DZ_THREADS) linear_dz(const D *__restrict__ do
                 *reinterpret_cast<uint4 *>(to + k * part_stride) = *reinterpret_cast<const uint4 *>(o);
             }
         } else {
+            if constexpr (std::is_same_v<T, __half>) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= scale;
+            }
             store_chunk(static_cast<T *>(to_raw) + row * ld_to, col, ld_to, true, v);
         }
     };
@@ -1443,6 +1528,7 @@ LinearWorkspace linear_workspace(const ep_ctx *ctx, int64_t rows, int n_in, int 
 struct BackwardWorkspace {
     void *dz, *x, *w;
     float *dbias_parts, *share;
+    Peaks peaks;   // of fp16 alone
     GemmPlan dx, dw;
     Packed dz_form;
     int slabs;   // blocks that share out the rows in linear_dz
@@ -1462,6 +1548,11 @@ BackwardWorkspace backward_workspace(const ep_ctx *ctx, int64_t rows, int n_in, 
     const int64_t want = std::max<int64_t>(1, (int64_t)ctx->sm_count * 4 / across);   // about what stays resident
     w.slabs = (int)std::max<int64_t>(1, std::min<int64_t>(want, ep::ceil_div(rows, 2 * DZ_ROWS)));
     w.dbias_parts = a.take<float>((size_t)w.slabs * n_out);
+    if (in_type == EP_F16) {
+        w.peaks.n = (int)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(rows * n_out, 256 * 16), (int64_t)ctx->sm_count * PEAK_BLOCKS_PER_SM));
+        w.peaks.each = a.take<float>(w.peaks.n + 1);
+        w.peaks.factor = w.peaks.each ? w.peaks.each + w.peaks.n : nullptr;
+    }
     w.dx = plan_gemm(ctx, std::max<int64_t>(rows, 1), n_in, n_out, in_type, in_type == EP_F32);
     w.dw = plan_gemm(ctx, n_out, n_in, std::max<int64_t>(rows, 1), in_type, in_type == EP_F32);
     w.share = a.take<float>(std::max(w.dx.share_bytes(rows), w.dw.share_bytes(n_out)) / sizeof(float));
@@ -1495,14 +1586,15 @@ int launch_few_rows(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int6
 
 template <typename T, typename D, int PARTS>
 void launch_dz(const BackwardWorkspace &w, const void *dout, const void *z, int act, int64_t rows, int n_out, bool write, bool sum,
-               bool vec, cudaStream_t stream) {
+               bool vec, bool scaled, cudaStream_t stream) {
+    if (scaled) linear_peaks<D><<<w.peaks.n, 256, 0, stream>>>((const D *)dout, rows * n_out, w.peaks.each);
     const dim3 grid((unsigned)ep::ceil_div(w.dz_form.ld, DZ_CHUNKS * 8), (unsigned)w.slabs);
     const size_t smem = vec ? (size_t)DZ_STAGES * dz_pieces<T, D>() * DZ_THREADS * 16 : 0;
     cudaFuncSetAttribute(linear_dz<T, D, PARTS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                          DZ_STAGES * dz_pieces<T, D>() * DZ_THREADS * 16);
     linear_dz<T, D, PARTS><<<grid, DZ_THREADS, smem, stream>>>((const D *)dout, (const T *)z, act, rows, n_out,
                                                                      write ? w.dz : nullptr, w.dz_form.ld, w.dz_form.part_stride,
-                                                                     sum ? w.dbias_parts : nullptr, vec);
+                                                                     sum ? w.dbias_parts : nullptr, vec, scaled ? w.peaks : Peaks{});
 }
 
 int linear_run(ep_ctx *ctx, const LinearWorkspace &ws, const void *x, int64_t ldx, const void *w, int64_t ldw, int in_type,
@@ -1530,20 +1622,21 @@ int linear_backward_run(ep_ctx *ctx, const BackwardWorkspace &ws, const void *do
     const bool copy = in_type == EP_F32 || !aligned;
     const bool direct = act == EP_ACT_NONE && dout_type == in_type && !copy && tma_ready(dout, n_out, in_type);
     const bool write = !direct && (dx || dweight);
+    const bool scaled = write && in_type == EP_F16 && (act != EP_ACT_NONE || dout_type != EP_F16);   // (dz is rounded)
     if (write || dbias) {
         const bool vec = n_out % 8 == 0 && ep::aligned(dout, 16) && ep::aligned(preact, 16);
         if (in_type == EP_F32)
-            launch_dz<float, float, 3>(ws, dout, preact, act, rows, n_out, write, dbias, vec, stream);
+            launch_dz<float, float, 3>(ws, dout, preact, act, rows, n_out, write, dbias, vec, scaled, stream);
         else if (in_type == EP_BF16 && dout_type == EP_BF16)
-            launch_dz<__nv_bfloat16, __nv_bfloat16, 1>(ws, dout, preact, act, rows, n_out, write, dbias, vec, stream);
+            launch_dz<__nv_bfloat16, __nv_bfloat16, 1>(ws, dout, preact, act, rows, n_out, write, dbias, vec, scaled, stream);
         else if (in_type == EP_BF16)
-            launch_dz<__nv_bfloat16, float, 1>(ws, dout, preact, act, rows, n_out, write, dbias, vec, stream);
+            launch_dz<__nv_bfloat16, float, 1>(ws, dout, preact, act, rows, n_out, write, dbias, vec, scaled, stream);
         else if (dout_type == EP_F16)
-            launch_dz<__half, __half, 1>(ws, dout, preact, act, rows, n_out, write, dbias, vec, stream);
+            launch_dz<__half, __half, 1>(ws, dout, preact, act, rows, n_out, write, dbias, vec, scaled, stream);
         else
-            launch_dz<__half, float, 1>(ws, dout, preact, act, rows, n_out, write, dbias, vec, stream);
+            launch_dz<__half, float, 1>(ws, dout, preact, act, rows, n_out, write, dbias, vec, scaled, stream);
         EP_CUDA(ctx, cudaGetLastError());
-        ++*kernels;
+        *kernels += scaled ? 2 : 1;
     }
     Operand dz;
     if (direct)
@@ -1553,6 +1646,7 @@ int linear_backward_run(ep_ctx *ctx, const BackwardWorkspace &ws, const void *do
     Epilogue e{};
     e.out_type = in_type;
     e.bias_type = EP_F32;
+    e.factor = scaled ? ws.peaks.factor : nullptr;
     Operand xs{}, wt{};
     int rc = EP_OK;
     bool folded = false;

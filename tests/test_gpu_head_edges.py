@@ -87,3 +87,58 @@ def test_an_infinity_in_fp32_is_nan_whatever_the_number_of_rows(rows, n_in, n_ou
 def test_a_sum_that_overflows_is_an_infinity():
     x, w = torch.full((2, 40), 1e20, device="cuda"), torch.full((9, 40), 1e20, device="cuda")
     assert bool(torch.isposinf(ep().ep_linear(x, w).out).all()) and bool(torch.isneginf(ep().ep_linear(-x, w).out).all())
+
+
+def fp16_gradients(dout, x, w, z, act):
+    """dx, dweight and dbias of fp16 operands against fp64.  dz keeps 11 bits wherever |dz| is above 2^-26 of the largest
+    |dout| and loses 2^-38 of that largest otherwise; the sums truncate 2^-22 a step of 16; one rounding ends it."""
+    r = ep().ep_linear_backward(dout, x, w, z, act)
+    slope = torch.ones_like(dout, dtype=torch.float64) if act == "none" else ref.slope(z.double(), act)
+    dz, lost = dout.double() * slope, 2.0 ** -38 * float(dout.double().abs().max())
+    unit = ref.UNIT[F16]
+    for got, a, b, steps in ((r.dx, dz, w.double(), w.shape[0] / 16), (r.dweight, dz.T, x.double(), x.shape[0] / 16)):
+        want, size = a @ b, a.abs() @ b.abs()
+        e = size * (2.0 ** -18 + unit + (steps + 4) * 2.0 ** -22) + lost * b.abs().sum(0)
+        ref.within(got, want, e + unit * (want.abs() + e) + ref.TINY[F16], "gradient")
+        assert float(want.abs().min()) > 2.0 ** -14          # (a result that fp16 holds)
+    want = dz.sum(0)
+    ref.within(r.dbias, want, dz.abs().sum(0) * (2.0 ** -18 + (64 + x.shape[0] / 64) * 2.0 ** -23), "dbias")
+
+
+@pytest.mark.parametrize("rows,n_in,n_out", [(20000, 64, 128), (20001, 33, 17)])
+@pytest.mark.parametrize("grad", [F32, F16])
+@pytest.mark.parametrize("act", ["none", "gelu", "silu"])
+def test_fp16_gradients_below_what_fp16_holds(rows, n_in, n_out, grad, act):
+    # a mean over very many rows without a loss scale: every element of dz is near or below fp16's smallest numbers, the
+    # sums over rows are not
+    g = torch.Generator(device="cuda").manual_seed(51)
+    uniform = lambda *s: torch.rand(*s, generator=g, device="cuda") + 0.5   # noqa: E731
+    x, w = uniform(rows, n_in).to(F16), (uniform(n_out, n_in) * 30000).to(F16)
+    z = (uniform(rows, n_out) * 0.1).to(F16)
+    fp16_gradients((uniform(rows, n_out) * (2.0 ** -27 if grad == F32 else 2.0 ** -23)).to(grad), x, w, z, act)
+
+
+@pytest.mark.parametrize("act", ["none", "gelu"])
+def test_fp16_gradients_above_what_fp16_holds(act):
+    g = torch.Generator(device="cuda").manual_seed(52)
+    uniform = lambda *s: torch.rand(*s, generator=g, device="cuda") + 0.5   # noqa: E731
+    x, w, z = (uniform(300, 40) * 1e-5).to(F16), (uniform(24, 40) * 1e-4).to(F16), uniform(300, 24).to(F16)
+    fp16_gradients(uniform(300, 24) * 1e6, x, w, z, act)
+    big = torch.full((300, 24), 65504.0, device="cuda", dtype=F16)          # times a slope above 1
+    fp16_gradients(big, x, w, torch.full_like(z, 1.5), "gelu")
+
+
+def test_fp16_gradients_that_are_zero_or_not_finite():
+    x, w = torch.ones(40, 16, device="cuda", dtype=F16), torch.ones(24, 16, device="cuda", dtype=F16)
+    zero = ep().ep_linear_backward(torch.zeros(40, 24, device="cuda"), x, w)
+    assert not bool(zero.dx.any()) and not bool(zero.dweight.any()) and not bool(zero.dbias.any())
+    dout = torch.full((40, 24), 1e-9, device="cuda")
+    clean = ep().ep_linear_backward(dout * 1e4, x, w)
+    for bad in (math.nan, math.inf):
+        d = dout * 1e4
+        d[3, 5] = bad
+        r = ep().ep_linear_backward(d, x, w)
+        keep = [i for i in range(40) if i != 3]
+        assert torch.equal(r.dx[keep], clean.dx[keep]) and not bool(torch.isfinite(r.dx[3]).any())
+        cols = [i for i in range(24) if i != 5]
+        assert torch.equal(r.dweight[cols], clean.dweight[cols]) and not bool(torch.isfinite(r.dweight[5]).any())
