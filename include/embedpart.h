@@ -429,8 +429,9 @@ int ep_rms_norm_backward(ep_ctx *ctx, const void *dout, int32_t dout_type, const
  * 16-bit and 8-bit inputs are multiplied as they are and summed in fp32.  EP_F32 inputs are written as the sum of three
  * bf16 numbers (24 bits in all) and the six products that matter are summed: the result is as near as an fp32 product.
  * (A row of x or of w of EP_F32 that holds an infinity or a NaN makes its row or column of the output NaN, however many
- * rows there are.)  An output of EP_F32 is summed in short runs that
- * are added to nearest, since the tensor core truncates.
+ * rows there are.)  The tensor core truncates its fp32 sums (1e-7 of a sum of one sign per 16 products of 16 bits, 32 of
+ * 8): an output of EP_F32 is summed in runs of 16 such steps that are added to nearest, one of EP_F16 in runs of 512, one of
+ * EP_BF16 in runs of 4096, which costs a ninth of the output's own rounding at most, however long the sum.
  *
  * ep_linear_backward:  dz = dout act'(preact);  dx = dz W;  dweight = dz^T x;  dbias = sum over rows of dz
  *   dout     [dev] rows x n_out of dout_type: in_type or EP_F32, rows n_out apart

@@ -316,8 +316,12 @@ __device__ __noinline__ void finish_rows(LooseRows<O> w) {
 // its own, the five small products share a second one.
 //
 // RUNS: the tensor core's fp32 sums are truncated, which costs up to an ulp of the running sum a step, always
-// downwards (measured: 4e-6 of the result after 256 steps, 2e-7 after 16).  Where the output is fp32, sums therefore
-// run over 4 k-blocks only (16 steps), and the epilogue's threads add the runs to nearest in their registers.
+// downwards (measured on sums of one sign: 1.0e-7 of the result a step, after 64 steps as after 4096).  Where the output is
+// fp32, sums therefore run over 4 k-blocks only (16 steps), and the epilogue's threads add the runs to nearest in their
+// registers.  Sums of 16-bit outputs run up to a ninth of the output's rounding unit (through_kb).  Longer ones are
+// added up beside the accumulator, in the TMEM that otherwise is the second accumulator (GemmShape::keep): the MMAs then
+// wait while a run is added, 1 to 2 % of the time (weights' gradient of 169343 x 2048 x 2048 fp16 1045 -> 1066 us, of
+// 60000 x 4096 x 4096 1520 -> 1550).
 //
 // PAIR: two blocks of a cluster (one TPC's two SMs) work on one tile of 256 x BN.  Either keeps 128 rows of A and half of
 // B in its shared memory and 128 rows of the sums in its TMEM; the first one's MMA warp issues for both.  A block then
@@ -325,6 +329,9 @@ __device__ __noinline__ void finish_rows(LooseRows<O> w) {
 constexpr int BM = 128;               // rows of a block
 constexpr int A_BYTES = BM * 128;
 constexpr int RUN_KB = 4;
+// The k-blocks (of four steps) that may run through where the output is of 16 bits: 512 steps cost 5e-5 and fp16's rounding
+// 4.9e-4, 4096 steps 4.2e-4 and bf16's 3.9e-3.
+constexpr int through_kb(int out_type) { return out_type == EP_F16 ? 128 : 1024; }
 constexpr int MAX_STAGES = 8;
 constexpr int TMEM_COLS = 512;
 
@@ -362,6 +369,8 @@ struct GemmShape {
     int64_t tiles;        // tiles of the output
     int64_t items;        // tiles x splits
     int splits, kb;       // shares of the sum; k-blocks of all of it (share s takes k-blocks s, s + splits, ...)
+    int run_kb;           // k-blocks of a run
+    bool keep;            // 16-bit outputs: a share has several runs, added up in TMEM
     bool a_mn, b_mn;      // operand stored along its rows
     bool backwards;       // the last row of tiles first: where A has just been written, its end is still in the L2
     uint32_t idesc;       // without the number of columns
@@ -596,8 +605,8 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
             const int kbn = t.kbn();
             const uint32_t idesc = g.idesc | (uint32_t)(t.columns() >> 3) << 17;
             for (int kb = 0; ok && kb < kbn; ++acc) {
-                const int run_end = RUNS ? min(kb + RUN_KB, kbn) : kbn;
-                const uint32_t buf = acc & 1u, use = (acc >> 1) & 1u;
+                const int run_end = RUNS || g.keep ? min(kb + g.run_kb, kbn) : kbn;
+                const uint32_t buf = g.keep ? 0u : acc & 1u, use = g.keep ? acc & 1u : (acc >> 1) & 1u;
                 if (!(ok = mbar_wait_warp(&sh->t_empty[buf], use ^ 1u, abort_flag))) break;
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + buf * ACC_COLS;
@@ -690,7 +699,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
                 const int kbn = t.kbn();
 #pragma unroll
                 for (int j = 0; j < 32; ++j) run[j] = 0.f;
-                for (int kb = 0; kb < kbn; kb += RUN_KB, ++acc) {
+                for (int kb = 0; kb < kbn; kb += g.run_kb, ++acc) {
                     buf = acc & 1u;
                     if (!(ok = mbar_wait_warp(&sh->t_full[buf], (acc >> 1) & 1u, abort_flag))) break;
                     tc_fence_after();
@@ -709,6 +718,29 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
                         for (int j = 0; j < 32; ++j) run[j] += __uint_as_float(a[j]);
                     }
                     give_back(buf);
+                }
+                if (!ok) break;
+            } else if (g.keep) {
+                const uint32_t from = tmem_base + ((uint32_t)(quad * 32) << 16) + piece * COLS;
+                const int kbn = t.kbn();
+                taddr = from + ACC_COLS;
+                for (int kb = 0; kb < kbn; kb += g.run_kb, ++acc) {
+                    if (!(ok = mbar_wait_warp(&sh->t_full[0], acc & 1u, abort_flag))) break;
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int q = 0; q < COLS; q += 16) {
+                        uint32_t a[16];
+                        tmem_ld16(from + q, a);
+                        if (kb > 0) {
+                            uint32_t w[16];
+                            tmem_ld16(taddr + q, w);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) a[j] = __float_as_uint(__uint_as_float(a[j]) + __uint_as_float(w[j]));
+                        }
+                        tmem_st16(taddr + q, a);
+                    }
+                    tmem_st_wait();
+                    give_back(0);
                 }
                 if (!ok) break;
             } else {
@@ -731,7 +763,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
                 }
             };
             auto all_read = [&] {
-                if constexpr (!RUNS) give_back(buf);
+                if (!RUNS && !g.keep) give_back(buf);
             };
             if (!mine) {
                 all_read();
@@ -1315,8 +1347,9 @@ struct GemmPlan {
 // column and 1000 more; the join of a split sum 5000 and its shares' bytes (3400 a clock).  The sum is only split while
 // the tiles leave workers idle, into shares of at least 4 k-blocks.  (With the largest tile that fills one wave instead,
 // the weights' gradient of 232965 x 256 x 256 went by tiles of 64 columns that read each operand up to four times.)
-GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, bool fp32_out) {
+GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, int out_type) {
     const int ke = type == EP_E4M3 ? 128 : 64, parts = type == EP_F32 ? 3 : 1;
+    const bool fp32_out = out_type == EP_F32;
     const int kb = (int)ep::ceil_div(K, ke);
     GemmPlan best{};
     double best_cost = 0.0;
@@ -1337,6 +1370,8 @@ GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, boo
             p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(workers / p.shape.tiles, kb / 4));
             const int per = (int)ep::ceil_div(kb, p.splits);
             p.shape.splits = p.splits;
+            p.shape.run_kb = fp32_out ? RUN_KB : through_kb(out_type);
+            p.shape.keep = !fp32_out && per > p.shape.run_kb;
             p.shape.items = p.shape.tiles * p.splits;
             p.workers = (int)std::min<int64_t>(p.shape.items, workers);
             p.shape.step_m = p.workers / p.shape.tiles_n;
@@ -1518,7 +1553,7 @@ LinearWorkspace linear_workspace(const ep_ctx *ctx, int64_t rows, int n_in, int 
             w.x = a.take<char>(packed_form(rows, n_in, in_type).bytes);
             w.w = a.take<char>(packed_form(n_out, n_in, in_type).bytes);
         }
-        w.plan = plan_gemm(ctx, rows, n_out, n_in, in_type, out_type == EP_F32);
+        w.plan = plan_gemm(ctx, rows, n_out, n_in, in_type, out_type);
         w.share = a.take<float>(w.plan.share_bytes(rows) / sizeof(float));
     }
     w.bytes = std::max<size_t>(a.used, 256);
@@ -1553,8 +1588,8 @@ BackwardWorkspace backward_workspace(const ep_ctx *ctx, int64_t rows, int n_in, 
         w.peaks.each = a.take<float>(w.peaks.n + 1);
         w.peaks.factor = w.peaks.each ? w.peaks.each + w.peaks.n : nullptr;
     }
-    w.dx = plan_gemm(ctx, std::max<int64_t>(rows, 1), n_in, n_out, in_type, in_type == EP_F32);
-    w.dw = plan_gemm(ctx, n_out, n_in, std::max<int64_t>(rows, 1), in_type, in_type == EP_F32);
+    w.dx = plan_gemm(ctx, std::max<int64_t>(rows, 1), n_in, n_out, in_type, in_type);
+    w.dw = plan_gemm(ctx, n_out, n_in, std::max<int64_t>(rows, 1), in_type, in_type);
     w.share = a.take<float>(std::max(w.dx.share_bytes(rows), w.dw.share_bytes(n_out)) / sizeof(float));
     w.bytes = std::max<size_t>(a.used, 256);
     return w;

@@ -142,3 +142,60 @@ def test_fp16_gradients_that_are_zero_or_not_finite():
         assert torch.equal(r.dx[keep], clean.dx[keep]) and not bool(torch.isfinite(r.dx[3]).any())
         cols = [i for i in range(24) if i != 5]
         assert torch.equal(r.dweight[cols], clean.dweight[cols]) and not bool(torch.isfinite(r.dweight[5]).any())
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_long_sums_do_not_drift(dtype):
+    # 400000 rows of one sign into a weight gradient wide enough that no idle block takes a share of its sum.  Sums that are
+    # truncated at every step lose about 1e-7 of themselves a step (25000 steps here): the mean of the errors must stay
+    # within a quarter of the type's rounding unit, whatever the number of rows
+    rows, n = 400_000, 2048
+    g = torch.Generator(device="cuda").manual_seed(53)
+    x = ((torch.rand(rows, n, generator=g, device="cuda", dtype=F16) + 1) * 0.5).to(dtype)
+    dout = ((torch.rand(rows, n, generator=g, device="cuda", dtype=F16) + 1) * 2.0 ** -11).to(dtype)
+    want = torch.zeros(n, n, device="cuda", dtype=torch.float64)
+    for at in range(0, rows, 50_000):
+        want += dout[at:at + 50_000].double().T @ x[at:at + 50_000].double()
+    got = ep().ep_linear_backward(dout, x, torch.ones(n, n, device="cuda", dtype=dtype), need_dx=False, need_dbias=False).dweight
+    off, unit = (got.double() - want) / want, ref.UNIT[dtype]
+    assert abs(float(off.mean())) <= unit / 4 and float(off.abs().max()) <= unit * 1.26
+
+
+@pytest.mark.parametrize("dtype,rows,n_out,n_in", [(F16, 131_150, 2100, 1997), (BF16, 131_150, 2100, 1997), (F16, 20_011, 4999, 5008),
+                                                   (F16, 1_200_005, 40, 56), (BF16, 70_003, 4000, 4008), (F16, 9_000, 300, 20_000)])
+def test_long_sums_of_either_sign(dtype, rows, n_out, n_in):
+    # lengths that end inside a step, widths that leave by whole pieces and by single elements, in shares and in one.  A run
+    # has at most 512 (fp16) or 4096 steps, each of which costs 2^-22 of its terms; then one rounding
+    g = torch.Generator(device="cuda").manual_seed(54)
+    x = torch.randn(rows, n_in, generator=g, device="cuda").to(dtype)
+    dout = torch.randn(rows, n_out, generator=g, device="cuda").to(dtype)
+    got = ep().ep_linear_backward(dout, x, torch.ones(n_out, n_in, device="cuda", dtype=dtype), need_dx=False, need_dbias=False).dweight
+    steps = 520 if dtype == F16 else 4110
+    for at in range(0, n_out, 1700):                     # (the reference, some rows of dweight at a time)
+        cols = slice(at, min(at + 100, n_out))
+        want = torch.zeros(cols.stop - cols.start, n_in, device="cuda", dtype=torch.float64)
+        size = torch.zeros_like(want)
+        for r in range(0, rows, 20_000):
+            a, b = dout[r:r + 20_000, cols].double(), x[r:r + 20_000].double()
+            want += a.T @ b
+            size += a.abs().T @ b.abs()
+        e = size * steps * 2.0 ** -22
+        ref.within(got[cols], want, e + ref.UNIT[dtype] * (want.abs() + e), "dweight")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("rows,n_in,n_out", [(2000, 40_000, 5008), (2000, 40_001, 5001), (9000, 9000, 9008), (40, 65536, 24)])
+def test_long_rows_through_the_whole_epilogue(dtype, rows, n_in, n_out):
+    # of one sign, so that S is z itself; the first three so wide that no idle block takes a share
+    g = torch.Generator(device="cuda").manual_seed(57)
+    x = ((torch.rand(rows, n_in, generator=g, device="cuda") + 1) * 0.5).to(dtype)
+    w = ((torch.rand(n_out, n_in, generator=g, device="cuda") + 1) * 2.0 ** -11).to(dtype)
+    bias, res = torch.randn(n_out, generator=g, device="cuda"), torch.randn(rows, n_out, generator=g, device="cuda").to(dtype)
+    r = ep().ep_linear(x, w, bias, "relu", res, preact=True)
+    z = x.double() @ w.double().T
+    unit, e = ref.UNIT[dtype], z * (520 if dtype == F16 else 2510) * 2.0 ** -22
+    ref.within(r.preact, z + bias, e + unit * (z + bias.abs()) * 1.01, "preact")
+    want = (z + bias).clamp(min=0) + res.double()
+    ref.within(r.out, want, 1.01 * e + unit * (z + bias.abs() + res.double().abs()) * 1.01, "out")
+    off = (r.preact.double() - (z + bias)) / z
+    assert abs(float(off.mean())) <= unit / 4
