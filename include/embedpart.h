@@ -480,7 +480,8 @@ int ep_linear_backward(ep_ctx *ctx, const void *dout, int32_t dout_type, const v
  *   dlogits = p (dp - sum_e p_e dp_e);  0 in rows that take no part
  *   logits, valid, k, renormalize, ids, counts, routed: as the forward took and returned them (a row's ids other than -1
  *            are distinct)
- *   dweights [dev] rows x k fp32 or NULL (zero);  dloss [dev] 1 fp32 or NULL (zero)
+ *   dweights [dev] rows x k fp32 or NULL (zero); what it holds in slots whose id is -1 does not matter
+ *   dloss    [dev] 1 fp32 or NULL (zero)
  *   dlogits  [dev] out, rows x parts of `type`
  * An id outside [-1, parts) raises EP_ERR_BAD_INDEX in the device status word and is skipped.
  */

@@ -384,11 +384,12 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) route_rows_backward(co
         int id;
         float dw;
     };
+    auto of_slot = [&](int id, float dw) { return id >= 0 && id < parts ? dw : 0.f; };   // (an empty slot's may be anything)
     auto look = [&](int64_t row) {
         Ahead a{row < rows && (!valid || valid[row]), -1, 0.f};
         if (dweights && row < rows && lane < k) {
             a.id = ids[row * k + lane];
-            a.dw = dweights[row * k + lane];
+            a.dw = of_slot(a.id, dweights[row * k + lane]);
         }
         return a;
     };
@@ -438,7 +439,10 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) route_rows_backward(co
                 return exp_fast(stream.element(first, id) - top) * inverse;
             };
             auto slots_after_first = [&](auto f) {
-                for (int q = lane + L; q < k; q += L) f(slot(ids[row * k + q]), dweights[row * k + q]);
+                for (int q = lane + L; q < k; q += L) {
+                    const int id = ids[row * k + q];
+                    f(slot(id), of_slot(id, dweights[row * k + q]));
+                }
             };
             if (part) {
                 first_w = slot(now.id);

@@ -199,3 +199,20 @@ def test_long_rows_through_the_whole_epilogue(dtype, rows, n_in, n_out):
     ref.within(r.out, want, 1.01 * e + unit * (z + bias.abs() + res.double().abs()) * 1.01, "out")
     off = (r.preact.double() - (z + bias)) / z
     assert abs(float(off.mean())) <= unit / 4
+
+
+@pytest.mark.parametrize("parts", [8, 130, 1100])
+@pytest.mark.parametrize("renormalize", [True, False])
+def test_the_gradient_of_a_slot_that_no_part_took_does_not_matter(parts, renormalize):
+    g = torch.Generator(device="cuda").manual_seed(55)
+    l = torch.randn(60, parts, generator=g, device="cuda")
+    l[::3] = -math.inf
+    l[::3, 5] = 1.0                                      # one part is open: slots 1 to 3 stay empty
+    l[6] = -math.inf                                     # none is
+    r = ep().ep_route(l, 4, None, renormalize)
+    assert r.ids[0].tolist() == [5, -1, -1, -1] and r.ids[6].tolist() == [-1] * 4
+    dw, dl = torch.randn(60, 4, generator=g, device="cuda"), torch.ones(1, device="cuda")
+    want = ep().ep_route_backward(l, r, torch.where(r.ids < 0, 0.0, dw), dl, None, renormalize)
+    for bad in (math.nan, math.inf, -math.inf):
+        assert torch.equal(ep().ep_route_backward(l, r, torch.where(r.ids < 0, bad, dw), dl, None, renormalize), want)
+    assert bool(torch.isfinite(want).all())
