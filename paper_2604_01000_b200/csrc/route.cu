@@ -384,12 +384,11 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) route_rows_backward(co
         int id;
         float dw;
     };
-    auto of_slot = [&](int id, float dw) { return id >= 0 && id < parts ? dw : 0.f; };   // (an empty slot's may be anything)
     auto look = [&](int64_t row) {
         Ahead a{row < rows && (!valid || valid[row]), -1, 0.f};
         if (dweights && row < rows && lane < k) {
             a.id = ids[row * k + lane];
-            a.dw = of_slot(a.id, dweights[row * k + lane]);
+            a.dw = dweights[row * k + lane];
         }
         return a;
     };
@@ -439,11 +438,9 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) route_rows_backward(co
                 return exp_fast(stream.element(first, id) - top) * inverse;
             };
             auto slots_after_first = [&](auto f) {
-                for (int q = lane + L; q < k; q += L) {
-                    const int id = ids[row * k + q];
-                    f(slot(id), of_slot(id, dweights[row * k + q]));
-                }
+                for (int q = lane + L; q < k; q += L) f(slot(ids[row * k + q]), dweights[row * k + q]);
             };
+            auto times = [](float w, float dw) { return w > 0.f ? dw * w : w; };   // (an empty slot's dw may be anything)
             if (part) {
                 first_w = slot(now.id);
                 first_id = now.id < parts ? now.id : -1;
@@ -451,15 +448,15 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) route_rows_backward(co
                     chosen = first_w;
                     slots_after_first([&](float w, float) { chosen += w; });
                 } else {
-                    pulled = now.dw * first_w;
-                    slots_after_first([&](float w, float dw) { pulled = fmaf(dw, w, pulled); });
+                    pulled = times(first_w, now.dw);
+                    slots_after_first([&](float w, float dw) { pulled += times(w, dw); });
                 }
             }
             if (renormalize) {
                 chosen = reduce_row<L, OpSum>(chosen, slots, turn);
                 if (part && chosen > 0.f) {
-                    pulled = now.dw * (first_w / chosen);
-                    slots_after_first([&](float w, float dw) { pulled = fmaf(dw, w / chosen, pulled); });
+                    pulled = times(first_w / chosen, now.dw);
+                    slots_after_first([&](float w, float dw) { pulled += times(w / chosen, dw); });
                 }
             }
             pulled = reduce_row<L, OpSum>(pulled, slots, turn);
