@@ -367,6 +367,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) route_rows_backward(co
         const double r = (double)max((long long)*routed, 1ll);
         unit = (float)((double)*dloss * (double)parts / ((double)k * r * r));
     }
+    const bool endless = !(fabsf(unit) < 1e28f);   // slopes may not be finite: a row that takes no part is not zero times them
 #pragma unroll
     for (int j = 0; j < V; ++j)
 #pragma unroll
@@ -469,6 +470,7 @@ __global__ void __launch_bounds__(THREADS, BLOCKS_PER_SM) route_rows_backward(co
             for (int i = 0; i < N; i += 2)
                 mul2(mul2(Pair(p[j][i], p[j][i + 1]), Pair(inverse)), add2(Pair(slope[j][i], slope[j][i + 1]), Pair(-back)))
                     .get(p[j][i], p[j][i + 1]);
+        if (endless && !part) Lay::set(0.f, p);
         T *to = dlogits + row * parts;
         if (mine) Lay::store(to, lane, parts, p);
         if (!dweights) continue;

@@ -216,3 +216,17 @@ def test_the_gradient_of_a_slot_that_no_part_took_does_not_matter(parts, renorma
     for bad in (math.nan, math.inf, -math.inf):
         assert torch.equal(ep().ep_route_backward(l, r, torch.where(r.ids < 0, bad, dw), dl, None, renormalize), want)
     assert bool(torch.isfinite(want).all())
+
+
+@pytest.mark.parametrize("parts", [8, 130, 1100])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_that_take_no_part_have_no_gradient_of_a_loss_that_is_not_finite(parts, dtype):
+    g = torch.Generator(device="cuda").manual_seed(56)
+    l = torch.randn(60, parts, generator=g, device="cuda").to(dtype)
+    valid = torch.ones(60, dtype=torch.uint8, device="cuda")
+    valid[::3] = 0
+    l[7] = -math.inf
+    r = ep().ep_route(l, 2, valid)
+    for bad in (math.nan, math.inf):
+        d = ep().ep_route_backward(l, r, torch.ones(60, 2, device="cuda"), torch.full((1,), bad, device="cuda"), valid)
+        assert not bool(d[::3].any()) and not bool(d[7].any()) and not bool(torch.isfinite(d[1]).all())
