@@ -34,6 +34,7 @@ static const char *const kRangeNames[EP_TIMER_COUNT] = {
 Timed::Timed(ep_ctx *c, cudaStream_t s, int t) : ctx(c), stream(s), timer(c->opt_timer_group * EP_TIMER_COUNT + t) {
     nvtxRangePushA(kRangeNames[t >= 0 && t < EP_TIMER_COUNT ? t : 0]);
     if (!ctx->opt_profile) return;
+    const std::lock_guard<std::mutex> one(ctx->timing);
     if (!ctx->spare_events.empty()) {
         start = ctx->spare_events.back();
         ctx->spare_events.pop_back();
@@ -48,6 +49,7 @@ void Timed::end(int kernels) {
     ctx->launches += kernels;
     nvtxRangePop();
     if (!start) return;
+    const std::lock_guard<std::mutex> one(ctx->timing);
     cudaEvent_t stop = nullptr;
     if (!ctx->spare_events.empty()) {
         stop = ctx->spare_events.back();
@@ -255,6 +257,7 @@ int ep_get_option(const ep_ctx *ctx, int option, int *value) {
 int ep_profile_read(ep_ctx *ctx, int timer, double *total_ms, int64_t *intervals) {
     if (!ctx || timer < 0 || timer >= 4 * EP_TIMER_COUNT) return EP_ERR_INVALID_ARG;
     DeviceGuard g(ctx->device);
+    const std::lock_guard<std::mutex> one(ctx->timing);
     double ms = 0.0;
     int64_t n = 0;
     std::vector<ep_timed_interval> keep;
@@ -277,7 +280,7 @@ int ep_profile_read(ep_ctx *ctx, int timer, double *total_ms, int64_t *intervals
     return EP_OK;
 }
 
-int64_t ep_launch_count(const ep_ctx *ctx) { return ctx ? ctx->launches : 0; }
+int64_t ep_launch_count(const ep_ctx *ctx) { return ctx ? (int64_t)ctx->launches : 0; }
 
 int ep_debug_counters(ep_ctx *ctx, int64_t *out) {
     if (!ctx || !out) return EP_ERR_INVALID_ARG;

@@ -41,6 +41,14 @@ void done(int64_t ctx, int status, const char *what = "") {
     throw py::value_error("status " + std::to_string(status));   // (not reached: the callable raises)
 }
 
+// The C call, with the interpreter's lock given up meanwhile: a launch that waits for room in the device's queue does not
+// stop the other Python threads.
+template <typename... P, typename... A>
+int unlocked(int (*f)(P...), A... args) {
+    const py::gil_scoped_release released;
+    return f(args...);
+}
+
 [[noreturn]] void refuse(const std::string &what) { throw py::value_error(what); }
 
 int type_of(ScalarType t) {
@@ -139,7 +147,7 @@ std::tuple<Tensor, Maybe, Tensor> rms_norm(int64_t ctx, int index, const Tensor 
     Maybe scale, hidden;
     if (o == at::kFloat8_e4m3fn) scale = d.empty({rows}, at::kFloat);
     if (residual) hidden = d.empty({rows, width}, t);
-    done(ctx, lib.rms_norm((ep_ctx *)ctx, ptr(x), type_of(t), ptr(residual), ptr(weight), type_of(weight), rows, (int32_t)width,
+    done(ctx, unlocked(lib.rms_norm, (ep_ctx *)ctx, ptr(x), type_of(t), ptr(residual), ptr(weight), type_of(weight), rows, (int32_t)width,
                            (float)eps, ptr(out), type_of(o), (float *)ptr(scale), ptr(hidden), d.stream()));
     return {out, scale, hidden ? *hidden : x};
 }
@@ -149,7 +157,7 @@ std::tuple<Tensor, Tensor> quantize_rows(int64_t ctx, int index, const Tensor &x
     d.matrix(x, "x", -1, -1);
     need(is_float(x.scalar_type()), "x must have dtype float32, bfloat16 or float16");
     const Tensor q = d.empty(x.sizes(), at::kFloat8_e4m3fn), scale = d.empty({x.size(0)}, at::kFloat);
-    done(ctx, lib.quantize_rows((ep_ctx *)ctx, ptr(x), type_of(x.scalar_type()), x.size(0), (int32_t)x.size(1), ptr(q),
+    done(ctx, unlocked(lib.quantize_rows, (ep_ctx *)ctx, ptr(x), type_of(x.scalar_type()), x.size(0), (int32_t)x.size(1), ptr(q),
                                 (float *)ptr(scale), d.stream()));
     return {q, scale};
 }
@@ -173,7 +181,7 @@ std::tuple<Tensor, Maybe> rms_norm_backward(int64_t ctx, int index, const Tensor
     const Tensor dx = d.empty({rows, width}, t);
     Maybe dweight;
     if (need_dweight) dweight = d.empty({width}, at::kFloat);
-    done(ctx, lib.rms_norm_backward((ep_ctx *)ctx, ptr(dout), type_of(dout.scalar_type()), ptr(hidden), type_of(t), ptr(weight),
+    done(ctx, unlocked(lib.rms_norm_backward, (ep_ctx *)ctx, ptr(dout), type_of(dout.scalar_type()), ptr(hidden), type_of(t), ptr(weight),
                                     type_of(weight), ptr(dhidden), rows, (int32_t)width, (float)eps, ptr(dx), (float *)ptr(dweight),
                                     ptr(ws), (size_t)ws.numel(), d.stream()));
     return {dx, dweight};
@@ -209,7 +217,7 @@ std::tuple<Tensor, Maybe> linear(int64_t ctx, int index, const Tensor &x, const 
     const Tensor out = d.empty({rows, n_out}, o);
     Maybe z;
     if (preact) z = d.empty({rows, n_out}, o);
-    done(ctx, lib.linear((ep_ctx *)ctx, ptr(x), row_stride(x), ptr(weight), row_stride(weight), type_of(t), (const float *)ptr(x_scale),
+    done(ctx, unlocked(lib.linear, (ep_ctx *)ctx, ptr(x), row_stride(x), ptr(weight), row_stride(weight), type_of(t), (const float *)ptr(x_scale),
                          (const float *)ptr(w_scale), ptr(bias), type_of(bias), a, ptr(residual), residual ? row_stride(*residual) : 0,
                          ptr(out), type_of(o), ptr(z), rows, (int32_t)n_in, (int32_t)n_out, ptr(ws), (size_t)ws.numel(), d.stream()));
     return {out, z};
@@ -242,7 +250,7 @@ std::tuple<Maybe, Maybe, Maybe> linear_backward(int64_t ctx, int index, const Te
     if (need_dx) dx = d.empty({rows, n_in}, t);
     if (need_dweight) dweight = d.empty({n_out, n_in}, t);
     if (need_dbias) dbias = d.empty({n_out}, at::kFloat);
-    done(ctx, lib.linear_backward((ep_ctx *)ctx, ptr(dout), type_of(dout.scalar_type()), a == EP_ACT_NONE ? nullptr : ptr(preact), a,
+    done(ctx, unlocked(lib.linear_backward, (ep_ctx *)ctx, ptr(dout), type_of(dout.scalar_type()), a == EP_ACT_NONE ? nullptr : ptr(preact), a,
                                   ptr(x), row_stride(x), ptr(weight), row_stride(weight), type_of(t), rows, (int32_t)n_in,
                                   (int32_t)n_out, ptr(dx), ptr(dweight), (float *)ptr(dbias), ptr(ws), (size_t)ws.numel(), d.stream()));
     return {dx, dweight, dbias};
@@ -267,7 +275,7 @@ std::tuple<Tensor, Tensor, Tensor, Tensor, Tensor, Tensor> route(int64_t ctx, in
     const Tensor ws = d.workspace(lib.route_bytes((ep_ctx *)ctx, rows, (int32_t)parts), "shape out of range");
     const Tensor ids = d.empty({rows, k}, at::kInt), weights = d.empty({rows, k}, at::kFloat), counts = d.empty({parts}, at::kLong),
                  prob = d.empty({parts}, at::kFloat), loss = d.empty({1}, at::kFloat), routed = d.empty({1}, at::kLong);
-    done(ctx, lib.route((ep_ctx *)ctx, ptr(logits), type_of(logits.scalar_type()), rows, (int32_t)parts, (int32_t)k,
+    done(ctx, unlocked(lib.route, (ep_ctx *)ctx, ptr(logits), type_of(logits.scalar_type()), rows, (int32_t)parts, (int32_t)k,
                         (const uint8_t *)ptr(valid), renormalize, (int32_t *)ptr(ids), (float *)ptr(weights), (int64_t *)ptr(counts),
                         (float *)ptr(prob), (float *)ptr(loss), (int64_t *)ptr(routed), ptr(ws), (size_t)ws.numel(), d.stream()));
     return {ids, weights, counts, prob, loss, routed};
@@ -292,7 +300,7 @@ Tensor route_backward(int64_t ctx, int index, const Tensor &logits, const Tensor
     d.of_type(dloss, "dloss", 1, at::kFloat);
     check_valid(d, valid, rows);
     const Tensor dlogits = d.empty({rows, parts}, logits.scalar_type());
-    done(ctx, lib.route_backward((ep_ctx *)ctx, ptr(logits), type_of(logits.scalar_type()), rows, (int32_t)parts, (int32_t)k,
+    done(ctx, unlocked(lib.route_backward, (ep_ctx *)ctx, ptr(logits), type_of(logits.scalar_type()), rows, (int32_t)parts, (int32_t)k,
                                  (const uint8_t *)ptr(valid), renormalize, (const int32_t *)ptr(ids), (const int64_t *)ptr(counts),
                                  (const int64_t *)ptr(routed), (const float *)ptr(dweights), (const float *)ptr(dloss), ptr(dlogits),
                                  d.stream()));

@@ -230,3 +230,100 @@ def test_rows_that_take_no_part_have_no_gradient_of_a_loss_that_is_not_finite(pa
     for bad in (math.nan, math.inf):
         d = ep().ep_route_backward(l, r, torch.ones(60, 2, device="cuda"), torch.full((1,), bad, device="cuda"), valid)
         assert not bool(d[::3].any()) and not bool(d[7].any()) and not bool(torch.isfinite(d[1]).all())
+
+
+def test_other_threads_run_while_a_call_waits():
+    # PyGILState_Check in the place of a C function answers 1, an error status, where the caller still holds the interpreter's lock
+    import ctypes
+
+    from paper_2604_01000_b200 import binding
+    m, x = ep(), torch.ones(4, 64, device="cuda")
+    w, h = torch.ones(8, 64, device="cuda"), torch.ones(4, 64, device="cuda")
+    calls = {"ep_rms_norm": lambda: m.ep_rms_norm(x), "ep_quantize_rows": lambda: m.ep_quantize_rows(x),
+             "ep_rms_norm_backward": lambda: m.ep_rms_norm_backward(h, x), "ep_linear": lambda: m.ep_linear(x, w),
+             "ep_linear_backward": lambda: m.ep_linear_backward(torch.ones(4, 8, device="cuda"), x, w),
+             "ep_route": lambda: m.ep_route(x), "ep_route_backward": lambda: m.ep_route_backward(x, r)}
+    r = m.ep_route(x)
+    head = binding._load_head()
+    lib = binding.load_library()
+    real = {n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in binding._HEAD_CALLS}
+    held = ctypes.cast(ctypes.pythonapi.PyGILState_Check, ctypes.c_void_p).value
+    try:
+        for name, call in calls.items():
+            head.bind(dict(real, **{name: held}), binding._raise_status)
+            call()
+    finally:
+        head.bind(real, binding._raise_status)
+    assert torch.equal(m.ep_route(x).ids, r.ids)
+
+
+def test_two_threads_on_two_streams_of_one_context():
+    import threading
+
+    m, ctx = ep(), ep().default_context()
+    g = torch.Generator(device="cuda").manual_seed(58)
+    sets = []
+    for n in (3000, 4001):
+        x, w = torch.randn(n, 192, generator=g, device="cuda").to(BF16), torch.randn(96, 192, generator=g, device="cuda").to(BF16)
+        sets.append((x, w))
+
+    def passes(x, w):
+        n = m.ep_rms_norm(x)
+        y = m.ep_linear(n.out, w, None, "gelu", preact=True)
+        r = m.ep_route(y.out, 2)
+        d = m.ep_linear_backward(m.ep_route_backward(y.out, r, r.weights, r.loss), n.out, w, y.preact, "gelu")
+        return [*y, *r, *d, m.ep_rms_norm_backward(d.dx, n.hidden).dx]
+    alone = [passes(*s) for s in sets]
+    torch.cuda.synchronize()
+    before, got, failed = ctx.launch_count(), [None, None], []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(50):
+                    got[i] = passes(*sets[i])
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:   # noqa: BLE001
+            failed.append(e)
+    ctx.set_profile(True)
+    try:
+        threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+    finally:
+        times = [ctx.profile_read(name) for name in ("norm", "linear", "route")]
+        ctx.set_profile(False)
+    assert not failed, failed
+    for a, b in zip(alone, got):
+        for p, q in zip(a, b):
+            assert torch.equal(p, q)
+    assert [n for _, n in times] == [200, 200, 200] and all(ms > 0 for ms, _ in times)
+    single = ctx.launch_count()
+    for s in sets:
+        passes(*s)
+    assert single - before == 50 * (ctx.launch_count() - single)
+    ctx.check()
+
+
+def test_calls_inside_a_cuda_graph():
+    m = ep()
+    g = torch.Generator(device="cuda").manual_seed(59)
+    x, w = torch.randn(3000, 100, generator=g, device="cuda").to(F16), torch.randn(60, 100, generator=g, device="cuda").to(F16)
+
+    def passes():
+        n = m.ep_rms_norm(x)
+        y = m.ep_linear(n.out, w, None, "silu", preact=True)
+        r = m.ep_route(y.out, 2, None, True)
+        d = m.ep_linear_backward(m.ep_route_backward(y.out, r, r.weights, r.loss, None, True).float(), n.out, w, y.preact, "silu")
+        return [*y, *r, *d, *m.ep_rms_norm_backward(d.dx, n.hidden)]
+    passes()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = passes()
+    x.copy_(torch.randn(3000, 100, generator=g, device="cuda"))
+    graph.replay()
+    for a, b in zip(passes(), got):
+        assert torch.equal(a, b)
