@@ -2,6 +2,7 @@
 from __future__ import annotations
 
 import ctypes
+import functools
 import importlib.machinery
 import importlib.util
 import os
@@ -263,8 +264,13 @@ class Context:
             raise EmbedPartError(rc, self._lib.ep_status_string(rc).decode())
         self._h = h
         self._address = h.value
-        self._head = _load_head()
         self._ws: Optional[torch.Tensor] = None
+
+    @functools.cached_property
+    def _head(self):
+        # at the first call of an operator that needs it: the extension is linked to torch's own libraries, and clustering,
+        # quality and reordering need no more than the CUDA library
+        return _load_head()
 
     def close(self):
         if getattr(self, "_h", None):

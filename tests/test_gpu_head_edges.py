@@ -327,3 +327,17 @@ def test_calls_inside_a_cuda_graph():
     graph.replay()
     for a, b in zip(passes(), got):
         assert torch.equal(a, b)
+
+
+def test_clustering_works_without_the_heads_extension(monkeypatch):
+    from paper_2604_01000_b200 import binding
+    monkeypatch.setattr(binding, "_head", None)
+    monkeypatch.setattr(binding, "_PKG", "/nonexistent")
+    ctx = binding.Context(0)
+    try:
+        x = torch.randn(500, 16, device="cuda")
+        assert ctx.kmeans(x, 4, 2, x[:4].contiguous()).assign.shape == (500,)
+        with pytest.raises(FileNotFoundError):
+            ctx.route(x)
+    finally:
+        ctx.close()
