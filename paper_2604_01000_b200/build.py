@@ -1,9 +1,11 @@
 """Builds libembedpart.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _head.so beside it."""
 from __future__ import annotations
 
+import importlib.metadata
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -25,7 +27,6 @@ HEAD = os.path.join(PKG, "_head.so")                      # tensor marshalling o
 
 def head_commands():
     """(compile, link) of _head.so: host code against torch's own headers and libraries."""
-    import sysconfig
     import torch
     base = os.path.dirname(torch.__file__)
     lib = os.path.join(base, "lib")
@@ -38,6 +39,11 @@ def head_commands():
              *inc, "-c", os.path.join(CSRC, "head_binding.cpp"), "-o", obj],
             [cxx, "-shared", obj, "-L", lib, "-Wl,-rpath," + lib, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch",
              "-ltorch_python", "-o"])
+
+
+def head_stamp():
+    """What _head.so is built for, besides its sources: another torch or Python has another binary interface."""
+    return "torch %s, python %s, %s" % (importlib.metadata.version("torch"), sysconfig.get_config_var("SOABI"), os.environ.get("CXX", "g++"))
 
 
 def sources():
@@ -70,10 +76,13 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
                 cmd.insert(1, "-Xptxas=-v")
             jobs.append(cmd)
 
-    head_src = os.path.join(CSRC, "head_binding.cpp")
-    head_new = not debug and (force or not os.path.exists(HEAD) or os.path.getmtime(HEAD) < max(os.path.getmtime(head_src), hdr))
-    if head_new:
-        jobs.append(head_commands()[0])
+    # the head's extension, the same beside either library
+    mark, stamp = os.path.join(globals()["OBJ"], "head_binding.stamp"), head_stamp()
+    head_new = force or not os.path.exists(HEAD) or os.path.getmtime(HEAD) < max(os.path.getmtime(os.path.join(CSRC, "head_binding.cpp")), hdr)
+    if not head_new:
+        head_new = not os.path.exists(mark) or open(mark).read() != stamp
+    head_jobs = [head_commands()[0]] if head_new else []
+    os.makedirs(globals()["OBJ"], exist_ok=True)
 
     def run(cmd):
         r = subprocess.run(cmd, capture_output=True, text=True)
@@ -81,8 +90,8 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
             raise RuntimeError("compiler failed: %s\n%s\n%s" % (" ".join(cmd), r.stdout, r.stderr))
         return r.stderr
 
-    with ThreadPoolExecutor(max_workers=max(1, min(8, len(jobs)))) as ex:
-        for log in ex.map(run, jobs):
+    with ThreadPoolExecutor(max_workers=max(1, min(8, len(jobs + head_jobs)))) as ex:
+        for log in ex.map(run, jobs + head_jobs):
             if verbose and log:
                 print(log, file=sys.stderr)
     if jobs or not os.path.exists(LIB):
@@ -94,6 +103,8 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
         tmp = HEAD + ".tmp.%d" % os.getpid()
         run([*head_commands()[1], tmp])
         os.replace(tmp, HEAD)
+        with open(mark, "w") as f:
+            f.write(stamp)
     return LIB
 
 
