@@ -237,19 +237,6 @@ def _context_of(t) -> "Context":
     return _default.get(idx) or default_context(idx if idx >= 0 else None)
 
 
-def _row_stride(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
-
-
-def _type_of(t: Optional[torch.Tensor]) -> int:
-    return 0 if t is None else TYPES[t.dtype]
-
-
-def _aligned(*ts: torch.Tensor) -> bool:
-    """Whether every matrix starts on a 16-byte boundary with rows a multiple of 16 bytes apart."""
-    return all(t.data_ptr() % 16 == 0 and _row_stride(t) * t.element_size() % 16 == 0 for t in ts)
-
-
 class Context:
     """Owns an ep_ctx for one device and a grow-only workspace tensor."""
 
