@@ -951,6 +951,19 @@ __global__ void __launch_bounds__(256) linear_join(const float *shares, int spli
 }
 
 // ---------------------------------------------------------------------------------------------- few rows
+// The sum of lane r's row: NaN where it is infinite because a number of that row of x, or of w, is.  (Rare, and kept out of
+// the way of what is not: written out in the kernel it made 8 rows of 1024 8 % slower.)
+__device__ __noinline__ float nan_of_infinities(float sum, const float *x, int64_t ldx, const float *w, int n_in) {
+    const int lane = threadIdx.x & 31;
+    for (unsigned left = __ballot_sync(FULL, isinf(sum)); left; left &= left - 1) {
+        const int r = __ffs(left) - 1;
+        bool infinite = false;
+        for (int c = lane; c < n_in; c += 32) infinite |= isinf(x[r * ldx + c]) || isinf(w[c]);
+        if (__any_sync(FULL, infinite) && lane == r) sum = CUDART_NAN_F;
+    }
+    return sum;
+}
+
 // Dot products: `share` warps of a block (1, 2, 4 or 8 of its 8) to one column of ROWS rows.  Their lanes share out the row
 // of W, in 16-byte chunks (VEC) or, where it is not aligned for that, element by element next to one another; W is read
 // once, x comes from the L1.  Sums are fp32 multiply-adds to nearest, so all types are exact to fp32 here.
@@ -997,13 +1010,8 @@ __global__ void __launch_bounds__(256) linear_few_rows(const T *__restrict__ x, 
     if constexpr (sizeof(T) == 4) {
         // The tiles split fp32 numbers, and an infinity splits into NaN: so it does here.  A sum is only infinite where an
         // operand is, or where it overflows, which stays an infinity.
-        if (col < e.N && mine == 0)
-            for (unsigned left = __ballot_sync(FULL, lane < ROWS && lane < e.M && isinf(v[0])); left; left &= left - 1) {
-                const int r = __ffs(left) - 1;
-                bool infinite = false;
-                for (int c = lane; c < n_in; c += 32) infinite |= isinf(x[r * ldx + c]) || isinf(w[col * ldw + c]);
-                if (__any_sync(FULL, infinite) && lane == r) v[0] = CUDART_NAN_F;
-            }
+        if (col < e.N && mine == 0 && __builtin_expect(__any_sync(FULL, isinf(v[0])), 0))
+            v[0] = nan_of_infinities(v[0], x, ldx, w + col * ldw, n_in);
     }
     if (col < e.N && mine == 0 && lane < ROWS && lane < e.M) {
         Columns<1> c;
