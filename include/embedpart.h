@@ -387,10 +387,10 @@ int ep_cluster_and_balance(ep_ctx *ctx, const float *emb, int64_t N, int32_t d, 
  *   hidden   [dev] out or NULL, rows x d of x_type: h (may be the same buffer as x or residual)
  *   eps      >= 0, finite.  The norm is taken of the fp32 sum, before hidden is rounded.
  * A row of zeros comes out as zeros, with eps = 0 too.  A row that holds a NaN comes out as NaN (scale included), one that
- * holds an infinity as NaN there and zero elsewhere.
+ * holds an infinity as NaN there and zero elsewhere, in 8 bits as NaN throughout (scale included).
  *
  * ep_quantize_rows: the 8-bit output on its own: q = x / scale, scale as above (weights and inputs of the
- * 8-bit form of ep_linear).
+ * 8-bit form of ep_linear).  A row that holds an infinity has an infinite scale and stands for NaN throughout.
  *
  * ep_rms_norm_backward: with rho = 1 / sqrt(mean(h^2) + eps), a = weight * dout:
  *   dx = rho (a - h rho^2 mean(a h)) + dhidden      (the gradient of x and, alike, of residual)

@@ -734,7 +734,8 @@ class Context:
     # Matrices are contiguous CUDA tensors on this device (x, weight and residual of linear may have strided rows); a
     # wrong type, shape or device raises ValueError, what the library refuses EmbedPartError.  Each call's workspace is
     # its own, ordered by the current stream, so calls on several streams, and from several threads, may overlap; the
-    # interpreter's lock is given up during the call of the library.
+    # interpreter's lock is given up during the call of the library.  None of them records a gradient for torch's autograd: what
+    # they return does not require one, whatever their inputs do, and the *_backward calls are made by hand.
     def rms_norm(self, x, weight=None, residual=None, eps: float = 1e-6, out_dtype=None) -> "NormResult":
         """weight * h / sqrt(mean(h^2) + eps) with h = x + residual; see ep_rms_norm."""
         return NormResult(*self._head.rms_norm(self._address, self.device.index, x, weight, residual, eps, out_dtype))

@@ -341,3 +341,21 @@ def test_clustering_works_without_the_heads_extension(monkeypatch):
             ctx.route(x)
     finally:
         ctx.close()
+
+
+@pytest.mark.parametrize("d", [40, 64, 2048])
+def test_infinities_in_8_bits(d):
+    x = torch.randn(5, d, generator=torch.Generator(device="cuda").manual_seed(60), device="cuda")
+    x[1, 3], x[3, d - 1] = math.inf, -math.inf
+    n, q = ep().ep_rms_norm(x, out_dtype=torch.float8_e4m3fn), ep().ep_quantize_rows(x)
+    for row in (1, 3):
+        assert bool(torch.isnan(n.out[row].float()).all()) and bool(torch.isnan(n.scale[row]))
+        assert bool(torch.isnan(q.q[row].float() * q.scale[row]).all()) and math.isinf(float(q.scale[row]))
+    for row in (0, 2, 4):
+        assert bool(torch.isfinite(n.out[row].float()).all()) and bool(torch.isfinite(q.q[row].float()).all())
+
+
+def test_no_gradient_is_recorded():
+    x, w = torch.ones(4, 16, device="cuda", requires_grad=True), torch.ones(8, 16, device="cuda", requires_grad=True)
+    assert not ep().ep_linear(x, w).out.requires_grad and not ep().ep_rms_norm(x).out.requires_grad
+    assert not ep().ep_route(x).weights.requires_grad
