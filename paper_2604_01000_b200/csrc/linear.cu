@@ -12,8 +12,9 @@
 //
 // Measured: 8192 x 4096 x 4096 fp16 193 us, 1430 TFLOP/s (tensor pipe 90 % busy; cuBLAS alone reaches 1669 in short bursts);
 // 2000 x 4096 x 4096 in 8 bits 31 us, 2150 TFLOP/s (1.7 waves of tiles, so 2); 169343 x 128 -> 512 bf16 41 us, 5.3 TB/s of
-// 6.5, with z kept 76 us, 5.2 TB/s; backward of 232965 x 256 x 256 bf16 through GELU 152 us: dz 60, dx 44, dW 46 and its
-// join 7, against 74 us for reading and writing everything once; one row of 1024 x 1024 3 us.
+// 6.5, with z kept 76 us, 5.2 TB/s; backward of 232965 x 256 x 256 bf16 through GELU 155 us: dz 62, dx 44, dW 46 and its
+// join 7, against 74 us for reading and writing everything once; one row of 1024 x 1024 3 us.  fp32 by six bf16 products:
+// 8192 x 4096 x 4096 1266 us, 217 TFLOP/s of 278 (a sixth of bf16's); 169343 x 128 -> 512 219 us.
 #include "ep_common.cuh"
 #include "rows.cuh"
 #include "tc_device.cuh"
@@ -344,7 +345,8 @@ struct GemmShared {
 // The shared memory of a block: ring of operand stages, then per epilogue warp room for chunks on their way out.
 // The epilogue's instructions follow one another closely (sum, bias, activation, store), so it takes warps to fill a
 // scheduler: 16 where every one of them still has 32 columns (169343 x 128 -> 512 bf16: 41 us against 51 with 8, through
-// GELU and with a residual 95 against 137).
+// GELU and with a residual 95 against 137; all of 16-bit outputs).  18 warps leave a thread 96 registers, which sums in
+// runs exceed: the kernel of split fp32 in pairs spills 336 bytes, two others of fp32 outputs 12.
 template <int BN, int PARTS, bool PAIR>
 struct TileMemory {
     static constexpr int EPI_WARPS = BN >= 128 ? 16 : 8;
@@ -1133,8 +1135,10 @@ struct Peaks {   // NULL: dz is written as it is
 };
 
 // dz = dout act'(z), written for the products (16 bits as they are, fp32 as three bf16 parts; rows ld_to apart, zero
-// beyond N), and the sums of its columns over this block's rows: part[blockIdx.y][N].  232965 x 256 bf16 through GELU:
-// 60 us, 6.0 TB/s, with instruction issue close behind (23 an element).
+// beyond N), and the sums of its columns over this block's rows: part[blockIdx.y][N].  One rounding of dz to the operands'
+// 16 bits, because the tensor core takes nothing wider beside them: it makes the products' error 1.4 times what rounding
+// them alone leaves (0.0023 for 0.0017 of bf16), and two parts would move ten bytes for seven.  232965 x 256 bf16 through
+// GELU: 62 us, 5.8 TB/s, with instruction issue close behind (25 an element).
 constexpr int DZ_CHUNKS = 16, DZ_ROWS = 16;   // a block covers 128 columns, 16 rows at a time
 constexpr int DZ_THREADS = DZ_CHUNKS * DZ_ROWS;
 constexpr int DZ_STAGES = 4;                  // rows in flight per thread and one more (see the ring in rows.cuh)
@@ -1271,7 +1275,7 @@ constexpr int MAX_WIDTH = 65536;
 // Whether the dot products serve rows x n_in -> n_out, and not the tiles.  They go by the CUDA cores, about 4 products a
 // picosecond: up to 2^24 products they are the faster ones (1024 x 1024 bf16: 8 rows in 4.8 us against 6.0; 4096 x 4096:
 // 1 row 6.9 against 10.0, 2 rows 12.3 against 10.0).  fp32 operands would first have to be split (4096 x 4096: 8 rows
-// 40 us against 65), so there they serve every call of up to 8 rows.
+// 38 us against 76), so there they serve every call of up to 8 rows.
 constexpr int FEW_ROWS = 8;
 bool few_rows(int64_t rows, int n_in, int n_out, int type) {
     return rows <= FEW_ROWS && (type == EP_F32 || rows * n_in * n_out <= (1ll << 24));

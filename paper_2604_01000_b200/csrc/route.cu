@@ -7,8 +7,8 @@
 // order.  One block (few rows) needs neither: it writes the results itself.
 //
 // Measured: 2449029 rows of 32 fp32 logits, k = 1: 75 us, 4.4 TB/s (68 us the pass, 8 the fold), bound by instruction issue
-// (19 instructions a logit, 0.7 issued a clock and scheduler); backward of 169343 x 257 bf16, k = 8: 84 us, 2.3 TB/s, bound
-// alike: rows of 514 bytes start anywhere, so that logits are picked and stored one by one; one row of 64: 4 us.
+// (19 instructions a logit, 0.7 issued a clock and scheduler); backward of 169343 x 257 bf16, k = 8, renormalised: 85 us, 2.2 TB/s
+// (78 not renormalised: the divisions and one sum more make a row's only weight a constant exactly), bound alike: rows of 514 bytes start anywhere, so that logits are picked and stored one by one; one row of 64: 4 us.
 #include "ep_common.cuh"
 #include "rows.cuh"
 
