@@ -87,7 +87,9 @@ enum {
     EP_TIMER_NORM = 9,           /* ep_rms_norm, ep_rms_norm_backward, ep_quantize_rows */
     EP_TIMER_LINEAR = 10,        /* all kernels of ep_linear and ep_linear_backward */
     EP_TIMER_ROUTE = 11,         /* all kernels of ep_route and ep_route_backward */
-    EP_TIMER_COUNT = 12
+    EP_TIMER_ENTROPY = 12,       /* all kernels of ep_cross_entropy and ep_cross_entropy_backward */
+    EP_TIMER_EXPERTS = 13,       /* all kernels of ep_experts */
+    EP_TIMER_COUNT = 14
 };
 
 /* Element types of the partition head's operators (ep_rms_norm, ep_linear, ep_route and their gradients). */
@@ -492,6 +494,48 @@ int ep_route(ep_ctx *ctx, const void *logits, int32_t type, int64_t rows, int32_
 int ep_route_backward(ep_ctx *ctx, const void *logits, int32_t type, int64_t rows, int32_t parts, int32_t k,
                       const uint8_t *valid, int32_t renormalize, const int32_t *ids, const int64_t *counts,
                       const int64_t *routed, const float *dweights, const float *dloss, void *dlogits, void *cuda_stream);
+
+/* --------------------------------------------------------------------------------------------
+ * ep_cross_entropy -- softmax cross entropy of x W^T + bias over many classes; the logits are never kept.
+ *
+ *   l = x W^T + bias;  lse[r] = log sum_c exp(l[r][c]);  row_loss[r] = lse[r] - l[r][targets[r]];
+ *   counted = R rows that take part;  loss = sum of row_loss / R
+ * (A head that names a row's cluster as ep_kmeans found it, or, with a class for every vertex, its neighbour.)
+ *
+ *   x        [dev] rows x n_in of in_type (EP_F32 / EP_BF16 / EP_F16), row i at element i * ldx (ldx >= n_in; ldw alike)
+ *   w        [dev] classes x n_in of in_type;  1 <= n_in <= 65536, 1 <= classes <= 2^24, 0 <= rows <= 2^31 - 256
+ *   bias     [dev] classes of bias_type (EP_F32 / EP_BF16 / EP_F16) or NULL; -infinity closes a class
+ *   targets  [dev] rows int32: the row's class, or -1: the row takes no part, whatever x holds there.  Others
+ *            raise EP_ERR_BAD_INDEX in the device status word and count as -1
+ *   loss     [dev] out, 1 fp32;  row_loss, lse [dev] out, rows fp32 each (0 in rows without a class)
+ *   counted  [dev] out, 1 int64
+ *   aligned  (of the queries) as for ep_linear
+ * A row whose every class is closed takes no part either (row_loss 0, lse -infinity).  A target that is closed while others are
+ * not has row_loss infinity.  A NaN or +infinity among the logits of a row that takes part makes its lse and loss
+ * NaN.  With R = 0 loss is 0.  The logits are summed in fp32 as ep_linear sums them for an EP_F32 output; EP_F32 inputs are split
+ * as there (an infinity in x or w of EP_F32 makes the logits it reaches NaN).
+ *
+ * ep_cross_entropy_backward:  G = (exp(l - lse) - [c = target]) g,  g[r] = dloss / R + drow_loss[r], 0 in rows that
+ * take no part;  dx = G W;  dweight = G^T x;  dbias = sum over rows of G
+ *   x, w, bias, targets: as the forward took them;  lse, counted: what it returned
+ *   dloss     [dev] 1 fp32 or NULL (zero);  drow_loss [dev] rows fp32 or NULL (zero)
+ *   dx        [dev] out or NULL, rows x n_in of in_type;  dweight [dev] out or NULL, classes x n_in of in_type
+ *   dbias     [dev] out or NULL, classes fp32
+ * The logits are made once more, a piece at a time.  G is rounded to in_type before the products of 16-bit types, for EP_F16
+ * after multiplication by the power of two that brings the largest |g| to 2^14 (the sums are scaled back): elements below
+ * 2^-39 of that largest are lost.
+ */
+size_t ep_cross_entropy_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t n_in, int32_t classes, int32_t in_type,
+                                        int32_t aligned);   /* 0 = invalid shape or type; at least 256 */
+int ep_cross_entropy(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int64_t ldw, int32_t in_type, const void *bias,
+                     int32_t bias_type, const int32_t *targets, int64_t rows, int32_t n_in, int32_t classes, float *loss,
+                     float *row_loss, float *lse, int64_t *counted, void *workspace, size_t workspace_bytes, void *cuda_stream);
+size_t ep_cross_entropy_backward_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t n_in, int32_t classes, int32_t in_type,
+                                                 int32_t aligned);
+int ep_cross_entropy_backward(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int64_t ldw, int32_t in_type, const void *bias,
+                              int32_t bias_type, const int32_t *targets, const float *lse, const int64_t *counted, const float *dloss,
+                              const float *drow_loss, int64_t rows, int32_t n_in, int32_t classes, void *dx, void *dweight,
+                              float *dbias, void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /* --------------------------------------------------------------------------------------------
  * Host-buffer variants.  Same operations and the same kernels; inputs and outputs are [host]

@@ -23,6 +23,9 @@ from .binding import (  # noqa: F401
     ep_route,
     ep_route_backward,
     RouteResult,
+    ep_cross_entropy,
+    ep_cross_entropy_backward,
+    CrossEntropyResult,
     library_path,
     load_library,
     EXPORTED_SYMBOLS,

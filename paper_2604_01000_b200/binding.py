@@ -29,6 +29,7 @@ EXPORTED_SYMBOLS = (
     "ep_rms_norm", "ep_quantize_rows", "ep_rms_norm_backward_workspace_bytes", "ep_rms_norm_backward",
     "ep_linear_workspace_bytes", "ep_linear", "ep_linear_backward_workspace_bytes", "ep_linear_backward",
     "ep_route_workspace_bytes", "ep_route", "ep_route_backward",
+    "ep_cross_entropy_workspace_bytes", "ep_cross_entropy", "ep_cross_entropy_backward_workspace_bytes", "ep_cross_entropy_backward",
 )
 
 EP_OK = 0
@@ -38,9 +39,10 @@ EP_OPT_TIMER_GROUP = 3
 EP_OPT_KMEANS_CAND_MB = 4
 EP_OPT_QUALITY_SLICE_KB = 5
 EP_OPT_KMEANS_ITERATIONS_PER_LAUNCH = 6
-TIMER_COUNT = 12
+TIMER_COUNT = 14
 TIMERS = {"kmeans_assign": 0, "kmeans_update": 1, "edge_cut": 2, "quality_prep": 3, "reorder": 4,
-          "kmeans_resolve": 5, "graph_bandwidth": 6, "relabel": 7, "balance": 8, "norm": 9, "linear": 10, "route": 11}
+          "kmeans_resolve": 5, "graph_bandwidth": 6, "relabel": 7, "balance": 8, "norm": 9, "linear": 10, "route": 11,
+          "entropy": 12, "experts": 13}
 KMEANS_PATHS = {"auto": 0, "simt": 1, "tensor": 2}
 
 
@@ -184,6 +186,15 @@ def load_library() -> ctypes.CDLL:
             lib.ep_route.restype = ctypes.c_int
             lib.ep_route_backward.argtypes = [vp, vp, i32, i64, i32, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp]
             lib.ep_route_backward.restype = ctypes.c_int
+            lib.ep_cross_entropy_workspace_bytes.argtypes = [vp, i64, i32, i32, i32, i32]
+            lib.ep_cross_entropy_workspace_bytes.restype = sz
+            lib.ep_cross_entropy.argtypes = [vp, vp, i64, vp, i64, i32, vp, i32, vp, i64, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+            lib.ep_cross_entropy.restype = ctypes.c_int
+            lib.ep_cross_entropy_backward_workspace_bytes.argtypes = [vp, i64, i32, i32, i32, i32]
+            lib.ep_cross_entropy_backward_workspace_bytes.restype = sz
+            lib.ep_cross_entropy_backward.argtypes = [vp, vp, i64, vp, i64, i32, vp, i32, vp, vp, vp, vp, vp, i64, i32, i32, vp, vp, vp,
+                                                      vp, sz, vp]
+            lib.ep_cross_entropy_backward.restype = ctypes.c_int
             _lib = lib
     return _lib
 
@@ -191,7 +202,9 @@ def load_library() -> ctypes.CDLL:
 _head = None
 _HEAD_CALLS = ("ep_rms_norm", "ep_quantize_rows", "ep_rms_norm_backward_workspace_bytes", "ep_rms_norm_backward",
                "ep_linear_workspace_bytes", "ep_linear", "ep_linear_backward_workspace_bytes", "ep_linear_backward",
-               "ep_route_workspace_bytes", "ep_route", "ep_route_backward")
+               "ep_route_workspace_bytes", "ep_route", "ep_route_backward",
+               "ep_cross_entropy_workspace_bytes", "ep_cross_entropy", "ep_cross_entropy_backward_workspace_bytes",
+               "ep_cross_entropy_backward")
 
 
 def _raise_status(ctx: int, status: int, what: str = ""):
@@ -773,6 +786,19 @@ class Context:
         return self._head.route_backward(self._address, self.device.index, logits, result.ids, result.counts, result.routed,
                                          dweights, dloss, valid, renormalize)
 
+    def cross_entropy(self, x, weight, targets, bias=None) -> "CrossEntropyResult":
+        """Softmax cross entropy of x weight^T + bias, without keeping the logits; targets: int32, -1 = the row takes no
+        part; see ep_cross_entropy."""
+        return CrossEntropyResult(*self._head.cross_entropy(self._address, self.device.index, x, weight, targets, bias))
+
+    def cross_entropy_backward(self, x, weight, targets, result: "CrossEntropyResult", bias=None, dloss=None, drow_loss=None,
+                               need_dx: bool = True, need_dweight: bool = True, need_dbias: bool = True) -> "LinearGradients":
+        """Gradients of x, weight and bias from that of the mean loss, of each row's or both; x, weight, targets and bias as the
+        forward took them, result what it returned; see ep_cross_entropy_backward."""
+        return LinearGradients(*self._head.cross_entropy_backward(self._address, self.device.index, x, weight, targets, result.lse,
+                                                                  result.counted, bias, dloss, drow_loss, need_dx, need_dweight,
+                                                                  need_dbias))
+
 
 class KMeansResult(NamedTuple):
     assign: torch.Tensor                 # int32 [N]
@@ -830,6 +856,13 @@ class RouteResult(NamedTuple):
     prob: torch.Tensor                   # float32 [parts]: mean probability over the routed rows
     loss: torch.Tensor                   # float32 [1]: the balance loss
     routed: torch.Tensor                 # int64 [1]: rows that took part
+
+
+class CrossEntropyResult(NamedTuple):
+    loss: torch.Tensor                   # float32 [1]: mean over the rows that take part
+    row_loss: torch.Tensor               # float32 [rows]
+    lse: torch.Tensor                    # float32 [rows]: what the backward pass takes
+    counted: torch.Tensor                # int64 [1]: rows that took part
 
 
 _default: dict[int, Context] = {}
@@ -902,6 +935,17 @@ def ep_route(logits, k=1, valid=None, renormalize=False) -> RouteResult:
 def ep_route_backward(logits, result, dweights=None, dloss=None, valid=None, renormalize=False) -> torch.Tensor:
     """Gradient of ep_route's logits."""
     return _context_of(logits).route_backward(logits, result, dweights, dloss, valid, renormalize)
+
+
+def ep_cross_entropy(x, weight, targets, bias=None) -> CrossEntropyResult:
+    """Softmax cross entropy of x weight^T + bias over many classes, without keeping the logits."""
+    return _context_of(x).cross_entropy(x, weight, targets, bias)
+
+
+def ep_cross_entropy_backward(x, weight, targets, result, bias=None, dloss=None, drow_loss=None, need_dx=True, need_dweight=True,
+                              need_dbias=True) -> LinearGradients:
+    """Gradients of ep_cross_entropy."""
+    return _context_of(x).cross_entropy_backward(x, weight, targets, result, bias, dloss, drow_loss, need_dx, need_dweight, need_dbias)
 
 
 REORDER_STATIC_MAX_N = 1 << 22

@@ -29,7 +29,8 @@ int cuda_fail(ep_ctx *ctx, cudaError_t e, const char *what) {
 // nothing while no tool is attached).
 static const char *const kRangeNames[EP_TIMER_COUNT] = {
     "ep:kmeans assign", "ep:kmeans update", "ep:edge cut", "ep:quality prep", "ep:reorder",
-    "ep:kmeans resolve", "ep:graph bandwidth", "ep:relabel", "ep:balance", "ep:norm", "ep:linear", "ep:route"};
+    "ep:kmeans resolve", "ep:graph bandwidth", "ep:relabel", "ep:balance", "ep:norm", "ep:linear", "ep:route",
+    "ep:cross entropy", "ep:experts"};
 
 Timed::Timed(ep_ctx *c, cudaStream_t s, int t) : ctx(c), stream(s), timer(c->opt_timer_group * EP_TIMER_COUNT + t) {
     nvtxRangePushA(kRangeNames[t >= 0 && t < EP_TIMER_COUNT ? t : 0]);

@@ -196,6 +196,43 @@ inline bool float_type(int type) { return type == EP_F32 || type == EP_BF16 || t
 // out[c] = sum of parts[r][c] over r = 0..n-1, in ascending order of fixed groups of r (fp64 inside).
 int sum_partials(ep_ctx *ctx, const float *parts, int n, int cols, float *out, cudaStream_t stream);
 
+// An operand as the tile kernel of linear.cu reads it: `parts` matrices [rows][cols], rows ld elements apart.
+struct Operand {
+    const void *base;
+    int type;             // EP_BF16, EP_F16, EP_E4M3 or EP_I8
+    int64_t rows;
+    int cols;
+    int64_t ld;
+    int parts;
+    int64_t part_stride;
+};
+// The copy of an operand that TMA can read: fp32 always (three bf16 parts), others when unaligned.
+struct Packed {
+    int ld, parts, type;
+    int64_t part_stride;
+    size_t bytes;
+};
+Packed packed_form(int64_t rows, int cols, int type);
+struct Matrix {
+    const void *base;   // NULL: not wanted
+    int64_t ld, rows;
+    int cols;
+    void *room;         // for its copy
+};
+// Two matrices copied into that form, in one launch.
+int make_operands(ep_ctx *ctx, const Matrix &first, const Matrix &second, int type, cudaStream_t stream, Operand *a, Operand *b,
+                  int *kernels);
+// out[M][N] = A B^T (+ what out holds, if accumulate) for the other files; *_mn: the operand is stored along its own rows, K of
+// them.  An operand with fewer than M or N rows counts as zero there.  factor: of fp16 results, a device value that the sums
+// are multiplied by, or NULL.  type: the operands' (EP_F32 where they have three parts).
+size_t product_bytes(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, int out_type);
+int product(ep_ctx *ctx, const Operand &a, bool a_mn, const Operand &b, bool b_mn, int64_t M, int N, int64_t K, void *out, int out_type,
+            bool accumulate, const float *factor, float *share, cudaStream_t stream, int *kernels);
+// The same of two operands that are stored along their own rows; B is other_b where the device value *other is not 0.
+int product_of_either(ep_ctx *ctx, const Operand &a, const Operand &b, const Operand &other_b, const int *other, int64_t M, int N,
+                      int64_t K, void *out, int out_type, bool accumulate, const float *factor, float *share, cudaStream_t stream,
+                      int *kernels);
+
 }  // namespace ep
 
 // ---- device helpers -------------------------------------------------------------------------------

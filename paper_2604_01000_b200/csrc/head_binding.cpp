@@ -1,5 +1,5 @@
 // Tensors in, tensors out for the partition head's operators: the checks, the allocations and the calls of the C ABI
-// (include/embedpart.h) for Context.rms_norm, .linear, .route and their gradients, compiled, because for one row
+// (include/embedpart.h) for Context.rms_norm, .linear, .route, .cross_entropy and their gradients, compiled, because for one row
 // marshalling is most of such a call (measured for routing one row: 22 us through ctypes, of which 6 us the C call).
 // The C functions are handed over as addresses of the library that the package has loaded.
 #include <ATen/core/Tensor.h>
@@ -32,6 +32,10 @@ struct Library {
     decltype(&ep_route_workspace_bytes) route_bytes;
     decltype(&ep_route) route;
     decltype(&ep_route_backward) route_backward;
+    decltype(&ep_cross_entropy_workspace_bytes) cross_entropy_bytes;
+    decltype(&ep_cross_entropy) cross_entropy;
+    decltype(&ep_cross_entropy_backward_workspace_bytes) cross_entropy_backward_bytes;
+    decltype(&ep_cross_entropy_backward) cross_entropy_backward;
 } lib{};
 PyObject *raise_status = nullptr;   // (context address, status, text or "") -> raises the package's exception
 
@@ -307,6 +311,64 @@ Tensor route_backward(int64_t ctx, int index, const Tensor &logits, const Tensor
     return dlogits;
 }
 
+// The inputs that both passes of the cross entropy take: checked alike.
+struct EntropyInputs {
+    int64_t rows, n_in, classes;
+    ScalarType type;
+    bool aligned;
+    EntropyInputs(const Device &d, const Tensor &x, const Tensor &weight, const Tensor &targets, const Maybe &bias) {
+        d.matrix(x, "x", -1, -1, true);
+        type = x.scalar_type();
+        need(is_float(type), "x must have dtype float32, bfloat16 or float16");
+        rows = x.size(0), n_in = x.size(1);
+        d.matrix(weight, "weight", -1, n_in, true);
+        need(weight.scalar_type() == type, "weight must have x's dtype");
+        classes = weight.size(0);
+        need(classes <= Device::most, "weight has too many rows");
+        d.of_type(targets, "targets", rows, at::kInt);
+        d.floats(bias, "bias", classes);
+        aligned = sixteen(x) && sixteen(weight);
+    }
+};
+
+std::tuple<Tensor, Tensor, Tensor, Tensor> cross_entropy(int64_t ctx, int index, const Tensor &x, const Tensor &weight, const Tensor &targets,
+                                                         const Maybe &bias) {
+    const Device d(ctx, index);
+    const EntropyInputs in(d, x, weight, targets, bias);
+    const Tensor ws = d.workspace(lib.cross_entropy_bytes((ep_ctx *)ctx, in.rows, (int32_t)in.n_in, (int32_t)in.classes, type_of(in.type),
+                                                          in.aligned),
+                                  "shape out of range");
+    const Tensor loss = d.empty({1}, at::kFloat), row_loss = d.empty({in.rows}, at::kFloat), lse = d.empty({in.rows}, at::kFloat),
+                 counted = d.empty({1}, at::kLong);
+    done(ctx, unlocked(lib.cross_entropy, (ep_ctx *)ctx, ptr(x), row_stride(x), ptr(weight), row_stride(weight), type_of(in.type), ptr(bias),
+                       type_of(bias), (const int32_t *)ptr(targets), in.rows, (int32_t)in.n_in, (int32_t)in.classes, (float *)ptr(loss),
+                       (float *)ptr(row_loss), (float *)ptr(lse), (int64_t *)ptr(counted), ptr(ws), (size_t)ws.numel(), d.stream()));
+    return {loss, row_loss, lse, counted};
+}
+
+std::tuple<Maybe, Maybe, Maybe> cross_entropy_backward(int64_t ctx, int index, const Tensor &x, const Tensor &weight, const Tensor &targets,
+                                                       const Tensor &lse, const Tensor &counted, const Maybe &bias, const Maybe &dloss,
+                                                       const Maybe &drow_loss, bool need_dx, bool need_dweight, bool need_dbias) {
+    const Device d(ctx, index);
+    const EntropyInputs in(d, x, weight, targets, bias);
+    d.of_type(lse, "result.lse", in.rows, at::kFloat);
+    d.of_type(counted, "result.counted", 1, at::kLong);
+    d.of_type(dloss, "dloss", 1, at::kFloat);
+    d.of_type(drow_loss, "drow_loss", in.rows, at::kFloat);
+    const Tensor ws = d.workspace(lib.cross_entropy_backward_bytes((ep_ctx *)ctx, in.rows, (int32_t)in.n_in, (int32_t)in.classes,
+                                                                   type_of(in.type), in.aligned),
+                                  "shape out of range");
+    Maybe dx, dweight, dbias;
+    if (need_dx) dx = d.empty({in.rows, in.n_in}, in.type);
+    if (need_dweight) dweight = d.empty({in.classes, in.n_in}, in.type);
+    if (need_dbias) dbias = d.empty({in.classes}, at::kFloat);
+    done(ctx, unlocked(lib.cross_entropy_backward, (ep_ctx *)ctx, ptr(x), row_stride(x), ptr(weight), row_stride(weight), type_of(in.type),
+                       ptr(bias), type_of(bias), (const int32_t *)ptr(targets), (const float *)ptr(lse), (const int64_t *)ptr(counted),
+                       (const float *)ptr(dloss), (const float *)ptr(drow_loss), in.rows, (int32_t)in.n_in, (int32_t)in.classes, ptr(dx),
+                       ptr(dweight), (float *)ptr(dbias), ptr(ws), (size_t)ws.numel(), d.stream()));
+    return {dx, dweight, dbias};
+}
+
 template <typename F>
 void take(F &f, const py::dict &addresses, const char *name) {
     f = reinterpret_cast<F>(addresses[name].cast<uintptr_t>());
@@ -327,6 +389,10 @@ PYBIND11_MODULE(_head, m) {
         take(lib.route_bytes, a, "ep_route_workspace_bytes");
         take(lib.route, a, "ep_route");
         take(lib.route_backward, a, "ep_route_backward");
+        take(lib.cross_entropy_bytes, a, "ep_cross_entropy_workspace_bytes");
+        take(lib.cross_entropy, a, "ep_cross_entropy");
+        take(lib.cross_entropy_backward_bytes, a, "ep_cross_entropy_backward_workspace_bytes");
+        take(lib.cross_entropy_backward, a, "ep_cross_entropy_backward");
         raise_status = on_error.release().ptr();   // kept for the life of the process
     });
     m.def("rms_norm", &rms_norm);
@@ -336,4 +402,6 @@ PYBIND11_MODULE(_head, m) {
     m.def("linear_backward", &linear_backward);
     m.def("route", &route);
     m.def("route_backward", &route_backward);
+    m.def("cross_entropy", &cross_entropy);
+    m.def("cross_entropy_backward", &cross_entropy_backward);
 }

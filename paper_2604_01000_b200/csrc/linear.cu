@@ -26,6 +26,9 @@
 
 using namespace eprow;
 using namespace eptc;
+using ep::Matrix;
+using ep::Operand;
+using ep::Packed;
 
 namespace {
 
@@ -43,6 +46,7 @@ struct Epilogue {
     bool vec;                         // out, preact, residual, bias, scales: 16-byte rows of whole 8-column chunks
     bool tma;                         // out and preact can be written by TMA, the residual read by 16 bytes
     const float *factor;              // of fp16 results: what the sums are multiplied by first (one value), or NULL
+    const int *other_b;               // where this device value is not 0, B is read by the map of z (there is no z then); or NULL
     float *share;                     // where a block's share of a split sum goes: [split][M][ld_share] fp32
     int ld_share;
 };
@@ -557,6 +561,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
         uint32_t it = 0, s = 0, ph = 0;
         bool ok = true;
         const uint32_t ring_base = smem_u32(ring);
+        const CUtensorMap *const from_b = e.other_b && *e.other_b ? &map_z : &map_b;
         for (Walk t(g, worker); ok && t.more(); t.next()) {
             const int m = t.m0() + (int)rank * BM, n = t.n0() + (int)rank * (t.columns() / 2);   // this block's rows of A and of B
             const int kbn = t.kbn();
@@ -579,11 +584,11 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
 #pragma unroll
                 for (int p = 0; p < PARTS; ++p, dst += B_BYTES) {
                     if (!g.b_mn)
-                        load_tile_elected<PAIR>(dst, &map_b, k, n, p, bar);
+                        load_tile_elected<PAIR>(dst, from_b, k, n, p, bar);
                     else {
 #pragma unroll
                         for (int b = 0; b < Mem::B_ROWS / 64; ++b)
-                            load_tile_elected<PAIR>(dst + b * 8192, &map_b, n + 64 * b, k, p, bar);
+                            load_tile_elected<PAIR>(dst + b * 8192, from_b, n + 64 * b, k, p, bar);
                     }
                 }
                 if (++s == (uint32_t)STAGES) {
@@ -1033,15 +1038,6 @@ __global__ void __launch_bounds__(256) linear_few_rows(const T *__restrict__ x, 
 }
 
 // ---------------------------------------------------------------------------------------------- operands
-// x = x1 + x2 + x3, each the bf16 nearest to what is left (x1 by truncation: it never overflows to infinity).
-__device__ __forceinline__ void split3(float x, __nv_bfloat16 (&p)[3]) {
-    const float a = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-    p[0] = __float2bfloat16_rn(a);
-    const float r = x - a;
-    p[1] = __float2bfloat16_rn(r);
-    p[2] = __float2bfloat16_rn(r - __bfloat162float(p[1]));
-}
-
 // Copies matrices (bound by memory: 84336 x 647 bf16 in 44 us, 5.0 TB/s): rows of `cols` elements `ld` apart to rows ld_to
 // apart (a multiple of 16 bytes; the tail is zero).
 // PARTS == 3: fp32 to three bf16 matrices, part_stride elements apart.  blockIdx.y chooses one of two matrices.
@@ -1298,17 +1294,6 @@ EncodeTiledFn encode_tiled_fn() {
     return fn;
 }
 
-// An operand as the tile kernel reads it: `parts` matrices [rows][cols], rows ld elements apart.
-struct Operand {
-    const void *base;
-    int type;             // EP_BF16, EP_F16 or EP_E4M3
-    int64_t rows;
-    int cols;
-    int64_t ld;
-    int parts;
-    int64_t part_stride;
-};
-
 // A tile of the operand is 128 bytes of k (K-major) or 64 of its columns x 64 k (MN-major) by box_rows rows.
 bool encode_operand(CUtensorMap *map, const Operand &o, bool mn, int box_rows) {
     EncodeTiledFn fn = encode_tiled_fn();
@@ -1448,7 +1433,8 @@ int launch_type(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &e
 // D = A B^T by tiles, with the epilogue; `share` is room for the shares of a split sum.  Adds to *kernels.
 // bias: sums to fold in the joining launch; without one (*folded stays false) that is left to the caller.
 int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand &b, bool b_mn, Epilogue e, float *share,
-             cudaStream_t stream, int *kernels, const BiasFold &bias = BiasFold{}, bool *folded = nullptr) {
+             cudaStream_t stream, int *kernels, const BiasFold &bias = BiasFold{}, bool *folded = nullptr,
+             const Operand *other_b = nullptr) {
     const uint32_t fmt = a.type == EP_BF16 ? 1u : 0u;   // f16 and e4m3 are both format 0 of their kinds
     p.shape.a_mn = a_mn;
     p.shape.b_mn = b_mn;
@@ -1458,6 +1444,7 @@ int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand
     e.ld_share = p.ld_share;
     Maps m{};
     bool ok = encode_operand(&m.a, a, a_mn, BM) && encode_operand(&m.b, b, b_mn, p.pair ? p.bn / 2 : p.bn);
+    if (other_b) ok = ok && encode_operand(&m.z, *other_b, b_mn, p.pair ? p.bn / 2 : p.bn);
     if (e.share)
         ok = ok && encode_result(&m.out, share, EP_F32, p.splits, e.M, p.ld_share, p.ld_share, p.bn);
     else if (e.tma)
@@ -1490,41 +1477,19 @@ int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand
 
 bool tma_ready(const void *p, int64_t ld, int type) { return ep::aligned(p, 16) && ld * ep::type_size(type) % 16 == 0; }
 
-// The copy of an operand that TMA can read: fp32 always (three bf16 parts), others when unaligned.
-struct Packed {
-    int ld, parts, type;
-    int64_t part_stride;
-    size_t bytes;
-};
-Packed packed_form(int64_t rows, int cols, int type) {
-    Packed p;
-    p.parts = type == EP_F32 ? 3 : 1;
-    p.type = type == EP_F32 ? EP_BF16 : type;
-    p.ld = (int)round_up(cols, type == EP_E4M3 ? 16 : 8);
-    p.part_stride = rows * p.ld;
-    p.bytes = (size_t)p.parts * (size_t)p.part_stride * (size_t)ep::type_size(p.type);
-    return p;
-}
-
-struct Matrix {
-    const void *base;   // NULL: not wanted
-    int64_t ld, rows;
-    int cols;
-    void *room;         // for its copy
-};
 // Two matrices as operands, copied first (in one launch) where they have to be.
 int make_operands(ep_ctx *ctx, const Matrix &first, const Matrix &second, int type, bool needs_copy, cudaStream_t stream,
                   Operand *a, Operand *b, int *kernels) {
     auto operand = [&](const Matrix &m) {
         if (!needs_copy) return Operand{m.base, type, m.rows, m.cols, m.ld, 1, 0};
-        const Packed p = packed_form(m.rows, m.cols, type);
+        const Packed p = ep::packed_form(m.rows, m.cols, type);
         return Operand{m.room, p.type, m.rows, m.cols, p.ld, p.parts, p.part_stride};
     };
     *a = operand(first);
     *b = operand(second);
     if (!needs_copy) return EP_OK;
     auto job = [&](const Matrix &m) {
-        const Packed p = packed_form(m.rows, m.cols, type);
+        const Packed p = ep::packed_form(m.rows, m.cols, type);
         return PackJob{m.base, m.room, m.ld, m.base ? m.rows : 0, p.part_stride, m.cols, p.ld};
     };
     const PackJob x = job(first), w = job(second);
@@ -1562,8 +1527,8 @@ LinearWorkspace linear_workspace(const ep_ctx *ctx, int64_t rows, int n_in, int 
     if (!few_rows(rows, n_in, n_out, in_type)) {
         const bool copy = in_type == EP_F32 || !aligned;
         if (copy) {
-            w.x = a.take<char>(packed_form(rows, n_in, in_type).bytes);
-            w.w = a.take<char>(packed_form(n_out, n_in, in_type).bytes);
+            w.x = a.take<char>(ep::packed_form(rows, n_in, in_type).bytes);
+            w.w = a.take<char>(ep::packed_form(n_out, n_in, in_type).bytes);
         }
         w.plan = plan_gemm(ctx, rows, n_out, n_in, in_type, out_type);
         w.share = a.take<float>(w.plan.share_bytes(rows) / sizeof(float));
@@ -1585,11 +1550,11 @@ BackwardWorkspace backward_workspace(const ep_ctx *ctx, int64_t rows, int n_in, 
     ep::Arena a(base);
     BackwardWorkspace w{};
     const bool copy = in_type == EP_F32 || !aligned;
-    w.dz_form = packed_form(rows, n_out, in_type);
+    w.dz_form = ep::packed_form(rows, n_out, in_type);
     w.dz = a.take<char>(w.dz_form.bytes);
     if (copy) {
-        w.x = a.take<char>(packed_form(rows, n_in, in_type).bytes);
-        w.w = a.take<char>(packed_form(n_out, n_in, in_type).bytes);
+        w.x = a.take<char>(ep::packed_form(rows, n_in, in_type).bytes);
+        w.w = a.take<char>(ep::packed_form(n_out, n_in, in_type).bytes);
     }
     const int across = (int)ep::ceil_div(w.dz_form.ld, DZ_CHUNKS * 8);
     const int64_t want = std::max<int64_t>(1, (int64_t)ctx->sm_count * 4 / across);   // about what stays resident
@@ -1731,6 +1696,66 @@ int linear_backward_run(ep_ctx *ctx, const BackwardWorkspace &ws, const void *do
 }
 
 }  // namespace
+
+namespace ep {
+
+Packed packed_form(int64_t rows, int cols, int type) {
+    Packed p;
+    p.parts = type == EP_F32 ? 3 : 1;
+    p.type = type == EP_F32 ? EP_BF16 : type;
+    p.ld = (int)round_up(cols, type == EP_E4M3 ? 16 : 8);
+    p.part_stride = rows * p.ld;
+    p.bytes = (size_t)p.parts * (size_t)p.part_stride * (size_t)type_size(p.type);
+    return p;
+}
+
+int make_operands(ep_ctx *ctx, const Matrix &first, const Matrix &second, int type, cudaStream_t stream, Operand *a, Operand *b,
+                  int *kernels) {
+    return ::make_operands(ctx, first, second, type, true, stream, a, b, kernels);
+}
+
+static GemmPlan product_plan(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, int out_type) {
+    GemmPlan p = plan_gemm(ctx, M, N, K, type, out_type);
+    // 16-bit operands whose result is rounded to their type in the end need no shorter runs than that
+    if (p.runs && type != EP_F32) p.shape.run_kb = through_kb(type);
+    return p;
+}
+
+size_t product_bytes(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, int out_type) {
+    return product_plan(ctx, M, N, K, type, out_type).share_bytes(M);
+}
+
+static int product_run(ep_ctx *ctx, const Operand &a, bool a_mn, const Operand &b, bool b_mn, const Operand *other_b, const int *other, int64_t M,
+                int N, int64_t K, void *out, int out_type, bool accumulate, const float *factor, float *share, cudaStream_t stream,
+                int *kernels) {
+    Epilogue e{};
+    e.bias_type = EP_F32;
+    e.out = out;
+    e.out_type = out_type;
+    e.residual = accumulate ? out : nullptr;
+    e.ldr = N;
+    e.factor = factor;
+    e.other_b = other;
+    e.M = M;
+    e.N = N;
+    e.vec = N % 8 == 0 && aligned(out, 16);
+    e.tma = tma_ready(out, N, out_type);
+    return run_gemm(ctx, product_plan(ctx, M, N, K, a.parts == 3 ? EP_F32 : a.type, out_type), a, a_mn, b, b_mn, e, share, stream, kernels,
+                    BiasFold{}, nullptr, other_b);
+}
+
+int product(ep_ctx *ctx, const Operand &a, bool a_mn, const Operand &b, bool b_mn, int64_t M, int N, int64_t K, void *out, int out_type,
+            bool accumulate, const float *factor, float *share, cudaStream_t stream, int *kernels) {
+    return product_run(ctx, a, a_mn, b, b_mn, nullptr, nullptr, M, N, K, out, out_type, accumulate, factor, share, stream, kernels);
+}
+
+int product_of_either(ep_ctx *ctx, const Operand &a, const Operand &b, const Operand &other_b, const int *other, int64_t M, int N,
+                      int64_t K, void *out, int out_type, bool accumulate, const float *factor, float *share, cudaStream_t stream,
+                      int *kernels) {
+    return product_run(ctx, a, true, b, true, &other_b, other, M, N, K, out, out_type, accumulate, factor, share, stream, kernels);
+}
+
+}  // namespace ep
 
 using namespace ep;
 

@@ -79,6 +79,15 @@ __device__ __forceinline__ e4m3 from_f32<e4m3>(float v) {
     return r;
 }
 
+// x = x1 + x2 + x3, each the bf16 nearest to what is left (x1 by truncation: it never overflows to infinity).
+__device__ __forceinline__ void split3(float x, __nv_bfloat16 (&p)[3]) {
+    const float a = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+    p[0] = __float2bfloat16_rn(a);
+    const float r = x - a;
+    p[1] = __float2bfloat16_rn(r);
+    p[2] = __float2bfloat16_rn(r - __bfloat162float(p[1]));
+}
+
 // Two floats to two e4m3 (a in the low byte).
 __device__ __forceinline__ uint16_t to_e4m3_pair(float a, float b) {
     return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);

@@ -122,3 +122,32 @@ def misaligned(t):
     view = room[1:1 + t.numel()].view(t.shape)
     view.copy_(t)
     return view
+
+
+def entropy(x, weight, targets, bias):
+    """(lse, row_loss, loss, counted, logits): rows whose target is -1 (or whose classes are all closed) take no part."""
+    l = x.double() @ weight.double().T
+    if bias is not None:
+        l = l + bias.double()
+    t = targets.long()
+    live = (t >= 0) & (t < weight.shape[0])
+    lse = torch.logsumexp(l, 1)
+    live = live & ~torch.isneginf(lse)
+    at = l.gather(1, t.clamp(0, weight.shape[0] - 1)[:, None])[:, 0]
+    row_loss = torch.where(live, lse - at, torch.zeros_like(lse))
+    return lse, row_loss, row_loss.sum() / max(1, int(live.sum())), int(live.sum()), l
+
+
+def entropy_slopes(l, lse, targets, dloss, drow, counted):
+    """(G, p |g|): the logits' gradient from a given lse, and the size of its terms."""
+    t = targets.long()
+    live = (t >= 0) & (t < l.shape[1]) & ~torch.isneginf(lse)
+    g = torch.zeros_like(lse.double()) if dloss is None else torch.full_like(lse.double(), float(dloss) / max(1, counted))
+    if drow is not None:
+        g = g + drow.double()
+    g = torch.where(live, g, torch.zeros_like(g))
+    p = torch.where(live[:, None], torch.exp(l - lse.double()[:, None]), torch.zeros_like(l))
+    G = p.clone()
+    rows = torch.nonzero(live)[:, 0]
+    G[rows, t[rows]] -= 1.0
+    return G * g[:, None], p * g.abs()[:, None]
