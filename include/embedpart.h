@@ -92,12 +92,14 @@ enum {
     EP_TIMER_COUNT = 14
 };
 
-/* Element types of the partition head's operators (ep_rms_norm, ep_linear, ep_route and their gradients). */
+/* Element types of the partition head's operators (ep_rms_norm, ep_linear, ep_route, ep_cross_entropy, their gradients, and
+ * ep_experts). */
 enum {
     EP_F32 = 0,
     EP_BF16 = 1,
     EP_F16 = 2,
-    EP_E4M3 = 3 /* 8 bits: 1 sign, 4 exponent, 3 mantissa bits, largest value 448, no infinities */
+    EP_E4M3 = 3, /* 8 bits: 1 sign, 4 exponent, 3 mantissa bits, largest value 448, no infinities */
+    EP_I8 = 4    /* 8-bit integers, -127 to 127 as ep_quantize_rows_to makes them */
 };
 
 /* Activations of ep_linear. */
@@ -383,16 +385,18 @@ int ep_cluster_and_balance(ep_ctx *ctx, const float *emb, int64_t N, int32_t d, 
  *   x        [dev] rows x d, x_type EP_F32 / EP_BF16 / EP_F16;  1 <= d <= 16384
  *   residual [dev] as x, or NULL (h = x)
  *   weight   [dev] d values of weight_type (EP_F32 / EP_BF16 / EP_F16), or NULL (all ones)
- *   out      [dev] rows x d of out_type: x_type, or EP_BF16 / EP_F16 from EP_F32, or EP_E4M3
- *   scale    [dev] rows fp32 with EP_E4M3, else NULL: out stands for out * scale[row], scale = the row's
- *            largest magnitude / 448 (0 for a row of zeros, whose out is 0)
+ *   out      [dev] rows x d of out_type: x_type, or EP_BF16 / EP_F16 from EP_F32, or EP_E4M3, or EP_I8
+ *   scale    [dev] rows fp32 with EP_E4M3 and EP_I8, else NULL: out stands for out * scale[row], scale = the row's
+ *            largest magnitude / 448, / 127 for EP_I8 (0 for a row of zeros, whose out is 0)
  *   hidden   [dev] out or NULL, rows x d of x_type: h (may be the same buffer as x or residual)
  *   eps      >= 0, finite.  The norm is taken of the fp32 sum, before hidden is rounded.
  * A row of zeros comes out as zeros, with eps = 0 too.  A row that holds a NaN comes out as NaN (scale included), one that
- * holds an infinity as NaN there and zero elsewhere, in 8 bits as NaN throughout (scale included).
+ * holds an infinity as NaN there and zero elsewhere, in 8 bits as NaN throughout (scale included; integers are 0 there).
  *
  * ep_quantize_rows: the 8-bit output on its own: q = x / scale, scale as above (weights and inputs of the
- * 8-bit form of ep_linear).  A row that holds an infinity has an infinite scale and stands for NaN throughout.
+ * 8-bit forms of ep_linear).  A row that holds an infinity has an infinite scale and stands for NaN throughout.
+ * ep_quantize_rows_to: the same with a choice of q_type: EP_E4M3, or EP_I8: q = x (1 / scale) to the nearest integer (ties to
+ * even), 0 throughout a row that holds a NaN or an infinity (its scale is not finite: it stands for NaN).
  *
  * ep_rms_norm_backward: with rho = 1 / sqrt(mean(h^2) + eps), a = weight * dout:
  *   dx = rho (a - h rho^2 mean(a h)) + dhidden      (the gradient of x and, alike, of residual)
@@ -408,6 +412,8 @@ int ep_rms_norm(ep_ctx *ctx, const void *x, int32_t x_type, const void *residual
                 void *hidden, void *cuda_stream);
 int ep_quantize_rows(ep_ctx *ctx, const void *x, int32_t x_type, int64_t rows, int32_t d, void *q, float *scale,
                      void *cuda_stream);
+int ep_quantize_rows_to(ep_ctx *ctx, const void *x, int32_t x_type, int64_t rows, int32_t d, void *q, int32_t q_type, float *scale,
+                        void *cuda_stream);
 size_t ep_rms_norm_backward_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t d);   /* 0 = invalid shape */
 int ep_rms_norm_backward(ep_ctx *ctx, const void *dout, int32_t dout_type, const void *hidden, int32_t h_type,
                          const void *weight, int32_t weight_type, const void *dhidden, int64_t rows, int32_t d, float eps,
@@ -416,15 +422,15 @@ int ep_rms_norm_backward(ep_ctx *ctx, const void *dout, int32_t dout_type, const
 /* --------------------------------------------------------------------------------------------
  * ep_linear -- product with a weight matrix, with bias, activation and residual in its epilogue.
  *
- *   z = x W^T + bias;  out = act(z) + residual       (EP_E4M3: z = x_scale[row] w_scale[column] (x W^T) + bias)
+ *   z = x W^T + bias;  out = act(z) + residual       (8 bits: z = x_scale[row] w_scale[column] (x W^T) + bias)
  *
  *   x        [dev] rows x n_in of in_type, row i at element i * ldx (ldx >= n_in; ldw, ldr alike)
  *   w        [dev] n_out x n_in of in_type, rows ldw apart
- *   in_type  EP_F32, EP_BF16, EP_F16, EP_E4M3;  1 <= n_in, n_out <= 65536;  0 <= rows <= 2^31 - 256
- *   x_scale  [dev] rows fp32, w_scale [dev] n_out fp32: both with EP_E4M3 (see ep_quantize_rows), else NULL
+ *   in_type  EP_F32, EP_BF16, EP_F16, EP_E4M3, EP_I8;  1 <= n_in, n_out <= 65536;  0 <= rows <= 2^31 - 256
+ *   x_scale  [dev] rows fp32, w_scale [dev] n_out fp32: both with 8 bits (see ep_quantize_rows), else NULL
  *   bias     [dev] n_out of bias_type (EP_F32 / EP_BF16 / EP_F16) or NULL;  act  EP_ACT_*
  *   residual [dev] rows x n_out of out_type, rows ldr apart, or NULL
- *   out      [dev] rows x n_out of out_type: in_type or EP_F32; EP_BF16, EP_F16 or EP_F32 from EP_E4M3
+ *   out      [dev] rows x n_out of out_type: in_type or EP_F32; EP_BF16, EP_F16 or EP_F32 from 8 bits
  *   preact   [dev] out or NULL, rows x n_out of out_type: z, which the backward pass wants
  *   aligned  (of the queries) 1 if every matrix of the call starts on a 16-byte boundary and its row stride is a
  *            multiple of 16 bytes, else 0: unaligned ones are first copied into the workspace
@@ -434,12 +440,14 @@ int ep_rms_norm_backward(ep_ctx *ctx, const void *dout, int32_t dout_type, const
  * rows there are.)  The tensor core truncates its fp32 sums (1e-7 of a sum of one sign per 16 products of 16 bits, 32 of
  * 8): an output of EP_F32 is summed in runs of 16 such steps that are added to nearest, one of EP_F16 in runs of 512, one of
  * EP_BF16 in runs of 4096, which costs a ninth of the output's own rounding at most, however long the sum.
+ * Sums of EP_I8 are exact, in 32-bit integers (any 8-bit values: 65536 products of -128 by -128 are 2^30); the scales, their
+ * product rounded first, come after.
  *
  * ep_linear_backward:  dz = dout act'(preact);  dx = dz W;  dweight = dz^T x;  dbias = sum over rows of dz
  *   dout     [dev] rows x n_out of dout_type: in_type or EP_F32, rows n_out apart
  *   preact   [dev] rows x n_out of in_type, or NULL with EP_ACT_NONE
  *   dx       [dev] out or NULL, rows x n_in of in_type;  dweight [dev] out or NULL, n_out x n_in of in_type
- *   dbias    [dev] out or NULL, n_out fp32 (summed from dz before it is rounded);  in_type is not EP_E4M3
+ *   dbias    [dev] out or NULL, n_out fp32 (summed from dz before it is rounded);  in_type is not of 8 bits
  * dz is rounded to in_type before the products of 16-bit types (their operands are 16 bits; dx and dweight are off by about 1.4
  * times the error that rounding them alone would leave).  For EP_F16 dz is scaled first, by the power of two that brings the
  * largest finite |dout| to 2^14, and the sums scaled back: elements below 2^-39 of that largest are lost, whatever its size.

@@ -26,7 +26,7 @@ EXPORTED_SYMBOLS = (
     "ep_balance_workspace_bytes", "ep_migrate", "ep_balance",
     "ep_cluster_and_balance_workspace_bytes", "ep_cluster_and_balance", "ep_selftest_wait_timeout", "ep_probe_gather",
     "ep_partition_and_reorder_host_arena_bytes", "ep_partition_and_reorder_host",
-    "ep_rms_norm", "ep_quantize_rows", "ep_rms_norm_backward_workspace_bytes", "ep_rms_norm_backward",
+    "ep_rms_norm", "ep_quantize_rows", "ep_quantize_rows_to", "ep_rms_norm_backward_workspace_bytes", "ep_rms_norm_backward",
     "ep_linear_workspace_bytes", "ep_linear", "ep_linear_backward_workspace_bytes", "ep_linear_backward",
     "ep_route_workspace_bytes", "ep_route", "ep_route_backward",
     "ep_cross_entropy_workspace_bytes", "ep_cross_entropy", "ep_cross_entropy_backward_workspace_bytes", "ep_cross_entropy_backward",
@@ -167,6 +167,8 @@ def load_library() -> ctypes.CDLL:
             lib.ep_rms_norm.restype = ctypes.c_int
             lib.ep_quantize_rows.argtypes = [vp, vp, i32, i64, i32, vp, vp, vp]
             lib.ep_quantize_rows.restype = ctypes.c_int
+            lib.ep_quantize_rows_to.argtypes = [vp, vp, i32, i64, i32, vp, i32, vp, vp]
+            lib.ep_quantize_rows_to.restype = ctypes.c_int
             lib.ep_rms_norm_backward_workspace_bytes.argtypes = [vp, i64, i32]
             lib.ep_rms_norm_backward_workspace_bytes.restype = sz
             lib.ep_rms_norm_backward.argtypes = [vp, vp, i32, vp, i32, vp, i32, vp, i64, i32, f32, vp, vp, vp, sz, vp]
@@ -200,7 +202,7 @@ def load_library() -> ctypes.CDLL:
 
 
 _head = None
-_HEAD_CALLS = ("ep_rms_norm", "ep_quantize_rows", "ep_rms_norm_backward_workspace_bytes", "ep_rms_norm_backward",
+_HEAD_CALLS = ("ep_rms_norm", "ep_quantize_rows_to", "ep_rms_norm_backward_workspace_bytes", "ep_rms_norm_backward",
                "ep_linear_workspace_bytes", "ep_linear", "ep_linear_backward_workspace_bytes", "ep_linear_backward",
                "ep_route_workspace_bytes", "ep_route", "ep_route_backward",
                "ep_cross_entropy_workspace_bytes", "ep_cross_entropy", "ep_cross_entropy_backward_workspace_bytes",
@@ -753,9 +755,9 @@ class Context:
         """weight * h / sqrt(mean(h^2) + eps) with h = x + residual; see ep_rms_norm."""
         return NormResult(*self._head.rms_norm(self._address, self.device.index, x, weight, residual, eps, out_dtype))
 
-    def quantize_rows(self, x) -> "QuantizedRows":
-        """Rows in 8 bits with a scale each: x ~ q * scale[:, None]; see ep_quantize_rows."""
-        return QuantizedRows(*self._head.quantize_rows(self._address, self.device.index, x))
+    def quantize_rows(self, x, dtype=None) -> "QuantizedRows":
+        """Rows in 8 bits (float8_e4m3fn, or int8) with a scale each: x ~ q * scale[:, None]; see ep_quantize_rows_to."""
+        return QuantizedRows(*self._head.quantize_rows(self._address, self.device.index, x, dtype))
 
     def rms_norm_backward(self, dout, hidden, weight=None, eps: float = 1e-6, dhidden=None,
                           need_dweight: bool = True) -> "NormGradients":
@@ -829,7 +831,7 @@ class NormResult(NamedTuple):
 
 
 class QuantizedRows(NamedTuple):
-    q: torch.Tensor                      # float8_e4m3fn [rows, d]
+    q: torch.Tensor                      # float8_e4m3fn or int8 [rows, d]
     scale: torch.Tensor                  # float32 [rows]
 
 
@@ -910,9 +912,9 @@ def ep_rms_norm_backward(dout, hidden, weight=None, eps=1e-6, dhidden=None, need
     return _context_of(hidden).rms_norm_backward(dout, hidden, weight, eps, dhidden, need_dweight)
 
 
-def ep_quantize_rows(x) -> QuantizedRows:
-    """Rows in 8 bits with a scale each, as ep_linear takes them."""
-    return _context_of(x).quantize_rows(x)
+def ep_quantize_rows(x, dtype=None) -> QuantizedRows:
+    """Rows in 8 bits (float8_e4m3fn, or int8) with a scale each, as ep_linear takes them."""
+    return _context_of(x).quantize_rows(x, dtype)
 
 
 def ep_linear(x, weight, bias=None, activation="none", residual=None, x_scale=None, weight_scale=None, out_dtype=None,

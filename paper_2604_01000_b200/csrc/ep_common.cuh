@@ -190,8 +190,9 @@ cudaError_t launch_early(void (*kernel)(P...), dim3 grid, dim3 block, size_t sme
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
 
-// ---- the partition head's operators (norm.cu, route.cu, linear.cu) ---------------------------------
-inline int type_size(int type) { return type == EP_F32 ? 4 : type == EP_BF16 || type == EP_F16 ? 2 : type == EP_E4M3 ? 1 : 0; }
+// ---- the partition head's operators (norm.cu, route.cu, linear.cu, entropy.cu) ----------------------
+inline int type_size(int type) { return type == EP_F32 ? 4 : type == EP_BF16 || type == EP_F16 ? 2 : type == EP_E4M3 || type == EP_I8 ? 1 : 0; }
+inline bool eight_bits(int type) { return type == EP_E4M3 || type == EP_I8; }
 inline bool float_type(int type) { return type == EP_F32 || type == EP_BF16 || type == EP_F16; }
 // out[c] = sum of parts[r][c] over r = 0..n-1, in ascending order of fixed groups of r (fp64 inside).
 int sum_partials(ep_ctx *ctx, const float *parts, int n, int cols, float *out, cudaStream_t stream);

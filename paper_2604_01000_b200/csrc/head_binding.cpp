@@ -22,7 +22,7 @@ namespace {
 
 struct Library {
     decltype(&ep_rms_norm) rms_norm;
-    decltype(&ep_quantize_rows) quantize_rows;
+    decltype(&ep_quantize_rows_to) quantize_rows;
     decltype(&ep_rms_norm_backward_workspace_bytes) rms_norm_backward_bytes;
     decltype(&ep_rms_norm_backward) rms_norm_backward;
     decltype(&ep_linear_workspace_bytes) linear_bytes;
@@ -61,10 +61,12 @@ int type_of(ScalarType t) {
         case at::kBFloat16: return EP_BF16;
         case at::kHalf: return EP_F16;
         case at::kFloat8_e4m3fn: return EP_E4M3;
+        case at::kChar: return EP_I8;
         default: return -1;
     }
 }
 bool is_float(ScalarType t) { return t == at::kFloat || t == at::kBFloat16 || t == at::kHalf; }
+bool eight_bits(ScalarType t) { return t == at::kFloat8_e4m3fn || t == at::kChar; }
 int type_of(const Maybe &t) { return t ? type_of(t->scalar_type()) : EP_F32; }
 void *ptr(const Tensor &t) { return t.data_ptr(); }
 void *ptr(const Maybe &t) { return t ? t->data_ptr() : nullptr; }
@@ -146,23 +148,25 @@ std::tuple<Tensor, Maybe, Tensor> rms_norm(int64_t ctx, int index, const Tensor 
         d.matrix(*residual, "residual", rows, width);
         need(residual->scalar_type() == t, "residual must have x's dtype");
     }
-    need(o == t || o == at::kFloat8_e4m3fn || (t == at::kFloat && is_float(o)), "no norm from " + types(t, o));
+    need(o == t || eight_bits(o) || (t == at::kFloat && is_float(o)), "no norm from " + types(t, o));
     const Tensor out = d.empty({rows, width}, o);
     Maybe scale, hidden;
-    if (o == at::kFloat8_e4m3fn) scale = d.empty({rows}, at::kFloat);
+    if (eight_bits(o)) scale = d.empty({rows}, at::kFloat);
     if (residual) hidden = d.empty({rows, width}, t);
     done(ctx, unlocked(lib.rms_norm, (ep_ctx *)ctx, ptr(x), type_of(t), ptr(residual), ptr(weight), type_of(weight), rows, (int32_t)width,
                            (float)eps, ptr(out), type_of(o), (float *)ptr(scale), ptr(hidden), d.stream()));
     return {out, scale, hidden ? *hidden : x};
 }
 
-std::tuple<Tensor, Tensor> quantize_rows(int64_t ctx, int index, const Tensor &x) {
+std::tuple<Tensor, Tensor> quantize_rows(int64_t ctx, int index, const Tensor &x, std::optional<ScalarType> dtype) {
     const Device d(ctx, index);
     d.matrix(x, "x", -1, -1);
     need(is_float(x.scalar_type()), "x must have dtype float32, bfloat16 or float16");
-    const Tensor q = d.empty(x.sizes(), at::kFloat8_e4m3fn), scale = d.empty({x.size(0)}, at::kFloat);
+    const ScalarType o = dtype.value_or(at::kFloat8_e4m3fn);
+    need(eight_bits(o), "rows are brought to float8_e4m3fn or int8");
+    const Tensor q = d.empty(x.sizes(), o), scale = d.empty({x.size(0)}, at::kFloat);
     done(ctx, unlocked(lib.quantize_rows, (ep_ctx *)ctx, ptr(x), type_of(x.scalar_type()), x.size(0), (int32_t)x.size(1), ptr(q),
-                                (float *)ptr(scale), d.stream()));
+                       type_of(o), (float *)ptr(scale), d.stream()));
     return {q, scale};
 }
 
@@ -197,14 +201,14 @@ std::tuple<Tensor, Maybe> linear(int64_t ctx, int index, const Tensor &x, const 
     const Device d(ctx, index);
     d.matrix(x, "x", -1, -1, true);
     const ScalarType t = x.scalar_type();
-    need(type_of(t) >= 0, "x must have dtype float32, bfloat16, float16 or float8_e4m3fn");
+    need(type_of(t) >= 0, "x must have dtype float32, bfloat16, float16, float8_e4m3fn or int8");
     const int64_t rows = x.size(0), n_in = x.size(1);
     d.matrix(weight, "weight", -1, n_in, true);
     need(weight.scalar_type() == t, "weight must have x's dtype");
     const int64_t n_out = weight.size(0);
     need(n_out <= Device::most, "weight has too many rows");
     const int a = activation(act);
-    const bool eight = t == at::kFloat8_e4m3fn;
+    const bool eight = eight_bits(t);
     const ScalarType o = out_dtype.value_or(eight ? at::kBFloat16 : t);
     need(is_float(o) && (eight || o == t || o == at::kFloat), "no product from " + types(t, o));
     need(eight == x_scale.has_value() && eight == w_scale.has_value(), "x_scale and weight_scale go with 8-bit inputs, and with no others");
@@ -379,7 +383,7 @@ void take(F &f, const py::dict &addresses, const char *name) {
 PYBIND11_MODULE(_head, m) {
     m.def("bind", [](const py::dict &a, py::object on_error) {
         take(lib.rms_norm, a, "ep_rms_norm");
-        take(lib.quantize_rows, a, "ep_quantize_rows");
+        take(lib.quantize_rows, a, "ep_quantize_rows_to");
         take(lib.rms_norm_backward_bytes, a, "ep_rms_norm_backward_workspace_bytes");
         take(lib.rms_norm_backward, a, "ep_rms_norm_backward");
         take(lib.linear_bytes, a, "ep_linear_workspace_bytes");

@@ -34,7 +34,7 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------- epilogue
 struct Epilogue {
-    const float *x_scale, *w_scale;   // of 8-bit inputs
+    const float *x_scale, *w_scale;   // of 8-bit inputs (both or neither)
     const void *bias;
     int bias_type, act;
     const void *residual;
@@ -375,6 +375,7 @@ struct GemmShape {
     int64_t tiles;        // tiles of the output
     int64_t items;        // tiles x splits
     int splits, kb;       // shares of the sum; k-blocks of all of it (share s takes k-blocks s, s + splits, ...)
+    int col_step;
     int run_kb;           // k-blocks of a run
     bool keep;            // 16-bit outputs: a share has several runs, added up in TMEM
     bool a_mn, b_mn;      // operand stored along its rows
@@ -394,14 +395,20 @@ struct GemmShape {
                  "l"(adesc), "l"(a1), "l"(a2), "l"(a3), "l"(bdesc), "l"(b1), "l"(b2), "l"(b3), "r"(idesc),                 \
                  "r"(accumulate_first)                                                                                     \
                  : "memory")
-template <bool F8, bool PAIR>
+// What the tensor core multiplies: 16-bit floats, e4m3, or 8-bit integers (whose sums are 32-bit integers).
+enum Kind { HALF, E8, INT };
+template <Kind KIND, bool PAIR>
 __device__ __forceinline__ void umma_kblock_elected(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint64_t astep,
                                                     uint64_t bstep, uint32_t idesc, uint32_t accumulate_first) {
     const uint64_t a1 = adesc + astep, a2 = a1 + astep, a3 = a2 + astep;
     const uint64_t b1 = bdesc + bstep, b2 = b1 + bstep, b3 = b2 + bstep;
-    if constexpr (F8 && PAIR)
+    if constexpr (KIND == INT && PAIR)
+        EP_UMMA_KBLOCK("2", "i8");
+    else if constexpr (KIND == INT)
+        EP_UMMA_KBLOCK("1", "i8");
+    else if constexpr (KIND == E8 && PAIR)
         EP_UMMA_KBLOCK("2", "f8f6f4");
-    else if constexpr (F8)
+    else if constexpr (KIND == E8)
         EP_UMMA_KBLOCK("1", "f8f6f4");
     else if constexpr (PAIR)
         EP_UMMA_KBLOCK("2", "f16");
@@ -493,12 +500,12 @@ struct Items {
     }
     __device__ __forceinline__ int m0() const { return (g.backwards ? g.tiles_m - 1 - tm : tm) * TILE_M; }
     __device__ __forceinline__ int n0() const { return tn * TILE_N; }
-    // Columns that the MMAs compute: the last tile's are cut to what the matrix has, in steps of 16.
-    __device__ __forceinline__ int columns() const { return min(TILE_N, (g.N - n0() + 15) & ~15); }
+    // Columns that the MMAs compute: the last tile's are cut to what the matrix has, in steps of 16 (integers: 32).
+    __device__ __forceinline__ int columns() const { return min(TILE_N, (g.N - n0() + g.col_step - 1) & -g.col_step); }
     __device__ __forceinline__ int kbn() const { return (g.kb - split + g.splits - 1) / g.splits; }
 };
 
-template <int BN, bool F8, int PARTS, bool RUNS, bool PAIR, typename O>
+template <int BN, Kind KIND, int PARTS, bool RUNS, bool PAIR, typename O>
 __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linear_tiles(const __grid_constant__ CUtensorMap map_a,
                                                                 const __grid_constant__ CUtensorMap map_b,
                                                                 const __grid_constant__ CUtensorMap map_out,
@@ -508,7 +515,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
     constexpr int B_BYTES = Mem::B_BYTES, STAGE_BYTES = Mem::STAGE_BYTES, STAGES = Mem::STAGES;
     constexpr int EPI_WARPS = Mem::EPI_WARPS, TMA_WARP = EPI_WARPS;
     constexpr int ACC_COLS = BN * (PARTS == 3 ? 2 : 1);
-    constexpr int KE = F8 ? 128 : 64;   // elements of k in a k-block
+    constexpr int KE = KIND == HALF ? 64 : 128;   // elements of k in a k-block
     constexpr int TILE_M = PAIR ? 2 * BM : BM;
     static_assert(2 * ACC_COLS <= TMEM_COLS, "accumulators");
     static_assert(PARTS == 1 || RUNS, "the split product is summed in runs");
@@ -622,13 +629,13 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
                     tc_fence_after();
                     const uint32_t a = ring_base + s * (uint32_t)STAGE_BYTES, b = a + PARTS * A_BYTES;
                     if constexpr (PARTS == 1) {
-                        umma_kblock_elected<F8, PAIR>(d_tmem, operand_desc(a, g.a_mn), operand_desc(b, g.b_mn), astep, bstep, idesc,
+                        umma_kblock_elected<KIND, PAIR>(d_tmem, operand_desc(a, g.a_mn), operand_desc(b, g.b_mn), astep, bstep, idesc,
                                                 first);
                     } else {
                         constexpr int pa[6] = {0, 2, 0, 1, 1, 0}, pb[6] = {0, 0, 2, 1, 0, 1};
 #pragma unroll
                         for (int q = 0; q < 6; ++q)
-                            umma_kblock_elected<F8, PAIR>(d_tmem + (q == 0 ? 0 : BN), operand_desc(a + pa[q] * A_BYTES, g.a_mn),
+                            umma_kblock_elected<KIND, PAIR>(d_tmem + (q == 0 ? 0 : BN), operand_desc(a + pa[q] * A_BYTES, g.a_mn),
                                                     operand_desc(b + pb[q] * B_BYTES, g.b_mn), astep, bstep, idesc,
                                                     q <= 1 ? first : 1u);
                     }
@@ -757,7 +764,8 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
                 tc_fence_after();
                 taddr = tmem_base + ((uint32_t)(quad * 32) << 16) + buf * ACC_COLS + piece * COLS;
             }
-            auto sums = [&](int q, float(&v)[32]) {
+            // (integers as floats, or, with `as_they_are`, as their bits)
+            auto sums = [&](int q, float(&v)[32], bool as_they_are) {
                 if constexpr (RUNS) {
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] = run[j];
@@ -766,7 +774,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
                     tmem_ld32_issue(taddr + q * 32, a);
                     tmem_ld_wait(a);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(a[j]);
+                    for (int j = 0; j < 32; ++j) v[j] = KIND == INT && !as_they_are ? (float)(int)a[j] : __uint_as_float(a[j]);
                 }
             };
             auto all_read = [&] {
@@ -780,7 +788,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
 #pragma unroll 1
                 for (int q = 0; q < SUBS && col + q * 32 < e.N; ++q) {
                     float v[32];
-                    sums(q, v);
+                    sums(q, v, true);
                     stores_read<0>();
                     ChunkStore<float, 32>::write(slot, lane, 0, v);
                     before_stores();
@@ -790,7 +798,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
             } else if (by_tma) {
                 const float xs = e.x_scale && row0 + lane < e.M ? e.x_scale[row0 + lane] : 0.f;
                 auto biased = [&](int q, float(&v)[32]) {
-                    sums(q, v);
+                    sums(q, v, false);
                     if (scaled) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] *= factor;
@@ -844,7 +852,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
                 for (int q = 0; q < SUBS; ++q) {
                     const int at = col + q * 32;
                     float v[32];
-                    sums(q, v);
+                    sums(q, v, false);
 #pragma unroll
                     for (int j = 0; j < 32; ++j) loose[lane * 32 + ((j + lane) & 31)] = scaled ? v[j] * factor : v[j];
                     __syncwarp();
@@ -891,7 +899,8 @@ struct BiasFold {
     float *dbias;
 };
 __host__ __device__ constexpr int join_chunks() { return 32; }
-template <typename O>
+// INTEGERS: the shares are 32-bit integers, and so is their sum.
+template <typename O, bool INTEGERS>
 __global__ void __launch_bounds__(256) linear_join(const float *shares, int splits, const Epilogue e, int join_blocks,
                                                    const BiasFold bias) {
     __shared__ __align__(16) float part[8][join_chunks()][9];
@@ -923,7 +932,14 @@ __global__ void __launch_bounds__(256) linear_join(const float *shares, int spli
     const int64_t row = i / chunks;
     const int col = (int)(i - row * chunks) * 8;
     ep_wait_for_launch_before();
-    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    using Sum = std::conditional_t<INTEGERS, int, float>;
+    auto sum_of = [](float bits) {
+        if constexpr (INTEGERS)
+            return __float_as_int(bits);
+        else
+            return bits;
+    };
+    Sum t[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     if (i < total) {
         const float *from = shares + ((int64_t)s0 * e.M + row) * e.ld_share + col;
         const int64_t apart = 8 * e.M * e.ld_share;
@@ -937,19 +953,27 @@ __global__ void __launch_bounds__(256) linear_join(const float *shares, int spli
             }
 #pragma unroll
             for (int q = 0; q < 5; ++q) {
-                v[0] += a[q].x, v[1] += a[q].y, v[2] += a[q].z, v[3] += a[q].w;
-                v[4] += b[q].x, v[5] += b[q].y, v[6] += b[q].z, v[7] += b[q].w;
+                t[0] += sum_of(a[q].x), t[1] += sum_of(a[q].y), t[2] += sum_of(a[q].z), t[3] += sum_of(a[q].w);
+                t[4] += sum_of(b[q].x), t[5] += sum_of(b[q].y), t[6] += sum_of(b[q].z), t[7] += sum_of(b[q].w);
             }
         }
     }
 #pragma unroll
-    for (int q = 0; q < 8; ++q) part[s0][threadIdx.x & 31][q] = v[q];
+    for (int q = 0; q < 8; ++q) {
+        if constexpr (INTEGERS)
+            part[s0][threadIdx.x & 31][q] = __int_as_float(t[q]);
+        else
+            part[s0][threadIdx.x & 31][q] = t[q];
+    }
     __syncthreads();
     if (s0 > 0 || i >= total) return;
 #pragma unroll
     for (int s = 1; s < 8; ++s)
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] += part[s][threadIdx.x][q];
+        for (int q = 0; q < 8; ++q) t[q] += sum_of(part[s][threadIdx.x][q]);
+    float v[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = (float)t[q];
     Columns<8> c;
     c.load(e, col);
     float add[8];
@@ -973,18 +997,41 @@ __device__ __noinline__ float nan_of_infinities(float sum, const float *x, int64
 
 // Dot products: `share` warps of a block (1, 2, 4 or 8 of its 8) to one column of ROWS rows.  Their lanes share out the row
 // of W, in 16-byte chunks (VEC) or, where it is not aligned for that, element by element next to one another; W is read
-// once, x comes from the L1.  Sums are fp32 multiply-adds to nearest, so all types are exact to fp32 here.
+// once, x comes from the L1.  Sums are fp32 multiply-adds to nearest, so all types are exact to fp32 here; of 8-bit integers
+// they are integers.
 template <typename T, int ROWS, bool VEC>
 __global__ void __launch_bounds__(256) linear_few_rows(const T *__restrict__ x, int64_t ldx, const T *__restrict__ w, int64_t ldw,
                                                        int n_in, const Epilogue e, int share) {
     constexpr int N = VEC ? 16 / (int)sizeof(T) : 1;
-    __shared__ float part[8][ROWS];
+    using Sum = std::conditional_t<std::is_same_v<T, i8>, int, float>;
+    __shared__ Sum part[8][ROWS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int col = (int)blockIdx.x * (8 / share) + warp / share, mine = warp % share;
-    float sum[ROWS];
+    Sum sum[ROWS];
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) sum[r] = 0.f;
-    if (col < e.N) {
+    for (int r = 0; r < ROWS; ++r) sum[r] = 0;
+    if (std::is_same_v<T, i8> && col < e.N) {
+        const T *wr = w + col * ldw;
+#pragma unroll 4
+        for (int c = (mine * 32 + lane) * N; c < n_in; c += share * 32 * N) {
+            if constexpr (VEC) {
+                const int4 a = *reinterpret_cast<const int4 *>(wr + c);
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    if (r < e.M) {
+                        const int4 b = *reinterpret_cast<const int4 *>(x + r * ldx + c);
+                        sum[r] = __dp4a(a.w, b.w, __dp4a(a.z, b.z, __dp4a(a.y, b.y, __dp4a(a.x, b.x, (int)sum[r]))));
+                    }
+                }
+            } else {
+                const int a = (int8_t)*reinterpret_cast<const uint8_t *>(wr + c);
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r)
+                    if (r < e.M) sum[r] += a * (int)(int8_t)*reinterpret_cast<const uint8_t *>(x + r * ldx + c);
+            }
+        }
+    }
+    if (!std::is_same_v<T, i8> && col < e.N) {
         const T *wr = w + col * ldw;
 #pragma unroll 4
         for (int c = (mine * 32 + lane) * N; c < n_in; c += share * 32 * N) {
@@ -1001,19 +1048,20 @@ __global__ void __launch_bounds__(256) linear_few_rows(const T *__restrict__ x, 
             }
         }
     }
-    float v[1] = {0.f};
+    Sum total = 0;
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
 #pragma unroll
         for (int o = 16; o >= 1; o >>= 1) sum[r] += __shfl_xor_sync(FULL, sum[r], o);
-        if (lane == r) v[0] = sum[r];
+        if (lane == r) total = sum[r];
     }
     if (share > 1) {
-        if (lane < ROWS) part[warp][lane] = v[0];
+        if (lane < ROWS) part[warp][lane] = total;
         __syncthreads();
         if (mine == 0 && lane < ROWS)
-            for (int s = 1; s < share; ++s) v[0] += part[warp + s][lane];
+            for (int s = 1; s < share; ++s) total += part[warp + s][lane];
     }
+    float v[1] = {(float)total};
     if constexpr (sizeof(T) == 4) {
         // The tiles split fp32 numbers, and an infinity splits into NaN: so it does here.  A sum is only infinite where an
         // operand is, or where it overflows, which stays an infinity.
@@ -1345,7 +1393,7 @@ struct GemmPlan {
 // the tiles leave workers idle, into shares of at least 4 k-blocks.  (With the largest tile that fills one wave instead,
 // the weights' gradient of 232965 x 256 x 256 went by tiles of 64 columns that read each operand up to four times.)
 GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, int out_type) {
-    const int ke = type == EP_E4M3 ? 128 : 64, parts = type == EP_F32 ? 3 : 1;
+    const int ke = ep::eight_bits(type) ? 128 : 64, parts = type == EP_F32 ? 3 : 1;
     const bool fp32_out = out_type == EP_F32;
     const int kb = (int)ep::ceil_div(K, ke);
     GemmPlan best{};
@@ -1354,7 +1402,7 @@ GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, int
         for (int bn : {256, 128, 64}) {
             if (bn == (pair ? 64 : 256) || (fp32_out && bn != (parts == 3 && !pair ? 64 : 128))) continue;
             GemmPlan p{};
-            p.runs = fp32_out;
+            p.runs = fp32_out && type != EP_I8;   // (integers are summed exactly)
             p.pair = pair;
             p.bn = bn;
             p.shape.M = M;
@@ -1367,8 +1415,9 @@ GemmPlan plan_gemm(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, int
             p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(workers / p.shape.tiles, kb / 4));
             const int per = (int)ep::ceil_div(kb, p.splits);
             p.shape.splits = p.splits;
+            p.shape.col_step = type == EP_I8 ? 32 : 16;
             p.shape.run_kb = fp32_out ? RUN_KB : through_kb(out_type);
-            p.shape.keep = !fp32_out && per > p.shape.run_kb;
+            p.shape.keep = !fp32_out && type != EP_I8 && per > p.shape.run_kb;
             p.shape.items = p.shape.tiles * p.splits;
             p.workers = (int)std::min<int64_t>(p.shape.items, workers);
             p.shape.step_m = p.workers / p.shape.tiles_n;
@@ -1391,9 +1440,9 @@ struct Maps {
     CUtensorMap a, b, out, z;   // out: of the shares, where the sum is split
 };
 
-template <int BN, bool F8, int PARTS, bool RUNS, bool PAIR, typename O>
+template <int BN, Kind KIND, int PARTS, bool RUNS, bool PAIR, typename O>
 int launch_tiles(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &e, cudaStream_t stream) {
-    auto kernel = linear_tiles<BN, F8, PARTS, RUNS, PAIR, O>;
+    auto kernel = linear_tiles<BN, KIND, PARTS, RUNS, PAIR, O>;
     constexpr size_t smem = TileMemory<BN, PARTS, PAIR>::TOTAL;
     EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     cudaLaunchConfig_t cfg{};
@@ -1413,21 +1462,31 @@ int launch_tiles(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &
     return EP_OK;
 }
 
-// (the type of the output is fp32 exactly where sums are kept in runs)
-template <bool F8, typename O>
+// (floats are summed in runs exactly where the output is fp32)
+template <Kind KIND, typename O>
 int launch_width(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &e, cudaStream_t stream) {
     if (p.pair)
-        return p.bn == 256 ? launch_tiles<256, F8, 1, false, true, O>(ctx, p, m, e, stream)
-                           : launch_tiles<128, F8, 1, false, true, O>(ctx, p, m, e, stream);
-    return p.bn == 128 ? launch_tiles<128, F8, 1, false, false, O>(ctx, p, m, e, stream)
-                       : launch_tiles<64, F8, 1, false, false, O>(ctx, p, m, e, stream);
+        return p.bn == 256 ? launch_tiles<256, KIND, 1, false, true, O>(ctx, p, m, e, stream)
+                           : launch_tiles<128, KIND, 1, false, true, O>(ctx, p, m, e, stream);
+    return p.bn == 128 ? launch_tiles<128, KIND, 1, false, false, O>(ctx, p, m, e, stream)
+                       : launch_tiles<64, KIND, 1, false, false, O>(ctx, p, m, e, stream);
 }
-template <bool F8>
+template <Kind KIND>
 int launch_type(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &e, cudaStream_t stream) {
-    if (p.runs)
-        return p.pair ? launch_tiles<128, F8, 1, true, true, float>(ctx, p, m, e, stream)
-                      : launch_tiles<128, F8, 1, true, false, float>(ctx, p, m, e, stream);
-    return e.out_type == EP_BF16 ? launch_width<F8, __nv_bfloat16>(ctx, p, m, e, stream) : launch_width<F8, __half>(ctx, p, m, e, stream);
+    constexpr bool RUNS = KIND != INT;
+    if (e.out_type == EP_F32)
+        return p.pair ? launch_tiles<128, KIND, 1, RUNS, true, float>(ctx, p, m, e, stream)
+                      : launch_tiles<128, KIND, 1, RUNS, false, float>(ctx, p, m, e, stream);
+    return e.out_type == EP_BF16 ? launch_width<KIND, __nv_bfloat16>(ctx, p, m, e, stream) : launch_width<KIND, __half>(ctx, p, m, e, stream);
+}
+template <bool INTEGERS>
+int launch_join(ep_ctx *ctx, unsigned grid, const float *share, const GemmPlan &p, const Epilogue &e, int blocks, const BiasFold &bias,
+                cudaStream_t stream) {
+    auto kernel = e.out_type == EP_BF16  ? linear_join<__nv_bfloat16, INTEGERS>
+                  : e.out_type == EP_F16 ? linear_join<__half, INTEGERS>
+                                         : linear_join<float, INTEGERS>;
+    EP_CUDA(ctx, ep::launch_early(kernel, dim3(grid), dim3(256), 0, stream, share, p.splits, e, blocks, bias));
+    return EP_OK;
 }
 
 // D = A B^T by tiles, with the epilogue; `share` is room for the shares of a split sum.  Adds to *kernels.
@@ -1435,10 +1494,11 @@ int launch_type(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &e
 int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand &b, bool b_mn, Epilogue e, float *share,
              cudaStream_t stream, int *kernels, const BiasFold &bias = BiasFold{}, bool *folded = nullptr,
              const Operand *other_b = nullptr) {
-    const uint32_t fmt = a.type == EP_BF16 ? 1u : 0u;   // f16 and e4m3 are both format 0 of their kinds
+    const uint32_t fmt = a.type == EP_BF16 || a.type == EP_I8 ? 1u : 0u;   // (f16 and e4m3 are format 0 of their kinds, signed bytes 1)
+    const uint32_t sum = a.type == EP_I8 ? 2u : 1u;                        // 32-bit integers, fp32
     p.shape.a_mn = a_mn;
     p.shape.b_mn = b_mn;
-    p.shape.idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
+    p.shape.idesc = (sum << 4) | (fmt << 7) | (fmt << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) |
                     ((uint32_t)((p.pair ? 2 * BM : BM) >> 4) << 24);
     e.share = p.splits > 1 ? share : nullptr;
     e.ld_share = p.ld_share;
@@ -1453,10 +1513,12 @@ int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand
     if (!ok) return ep::fail(ctx, EP_ERR_CUDA, "cuTensorMapEncodeTiled failed for a product of %lld x %d", (long long)e.M, e.N);
     int rc;
     if (a.parts == 3)
-        rc = p.pair ? launch_tiles<128, false, 3, true, true, float>(ctx, p, m, e, stream)
-                    : launch_tiles<64, false, 3, true, false, float>(ctx, p, m, e, stream);
+        rc = p.pair ? launch_tiles<128, HALF, 3, true, true, float>(ctx, p, m, e, stream)
+                    : launch_tiles<64, HALF, 3, true, false, float>(ctx, p, m, e, stream);
     else
-        rc = a.type == EP_E4M3 ? launch_type<true>(ctx, p, m, e, stream) : launch_type<false>(ctx, p, m, e, stream);
+        rc = a.type == EP_E4M3 ? launch_type<E8>(ctx, p, m, e, stream)
+             : a.type == EP_I8 ? launch_type<INT>(ctx, p, m, e, stream)
+                               : launch_type<HALF>(ctx, p, m, e, stream);
     if (rc != EP_OK) return rc;
     ++*kernels;
     if (p.splits > 1) {
@@ -1464,12 +1526,9 @@ int run_gemm(ep_ctx *ctx, GemmPlan p, const Operand &a, bool a_mn, const Operand
         const int blocks = (int)ep::ceil_div(e.M * ((e.N + 7) / 8), join_chunks());
         const unsigned grid = (unsigned)(blocks + (bias.parts ? ep::ceil_div(bias.n_out, 8) : 0));
         if (folded) *folded = bias.parts != nullptr;
-        if (e.out_type == EP_BF16)
-            EP_CUDA(ctx, ep::launch_early(linear_join<__nv_bfloat16>, dim3(grid), dim3(256), 0, stream, (const float *)share, p.splits, e, blocks, bias));
-        else if (e.out_type == EP_F16)
-            EP_CUDA(ctx, ep::launch_early(linear_join<__half>, dim3(grid), dim3(256), 0, stream, (const float *)share, p.splits, e, blocks, bias));
-        else
-            EP_CUDA(ctx, ep::launch_early(linear_join<float>, dim3(grid), dim3(256), 0, stream, (const float *)share, p.splits, e, blocks, bias));
+        rc = a.type == EP_I8 ? launch_join<true>(ctx, grid, share, p, e, blocks, bias, stream)
+                             : launch_join<false>(ctx, grid, share, p, e, blocks, bias, stream);
+        if (rc != EP_OK) return rc;
         ++*kernels;
     }
     return EP_OK;
@@ -1497,7 +1556,7 @@ int make_operands(ep_ctx *ctx, const Matrix &first, const Matrix &second, int ty
     const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(threads, 256), (int64_t)ctx->sm_count * PACK_BLOCKS_PER_SM)), 2);
     if (type == EP_F32)
         pack_rows<float, __nv_bfloat16, 3><<<grid, 256, 0, stream>>>(x, w);
-    else if (type == EP_E4M3)
+    else if (ep::eight_bits(type))
         pack_rows<uint8_t, uint8_t, 1><<<grid, 256, 0, stream>>>(x, w);
     else
         pack_rows<uint16_t, uint16_t, 1><<<grid, 256, 0, stream>>>(x, w);
@@ -1510,7 +1569,7 @@ bool linear_shape_ok(int64_t rows, int n_in, int n_out) {
     return rows >= 0 && rows <= (1ll << 31) - 256 && n_in >= 1 && n_in <= MAX_WIDTH && n_out >= 1 && n_out <= MAX_WIDTH;
 }
 bool linear_types_ok(int in_type, int out_type) {
-    if (in_type == EP_E4M3) return ep::float_type(out_type);
+    if (ep::eight_bits(in_type)) return ep::float_type(out_type);
     return ep::float_type(in_type) && (out_type == in_type || out_type == EP_F32);
 }
 
@@ -1593,6 +1652,7 @@ int launch_few_rows(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int6
     if (in_type == EP_F32) return launch_few_rows_of<ROWS, float>(ctx, x, ldx, w, ldw, n_in, e, vec, stream);
     if (in_type == EP_BF16) return launch_few_rows_of<ROWS, __nv_bfloat16>(ctx, x, ldx, w, ldw, n_in, e, vec, stream);
     if (in_type == EP_F16) return launch_few_rows_of<ROWS, __half>(ctx, x, ldx, w, ldw, n_in, e, vec, stream);
+    if (in_type == EP_I8) return launch_few_rows_of<ROWS, i8>(ctx, x, ldx, w, ldw, n_in, e, vec, stream);
     return launch_few_rows_of<ROWS, e4m3>(ctx, x, ldx, w, ldw, n_in, e, vec, stream);
 }
 
@@ -1703,7 +1763,7 @@ Packed packed_form(int64_t rows, int cols, int type) {
     Packed p;
     p.parts = type == EP_F32 ? 3 : 1;
     p.type = type == EP_F32 ? EP_BF16 : type;
-    p.ld = (int)round_up(cols, type == EP_E4M3 ? 16 : 8);
+    p.ld = (int)round_up(cols, eight_bits(type) ? 16 : 8);
     p.part_stride = rows * p.ld;
     p.bytes = (size_t)p.parts * (size_t)p.part_stride * (size_t)type_size(p.type);
     return p;
@@ -1783,7 +1843,7 @@ int ep_linear(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int64_t ld
     if (act < EP_ACT_NONE || act > EP_ACT_SILU) return fail(ctx, EP_ERR_INVALID_ARG, "unknown activation %d", act);
     if (ldx < n_in || ldw < n_in || (residual && ldr < n_out)) return fail(ctx, EP_ERR_INVALID_ARG, "a row stride is shorter than its row");
     if (rows == 0) return EP_OK;
-    if ((in_type == EP_E4M3) != (x_scale != nullptr) || (in_type == EP_E4M3) != (w_scale != nullptr))
+    if (eight_bits(in_type) != (x_scale != nullptr) || eight_bits(in_type) != (w_scale != nullptr))
         return fail(ctx, EP_ERR_INVALID_ARG, "scales go with 8-bit inputs, and with no others");
     if (!x || !w || !out || !type_aligned(x, in_type) || !type_aligned(w, in_type) || !type_aligned(out, out_type) ||
         !type_aligned(preact, out_type) || !type_aligned(residual, out_type) || !type_aligned(bias, bias ? bias_type : EP_E4M3) ||

@@ -10,6 +10,7 @@
 #include "rows.cuh"
 
 #include <algorithm>
+#include <type_traits>
 
 using namespace eprow;
 
@@ -19,7 +20,8 @@ namespace {
 template <int L>
 constexpr int block_threads() { return L > 32 ? L : 256; }
 
-constexpr float E4M3_TOP = 448.f;
+template <typename O>
+constexpr float largest() { return std::is_same_v<O, i8> ? 127.f : 448.f; }   // of an 8-bit type
 
 // rho = 1 / sqrt(mean(h^2) + eps) of a row, from this thread's share `ss` of the sum of squares.  Where the fp32 squares
 // leave the range that is safe for their sum (a row of magnitudes below 1e-15 or above 1e18, or of zeros) they are taken
@@ -102,12 +104,17 @@ __global__ void __launch_bounds__(block_threads<Lay::L>()) norm_rows(const T *x,
             for (int j = 0; j < V; ++j)
 #pragma unroll
                 for (int i = 0; i < N; ++i) top = OpMax::apply(top, fabsf(h[j][i]));
-            const float s = reduce_row<L, OpMax>(top, slots, turn) / E4M3_TOP;
-            if (s > 0.f && s < 1.17549435e-38f) {   // no finite reciprocal worth multiplying by: divide
+            const float s = reduce_row<L, OpMax>(top, slots, turn) / largest<O>();
+            if (std::is_same_v<O, i8> && !(s < INFINITY)) {   // integers have no NaN: the scale alone says so
+                Lay::set(0.f, h);
+            } else if (s > 0.f && s < 1.17549435e-38f) {   // no finite reciprocal worth multiplying by: divide
 #pragma unroll
                 for (int j = 0; j < V; ++j)
 #pragma unroll
-                    for (int i = 0; i < N; ++i) h[j][i] = h[j][i] / s;
+                    for (int i = 0; i < N; ++i) {
+                        h[j][i] = h[j][i] / s;   // (s has few bits: past the largest integer by half of it at most)
+                        if constexpr (std::is_same_v<O, i8>) h[j][i] = fminf(fmaxf(h[j][i], -127.f), 127.f);
+                    }
             } else {
                 const float inverse = s == 0.f ? 0.f : 1.f / s;
 #pragma unroll
@@ -333,7 +340,13 @@ int launch_norm_out(const NormArgs &a, int out_type) {
         if (out_type == EP_F16) return launch_norm<T, __half, true>(a);
     }
     if (out_type == EP_E4M3) return launch_norm<T, e4m3, true>(a);
+    if (out_type == EP_I8) return launch_norm<T, i8, true>(a);
     return launch_norm<T, T, true>(a);
+}
+
+template <typename T>
+int launch_quantize(const NormArgs &a, int out_type) {
+    return out_type == EP_I8 ? launch_norm<T, i8, false>(a) : launch_norm<T, e4m3, false>(a);
 }
 
 struct BackArgs {
@@ -414,9 +427,9 @@ int norm_call(ep_ctx *ctx, bool norm, const void *x, int x_type, const void *res
     Timed tm(ctx, stream, EP_TIMER_NORM);
     int rc;
     if (!norm)
-        rc = x_type == EP_F32    ? launch_norm<float, e4m3, false>(a)
-             : x_type == EP_BF16 ? launch_norm<__nv_bfloat16, e4m3, false>(a)
-                                 : launch_norm<__half, e4m3, false>(a);
+        rc = x_type == EP_F32    ? launch_quantize<float>(a, out_type)
+             : x_type == EP_BF16 ? launch_quantize<__nv_bfloat16>(a, out_type)
+                                 : launch_quantize<__half>(a, out_type);
     else
         rc = x_type == EP_F32    ? launch_norm_out<float>(a, out_type)
              : x_type == EP_BF16 ? launch_norm_out<__nv_bfloat16>(a, out_type)
@@ -435,11 +448,11 @@ int ep_rms_norm(ep_ctx *ctx, const void *x, int32_t x_type, const void *residual
     if (!ctx) return EP_ERR_INVALID_ARG;
     if (!norm_shape_ok(rows, d)) return fail(ctx, EP_ERR_INVALID_ARG, "rows %lld or d %d out of range", (long long)rows, d);
     if (!float_type(x_type) || (weight && !float_type(weight_type)) ||
-        !(out_type == x_type || out_type == EP_E4M3 || (x_type == EP_F32 && float_type(out_type))))
+        !(out_type == x_type || eight_bits(out_type) || (x_type == EP_F32 && float_type(out_type))))
         return fail(ctx, EP_ERR_INVALID_ARG, "no norm from type %d to type %d", x_type, out_type);
     if (!(eps >= 0.f) || eps > 3e38f) return fail(ctx, EP_ERR_INVALID_ARG, "eps must be finite and not negative");
     if (rows == 0) return EP_OK;
-    if ((out_type == EP_E4M3) != (scale != nullptr))
+    if (eight_bits(out_type) != (scale != nullptr))
         return fail(ctx, EP_ERR_INVALID_ARG, "scale goes with an 8-bit output, and with no other");
     if (!x || !out || !element_aligned(x, x_type) || !element_aligned(residual, x_type) || !element_aligned(out, out_type) ||
         !element_aligned(hidden, x_type) || !element_aligned(weight, weight ? weight_type : EP_E4M3) || !aligned(scale, 4))
@@ -448,16 +461,22 @@ int ep_rms_norm(ep_ctx *ctx, const void *x, int32_t x_type, const void *residual
                      static_cast<cudaStream_t>(cuda_stream));
 }
 
-int ep_quantize_rows(ep_ctx *ctx, const void *x, int32_t x_type, int64_t rows, int32_t d, void *q, float *scale,
-                     void *cuda_stream) {
+int ep_quantize_rows_to(ep_ctx *ctx, const void *x, int32_t x_type, int64_t rows, int32_t d, void *q, int32_t q_type, float *scale,
+                        void *cuda_stream) {
     if (!ctx) return EP_ERR_INVALID_ARG;
     if (!norm_shape_ok(rows, d)) return fail(ctx, EP_ERR_INVALID_ARG, "rows %lld or d %d out of range", (long long)rows, d);
-    if (!float_type(x_type)) return fail(ctx, EP_ERR_INVALID_ARG, "rows of type %d cannot be brought to 8 bits", x_type);
+    if (!float_type(x_type) || !eight_bits(q_type))
+        return fail(ctx, EP_ERR_INVALID_ARG, "rows of type %d cannot be brought to 8 bits of type %d", x_type, q_type);
     if (rows == 0) return EP_OK;
     if (!x || !q || !scale || !element_aligned(x, x_type) || !aligned(scale, 4))
         return fail(ctx, EP_ERR_INVALID_ARG, "null or misaligned pointer");
-    return norm_call(ctx, false, x, x_type, nullptr, nullptr, EP_F32, rows, d, 0.f, q, EP_E4M3, scale, nullptr,
+    return norm_call(ctx, false, x, x_type, nullptr, nullptr, EP_F32, rows, d, 0.f, q, q_type, scale, nullptr,
                      static_cast<cudaStream_t>(cuda_stream));
+}
+
+int ep_quantize_rows(ep_ctx *ctx, const void *x, int32_t x_type, int64_t rows, int32_t d, void *q, float *scale,
+                     void *cuda_stream) {
+    return ep_quantize_rows_to(ctx, x, x_type, rows, d, q, EP_E4M3, scale, cuda_stream);
 }
 
 size_t ep_rms_norm_backward_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t d) {

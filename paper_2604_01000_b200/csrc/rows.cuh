@@ -55,6 +55,9 @@ __device__ __forceinline__ Pair add2(Pair a, Pair b) {
 struct e4m3 {
     uint8_t bits;
 };
+struct i8 {
+    uint8_t bits;
+};
 
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -62,6 +65,8 @@ __device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
 __device__ __forceinline__ float to_f32(e4m3 v) {
     return __half2float(__half(__nv_cvt_fp8_to_halfraw(v.bits, __NV_E4M3)));
 }
+
+__device__ __forceinline__ float to_f32(i8 v) { return (float)(int8_t)v.bits; }
 
 // Every rounding is to nearest, ties to even; e4m3 saturates at 448 (its callers scale to that range first).
 template <typename T>
@@ -88,9 +93,21 @@ __device__ __forceinline__ void split3(float x, __nv_bfloat16 (&p)[3]) {
     p[2] = __float2bfloat16_rn(r - __bfloat162float(p[1]));
 }
 
-// Two floats to two e4m3 (a in the low byte).
-__device__ __forceinline__ uint16_t to_e4m3_pair(float a, float b) {
+// A number below 2^22 to the nearest integer (ties to even), whose low byte is its two's complement.
+__device__ __forceinline__ uint32_t to_integer(float v) { return __float_as_uint(v + 12582912.f); }
+template <>
+__device__ __forceinline__ i8 from_f32<i8>(float v) { return i8{(uint8_t)to_integer(v)}; }
+
+// Two floats to two 8-bit numbers (a in the low byte).
+template <typename T>
+__device__ __forceinline__ uint16_t to_8_bit_pair(float a, float b);
+template <>
+__device__ __forceinline__ uint16_t to_8_bit_pair<e4m3>(float a, float b) {
     return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+}
+template <>
+__device__ __forceinline__ uint16_t to_8_bit_pair<i8>(float a, float b) {
+    return (uint16_t)__byte_perm(to_integer(a), to_integer(b), 0x0040);
 }
 
 // One vector parameter (a norm's weight, a product's bias) of type EP_F32, EP_BF16 or EP_F16.
@@ -150,7 +167,7 @@ __device__ __forceinline__ void store_chunk(T *row, int col, int width, bool vec
             constexpr int PIECES = B > 16 ? B / 16 : 1;
             if constexpr (sizeof(T) == 1 && N % 2 == 0) {   // (8 bits are converted two at a time)
 #pragma unroll
-                for (int i = 0; i < N; i += 2) reinterpret_cast<uint16_t *>(e)[i / 2] = to_e4m3_pair(v[i], v[i + 1]);
+                for (int i = 0; i < N; i += 2) reinterpret_cast<uint16_t *>(e)[i / 2] = to_8_bit_pair<T>(v[i], v[i + 1]);
             } else {
 #pragma unroll
                 for (int i = 0; i < N; ++i) e[i] = from_f32<T>(v[i]);
@@ -292,7 +309,7 @@ struct Layout {
         } else if constexpr (sizeof(T) == 1) {
 #pragma unroll
             for (int i = 0; i < N; i += 2) {
-                const uint16_t two = to_e4m3_pair(v[i], v[i + 1]);
+                const uint16_t two = to_8_bit_pair<T>(v[i], v[i + 1]);
                 if (inside(lane, j, i, width)) row[col(lane, j, i)].bits = (uint8_t)two;
                 if (inside(lane, j, i + 1, width)) row[col(lane, j, i + 1)].bits = (uint8_t)(two >> 8);
             }
