@@ -546,6 +546,34 @@ int ep_cross_entropy_backward(ep_ctx *ctx, const void *x, int64_t ldx, const voi
                               float *dbias, void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /* --------------------------------------------------------------------------------------------
+ * ep_experts -- a layer of experts for a few rows: the router, and both products of the parts it chooses, in one call.
+ *
+ *   p = softmax(x Wr^T + br) over the parts;  ids, weights: the k best of each row, as ep_route chooses and weighs them;
+ *   out = sum_i weights[i] (W2[ids[i]] act(W1[ids[i]] x + b1[ids[i]]) + b2[ids[i]]) + residual
+ *
+ *   x        [dev] rows x n_in of type EP_F32 / EP_BF16 / EP_F16, row i at element i * ldx;  0 <= rows <= 64
+ *            (EP_ERR_UNSUPPORTED above: more rows are worth a product for each part)
+ *   router   [dev] experts x n_in of type;  router_bias [dev] experts of router_bias_type or NULL; -infinity closes a part
+ *   valid    [dev] rows bytes or NULL: 0 = the row takes no part (ids -1, weights 0, out = residual)
+ *   k        1 <= k <= min(experts, 32);  1 <= experts <= 4096;  1 <= n_in, n_hidden, n_out <= 65536
+ *   w1       [dev] experts x n_hidden x n_in, w2 [dev] experts x n_out x n_hidden, of w_type: type, or EP_I8
+ *   w1_scale [dev] experts x n_hidden fp32, w2_scale [dev] experts x n_out fp32: with EP_I8 (a row of weights stands for itself
+ *            times its scale, see ep_quantize_rows_to), else NULL
+ *   b1       [dev] experts x n_hidden, b2 [dev] experts x n_out, of bias_type, or NULL;  act  EP_ACT_*
+ *   residual [dev] rows x n_out of type, rows ldr apart, or NULL
+ *   out      [dev] out, rows x n_out of type;  ids [dev] out, rows x k int32;  weights [dev] out, rows x k fp32
+ * Sums are fp32 multiply-adds, the hidden values stay in fp32, out is rounded once.  Parts that no row chose are not read.
+ * Logits, ties, NaN and infinities among them as for ep_route.
+ */
+size_t ep_experts_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t n_in, int32_t n_hidden, int32_t n_out, int32_t experts,
+                                  int32_t k);   /* 0 = invalid shape; at least 256 */
+int ep_experts(ep_ctx *ctx, const void *x, int64_t ldx, int32_t type, const void *router, const void *router_bias,
+               int32_t router_bias_type, const uint8_t *valid, int32_t k, int32_t renormalize, const void *w1, const float *w1_scale,
+               const void *b1, const void *w2, const float *w2_scale, const void *b2, int32_t w_type, int32_t bias_type, int32_t act,
+               const void *residual, int64_t ldr, void *out, int32_t *ids, float *weights, int64_t rows, int32_t n_in,
+               int32_t n_hidden, int32_t n_out, int32_t experts, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* --------------------------------------------------------------------------------------------
  * Host-buffer variants.  Same operations and the same kernels; inputs and outputs are [host]
  * pointers.  Each call copies its inputs into `arena` (a [dev] scratch block of at least
  * *_host_arena_bytes bytes, 256-byte aligned, which also holds the kernel workspace), runs, and

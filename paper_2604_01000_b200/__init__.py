@@ -26,6 +26,7 @@ from .binding import (  # noqa: F401
     ep_cross_entropy,
     ep_cross_entropy_backward,
     CrossEntropyResult,
+    ep_experts,
     library_path,
     load_library,
     EXPORTED_SYMBOLS,

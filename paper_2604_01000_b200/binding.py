@@ -30,6 +30,7 @@ EXPORTED_SYMBOLS = (
     "ep_linear_workspace_bytes", "ep_linear", "ep_linear_backward_workspace_bytes", "ep_linear_backward",
     "ep_route_workspace_bytes", "ep_route", "ep_route_backward",
     "ep_cross_entropy_workspace_bytes", "ep_cross_entropy", "ep_cross_entropy_backward_workspace_bytes", "ep_cross_entropy_backward",
+    "ep_experts_workspace_bytes", "ep_experts",
 )
 
 EP_OK = 0
@@ -197,6 +198,11 @@ def load_library() -> ctypes.CDLL:
             lib.ep_cross_entropy_backward.argtypes = [vp, vp, i64, vp, i64, i32, vp, i32, vp, vp, vp, vp, vp, i64, i32, i32, vp, vp, vp,
                                                       vp, sz, vp]
             lib.ep_cross_entropy_backward.restype = ctypes.c_int
+            lib.ep_experts_workspace_bytes.argtypes = [vp, i64, i32, i32, i32, i32, i32]
+            lib.ep_experts_workspace_bytes.restype = sz
+            lib.ep_experts.argtypes = [vp, vp, i64, i32, vp, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, vp, i32, i32, i32, vp, i64, vp, vp, vp,
+                                       i64, i32, i32, i32, i32, vp, sz, vp]
+            lib.ep_experts.restype = ctypes.c_int
             _lib = lib
     return _lib
 
@@ -206,7 +212,7 @@ _HEAD_CALLS = ("ep_rms_norm", "ep_quantize_rows_to", "ep_rms_norm_backward_works
                "ep_linear_workspace_bytes", "ep_linear", "ep_linear_backward_workspace_bytes", "ep_linear_backward",
                "ep_route_workspace_bytes", "ep_route", "ep_route_backward",
                "ep_cross_entropy_workspace_bytes", "ep_cross_entropy", "ep_cross_entropy_backward_workspace_bytes",
-               "ep_cross_entropy_backward")
+               "ep_cross_entropy_backward", "ep_experts_workspace_bytes", "ep_experts")
 
 
 def _raise_status(ctx: int, status: int, what: str = ""):
@@ -801,6 +807,14 @@ class Context:
                                                                   result.counted, bias, dloss, drow_loss, need_dx, need_dweight,
                                                                   need_dbias))
 
+    def experts(self, x, router, w1, w2, k: int = 1, router_bias=None, b1=None, b2=None, activation: str = "gelu",
+                renormalize: bool = False, residual=None, w1_scale=None, w2_scale=None, valid=None) -> "ExpertsResult":
+        """A layer of experts for up to 64 rows: each row's k best parts by x router^T + router_bias, both products of every
+        chosen part, their weighted sum (+ residual).  w1: [parts, hidden, n_in], w2: [parts, n_out, hidden], of x's dtype or
+        int8 with a float32 scale for each row of each matrix; see ep_experts."""
+        return ExpertsResult(*self._head.experts(self._address, self.device.index, x, router, w1, w2, k, router_bias, b1, b2, activation,
+                                                 renormalize, residual, w1_scale, w2_scale, valid))
+
 
 class KMeansResult(NamedTuple):
     assign: torch.Tensor                 # int32 [N]
@@ -865,6 +879,12 @@ class CrossEntropyResult(NamedTuple):
     row_loss: torch.Tensor               # float32 [rows]
     lse: torch.Tensor                    # float32 [rows]: what the backward pass takes
     counted: torch.Tensor                # int64 [1]: rows that took part
+
+
+class ExpertsResult(NamedTuple):
+    out: torch.Tensor                    # [rows, n_out]
+    ids: torch.Tensor                    # int32 [rows, k], -1 = no part
+    weights: torch.Tensor                # float32 [rows, k]
 
 
 _default: dict[int, Context] = {}
@@ -948,6 +968,12 @@ def ep_cross_entropy_backward(x, weight, targets, result, bias=None, dloss=None,
                               need_dbias=True) -> LinearGradients:
     """Gradients of ep_cross_entropy."""
     return _context_of(x).cross_entropy_backward(x, weight, targets, result, bias, dloss, drow_loss, need_dx, need_dweight, need_dbias)
+
+
+def ep_experts(x, router, w1, w2, k=1, router_bias=None, b1=None, b2=None, activation="gelu", renormalize=False, residual=None,
+               w1_scale=None, w2_scale=None, valid=None) -> ExpertsResult:
+    """A layer of experts for a few rows: router, the chosen parts' products, and their weighted sum."""
+    return _context_of(x).experts(x, router, w1, w2, k, router_bias, b1, b2, activation, renormalize, residual, w1_scale, w2_scale, valid)
 
 
 REORDER_STATIC_MAX_N = 1 << 22

@@ -1,5 +1,5 @@
 // Tensors in, tensors out for the partition head's operators: the checks, the allocations and the calls of the C ABI
-// (include/embedpart.h) for Context.rms_norm, .linear, .route, .cross_entropy and their gradients, compiled, because for one row
+// (include/embedpart.h) for Context.rms_norm, .linear, .route, .cross_entropy, their gradients and .experts, compiled, because for one row
 // marshalling is most of such a call (measured for routing one row: 22 us through ctypes, of which 6 us the C call).
 // The C functions are handed over as addresses of the library that the package has loaded.
 #include <ATen/core/Tensor.h>
@@ -36,6 +36,8 @@ struct Library {
     decltype(&ep_cross_entropy) cross_entropy;
     decltype(&ep_cross_entropy_backward_workspace_bytes) cross_entropy_backward_bytes;
     decltype(&ep_cross_entropy_backward) cross_entropy_backward;
+    decltype(&ep_experts_workspace_bytes) experts_bytes;
+    decltype(&ep_experts) experts;
 } lib{};
 PyObject *raise_status = nullptr;   // (context address, status, text or "") -> raises the package's exception
 
@@ -373,6 +375,78 @@ std::tuple<Maybe, Maybe, Maybe> cross_entropy_backward(int64_t ctx, int index, c
     return {dx, dweight, dbias};
 }
 
+std::tuple<Tensor, Tensor, Tensor> experts(int64_t ctx, int index, const Tensor &x, const Tensor &router, const Tensor &w1, const Tensor &w2,
+                                           int64_t k, const Maybe &router_bias, const Maybe &b1, const Maybe &b2, const std::string &act,
+                                           bool renormalize, const Maybe &residual, const Maybe &w1_scale, const Maybe &w2_scale,
+                                           const Maybe &valid) {
+    const Device d(ctx, index);
+    d.matrix(x, "x", -1, -1, true);
+    const ScalarType t = x.scalar_type();
+    need(is_float(t), "x must have dtype float32, bfloat16 or float16");
+    const int64_t rows = x.size(0), n_in = x.size(1);
+    d.matrix(router, "router", -1, n_in);
+    need(router.scalar_type() == t, "router must have x's dtype");
+    const int64_t parts = router.size(0);
+    need(parts <= Device::most, "router has too many rows");
+    // stacks: one matrix, or vector, for each part
+    auto stack = [&](const Tensor &m, const char *name, std::initializer_list<int64_t> size) {
+        d.on(m, name);
+        std::string wanted;
+        bool ok = m.dim() == (int64_t)size.size() && m.is_contiguous();
+        int64_t i = 0;
+        for (const int64_t s : size) {
+            ok = ok && (s < 0 || m.size(i) == s);
+            wanted += (i ? ", " : "") + (s < 0 ? std::string("any") : std::to_string(s));
+            ++i;
+        }
+        if (!ok) refuse(std::string(name) + " must be contiguous of shape (" + wanted + "), not " + shape_of(m));
+        for (i = 0; i < m.dim(); ++i)
+            if (m.size(i) > Device::most) refuse(std::string(name) + " is too wide");
+    };
+    stack(w1, "w1", {parts, -1, n_in});
+    const int64_t hidden = w1.size(1);
+    stack(w2, "w2", {parts, -1, hidden});
+    const int64_t n_out = w2.size(1);
+    const ScalarType w = w1.scalar_type();
+    need(w2.scalar_type() == w && (w == t || w == at::kChar), "w1 and w2 must both have x's dtype or int8");
+    need((w == at::kChar) == w1_scale.has_value() && (w == at::kChar) == w2_scale.has_value(),
+         "w1_scale and w2_scale go with int8 weights, and with no others");
+    auto scale = [&](const Maybe &s, const char *name, int64_t n) {
+        if (!s) return;
+        stack(*s, name, {parts, n});
+        need(s->scalar_type() == at::kFloat, std::string(name) + " must have dtype float32");
+    };
+    scale(w1_scale, "w1_scale", hidden);
+    scale(w2_scale, "w2_scale", n_out);
+    auto bias = [&](const Maybe &b, const char *name, int64_t n) {
+        if (!b) return;
+        stack(*b, name, {parts, n});
+        need(is_float(b->scalar_type()), std::string(name) + " must have dtype float32, bfloat16 or float16");
+    };
+    bias(b1, "b1", hidden);
+    bias(b2, "b2", n_out);
+    need(!b1 || !b2 || b1->scalar_type() == b2->scalar_type(), "b1 and b2 must have the same dtype");
+    d.floats(router_bias, "router_bias", parts);
+    const int a = activation(act);
+    check_k(k, parts);
+    check_valid(d, valid, rows);
+    if (residual) {
+        d.matrix(*residual, "residual", rows, n_out, true);
+        need(residual->scalar_type() == t, "residual must have x's dtype");
+    }
+    need(rows <= 64, "a layer of experts takes up to 64 rows, not " + std::to_string(rows));
+    const Tensor ws = d.workspace(lib.experts_bytes((ep_ctx *)ctx, rows, (int32_t)n_in, (int32_t)hidden, (int32_t)n_out, (int32_t)parts,
+                                                    (int32_t)k),
+                                  "shape out of range");
+    const Tensor out = d.empty({rows, n_out}, t), ids = d.empty({rows, k}, at::kInt), weights = d.empty({rows, k}, at::kFloat);
+    done(ctx, unlocked(lib.experts, (ep_ctx *)ctx, ptr(x), row_stride(x), type_of(t), ptr(router), ptr(router_bias), type_of(router_bias),
+                       (const uint8_t *)ptr(valid), (int32_t)k, renormalize, ptr(w1), (const float *)ptr(w1_scale), ptr(b1), ptr(w2),
+                       (const float *)ptr(w2_scale), ptr(b2), type_of(w), type_of(b1 ? b1 : b2), a, ptr(residual),
+                       residual ? row_stride(*residual) : 0, ptr(out), (int32_t *)ptr(ids), (float *)ptr(weights), rows, (int32_t)n_in,
+                       (int32_t)hidden, (int32_t)n_out, (int32_t)parts, ptr(ws), (size_t)ws.numel(), d.stream()));
+    return {out, ids, weights};
+}
+
 template <typename F>
 void take(F &f, const py::dict &addresses, const char *name) {
     f = reinterpret_cast<F>(addresses[name].cast<uintptr_t>());
@@ -397,6 +471,8 @@ PYBIND11_MODULE(_head, m) {
         take(lib.cross_entropy, a, "ep_cross_entropy");
         take(lib.cross_entropy_backward_bytes, a, "ep_cross_entropy_backward_workspace_bytes");
         take(lib.cross_entropy_backward, a, "ep_cross_entropy_backward");
+        take(lib.experts_bytes, a, "ep_experts_workspace_bytes");
+        take(lib.experts, a, "ep_experts");
         raise_status = on_error.release().ptr();   // kept for the life of the process
     });
     m.def("rms_norm", &rms_norm);
@@ -408,4 +484,5 @@ PYBIND11_MODULE(_head, m) {
     m.def("route_backward", &route_backward);
     m.def("cross_entropy", &cross_entropy);
     m.def("cross_entropy_backward", &cross_entropy_backward);
+    m.def("experts", &experts);
 }
