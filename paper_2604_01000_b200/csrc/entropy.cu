@@ -3,22 +3,28 @@
 //     l = x W^T + b;   lse = log sum_c exp l_c;   row_loss = lse - l_target;   loss = mean of row_loss over the rows that count
 //     G = (exp(l - lse) - [c = target]) g,  g = dloss / rows + drow;   dx = G W;   dW = G^T x;   db = column sums of G
 //
-// A piece (some rows by some classes) of logits is made by the products' tile kernel and stays in the L2; the row
-// kernels here go over it: the forward's keep a running maximum and sum for each row, the backward's make G of it, in the
-// operands' type, for two more products.
+// Of 16-bit inputs a tile of logits never leaves the tensor memory: the threads that read it there keep a running maximum
+// and sum for each row (forward), or make a tile of G of it (backward), in the operands' type, for two more products.  G exists a
+// piece at a time (some rows by some classes, small enough to stay in the L2 until both products have read it).
+// fp32 inputs are split into three bf16 numbers as in linear.cu; a piece of their logits is made by the products' own tile
+// kernel, and row kernels go over it to the same ends.
 #include "ep_common.cuh"
 #include "rows.cuh"
+#include "tile_device.cuh"
 
 #include <algorithm>
+#include <cfloat>
+#include <type_traits>
 
 using namespace eprow;
+using namespace eptile;
 using ep::Matrix;
 using ep::Operand;
 using ep::Packed;
 
 namespace {
 
-constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 // What is known of a row's softmax: exponentials sum to s with the maximum m taken out.
 struct Running {
@@ -37,14 +43,433 @@ __device__ __forceinline__ int target_of(const int32_t *targets, int64_t row, in
     return -1;
 }
 
+// ---------------------------------------------------------------------------------------------- logits by tiles
+//
+// A pair of blocks works on 256 rows x 256 classes at a time (see linear.cu, whose pipeline this is: one warp loads, one of
+// the first block multiplies, 16 finish a tile while the next one is being summed).  Workers share out the tiles evenly, in
+// one long line: row tile after row tile in the forward (a thread keeps its row's statistics from tile to tile), class tile after
+// class tile in the backward (a thread keeps its classes' sums), each worker a stretch of it.  What a worker has when its
+// stretch or its row (class) tile ends is a partial result, number `worker - first worker of that tile`.
+constexpr int TILE = 256;
+constexpr int BLOCK_ROWS = 128, PIECE_COLS = 64;   // a block's rows; the columns of a warp that finishes tiles
+constexpr int EPI_WARPS = 16, TILE_THREADS = 32 * (EPI_WARPS + 2);
+constexpr int STAGE_BYTES = 2 * BLOCK_ROWS * 128, SLOT_BYTES = 4096;
+
+struct TileShared {
+    uint64_t full[8], empty[8], t_full[2], t_empty[2], drain;
+    uint32_t tmem_base;
+    int abort;
+};
+template <bool GRAD>
+struct TileMemory {
+    static constexpr int STAGING = GRAD ? EPI_WARPS * SLOT_BYTES : 0;
+    static constexpr int STAGES = GRAD ? 5 : 6;
+    static constexpr int RING = STAGES * STAGE_BYTES;
+    static constexpr size_t TOTAL = 1024 + RING + STAGING + sizeof(TileShared);
+    static_assert(TOTAL <= 227 * 1024, "shared memory of a block");
+};
+
+// tiles = outer x inner, in a line with `inner` fastest; worker w of n has [tiles w / n, tiles (w + 1) / n).
+struct Line {
+    int64_t tiles;
+    int inner, workers;
+    __host__ __device__ int64_t begin(int w) const { return tiles * w / workers; }   // (below 2^47)
+    __host__ __device__ int worker_of(int64_t tile) const { return (int)(((tile + 1) * workers - 1) / tiles); }
+    __host__ __device__ int first_worker(int64_t outer) const { return worker_of(outer * inner); }
+    __host__ __device__ int last_worker(int64_t outer) const { return worker_of(outer * inner + inner - 1); }
+};
+struct Stretch {
+    int64_t left;
+    int outer, inner;
+    const int inners;
+    __device__ __forceinline__ Stretch(const Line &l, int worker) : inners(l.inner) {
+        const int64_t from = l.begin(worker);
+        left = l.begin(worker + 1) - from;
+        outer = (int)(from / l.inner);
+        inner = (int)(from - (int64_t)outer * l.inner);
+    }
+    __device__ __forceinline__ bool more() const { return left > 0; }
+    __device__ __forceinline__ void next() {
+        --left;
+        if (++inner == inners) {
+            inner = 0;
+            ++outer;
+        }
+    }
+};
+
+// What the blocks of entropy_weights have found, together.  fp16 holds nothing below 2^-25, where a mean over many rows puts
+// whole gradients: G is multiplied by the power of two that brings the largest |g| to [2^14, 2^15) (|p - 1| is at most 1), and
+// the products' sums by its inverse.
+struct Scale {
+    float up, down;
+    int unclean;
+};
+struct RowInfo {   // of the backward
+    float shift;   // -lse / log 2
+    float g;
+    int target;    // -1: none
+    float cap;     // infinity; of rows that take no part, -infinity: the largest exponent
+};
+struct TileWork {
+    int64_t M;
+    int N, class0, kb;
+    Line line;
+    uint32_t idesc;
+    const float *bias;        // / log 2, of all classes, padded by a tile; or NULL
+    const int32_t *targets;
+    float2 *partial;          // forward: [number * 4 + piece][M], over log 2
+    float *at_target;
+    unsigned *ticket;
+    const RowInfo *rows;      // backward
+    const Scale *scale;
+    float *sums;              // [number * 8 + block's and warp's rows][stride], or NULL
+    int64_t stride;
+};
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// 16 lanes of 64 accumulator columns: lane l holds rows l / 4 and l / 4 + 8, of each 8 columns two from 2 (l % 4) on:
+// v[4 c + 2 r + i] is column 8 c + 2 (l % 4) + i of row l / 4 + 8 r.
+__device__ __forceinline__ void tmem_ld_rows16(uint32_t taddr, uint32_t (&v)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+          "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+          "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+        : "r"(taddr)
+        : "memory");
+}
+// Four 8 x 8 matrices of 16-bit elements in the layout above, lane l's address that of row l % 8 of matrix l / 8.
+__device__ __forceinline__ void store_matrices(void *at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(smem_u32(at)), "r"(a), "r"(b), "r"(c), "r"(d)
+                 : "memory");
+}
+template <typename T>
+__device__ __forceinline__ uint32_t packed(float lo, float hi) {
+    if constexpr (std::is_same_v<T, __half>) {
+        const __half2 v = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    } else {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    }
+}
+
+template <bool GRAD, typename T>
+__global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                                                                 const __grid_constant__ CUtensorMap map_g, const TileWork e, int *status) {
+    using Mem = TileMemory<GRAD>;
+    constexpr int STAGES = Mem::STAGES;
+    extern __shared__ char smem_raw[];
+    char *ring = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    char *staging = ring + Mem::RING;
+    TileShared *sh = reinterpret_cast<TileShared *>(staging + Mem::STAGING);
+    const uint32_t rank = cluster_rank();     // rank 0 issues the MMAs
+    const int worker = blockIdx.x >> 1;
+    volatile int *abort_flag = &sh->abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(&sh->full[s], 1);
+            mbar_init(&sh->empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&sh->t_full[b], 1);
+            mbar_init(&sh->t_empty[b], 2 * EPI_WARPS);   // (of both blocks, at the first one's)
+        }
+        mbar_init(&sh->drain, 1);
+        sh->abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)), "r"(2 * TILE)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_meet();   // the other block's barriers are ready
+    tc_fence_after();
+    ep_wait_for_launch_before();
+    ep_let_next_launch_start();
+    const uint32_t tmem_base = sh->tmem_base;
+    if (!GRAD && blockIdx.x == 0 && threadIdx.x == 0) *e.ticket = 0;   // of entropy_finish
+    auto row_tile = [](const Stretch &t) { return GRAD ? t.inner : t.outer; };
+    auto class_tile = [](const Stretch &t) { return GRAD ? t.outer : t.inner; };
+    // columns that the MMAs compute: the last tile's are cut to what there is
+    auto columns = [&](int n) { return min(TILE, (e.N - n * TILE + 31) & ~31); };
+
+    if (warp == EPI_WARPS) {
+        uint32_t it = 0, s = 0, ph = 0;
+        bool ok = true;
+        const uint32_t ring_base = smem_u32(ring);
+        for (Stretch t(e.line, worker); ok && t.more(); t.next()) {
+            const int m = row_tile(t) * TILE + (int)rank * BLOCK_ROWS, n = class_tile(t) * TILE + (int)rank * (columns(class_tile(t)) / 2);
+            for (int kb = 0; kb < e.kb; ++kb, ++it) {
+                if (!(ok = mbar_wait_warp(&sh->empty[s], ph ^ 1u, abort_flag))) break;
+                if (rank == 0) mbar_expect_tx_elected(&sh->full[s], 2 * STAGE_BYTES);
+                const uint32_t bar = in_block(smem_u32(&sh->full[s]), 0), dst = ring_base + s * (uint32_t)STAGE_BYTES;
+                load_tile_elected<true>(dst, &map_x, kb * 64, m, 0, bar);
+                load_tile_elected<true>(dst + BLOCK_ROWS * 128, &map_w, kb * 64, n, 0, bar);
+                if (++s == (uint32_t)STAGES) {
+                    s = 0;
+                    ph ^= 1u;
+                }
+            }
+        }
+        // after an abort the loads already issued get time to land before the block leaves
+        if (rank == 0 && lane == 0 && (!ok || *abort_flag))
+#pragma unroll 1
+            for (uint32_t j = it > (uint32_t)STAGES ? it - (uint32_t)STAGES : 0u; j < it; ++j)
+                mbar_wait_quiet(&sh->full[j % (uint32_t)STAGES], (j / (uint32_t)STAGES) & 1u, DRAIN_LIMIT_CLOCKS);
+    } else if (warp == EPI_WARPS + 1) {
+        uint32_t acc = 0, s = 0, ph = 0;
+        bool ok = true;
+        const uint32_t ring_base = smem_u32(ring);
+        for (Stretch t(e.line, worker); rank == 0 && ok && t.more(); t.next(), ++acc) {
+            const uint32_t idesc = e.idesc | (uint32_t)(columns(class_tile(t)) >> 3) << 17;
+            const uint32_t buf = acc & 1u;
+            if (!(ok = mbar_wait_warp(&sh->t_empty[buf], ((acc >> 1) & 1u) ^ 1u, abort_flag))) break;
+            tc_fence_after();
+            for (int kb = 0; kb < e.kb; ++kb) {
+                if (!(ok = mbar_wait_warp(&sh->full[s], ph, abort_flag))) break;
+                tc_fence_after();
+                const uint32_t a = ring_base + s * (uint32_t)STAGE_BYTES;
+                umma_kblock_elected<HALF, true>(tmem_base + buf * TILE, operand_desc(a, false), operand_desc(a + BLOCK_ROWS * 128, false), 2,
+                                                2, idesc, kb > 0);
+                commit_elected<true>(&sh->empty[s]);
+                if (++s == (uint32_t)STAGES) {
+                    s = 0;
+                    ph ^= 1u;
+                }
+            }
+            if (ok) commit_elected<true>(&sh->t_full[buf]);
+        }
+        if (rank == 0 && __any_sync(FULL, !ok || *abort_flag)) {
+            commit_elected<true>(&sh->drain);
+            if (lane == 0) mbar_wait_quiet(&sh->drain, 0u, DRAIN_LIMIT_CLOCKS);
+        }
+    } else {
+        const int quad = warp & 3, piece = warp >> 2;   // TMEM lanes 32 quad.. and 64 columns are this warp's
+        const uint32_t t_empty = in_block(smem_u32(&sh->t_empty[0]), 0);
+        const uint32_t from = tmem_base + ((uint32_t)(quad * 32) << 16) + piece * PIECE_COLS;
+        auto give_back = [&](uint32_t buf) {   // the accumulator, once every column of it is in registers
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_at(t_empty + buf * 8);
+        };
+        uint32_t acc = 0;
+        if constexpr (!GRAD) {
+            float top = -FLT_MAX, sum = 0.f;   // (finite from the start: what is closed is below it)
+            int target = -1;
+            for (Stretch t(e.line, worker); t.more(); t.next(), ++acc) {
+                const int64_t row = (int64_t)t.outer * TILE + rank * BLOCK_ROWS + quad * 32 + lane;
+                const int col = t.inner * TILE + piece * PIECE_COLS;
+                if (acc == 0 || t.inner == 0) target = row < e.M ? e.targets[row] : -1;
+                const uint32_t buf = acc & 1u;
+                if (!mbar_wait_warp(&sh->t_full[buf], (acc >> 1) & 1u, abort_flag)) break;
+                tc_fence_after();
+                if (col < e.N && row - lane < e.M) {
+                    uint32_t a[32], b[32];
+                    tmem_ld32_issue(from + buf * TILE, a);
+                    tmem_ld32_issue(from + buf * TILE + 32, b);
+                    tmem_ld_wait(a);
+                    tmem_ld_wait(b);
+                    give_back(buf);
+                    Pair v[32];
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        v[j] = Pair(__uint_as_float(a[2 * j]), __uint_as_float(a[2 * j + 1]));
+                        v[16 + j] = Pair(__uint_as_float(b[2 * j]), __uint_as_float(b[2 * j + 1]));
+                    }
+                    const bool biased = e.bias != nullptr;
+                    if (biased) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) {
+                            const float4 add = *reinterpret_cast<const float4 *>(e.bias + col + 2 * j);
+                            v[j] = fma2(v[j], Pair(LOG2E), Pair(add.x, add.y));
+                            v[j + 1] = fma2(v[j + 1], Pair(LOG2E), Pair(add.z, add.w));
+                        }
+                    }
+                    float f[64];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j].get(f[2 * j], f[2 * j + 1]);
+                    if (col + PIECE_COLS > e.N) {
+#pragma unroll
+                        for (int j = 0; j < 64; ++j) f[j] = col + j < e.N ? f[j] : -INFINITY;
+                    }
+                    const int mine = target - col;
+                    if (__any_sync(FULL, (unsigned)mine < 64u)) {
+                        float at = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 64; ++j) at = j == mine ? f[j] : at;
+                        if ((unsigned)mine < 64u) e.at_target[row] = biased ? at : at * LOG2E;
+                    }
+                    float high = f[0];
+#pragma unroll
+                    for (int j = 1; j + 1 < 64; j += 2) high = max3(high, f[j], f[j + 1]);
+                    high = fmaxf(high, f[63]);
+                    const float scale = biased ? 1.f : LOG2E;
+                    const float now = fmaxf(top, high * scale);
+                    sum *= exp2_fast(top - now);
+                    top = now;
+                    Pair s0(0.f), s1(0.f);
+#pragma unroll
+                    for (int j = 0; j < 64; j += 4) {
+                        float x0, x1, x2, x3;
+                        fma2(Pair(f[j], f[j + 1]), Pair(scale), Pair(-now)).get(x0, x1);
+                        fma2(Pair(f[j + 2], f[j + 3]), Pair(scale), Pair(-now)).get(x2, x3);
+                        s0 = add2(s0, Pair(exp2_fast(x0), exp2_fast(x1)));
+                        s1 = add2(s1, Pair(exp2_fast(x2), exp2_fast(x3)));
+                    }
+                    float lo, hi;
+                    add2(s0, s1).get(lo, hi);
+                    sum += lo + hi;
+                } else
+                    give_back(buf);
+                if (t.left == 1 || t.inner + 1 == t.inners) {
+                    if (row < e.M) e.partial[((int64_t)(worker - e.line.first_worker(t.outer)) * 4 + piece) * e.M + row] = make_float2(top, sum);
+                    top = -FLT_MAX;
+                    sum = 0.f;
+                }
+            }
+        } else {
+            char *slot = staging + warp * SLOT_BYTES;
+            const float up = e.scale->up, down = e.scale->down;
+            Pair sums[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) sums[c] = Pair(0.f);
+            Pair bias[8];
+            for (Stretch t(e.line, worker); t.more(); t.next(), ++acc) {
+                const int64_t row0 = (int64_t)t.inner * TILE + rank * BLOCK_ROWS + quad * 32;
+                const int col = t.outer * TILE + piece * PIECE_COLS;
+                if (e.bias && (acc == 0 || t.inner == 0)) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        const float2 b = *reinterpret_cast<const float2 *>(e.bias + e.class0 + col + 8 * c + 2 * (lane & 3));
+                        bias[c] = Pair(b.x, b.y);
+                    }
+                }
+                RowInfo info[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t row = row0 + 8 * i + (lane >> 2);
+                    info[i] = row < e.M ? e.rows[row] : RowInfo{0.f, 0.f, -1, -INFINITY};
+                }
+                const uint32_t buf = acc & 1u;
+                if (!mbar_wait_warp(&sh->t_full[buf], (acc >> 1) & 1u, abort_flag)) break;
+                tc_fence_after();
+                if (col < e.N && row0 < e.M) {
+                    stores_read<0>();
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t a[32];
+                        tmem_ld_rows16(from + buf * TILE + ((uint32_t)(16 * h) << 16), a);
+                        tmem_ld_wait(a);
+                        if (h == 1) give_back(buf);
+                        float f[32];
+#pragma unroll
+                        for (int c = 0; c < 8; ++c)
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) {
+                                Pair v = fma2(Pair(__uint_as_float(a[4 * c + 2 * r]), __uint_as_float(a[4 * c + 2 * r + 1])), Pair(LOG2E),
+                                              Pair(info[2 * h + r].shift));
+                                if (e.bias) v = add2(v, bias[c]);
+                                v.get(f[4 * c + 2 * r], f[4 * c + 2 * r + 1]);
+                            }
+                        if (__any_sync(FULL, info[2 * h].cap < 0.f || info[2 * h + 1].cap < 0.f)) {   // whatever such rows hold
+#pragma unroll
+                            for (int q = 0; q < 32; ++q) f[q] = fminf(f[q], info[2 * h + (q >> 1 & 1)].cap);
+                        }
+#pragma unroll
+                        for (int q = 0; q < 32; ++q) f[q] = exp2_fast(f[q]);
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const int at = info[2 * h + r].target - e.class0 - col;
+                            const bool mine = (unsigned)at < 64u && ((at >> 1) & 3) == (lane & 3) && info[2 * h + r].target >= 0;
+                            const int index = mine ? (at >> 3) * 2 + (at & 1) : -1;
+                            if (__any_sync(FULL, mine)) {
+#pragma unroll
+                                for (int q = 0; q < 16; ++q) f[4 * (q >> 1) + 2 * r + (q & 1)] -= q == index ? 1.f : 0.f;
+                            }
+                        }
+                        uint32_t out[16];
+#pragma unroll
+                        for (int c = 0; c < 8; ++c)
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) {
+                                const Pair g = mul2(Pair(f[4 * c + 2 * r], f[4 * c + 2 * r + 1]), Pair(info[2 * h + r].g * up));
+                                if (e.sums) sums[c] = add2(sums[c], g);
+                                float lo, hi;
+                                g.get(lo, hi);
+                                out[2 * c + r] = packed<T>(lo, hi);
+                            }
+                        const int r = 16 * h + (lane & 15);   // the row whose address this lane gives
+#pragma unroll
+                        for (int c = 0; c < 8; c += 2)
+                            store_matrices(slot + r * 128 + (((c + (lane >> 4)) ^ (r & 7)) << 4), out[2 * c], out[2 * c + 1], out[2 * c + 2],
+                                           out[2 * c + 3]);
+                    }
+                    before_stores();
+                    tma_store_3d_elected(&map_g, slot, col, (int)row0, 0);
+                } else
+                    give_back(buf);
+                if (e.sums && (t.left == 1 || t.inner + 1 == t.inners)) {
+                    float *to = e.sums + ((int64_t)(worker - e.line.first_worker(t.outer)) * 8 + rank * 4 + quad) * e.stride + col;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        float lo, hi;
+                        sums[c].get(lo, hi);
+#pragma unroll
+                        for (int o = 4; o < 32; o <<= 1) {
+                            lo += __shfl_xor_sync(FULL, lo, o);
+                            hi += __shfl_xor_sync(FULL, hi, o);
+                        }
+                        const int at = 8 * c + 2 * (lane & 3);
+                        if (lane < 4 && col + at < e.N) to[at] = lo * down;
+                        if (lane < 4 && col + at + 1 < e.N) to[at + 1] = hi * down;
+                        sums[c] = Pair(0.f);
+                    }
+                }
+            }
+        }
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");   // what has been stored is written before the block ends
+    }
+    __syncthreads();
+    cluster_meet();   // neither block leaves while the other may still signal it
+    if (sh->abort && threadIdx.x == 0) ep_raise(status, EP_ERR_TIMEOUT);
+    if (warp == 0) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * TILE) : "memory");
+    }
+}
+
+// The classes' bias over log 2, padded to whole tiles.
+__global__ void __launch_bounds__(256) entropy_bias(const void *bias, int type, int classes, int padded, float *out) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= padded) return;
+    // (a finite bias stays finite: only -infinity closes a class)
+    const float b = c < classes ? load_param(bias, type, c) : 0.f;
+    out[c] = fabsf(b) < INFINITY ? fminf(fmaxf(b * LOG2E, -FLT_MAX), FLT_MAX) : b;
+}
+
 // ---------------------------------------------------------------------------------------------- forward
 // The statistics of rows over one piece of classes, added to those of the pieces before (first: there are none).
 // WARPS warps to a row.
 template <int WARPS>
 __global__ void __launch_bounds__(256) entropy_rows(const float *__restrict__ logits, int ld, int64_t rows, int classes, int class0,
                                                     const void *__restrict__ bias, int bias_type, const int32_t *__restrict__ targets,
-                                                    bool first, float2 *running, float *at_target) {
+                                                    bool first, float2 *running, float *at_target, unsigned *ticket) {
     __shared__ Running part[8];
+    if (blockIdx.x == 0 && threadIdx.x == 0) *ticket = 0;   // of entropy_finish
     const int lane = threadIdx.x % (32 * WARPS), warp = threadIdx.x >> 5;
     const int64_t row = (int64_t)blockIdx.x * (8 / WARPS) + warp / WARPS;
     Running r{-INFINITY, 0.f};
@@ -88,79 +513,103 @@ __global__ void __launch_bounds__(256) entropy_rows(const float *__restrict__ lo
     }
 }
 
-// lse and loss of each row from its statistics, and each block's sum of losses and count of rows that take part.
-constexpr int FINISH_ROWS = 1024;   // a block's
-__global__ void __launch_bounds__(256) entropy_finish(const float2 *__restrict__ running, const float *__restrict__ at_target,
-                                                      const int32_t *__restrict__ targets, int64_t rows, int classes, float *lse,
-                                                      float *row_loss, double *sums, long long *counts, int *status) {
+// Where the statistics of a row are: one pair, or as many as the tile kernel's workers left.
+struct Statistics {
+    const float2 *all;
+    int64_t M;
+    bool tiled;      // [4 number + piece][M], over log 2
+    Line line;
+    __device__ __forceinline__ Running of(int64_t row) const {
+        if (!tiled) return Running{all[row].x, all[row].y};
+        const int64_t tile = row / TILE;
+        const int n = 4 * (line.last_worker(tile) - line.first_worker(tile) + 1);
+        float top = -FLT_MAX, sum = 0.f;
+        for (int i = 0; i < n; i += 4) {
+            float2 v[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = all[(int64_t)(i + q) * M + row];
+            const float now = fmaxf(max3(v[0].x, v[1].x, v[2].x), fmaxf(v[3].x, top));
+            sum *= exp2_fast(top - now);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sum = fmaf(v[q].y, exp2_fast(v[q].x - now), sum);
+            top = now;
+        }
+        return Running{sum == 0.f ? -INFINITY : top * LN2, sum};
+    }
+};
+
+// lse and loss of each row from its statistics, and each block's sum of losses and count of rows that take part; the block
+// that finishes last (the ticket tells) makes the mean of them.
+constexpr int FINISH_ROWS = 256;   // a block's
+struct Finish {
+    double *sums;
+    long long *counts;
+    unsigned *ticket;
+    float *loss;
+    long long *counted;
+};
+__device__ __forceinline__ void sum_block(double &total, long long &live, double (&sum)[8], long long (&count)[8]) {
+#pragma unroll
+    for (int o = 16; o >= 1; o >>= 1) {
+        total += __shfl_xor_sync(FULL, total, o);
+        live += __shfl_xor_sync(FULL, live, o);
+    }
+    if ((threadIdx.x & 31) == 0) {
+        sum[threadIdx.x >> 5] = total;
+        count[threadIdx.x >> 5] = live;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0)
+        for (int w = 1; w < 8; ++w) {
+            total += sum[w];
+            live += count[w];
+        }
+}
+__global__ void __launch_bounds__(256) entropy_finish(const Statistics stats, const float *at_target, const int32_t *targets, int64_t rows,
+                                                      int classes, float *lse, float *row_loss, const Finish f, int *status) {
     __shared__ double sum[8];
-    __shared__ int count[8];
+    __shared__ long long count[8];
+    __shared__ bool last;
+    ep_wait_for_launch_before();
     double total = 0.0;
-    int live = 0;
-    for (int i = threadIdx.x; i < FINISH_ROWS; i += 256) {
-        const int64_t row = (int64_t)blockIdx.x * FINISH_ROWS + i;
-        if (row >= rows) break;
+    long long live = 0;
+    const int64_t row = (int64_t)blockIdx.x * FINISH_ROWS + threadIdx.x;
+    if (row < rows) {
         float z = 0.f, loss = 0.f;
         if (target_of(targets, row, classes, status) >= 0) {
-            const float2 r = running[row];
-            z = r.x + logf(r.y);
-            if (r.x == -INFINITY && r.y == 0.f)   // every class is closed: the row takes no part
+            const Running r = stats.of(row);
+            z = r.m + logf(r.s);
+            if (r.m == -INFINITY && r.s == 0.f)   // every class is closed: the row takes no part
                 z = -INFINITY;
             else {
-                loss = z - at_target[row];
-                ++live;
+                loss = z - at_target[row] * (stats.tiled ? LN2 : 1.f);
+                live = 1;
             }
         }
         lse[row] = z;
         row_loss[row] = loss;
-        total += (double)loss;
+        total = (double)loss;
     }
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) {
-        total += __shfl_xor_sync(FULL, total, o);
-        live += __shfl_xor_sync(FULL, live, o);
-    }
-    if ((threadIdx.x & 31) == 0) {
-        sum[threadIdx.x >> 5] = total;
-        count[threadIdx.x >> 5] = live;
+    sum_block(total, live, sum, count);
+    if (threadIdx.x == 0) {
+        f.sums[blockIdx.x] = total;
+        f.counts[blockIdx.x] = live;
+        __threadfence();
+        last = atomicAdd(f.ticket, 1u) == gridDim.x - 1;
     }
     __syncthreads();
+    if (!last) return;
+    __threadfence();
+    total = 0.0;
+    live = 0;
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += 256) {
+        total += __ldcg(f.sums + i);
+        live += __ldcg(f.counts + i);
+    }
+    sum_block(total, live, sum, count);
     if (threadIdx.x == 0) {
-        for (int w = 1; w < 8; ++w) {
-            total += sum[w];
-            live += count[w];
-        }
-        sums[blockIdx.x] = total;
-        counts[blockIdx.x] = live;
-    }
-}
-__global__ void __launch_bounds__(256) entropy_mean(const double *__restrict__ sums, const long long *__restrict__ counts, int blocks,
-                                                    float *loss, long long *counted) {
-    __shared__ double sum[8];
-    __shared__ long long count[8];
-    double total = 0.0;
-    long long live = 0;
-    for (int i = threadIdx.x; i < blocks; i += 256) {
-        total += sums[i];
-        live += counts[i];
-    }
-#pragma unroll
-    for (int o = 16; o >= 1; o >>= 1) {
-        total += __shfl_xor_sync(FULL, total, o);
-        live += __shfl_xor_sync(FULL, live, o);
-    }
-    if ((threadIdx.x & 31) == 0) {
-        sum[threadIdx.x >> 5] = total;
-        count[threadIdx.x >> 5] = live;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < 8; ++w) {
-            total += sum[w];
-            live += count[w];
-        }
-        *loss = (float)(total / (double)(live > 0 ? live : 1));
-        *counted = live;
+        *f.loss = (float)(total / (double)(live > 0 ? live : 1));
+        *f.counted = live;
     }
 }
 
@@ -172,7 +621,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) entropy_weights(const float *__restrict__ lse, const int32_t *__restrict__ targets, int64_t rows,
                                                        int classes, const long long *__restrict__ counted,
                                                        const float *__restrict__ dloss, const float *__restrict__ drow,
-                                                       const T *__restrict__ x, int64_t ldx, int n_in, float *weights, float *peaks,
+                                                       const T *__restrict__ x, int64_t ldx, int n_in, RowInfo *info, float *peaks,
                                                        int *unclean, int *status) {
     __shared__ int bad_rows;
     __shared__ float tops[8];
@@ -187,7 +636,8 @@ __global__ void __launch_bounds__(256) entropy_weights(const float *__restrict__
         if (row < rows) {
             dead = target_of(targets, row, classes, status) < 0 || lse[row] == -INFINITY;
             const float g = dead ? 0.f : (float)(mean + (drow ? (double)drow[row] : 0.0));
-            weights[row] = g;
+            const float z = lse[row];
+            info[row] = dead ? RowInfo{0.f, 0.f, -1, -INFINITY} : RowInfo{-z * LOG2E, z != z ? z : g, targets[row], INFINITY};
             if (fabsf(g) < INFINITY) top = fmaxf(top, fabsf(g));
         }
         if (!x) continue;
@@ -209,13 +659,6 @@ __global__ void __launch_bounds__(256) entropy_weights(const float *__restrict__
     }
 }
 
-// What the blocks of entropy_weights have found, together.  fp16 holds nothing below 2^-25, where a mean over many rows puts
-// whole gradients: G is multiplied by the power of two that brings the largest |g| to [2^14, 2^15) (|p - 1| is at most 1), and
-// the products' sums by its inverse.
-struct Scale {
-    float up, down;
-    int unclean;
-};
 __global__ void __launch_bounds__(256) entropy_scale(const float *__restrict__ peaks, const int *__restrict__ unclean, int n, bool scaled,
                                                      Scale *out) {
     __shared__ float tops[8];
@@ -240,13 +683,11 @@ __global__ void __launch_bounds__(256) entropy_scale(const float *__restrict__ p
 // copy of x already, of `parts` matrices.
 template <typename E>
 __global__ void __launch_bounds__(256) entropy_clean(const E *__restrict__ from, int64_t ld, int64_t rows, int cols,
-                                                     const int32_t *__restrict__ targets, const float *__restrict__ lse, int classes,
-                                                     const Scale *scale, E *to, int ld_to, int parts, int64_t part_stride) {
+                                                     const RowInfo *__restrict__ info, const Scale *scale, E *to, int ld_to, int parts, int64_t part_stride) {
     if (!scale->unclean) return;
     const int lane = threadIdx.x & 31;
     for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < rows; row += (int64_t)gridDim.x * 8) {
-        const int t = targets[row];
-        const bool dead = t < 0 || t >= classes || lse[row] == -INFINITY;
+        const bool dead = info[row].target < 0;
         if (from)
             for (int c = lane; c < cols; c += 32) to[row * ld_to + c] = dead ? E{} : from[row * ld + c];
         else if (dead)
@@ -260,8 +701,8 @@ __global__ void __launch_bounds__(256) entropy_clean(const E *__restrict__ from,
 constexpr int G_CHUNKS = 16, G_ROWS = 16;   // a block covers 128 classes, 16 rows at a time
 template <typename T>
 __global__ void __launch_bounds__(256) entropy_slopes(const float *__restrict__ logits, int ld, int64_t rows, int classes, int class0,
-                                                      const void *__restrict__ bias, int bias_type, const int32_t *__restrict__ targets,
-                                                      const float *__restrict__ lse, const float *__restrict__ weights,
+                                                      const void *__restrict__ bias, int bias_type,
+                                                      const float *__restrict__ lse, const RowInfo *__restrict__ info,
                                                       const Scale *__restrict__ scale, void *to_raw, int64_t part_stride, float *part,
                                                       int64_t stride) {
     constexpr bool SPLIT = sizeof(T) == 4;
@@ -279,12 +720,13 @@ __global__ void __launch_bounds__(256) entropy_slopes(const float *__restrict__ 
         for (int64_t row = (int64_t)blockIdx.y * G_ROWS + r0; row < rows; row += (int64_t)gridDim.y * G_ROWS) {
             float v[8];
             load_chunk(logits + row * ld, col, 1 << 30, true, 0.f, v);
-            const float g = weights[row], z = lse[row];
-            const int mine = g != 0.f ? targets[row] - class0 : -1;
+            const float g = info[row].g, z = lse[row];
+            const bool live = info[row].target >= 0;
+            const int mine = live ? info[row].target - class0 : -1;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float p = exp_fast(v[i] + b[i] - z) - (col + i == mine ? 1.f : 0.f);
-                v[i] = g != 0.f && col + i < classes ? p * g : 0.f;
+                v[i] = live && col + i < classes ? p * g : 0.f;
                 sum[i] += v[i];
                 v[i] *= up;
             }
@@ -331,7 +773,8 @@ __global__ void __launch_bounds__(256) entropy_round(const float *__restrict__ s
 
 // ---------------------------------------------------------------------------------------------- host side
 constexpr int MAX_WIDTH = 65536, MAX_CLASSES = 1 << 24;
-constexpr int64_t PIECE = 1 << 24;   // elements of a piece
+// Elements of a piece: of fp32 logits, of which G is made beside them; of G alone.
+constexpr int64_t LOGITS_PIECE = 1 << 24, SLOPES_PIECE = 1 << 25;
 
 // Rows x classes in pieces; of the shorter side as much as goes, so that little of what is summed over pieces is large.
 struct Pieces {
@@ -340,15 +783,15 @@ struct Pieces {
     int64_t across;   // pieces along the rows
     int down;         // and along the classes
 };
-Pieces make_pieces(int64_t rows, int classes) {
+Pieces make_pieces(int64_t rows, int classes, int64_t piece) {
     Pieces p;
     auto up = [](int64_t v) { return std::max<int64_t>(1, (v + 255) / 256) * 256; };
     if (rows >= classes) {
         p.classes = std::min(classes, 16384);
-        p.rows = std::min(rows, std::max<int64_t>(256, PIECE / up(p.classes) / 256 * 256));
+        p.rows = std::min(rows, std::max<int64_t>(256, piece / up(p.classes) / 256 * 256));
     } else {
         p.rows = std::min<int64_t>(rows, 16384);
-        p.classes = (int)std::min<int64_t>(classes, std::max<int64_t>(256, PIECE / up(p.rows) / 256 * 256));
+        p.classes = (int)std::min<int64_t>(classes, std::max<int64_t>(256, piece / up(p.rows) / 256 * 256));
     }
     p.across = rows ? ep::ceil_div(rows, p.rows) : 0;
     p.down = (int)ep::ceil_div(classes, p.classes);
@@ -369,78 +812,16 @@ bool entropy_shape_ok(int64_t rows, int n_in, int classes) {
     return rows >= 0 && rows <= (1ll << 31) - 256 && n_in >= 1 && n_in <= MAX_WIDTH && classes >= 1 && classes <= MAX_CLASSES;
 }
 
-struct ForwardSpace {
-    void *x, *w;
-    float *logits, *share, *at_target;
-    float2 *running;
-    double *sums;
-    long long *counts;
-    Pieces pieces;
-    size_t bytes;
-};
-ForwardSpace forward_space(const ep_ctx *ctx, int64_t rows, int n_in, int classes, int type, bool aligned, void *base) {
-    ep::Arena a(base);
-    ForwardSpace s{};
-    s.pieces = make_pieces(rows, classes);
-    if (type == EP_F32 || !aligned) {
-        s.x = a.take<char>(ep::packed_form(rows, n_in, type).bytes);
-        s.w = a.take<char>(ep::packed_form(classes, n_in, type).bytes);
-    }
-    if (rows) {
-        s.logits = a.take<float>(s.pieces.rows * padded(s.pieces.classes));
-        s.share = a.take<float>(most_of(s.pieces, rows, classes, [&](int64_t r, int c) { return ep::product_bytes(ctx, r, padded(c), n_in, type, EP_F32); }) / 4);
-    }
-    s.at_target = a.take<float>(rows);
-    s.running = a.take<float2>(rows);
-    s.sums = a.take<double>(ep::ceil_div(rows, FINISH_ROWS));
-    s.counts = a.take<long long>(ep::ceil_div(rows, FINISH_ROWS));
-    s.bytes = std::max<size_t>(a.used, 256);
-    return s;
+Line line_of(const ep_ctx *ctx, int64_t outer, int64_t inner) {
+    Line l;
+    l.tiles = outer * inner;
+    l.inner = (int)inner;
+    l.workers = (int)std::min<int64_t>(l.tiles, ctx->sm_count / 2);
+    return l;
 }
-
-struct Backward {
-    void *x, *w;          // copies
-    void *g;
-    float *logits, *share, *dx, *dweight, *part, *weights, *peaks;
-    int *unclean;
-    Scale *scale;
-    Pieces pieces;
-    int blocks;           // of entropy_weights
-    int slabs;            // of a piece's rows, for the columns' sums
-    size_t bytes;
-};
-Backward backward_space(const ep_ctx *ctx, int64_t rows, int n_in, int classes, int type, bool aligned, void *base) {
-    ep::Arena a(base);
-    Backward s{};
-    s.pieces = make_pieces(rows, classes);
-    const Pieces &p = s.pieces;
-    const Packed x = ep::packed_form(rows, n_in, type);
-    s.x = a.take<char>(x.bytes);   // (of aligned 16-bit x too: see entropy_clean)
-    if (type == EP_F32 || !aligned) s.w = a.take<char>(ep::packed_form(classes, n_in, type).bytes);
-    if (rows) {
-        s.g = a.take<char>(ep::packed_form(p.rows, p.classes, type).bytes);
-        s.logits = a.take<float>(p.rows * padded(p.classes));
-        s.share = a.take<float>(most_of(p, rows, classes, [&](int64_t r, int c) {
-                                    size_t most = ep::product_bytes(ctx, r, padded(c), n_in, type, EP_F32);
-                                    for (int out : {type, (int)EP_F32}) {
-                                        most = std::max(most, ep::product_bytes(ctx, r, n_in, c, type, out));
-                                        most = std::max(most, ep::product_bytes(ctx, c, n_in, r, type, out));
-                                    }
-                                    return most;
-                                }) / 4);
-        if (type != EP_F32 && p.down > 1) s.dx = a.take<float>(p.rows * n_in);
-        if (type != EP_F32 && p.across > 1) s.dweight = a.take<float>((int64_t)classes * n_in);
-        const int want = std::max(1, ctx->sm_count * 4 / (int)ep::ceil_div(p.classes, G_CHUNKS * 8));
-        s.slabs = (int)std::max<int64_t>(1, std::min<int64_t>(want, ep::ceil_div(p.rows, 2 * G_ROWS)));
-        s.part = a.take<float>((size_t)p.across * s.slabs * classes);
-    }
-    s.weights = a.take<float>(rows);
-    s.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(rows, 256), ctx->sm_count * 2));
-    s.peaks = a.take<float>(s.blocks);
-    s.unclean = a.take<int>(s.blocks);
-    s.scale = a.take<Scale>(1);
-    s.bytes = std::max<size_t>(a.used, 256);
-    return s;
+// The most workers that share a tile of the outer kind.
+int64_t most_workers(const Line &l) {
+    return std::min<int64_t>(l.workers, ep::ceil_div(l.inner, std::max<int64_t>(1, l.tiles / l.workers)) + 1);
 }
 
 struct Inputs {
@@ -459,6 +840,20 @@ struct Inputs {
     int kernels;
 };
 
+// Copies of the operands, and the bias as the tile kernel reads it.
+struct Copies {
+    void *x, *w;
+    float *bias;
+};
+Copies copies_space(ep::Arena &a, int64_t rows, int n_in, int classes, int type, bool aligned, bool x_always) {
+    Copies c{};
+    const bool copy = type == EP_F32 || !aligned;
+    if (copy || x_always) c.x = a.take<char>(ep::packed_form(rows, n_in, type).bytes);
+    if (copy) c.w = a.take<char>(ep::packed_form(classes, n_in, type).bytes);
+    if (type != EP_F32) c.bias = a.take<float>(ep::ceil_div(classes, TILE) * TILE);
+    return c;
+}
+
 // `rows` of an operand from row `first` on.
 Operand rows_of(Operand o, int64_t first, int64_t rows) {
     o.base = static_cast<const char *>(o.base) + first * o.ld * ep::type_size(o.type);
@@ -466,12 +861,18 @@ Operand rows_of(Operand o, int64_t first, int64_t rows) {
     return o;
 }
 
-int operands(ep_ctx *ctx, Inputs &in, void *x_room, void *w_room, Operand *x, Operand *w) {
+int operands(ep_ctx *ctx, Inputs &in, const Copies &c, Operand *x, Operand *w) {
+    if (c.bias && in.bias) {
+        const int n = (int)ep::ceil_div(in.classes, TILE) * TILE;
+        entropy_bias<<<n / 256, 256, 0, in.stream>>>(in.bias, in.bias_type, in.classes, n, c.bias);
+        EP_CUDA(ctx, cudaGetLastError());
+        ++in.kernels;
+    }
     *x = Operand{in.x, in.type, in.rows, in.n_in, in.ldx, 1, 0};
     *w = Operand{in.w, in.type, in.classes, in.n_in, in.ldw, 1, 0};
     if (in.type != EP_F32 && in.aligned) return EP_OK;
-    return ep::make_operands(ctx, Matrix{in.x, in.ldx, in.rows, in.n_in, x_room}, Matrix{in.w, in.ldw, in.classes, in.n_in, w_room},
-                             in.type, in.stream, x, w, &in.kernels);
+    return ep::make_operands(ctx, Matrix{in.x, in.ldx, in.rows, in.n_in, c.x}, Matrix{in.w, in.ldw, in.classes, in.n_in, c.w}, in.type,
+                             in.stream, x, w, &in.kernels);
 }
 
 int logits_of(ep_ctx *ctx, Inputs &in, const Operand &x, const Operand &w, int64_t row0, int64_t rows, int class0, int classes,
@@ -480,11 +881,92 @@ int logits_of(ep_ctx *ctx, Inputs &in, const Operand &x, const Operand &w, int64
                        EP_F32, false, nullptr, share, in.stream, &in.kernels);
 }
 
+template <bool GRAD, typename T>
+int launch_tiles_of(ep_ctx *ctx, const CUtensorMap &x, const CUtensorMap &w, const CUtensorMap &g, const TileWork &e, cudaStream_t stream) {
+    auto kernel = entropy_tiles<GRAD, T>;
+    constexpr size_t smem = TileMemory<GRAD>::TOTAL;
+    EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(2 * e.line.workers));
+    cfg.blockDim = dim3(TILE_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attrs[2] = {};
+    attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attrs[0].val.programmaticStreamSerializationAllowed = 1;
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = 2;
+    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+    cfg.attrs = attrs;
+    cfg.numAttrs = 2;
+    EP_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, x, w, g, e, ctx->d_status));
+    return EP_OK;
+}
+// g: of the backward, [rows][ld].
+template <bool GRAD>
+int launch_tiles(ep_ctx *ctx, const Operand &x, const Operand &w, void *g, int64_t ld, TileWork &e, cudaStream_t stream, int *kernels) {
+    const uint32_t fmt = x.type == EP_BF16 ? 1u : 0u;
+    e.idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(TILE >> 4) << 24);
+    e.kb = (int)ep::ceil_div(x.cols, 64);
+    CUtensorMap mx{}, mw{}, mg{};
+    if (!encode_operand(&mx, x, false, BLOCK_ROWS) || !encode_operand(&mw, w, false, BLOCK_ROWS) ||
+        (GRAD && !encode_result(&mg, g, x.type, 1, e.M, e.N, ld, TILE)))
+        return ep::fail(ctx, EP_ERR_CUDA, "cuTensorMapEncodeTiled failed for %lld rows of %d classes", (long long)e.M, e.N);
+    ++*kernels;
+    return x.type == EP_BF16 ? launch_tiles_of<GRAD, __nv_bfloat16>(ctx, mx, mw, mg, e, stream)
+                             : launch_tiles_of<GRAD, __half>(ctx, mx, mw, mg, e, stream);
+}
+
+struct ForwardSpace {
+    Copies copies;
+    float *logits, *share, *at_target;
+    float2 *stats;
+    Finish finish;
+    Pieces pieces;   // of fp32
+    Line line;       // of 16 bits
+    size_t bytes;
+};
+ForwardSpace forward_space(const ep_ctx *ctx, int64_t rows, int n_in, int classes, int type, bool aligned, void *base) {
+    ep::Arena a(base);
+    ForwardSpace s{};
+    s.copies = copies_space(a, rows, n_in, classes, type, aligned, false);
+    if (rows && type == EP_F32) {
+        s.pieces = make_pieces(rows, classes, LOGITS_PIECE);
+        s.logits = a.take<float>(s.pieces.rows * padded(s.pieces.classes));
+        s.share = a.take<float>(most_of(s.pieces, rows, classes, [&](int64_t r, int c) { return ep::product_bytes(ctx, r, padded(c), n_in, type, EP_F32); }) / 4);
+        s.stats = a.take<float2>(rows);
+    } else if (rows) {
+        s.line = line_of(ctx, ep::ceil_div(rows, TILE), ep::ceil_div(classes, TILE));
+        s.stats = a.take<float2>((size_t)most_workers(s.line) * 4 * rows);
+    }
+    s.at_target = a.take<float>(rows);
+    s.finish.sums = a.take<double>(ep::ceil_div(rows, FINISH_ROWS));
+    s.finish.counts = a.take<long long>(ep::ceil_div(rows, FINISH_ROWS));
+    s.finish.ticket = a.take<unsigned>(1);
+    s.bytes = std::max<size_t>(a.used, 256);
+    return s;
+}
+
 int forward_run(ep_ctx *ctx, Inputs &in, const ForwardSpace &s, float *loss, float *row_loss, float *lse, long long *counted) {
     Operand x, w;
-    int rc = operands(ctx, in, s.x, s.w, &x, &w);
+    int rc = operands(ctx, in, s.copies, &x, &w);
+    if (rc != EP_OK) return rc;
+    Statistics stats{s.stats, in.rows, in.type != EP_F32, s.line};
+    if (stats.tiled) {
+        TileWork e{};
+        e.M = in.rows;
+        e.N = in.classes;
+        e.line = s.line;
+        e.bias = in.bias ? s.copies.bias : nullptr;
+        e.targets = in.targets;
+        e.partial = s.stats;
+        e.at_target = s.at_target;
+        e.ticket = s.finish.ticket;
+        rc = launch_tiles<false>(ctx, x, w, nullptr, 0, e, in.stream, &in.kernels);
+        if (rc != EP_OK) return rc;
+    }
     const Pieces &p = s.pieces;
-    for (int64_t row0 = 0; rc == EP_OK && row0 < in.rows; row0 += p.rows)
+    for (int64_t row0 = 0; !stats.tiled && row0 < in.rows; row0 += p.rows)
         for (int class0 = 0; class0 < in.classes; class0 += p.classes) {
             const int64_t rows = std::min(p.rows, in.rows - row0);
             const int classes = std::min(p.classes, in.classes - class0);
@@ -494,18 +976,67 @@ int forward_run(ep_ctx *ctx, Inputs &in, const ForwardSpace &s, float *loss, flo
             auto kernel = wide ? entropy_rows<8> : entropy_rows<1>;
             kernel<<<(unsigned)ep::ceil_div(rows, wide ? 1 : 8), 256, 0, in.stream>>>(
                 s.logits, padded(classes), rows, classes, class0, in.bias, in.bias_type, in.targets + row0, class0 == 0,
-                s.running + row0, s.at_target + row0);
+                s.stats + row0, s.at_target + row0, s.finish.ticket);
             EP_CUDA(ctx, cudaGetLastError());
             ++in.kernels;
         }
-    if (rc != EP_OK) return rc;
-    const int blocks = (int)ep::ceil_div(in.rows, FINISH_ROWS);
-    entropy_finish<<<blocks, 256, 0, in.stream>>>(s.running, s.at_target, in.targets, in.rows, in.classes, lse, row_loss, s.sums,
-                                                  s.counts, ctx->d_status);
-    entropy_mean<<<1, 256, 0, in.stream>>>(s.sums, s.counts, blocks, loss, counted);
-    EP_CUDA(ctx, cudaGetLastError());
-    in.kernels += 2;
+    Finish f = s.finish;
+    f.loss = loss;
+    f.counted = counted;
+    EP_CUDA(ctx, ep::launch_early(entropy_finish, dim3((unsigned)ep::ceil_div(in.rows, FINISH_ROWS)), dim3(256), 0, in.stream, stats, s.at_target,
+                                  in.targets, in.rows, in.classes, lse, row_loss, f, ctx->d_status));
+    ++in.kernels;
     return EP_OK;
+}
+
+struct Backward {
+    Copies copies;
+    void *g;
+    float *logits, *share, *dx, *dweight, *part, *peaks;
+    RowInfo *rows;
+    int *unclean;
+    Scale *scale;
+    Pieces pieces;
+    int blocks;           // of entropy_weights
+    int64_t slabs;        // partial sums of a piece's columns
+    size_t bytes;
+};
+Backward backward_space(const ep_ctx *ctx, int64_t rows, int n_in, int classes, int type, bool aligned, void *base) {
+    ep::Arena a(base);
+    Backward s{};
+    const bool f32 = type == EP_F32;
+    s.copies = copies_space(a, rows, n_in, classes, type, aligned, true);   // (x: see entropy_clean)
+    if (rows) {
+        s.pieces = make_pieces(rows, classes, f32 ? LOGITS_PIECE : SLOPES_PIECE);
+        const Pieces &p = s.pieces;
+        s.g = a.take<char>(ep::packed_form(p.rows, p.classes, type).bytes);
+        if (f32) s.logits = a.take<float>(p.rows * padded(p.classes));
+        s.share = a.take<float>(most_of(p, rows, classes, [&](int64_t r, int c) {
+                                    size_t most = f32 ? ep::product_bytes(ctx, r, padded(c), n_in, type, EP_F32) : 0;
+                                    for (int out : {type, (int)EP_F32}) {
+                                        most = std::max(most, ep::product_bytes(ctx, r, n_in, c, type, out));
+                                        most = std::max(most, ep::product_bytes(ctx, c, n_in, r, type, out));
+                                    }
+                                    return most;
+                                }) / 4);
+        if (!f32 && p.down > 1) s.dx = a.take<float>(p.rows * n_in);
+        if (!f32 && p.across > 1) s.dweight = a.take<float>((int64_t)classes * n_in);
+        if (f32) {
+            const int want = std::max(1, ctx->sm_count * 4 / (int)ep::ceil_div(p.classes, G_CHUNKS * 8));
+            s.slabs = std::max<int64_t>(1, std::min<int64_t>(want, ep::ceil_div(p.rows, 2 * G_ROWS)));
+        } else
+            s.slabs = 8 * (int64_t)most_of(p, rows, classes, [&](int64_t r, int c) {
+                          return most_workers(line_of(ctx, ep::ceil_div(c, TILE), ep::ceil_div(r, TILE)));
+                      });
+        s.part = a.take<float>((size_t)p.across * s.slabs * classes);
+    }
+    s.rows = a.take<RowInfo>(rows);
+    s.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(rows, 256), ctx->sm_count * 2));
+    s.peaks = a.take<float>(s.blocks);
+    s.unclean = a.take<int>(s.blocks);
+    s.scale = a.take<Scale>(1);
+    s.bytes = std::max<size_t>(a.used, 256);
+    return s;
 }
 
 struct Given {
@@ -520,15 +1051,46 @@ struct Wanted {
 template <typename T>
 void launch_weights(ep_ctx *ctx, const Inputs &in, const Backward &s, const Given &g, bool look) {
     entropy_weights<T><<<s.blocks, 256, 0, in.stream>>>(g.lse, in.targets, in.rows, in.classes, g.counted, g.dloss, g.drow,
-                                                        look ? (const T *)in.x : nullptr, in.ldx, in.n_in, s.weights, s.peaks, s.unclean,
+                                                        look ? (const T *)in.x : nullptr, in.ldx, in.n_in, s.rows, s.peaks, s.unclean,
                                                         ctx->d_status);
     entropy_scale<<<1, 256, 0, in.stream>>>(s.peaks, s.unclean, s.blocks, in.type == EP_F16, s.scale);
 }
 
-template <typename T>
-void launch_round(const float *sums, int64_t n, const Scale *scale, void *out, int sm_count, cudaStream_t stream) {
-    const int grid = (int)std::min<int64_t>(ep::ceil_div(n, 1024), (int64_t)sm_count * 8);
-    entropy_round<T><<<grid, 256, 0, stream>>>(sums, n, scale, static_cast<T *>(out));
+int launch_round(ep_ctx *ctx, Inputs &in, const float *sums, int64_t n, const Scale *scale, void *out) {
+    const int grid = (int)std::min<int64_t>(ep::ceil_div(n, 1024), (int64_t)ctx->sm_count * 8);
+    if (in.type == EP_BF16)
+        entropy_round<<<grid, 256, 0, in.stream>>>(sums, n, scale, static_cast<__nv_bfloat16 *>(out));
+    else
+        entropy_round<<<grid, 256, 0, in.stream>>>(sums, n, scale, static_cast<__half *>(out));
+    EP_CUDA(ctx, cudaGetLastError());
+    ++in.kernels;
+    return EP_OK;
+}
+
+// G of one piece, and its columns' partial sums.
+int slopes_of(ep_ctx *ctx, Inputs &in, const Backward &s, const Given &given, const Operand &x, const Operand &w, int64_t row0, int64_t rows,
+              int class0, int classes, const Packed &f, bool wanted, float *part) {
+    if (in.type == EP_F32) {
+        const int rc = logits_of(ctx, in, x, w, row0, rows, class0, classes, s.logits, s.share);
+        if (rc != EP_OK) return rc;
+        entropy_slopes<float><<<dim3((unsigned)ep::ceil_div(f.ld, G_CHUNKS * 8), (unsigned)s.slabs), 256, 0, in.stream>>>(
+            s.logits, f.ld, rows, classes, class0, in.bias, in.bias_type, given.lse + row0, s.rows + row0, s.scale, wanted ? s.g : nullptr,
+            f.part_stride, part, in.classes);
+        EP_CUDA(ctx, cudaGetLastError());
+        ++in.kernels;
+        return EP_OK;
+    }
+    TileWork e{};
+    e.M = rows;
+    e.N = classes;
+    e.class0 = class0;
+    e.line = line_of(ctx, ep::ceil_div(classes, TILE), ep::ceil_div(rows, TILE));
+    e.bias = in.bias ? s.copies.bias : nullptr;
+    e.rows = s.rows + row0;
+    e.scale = s.scale;
+    e.sums = part;
+    e.stride = in.classes;
+    return launch_tiles<true>(ctx, rows_of(x, row0, rows), rows_of(w, class0, classes), s.g, f.ld, e, in.stream, &in.kernels);
 }
 
 int backward_run(ep_ctx *ctx, Inputs &in, const Backward &s, const Given &given, const Wanted &out) {
@@ -541,23 +1103,25 @@ int backward_run(ep_ctx *ctx, Inputs &in, const Backward &s, const Given &given,
     EP_CUDA(ctx, cudaGetLastError());
     in.kernels += 2;
     Operand x, w;
-    int rc = operands(ctx, in, s.x, s.w, &x, &w);
+    int rc = operands(ctx, in, s.copies, &x, &w);
     if (rc != EP_OK) return rc;
     Operand clean = x;   // x as dW reads it where a row that takes no part holds an infinity or a NaN
     if (out.dweight) {
         const bool direct = x.base == in.x;
         const Packed f = ep::packed_form(in.rows, in.n_in, in.type);
         const int grid = (int)std::min<int64_t>(ep::ceil_div(in.rows, 8), (int64_t)ctx->sm_count * 8);
-        entropy_clean<uint16_t><<<grid, 256, 0, in.stream>>>(direct ? (const uint16_t *)in.x : nullptr, in.ldx, in.rows, in.n_in, in.targets,
-                                                             given.lse, in.classes, s.scale, (uint16_t *)s.x, f.ld, f.parts, f.part_stride);
+        entropy_clean<uint16_t><<<grid, 256, 0, in.stream>>>(direct ? (const uint16_t *)in.x : nullptr, in.ldx, in.rows, in.n_in, s.rows,
+                                                             s.scale, (uint16_t *)s.copies.x, f.ld, f.parts, f.part_stride);
         EP_CUDA(ctx, cudaGetLastError());
         ++in.kernels;
-        if (direct) clean = Operand{s.x, in.type, in.rows, in.n_in, f.ld, 1, 0};
+        if (direct) clean = Operand{s.copies.x, in.type, in.rows, in.n_in, f.ld, 1, 0};
     }
     const Pieces &p = s.pieces;
     const bool f32 = in.type == EP_F32;
     const size_t size = ep::type_size(in.type);
     const float *factor = in.type == EP_F16 ? &s.scale->down : nullptr;
+    if (out.dbias && !f32)   // (not every piece has as many partial sums)
+        EP_CUDA(ctx, cudaMemsetAsync(s.part, 0, sizeof(float) * p.across * s.slabs * in.classes, in.stream));
     int64_t slab = 0;
     for (int64_t row0 = 0; row0 < in.rows; row0 += p.rows) {
         const int64_t rows = std::min(p.rows, in.rows - row0);
@@ -565,16 +1129,10 @@ int backward_run(ep_ctx *ctx, Inputs &in, const Backward &s, const Given &given,
         char *dx_rows = out.dx ? static_cast<char *>(out.dx) + row0 * in.n_in * size : nullptr;
         for (int class0 = 0; class0 < in.classes; class0 += p.classes) {
             const int classes = std::min(p.classes, in.classes - class0);
-            rc = logits_of(ctx, in, x, w, row0, rows, class0, classes, s.logits, s.share);
-            if (rc != EP_OK) return rc;
             const Packed f = ep::packed_form(rows, classes, in.type);
-            const dim3 grid((unsigned)ep::ceil_div(f.ld, G_CHUNKS * 8), (unsigned)s.slabs);
-            auto kernel = f32 ? entropy_slopes<float> : in.type == EP_BF16 ? entropy_slopes<__nv_bfloat16> : entropy_slopes<__half>;
-            kernel<<<grid, 256, 0, in.stream>>>(s.logits, f.ld, rows, classes, class0, in.bias, in.bias_type, in.targets + row0,
-                                                given.lse + row0, s.weights + row0, s.scale, out.dx || out.dweight ? s.g : nullptr,
-                                                f.part_stride, out.dbias ? s.part + slab * in.classes + class0 : nullptr, in.classes);
-            EP_CUDA(ctx, cudaGetLastError());
-            ++in.kernels;
+            rc = slopes_of(ctx, in, s, given, x, w, row0, rows, class0, classes, f, out.dx || out.dweight,
+                           out.dbias ? s.part + slab * in.classes + class0 : nullptr);
+            if (rc != EP_OK) return rc;
             const Operand g{s.g, f.type, rows, classes, f.ld, f.parts, f.part_stride};
             if (out.dx) {
                 const bool add = p.down > 1;
@@ -593,23 +1151,14 @@ int backward_run(ep_ctx *ctx, Inputs &in, const Backward &s, const Given &given,
             }
         }
         if (out.dx && p.down > 1 && !f32) {
-            if (in.type == EP_BF16)
-                launch_round<__nv_bfloat16>(s.dx, rows * in.n_in, s.scale, dx_rows, ctx->sm_count, in.stream);
-            else
-                launch_round<__half>(s.dx, rows * in.n_in, s.scale, dx_rows, ctx->sm_count, in.stream);
-            EP_CUDA(ctx, cudaGetLastError());
-            ++in.kernels;
+            rc = launch_round(ctx, in, s.dx, rows * in.n_in, s.scale, dx_rows);
+            if (rc != EP_OK) return rc;
         }
         slab += s.slabs;
     }
     if (out.dweight && p.across > 1 && !f32) {
-        const int64_t n = (int64_t)in.classes * in.n_in;
-        if (in.type == EP_BF16)
-            launch_round<__nv_bfloat16>(s.dweight, n, s.scale, out.dweight, ctx->sm_count, in.stream);
-        else
-            launch_round<__half>(s.dweight, n, s.scale, out.dweight, ctx->sm_count, in.stream);
-        EP_CUDA(ctx, cudaGetLastError());
-        ++in.kernels;
+        rc = launch_round(ctx, in, s.dweight, (int64_t)in.classes * in.n_in, s.scale, out.dweight);
+        if (rc != EP_OK) return rc;
     }
     if (out.dbias) {
         rc = ep::sum_partials(ctx, s.part, (int)slab, in.classes, out.dbias, in.stream);
