@@ -105,11 +105,12 @@ struct Scale {
     float up, down;
     int unclean;
 };
-struct RowInfo {   // of the backward
-    float shift;   // -lse / log 2
-    float g;
-    int target;    // -1: none
-    float cap;     // infinity; of rows that take no part, -infinity: the largest exponent
+// What the backward knows of each row, padded by a tile.  Rows that take no part, and those past the end: -infinity, 0, -1.
+struct RowInfo {
+    float *shift;   // -lse / log 2
+    float *g;
+    int *target;
+    __host__ __device__ RowInfo from(int64_t row) const { return RowInfo{shift + row, g + row, target + row}; }
 };
 struct TileWork {
     int64_t M;
@@ -121,7 +122,7 @@ struct TileWork {
     float2 *partial;          // forward: [number * 4 + piece][M], over log 2
     float *at_target;
     unsigned *ticket;
-    const RowInfo *rows;      // backward
+    RowInfo rows;             // backward
     const Scale *scale;
     float *sums;              // [number * 8 + block's and warp's rows][stride], or NULL
     int64_t stride;
@@ -164,7 +165,8 @@ __device__ __forceinline__ uint32_t packed(float lo, float hi) {
 
 template <bool GRAD, typename T>
 __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
-                                                                 const __grid_constant__ CUtensorMap map_g, const TileWork e, int *status) {
+                                                                 const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_clean,
+                                                                 const TileWork e, int *status) {
     using Mem = TileMemory<GRAD>;
     constexpr int STAGES = Mem::STAGES;
     extern __shared__ char smem_raw[];
@@ -211,13 +213,14 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
         uint32_t it = 0, s = 0, ph = 0;
         bool ok = true;
         const uint32_t ring_base = smem_u32(ring);
+        const CUtensorMap *const from_x = GRAD && e.scale->unclean ? &map_clean : &map_x;
         for (Stretch t(e.line, worker); ok && t.more(); t.next()) {
             const int m = row_tile(t) * TILE + (int)rank * BLOCK_ROWS, n = class_tile(t) * TILE + (int)rank * (columns(class_tile(t)) / 2);
             for (int kb = 0; kb < e.kb; ++kb, ++it) {
                 if (!(ok = mbar_wait_warp(&sh->empty[s], ph ^ 1u, abort_flag))) break;
                 if (rank == 0) mbar_expect_tx_elected(&sh->full[s], 2 * STAGE_BYTES);
                 const uint32_t bar = in_block(smem_u32(&sh->full[s]), 0), dst = ring_base + s * (uint32_t)STAGE_BYTES;
-                load_tile_elected<true>(dst, &map_x, kb * 64, m, 0, bar);
+                load_tile_elected<true>(dst, from_x, kb * 64, m, 0, bar);
                 load_tile_elected<true>(dst + BLOCK_ROWS * 128, &map_w, kb * 64, n, 0, bar);
                 if (++s == (uint32_t)STAGES) {
                     s = 0;
@@ -358,11 +361,14 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
                         bias[c] = Pair(b.x, b.y);
                     }
                 }
-                RowInfo info[4];
+                float shift[4], weight[4];
+                int target[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int64_t row = row0 + 8 * i + (lane >> 2);
-                    info[i] = row < e.M ? e.rows[row] : RowInfo{0.f, 0.f, -1, -INFINITY};
+                    shift[i] = e.rows.shift[row];
+                    weight[i] = e.rows.g[row] * up;
+                    target[i] = e.rows.target[row];
                 }
                 const uint32_t buf = acc & 1u;
                 if (!mbar_wait_warp(&sh->t_full[buf], (acc >> 1) & 1u, abort_flag)) break;
@@ -381,20 +387,16 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
 #pragma unroll
                             for (int r = 0; r < 2; ++r) {
                                 Pair v = fma2(Pair(__uint_as_float(a[4 * c + 2 * r]), __uint_as_float(a[4 * c + 2 * r + 1])), Pair(LOG2E),
-                                              Pair(info[2 * h + r].shift));
+                                              Pair(shift[2 * h + r]));
                                 if (e.bias) v = add2(v, bias[c]);
                                 v.get(f[4 * c + 2 * r], f[4 * c + 2 * r + 1]);
                             }
-                        if (__any_sync(FULL, info[2 * h].cap < 0.f || info[2 * h + 1].cap < 0.f)) {   // whatever such rows hold
-#pragma unroll
-                            for (int q = 0; q < 32; ++q) f[q] = fminf(f[q], info[2 * h + (q >> 1 & 1)].cap);
-                        }
 #pragma unroll
                         for (int q = 0; q < 32; ++q) f[q] = exp2_fast(f[q]);
 #pragma unroll
                         for (int r = 0; r < 2; ++r) {
-                            const int at = info[2 * h + r].target - e.class0 - col;
-                            const bool mine = (unsigned)at < 64u && ((at >> 1) & 3) == (lane & 3) && info[2 * h + r].target >= 0;
+                            const int at = target[2 * h + r] - e.class0 - col;
+                            const bool mine = target[2 * h + r] >= 0 && (unsigned)at < 64u && ((at >> 1) & 3) == (lane & 3);
                             const int index = mine ? (at >> 3) * 2 + (at & 1) : -1;
                             if (__any_sync(FULL, mine)) {
 #pragma unroll
@@ -406,7 +408,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
                         for (int c = 0; c < 8; ++c)
 #pragma unroll
                             for (int r = 0; r < 2; ++r) {
-                                const Pair g = mul2(Pair(f[4 * c + 2 * r], f[4 * c + 2 * r + 1]), Pair(info[2 * h + r].g * up));
+                                const Pair g = mul2(Pair(f[4 * c + 2 * r], f[4 * c + 2 * r + 1]), Pair(weight[2 * h + r]));
                                 if (e.sums) sums[c] = add2(sums[c], g);
                                 float lo, hi;
                                 g.get(lo, hi);
@@ -449,6 +451,419 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
     if (warp == 0) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * TILE) : "memory");
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- backward of narrow rows
+//
+// Rows of up to 256 elements leave room in the tensor memory for 128 rows of a gradient beside the logits, so G need not
+// leave the SM either.  One kernel serves both gradients, the roles of x and W exchanged: 128 rows P of one stay in
+// shared memory, tiles Q of BQ rows of the other go by;
+//     S = P Q^T;   G = slopes of S, in the operands' type, where S was;   acc += G Q
+// with S and acc in the tensor memory and G multiplied from there (a product whose first operand is in the tensor memory
+// reads half as much of the shared memory, which otherwise could not keep up).  P = rows of x gives dx, P = classes gives dW
+// and dbias; the logits are so made twice, four products in all where three would do, but G (two bytes for 4 n_in operations, written
+// once and read twice) is not moved.  Of 18 warps one loads, one multiplies, 16 make G, a thread a row of S and 32 columns.
+// Workers (SMs) share out the tiles as in entropy_tiles; who has only a part of a P tile leaves its sums for entropy_join.
+constexpr int FUSED_WIDTH = 256;   // the widest rows
+constexpr int P_ROWS = 128;
+struct FusedShared {
+    uint64_t full[8], empty[8], p_full[2], p_empty[2], s_full[4], g_full[4], done[4], acc_full, acc_empty, sums_full, drain;
+    uint32_t tmem_base;
+    int abort;
+    float sums[4][P_ROWS];
+};
+// BQ = 128: rows of up to 128 elements; 64: up to 256.
+template <bool DW, int BQ>
+struct FusedMemory {
+    static constexpr int BOXES = BQ == 128 ? 2 : 4;              // of 64 elements, of a row at most
+    static constexpr int P_BUFFERS = BQ == 128 ? 2 : 1;
+    static constexpr int P_BYTES = BOXES * P_ROWS * 128;
+    static constexpr int EXTRA = DW ? 3 * BQ * 4 : BQ * 4;       // what is known of Q's rows: shift, g, target; or the classes' bias
+    static constexpr int Q_BYTES = BOXES * BQ * 128, STAGE = Q_BYTES + 2048;
+    static constexpr int STAGES = BQ == 128 ? 4 : 4;
+    static constexpr int LOGITS = 3;                             // tiles of S in the tensor memory
+    static constexpr int ACC = LOGITS * BQ;                      // the columns before the sums
+    static constexpr size_t TOTAL = 1024 + P_BUFFERS * P_BYTES + STAGES * STAGE + sizeof(FusedShared);
+    static_assert(TOTAL <= 227 * 1024 && ACC + BOXES * 64 <= 512, "a block's shared and tensor memory");
+};
+struct FusedWork {
+    int64_t P, Q;             // rows of either
+    int width, boxes;         // of a row, and its boxes
+    Line line;
+    uint32_t idesc_s, idesc_acc;
+    const float *bias;        // of the classes, over log 2, padded; or NULL
+    RowInfo rows;
+    const Scale *scale;
+    void *out;                // or NULL
+    float *dbias;             // of DW, or NULL
+    bool vec;                 // out can be written by 16 bytes
+    float *share;             // [2 worker + segment][P_ROWS][share_ld]: sums of part of a P tile; then its dbias [..][P_ROWS]
+    float *share_bias;
+    int share_ld;
+};
+// Where a worker's part of P tile `tile` lies: its first segment's place, or its last one's.
+__host__ __device__ __forceinline__ int64_t share_of(const Line &l, int worker, int64_t tile) {
+    return 2 * worker + (l.begin(worker) / l.inner == tile ? 0 : 1);
+}
+
+__device__ __forceinline__ void bulk_load_elected(uint32_t dst, const void *src, uint32_t bytes, uint64_t *bar) {
+    asm volatile("{\n.reg .pred pe;\nelect.sync _|pe, 0xffffffff;\n"
+                 "@pe cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n}" ::"r"(dst), "l"(src),
+                 "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+// acc += G Q over 64 columns of G: four steps of 16, G in the tensor memory (two of 32 columns each, packed in 16 of theirs).
+__device__ __forceinline__ void umma_from_tmem_elected(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accumulate_first) {
+    const uint64_t b1 = b + (2048 >> 4), b2 = b1 + (2048 >> 4), b3 = b2 + (2048 >> 4);
+    asm volatile("{\n.reg .pred pe, pa, pt;\n"
+                 "elect.sync _|pe, 0xffffffff;\n"
+                 "setp.ne.b32 pa, %10, 0;\nsetp.eq.b32 pt, 0, 0;\n"
+                 "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %5, %9, pa;\n"
+                 "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [%2], %6, %9, pt;\n"
+                 "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [%3], %7, %9, pt;\n"
+                 "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [%4], %8, %9, pt;\n}" ::"r"(d_tmem),
+                 "r"(a_tmem), "r"(a_tmem + 8), "r"(a_tmem + 32), "r"(a_tmem + 40), "l"(b), "l"(b1), "l"(b2), "l"(b3), "r"(idesc),
+                 "r"(accumulate_first)
+                 : "memory");
+}
+
+template <bool DW, int BQ, typename T>
+__global__ void __launch_bounds__(TILE_THREADS, 1) entropy_fused(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q,
+                                                                 const __grid_constant__ CUtensorMap map_clean, const FusedWork e, int *status) {
+    using Mem = FusedMemory<DW, BQ>;
+    constexpr int STAGES = Mem::STAGES, LOGITS = Mem::LOGITS;
+    constexpr int COLUMN_WARPS = BQ / 32, GROUPS = 4 / COLUMN_WARPS;   // warps to a row of S; groups of warps that take tiles in turn
+    extern __shared__ char smem_raw[];
+    char *p_room = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    char *ring = p_room + Mem::P_BUFFERS * Mem::P_BYTES;               // [STAGES] of Q
+    char *extras = ring + STAGES * Mem::Q_BYTES;                       // [STAGES][2048]
+    FusedShared *sh = reinterpret_cast<FusedShared *>(extras + STAGES * 2048);
+    const int worker = blockIdx.x;
+    volatile int *abort_flag = &sh->abort;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(&sh->full[s], 1);
+            mbar_init(&sh->empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&sh->p_full[b], 1);
+            mbar_init(&sh->p_empty[b], 1);
+        }
+        for (int b = 0; b < LOGITS; ++b) {
+            mbar_init(&sh->s_full[b], 1);
+            mbar_init(&sh->g_full[b], 4 * COLUMN_WARPS);
+            mbar_init(&sh->done[b], 1);
+        }
+        mbar_init(&sh->acc_full, 1);
+        mbar_init(&sh->acc_empty, EPI_WARPS);
+        mbar_init(&sh->sums_full, EPI_WARPS);
+        mbar_init(&sh->drain, 1);
+        sh->abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem_base)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    ep_wait_for_launch_before();
+    ep_let_next_launch_start();
+    const uint32_t tmem_base = sh->tmem_base;
+
+    if (warp == EPI_WARPS) {
+        const bool unclean = e.scale->unclean;
+        const CUtensorMap *const from_p = !DW && unclean ? &map_clean : &map_p, *const from_q = DW && unclean ? &map_clean : &map_q;
+        uint32_t it = 0, s = 0, ph = 0, pb = 0, pph = 0, p_loads = 0;
+        bool ok = true;
+        for (Stretch t(e.line, worker); ok && t.more(); t.next(), ++it) {
+            if (it == 0 || t.inner == 0) {
+                if (!(ok = mbar_wait_warp(&sh->p_empty[pb], pph ^ 1u, abort_flag))) break;
+                mbar_expect_tx_elected(&sh->p_full[pb], e.boxes * P_ROWS * 128);
+                for (int b = 0; b < e.boxes; ++b)
+                    load_tile_elected<false>(smem_u32(p_room) + pb * Mem::P_BYTES + b * P_ROWS * 128, from_p, b * 64, t.outer * P_ROWS, 0,
+                                             smem_u32(&sh->p_full[pb]));
+                ++p_loads;
+                if (++pb == Mem::P_BUFFERS) {
+                    pb = 0;
+                    pph ^= 1u;
+                }
+            }
+            if (!(ok = mbar_wait_warp(&sh->empty[s], ph ^ 1u, abort_flag))) break;
+            const int q0 = t.inner * BQ;
+            const bool extra = DW || e.bias;
+            mbar_expect_tx_elected(&sh->full[s], e.boxes * BQ * 128 + (extra ? Mem::EXTRA : 0));
+            for (int b = 0; b < e.boxes; ++b)
+                load_tile_elected<false>(smem_u32(ring) + s * Mem::Q_BYTES + b * BQ * 128, from_q, b * 64, q0, 0, smem_u32(&sh->full[s]));
+            const uint32_t known = smem_u32(extras) + s * 2048;
+            if (DW) {
+                bulk_load_elected(known, e.rows.shift + q0, BQ * 4, &sh->full[s]);
+                bulk_load_elected(known + BQ * 4, e.rows.g + q0, BQ * 4, &sh->full[s]);
+                bulk_load_elected(known + 2 * BQ * 4, e.rows.target + q0, BQ * 4, &sh->full[s]);
+            } else if (extra)
+                bulk_load_elected(known, e.bias + q0, BQ * 4, &sh->full[s]);
+            if (++s == (uint32_t)STAGES) {
+                s = 0;
+                ph ^= 1u;
+            }
+        }
+        // after an abort the loads already issued get time to land before the block leaves
+        if (lane == 0 && (!ok || *abort_flag)) {
+#pragma unroll 1
+            for (uint32_t j = it > (uint32_t)STAGES ? it - (uint32_t)STAGES : 0u; j < it; ++j)
+                mbar_wait_quiet(&sh->full[j % (uint32_t)STAGES], (j / (uint32_t)STAGES) & 1u, DRAIN_LIMIT_CLOCKS);
+#pragma unroll 1
+            for (uint32_t j = p_loads > (uint32_t)Mem::P_BUFFERS ? p_loads - (uint32_t)Mem::P_BUFFERS : 0u; j < p_loads; ++j)
+                mbar_wait_quiet(&sh->p_full[j % (uint32_t)Mem::P_BUFFERS], (j / (uint32_t)Mem::P_BUFFERS) & 1u, DRAIN_LIMIT_CLOCKS);
+        }
+    } else if (warp == EPI_WARPS + 1) {
+        bool ok = true;
+        const uint32_t p_base = smem_u32(p_room), q_base = smem_u32(ring);
+        // S of one tile, LOGITS - 1 tiles ahead of the sums
+        Stretch ts(e.line, worker);
+        uint32_t js = 0, pb = 0, pph = 0;
+        auto logits = [&] {
+            if (!ts.more()) return;
+            if ((js == 0 || ts.inner == 0) && !(ok = mbar_wait_warp(&sh->p_full[pb], pph, abort_flag))) return;
+            const uint32_t s = js % STAGES, buf = js % LOGITS;
+            if (!(ok = mbar_wait_warp(&sh->full[s], (js / STAGES) & 1u, abort_flag))) return;
+            if (js >= (uint32_t)LOGITS && !(ok = mbar_wait_warp(&sh->done[buf], (js / LOGITS - 1) & 1u, abort_flag))) return;
+            tc_fence_after();
+            for (int b = 0; b < e.boxes; ++b)
+                umma_kblock_elected<HALF, false>(tmem_base + buf * BQ, operand_desc(p_base + pb * Mem::P_BYTES + b * P_ROWS * 128, false),
+                                                 operand_desc(q_base + s * Mem::Q_BYTES + b * BQ * 128, false), 2, 2, e.idesc_s, b > 0);
+            commit_elected<false>(&sh->s_full[buf]);
+            if (ts.left == 1 || ts.inner + 1 == ts.inners) {
+                commit_elected<false>(&sh->p_empty[pb]);
+                if (++pb == Mem::P_BUFFERS) {
+                    pb = 0;
+                    pph ^= 1u;
+                }
+            }
+            ts.next();
+            ++js;
+        };
+        for (int l = 0; ok && l < LOGITS - 1; ++l) logits();
+        uint32_t jp = 0, segment = 0;
+        for (Stretch t(e.line, worker); ok && t.more(); t.next(), ++jp) {
+            const uint32_t s = jp % STAGES, buf = jp % LOGITS;
+            const bool first = jp == 0 || t.inner == 0;
+            if (!(ok = mbar_wait_warp(&sh->g_full[buf], (jp / LOGITS) & 1u, abort_flag))) break;
+            if (first && !(ok = mbar_wait_warp(&sh->acc_empty, (segment & 1u) ^ 1u, abort_flag))) break;
+            tc_fence_after();
+            // (Q read along its rows: boxes of 64 elements lie BQ rows apart)
+            const uint64_t q = ((uint64_t)((q_base + s * Mem::Q_BYTES) & 0x3FFFFu) >> 4) | ((uint64_t)(BQ * 128 >> 4) << 16) |
+                               ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+#pragma unroll
+            for (int k = 0; k < BQ / 64; ++k)
+                umma_from_tmem_elected(tmem_base + Mem::ACC, tmem_base + buf * BQ + k * 64, q + k * (4 * 2048 >> 4), e.idesc_acc,
+                                       !first || k > 0);
+            commit_elected<false>(&sh->empty[s]);
+            commit_elected<false>(&sh->done[buf]);
+            if (t.left == 1 || t.inner + 1 == t.inners) {
+                commit_elected<false>(&sh->acc_full);
+                ++segment;
+            }
+            logits();
+        }
+        if (__any_sync(FULL, !ok || *abort_flag)) {
+            commit_elected<false>(&sh->drain);
+            if (lane == 0) mbar_wait_quiet(&sh->drain, 0u, DRAIN_LIMIT_CLOCKS);
+        }
+    } else {
+        const int quad = warp & 3, column = warp >> 2;   // TMEM lanes 32 quad.., and which of the warps that share them
+        const int piece = column % COLUMN_WARPS, group = column / COLUMN_WARPS;
+        const uint32_t lanes = tmem_base + ((uint32_t)(quad * 32) << 16);
+        const float up = e.scale->up, down = e.scale->down;
+        uint32_t j = 0, segment = 0;
+        int64_t p = 0;
+        int target = -1;                                       // of dx: what is known of this thread's row; of dW: its class's bias
+        float shift = 0.f, weight = 0.f, bias = 0.f, total = 0.f;
+        for (Stretch t(e.line, worker); t.more(); t.next(), ++j) {
+            if (j == 0 || t.inner == 0) {
+                p = (int64_t)t.outer * P_ROWS + quad * 32 + lane;
+                if constexpr (DW) {
+                    bias = e.bias ? e.bias[p] : 0.f;           // (padded)
+                    total = 0.f;
+                } else {
+                    shift = e.rows.shift[p];
+                    weight = e.rows.g[p] * up;
+                    target = e.rows.target[p];
+                }
+            }
+            if (GROUPS == 1 || j % GROUPS == (uint32_t)group) {
+                const uint32_t s = j % STAGES, buf = j % LOGITS;
+                if (!mbar_wait_warp(&sh->s_full[buf], (j / LOGITS) & 1u, abort_flag)) break;
+                if (!mbar_wait_warp(&sh->full[s], (j / STAGES) & 1u, abort_flag)) break;   // (long since: what came with Q is there to read)
+                tc_fence_after();
+                const float *known = reinterpret_cast<const float *>(extras + s * 2048) + piece * 32;
+                const int q0 = t.inner * BQ + piece * 32;
+                const uint32_t at = lanes + buf * BQ + piece * 32;
+                uint32_t a[32];
+                tmem_ld32_issue(at, a);
+                // where a row's class is among these, its probability less one
+                int mine = -1;
+                bool any;
+                if constexpr (DW) {
+                    const int class0 = (int)p - lane, theirs = reinterpret_cast<const int *>(known)[2 * BQ + lane] - class0;
+                    any = __any_sync(FULL, (unsigned)theirs < 32u);
+                } else {
+                    mine = target >= 0 ? target - q0 : -1;
+                    any = __any_sync(FULL, (unsigned)mine < 32u);
+                }
+                tmem_ld_wait(a);
+                uint32_t out[16];
+#pragma unroll
+                for (int c = 0; c < 32; c += 4) {
+                    float x[4];
+                    Pair v0(__uint_as_float(a[c]), __uint_as_float(a[c + 1])), v1(__uint_as_float(a[c + 2]), __uint_as_float(a[c + 3]));
+                    if constexpr (DW) {
+                        const float4 z = *reinterpret_cast<const float4 *>(known + c);
+                        v0 = fma2(v0, Pair(LOG2E), Pair(z.x, z.y));
+                        v1 = fma2(v1, Pair(LOG2E), Pair(z.z, z.w));
+                        if (e.bias) {
+                            v0 = add2(v0, Pair(bias));
+                            v1 = add2(v1, Pair(bias));
+                        }
+                    } else {
+                        v0 = fma2(v0, Pair(LOG2E), Pair(shift));
+                        v1 = fma2(v1, Pair(LOG2E), Pair(shift));
+                        if (e.bias) {
+                            const float4 b = *reinterpret_cast<const float4 *>(known + c);
+                            v0 = add2(v0, Pair(b.x, b.y));
+                            v1 = add2(v1, Pair(b.z, b.w));
+                        }
+                    }
+                    v0.get(x[0], x[1]);
+                    v1.get(x[2], x[3]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = exp2_fast(x[i]);
+                    if (any) {
+                        if constexpr (DW) {
+                            const int4 k = *reinterpret_cast<const int4 *>(known + 2 * BQ + c);
+                            x[0] -= k.x == (int)p ? 1.f : 0.f;
+                            x[1] -= k.y == (int)p ? 1.f : 0.f;
+                            x[2] -= k.z == (int)p ? 1.f : 0.f;
+                            x[3] -= k.w == (int)p ? 1.f : 0.f;
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) x[i] -= c + i == mine ? 1.f : 0.f;
+                        }
+                    }
+                    Pair g0, g1;
+                    if constexpr (DW) {
+                        const float4 w = *reinterpret_cast<const float4 *>(known + BQ + c);
+                        g0 = mul2(Pair(x[0], x[1]), Pair(w.x, w.y));
+                        g1 = mul2(Pair(x[2], x[3]), Pair(w.z, w.w));
+                        if (e.dbias) {
+                            float lo, hi;
+                            add2(g0, g1).get(lo, hi);
+                            total += lo + hi;
+                        }
+                        if constexpr (std::is_same_v<T, __half>) {
+                            g0 = mul2(g0, Pair(up));
+                            g1 = mul2(g1, Pair(up));
+                        }
+                    } else {
+                        g0 = mul2(Pair(x[0], x[1]), Pair(weight));
+                        g1 = mul2(Pair(x[2], x[3]), Pair(weight));
+                    }
+                    float lo, hi;
+                    g0.get(lo, hi);
+                    out[c / 2] = packed<T>(lo, hi);
+                    g1.get(lo, hi);
+                    out[c / 2 + 1] = packed<T>(lo, hi);
+                }
+                tmem_st16(at, out);   // (over columns that this warp alone has read)
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh->g_full[buf]);
+            }
+            if (t.left > 1 && t.inner + 1 < t.inners) continue;
+            // the end of a P tile, or of this worker's part of it
+            if (!mbar_wait_warp(&sh->acc_full, segment & 1u, abort_flag)) break;
+            ++segment;
+            tc_fence_after();
+            const bool whole = e.line.first_worker(t.outer) == e.line.last_worker(t.outer);
+            const int64_t place = share_of(e.line, worker, t.outer);
+#pragma unroll 1
+            for (int c0 = column * 32; c0 < e.width && e.out; c0 += 128) {
+                uint32_t a[32];
+                tmem_ld32_issue(lanes + Mem::ACC + c0, a);
+                tmem_ld_wait(a);
+                float v[32];
+#pragma unroll
+                for (int c = 0; c < 32; ++c) v[c] = __uint_as_float(a[c]);
+                if (!whole) {
+                    float *to = e.share + (place * P_ROWS + quad * 32 + lane) * e.share_ld + c0;
+#pragma unroll
+                    for (int c = 0; c < 32; c += 4) *reinterpret_cast<float4 *>(to + c) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+                } else if (p < e.P) {
+                    T *to = static_cast<T *>(e.out) + p * e.width;
+#pragma unroll
+                    for (int c = 0; c < 32; c += 8) {
+                        float w[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) w[i] = v[c + i] * down;
+                        store_chunk(to, c0 + c, e.width, e.vec, w);
+                    }
+                }
+            }
+            if constexpr (DW) {
+                if (e.dbias) {   // a class's sums are those of its row's four warps, in order
+                    sh->sums[column][quad * 32 + lane] = total;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sh->sums_full);
+                    if (column == 0) {   // (the others write there again only after these have given the sums of products back)
+                        if (!mbar_wait_warp(&sh->sums_full, (segment & 1u) ^ 1u, abort_flag)) break;
+                        const int c = quad * 32 + lane;
+                        const float sum = (sh->sums[0][c] + sh->sums[1][c]) + (sh->sums[2][c] + sh->sums[3][c]);
+                        if (!whole)
+                            e.share_bias[place * P_ROWS + c] = sum;
+                        else if (p < e.P)
+                            e.dbias[p] = sum;
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh->acc_empty);
+        }
+    }
+    __syncthreads();
+    if (sh->abort && threadIdx.x == 0) ep_raise(status, EP_ERR_TIMEOUT);
+    if (warp == 0) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
+    }
+}
+
+// The sums of P tiles that several workers had a part of, in the workers' order: 16 rows a block.
+template <typename T>
+__global__ void __launch_bounds__(256) entropy_join(const FusedWork e) {
+    const int64_t tile = blockIdx.x;
+    ep_wait_for_launch_before();
+    const int w0 = e.line.first_worker(tile), w1 = e.line.last_worker(tile);
+    if (w0 == w1) return;
+    const float down = e.scale->down;
+    const int row0 = blockIdx.y * 16;
+    for (int i = threadIdx.x; i < 16 * e.width && e.out; i += 256) {
+        const int row = row0 + i / e.width, c = i % e.width;
+        const int64_t p = tile * P_ROWS + row;
+        if (p >= e.P) break;
+        float sum = 0.f;
+        for (int w = w0; w <= w1; ++w) sum += e.share[(share_of(e.line, w, tile) * P_ROWS + row) * e.share_ld + c];
+        static_cast<T *>(e.out)[p * e.width + c] = from_f32<T>(sum * down);
+    }
+    if (e.dbias && threadIdx.x < 16 && tile * P_ROWS + row0 + threadIdx.x < e.P) {
+        float sum = 0.f;
+        for (int w = w0; w <= w1; ++w) sum += e.share_bias[share_of(e.line, w, tile) * P_ROWS + row0 + threadIdx.x];
+        e.dbias[tile * P_ROWS + row0 + threadIdx.x] = sum;
     }
 }
 
@@ -614,14 +1029,14 @@ __global__ void __launch_bounds__(256) entropy_finish(const Statistics stats, co
 }
 
 // ---------------------------------------------------------------------------------------------- backward
-// The rows' weights g (0 for rows that take no part), and each block's largest finite |g|.  A row that takes no part counts for
-// nothing, whatever x holds there; but 0 times an infinity or a NaN is NaN, so such rows of x are looked through: a block's
-// unclean is 1 where one holds any, and dW is then made of a copy of x with zeros there.
+// What is known of each row, and each block's largest finite |g|.  A row that takes no part counts for nothing, whatever x holds
+// there; but 0 times an infinity or a NaN is NaN, so such rows of x are looked through: a block's `unclean` is 1 where one
+// holds any (or numbers so large that a logit might overflow), and the products then read a copy of x with zeros there.
 template <typename T>
 __global__ void __launch_bounds__(256) entropy_weights(const float *__restrict__ lse, const int32_t *__restrict__ targets, int64_t rows,
                                                        int classes, const long long *__restrict__ counted,
                                                        const float *__restrict__ dloss, const float *__restrict__ drow,
-                                                       const T *__restrict__ x, int64_t ldx, int n_in, RowInfo *info, float *peaks,
+                                                       const void *__restrict__ x, int64_t ldx, int n_in, RowInfo info, float *peaks,
                                                        int *unclean, int *status) {
     __shared__ int bad_rows;
     __shared__ float tops[8];
@@ -637,14 +1052,20 @@ __global__ void __launch_bounds__(256) entropy_weights(const float *__restrict__
             dead = target_of(targets, row, classes, status) < 0 || lse[row] == -INFINITY;
             const float g = dead ? 0.f : (float)(mean + (drow ? (double)drow[row] : 0.0));
             const float z = lse[row];
-            info[row] = dead ? RowInfo{0.f, 0.f, -1, -INFINITY} : RowInfo{-z * LOG2E, z != z ? z : g, targets[row], INFINITY};
+            info.shift[row] = dead ? -INFINITY : -z * LOG2E;
+            info.g[row] = z != z ? z : g;
+            info.target[row] = dead ? -1 : targets[row];
             if (fabsf(g) < INFINITY) top = fmaxf(top, fabsf(g));
         }
-        if (!x) continue;
+        else if (row < (rows + TILE - 1) / TILE * TILE) {
+            info.shift[row] = -INFINITY;
+            info.g[row] = 0.f;
+            info.target[row] = -1;
+        }
         for (unsigned left = __ballot_sync(FULL, dead); left; left &= left - 1) {
-            const T *from = x + (row0 + (threadIdx.x & ~31) + __ffs(left) - 1) * ldx;
+            const T *from = static_cast<const T *>(x) + (row0 + (threadIdx.x & ~31) + __ffs(left) - 1) * ldx;
             bool bad = false;
-            for (int c = lane; c < n_in; c += 32) bad |= !(fabsf(to_f32(from[c])) < INFINITY);
+            for (int c = lane; c < n_in; c += 32) bad |= !(fabsf(to_f32(from[c])) < 1e18f);
             if (bad) bad_rows = 1;
         }
     }
@@ -683,11 +1104,11 @@ __global__ void __launch_bounds__(256) entropy_scale(const float *__restrict__ p
 // copy of x already, of `parts` matrices.
 template <typename E>
 __global__ void __launch_bounds__(256) entropy_clean(const E *__restrict__ from, int64_t ld, int64_t rows, int cols,
-                                                     const RowInfo *__restrict__ info, const Scale *scale, E *to, int ld_to, int parts, int64_t part_stride) {
+                                                     const RowInfo info, const Scale *scale, E *to, int ld_to, int parts, int64_t part_stride) {
     if (!scale->unclean) return;
     const int lane = threadIdx.x & 31;
     for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < rows; row += (int64_t)gridDim.x * 8) {
-        const bool dead = info[row].target < 0;
+        const bool dead = info.target[row] < 0;
         if (from)
             for (int c = lane; c < cols; c += 32) to[row * ld_to + c] = dead ? E{} : from[row * ld + c];
         else if (dead)
@@ -702,7 +1123,7 @@ constexpr int G_CHUNKS = 16, G_ROWS = 16;   // a block covers 128 classes, 16 ro
 template <typename T>
 __global__ void __launch_bounds__(256) entropy_slopes(const float *__restrict__ logits, int ld, int64_t rows, int classes, int class0,
                                                       const void *__restrict__ bias, int bias_type,
-                                                      const float *__restrict__ lse, const RowInfo *__restrict__ info,
+                                                      const float *__restrict__ lse, const RowInfo info,
                                                       const Scale *__restrict__ scale, void *to_raw, int64_t part_stride, float *part,
                                                       int64_t stride) {
     constexpr bool SPLIT = sizeof(T) == 4;
@@ -720,9 +1141,10 @@ __global__ void __launch_bounds__(256) entropy_slopes(const float *__restrict__ 
         for (int64_t row = (int64_t)blockIdx.y * G_ROWS + r0; row < rows; row += (int64_t)gridDim.y * G_ROWS) {
             float v[8];
             load_chunk(logits + row * ld, col, 1 << 30, true, 0.f, v);
-            const float g = info[row].g, z = lse[row];
-            const bool live = info[row].target >= 0;
-            const int mine = live ? info[row].target - class0 : -1;
+            const float g = info.g[row], z = lse[row];
+            const int target = info.target[row];
+            const bool live = target >= 0;
+            const int mine = live ? target - class0 : -1;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float p = exp_fast(v[i] + b[i] - z) - (col + i == mine ? 1.f : 0.f);
@@ -882,7 +1304,8 @@ int logits_of(ep_ctx *ctx, Inputs &in, const Operand &x, const Operand &w, int64
 }
 
 template <bool GRAD, typename T>
-int launch_tiles_of(ep_ctx *ctx, const CUtensorMap &x, const CUtensorMap &w, const CUtensorMap &g, const TileWork &e, cudaStream_t stream) {
+int launch_tiles_of(ep_ctx *ctx, const CUtensorMap &x, const CUtensorMap &w, const CUtensorMap &g, const CUtensorMap &clean,
+                    const TileWork &e, cudaStream_t stream) {
     auto kernel = entropy_tiles<GRAD, T>;
     constexpr size_t smem = TileMemory<GRAD>::TOTAL;
     EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
@@ -899,22 +1322,23 @@ int launch_tiles_of(ep_ctx *ctx, const CUtensorMap &x, const CUtensorMap &w, con
     attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
     cfg.attrs = attrs;
     cfg.numAttrs = 2;
-    EP_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, x, w, g, e, ctx->d_status));
+    EP_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, x, w, g, clean, e, ctx->d_status));
     return EP_OK;
 }
 // g: of the backward, [rows][ld].
 template <bool GRAD>
-int launch_tiles(ep_ctx *ctx, const Operand &x, const Operand &w, void *g, int64_t ld, TileWork &e, cudaStream_t stream, int *kernels) {
+int launch_tiles(ep_ctx *ctx, const Operand &x, const Operand &w, void *g, int64_t ld, const Operand &clean, TileWork &e,
+                 cudaStream_t stream, int *kernels) {
     const uint32_t fmt = x.type == EP_BF16 ? 1u : 0u;
     e.idesc = (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(TILE >> 4) << 24);
     e.kb = (int)ep::ceil_div(x.cols, 64);
-    CUtensorMap mx{}, mw{}, mg{};
+    CUtensorMap mx{}, mw{}, mg{}, mc{};
     if (!encode_operand(&mx, x, false, BLOCK_ROWS) || !encode_operand(&mw, w, false, BLOCK_ROWS) ||
-        (GRAD && !encode_result(&mg, g, x.type, 1, e.M, e.N, ld, TILE)))
+        (GRAD && !(encode_result(&mg, g, x.type, 1, e.M, e.N, ld, TILE) && encode_operand(&mc, clean, false, BLOCK_ROWS))))
         return ep::fail(ctx, EP_ERR_CUDA, "cuTensorMapEncodeTiled failed for %lld rows of %d classes", (long long)e.M, e.N);
     ++*kernels;
-    return x.type == EP_BF16 ? launch_tiles_of<GRAD, __nv_bfloat16>(ctx, mx, mw, mg, e, stream)
-                             : launch_tiles_of<GRAD, __half>(ctx, mx, mw, mg, e, stream);
+    return x.type == EP_BF16 ? launch_tiles_of<GRAD, __nv_bfloat16>(ctx, mx, mw, mg, mc, e, stream)
+                             : launch_tiles_of<GRAD, __half>(ctx, mx, mw, mg, mc, e, stream);
 }
 
 struct ForwardSpace {
@@ -962,7 +1386,7 @@ int forward_run(ep_ctx *ctx, Inputs &in, const ForwardSpace &s, float *loss, flo
         e.partial = s.stats;
         e.at_target = s.at_target;
         e.ticket = s.finish.ticket;
-        rc = launch_tiles<false>(ctx, x, w, nullptr, 0, e, in.stream, &in.kernels);
+        rc = launch_tiles<false>(ctx, x, w, nullptr, 0, x, e, in.stream, &in.kernels);
         if (rc != EP_OK) return rc;
     }
     const Pieces &p = s.pieces;
@@ -993,7 +1417,7 @@ struct Backward {
     Copies copies;
     void *g;
     float *logits, *share, *dx, *dweight, *part, *peaks;
-    RowInfo *rows;
+    RowInfo rows;
     int *unclean;
     Scale *scale;
     Pieces pieces;
@@ -1030,7 +1454,8 @@ Backward backward_space(const ep_ctx *ctx, int64_t rows, int n_in, int classes, 
                       });
         s.part = a.take<float>((size_t)p.across * s.slabs * classes);
     }
-    s.rows = a.take<RowInfo>(rows);
+    const int64_t all = ep::ceil_div(rows, TILE) * TILE;
+    s.rows = RowInfo{a.take<float>(all), a.take<float>(all), a.take<int>(all)};
     s.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(rows, 256), ctx->sm_count * 2));
     s.peaks = a.take<float>(s.blocks);
     s.unclean = a.take<int>(s.blocks);
@@ -1048,12 +1473,29 @@ struct Wanted {
     float *dbias;
 };
 
-template <typename T>
-void launch_weights(ep_ctx *ctx, const Inputs &in, const Backward &s, const Given &g, bool look) {
-    entropy_weights<T><<<s.blocks, 256, 0, in.stream>>>(g.lse, in.targets, in.rows, in.classes, g.counted, g.dloss, g.drow,
-                                                        look ? (const T *)in.x : nullptr, in.ldx, in.n_in, s.rows, s.peaks, s.unclean,
-                                                        ctx->d_status);
+// What is known of the rows, and the operands: x, x without what rows that take no part hold, and W.
+template <typename Space>
+int prepare(ep_ctx *ctx, Inputs &in, const Space &s, const Given &g, Operand *x, Operand *clean, Operand *w) {
+    auto weights = in.type == EP_F32 ? (void (*)(const float *, const int32_t *, int64_t, int, const long long *, const float *, const float *,
+                                                 const void *, int64_t, int, RowInfo, float *, int *, int *))entropy_weights<float>
+                   : in.type == EP_BF16 ? entropy_weights<__nv_bfloat16>
+                                        : entropy_weights<__half>;
+    weights<<<s.blocks, 256, 0, in.stream>>>(g.lse, in.targets, in.rows, in.classes, g.counted, g.dloss, g.drow, in.x, in.ldx, in.n_in, s.rows,
+                                             s.peaks, s.unclean, ctx->d_status);
     entropy_scale<<<1, 256, 0, in.stream>>>(s.peaks, s.unclean, s.blocks, in.type == EP_F16, s.scale);
+    EP_CUDA(ctx, cudaGetLastError());
+    in.kernels += 2;
+    const int rc = operands(ctx, in, s.copies, x, w);
+    if (rc != EP_OK) return rc;
+    const bool direct = x->base == in.x;
+    const Packed f = ep::packed_form(in.rows, in.n_in, in.type);
+    const int grid = (int)std::min<int64_t>(ep::ceil_div(in.rows, 8), (int64_t)ctx->sm_count * 8);
+    entropy_clean<<<grid, 256, 0, in.stream>>>(direct ? (const uint16_t *)in.x : nullptr, in.ldx, in.rows, in.n_in, s.rows, s.scale,
+                                               (uint16_t *)s.copies.x, f.ld, f.parts, f.part_stride);
+    EP_CUDA(ctx, cudaGetLastError());
+    ++in.kernels;
+    *clean = direct ? Operand{s.copies.x, in.type, in.rows, in.n_in, f.ld, 1, 0} : *x;
+    return EP_OK;
 }
 
 int launch_round(ep_ctx *ctx, Inputs &in, const float *sums, int64_t n, const Scale *scale, void *out) {
@@ -1068,13 +1510,13 @@ int launch_round(ep_ctx *ctx, Inputs &in, const float *sums, int64_t n, const Sc
 }
 
 // G of one piece, and its columns' partial sums.
-int slopes_of(ep_ctx *ctx, Inputs &in, const Backward &s, const Given &given, const Operand &x, const Operand &w, int64_t row0, int64_t rows,
+int slopes_of(ep_ctx *ctx, Inputs &in, const Backward &s, const Given &given, const Operand &x, const Operand &clean, const Operand &w, int64_t row0, int64_t rows,
               int class0, int classes, const Packed &f, bool wanted, float *part) {
     if (in.type == EP_F32) {
         const int rc = logits_of(ctx, in, x, w, row0, rows, class0, classes, s.logits, s.share);
         if (rc != EP_OK) return rc;
         entropy_slopes<float><<<dim3((unsigned)ep::ceil_div(f.ld, G_CHUNKS * 8), (unsigned)s.slabs), 256, 0, in.stream>>>(
-            s.logits, f.ld, rows, classes, class0, in.bias, in.bias_type, given.lse + row0, s.rows + row0, s.scale, wanted ? s.g : nullptr,
+            s.logits, f.ld, rows, classes, class0, in.bias, in.bias_type, given.lse + row0, s.rows.from(row0), s.scale, wanted ? s.g : nullptr,
             f.part_stride, part, in.classes);
         EP_CUDA(ctx, cudaGetLastError());
         ++in.kernels;
@@ -1086,36 +1528,17 @@ int slopes_of(ep_ctx *ctx, Inputs &in, const Backward &s, const Given &given, co
     e.class0 = class0;
     e.line = line_of(ctx, ep::ceil_div(classes, TILE), ep::ceil_div(rows, TILE));
     e.bias = in.bias ? s.copies.bias : nullptr;
-    e.rows = s.rows + row0;
+    e.rows = s.rows.from(row0);
     e.scale = s.scale;
     e.sums = part;
     e.stride = in.classes;
-    return launch_tiles<true>(ctx, rows_of(x, row0, rows), rows_of(w, class0, classes), s.g, f.ld, e, in.stream, &in.kernels);
+    return launch_tiles<true>(ctx, rows_of(x, row0, rows), rows_of(w, class0, classes), s.g, f.ld, rows_of(clean, row0, rows), e, in.stream, &in.kernels);
 }
 
 int backward_run(ep_ctx *ctx, Inputs &in, const Backward &s, const Given &given, const Wanted &out) {
-    if (in.type == EP_F32)
-        launch_weights<float>(ctx, in, s, given, out.dweight);
-    else if (in.type == EP_BF16)
-        launch_weights<__nv_bfloat16>(ctx, in, s, given, out.dweight);
-    else
-        launch_weights<__half>(ctx, in, s, given, out.dweight);
-    EP_CUDA(ctx, cudaGetLastError());
-    in.kernels += 2;
-    Operand x, w;
-    int rc = operands(ctx, in, s.copies, &x, &w);
+    Operand x, clean, w;
+    int rc = prepare(ctx, in, s, given, &x, &clean, &w);
     if (rc != EP_OK) return rc;
-    Operand clean = x;   // x as dW reads it where a row that takes no part holds an infinity or a NaN
-    if (out.dweight) {
-        const bool direct = x.base == in.x;
-        const Packed f = ep::packed_form(in.rows, in.n_in, in.type);
-        const int grid = (int)std::min<int64_t>(ep::ceil_div(in.rows, 8), (int64_t)ctx->sm_count * 8);
-        entropy_clean<uint16_t><<<grid, 256, 0, in.stream>>>(direct ? (const uint16_t *)in.x : nullptr, in.ldx, in.rows, in.n_in, s.rows,
-                                                             s.scale, (uint16_t *)s.copies.x, f.ld, f.parts, f.part_stride);
-        EP_CUDA(ctx, cudaGetLastError());
-        ++in.kernels;
-        if (direct) clean = Operand{s.copies.x, in.type, in.rows, in.n_in, f.ld, 1, 0};
-    }
     const Pieces &p = s.pieces;
     const bool f32 = in.type == EP_F32;
     const size_t size = ep::type_size(in.type);
@@ -1130,7 +1553,7 @@ int backward_run(ep_ctx *ctx, Inputs &in, const Backward &s, const Given &given,
         for (int class0 = 0; class0 < in.classes; class0 += p.classes) {
             const int classes = std::min(p.classes, in.classes - class0);
             const Packed f = ep::packed_form(rows, classes, in.type);
-            rc = slopes_of(ctx, in, s, given, x, w, row0, rows, class0, classes, f, out.dx || out.dweight,
+            rc = slopes_of(ctx, in, s, given, x, clean, w, row0, rows, class0, classes, f, out.dx || out.dweight,
                            out.dbias ? s.part + slab * in.classes + class0 : nullptr);
             if (rc != EP_OK) return rc;
             const Operand g{s.g, f.type, rows, classes, f.ld, f.parts, f.part_stride};
@@ -1166,6 +1589,94 @@ int backward_run(ep_ctx *ctx, Inputs &in, const Backward &s, const Given &given,
         ++in.kernels;
     }
     return EP_OK;
+}
+
+// ---- the backward of narrow rows
+bool narrow(int n_in, int type) { return type != EP_F32 && n_in <= FUSED_WIDTH; }
+int q_rows(int n_in) { return n_in <= 128 ? 128 : 64; }
+Line fused_line(const ep_ctx *ctx, int64_t p, int64_t q, int n_in) {
+    Line l;
+    l.inner = (int)ep::ceil_div(q, q_rows(n_in));
+    l.tiles = ep::ceil_div(p, P_ROWS) * l.inner;
+    l.workers = (int)std::min<int64_t>(l.tiles, ctx->sm_count);
+    return l;
+}
+int share_width(int n_in) { return (n_in + 31) & ~31; }
+
+struct NarrowSpace {
+    Copies copies;
+    RowInfo rows;
+    float *peaks, *share, *share_bias;
+    int *unclean;
+    Scale *scale;
+    int blocks;
+    size_t bytes;
+};
+NarrowSpace narrow_space(const ep_ctx *ctx, int64_t rows, int n_in, int classes, int type, bool aligned, void *base) {
+    ep::Arena a(base);
+    NarrowSpace s{};
+    s.copies = copies_space(a, rows, n_in, classes, type, aligned, true);
+    const int64_t all = ep::ceil_div(rows, TILE) * TILE;
+    s.rows = RowInfo{a.take<float>(all), a.take<float>(all), a.take<int>(all)};
+    s.share = a.take<float>((size_t)ctx->sm_count * 2 * P_ROWS * share_width(n_in));
+    s.share_bias = a.take<float>((size_t)ctx->sm_count * 2 * P_ROWS);
+    s.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(rows, 256), ctx->sm_count * 2));
+    s.peaks = a.take<float>(s.blocks);
+    s.unclean = a.take<int>(s.blocks);
+    s.scale = a.take<Scale>(1);
+    s.bytes = std::max<size_t>(a.used, 256);
+    return s;
+}
+
+template <bool DW, int BQ, typename T>
+int launch_fused_of(ep_ctx *ctx, const CUtensorMap &p, const CUtensorMap &q, const CUtensorMap &clean, const FusedWork &e, cudaStream_t stream) {
+    auto kernel = entropy_fused<DW, BQ, T>;
+    constexpr size_t smem = FusedMemory<DW, BQ>::TOTAL;
+    EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    EP_CUDA(ctx, ep::launch_early(kernel, dim3((unsigned)e.line.workers), dim3(TILE_THREADS), smem, stream, p, q, clean, e, ctx->d_status));
+    EP_CUDA(ctx, ep::launch_early(entropy_join<T>, dim3((unsigned)ep::ceil_div(e.P, P_ROWS), P_ROWS / 16), dim3(256), 0, stream, e));
+    return EP_OK;
+}
+// Gradient of x (P = x, Q = W) or of W (P = W, Q = x).
+template <bool DW>
+int launch_fused(ep_ctx *ctx, Inputs &in, const NarrowSpace &s, const Operand &x, const Operand &clean, const Operand &w, void *out,
+                 float *dbias) {
+    FusedWork e{};
+    e.P = DW ? in.classes : in.rows;
+    e.Q = DW ? in.rows : in.classes;
+    e.width = in.n_in;
+    e.boxes = (int)ep::ceil_div(in.n_in, 64);
+    e.line = fused_line(ctx, e.P, e.Q, in.n_in);
+    const int bq = q_rows(in.n_in), columns = (in.n_in + 15) & ~15;
+    const uint32_t fmt = in.type == EP_BF16 ? 1u : 0u, common = (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(P_ROWS >> 4) << 24);
+    e.idesc_s = common | ((uint32_t)(bq >> 3) << 17);
+    e.idesc_acc = common | (1u << 16) | ((uint32_t)(columns >> 3) << 17);
+    e.bias = in.bias ? s.copies.bias : nullptr;
+    e.rows = s.rows;
+    e.scale = s.scale;
+    e.out = out;
+    e.dbias = dbias;
+    e.vec = in.n_in % 8 == 0 && ep::aligned(out, 16);
+    e.share = s.share;
+    e.share_bias = s.share_bias;
+    e.share_ld = share_width(in.n_in);
+    CUtensorMap mp{}, mq{}, mc{};
+    if (!encode_operand(&mp, DW ? w : x, false, P_ROWS) || !encode_operand(&mq, DW ? x : w, false, bq) ||
+        !encode_operand(&mc, clean, false, DW ? bq : P_ROWS))
+        return ep::fail(ctx, EP_ERR_CUDA, "cuTensorMapEncodeTiled failed for %lld rows of %d classes", (long long)in.rows, in.classes);
+    in.kernels += 2;
+    if (in.type == EP_BF16)
+        return bq == 128 ? launch_fused_of<DW, 128, __nv_bfloat16>(ctx, mp, mq, mc, e, in.stream)
+                         : launch_fused_of<DW, 64, __nv_bfloat16>(ctx, mp, mq, mc, e, in.stream);
+    return bq == 128 ? launch_fused_of<DW, 128, __half>(ctx, mp, mq, mc, e, in.stream) : launch_fused_of<DW, 64, __half>(ctx, mp, mq, mc, e, in.stream);
+}
+
+int narrow_backward_run(ep_ctx *ctx, Inputs &in, const NarrowSpace &s, const Given &given, const Wanted &out) {
+    Operand x, clean, w;
+    int rc = prepare(ctx, in, s, given, &x, &clean, &w);
+    if (rc == EP_OK && out.dx) rc = launch_fused<false>(ctx, in, s, x, clean, w, out.dx, nullptr);
+    if (rc == EP_OK && (out.dweight || out.dbias)) rc = launch_fused<true>(ctx, in, s, x, clean, w, out.dweight, out.dbias);
+    return rc;
 }
 
 }  // namespace
@@ -1226,7 +1737,8 @@ int ep_cross_entropy(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int
 size_t ep_cross_entropy_backward_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t n_in, int32_t classes, int32_t in_type,
                                                  int32_t is_aligned) {
     if (!ctx || !entropy_shape_ok(rows, n_in, classes) || !float_type(in_type)) return 0;
-    return backward_space(ctx, rows, n_in, classes, in_type, is_aligned != 0, nullptr).bytes;
+    return narrow(n_in, in_type) ? narrow_space(ctx, rows, n_in, classes, in_type, is_aligned != 0, nullptr).bytes
+                                 : backward_space(ctx, rows, n_in, classes, in_type, is_aligned != 0, nullptr).bytes;
 }
 
 int ep_cross_entropy_backward(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int64_t ldw, int32_t in_type, const void *bias,
@@ -1248,11 +1760,15 @@ int ep_cross_entropy_backward(ep_ctx *ctx, const void *x, int64_t ldx, const voi
     }
     if (!dx && !dweight && !dbias) return EP_OK;
     in.aligned = can_be_read_by_tma(x, ldx, in_type) && can_be_read_by_tma(w, ldw, in_type);
-    const Backward s = backward_space(ctx, rows, n_in, classes, in_type, in.aligned, workspace);
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < s.bytes)
+    const bool small = narrow(n_in, in_type);
+    const Backward s = small ? Backward{} : backward_space(ctx, rows, n_in, classes, in_type, in.aligned, workspace);
+    const NarrowSpace n = small ? narrow_space(ctx, rows, n_in, classes, in_type, in.aligned, workspace) : NarrowSpace{};
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < std::max(s.bytes, n.bytes))
         return fail(ctx, EP_ERR_WORKSPACE, "workspace too small or misaligned");
+    const Given given{lse, dloss, drow_loss, reinterpret_cast<const long long *>(counted)};
+    const Wanted out{dx, dweight, dbias};
     Timed tm(ctx, in.stream, EP_TIMER_ENTROPY);
-    rc = backward_run(ctx, in, s, Given{lse, dloss, drow_loss, reinterpret_cast<const long long *>(counted)}, Wanted{dx, dweight, dbias});
+    rc = small ? narrow_backward_run(ctx, in, n, given, out) : backward_run(ctx, in, s, given, out);
     tm.end(in.kernels);
     return rc;
 }

@@ -107,7 +107,8 @@ def trained(rows, n_in, classes, dtype, seed, dead=0.0):
 
 
 SHAPES = [(1, 8, 2), (1, 64, 4096), (2, 65, 3), (7, 128, 1), (8, 1, 77), (33, 257, 129), (64, 128, 256), (128, 64, 32), (129, 100, 1000),
-          (300, 72, 5003), (1000, 128, 4096), (2999, 65, 257), (70, 48, 40000), (4097, 16, 33)]
+          (300, 72, 5003), (1000, 128, 4096), (2999, 65, 257), (70, 48, 40000), (4097, 16, 33), (500, 256, 700), (129, 272, 300),
+          (1000, 129, 5000), (257, 1024, 1000)]
 
 
 @pytest.mark.parametrize("rows,n_in,classes", SHAPES)
@@ -122,7 +123,8 @@ def test_shapes(rows, n_in, classes, dtype):
     backward(x, w, t, r, b, None, rand((rows,), F32, 7))
 
 
-@pytest.mark.parametrize("rows,n_in,classes", [(20000, 40, 2500), (2500, 40, 20000), (17000, 24, 17000)])
+@pytest.mark.parametrize("rows,n_in,classes", [(20000, 40, 2500), (2500, 40, 20000), (17000, 24, 17000), (20000, 264, 2500), (2500, 264, 20000),
+                                                  (40000, 200, 300), (300, 200, 40000)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_several_pieces(rows, n_in, classes, dtype):
     x, w, t = trained(rows, n_in, classes, dtype, 8, 0.1)
