@@ -107,7 +107,7 @@ struct Scale {
 };
 // What the backward knows of each row, padded by a tile.  Rows that take no part, and those past the end: -infinity, 0, -1.
 struct RowInfo {
-    float *shift;   // -lse / log 2
+    float *shift;   // -lse / log 2 + log2 |g|: the slope of a class that is not the target is 2^(l / log 2 + shift), or minus that
     float *g;
     int *target;
     __host__ __device__ RowInfo from(int64_t row) const { return RowInfo{shift + row, g + row, target + row}; }
@@ -132,6 +132,12 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
+}
+// One column of this warp's lanes.
+__device__ __forceinline__ float tmem_ld_column(uint32_t taddr) {
+    uint32_t v;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\ntcgen05.wait::ld.sync.aligned;" : "=r"(v) : "r"(taddr) : "memory");
+    return __uint_as_float(v);
 }
 // 16 lanes of 64 accumulator columns: lane l holds rows l / 4 and l / 4 + 8, of each 8 columns two from 2 (l % 4) on:
 // v[4 c + 2 r + i] is column 8 c + 2 (l % 4) + i of row l / 4 + 8 r.
@@ -163,7 +169,8 @@ __device__ __forceinline__ uint32_t packed(float lo, float hi) {
     }
 }
 
-template <bool GRAD, typename T>
+// (BIASED: of the forward alone)
+template <bool GRAD, bool BIASED, typename T>
 __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                                                                  const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_clean,
                                                                  const TileWork e, int *status) {
@@ -281,61 +288,72 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
                 if (!mbar_wait_warp(&sh->t_full[buf], (acc >> 1) & 1u, abort_flag)) break;
                 tc_fence_after();
                 if (col < e.N && row - lane < e.M) {
-                    uint32_t a[32], b[32];
-                    tmem_ld32_issue(from + buf * TILE, a);
-                    tmem_ld32_issue(from + buf * TILE + 32, b);
-                    tmem_ld_wait(a);
-                    tmem_ld_wait(b);
+                    const uint32_t at = from + buf * TILE;
+                    uint32_t a[64];
+                    tmem_ld32_issue(at, reinterpret_cast<uint32_t(&)[32]>(a[0]));
+                    tmem_ld32_issue(at + 32, reinterpret_cast<uint32_t(&)[32]>(a[32]));
+                    // The logits of targets among these columns: a column to each, read once more.
+                    const int mine = target >= 0 ? target - col : -1;
+                    unsigned hits = __ballot_sync(FULL, (unsigned)mine < 64u);
+                    const bool few = __popc(hits) <= 4;
+                    float found = 0.f;
+                    for (; few && hits; hits &= hits - 1) {
+                        const int who = __ffs(hits) - 1;
+                        const float v = tmem_ld_column(at + __shfl_sync(FULL, mine, who));
+                        if (lane == who) found = v;
+                    }
+                    tmem_ld_wait(reinterpret_cast<uint32_t(&)[32]>(a[0]));
+                    tmem_ld_wait(reinterpret_cast<uint32_t(&)[32]>(a[32]));
                     give_back(buf);
-                    Pair v[32];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) {
-                        v[j] = Pair(__uint_as_float(a[2 * j]), __uint_as_float(a[2 * j + 1]));
-                        v[16 + j] = Pair(__uint_as_float(b[2 * j]), __uint_as_float(b[2 * j + 1]));
-                    }
-                    const bool biased = e.bias != nullptr;
-                    if (biased) {
-#pragma unroll
-                        for (int j = 0; j < 32; j += 2) {
-                            const float4 add = *reinterpret_cast<const float4 *>(e.bias + col + 2 * j);
-                            v[j] = fma2(v[j], Pair(LOG2E), Pair(add.x, add.y));
-                            v[j + 1] = fma2(v[j + 1], Pair(LOG2E), Pair(add.z, add.w));
-                        }
-                    }
                     float f[64];
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j].get(f[2 * j], f[2 * j + 1]);
+                    for (int j = 0; j < 64; ++j) f[j] = __uint_as_float(a[j]);
+                    if (!few) {
+#pragma unroll
+                        for (int j = 0; j < 64; ++j) found = j == mine ? f[j] : found;
+                    }
+                    if ((unsigned)mine < 64u) e.at_target[row] = BIASED ? fmaf(found, LOG2E, e.bias[target]) : found * LOG2E;
+                    if (BIASED) {
+#pragma unroll
+                        for (int j = 0; j < 64; j += 4) {
+                            const float4 add = *reinterpret_cast<const float4 *>(e.bias + col + j);
+                            fma2(Pair(f[j], f[j + 1]), Pair(LOG2E), Pair(add.x, add.y)).get(f[j], f[j + 1]);
+                            fma2(Pair(f[j + 2], f[j + 3]), Pair(LOG2E), Pair(add.z, add.w)).get(f[j + 2], f[j + 3]);
+                        }
+                    }
                     if (col + PIECE_COLS > e.N) {
 #pragma unroll
                         for (int j = 0; j < 64; ++j) f[j] = col + j < e.N ? f[j] : -INFINITY;
                     }
-                    const int mine = target - col;
-                    if (__any_sync(FULL, (unsigned)mine < 64u)) {
-                        float at = 0.f;
+                    constexpr float scale = BIASED ? 1.f : LOG2E;
+                    auto sum_below = [&](float shift) {   // of 2^(f - shift)
+                        Pair s0(0.f), s1(0.f);
 #pragma unroll
-                        for (int j = 0; j < 64; ++j) at = j == mine ? f[j] : at;
-                        if ((unsigned)mine < 64u) e.at_target[row] = biased ? at : at * LOG2E;
-                    }
+                        for (int j = 0; j < 64; j += 4) {
+                            float x0, x1, x2, x3;
+                            fma2(Pair(f[j], f[j + 1]), Pair(scale), Pair(-shift)).get(x0, x1);
+                            fma2(Pair(f[j + 2], f[j + 3]), Pair(scale), Pair(-shift)).get(x2, x3);
+                            s0 = add2(s0, Pair(exp2_fast(x0), exp2_fast(x1)));
+                            s1 = add2(s1, Pair(exp2_fast(x2), exp2_fast(x3)));
+                        }
+                        float lo, hi;
+                        add2(s0, s1).get(lo, hi);
+                        return lo + hi;
+                    };
+                    // What is taken out of the exponents need not be the maximum, only near it: the largest so far does unless this
+                    // tile goes above it by 2^64, and its exponentials need not wait for the maximum to be known.
+                    float more = sum_below(top);
                     float high = f[0];
 #pragma unroll
                     for (int j = 1; j + 1 < 64; j += 2) high = max3(high, f[j], f[j + 1]);
-                    high = fmaxf(high, f[63]);
-                    const float scale = biased ? 1.f : LOG2E;
-                    const float now = fmaxf(top, high * scale);
-                    sum *= exp2_fast(top - now);
-                    top = now;
-                    Pair s0(0.f), s1(0.f);
-#pragma unroll
-                    for (int j = 0; j < 64; j += 4) {
-                        float x0, x1, x2, x3;
-                        fma2(Pair(f[j], f[j + 1]), Pair(scale), Pair(-now)).get(x0, x1);
-                        fma2(Pair(f[j + 2], f[j + 3]), Pair(scale), Pair(-now)).get(x2, x3);
-                        s0 = add2(s0, Pair(exp2_fast(x0), exp2_fast(x1)));
-                        s1 = add2(s1, Pair(exp2_fast(x2), exp2_fast(x3)));
+                    high = fmaxf(high, f[63]) * scale;
+                    if (__any_sync(FULL, high > top + 64.f)) {
+                        const float now = fmaxf(top, high);
+                        sum *= exp2_fast(top - now);
+                        top = now;
+                        more = sum_below(top);
                     }
-                    float lo, hi;
-                    add2(s0, s1).get(lo, hi);
-                    sum += lo + hi;
+                    sum += more;
                 } else
                     give_back(buf);
                 if (t.left == 1 || t.inner + 1 == t.inners) {
@@ -361,13 +379,14 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
                         bias[c] = Pair(b.x, b.y);
                     }
                 }
-                float shift[4], weight[4];
+                float shift[4], weight[4], sign[4];
                 int target[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int64_t row = row0 + 8 * i + (lane >> 2);
                     shift[i] = e.rows.shift[row];
-                    weight[i] = e.rows.g[row] * up;
+                    weight[i] = fabsf(e.rows.g[row]);
+                    sign[i] = e.rows.g[row] < 0.f ? -up : up;
                     target[i] = e.rows.target[row];
                 }
                 const uint32_t buf = acc & 1u;
@@ -400,7 +419,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
                             const int index = mine ? (at >> 3) * 2 + (at & 1) : -1;
                             if (__any_sync(FULL, mine)) {
 #pragma unroll
-                                for (int q = 0; q < 16; ++q) f[4 * (q >> 1) + 2 * r + (q & 1)] -= q == index ? 1.f : 0.f;
+                                for (int q = 0; q < 16; ++q) f[4 * (q >> 1) + 2 * r + (q & 1)] -= q == index ? weight[2 * h + r] : 0.f;
                             }
                         }
                         uint32_t out[16];
@@ -408,7 +427,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
                         for (int c = 0; c < 8; ++c)
 #pragma unroll
                             for (int r = 0; r < 2; ++r) {
-                                const Pair g = mul2(Pair(f[4 * c + 2 * r], f[4 * c + 2 * r + 1]), Pair(weight[2 * h + r]));
+                                const Pair g = mul2(Pair(f[4 * c + 2 * r], f[4 * c + 2 * r + 1]), Pair(sign[2 * h + r]));
                                 if (e.sums) sums[c] = add2(sums[c], g);
                                 float lo, hi;
                                 g.get(lo, hi);
@@ -459,16 +478,17 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
 // Rows of up to 256 elements leave room in the tensor memory for 128 rows of a gradient beside the logits, so G need not
 // leave the SM either.  One kernel serves both gradients, the roles of x and W exchanged: 128 rows P of one stay in
 // shared memory, tiles Q of BQ rows of the other go by;
-//     S = P Q^T;   G = slopes of S, in the operands' type, where S was;   acc += G Q
-// with S and acc in the tensor memory and G multiplied from there (a product whose first operand is in the tensor memory
+//     S = P Q^T;   G = slopes of S, in the operands' type;   acc += G Q
+// with all three in the tensor memory and G multiplied from there (a product whose first operand is in the tensor memory
 // reads half as much of the shared memory, which otherwise could not keep up).  P = rows of x gives dx, P = classes gives dW
 // and dbias; the logits are so made twice, four products in all where three would do, but G (two bytes for 4 n_in operations, written
-// once and read twice) is not moved.  Of 18 warps one loads, one multiplies, 16 make G, a thread a row of S and 32 columns.
+// once and read twice) is not moved.  Of 19 warps one loads, one makes S, one adds up, 16 make G: groups of
+// them take tiles in turn, a thread a row of S and 64 columns.
 // Workers (SMs) share out the tiles as in entropy_tiles; who has only a part of a P tile leaves its sums for entropy_join.
 constexpr int FUSED_WIDTH = 256;   // the widest rows
-constexpr int P_ROWS = 128;
+constexpr int P_ROWS = 128, FUSED_THREADS = 32 * (EPI_WARPS + 3);
 struct FusedShared {
-    uint64_t full[8], empty[8], p_full[2], p_empty[2], s_full[4], g_full[4], done[4], acc_full, acc_empty, sums_full, drain;
+    uint64_t full[8], empty[8], p_full[2], p_empty[2], s_full[4], s_empty[4], g_full[4], g_empty[4], acc_full, acc_empty, sums_full, drain[2];
     uint32_t tmem_base;
     int abort;
     float sums[4][P_ROWS];
@@ -482,8 +502,9 @@ struct FusedMemory {
     static constexpr int EXTRA = DW ? 3 * BQ * 4 : BQ * 4;       // what is known of Q's rows: shift, g, target; or the classes' bias
     static constexpr int Q_BYTES = BOXES * BQ * 128, STAGE = Q_BYTES + 2048;
     static constexpr int STAGES = BQ == 128 ? 4 : 4;
-    static constexpr int LOGITS = 3;                             // tiles of S in the tensor memory
-    static constexpr int ACC = LOGITS * BQ;                      // the columns before the sums
+    // The tensor memory: two tiles of S, a few of G (two of its numbers to a column), the sums.
+    static constexpr int LOGITS = 2, SLOPES = BQ == 128 ? 2 : 4;
+    static constexpr int G_AT = LOGITS * BQ, ACC = G_AT + SLOPES * BQ / 2;
     static constexpr size_t TOTAL = 1024 + P_BUFFERS * P_BYTES + STAGES * STAGE + sizeof(FusedShared);
     static_assert(TOTAL <= 227 * 1024 && ACC + BOXES * 64 <= 512, "a block's shared and tensor memory");
 };
@@ -513,7 +534,7 @@ __device__ __forceinline__ void bulk_load_elected(uint32_t dst, const void *src,
                  "r"(bytes), "r"(smem_u32(bar))
                  : "memory");
 }
-// acc += G Q over 64 columns of G: four steps of 16, G in the tensor memory (two of 32 columns each, packed in 16 of theirs).
+// acc += G Q over 64 columns of G: four steps of 16, G in the tensor memory, two of its numbers to a column.
 __device__ __forceinline__ void umma_from_tmem_elected(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accumulate_first) {
     const uint64_t b1 = b + (2048 >> 4), b2 = b1 + (2048 >> 4), b3 = b2 + (2048 >> 4);
     asm volatile("{\n.reg .pred pe, pa, pt;\n"
@@ -523,17 +544,20 @@ __device__ __forceinline__ void umma_from_tmem_elected(uint32_t d_tmem, uint32_t
                  "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [%2], %6, %9, pt;\n"
                  "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [%3], %7, %9, pt;\n"
                  "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [%4], %8, %9, pt;\n}" ::"r"(d_tmem),
-                 "r"(a_tmem), "r"(a_tmem + 8), "r"(a_tmem + 32), "r"(a_tmem + 40), "l"(b), "l"(b1), "l"(b2), "l"(b3), "r"(idesc),
+                 "r"(a_tmem), "r"(a_tmem + 8), "r"(a_tmem + 16), "r"(a_tmem + 24), "l"(b), "l"(b1), "l"(b2), "l"(b3), "r"(idesc),
                  "r"(accumulate_first)
                  : "memory");
 }
 
-template <bool DW, int BQ, typename T>
-__global__ void __launch_bounds__(TILE_THREADS, 1) entropy_fused(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q,
+template <bool DW, bool BIASED, int BQ, typename T>
+__global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q,
                                                                  const __grid_constant__ CUtensorMap map_clean, const FusedWork e, int *status) {
     using Mem = FusedMemory<DW, BQ>;
-    constexpr int STAGES = Mem::STAGES, LOGITS = Mem::LOGITS;
-    constexpr int COLUMN_WARPS = BQ / 32, GROUPS = 4 / COLUMN_WARPS;   // warps to a row of S; groups of warps that take tiles in turn
+    constexpr int STAGES = Mem::STAGES, LOGITS = Mem::LOGITS, SLOPES = Mem::SLOPES;
+    // Warps to a row of S; groups of warps that take tiles in turn.  What a group waits for has barriers of its own (a barrier that
+    // went on by two phases meanwhile could not be told from one that has not moved).
+    constexpr int COLUMN_WARPS = BQ / 64, GROUPS = 4 / COLUMN_WARPS;
+    static_assert(STAGES % GROUPS == 0 && SLOPES % GROUPS == 0 && GROUPS <= 4, "a group's stages and slopes are its own");
     extern __shared__ char smem_raw[];
     char *p_room = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     char *ring = p_room + Mem::P_BUFFERS * Mem::P_BYTES;               // [STAGES] of Q
@@ -552,15 +576,19 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_fused(const __grid_co
             mbar_init(&sh->p_full[b], 1);
             mbar_init(&sh->p_empty[b], 1);
         }
-        for (int b = 0; b < LOGITS; ++b) {
+        for (int b = 0; b < GROUPS; ++b) {
             mbar_init(&sh->s_full[b], 1);
+            mbar_init(&sh->s_empty[b], 4 * COLUMN_WARPS);
+        }
+        for (int b = 0; b < SLOPES; ++b) {
             mbar_init(&sh->g_full[b], 4 * COLUMN_WARPS);
-            mbar_init(&sh->done[b], 1);
+            mbar_init(&sh->g_empty[b], 1);
         }
         mbar_init(&sh->acc_full, 1);
         mbar_init(&sh->acc_empty, EPI_WARPS);
         mbar_init(&sh->sums_full, EPI_WARPS);
-        mbar_init(&sh->drain, 1);
+        mbar_init(&sh->drain[0], 1);
+        mbar_init(&sh->drain[1], 1);
         sh->abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -573,7 +601,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_fused(const __grid_co
     tc_fence_after();
     ep_wait_for_launch_before();
     ep_let_next_launch_start();
-    const uint32_t tmem_base = sh->tmem_base;
+    constexpr uint32_t tmem_base = 0;   // of an allocation of all 512 columns (known as such, addresses need no registers of a lane)
 
     if (warp == EPI_WARPS) {
         const bool unclean = e.scale->unclean;
@@ -595,7 +623,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_fused(const __grid_co
             }
             if (!(ok = mbar_wait_warp(&sh->empty[s], ph ^ 1u, abort_flag))) break;
             const int q0 = t.inner * BQ;
-            const bool extra = DW || e.bias;
+            constexpr bool extra = DW || BIASED;
             mbar_expect_tx_elected(&sh->full[s], e.boxes * BQ * 128 + (extra ? Mem::EXTRA : 0));
             for (int b = 0; b < e.boxes; ++b)
                 load_tile_elected<false>(smem_u32(ring) + s * Mem::Q_BYTES + b * BQ * 128, from_q, b * 64, q0, 0, smem_u32(&sh->full[s]));
@@ -623,36 +651,44 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_fused(const __grid_co
     } else if (warp == EPI_WARPS + 1) {
         bool ok = true;
         const uint32_t p_base = smem_u32(p_room), q_base = smem_u32(ring);
-        // S of one tile, LOGITS - 1 tiles ahead of the sums
-        Stretch ts(e.line, worker);
-        uint32_t js = 0, pb = 0, pph = 0;
-        auto logits = [&] {
-            if (!ts.more()) return;
-            if ((js == 0 || ts.inner == 0) && !(ok = mbar_wait_warp(&sh->p_full[pb], pph, abort_flag))) return;
-            const uint32_t s = js % STAGES, buf = js % LOGITS;
-            if (!(ok = mbar_wait_warp(&sh->full[s], (js / STAGES) & 1u, abort_flag))) return;
-            if (js >= (uint32_t)LOGITS && !(ok = mbar_wait_warp(&sh->done[buf], (js / LOGITS - 1) & 1u, abort_flag))) return;
+        uint32_t j = 0, s = 0, ph = 0, buf = 0, pb = 0, pph = 0;
+        for (Stretch t(e.line, worker); t.more(); t.next(), ++j) {
+            if ((j == 0 || t.inner == 0) && !(ok = mbar_wait_warp(&sh->p_full[pb], pph, abort_flag))) break;
+            if (!(ok = mbar_wait_warp(&sh->full[s], ph, abort_flag))) break;
+            if (j >= (uint32_t)LOGITS) {
+                const uint32_t before = j - LOGITS;
+                if (!(ok = mbar_wait_warp(&sh->s_empty[before % GROUPS], (before / GROUPS) & 1u, abort_flag))) break;
+            }
             tc_fence_after();
-            for (int b = 0; b < e.boxes; ++b)
-                umma_kblock_elected<HALF, false>(tmem_base + buf * BQ, operand_desc(p_base + pb * Mem::P_BYTES + b * P_ROWS * 128, false),
+#pragma unroll
+            for (int b = 0; b < Mem::BOXES; ++b)
+                if (b < e.boxes) umma_kblock_elected<HALF, false>(tmem_base + buf * BQ, operand_desc(p_base + pb * Mem::P_BYTES + b * P_ROWS * 128, false),
                                                  operand_desc(q_base + s * Mem::Q_BYTES + b * BQ * 128, false), 2, 2, e.idesc_s, b > 0);
-            commit_elected<false>(&sh->s_full[buf]);
-            if (ts.left == 1 || ts.inner + 1 == ts.inners) {
+            commit_elected<false>(&sh->s_full[j % GROUPS]);
+            if (t.left == 1 || t.inner + 1 == t.inners) {
                 commit_elected<false>(&sh->p_empty[pb]);
                 if (++pb == Mem::P_BUFFERS) {
                     pb = 0;
                     pph ^= 1u;
                 }
             }
-            ts.next();
-            ++js;
-        };
-        for (int l = 0; ok && l < LOGITS - 1; ++l) logits();
-        uint32_t jp = 0, segment = 0;
-        for (Stretch t(e.line, worker); ok && t.more(); t.next(), ++jp) {
-            const uint32_t s = jp % STAGES, buf = jp % LOGITS;
-            const bool first = jp == 0 || t.inner == 0;
-            if (!(ok = mbar_wait_warp(&sh->g_full[buf], (jp / LOGITS) & 1u, abort_flag))) break;
+            if (++s == (uint32_t)STAGES) {
+                s = 0;
+                ph ^= 1u;
+            }
+            if (++buf == (uint32_t)LOGITS) buf = 0;
+        }
+        if (__any_sync(FULL, !ok || *abort_flag)) {
+            commit_elected<false>(&sh->drain[0]);
+            if (lane == 0) mbar_wait_quiet(&sh->drain[0], 0u, DRAIN_LIMIT_CLOCKS);
+        }
+    } else if (warp == EPI_WARPS + 2) {
+        bool ok = true;
+        const uint32_t q_base = smem_u32(ring);
+        uint32_t j = 0, s = 0, buf = 0, lap = 0, segment = 0;
+        for (Stretch t(e.line, worker); t.more(); t.next(), ++j) {
+            const bool first = j == 0 || t.inner == 0;
+            if (!(ok = mbar_wait_warp(&sh->g_full[buf], lap, abort_flag))) break;
             if (first && !(ok = mbar_wait_warp(&sh->acc_empty, (segment & 1u) ^ 1u, abort_flag))) break;
             tc_fence_after();
             // (Q read along its rows: boxes of 64 elements lie BQ rows apart)
@@ -660,19 +696,23 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_fused(const __grid_co
                                ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 #pragma unroll
             for (int k = 0; k < BQ / 64; ++k)
-                umma_from_tmem_elected(tmem_base + Mem::ACC, tmem_base + buf * BQ + k * 64, q + k * (4 * 2048 >> 4), e.idesc_acc,
+                umma_from_tmem_elected(tmem_base + Mem::ACC, tmem_base + Mem::G_AT + buf * (BQ / 2) + k * 32, q + k * (4 * 2048 >> 4), e.idesc_acc,
                                        !first || k > 0);
             commit_elected<false>(&sh->empty[s]);
-            commit_elected<false>(&sh->done[buf]);
+            commit_elected<false>(&sh->g_empty[buf]);
             if (t.left == 1 || t.inner + 1 == t.inners) {
                 commit_elected<false>(&sh->acc_full);
                 ++segment;
             }
-            logits();
+            if (++s == (uint32_t)STAGES) s = 0;
+            if (++buf == (uint32_t)SLOPES) {
+                buf = 0;
+                lap ^= 1u;
+            }
         }
         if (__any_sync(FULL, !ok || *abort_flag)) {
-            commit_elected<false>(&sh->drain);
-            if (lane == 0) mbar_wait_quiet(&sh->drain, 0u, DRAIN_LIMIT_CLOCKS);
+            commit_elected<false>(&sh->drain[1]);
+            if (lane == 0) mbar_wait_quiet(&sh->drain[1], 0u, DRAIN_LIMIT_CLOCKS);
         }
     } else {
         const int quad = warp & 3, column = warp >> 2;   // TMEM lanes 32 quad.., and which of the warps that share them
@@ -681,108 +721,116 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_fused(const __grid_co
         const float up = e.scale->up, down = e.scale->down;
         uint32_t j = 0, segment = 0;
         int64_t p = 0;
-        int target = -1;                                       // of dx: what is known of this thread's row; of dW: its class's bias
-        float shift = 0.f, weight = 0.f, bias = 0.f, total = 0.f;
+        // of dx: what is known of this thread's row; of dW: its class's bias, and the scale of fp16
+        int target = -1;
+        float shift = 0.f, weight = 0.f, bias = 0.f;
+        bool negative = false;                                 // some row's g is
+        const float log_up = std::is_same_v<T, __half> ? log2f(up) : 0.f;
+        Pair total(0.f);
         for (Stretch t(e.line, worker); t.more(); t.next(), ++j) {
             if (j == 0 || t.inner == 0) {
                 p = (int64_t)t.outer * P_ROWS + quad * 32 + lane;
                 if constexpr (DW) {
-                    bias = e.bias ? e.bias[p] : 0.f;           // (padded)
-                    total = 0.f;
+                    if (BIASED) bias = (e.bias ? e.bias[p] : 0.f) + log_up;   // (padded)
+                    total = Pair(0.f);
                 } else {
-                    shift = e.rows.shift[p];
+                    shift = e.rows.shift[p] + log_up;
                     weight = e.rows.g[p] * up;
                     target = e.rows.target[p];
+                    negative = __any_sync(FULL, weight < 0.f);
                 }
             }
-            if (GROUPS == 1 || j % GROUPS == (uint32_t)group) {
-                const uint32_t s = j % STAGES, buf = j % LOGITS;
-                if (!mbar_wait_warp(&sh->s_full[buf], (j / LOGITS) & 1u, abort_flag)) break;
-                if (!mbar_wait_warp(&sh->full[s], (j / STAGES) & 1u, abort_flag)) break;   // (long since: what came with Q is there to read)
+            if (j % GROUPS == (uint32_t)group) {
+                const uint32_t s = j % STAGES, buf = j % LOGITS, gbuf = j % SLOPES;
+                if (!mbar_wait_warp(&sh->s_full[group], (j / GROUPS) & 1u, abort_flag)) break;
+                // (long since: what came with Q is there to read)
+                if ((DW || BIASED) && !mbar_wait_warp(&sh->full[s], (j / STAGES) & 1u, abort_flag)) break;
                 tc_fence_after();
-                const float *known = reinterpret_cast<const float *>(extras + s * 2048) + piece * 32;
-                const int q0 = t.inner * BQ + piece * 32;
-                const uint32_t at = lanes + buf * BQ + piece * 32;
-                uint32_t a[32];
-                tmem_ld32_issue(at, a);
-                // where a row's class is among these, its probability less one
+                const float *known = reinterpret_cast<const float *>(extras + s * 2048) + piece * 64;
+                const uint32_t at = lanes + buf * BQ + piece * 64, to = lanes + Mem::G_AT + gbuf * (BQ / 2) + piece * 32;
+                uint32_t a[2][32];
+                tmem_ld32_issue(at, a[0]);
+                tmem_ld32_issue(at + 32, a[1]);
+                // Where a row's class is among these columns, its slope is its share less all of g; and slopes may be negative.
+                // Both are rare and out of the way of what is not.
                 int mine = -1;
-                bool any;
+                bool special[2];
                 if constexpr (DW) {
-                    const int class0 = (int)p - lane, theirs = reinterpret_cast<const int *>(known)[2 * BQ + lane] - class0;
-                    any = __any_sync(FULL, (unsigned)theirs < 32u);
+                    const int class0 = (int)p - lane;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        special[h] = __any_sync(FULL, (unsigned)(reinterpret_cast<const int *>(known)[2 * BQ + 32 * h + lane] - class0) < 32u ||
+                                                          known[BQ + 32 * h + lane] < 0.f);
                 } else {
-                    mine = target >= 0 ? target - q0 : -1;
-                    any = __any_sync(FULL, (unsigned)mine < 32u);
+                    mine = target >= 0 ? target - t.inner * BQ - piece * 64 : -1;
+                    special[0] = negative || __any_sync(FULL, (unsigned)mine < 32u);
+                    special[1] = negative || __any_sync(FULL, (unsigned)(mine - 32) < 32u);
                 }
-                tmem_ld_wait(a);
-                uint32_t out[16];
+                tmem_ld_wait(a[0]);
+                tmem_ld_wait(a[1]);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sh->s_empty[group]);
+                // (what was there has long been multiplied)
+                if (!mbar_wait_warp(&sh->g_empty[gbuf], ((j / SLOPES) & 1u) ^ 1u, abort_flag)) break;
+                tc_fence_after();
+                auto half = [&](int h, auto rare) {
+                    const float *k = known + 32 * h;
+                    float x[32];
 #pragma unroll
-                for (int c = 0; c < 32; c += 4) {
-                    float x[4];
-                    Pair v0(__uint_as_float(a[c]), __uint_as_float(a[c + 1])), v1(__uint_as_float(a[c + 2]), __uint_as_float(a[c + 3]));
-                    if constexpr (DW) {
-                        const float4 z = *reinterpret_cast<const float4 *>(known + c);
-                        v0 = fma2(v0, Pair(LOG2E), Pair(z.x, z.y));
-                        v1 = fma2(v1, Pair(LOG2E), Pair(z.z, z.w));
-                        if (e.bias) {
-                            v0 = add2(v0, Pair(bias));
-                            v1 = add2(v1, Pair(bias));
-                        }
-                    } else {
-                        v0 = fma2(v0, Pair(LOG2E), Pair(shift));
-                        v1 = fma2(v1, Pair(LOG2E), Pair(shift));
-                        if (e.bias) {
-                            const float4 b = *reinterpret_cast<const float4 *>(known + c);
-                            v0 = add2(v0, Pair(b.x, b.y));
-                            v1 = add2(v1, Pair(b.z, b.w));
-                        }
-                    }
-                    v0.get(x[0], x[1]);
-                    v1.get(x[2], x[3]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = exp2_fast(x[i]);
-                    if (any) {
+                    for (int c = 0; c < 32; c += 4) {
+                        Pair v0(__uint_as_float(a[h][c]), __uint_as_float(a[h][c + 1])), v1(__uint_as_float(a[h][c + 2]), __uint_as_float(a[h][c + 3]));
                         if constexpr (DW) {
-                            const int4 k = *reinterpret_cast<const int4 *>(known + 2 * BQ + c);
-                            x[0] -= k.x == (int)p ? 1.f : 0.f;
-                            x[1] -= k.y == (int)p ? 1.f : 0.f;
-                            x[2] -= k.z == (int)p ? 1.f : 0.f;
-                            x[3] -= k.w == (int)p ? 1.f : 0.f;
+                            const float4 z = *reinterpret_cast<const float4 *>(k + c);
+                            v0 = fma2(v0, Pair(LOG2E), Pair(z.x, z.y));
+                            v1 = fma2(v1, Pair(LOG2E), Pair(z.z, z.w));
+                            if constexpr (BIASED) {
+                                v0 = add2(v0, Pair(bias));
+                                v1 = add2(v1, Pair(bias));
+                            }
                         } else {
+                            v0 = fma2(v0, Pair(LOG2E), Pair(shift));
+                            v1 = fma2(v1, Pair(LOG2E), Pair(shift));
+                            if constexpr (BIASED) {
+                                const float4 b = *reinterpret_cast<const float4 *>(k + c);
+                                v0 = add2(v0, Pair(b.x, b.y));
+                                v1 = add2(v1, Pair(b.z, b.w));
+                            }
+                        }
+                        v0.get(x[c], x[c + 1]);
+                        v1.get(x[c + 2], x[c + 3]);
+                    }
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) x[i] -= c + i == mine ? 1.f : 0.f;
+                    for (int c = 0; c < 32; ++c) x[c] = exp2_fast(x[c]);
+                    if constexpr (decltype(rare)::value) {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) {
+                            if constexpr (DW) {
+                                const float g = k[BQ + c];
+                                x[c] = copysignf(1.f, g) * x[c] - (reinterpret_cast<const int *>(k)[2 * BQ + c] == (int)p ? g * up : 0.f);
+                            } else
+                                x[c] = copysignf(1.f, weight) * x[c] - (32 * h + c == mine ? weight : 0.f);
                         }
                     }
-                    Pair g0, g1;
-                    if constexpr (DW) {
-                        const float4 w = *reinterpret_cast<const float4 *>(known + BQ + c);
-                        g0 = mul2(Pair(x[0], x[1]), Pair(w.x, w.y));
-                        g1 = mul2(Pair(x[2], x[3]), Pair(w.z, w.w));
-                        if (e.dbias) {
-                            float lo, hi;
-                            add2(g0, g1).get(lo, hi);
-                            total += lo + hi;
-                        }
-                        if constexpr (std::is_same_v<T, __half>) {
-                            g0 = mul2(g0, Pair(up));
-                            g1 = mul2(g1, Pair(up));
-                        }
-                    } else {
-                        g0 = mul2(Pair(x[0], x[1]), Pair(weight));
-                        g1 = mul2(Pair(x[2], x[3]), Pair(weight));
+                    uint32_t out[16];
+#pragma unroll
+                    for (int c = 0; c < 32; c += 2) {
+                        if (DW) total = add2(total, Pair(x[c], x[c + 1]));
+                        out[c / 2] = packed<T>(x[c], x[c + 1]);
                     }
-                    float lo, hi;
-                    g0.get(lo, hi);
-                    out[c / 2] = packed<T>(lo, hi);
-                    g1.get(lo, hi);
-                    out[c / 2 + 1] = packed<T>(lo, hi);
+                    tmem_st16(to + 16 * h, out);
+                };
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (special[h])
+                        half(h, std::true_type{});
+                    else
+                        half(h, std::false_type{});
                 }
-                tmem_st16(at, out);   // (over columns that this warp alone has read)
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&sh->g_full[buf]);
+                if (lane == 0) mbar_arrive(&sh->g_full[gbuf]);
             }
             if (t.left > 1 && t.inner + 1 < t.inners) continue;
             // the end of a P tile, or of this worker's part of it
@@ -816,7 +864,9 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_fused(const __grid_co
             }
             if constexpr (DW) {
                 if (e.dbias) {   // a class's sums are those of its row's four warps, in order
-                    sh->sums[column][quad * 32 + lane] = total;
+                    float lo, hi;
+                    total.get(lo, hi);
+                    sh->sums[column][quad * 32 + lane] = (lo + hi) * down;
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh->sums_full);
                     if (column == 0) {   // (the others write there again only after these have given the sums of products back)
@@ -839,30 +889,40 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_fused(const __grid_co
     if (sh->abort && threadIdx.x == 0) ep_raise(status, EP_ERR_TIMEOUT);
     if (warp == 0) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(sh->tmem_base), "r"(512) : "memory");
     }
 }
 
-// The sums of P tiles that several workers had a part of, in the workers' order: 16 rows a block.
+// The sums of P tiles that several workers had a part of, in the workers' order.  The tile that worker blockIdx.x begins inside
+// of, if it is the first to do so; 16 rows a block.
 template <typename T>
 __global__ void __launch_bounds__(256) entropy_join(const FusedWork e) {
-    const int64_t tile = blockIdx.x;
     ep_wait_for_launch_before();
+    const int64_t begin = e.line.begin(blockIdx.x), tile = begin / e.line.inner;
     const int w0 = e.line.first_worker(tile), w1 = e.line.last_worker(tile);
-    if (w0 == w1) return;
+    if (w0 == w1 || (int)blockIdx.x != (begin == tile * e.line.inner ? w0 : w0 + 1)) return;
     const float down = e.scale->down;
-    const int row0 = blockIdx.y * 16;
-    for (int i = threadIdx.x; i < 16 * e.width && e.out; i += 256) {
-        const int row = row0 + i / e.width, c = i % e.width;
+    const int row0 = blockIdx.y * 16, chunks = e.share_ld / 4;
+    // (the first worker has it as its last segment unless that is its only one, the others as their first)
+    const int64_t first = share_of(e.line, w0, tile);
+    auto place = [&](int w) { return w == w0 ? first : 2 * (int64_t)w; };
+    for (int i = threadIdx.x; i < 16 * chunks && e.out; i += 256) {
+        const int row = row0 + i / chunks, c = (i - i / chunks * chunks) * 4;
         const int64_t p = tile * P_ROWS + row;
         if (p >= e.P) break;
-        float sum = 0.f;
-        for (int w = w0; w <= w1; ++w) sum += e.share[(share_of(e.line, w, tile) * P_ROWS + row) * e.share_ld + c];
-        static_cast<T *>(e.out)[p * e.width + c] = from_f32<T>(sum * down);
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int w = w0; w <= w1; ++w) {
+            const float4 v = *reinterpret_cast<const float4 *>(e.share + (place(w) * P_ROWS + row) * e.share_ld + c);
+            sum[0] += v.x, sum[1] += v.y, sum[2] += v.z, sum[3] += v.w;
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sum[q] *= down;
+        store_chunk(static_cast<T *>(e.out) + p * e.width, c, e.width, e.vec, sum);
     }
     if (e.dbias && threadIdx.x < 16 && tile * P_ROWS + row0 + threadIdx.x < e.P) {
         float sum = 0.f;
-        for (int w = w0; w <= w1; ++w) sum += e.share_bias[share_of(e.line, w, tile) * P_ROWS + row0 + threadIdx.x];
+        for (int w = w0; w <= w1; ++w) sum += e.share_bias[place(w) * P_ROWS + row0 + threadIdx.x];
         e.dbias[tile * P_ROWS + row0 + threadIdx.x] = sum;
     }
 }
@@ -1052,7 +1112,7 @@ __global__ void __launch_bounds__(256) entropy_weights(const float *__restrict__
             dead = target_of(targets, row, classes, status) < 0 || lse[row] == -INFINITY;
             const float g = dead ? 0.f : (float)(mean + (drow ? (double)drow[row] : 0.0));
             const float z = lse[row];
-            info.shift[row] = dead ? -INFINITY : -z * LOG2E;
+            info.shift[row] = dead ? -INFINITY : log2f(fabsf(g)) - z * LOG2E;
             info.g[row] = z != z ? z : g;
             info.target[row] = dead ? -1 : targets[row];
             if (fabsf(g) < INFINITY) top = fmaxf(top, fabsf(g));
@@ -1303,10 +1363,10 @@ int logits_of(ep_ctx *ctx, Inputs &in, const Operand &x, const Operand &w, int64
                        EP_F32, false, nullptr, share, in.stream, &in.kernels);
 }
 
-template <bool GRAD, typename T>
+template <bool GRAD, bool BIASED, typename T>
 int launch_tiles_of(ep_ctx *ctx, const CUtensorMap &x, const CUtensorMap &w, const CUtensorMap &g, const CUtensorMap &clean,
                     const TileWork &e, cudaStream_t stream) {
-    auto kernel = entropy_tiles<GRAD, T>;
+    auto kernel = entropy_tiles<GRAD, BIASED, T>;
     constexpr size_t smem = TileMemory<GRAD>::TOTAL;
     EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     cudaLaunchConfig_t cfg{};
@@ -1337,8 +1397,13 @@ int launch_tiles(ep_ctx *ctx, const Operand &x, const Operand &w, void *g, int64
         (GRAD && !(encode_result(&mg, g, x.type, 1, e.M, e.N, ld, TILE) && encode_operand(&mc, clean, false, BLOCK_ROWS))))
         return ep::fail(ctx, EP_ERR_CUDA, "cuTensorMapEncodeTiled failed for %lld rows of %d classes", (long long)e.M, e.N);
     ++*kernels;
-    return x.type == EP_BF16 ? launch_tiles_of<GRAD, __nv_bfloat16>(ctx, mx, mw, mg, mc, e, stream)
-                             : launch_tiles_of<GRAD, __half>(ctx, mx, mw, mg, mc, e, stream);
+    if constexpr (!GRAD) {
+        if (e.bias)
+            return x.type == EP_BF16 ? launch_tiles_of<GRAD, true, __nv_bfloat16>(ctx, mx, mw, mg, mc, e, stream)
+                                     : launch_tiles_of<GRAD, true, __half>(ctx, mx, mw, mg, mc, e, stream);
+    }
+    return x.type == EP_BF16 ? launch_tiles_of<GRAD, false, __nv_bfloat16>(ctx, mx, mw, mg, mc, e, stream)
+                             : launch_tiles_of<GRAD, false, __half>(ctx, mx, mw, mg, mc, e, stream);
 }
 
 struct ForwardSpace {
@@ -1628,13 +1693,13 @@ NarrowSpace narrow_space(const ep_ctx *ctx, int64_t rows, int n_in, int classes,
     return s;
 }
 
-template <bool DW, int BQ, typename T>
+template <bool DW, bool BIASED, int BQ, typename T>
 int launch_fused_of(ep_ctx *ctx, const CUtensorMap &p, const CUtensorMap &q, const CUtensorMap &clean, const FusedWork &e, cudaStream_t stream) {
-    auto kernel = entropy_fused<DW, BQ, T>;
+    auto kernel = entropy_fused<DW, BIASED, BQ, T>;
     constexpr size_t smem = FusedMemory<DW, BQ>::TOTAL;
     EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    EP_CUDA(ctx, ep::launch_early(kernel, dim3((unsigned)e.line.workers), dim3(TILE_THREADS), smem, stream, p, q, clean, e, ctx->d_status));
-    EP_CUDA(ctx, ep::launch_early(entropy_join<T>, dim3((unsigned)ep::ceil_div(e.P, P_ROWS), P_ROWS / 16), dim3(256), 0, stream, e));
+    EP_CUDA(ctx, ep::launch_early(kernel, dim3((unsigned)e.line.workers), dim3(FUSED_THREADS), smem, stream, p, q, clean, e, ctx->d_status));
+    EP_CUDA(ctx, ep::launch_early(entropy_join<T>, dim3((unsigned)e.line.workers, P_ROWS / 16), dim3(256), 0, stream, e));
     return EP_OK;
 }
 // Gradient of x (P = x, Q = W) or of W (P = W, Q = x).
@@ -1665,10 +1730,16 @@ int launch_fused(ep_ctx *ctx, Inputs &in, const NarrowSpace &s, const Operand &x
         !encode_operand(&mc, clean, false, DW ? bq : P_ROWS))
         return ep::fail(ctx, EP_ERR_CUDA, "cuTensorMapEncodeTiled failed for %lld rows of %d classes", (long long)in.rows, in.classes);
     in.kernels += 2;
+    // (dW of fp16 takes the power of two that G is scaled by with the bias)
+    const bool biased = e.bias || (DW && in.type == EP_F16);
+    auto launch = [&](auto biased, auto type) {
+        using T = decltype(type);
+        return bq == 128 ? launch_fused_of<DW, decltype(biased)::value, 128, T>(ctx, mp, mq, mc, e, in.stream)
+                         : launch_fused_of<DW, decltype(biased)::value, 64, T>(ctx, mp, mq, mc, e, in.stream);
+    };
     if (in.type == EP_BF16)
-        return bq == 128 ? launch_fused_of<DW, 128, __nv_bfloat16>(ctx, mp, mq, mc, e, in.stream)
-                         : launch_fused_of<DW, 64, __nv_bfloat16>(ctx, mp, mq, mc, e, in.stream);
-    return bq == 128 ? launch_fused_of<DW, 128, __half>(ctx, mp, mq, mc, e, in.stream) : launch_fused_of<DW, 64, __half>(ctx, mp, mq, mc, e, in.stream);
+        return biased ? launch(std::true_type{}, __nv_bfloat16{}) : launch(std::false_type{}, __nv_bfloat16{});
+    return biased ? launch(std::true_type{}, __half{}) : launch(std::false_type{}, __half{});
 }
 
 int narrow_backward_run(ep_ctx *ctx, Inputs &in, const NarrowSpace &s, const Given &given, const Wanted &out) {
