@@ -1122,11 +1122,18 @@ __global__ void __launch_bounds__(256) entropy_weights(const float *__restrict__
             info.g[row] = 0.f;
             info.target[row] = -1;
         }
-        for (unsigned left = __ballot_sync(FULL, dead); left; left &= left - 1) {
-            const T *from = static_cast<const T *>(x) + (row0 + (threadIdx.x & ~31) + __ffs(left) - 1) * ldx;
-            bool bad = false;
-            for (int c = lane; c < n_in; c += 32) bad |= !(fabsf(to_f32(from[c])) < 1e18f);
-            if (bad) bad_rows = 1;
+        // four rows at a time, 8 lanes to each
+        for (unsigned left = __ballot_sync(FULL, dead); left;) {
+            unsigned mine = left;
+            for (int i = 0; i < (lane >> 3); ++i) mine &= mine - 1;
+            if (mine) {
+                const T *from = static_cast<const T *>(x) + (row0 + (threadIdx.x & ~31) + __ffs(mine) - 1) * ldx;
+                bool bad = false;
+#pragma unroll 8
+                for (int c = lane & 7; c < n_in; c += 8) bad |= !(fabsf(to_f32(from[c])) < 1e18f);
+                if (bad) bad_rows = 1;
+            }
+            for (int i = 0; i < 4; ++i) left &= left - 1;
         }
     }
 #pragma unroll

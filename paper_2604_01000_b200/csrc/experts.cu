@@ -48,43 +48,83 @@ struct Chunk {
             for (int i = 0; i < N; ++i) e[i] = c + i * 32 + lane < n ? row[c + i * 32 + lane] : T{};
         }
     }
-    __device__ __forceinline__ Pair pair(int i) const { return Pair(to_f32(e[2 * i]), to_f32(e[2 * i + 1])); }
+    // Elements 2 i and 2 i + 1.  (Integers without the conversion instruction, which runs at a quarter of this rate: the byte less
+    // its sign's offset into the low bits of 2^23, and the offset off again.)
+    __device__ __forceinline__ Pair pair(int i) const {
+        if constexpr (std::is_same_v<T, i8> && VEC) {
+            const uint32_t w = reinterpret_cast<const uint32_t *>(e)[i / 2] ^ 0x80808080u;
+            return add2(Pair(__uint_as_float(__byte_perm(w, 0x4B000000u, 0x7640 + (i & 1) * 2)),
+                             __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7641 + (i & 1) * 2))),
+                        Pair(-8388736.f));
+        } else
+            return Pair(to_f32(e[2 * i]), to_f32(e[2 * i + 1]));
+    }
 };
 
-// sum[j][r] = w_j . x_r over this lane's columns.
-template <typename W, typename X, bool VEC, int J, int R>
-__device__ __forceinline__ void dots(const W *const (&w)[J], const X *const (&x)[R], int from, int to, int n, int lane, float (&sum)[J][R]) {
-    constexpr int N = 16 / (int)sizeof(W);
-    Pair t[J][R];
-#pragma unroll
-    for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int r = 0; r < R; ++r) t[j][r] = Pair(0.f);
-#pragma unroll 2
-    for (int c = from; c < to; c += 32 * N) {
-        Chunk<W, N, VEC> a[J];
-#pragma unroll
-        for (int j = 0; j < J; ++j) a[j].load(w[j], c, lane, n);
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            Chunk<X, N, VEC> b;
-            b.load(x[r], c, lane, n);
-#pragma unroll
-            for (int i = 0; i < N / 2; ++i) {
-                const Pair v = b.pair(i);
-#pragma unroll
-                for (int j = 0; j < J; ++j) t[j][r] = fma2(a[j].pair(i), v, t[j][r]);
-            }
-        }
-    }
+// Sums over the lanes: half of them stay with either half of the lanes, until there is one to each.  The sum of pair j R + r
+// goes to the lanes from (j R + r) 32 / (J R) on.
+template <int J, int R>
+__device__ __forceinline__ float over_lanes(const Pair (&t)[J][R], int lane) {
+    constexpr int M = J * R;
+    float v[M];
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             float lo, hi;
             t[j][r].get(lo, hi);
-            sum[j][r] = lo + hi;
+            v[j * R + r] = lo + hi;
         }
+    int o = 16;
+#pragma unroll
+    for (int m = M / 2; m >= 1; m /= 2, o /= 2) {
+        const bool upper = lane & o;
+#pragma unroll
+        for (int i = 0; i < m; ++i) {
+            const float mine = upper ? v[i + m] : v[i], theirs = upper ? v[i] : v[i + m];
+            v[i] = mine + __shfl_xor_sync(FULL, theirs, o);
+        }
+    }
+#pragma unroll
+    for (; o >= 1; o /= 2) v[0] += __shfl_xor_sync(FULL, v[0], o);
+    return v[0];
+}
+
+// What a lane takes of a row at a time: 16 bytes, or, where rows are not aligned for that, 4 elements.
+template <typename W, bool VEC>
+constexpr int step_elements() { return VEC ? 16 / (int)sizeof(W) : 4; }
+// w_j . x_r over a share of the columns, for J rows of weights and R rows of x, read straight into registers.
+template <typename W, typename X, bool VEC, int J, int R>
+__device__ __forceinline__ float dots(const W *const (&w)[J], const X *const (&x)[R], int from, int to, int n, int lane) {
+    constexpr int N = step_elements<W, VEC>(), AHEAD = 2;
+    Pair t[J][R];
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int r = 0; r < R; ++r) t[j][r] = Pair(0.f);
+    for (int c0 = from; c0 < to; c0 += AHEAD * 32 * N) {
+        Chunk<W, N, VEC> a[AHEAD][J];
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q)
+#pragma unroll
+            for (int j = 0; j < J; ++j) a[q][j].load(w[j], c0 + q * 32 * N, lane, n);
+#pragma unroll
+        for (int q = 0; q < AHEAD; ++q) {
+            if (q > 0 && c0 + q * 32 * N >= to) break;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                Chunk<X, N, VEC> b;
+                b.load(x[r], c0 + q * 32 * N, lane, n);
+#pragma unroll
+                for (int i = 0; i < N / 2; ++i) {
+                    const Pair v = b.pair(i);
+#pragma unroll
+                    for (int j = 0; j < J; ++j) t[j][r] = fma2(a[q][j].pair(i), v, t[j][r]);
+                }
+            }
+        }
+    }
+    return over_lanes(t, lane);
 }
 __device__ __forceinline__ float over_lanes(float v) {
 #pragma unroll
@@ -92,34 +132,146 @@ __device__ __forceinline__ float over_lanes(float v) {
     return v;
 }
 
+template <typename W>
+struct Rows {
+    const W *first;
+    int64_t ld;
+    int count, from, to;   // rows, columns
+};
+// Products of (up to) four rows of weights that are not aligned for 16-byte accesses.
+template <typename W, typename X, int R>
+__device__ __forceinline__ float straight(const Rows<W> &rows, const X *const (&x)[R], int lane) {
+    const W *w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = rows.first + min(j, rows.count - 1) * rows.ld;
+    return dots<W, X, false, 4, R>(w, x, rows.from, rows.to, rows.to, lane);
+}
+// item(n) with the n of 1, 2, 4 and 8 that `count` rows need.
+template <typename Item>
+__device__ __forceinline__ void by_rows(int count, Item &item) {
+    if (count == 1)
+        item(std::integral_constant<int, 1>{});
+    else if (count == 2)
+        item(std::integral_constant<int, 2>{});
+    else if (count <= 4)
+        item(std::integral_constant<int, 4>{});
+    else
+        item(std::integral_constant<int, 8>{});
+}
+// Rows of weights on their way to shared memory, STREAM_STAGES - 1 steps ahead of their use and past the end of an item (four
+// rows, and the columns that are wanted of them): what is in flight is what a warp gets out of the memory (weights read by the
+// item into registers, used, and only then the next: 1.8 TB/s).  Each lane reads back what it copied itself.
+constexpr int STREAM_ROWS = 4, STREAM_STAGES = 4;
+constexpr size_t STREAM_BYTES = (size_t)STREAM_STAGES * STREAM_ROWS * THREADS * 16;
+template <typename W, typename Find>
+struct Stream {
+    static constexpr int N = 16 / (int)sizeof(W);
+    uint4 *mine;
+    const Find &find;      // the rows of an item
+    const int64_t items, step;
+    int64_t item;
+    Rows<W> rows;
+    int c, to_stage, stage;
+    __device__ __forceinline__ Stream(void *room, const Find &f, int64_t first, int64_t all, int64_t by)
+        : mine(static_cast<uint4 *>(room) + threadIdx.x), find(f), items(all), step(by), item(first), to_stage(0), stage(0) {
+        open();
+        for (int s = 0; s < STREAM_STAGES - 1; ++s) fetch();
+    }
+    __device__ __forceinline__ void open() {
+        if (item < items) {
+            rows = find(item);
+            c = rows.from;
+        }
+    }
+    __device__ __forceinline__ void fetch() {
+        if (item < items) {
+            const int col = c + (threadIdx.x & 31) * N;
+            if (col < rows.to) {
+                uint4 *to = mine + to_stage * STREAM_ROWS * THREADS;
+                const W *from = rows.first + col;
+#pragma unroll
+                for (int j = 0; j < STREAM_ROWS; ++j)
+                    if (j < rows.count) copy_async<16>(to + j * THREADS, from + j * rows.ld);
+            }
+            c += 32 * N;
+            if (c >= rows.to) {
+                item += step;
+                open();
+            }
+        }
+        copies_end_group();
+        to_stage = to_stage + 1 == STREAM_STAGES ? 0 : to_stage + 1;
+    }
+    // w_j . x_r of the item whose turn it is (its columns are from..to).
+    template <typename X, int R>
+    __device__ __forceinline__ void add(const X *const (&x)[R], int from, int to, Pair (&t)[STREAM_ROWS][R]) {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int j = 0; j < STREAM_ROWS; ++j)
+#pragma unroll
+            for (int r = 0; r < R; ++r) t[j][r] = Pair(0.f);
+#pragma unroll 1
+        for (int c0 = from; c0 < to; c0 += 32 * N) {
+            fetch();
+            copies_wait<STREAM_STAGES - 1>();
+            const int col = c0 + lane * N;
+            const bool there = col < to;
+            Chunk<W, N, true> a[STREAM_ROWS];
+#pragma unroll
+            for (int j = 0; j < STREAM_ROWS; ++j) {
+                // (rows past the last are whatever was there before: their sums go nowhere)
+                const uint4 v = mine[(stage * STREAM_ROWS + j) * THREADS];
+                *reinterpret_cast<uint4 *>(a[j].e) = there ? v : make_uint4(0, 0, 0, 0);
+            }
+            // a few columns at a time: what is converted has to fit the registers beside the sums
+            constexpr int SOME = R >= 8 || sizeof(X) == 4 || N < 8 ? 4 : 8;
+#pragma unroll
+            for (int q = 0; q < N; q += SOME) {
+                Pair w[STREAM_ROWS][SOME / 2];
+#pragma unroll
+                for (int j = 0; j < STREAM_ROWS; ++j)
+#pragma unroll
+                    for (int i = 0; i < SOME / 2; ++i) w[j][i] = a[j].pair(q / 2 + i);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    using Bytes = typename Raw<SOME * (int)sizeof(X)>::type;
+                    alignas(16) X b[SOME];
+                    *reinterpret_cast<Bytes *>(b) = there ? *reinterpret_cast<const Bytes *>(x[r] + col + q) : Bytes{};
+#pragma unroll
+                    for (int i = 0; i < SOME / 2; ++i) {
+                        const Pair v(to_f32(b[2 * i]), to_f32(b[2 * i + 1]));
+#pragma unroll
+                        for (int j = 0; j < STREAM_ROWS; ++j) t[j][r] = fma2(w[j][i], v, t[j][r]);
+                    }
+                }
+            }
+            stage = stage + 1 == STREAM_STAGES ? 0 : stage + 1;
+        }
+    }
+    template <typename X, int R>
+    __device__ __forceinline__ float dots(const X *const (&x)[R], int from, int to) {
+        Pair t[STREAM_ROWS][R];
+        add<X, R>(x, from, to, t);
+        return over_lanes(t, threadIdx.x & 31);
+    }
+};
+
 // ---------------------------------------------------------------------------------------------- router
-// logits[row][e] = x Wr^T + br: a warp to a part and up to 8 rows.
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) experts_logits(const T *x, int64_t ldx, const T *router, const void *bias, int bias_type, int rows,
+// logits[row][e] = x Wr^T + br: a warp to a part and R rows.
+template <typename T, bool VEC, int R>
+__global__ void __launch_bounds__(128) experts_logits(const T *x, int64_t ldx, const T *router, const void *bias, int bias_type, int rows,
                                                       int n_in, int experts, float *logits) {
-    const int lane = threadIdx.x & 31, e = blockIdx.x * 8 + (threadIdx.x >> 5), row0 = blockIdx.y * GROUP;
+    const int lane = threadIdx.x & 31, e = blockIdx.x * 4 + (threadIdx.x >> 5), row0 = blockIdx.y * R;
     ep_let_next_launch_start();
     if (e >= experts) return;
     const T *w[1] = {router + (int64_t)e * n_in};
-    const T *xs[GROUP];
+    const T *xs[R];
 #pragma unroll
-    for (int r = 0; r < GROUP; ++r) xs[r] = x + min(row0 + r, rows - 1) * ldx;
+    for (int r = 0; r < R; ++r) xs[r] = x + min(row0 + r, rows - 1) * ldx;
     const float add = bias ? load_param(bias, bias_type, e) : 0.f;
-    if (rows - row0 == 1) {
-        const T *one[1] = {xs[0]};
-        float sum[1][1];
-        dots<T, T, VEC, 1, 1>(w, one, 0, n_in, n_in, lane, sum);
-        const float v = over_lanes(sum[0][0]);
-        if (lane == 0) logits[row0 * experts + e] = v + add;
-    } else {
-        float sum[1][GROUP];
-        dots<T, T, VEC, 1, GROUP>(w, xs, 0, n_in, n_in, lane, sum);
-#pragma unroll
-        for (int r = 0; r < GROUP; ++r) {
-            const float v = over_lanes(sum[0][r]);
-            if (lane == 0 && row0 + r < rows) logits[(row0 + r) * experts + e] = v + add;
-        }
-    }
+    const float v = dots<T, T, VEC, 1, R>(w, xs, 0, n_in, n_in, lane);
+    const int r = lane / (32 / R);
+    if (lane % (32 / R) == 0 && row0 + r < rows) logits[(row0 + r) * experts + e] = v + add;
 }
 
 // A row's k best parts and their weights (as ep_route), by one warp.
@@ -237,6 +389,60 @@ __global__ void __launch_bounds__(1024) experts_choose(const float *logits, cons
     }
 }
 
+// The same by every block of the first product for itself, for a few rows (a launch less): ids, weights and the plan come to
+// shared memory, and from the first block to where the launches that follow look for them.
+constexpr int OWN_ROWS = 16, OWN_SLOTS = 64;
+struct OwnPlan {
+    int32_t ids[OWN_SLOTS];
+    float weights[OWN_SLOTS];
+    int sorted[OWN_SLOTS];
+    Group groups[OWN_SLOTS];
+    int n_groups;
+    bool starts[OWN_SLOTS];   // a group
+};
+__device__ void choose_here(const float *logits, const uint8_t *valid, int rows, int experts, int k, bool renormalize, OwnPlan &own, bool tell,
+                            int32_t *ids, float *weights, const Plan &plan) {
+    const int lane = threadIdx.x & 31, slots = rows * k, s = threadIdx.x;
+    for (int r = threadIdx.x >> 5; r < rows; r += (int)(blockDim.x >> 5))
+        choose(logits + r * experts, experts, k, !valid || valid[r], renormalize, lane, own.ids + r * k, own.weights + r * k);
+    __syncthreads();
+    // (in an order that all blocks agree on: they share out the groups by their numbers)
+    const int e = s < slots ? own.ids[s] : -1;
+    int before = 0, of_part = 0, earlier = 0, number = 0;   // slots of lower parts; slots of this part, and those of them before this one
+    if (s < slots) {
+        for (int q = 0; q < slots; ++q) {
+            const int o = own.ids[q];
+            before += o >= 0 && o < e;
+            of_part += o == e;
+            earlier += o == e && q < s;
+        }
+        own.starts[s] = e >= 0 && earlier % GROUP == 0;
+    }
+    __syncthreads();
+    if (s < slots) {
+        for (int q = 0; q < slots; ++q) number += own.starts[q] && (own.ids[q] < e || (own.ids[q] == e && q < s));
+        const int at = e < 0 ? -1 : before + earlier;
+        if (e >= 0) {
+            own.sorted[at] = s;
+            if (own.starts[s]) own.groups[number] = Group{e, at, min(of_part - earlier, GROUP)};
+        }
+        if (tell) {
+            plan.place[s] = at;
+            ids[s] = e;
+            weights[s] = own.weights[s];
+        }
+    }
+    if (s < 32) {
+        int n = 0;
+        for (int q = s; q < slots; q += 32) n += own.starts[q];
+        n = __reduce_add_sync(FULL, n);
+        if (s == 0) own.n_groups = n;
+    }
+    __syncthreads();
+    if (tell && s < own.n_groups) plan.groups[s] = own.groups[s];
+    if (tell && s == 0) *plan.n_groups = own.n_groups;
+}
+
 // ---------------------------------------------------------------------------------------------- products
 struct Weights {
     const void *w;
@@ -245,109 +451,131 @@ struct Weights {
     int bias_type;
 };
 
-// hidden[place][j] = act(W1[e][j] . x + b1[e][j]): a warp to J rows of a part's weights.
-template <typename T, typename W, bool VEC, int J, int R>
-__device__ __forceinline__ void hidden_of(const T *x, int64_t ldx, const Weights &w1, int n_in, int n_hidden, int act, int k, const Plan &p,
-                                          const Group &g, int j0, float *hidden, int lane) {
-    const W *w[J];
+// hidden[place][j] = act(W1[e][j] . x + b1[e][j]): a warp to 4 rows of a part's weights; dots: their products with R rows of x.
+template <typename T, int R, typename Dots>
+__device__ __forceinline__ void hidden_of(const T *x, int64_t ldx, const Weights &w1, int n_hidden, int act, int k, const int *sorted,
+                                          const Group &g, int j0, float *hidden, int lane, Dots dots) {
     const T *xs[R];
 #pragma unroll
-    for (int j = 0; j < J; ++j) w[j] = static_cast<const W *>(w1.w) + ((int64_t)g.expert * n_hidden + min(j0 + j, n_hidden - 1)) * n_in;
-#pragma unroll
-    for (int r = 0; r < R; ++r) xs[r] = x + (p.sorted[g.first + min(r, g.count - 1)] / k) * ldx;
-    float sum[J][R];
-    dots<W, T, VEC, J, R>(w, xs, 0, n_in, n_in, lane, sum);
-    // sum q of the J x R goes to lane q
-    float v[1] = {0.f};
-#pragma unroll
-    for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const float t = over_lanes(sum[j][r]);
-            if (lane == j * R + r) v[0] = t;
-        }
-    const int j = j0 + lane / R, r = lane % R;
-    if (lane < J * R && j < n_hidden && r < g.count) {
-        const int64_t at = (int64_t)g.expert * n_hidden + j;
-        if (w1.scale) v[0] *= w1.scale[at];
-        if (w1.bias) v[0] += load_param(w1.bias, w1.bias_type, at);
+    for (int r = 0; r < R; ++r) xs[r] = x + (sorted[g.first + min(r, g.count - 1)] / k) * ldx;
+    constexpr int LANES = 32 / (STREAM_ROWS * R);
+    const int j = j0 + lane / LANES / R, r = lane / LANES % R;
+    const bool mine = lane % LANES == 0 && j < n_hidden && r < g.count;
+    const int64_t at = (int64_t)g.expert * n_hidden + j;
+    const float scale = mine && w1.scale ? w1.scale[at] : 1.f, bias = mine && w1.bias ? load_param(w1.bias, w1.bias_type, at) : 0.f;
+    float v[1] = {dots(xs)};
+    if (mine) {
+        v[0] = fmaf(v[0], scale, bias);
         activate(v, act);
         hidden[(int64_t)(g.first + r) * n_hidden + j] = v[0];
     }
 }
+struct Router {   // of a layer whose blocks choose for themselves
+    bool here;
+    const float *logits;
+    const uint8_t *valid;
+    int rows, experts;
+    bool renormalize;
+    int32_t *ids;
+    float *weights;
+};
+// Asks for bytes [from, to) of [0, all) of the L2 (in whole 16 bytes).
+__device__ __forceinline__ void ask_l2(const char *base, int64_t all, int part, int parts) {
+    const int64_t from = all * part / parts & ~int64_t(15), to = all * (part + 1) / parts & ~int64_t(15);
+    if (to > from) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(base + from), "r"((uint32_t)(to - from)) : "memory");
+}
 template <typename T, typename W, bool VEC>
 __global__ void __launch_bounds__(THREADS) experts_hidden(const T *x, int64_t ldx, Weights w1, int n_in, int n_hidden, int act, int k, Plan p,
-                                                          float *hidden) {
-    constexpr int J = 4;
+                                                          Router router, const void *w2, int64_t w2_bytes, float *hidden) {
+    __shared__ OwnPlan own;
     const int lane = threadIdx.x & 31;
     ep_wait_for_launch_before();
     ep_let_next_launch_start();
-    const int across = (n_hidden + J - 1) / J;
-    const int64_t items = (int64_t)*p.n_groups * across, step = (int64_t)gridDim.x * WARPS;
-    for (int64_t i = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5); i < items; i += step) {
-        const Group g = p.groups[i / across];
-        const int j0 = (int)(i % across) * J;
-        if (g.count == 1)
-            hidden_of<T, W, VEC, J, 1>(x, ldx, w1, n_in, n_hidden, act, k, p, g, j0, hidden, lane);
-        else if (g.count == 2)
-            hidden_of<T, W, VEC, J, 2>(x, ldx, w1, n_in, n_hidden, act, k, p, g, j0, hidden, lane);
-        else if (g.count <= 4)
-            hidden_of<T, W, VEC, J, 4>(x, ldx, w1, n_in, n_hidden, act, k, p, g, j0, hidden, lane);
-        else
-            hidden_of<T, W, VEC, J, 8>(x, ldx, w1, n_in, n_hidden, act, k, p, g, j0, hidden, lane);
+    const int *sorted = p.sorted;
+    const Group *groups = p.groups;
+    if (router.here) {
+        choose_here(router.logits, router.valid, router.rows, router.experts, k, router.renormalize, own, blockIdx.x == 0, router.ids,
+                    router.weights, p);
+        sorted = own.sorted;
+        groups = own.groups;
     }
+    const int n_groups = router.here ? own.n_groups : *p.n_groups;
+    // While this product waits for its own weights, those of the next one come to the L2, where they fit it.
+    if (w2_bytes && threadIdx.x < n_groups)
+        ask_l2(static_cast<const char *>(w2) + groups[threadIdx.x].expert * w2_bytes, w2_bytes, blockIdx.x, gridDim.x);
+    const int across = (n_hidden + STREAM_ROWS - 1) / STREAM_ROWS;
+    const int64_t items = (int64_t)n_groups * across, step = (int64_t)gridDim.x * WARPS, first = (int64_t)(threadIdx.x >> 5) * gridDim.x + blockIdx.x;
+    auto rows_of = [&](int64_t i) {
+        const int q = (int)(i / across), j0 = (int)(i - (int64_t)q * across) * STREAM_ROWS;
+        return Rows<W>{static_cast<const W *>(w1.w) + ((int64_t)groups[q].expert * n_hidden + j0) * n_in, n_in, min(STREAM_ROWS, n_hidden - j0), 0,
+                       n_in};
+    };
+    // each item's products by the rows that its group has
+    auto all = [&](auto products) {
+        for (int64_t i = first; i < items; i += step) {
+            const int q = (int)(i / across), j0 = (int)(i - (int64_t)q * across) * STREAM_ROWS;
+            const Group g = groups[q];
+            auto item = [&](auto rows) {
+                hidden_of<T, decltype(rows)::value>(x, ldx, w1, n_hidden, act, k, sorted, g, j0, hidden, lane,
+                                                    [&](const T *const (&xs)[decltype(rows)::value]) { return products(i, xs); });
+            };
+            by_rows(g.count, item);
+        }
+    };
+    if constexpr (VEC) {
+        extern __shared__ uint4 ring[];
+        Stream<W, decltype(rows_of)> stream(ring, rows_of, first, items, step);
+        all([&](int64_t, const auto &xs) { return stream.dots(xs, 0, n_in); });
+        copies_wait<0>();
+    } else
+        all([&](int64_t i, const auto &xs) { return straight<W>(rows_of(i), xs, lane); });
 }
 
 // y[share][place][column of the block] = W2[e][column] . hidden over one share of the hidden values.
-template <typename W, bool VEC, int J, int R>
-__device__ __forceinline__ void output_of(const Weights &w2, int n_hidden, int n_out, const Group &g, int col0, int from, int to, const float *hidden,
-                                          float *y, int cols, int at, int lane) {
-    const W *w[J];
+template <int R, typename Dots>
+__device__ __forceinline__ void output_of(const float *hidden, int n_hidden, const Group &g, float *y, int cols, int at, int lane, Dots dots) {
     const float *xs[R];
 #pragma unroll
-    for (int j = 0; j < J; ++j) w[j] = static_cast<const W *>(w2.w) + ((int64_t)g.expert * n_out + min(col0 + j, n_out - 1)) * n_hidden;
-#pragma unroll
     for (int r = 0; r < R; ++r) xs[r] = hidden + (int64_t)(g.first + min(r, g.count - 1)) * n_hidden;
-    float sum[J][R];
-    dots<W, float, VEC, J, R>(w, xs, from, to, to, lane, sum);
-    float v = 0.f;
-#pragma unroll
-    for (int j = 0; j < J; ++j)
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const float t = over_lanes(sum[j][r]);
-            if (lane == j * R + r) v = t;
-        }
-    const int j = lane / R, r = lane % R;
-    if (lane < J * R && at + j < cols && r < g.count) y[(g.first + r) * cols + at + j] = v;
+    const float v = dots(xs);
+    constexpr int LANES = 32 / (STREAM_ROWS * R);
+    const int j = lane / LANES / R, r = lane / LANES % R;
+    if (lane % LANES == 0 && at + j < cols && r < g.count) y[(g.first + r) * cols + at + j] = v;
 }
-// A block has `cols` columns of the output, of all rows; its warps share out groups, columns and shares of the hidden values.
+// A block has `cols` columns of the output, of all rows; its warps share out groups, 4 columns at a time, and shares of the hidden values.
 template <typename T, typename W, bool VEC>
 __global__ void __launch_bounds__(THREADS) experts_output(const float *hidden, Weights w2, int n_hidden, int n_out, int rows, int k, Plan p,
                                                           const int32_t *ids, const float *weights, const T *residual, int64_t ldr, T *out,
                                                           int cols, int shares, int per_share) {
-    constexpr int J = 4;
-    extern __shared__ float y[];   // [shares][rows * k][cols]
+    extern __shared__ uint4 ring[];   // of the weights, where VEC; then y[shares][rows * k][cols]
+    float *y = reinterpret_cast<float *>(reinterpret_cast<char *>(ring) + (VEC ? STREAM_BYTES : 0));
     const int lane = threadIdx.x & 31, slots = rows * k;
     const int col0 = blockIdx.x * cols, mine = min(cols, n_out - col0);
     ep_wait_for_launch_before();
-    const int across = (mine + J - 1) / J;
-    const int items = *p.n_groups * across * shares;
-    for (int i = threadIdx.x >> 5; i < items; i += WARPS) {
-        const int share = i % shares, q = i / shares;
-        const Group g = p.groups[q / across];
-        const int at = q % across * J;
-        const int from = share * per_share, to = min(from + per_share, n_hidden);
-        float *ys = y + share * slots * cols;
-        if (g.count == 1)
-            output_of<W, VEC, J, 1>(w2, n_hidden, n_out, g, col0 + at, from, to, hidden, ys, cols, at, lane);
-        else if (g.count == 2)
-            output_of<W, VEC, J, 2>(w2, n_hidden, n_out, g, col0 + at, from, to, hidden, ys, cols, at, lane);
-        else if (g.count <= 4)
-            output_of<W, VEC, J, 4>(w2, n_hidden, n_out, g, col0 + at, from, to, hidden, ys, cols, at, lane);
-        else
-            output_of<W, VEC, J, 8>(w2, n_hidden, n_out, g, col0 + at, from, to, hidden, ys, cols, at, lane);
-    }
+    const int across = (mine + STREAM_ROWS - 1) / STREAM_ROWS;
+    const int items = *p.n_groups * across * shares, first = threadIdx.x >> 5;
+    auto rows_of = [&](int64_t i) {
+        const int share = (int)i % shares, q = (int)i / shares, at = q % across * STREAM_ROWS, from = share * per_share;
+        return Rows<W>{static_cast<const W *>(w2.w) + ((int64_t)p.groups[q / across].expert * n_out + col0 + at) * n_hidden, n_hidden,
+                       min(STREAM_ROWS, mine - at), from, min(from + per_share, n_hidden)};
+    };
+    auto all = [&](auto products) {
+        for (int i = first; i < items; i += WARPS) {
+            const int share = i % shares, q = i / shares, at = q % across * STREAM_ROWS;
+            const Group g = p.groups[q / across];
+            auto item = [&](auto rows) {
+                output_of<decltype(rows)::value>(hidden, n_hidden, g, y + share * slots * cols, cols, at, lane,
+                                                 [&](const float *const (&xs)[decltype(rows)::value]) { return products(i, xs, share); });
+            };
+            by_rows(g.count, item);
+        }
+    };
+    if constexpr (VEC) {
+        Stream<W, decltype(rows_of)> stream(ring, rows_of, first, items, WARPS);
+        all([&](int, const auto &xs, int share) { return stream.dots(xs, share * per_share, min(share * per_share + per_share, n_hidden)); });
+        copies_wait<0>();
+    } else
+        all([&](int i, const auto &xs, int) { return straight<W>(rows_of(i), xs, lane); });
     __syncthreads();
     for (int i = threadIdx.x; i < rows * mine; i += THREADS) {
         const int row = i / mine, c = i - row * mine;
@@ -407,43 +635,64 @@ Space space(int64_t rows, int n_hidden, int experts, int k, void *base) {
     return s;
 }
 
+constexpr int64_t L2_SHARE = 48ll << 20;   // what the next product's weights may take of the L2
+
 template <typename T, typename W, bool VEC>
-int run_products(ep_ctx *ctx, const Layer &l, const Space &s) {
-    constexpr int STEP = 32 * 16 / (int)sizeof(W);   // columns that a warp takes at a time
+int run_products(ep_ctx *ctx, const Layer &l, const Space &s, const Router &router) {
     const int slots = (int)l.rows * l.k;
-    EP_CUDA(ctx, ep::launch_early(experts_hidden<T, W, VEC>, dim3(ctx->sm_count), dim3(THREADS), 0, l.stream, (const T *)l.x, l.ldx, l.w1,
-                                  l.n_in, l.n_hidden, l.act, l.k, s.plan, s.hidden));
-    const int cols = std::max(1, std::min({(int)ep::ceil_div(l.n_out, ctx->sm_count), (int)(160 * 1024 / (sizeof(float) * slots)), 64}));
+    const int64_t w2_bytes = (int64_t)l.n_out * l.n_hidden * sizeof(W);
+    // (at most one group to a slot; what is asked for starts on 16 bytes)
+    const bool ask = ep::aligned(l.w2.w, 16) && w2_bytes % 16 == 0 && w2_bytes * std::min(slots, l.experts) <= L2_SHARE;
+    const size_t ring = VEC ? STREAM_BYTES : 0;
+    auto first = experts_hidden<T, W, VEC>;
+    if (VEC) EP_CUDA(ctx, cudaFuncSetAttribute(first, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ring));
+    EP_CUDA(ctx, ep::launch_early(first, dim3(ctx->sm_count), dim3(THREADS), ring, l.stream, (const T *)l.x, l.ldx, l.w1, l.n_in, l.n_hidden,
+                                  l.act, l.k, s.plan, router, l.w2.w, ask ? w2_bytes : (int64_t)0, s.hidden));
+    constexpr int STEP = 32 * step_elements<W, VEC>();   // columns that a warp takes at a time
+    constexpr size_t ROOM = 80 * 1024;                   // of y
+    const int cols = std::max(1, std::min({(int)ep::ceil_div(l.n_out, ctx->sm_count), (int)(ROOM / (sizeof(float) * slots)), 64}));
     // shares of the hidden values, so that every warp has something to do
-    const int items = l.k * (int)ep::ceil_div(cols, 4);
-    int shares = std::max(1, std::min({WARPS / items, (int)ep::ceil_div(l.n_hidden, 2 * STEP), (int)(160 * 1024 / (sizeof(float) * slots * cols))}));
+    const int items = l.k * (int)ep::ceil_div(cols, STREAM_ROWS);
+    int shares = std::max(1, std::min({WARPS / items, (int)ep::ceil_div(l.n_hidden, 2 * STEP), (int)(ROOM / (sizeof(float) * slots * cols))}));
     const int per_share = (int)ep::ceil_div(ep::ceil_div(l.n_hidden, shares), STEP) * STEP;
     shares = (int)ep::ceil_div(l.n_hidden, per_share);
-    const size_t smem = sizeof(float) * shares * slots * cols;
-    auto kernel = experts_output<T, W, VEC>;
-    if (smem > 48 * 1024) EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    EP_CUDA(ctx, ep::launch_early(kernel, dim3((unsigned)ep::ceil_div(l.n_out, cols)), dim3(THREADS), smem, l.stream, s.hidden, l.w2, l.n_hidden,
-                                  l.n_out, (int)l.rows, l.k, s.plan, l.ids, l.weights, (const T *)l.residual, l.ldr, (T *)l.out, cols,
-                                  shares, per_share));
+    auto second = experts_output<T, W, VEC>;
+    EP_CUDA(ctx, cudaFuncSetAttribute(second, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(ring + ROOM)));
+    EP_CUDA(ctx, ep::launch_early(second, dim3((unsigned)ep::ceil_div(l.n_out, cols)), dim3(THREADS), ring + sizeof(float) * shares * slots * cols,
+                                  l.stream, s.hidden, l.w2, l.n_hidden, l.n_out, (int)l.rows, l.k, s.plan, l.ids, l.weights,
+                                  (const T *)l.residual, l.ldr, (T *)l.out, cols, shares, per_share));
     return EP_OK;
 }
 
 bool sixteen(const void *p, int64_t ld, int size) { return ep::aligned(p, 16) && ld * size % 16 == 0; }
 
+template <typename T, bool VEC>
+int launch_logits(ep_ctx *ctx, const Layer &l, float *logits) {
+    const int r = l.rows == 1 ? 1 : l.rows == 2 ? 2 : 4;
+    auto kernel = r == 1 ? experts_logits<T, VEC, 1> : r == 2 ? experts_logits<T, VEC, 2> : experts_logits<T, VEC, 4>;
+    kernel<<<dim3((unsigned)ep::ceil_div(l.experts, 4), (unsigned)ep::ceil_div(l.rows, r)), 128, 0, l.stream>>>(
+        (const T *)l.x, l.ldx, (const T *)l.router, l.router_bias, l.router_bias_type, (int)l.rows, l.n_in, l.experts, logits);
+    EP_CUDA(ctx, cudaGetLastError());
+    return EP_OK;
+}
 template <typename T>
-int run_layer(ep_ctx *ctx, const Layer &l, const Space &s) {
+int run_layer(ep_ctx *ctx, const Layer &l, const Space &s, int *kernels) {
     const int size = sizeof(T), w_size = ep::type_size(l.w_type);
     const bool x_ready = sixteen(l.x, l.ldx, size);
-    const dim3 grid((unsigned)ep::ceil_div(l.experts, 8), (unsigned)ep::ceil_div(l.rows, GROUP));
-    auto logits = x_ready && sixteen(l.router, l.n_in, size) ? experts_logits<T, true> : experts_logits<T, false>;
-    logits<<<grid, 256, 0, l.stream>>>((const T *)l.x, l.ldx, (const T *)l.router, l.router_bias, l.router_bias_type, (int)l.rows, l.n_in,
-                                       l.experts, s.logits);
-    EP_CUDA(ctx, cudaGetLastError());
-    EP_CUDA(ctx, ep::launch_early(experts_choose, dim3(1), dim3(1024), 0, l.stream, s.logits, l.valid, (int)l.rows, l.experts, l.k,
-                                  l.renormalize, l.ids, l.weights, s.plan));
+    int rc = x_ready && sixteen(l.router, l.n_in, size) ? launch_logits<T, true>(ctx, l, s.logits) : launch_logits<T, false>(ctx, l, s.logits);
+    if (rc != EP_OK) return rc;
+    // each block for itself where a warp has a row and few logits to look at
+    const Router router{l.rows <= OWN_ROWS && l.rows * l.k <= OWN_SLOTS && l.experts <= 256, s.logits, l.valid, (int)l.rows, l.experts,
+                        l.renormalize, l.ids, l.weights};
+    *kernels = 3;
+    if (!router.here) {
+        EP_CUDA(ctx, ep::launch_early(experts_choose, dim3(1), dim3(1024), 0, l.stream, s.logits, l.valid, (int)l.rows, l.experts, l.k,
+                                      l.renormalize, l.ids, l.weights, s.plan));
+        *kernels = 4;
+    }
     const bool vec = x_ready && sixteen(l.w1.w, l.n_in, w_size) && sixteen(l.w2.w, l.n_hidden, w_size);
-    if (l.w_type == EP_I8) return vec ? run_products<T, i8, true>(ctx, l, s) : run_products<T, i8, false>(ctx, l, s);
-    return vec ? run_products<T, T, true>(ctx, l, s) : run_products<T, T, false>(ctx, l, s);
+    if (l.w_type == EP_I8) return vec ? run_products<T, i8, true>(ctx, l, s, router) : run_products<T, i8, false>(ctx, l, s, router);
+    return vec ? run_products<T, T, true>(ctx, l, s, router) : run_products<T, T, false>(ctx, l, s, router);
 }
 
 bool experts_shape_ok(int64_t rows, int n_in, int n_hidden, int n_out, int experts, int k) {
@@ -500,10 +749,11 @@ int ep_experts(ep_ctx *ctx, const void *x, int64_t ldx, int32_t type, const void
                   experts, static_cast<cudaStream_t>(cuda_stream)};
     DeviceGuard guard(ctx->device);
     Timed tm(ctx, l.stream, EP_TIMER_EXPERTS);
-    const int rc = type == EP_F32    ? run_layer<float>(ctx, l, s)
-                   : type == EP_BF16 ? run_layer<__nv_bfloat16>(ctx, l, s)
-                                     : run_layer<__half>(ctx, l, s);
-    tm.end(rc == EP_OK ? 4 : 0);
+    int kernels = 0;
+    const int rc = type == EP_F32    ? run_layer<float>(ctx, l, s, &kernels)
+                   : type == EP_BF16 ? run_layer<__nv_bfloat16>(ctx, l, s, &kernels)
+                                     : run_layer<__half>(ctx, l, s, &kernels);
+    tm.end(rc == EP_OK ? kernels : 0);
     return rc;
 }
 
