@@ -392,51 +392,55 @@ __global__ void __launch_bounds__(1024) experts_choose(const float *logits, cons
 // The same by every block of the first product for itself, for a few rows (a launch less): ids, weights and the plan come to
 // shared memory, and from the first block to where the launches that follow look for them.
 constexpr int OWN_ROWS = 16, OWN_SLOTS = 64;
-struct OwnPlan {
+struct alignas(16) OwnPlan {
     int32_t ids[OWN_SLOTS];
+    int starts[OWN_SLOTS];   // where a group starts that a slot is the first of
     float weights[OWN_SLOTS];
     int sorted[OWN_SLOTS];
     Group groups[OWN_SLOTS];
     int n_groups;
-    bool starts[OWN_SLOTS];   // a group
 };
 __device__ void choose_here(const float *logits, const uint8_t *valid, int rows, int experts, int k, bool renormalize, OwnPlan &own, bool tell,
                             int32_t *ids, float *weights, const Plan &plan) {
     const int lane = threadIdx.x & 31, slots = rows * k, s = threadIdx.x;
+    if (s >= slots && s < OWN_SLOTS) own.ids[s] = -1;
     for (int r = threadIdx.x >> 5; r < rows; r += (int)(blockDim.x >> 5))
         choose(logits + r * experts, experts, k, !valid || valid[r], renormalize, lane, own.ids + r * k, own.weights + r * k);
     __syncthreads();
     // (in an order that all blocks agree on: they share out the groups by their numbers)
     const int e = s < slots ? own.ids[s] : -1;
     int before = 0, of_part = 0, earlier = 0, number = 0;   // slots of lower parts; slots of this part, and those of them before this one
-    if (s < slots) {
-        for (int q = 0; q < slots; ++q) {
-            const int o = own.ids[q];
-            before += o >= 0 && o < e;
-            of_part += o == e;
-            earlier += o == e && q < s;
+    if (s < OWN_SLOTS) {   // (slots past the last hold -1)
+#pragma unroll 4
+        for (int q = 0; q < OWN_SLOTS; q += 4) {
+            if (q >= slots) break;
+            const int4 o = *reinterpret_cast<const int4 *>(own.ids + q);
+            before += (o.x >= 0 && o.x < e) + (o.y >= 0 && o.y < e) + (o.z >= 0 && o.z < e) + (o.w >= 0 && o.w < e);
+            of_part += (o.x == e) + (o.y == e) + (o.z == e) + (o.w == e);
+            earlier += (o.x == e && q < s) + (o.y == e && q + 1 < s) + (o.z == e && q + 2 < s) + (o.w == e && q + 3 < s);
         }
-        own.starts[s] = e >= 0 && earlier % GROUP == 0;
-    }
-    __syncthreads();
-    if (s < slots) {
-        for (int q = 0; q < slots; ++q) number += own.starts[q] && (own.ids[q] < e || (own.ids[q] == e && q < s));
         const int at = e < 0 ? -1 : before + earlier;
-        if (e >= 0) {
-            own.sorted[at] = s;
-            if (own.starts[s]) own.groups[number] = Group{e, at, min(of_part - earlier, GROUP)};
-        }
-        if (tell) {
+        // a group starts at every eighth slot of a part; its number is that of the groups that start before it in the sorted list
+        own.starts[s] = e >= 0 && earlier % GROUP == 0 ? at : 1 << 30;
+        if (e >= 0) own.sorted[at] = s;
+        if (tell && s < slots) {
             plan.place[s] = at;
             ids[s] = e;
             weights[s] = own.weights[s];
         }
     }
-    if (s < 32) {
-        int n = 0;
-        for (int q = s; q < slots; q += 32) n += own.starts[q];
-        n = __reduce_add_sync(FULL, n);
-        if (s == 0) own.n_groups = n;
+    __syncthreads();
+    if (s < OWN_SLOTS) {
+        const int at = own.starts[s];
+        int all = 0;
+#pragma unroll 4
+        for (int q = 0; q < OWN_SLOTS; q += 4) {
+            const int4 o = *reinterpret_cast<const int4 *>(own.starts + q);
+            number += (o.x < at) + (o.y < at) + (o.z < at) + (o.w < at);
+            all += (o.x < 1 << 30) + (o.y < 1 << 30) + (o.z < 1 << 30) + (o.w < 1 << 30);
+        }
+        if (at < 1 << 30) own.groups[number] = Group{e, at, min(of_part - earlier, GROUP)};
+        if (s == 0) own.n_groups = all;
     }
     __syncthreads();
     if (tell && s < own.n_groups) plan.groups[s] = own.groups[s];
@@ -595,6 +599,223 @@ __global__ void __launch_bounds__(THREADS) experts_output(const float *hidden, W
     }
 }
 
+// ---------------------------------------------------------------------------------------------- products by matrix instructions
+//
+// Where there are enough rows of weights to keep every warp busy 16 at a time, a warp multiplies 16 of them with the (up to 8)
+// rows of a group by matrix instructions, 16 x 8 x 16 at a time: a number of weights then costs a third of the instructions, most
+// of them for making 8-bit integers 16-bit floats (which hold them exactly).  The order of the columns within a step is the lanes'
+// own: each takes 16 bytes of its rows of weights, and the same columns of its row of x.  Hidden values go to the second
+// product as the sum of two bf16 numbers (16 bits, beside outputs of 8 or 11 bits).
+template <typename M>
+__device__ __forceinline__ void multiply(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    if constexpr (std::is_same_v<M, __half>)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// 16 bytes of weights as pairs of M.
+template <typename M, typename W>
+__device__ __forceinline__ void as_pairs(const uint4 &v, uint32_t (&p)[4 * sizeof(M) / sizeof(W)]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if constexpr (!std::is_same_v<W, i8>)
+            p[q] = w[q];
+        else if constexpr (std::is_same_v<M, __half>) {
+            const uint32_t u = w[q] ^ 0x80808080u;   // 1024 and the byte, less 1024 + 128
+            const __half2 off = __half2half2(__ushort_as_half(0x6480));
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const uint32_t h = __byte_perm(u, 0x64646464u, i ? 0x4342 : 0x4140);
+                const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&h), off);
+                p[2 * q + i] = *reinterpret_cast<const uint32_t *>(&r);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {            // 128 and the low seven bits, less 128 or, of a negative number, 256
+                const uint32_t b = __byte_perm(w[q], 0u, i ? 0x4342 : 0x4140);
+                const uint32_t low = (b & 0x007f007fu) | 0x43004300u, off = (b & 0x00800080u) | 0x43004300u;
+                const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&low), *reinterpret_cast<const __nv_bfloat162 *>(&off));
+                p[2 * q + i] = *reinterpret_cast<const uint32_t *>(&r);
+            }
+        }
+    }
+}
+
+struct TensorWork {
+    const void *x;               // rows of x, or hidden values: high parts, and `low` further on low parts
+    int64_t ldx, low;
+    const void *w;               // [experts][rows][cols]
+    int rows, cols, k;
+    const float *scale;
+    const void *bias;
+    int bias_type, act;
+    int shares, per_share;       // of the columns
+    __nv_bfloat16 *hidden;       // out of the first product
+    float *y;                    // out of the second: [share][slots][rows]
+    int slots;
+};
+// The items of one product: group, 16 rows of weights, share of the columns.
+template <typename W>
+struct TensorItems {
+    const TensorWork &e;
+    const Group *groups;
+    int across;
+    struct Item {
+        Group g;
+        int row0, share, from, to;
+    };
+    __device__ __forceinline__ Item operator()(int64_t i) const {
+        const int share = (int)(i % e.shares), q = (int)(i / e.shares), from = share * e.per_share;
+        return Item{groups[q / across], q % across * 16, share, from, min(from + e.per_share, e.cols)};
+    }
+};
+constexpr int TENSOR_STAGES = 3, TENSOR_BLOCKS = 2;   // blocks to an SM: a step is a chain of dependent instructions
+constexpr size_t TENSOR_BYTES = (size_t)TENSOR_STAGES * 4 * THREADS * 16;
+
+// SECOND: from hidden values (two bf16 parts) to y; otherwise from x to hidden values.  M: what the matrix instructions take.
+template <bool SECOND, typename M, typename W>
+__global__ void __launch_bounds__(THREADS, TENSOR_BLOCKS) experts_tensor(const TensorWork e, Plan p, Router router, const void *next, int64_t next_bytes) {
+    constexpr int N = 16 / (int)sizeof(W), PAIRS = N / 2;
+    extern __shared__ uint4 ring[];   // [TENSOR_STAGES][4][THREADS]
+    __shared__ OwnPlan own;
+    const int lane = threadIdx.x & 31;
+    ep_wait_for_launch_before();
+    ep_let_next_launch_start();
+    const int *sorted = p.sorted;
+    const Group *groups = p.groups;
+    if (!SECOND && router.here) {
+        choose_here(router.logits, router.valid, router.rows, router.experts, e.k, router.renormalize, own, blockIdx.x == 0, router.ids,
+                    router.weights, p);
+        sorted = own.sorted;
+        groups = own.groups;
+    }
+    const int n_groups = !SECOND && router.here ? own.n_groups : *p.n_groups;
+    if (!SECOND && next_bytes && threadIdx.x < n_groups)
+        ask_l2(static_cast<const char *>(next) + groups[threadIdx.x].expert * next_bytes, next_bytes, blockIdx.x, gridDim.x);
+    const TensorItems<W> item_of{e, groups, (e.rows + 15) / 16};
+    const int64_t items = (int64_t)n_groups * item_of.across * e.shares, step = (int64_t)gridDim.x * WARPS;
+    const int64_t first = (int64_t)(threadIdx.x >> 5) * gridDim.x + blockIdx.x;
+    // rows of weights on their way, as in Stream: of rows lane / 4 and that + 8, two steps of 4 lanes x 16 bytes
+    uint4 *mine = ring + threadIdx.x;
+    int64_t ahead = first;
+    typename TensorItems<W>::Item f{};
+    int c_ahead = 0, to_stage = 0, stage = 0;
+    auto open = [&] {
+        if (ahead < items) {
+            f = item_of(ahead);
+            c_ahead = f.from;
+        }
+    };
+    auto fetch = [&] {
+        if (ahead < items) {
+            uint4 *to = mine + to_stage * 4 * THREADS;
+            const W *base = static_cast<const W *>(e.w) + (int64_t)f.g.expert * e.rows * e.cols;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int row = f.row0 + (lane >> 2) + 8 * (q & 1), col = c_ahead + (lane & 3) * N + (q >> 1) * 4 * N;
+                if (row < e.rows && col < f.to) copy_async<16>(to + q * THREADS, base + (int64_t)row * e.cols + col);
+            }
+            c_ahead += 8 * N;
+            if (c_ahead >= f.to) {
+                ahead += step;
+                open();
+            }
+        }
+        copies_end_group();
+        to_stage = to_stage + 1 == TENSOR_STAGES ? 0 : to_stage + 1;
+    };
+    open();
+    for (int s = 0; s < TENSOR_STAGES - 1; ++s) fetch();
+    for (int64_t i = first; i < items; i += step) {
+        const auto it = item_of(i);
+        const int n = lane >> 2;                     // this lane's row of x
+        const bool there = n < it.g.count;
+        const int place = it.g.first + (there ? n : 0);
+        const M *x = static_cast<const M *>(e.x) + (SECOND ? (int64_t)place * e.cols : (sorted[place] / e.k) * e.ldx);
+        float d[2][4] = {};
+#pragma unroll 1
+        for (int c0 = it.from; c0 < it.to; c0 += 8 * N) {
+            fetch();
+            copies_wait<TENSOR_STAGES - 1>();
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int col = c0 + (lane & 3) * N + h * 4 * N;
+                const bool in = col < it.to;
+                uint4 v[2];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    v[r] = mine[(stage * 4 + 2 * h + r) * THREADS];
+                    // (a row past the last: whatever was there before, and its sums go nowhere)
+                    if (!in) v[r] = make_uint4(0, 0, 0, 0);
+                }
+                uint32_t a[2][PAIRS];
+                as_pairs<M, W>(v[0], a[0]);
+                as_pairs<M, W>(v[1], a[1]);
+#pragma unroll
+                for (int part = 0; part < (SECOND ? 2 : 1); ++part) {
+                    uint32_t b[PAIRS];
+#pragma unroll
+                    for (int q = 0; q < PAIRS / 4; ++q) {
+                        const uint4 u = there && in ? reinterpret_cast<const uint4 *>(x + part * e.low + col)[q] : make_uint4(0, 0, 0, 0);
+                        b[4 * q] = u.x, b[4 * q + 1] = u.y, b[4 * q + 2] = u.z, b[4 * q + 3] = u.w;
+                    }
+#pragma unroll
+                    for (int q = 0; q < PAIRS; q += 2) multiply<M>(d[q / 2 & 1], a[0][q], a[1][q], a[0][q + 1], a[1][q + 1], b[q], b[q + 1]);
+                }
+            }
+            stage = stage + 1 == TENSOR_STAGES ? 0 : stage + 1;
+        }
+        // this lane's sums: rows of weights lane / 4 and that + 8, rows of x 2 (lane % 4) and the next
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int row = it.row0 + (lane >> 2) + 8 * (q >> 1), r = 2 * (lane & 3) + (q & 1);
+            if (row >= e.rows || r >= it.g.count) continue;
+            float v[1] = {d[0][q] + d[1][q]};
+            if constexpr (SECOND)
+                e.y[((int64_t)it.share * e.slots + it.g.first + r) * e.rows + row] = v[0];
+            else {
+                const int64_t at = (int64_t)it.g.expert * e.rows + row;
+                v[0] = fmaf(v[0], e.scale ? e.scale[at] : 1.f, e.bias ? load_param(e.bias, e.bias_type, at) : 0.f);
+                activate(v, e.act);
+                const __nv_bfloat16 high = __float2bfloat16_rn(v[0]);
+                __nv_bfloat16 *to = e.hidden + (int64_t)(it.g.first + r) * e.rows + row;
+                to[0] = high;
+                // (an infinity or a NaN has no rest)
+                to[e.low] = __float2bfloat16_rn(fabsf(v[0]) < 3e38f ? v[0] - __bfloat162float(high) : 0.f);
+            }
+        }
+    }
+    copies_wait<0>();
+}
+
+// out = sum of the slots' outputs by their weights + residual.
+template <typename T>
+__global__ void __launch_bounds__(256) experts_sum(const float *y, int shares, int rows, int n_out, int k, Plan p, const int32_t *ids,
+                                                   const float *weights, const float *scale, const void *bias, int bias_type,
+                                                   const T *residual, int64_t ldr, T *out) {
+    ep_wait_for_launch_before();
+    const int i = blockIdx.x * 256 + threadIdx.x, row = i / n_out, c = i - row * n_out, slots = rows * k;
+    if (row >= rows) return;
+    float sum = 0.f;
+    for (int s = 0; s < k; ++s) {
+        const int slot = row * k + s, at = p.place[slot];
+        if (at < 0) continue;
+        float v = 0.f;
+        for (int h = 0; h < shares; ++h) v += y[((int64_t)h * slots + at) * n_out + c];
+        const int64_t param = (int64_t)ids[slot] * n_out + c;
+        if (scale) v *= scale[param];
+        if (bias) v += load_param(bias, bias_type, param);
+        sum = fmaf(weights[slot], v, sum);
+    }
+    if (residual) sum += to_f32(residual[row * ldr + c]);
+    out[(int64_t)row * n_out + c] = from_f32<T>(sum);
+}
+
 // ---------------------------------------------------------------------------------------------- host side
 struct Layer {
     const void *x;
@@ -617,16 +838,18 @@ struct Layer {
     cudaStream_t stream;
 };
 struct Space {
-    float *logits, *hidden;
+    float *logits, *hidden, *y;
     Plan plan;
     size_t bytes;
 };
-Space space(int64_t rows, int n_hidden, int experts, int k, void *base) {
+constexpr int MAX_SHARES = 4;   // of the hidden values, between warps of the second product by matrix instructions
+Space space(int64_t rows, int n_hidden, int n_out, int experts, int k, void *base) {
     ep::Arena a(base);
     Space s{};
     const size_t slots = rows * k;
     s.logits = a.take<float>(rows * experts);
     s.hidden = a.take<float>(slots * n_hidden);
+    s.y = a.take<float>(slots * n_out * MAX_SHARES);
     s.plan.n_groups = a.take<int>(1);
     s.plan.groups = a.take<Group>(slots);
     s.plan.sorted = a.take<int>(slots);
@@ -664,6 +887,61 @@ int run_products(ep_ctx *ctx, const Layer &l, const Space &s, const Router &rout
     return EP_OK;
 }
 
+// Both products by matrix instructions; M of the first as x, of the second bf16.
+template <typename T, typename W>
+int run_tensor(ep_ctx *ctx, const Layer &l, const Space &s, const Router &router) {
+    const int slots = (int)l.rows * l.k;
+    const int64_t w2_bytes = (int64_t)l.n_out * l.n_hidden * sizeof(W);
+    const bool ask = w2_bytes % 16 == 0 && w2_bytes * std::min(slots, l.experts) <= L2_SHARE;
+    TensorWork a{};
+    a.x = l.x;
+    a.ldx = l.ldx;
+    a.low = (int64_t)slots * l.n_hidden;
+    a.w = l.w1.w;
+    a.rows = l.n_hidden;
+    a.cols = l.n_in;
+    a.k = l.k;
+    a.scale = l.w1.scale;
+    a.bias = l.w1.bias;
+    a.bias_type = l.w1.bias_type;
+    a.act = l.act;
+    a.shares = 1;
+    a.per_share = l.n_in;
+    a.hidden = reinterpret_cast<__nv_bfloat16 *>(s.hidden);
+    a.slots = slots;
+    auto first = experts_tensor<false, T, W>;
+    EP_CUDA(ctx, cudaFuncSetAttribute(first, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TENSOR_BYTES));
+    EP_CUDA(ctx, ep::launch_early(first, dim3(ctx->sm_count * TENSOR_BLOCKS), dim3(THREADS), TENSOR_BYTES, l.stream, a, s.plan, router, l.w2.w,
+                                  ask ? w2_bytes : (int64_t)0));
+    TensorWork b{};
+    b.x = s.hidden;
+    b.low = a.low;
+    b.w = l.w2.w;
+    b.rows = l.n_out;
+    b.cols = l.n_hidden;
+    b.k = l.k;
+    constexpr int STEP = 8 * 16 / (int)sizeof(W);
+    b.shares = (int)std::max<int64_t>(1, std::min<int64_t>(MAX_SHARES, ep::ceil_div(l.n_hidden, 4 * STEP)));
+    b.per_share = (int)ep::ceil_div(ep::ceil_div(l.n_hidden, b.shares), STEP) * STEP;
+    b.shares = (int)ep::ceil_div(l.n_hidden, b.per_share);
+    b.y = s.y;
+    b.slots = slots;
+    auto second = experts_tensor<true, __nv_bfloat16, W>;
+    EP_CUDA(ctx, cudaFuncSetAttribute(second, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TENSOR_BYTES));
+    EP_CUDA(ctx, ep::launch_early(second, dim3(ctx->sm_count * TENSOR_BLOCKS), dim3(THREADS), TENSOR_BYTES, l.stream, b, s.plan, router, (const void *)nullptr,
+                                  (int64_t)0));
+    EP_CUDA(ctx, ep::launch_early(experts_sum<T>, dim3((unsigned)ep::ceil_div(l.rows * l.n_out, 256)), dim3(256), 0, l.stream, s.y, b.shares,
+                                  (int)l.rows, l.n_out, l.k, s.plan, l.ids, l.weights, l.w2.scale, l.w2.bias, l.w2.bias_type,
+                                  (const T *)l.residual, l.ldr, (T *)l.out));
+    return EP_OK;
+}
+// Whether there is a tile of 16 rows of weights for every warp of the first product, of the experts that `rows` rows are likely to choose.
+bool enough_for_tensor(const ep_ctx *ctx, const Layer &l) {
+    double missed = 1.0;
+    for (int r = 0; r < (int)l.rows; ++r) missed *= 1.0 - (double)l.k / l.experts;
+    return l.experts * (1.0 - missed) * (l.n_hidden / 16) >= ctx->sm_count * TENSOR_BLOCKS * WARPS;
+}
+
 bool sixteen(const void *p, int64_t ld, int size) { return ep::aligned(p, 16) && ld * size % 16 == 0; }
 
 template <typename T, bool VEC>
@@ -691,6 +969,18 @@ int run_layer(ep_ctx *ctx, const Layer &l, const Space &s, int *kernels) {
         *kernels = 4;
     }
     const bool vec = x_ready && sixteen(l.w1.w, l.n_in, w_size) && sixteen(l.w2.w, l.n_hidden, w_size);
+    if constexpr (!std::is_same_v<T, float>) {
+        if (vec && l.n_hidden % 8 == 0 && enough_for_tensor(ctx, l)) {
+            if (l.w_type == EP_I8) {
+                ++*kernels;
+                return run_tensor<T, i8>(ctx, l, s, router);
+            }
+            if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+                ++*kernels;
+                return run_tensor<T, T>(ctx, l, s, router);
+            }
+        }
+    }
     if (l.w_type == EP_I8) return vec ? run_products<T, i8, true>(ctx, l, s, router) : run_products<T, i8, false>(ctx, l, s, router);
     return vec ? run_products<T, T, true>(ctx, l, s, router) : run_products<T, T, false>(ctx, l, s, router);
 }
@@ -714,7 +1004,7 @@ extern "C" {
 size_t ep_experts_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t n_in, int32_t n_hidden, int32_t n_out, int32_t experts,
                                   int32_t k) {
     if (!ctx || !experts_shape_ok(rows, n_in, n_hidden, n_out, experts, k)) return 0;
-    return space(rows, n_hidden, experts, k, nullptr).bytes;
+    return space(rows, n_hidden, n_out, experts, k, nullptr).bytes;
 }
 
 int ep_experts(ep_ctx *ctx, const void *x, int64_t ldx, int32_t type, const void *router, const void *router_bias,
@@ -741,7 +1031,7 @@ int ep_experts(ep_ctx *ctx, const void *x, int64_t ldx, int32_t type, const void
         !element_aligned(b2, b2 ? bias_type : EP_I8) || !aligned(w1_scale, 4) || !aligned(w2_scale, 4) || !aligned(ids, 4) ||
         !aligned(weights, 4))
         return fail(ctx, EP_ERR_INVALID_ARG, "null or misaligned pointer");
-    const Space s = space(rows, n_hidden, experts, k, workspace);
+    const Space s = space(rows, n_hidden, n_out, experts, k, workspace);
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < s.bytes)
         return fail(ctx, EP_ERR_WORKSPACE, "workspace too small or misaligned");
     const Layer l{x,   ldx, type, router, router_bias, router_bias_type, valid, k, renormalize != 0, Weights{w1, w1_scale, b1, bias_type},

@@ -4,6 +4,7 @@ Bounds.  A dot product of n numbers, summed in fp32 by 32 lanes that take at lea
 the sum of its terms' sizes; 8-bit weights add one rounding for their scale.  Router logits are off by that (e), weights by 2 e + 2^-19 of
 themselves (renormalised: twice that), hidden values by their product's error, by 2^-20 of what the activation adds and by its slope (at
 most 1.13), outputs by what the errors of hidden values and weights make in them; one rounding ends it.
+Rows of 16 bits may hold their hidden values as two bf16 numbers, 2^-17 of themselves off.
 """
 import math
 
@@ -69,6 +70,8 @@ def check(x, router, w1, w2, s1, s2, k=1, router_bias=None, b1=None, b2=None, ac
             dz = S * (dot_error(x.shape[1]) + 2.0 ** -24) + 2.0 ** -23 * z.abs()
             h = ref.act(z, act)
             dh = 1.13 * dz + 2.0 ** -20 * (h.abs() + z.abs() * 2.0 ** -4)
+            if dt != F32:
+                dh = dh + 2.0 ** -17 * h.abs()
             y, dy = b @ h, b.abs() @ dh + (b.abs() @ h.abs()) * (dot_error(w1.shape[1]) + 2.0 ** -24)
             y = y if b2 is None else y + b2[p].double()
             total[row] += w[row, i] * y
@@ -81,7 +84,8 @@ def check(x, router, w1, w2, s1, s2, k=1, router_bias=None, b1=None, b2=None, ac
 
 
 SHAPES = [(1, 64, 128, 64, 8, 2), (1, 1024, 4096, 1024, 64, 2), (1, 1, 1, 1, 1, 1), (2, 33, 65, 17, 3, 3), (3, 500, 77, 130, 5, 1), (7, 333, 1029, 77, 5, 3),
-          (16, 128, 256, 512, 32, 2), (9, 72, 40, 24, 2, 1), (33, 48, 96, 1000, 7, 4), (64, 64, 64, 64, 300, 8), (64, 16, 32, 8, 4096, 32), (40, 96, 2000, 33, 40, 32)]
+          (16, 128, 256, 512, 32, 2), (9, 72, 40, 24, 2, 1), (33, 48, 96, 1000, 7, 4), (64, 64, 64, 64, 300, 8), (64, 16, 32, 8, 4096, 32), (40, 96, 2000, 33, 40, 32),
+          (40, 64, 1528, 72, 40, 4), (64, 48, 4096, 24, 12, 2), (9, 32, 2064, 40, 40, 6), (20, 112, 1936, 130, 60, 3)]
 
 
 @pytest.mark.parametrize("rows,n_in,hidden,n_out,parts,k", SHAPES)
