@@ -165,42 +165,47 @@ constexpr int STREAM_ROWS = 4, STREAM_STAGES = 4;
 constexpr size_t STREAM_BYTES = (size_t)STREAM_STAGES * STREAM_ROWS * THREADS * 16;
 template <typename W, typename Find>
 struct Stream {
-    static constexpr int N = 16 / (int)sizeof(W);
-    uint4 *mine;
+    static constexpr int N = 16 / (int)sizeof(W), ROW = THREADS * 16, STAGE = STREAM_ROWS * ROW;   // bytes between rows, between stages
     const Find &find;      // the rows of an item
     const int64_t items, step;
+    const char *const mine;
     int64_t item;
-    Rows<W> rows;
-    int c, to_stage, stage;
+    const char *from;      // this lane's next chunk of the first row
+    int64_t ld;            // bytes from row to row
+    int count, left;       // rows; columns that are still to come, of all lanes
+    int to_at, at;         // stages, in bytes
     __device__ __forceinline__ Stream(void *room, const Find &f, int64_t first, int64_t all, int64_t by)
-        : mine(static_cast<uint4 *>(room) + threadIdx.x), find(f), items(all), step(by), item(first), to_stage(0), stage(0) {
+        : find(f), items(all), step(by), mine(static_cast<const char *>(room) + threadIdx.x * 16), item(first), from(nullptr), ld(0), count(0),
+          left(0), to_at(0), at(0) {
         open();
         for (int s = 0; s < STREAM_STAGES - 1; ++s) fetch();
     }
     __device__ __forceinline__ void open() {
         if (item < items) {
-            rows = find(item);
-            c = rows.from;
+            const Rows<W> r = find(item);
+            from = reinterpret_cast<const char *>(r.first + r.from) + (threadIdx.x & 31) * 16;
+            ld = r.ld * (int64_t)sizeof(W);
+            count = r.count;
+            left = r.to - r.from;
         }
     }
     __device__ __forceinline__ void fetch() {
-        if (item < items) {
-            const int col = c + (threadIdx.x & 31) * N;
-            if (col < rows.to) {
-                uint4 *to = mine + to_stage * STREAM_ROWS * THREADS;
-                const W *from = rows.first + col;
+        if (left > 0) {
+            if ((int)(threadIdx.x & 31) * N < left) {
+                char *to = const_cast<char *>(mine) + to_at;
 #pragma unroll
                 for (int j = 0; j < STREAM_ROWS; ++j)
-                    if (j < rows.count) copy_async<16>(to + j * THREADS, from + j * rows.ld);
+                    if (j < count) copy_async<16>(to + j * ROW, from + j * ld);
             }
-            c += 32 * N;
-            if (c >= rows.to) {
+            from += 512;
+            left -= 32 * N;
+            if (left <= 0) {
                 item += step;
                 open();
             }
         }
         copies_end_group();
-        to_stage = to_stage + 1 == STREAM_STAGES ? 0 : to_stage + 1;
+        to_at = to_at + STAGE == STREAM_STAGES * STAGE ? 0 : to_at + STAGE;
     }
     // w_j . x_r of the item whose turn it is (its columns are from..to).
     template <typename X, int R>
@@ -220,7 +225,7 @@ struct Stream {
 #pragma unroll
             for (int j = 0; j < STREAM_ROWS; ++j) {
                 // (rows past the last are whatever was there before: their sums go nowhere)
-                const uint4 v = mine[(stage * STREAM_ROWS + j) * THREADS];
+                const uint4 v = *reinterpret_cast<const uint4 *>(mine + at + j * ROW);
                 *reinterpret_cast<uint4 *>(a[j].e) = there ? v : make_uint4(0, 0, 0, 0);
             }
             // a few columns at a time: what is converted has to fit the registers beside the sums
@@ -245,7 +250,7 @@ struct Stream {
                     }
                 }
             }
-            stage = stage + 1 == STREAM_STAGES ? 0 : stage + 1;
+            at = at + STAGE == STREAM_STAGES * STAGE ? 0 : at + STAGE;
         }
     }
     template <typename X, int R>
@@ -274,31 +279,38 @@ __global__ void __launch_bounds__(128) experts_logits(const T *x, int64_t ldx, c
     if (lane % (32 / R) == 0 && row0 + r < rows) logits[(row0 + r) * experts + e] = v + add;
 }
 
-// A row's k best parts and their weights (as ep_route), by one warp.
-__device__ void choose(const float *l, int experts, int k, bool part, bool renormalize, int lane, int32_t *ids, float *weights) {
+// A row's k best parts and their weights (as ep_route), by one warp.  (The first 128 logits are kept in registers.)
+__device__ void choose(const float *logits, int experts, int k, bool part, bool renormalize, int lane, int32_t *ids, float *weights) {
+    constexpr int KEPT = 4;
+    float kept[KEPT];
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) kept[i] = part && 32 * i + lane < experts ? logits[32 * i + lane] : -INFINITY;
+    auto each = [&](auto f) {
+        if (!part) return;
+#pragma unroll
+        for (int i = 0; i < KEPT; ++i)
+            if (32 * i < experts) f(kept[i], 32 * i + lane);
+        for (int e = 32 * KEPT + lane; e < experts; e += 32) f(logits[e], e);
+    };
     float top = -INFINITY;
-    if (part)
-        for (int e = lane; e < experts; e += 32) top = fmaxf(top, l[e]);
+    each([&](float v, int) { top = fmaxf(top, v); });
 #pragma unroll
     for (int o = 16; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
     part = part && top > -INFINITY;
     float s = 0.f;
-    if (part)
-        for (int e = lane; e < experts; e += 32) s += exp_fast(l[e] - top);
+    each([&](float v, int) { s += exp_fast(v - top); });
     s = over_lanes(s);
     float last = INFINITY, chosen = 0.f, mine = 0.f;
     int last_e = -1, mine_e = -1;
     for (int i = 0; i < k; ++i) {   // the best that comes after the one before: lower, or as high with a higher number
         float v = -INFINITY;
         int at = MAX_EXPERTS;
-        if (part)
-            for (int e = lane; e < experts; e += 32) {
-                const float u = l[e];
-                if (u > v && (u < last || (u == last && e > last_e))) {
-                    v = u;
-                    at = e;
-                }
+        each([&](float u, int e) {
+            if (u > v && (u < last || (u == last && e > last_e))) {
+                v = u;
+                at = e;
             }
+        });
 #pragma unroll
         for (int o = 16; o >= 1; o >>= 1) {
             const float ov = __shfl_xor_sync(FULL, v, o);
@@ -389,62 +401,76 @@ __global__ void __launch_bounds__(1024) experts_choose(const float *logits, cons
     }
 }
 
-// The same by every block of the first product for itself, for a few rows (a launch less): ids, weights and the plan come to
-// shared memory, and from the first block to where the launches that follow look for them.
-constexpr int OWN_ROWS = 16, OWN_SLOTS = 64;
-struct alignas(16) OwnPlan {
-    int32_t ids[OWN_SLOTS];
-    int starts[OWN_SLOTS];   // where a group starts that a slot is the first of
-    float weights[OWN_SLOTS];
-    int sorted[OWN_SLOTS];
-    Group groups[OWN_SLOTS];
-    int n_groups;
+// The same for up to 64 slots, each compared with the others.
+constexpr int FEW_SLOTS = 64;
+struct alignas(16) FewSlots {
+    int32_t ids[FEW_SLOTS];
+    int starts[FEW_SLOTS];   // where a group starts that a slot is the first of
 };
-__device__ void choose_here(const float *logits, const uint8_t *valid, int rows, int experts, int k, bool renormalize, OwnPlan &own, bool tell,
-                            int32_t *ids, float *weights, const Plan &plan) {
-    const int lane = threadIdx.x & 31, slots = rows * k, s = threadIdx.x;
-    if (s >= slots && s < OWN_SLOTS) own.ids[s] = -1;
-    for (int r = threadIdx.x >> 5; r < rows; r += (int)(blockDim.x >> 5))
-        choose(logits + r * experts, experts, k, !valid || valid[r], renormalize, lane, own.ids + r * k, own.weights + r * k);
-    __syncthreads();
-    // (in an order that all blocks agree on: they share out the groups by their numbers)
-    const int e = s < slots ? own.ids[s] : -1;
-    int before = 0, of_part = 0, earlier = 0, number = 0;   // slots of lower parts; slots of this part, and those of them before this one
-    if (s < OWN_SLOTS) {   // (slots past the last hold -1)
+__device__ void plan_few(FewSlots &few, int slots, const Plan &plan) {
+    const int s = threadIdx.x, e = s < FEW_SLOTS ? few.ids[s] : -1;   // (slots past the last hold -1)
+    int before = 0, of_part = 0, earlier = 0, at = -1;                // slots of lower parts; slots of this part, and those of them before this one
+    if (s < FEW_SLOTS) {
 #pragma unroll 4
-        for (int q = 0; q < OWN_SLOTS; q += 4) {
+        for (int q = 0; q < FEW_SLOTS; q += 4) {
             if (q >= slots) break;
-            const int4 o = *reinterpret_cast<const int4 *>(own.ids + q);
+            const int4 o = *reinterpret_cast<const int4 *>(few.ids + q);
             before += (o.x >= 0 && o.x < e) + (o.y >= 0 && o.y < e) + (o.z >= 0 && o.z < e) + (o.w >= 0 && o.w < e);
             of_part += (o.x == e) + (o.y == e) + (o.z == e) + (o.w == e);
             earlier += (o.x == e && q < s) + (o.y == e && q + 1 < s) + (o.z == e && q + 2 < s) + (o.w == e && q + 3 < s);
         }
-        const int at = e < 0 ? -1 : before + earlier;
+        at = e < 0 ? -1 : before + earlier;
         // a group starts at every eighth slot of a part; its number is that of the groups that start before it in the sorted list
-        own.starts[s] = e >= 0 && earlier % GROUP == 0 ? at : 1 << 30;
-        if (e >= 0) own.sorted[at] = s;
-        if (tell && s < slots) {
-            plan.place[s] = at;
-            ids[s] = e;
-            weights[s] = own.weights[s];
-        }
+        few.starts[s] = e >= 0 && earlier % GROUP == 0 ? at : 1 << 30;
+        if (e >= 0) plan.sorted[at] = s;
+        if (s < slots) plan.place[s] = at;
     }
     __syncthreads();
-    if (s < OWN_SLOTS) {
-        const int at = own.starts[s];
-        int all = 0;
+    if (s < FEW_SLOTS) {
+        const int mine = few.starts[s];
+        int number = 0, all = 0;
 #pragma unroll 4
-        for (int q = 0; q < OWN_SLOTS; q += 4) {
-            const int4 o = *reinterpret_cast<const int4 *>(own.starts + q);
-            number += (o.x < at) + (o.y < at) + (o.z < at) + (o.w < at);
+        for (int q = 0; q < FEW_SLOTS; q += 4) {
+            const int4 o = *reinterpret_cast<const int4 *>(few.starts + q);
+            number += (o.x < mine) + (o.y < mine) + (o.z < mine) + (o.w < mine);
             all += (o.x < 1 << 30) + (o.y < 1 << 30) + (o.z < 1 << 30) + (o.w < 1 << 30);
         }
-        if (at < 1 << 30) own.groups[number] = Group{e, at, min(of_part - earlier, GROUP)};
-        if (s == 0) own.n_groups = all;
+        if (mine < 1 << 30) plan.groups[number] = Group{e, at, min(of_part - earlier, GROUP)};
+        if (s == 0) *plan.n_groups = all;
+    }
+}
+
+// All of the router in one launch, for a few rows: the blocks of a cluster share out the dot products, then the first one chooses
+// and plans.
+constexpr int ROUTER_BLOCKS = 8, ROUTER_JOBS = 4 * ROUTER_BLOCKS * WARPS;   // (a warp's dot products, four one after another at most)
+template <typename T, bool VEC, int R>
+__global__ void __launch_bounds__(THREADS) experts_router(const T *x, int64_t ldx, const T *router, const void *bias, int bias_type, int rows,
+                                                          int n_in, int experts, float *logits, const uint8_t *valid, int k, bool renormalize,
+                                                          int32_t *ids, float *weights, Plan plan) {
+    __shared__ FewSlots few;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, across = (rows + R - 1) / R;
+    ep_let_next_launch_start();
+    for (int job = warp * ROUTER_BLOCKS + blockIdx.x; job < experts * across; job += ROUTER_BLOCKS * WARPS) {
+        const int e = job / across, row0 = (job - e * across) * R;
+        const T *w[1] = {router + (int64_t)e * n_in};
+        const T *xs[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) xs[r] = x + min(row0 + r, rows - 1) * ldx;
+        const float v = dots<T, T, VEC, 1, R>(w, xs, 0, n_in, n_in, lane);
+        const int r = lane / (32 / R);
+        if (lane % (32 / R) == 0 && row0 + r < rows) logits[(row0 + r) * experts + e] = v + (bias ? load_param(bias, bias_type, e) : 0.f);
+    }
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (blockIdx.x != 0) return;
+    const int slots = rows * k;
+    if (threadIdx.x < FEW_SLOTS) few.ids[threadIdx.x] = -1;
+    __syncthreads();
+    for (int r = warp; r < rows; r += WARPS) {
+        choose(logits + r * experts, experts, k, !valid || valid[r], renormalize, lane, ids + r * k, weights + r * k);
+        if (lane < k) few.ids[r * k + lane] = ids[r * k + lane];   // (written by this lane)
     }
     __syncthreads();
-    if (tell && s < own.n_groups) plan.groups[s] = own.groups[s];
-    if (tell && s == 0) *plan.n_groups = own.n_groups;
+    plan_few(few, slots, plan);
 }
 
 // ---------------------------------------------------------------------------------------------- products
@@ -474,15 +500,6 @@ __device__ __forceinline__ void hidden_of(const T *x, int64_t ldx, const Weights
         hidden[(int64_t)(g.first + r) * n_hidden + j] = v[0];
     }
 }
-struct Router {   // of a layer whose blocks choose for themselves
-    bool here;
-    const float *logits;
-    const uint8_t *valid;
-    int rows, experts;
-    bool renormalize;
-    int32_t *ids;
-    float *weights;
-};
 // Asks for bytes [from, to) of [0, all) of the L2 (in whole 16 bytes).
 __device__ __forceinline__ void ask_l2(const char *base, int64_t all, int part, int parts) {
     const int64_t from = all * part / parts & ~int64_t(15), to = all * (part + 1) / parts & ~int64_t(15);
@@ -490,20 +507,13 @@ __device__ __forceinline__ void ask_l2(const char *base, int64_t all, int part, 
 }
 template <typename T, typename W, bool VEC>
 __global__ void __launch_bounds__(THREADS) experts_hidden(const T *x, int64_t ldx, Weights w1, int n_in, int n_hidden, int act, int k, Plan p,
-                                                          Router router, const void *w2, int64_t w2_bytes, float *hidden) {
-    __shared__ OwnPlan own;
+                                                          const void *w2, int64_t w2_bytes, float *hidden) {
     const int lane = threadIdx.x & 31;
     ep_wait_for_launch_before();
     ep_let_next_launch_start();
     const int *sorted = p.sorted;
     const Group *groups = p.groups;
-    if (router.here) {
-        choose_here(router.logits, router.valid, router.rows, router.experts, k, router.renormalize, own, blockIdx.x == 0, router.ids,
-                    router.weights, p);
-        sorted = own.sorted;
-        groups = own.groups;
-    }
-    const int n_groups = router.here ? own.n_groups : *p.n_groups;
+    const int n_groups = *p.n_groups;
     // While this product waits for its own weights, those of the next one come to the L2, where they fit it.
     if (w2_bytes && threadIdx.x < n_groups)
         ask_l2(static_cast<const char *>(w2) + groups[threadIdx.x].expert * w2_bytes, w2_bytes, blockIdx.x, gridDim.x);
@@ -674,60 +684,64 @@ struct TensorItems {
         return Item{groups[q / across], q % across * 16, share, from, min(from + e.per_share, e.cols)};
     }
 };
-constexpr int TENSOR_STAGES = 3, TENSOR_BLOCKS = 2;   // blocks to an SM: a step is a chain of dependent instructions
+constexpr int TENSOR_STAGES = 4;   // (two blocks to an SM with three stages each: 90 us where this takes 80)
 constexpr size_t TENSOR_BYTES = (size_t)TENSOR_STAGES * 4 * THREADS * 16;
 
 // SECOND: from hidden values (two bf16 parts) to y; otherwise from x to hidden values.  M: what the matrix instructions take.
 template <bool SECOND, typename M, typename W>
-__global__ void __launch_bounds__(THREADS, TENSOR_BLOCKS) experts_tensor(const TensorWork e, Plan p, Router router, const void *next, int64_t next_bytes) {
+__global__ void __launch_bounds__(THREADS) experts_tensor(const TensorWork e, Plan p, const void *next, int64_t next_bytes) {
     constexpr int N = 16 / (int)sizeof(W), PAIRS = N / 2;
     extern __shared__ uint4 ring[];   // [TENSOR_STAGES][4][THREADS]
-    __shared__ OwnPlan own;
     const int lane = threadIdx.x & 31;
     ep_wait_for_launch_before();
     ep_let_next_launch_start();
     const int *sorted = p.sorted;
     const Group *groups = p.groups;
-    if (!SECOND && router.here) {
-        choose_here(router.logits, router.valid, router.rows, router.experts, e.k, router.renormalize, own, blockIdx.x == 0, router.ids,
-                    router.weights, p);
-        sorted = own.sorted;
-        groups = own.groups;
-    }
-    const int n_groups = !SECOND && router.here ? own.n_groups : *p.n_groups;
+    const int n_groups = *p.n_groups;
     if (!SECOND && next_bytes && threadIdx.x < n_groups)
         ask_l2(static_cast<const char *>(next) + groups[threadIdx.x].expert * next_bytes, next_bytes, blockIdx.x, gridDim.x);
     const TensorItems<W> item_of{e, groups, (e.rows + 15) / 16};
     const int64_t items = (int64_t)n_groups * item_of.across * e.shares, step = (int64_t)gridDim.x * WARPS;
     const int64_t first = (int64_t)(threadIdx.x >> 5) * gridDim.x + blockIdx.x;
     // rows of weights on their way, as in Stream: of rows lane / 4 and that + 8, two steps of 4 lanes x 16 bytes
-    uint4 *mine = ring + threadIdx.x;
+    constexpr int PIECE = THREADS * 16, STAGE = 4 * PIECE;
+    char *const mine = reinterpret_cast<char *>(ring) + threadIdx.x * 16;
     int64_t ahead = first;
-    typename TensorItems<W>::Item f{};
-    int c_ahead = 0, to_stage = 0, stage = 0;
+    const char *from[2] = {};   // this lane's next chunk of either row
+    int left = 0, left_here[2] = {};   // columns still to come: of all lanes, and of either row from this lane's chunk on
+    int to_at = 0, at = 0;      // stages, in bytes
     auto open = [&] {
         if (ahead < items) {
-            f = item_of(ahead);
-            c_ahead = f.from;
+            const auto f = item_of(ahead);
+            left = f.to - f.from;
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int row = f.row0 + (lane >> 2) + 8 * r;
+                from[r] = reinterpret_cast<const char *>(static_cast<const W *>(e.w) + ((int64_t)f.g.expert * e.rows + row) * e.cols + f.from) +
+                          (lane & 3) * 16;
+                left_here[r] = row < e.rows ? left - (lane & 3) * N : 0;
+            }
         }
     };
     auto fetch = [&] {
-        if (ahead < items) {
-            uint4 *to = mine + to_stage * 4 * THREADS;
-            const W *base = static_cast<const W *>(e.w) + (int64_t)f.g.expert * e.rows * e.cols;
+        if (left > 0) {
+            char *to = mine + to_at;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int row = f.row0 + (lane >> 2) + 8 * (q & 1), col = c_ahead + (lane & 3) * N + (q >> 1) * 4 * N;
-                if (row < e.rows && col < f.to) copy_async<16>(to + q * THREADS, base + (int64_t)row * e.cols + col);
+            for (int q = 0; q < 4; ++q)
+                if (left_here[q & 1] > (q >> 1) * 4 * N) copy_async<16>(to + q * PIECE, from[q & 1] + (q >> 1) * 64);
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                from[r] += 128;
+                left_here[r] -= 8 * N;
             }
-            c_ahead += 8 * N;
-            if (c_ahead >= f.to) {
+            left -= 8 * N;
+            if (left <= 0) {
                 ahead += step;
                 open();
             }
         }
         copies_end_group();
-        to_stage = to_stage + 1 == TENSOR_STAGES ? 0 : to_stage + 1;
+        to_at = to_at + STAGE == TENSOR_STAGES * STAGE ? 0 : to_at + STAGE;
     };
     open();
     for (int s = 0; s < TENSOR_STAGES - 1; ++s) fetch();
@@ -749,7 +763,7 @@ __global__ void __launch_bounds__(THREADS, TENSOR_BLOCKS) experts_tensor(const T
                 uint4 v[2];
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    v[r] = mine[(stage * 4 + 2 * h + r) * THREADS];
+                    v[r] = *reinterpret_cast<const uint4 *>(mine + at + (2 * h + r) * PIECE);
                     // (a row past the last: whatever was there before, and its sums go nowhere)
                     if (!in) v[r] = make_uint4(0, 0, 0, 0);
                 }
@@ -768,7 +782,7 @@ __global__ void __launch_bounds__(THREADS, TENSOR_BLOCKS) experts_tensor(const T
                     for (int q = 0; q < PAIRS; q += 2) multiply<M>(d[q / 2 & 1], a[0][q], a[1][q], a[0][q + 1], a[1][q + 1], b[q], b[q + 1]);
                 }
             }
-            stage = stage + 1 == TENSOR_STAGES ? 0 : stage + 1;
+            at = at + STAGE == TENSOR_STAGES * STAGE ? 0 : at + STAGE;
         }
         // this lane's sums: rows of weights lane / 4 and that + 8, rows of x 2 (lane % 4) and the next
 #pragma unroll
@@ -861,7 +875,7 @@ Space space(int64_t rows, int n_hidden, int n_out, int experts, int k, void *bas
 constexpr int64_t L2_SHARE = 48ll << 20;   // what the next product's weights may take of the L2
 
 template <typename T, typename W, bool VEC>
-int run_products(ep_ctx *ctx, const Layer &l, const Space &s, const Router &router) {
+int run_products(ep_ctx *ctx, const Layer &l, const Space &s) {
     const int slots = (int)l.rows * l.k;
     const int64_t w2_bytes = (int64_t)l.n_out * l.n_hidden * sizeof(W);
     // (at most one group to a slot; what is asked for starts on 16 bytes)
@@ -870,7 +884,7 @@ int run_products(ep_ctx *ctx, const Layer &l, const Space &s, const Router &rout
     auto first = experts_hidden<T, W, VEC>;
     if (VEC) EP_CUDA(ctx, cudaFuncSetAttribute(first, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ring));
     EP_CUDA(ctx, ep::launch_early(first, dim3(ctx->sm_count), dim3(THREADS), ring, l.stream, (const T *)l.x, l.ldx, l.w1, l.n_in, l.n_hidden,
-                                  l.act, l.k, s.plan, router, l.w2.w, ask ? w2_bytes : (int64_t)0, s.hidden));
+                                  l.act, l.k, s.plan, l.w2.w, ask ? w2_bytes : (int64_t)0, s.hidden));
     constexpr int STEP = 32 * step_elements<W, VEC>();   // columns that a warp takes at a time
     constexpr size_t ROOM = 80 * 1024;                   // of y
     const int cols = std::max(1, std::min({(int)ep::ceil_div(l.n_out, ctx->sm_count), (int)(ROOM / (sizeof(float) * slots)), 64}));
@@ -889,7 +903,7 @@ int run_products(ep_ctx *ctx, const Layer &l, const Space &s, const Router &rout
 
 // Both products by matrix instructions; M of the first as x, of the second bf16.
 template <typename T, typename W>
-int run_tensor(ep_ctx *ctx, const Layer &l, const Space &s, const Router &router) {
+int run_tensor(ep_ctx *ctx, const Layer &l, const Space &s) {
     const int slots = (int)l.rows * l.k;
     const int64_t w2_bytes = (int64_t)l.n_out * l.n_hidden * sizeof(W);
     const bool ask = w2_bytes % 16 == 0 && w2_bytes * std::min(slots, l.experts) <= L2_SHARE;
@@ -911,7 +925,7 @@ int run_tensor(ep_ctx *ctx, const Layer &l, const Space &s, const Router &router
     a.slots = slots;
     auto first = experts_tensor<false, T, W>;
     EP_CUDA(ctx, cudaFuncSetAttribute(first, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TENSOR_BYTES));
-    EP_CUDA(ctx, ep::launch_early(first, dim3(ctx->sm_count * TENSOR_BLOCKS), dim3(THREADS), TENSOR_BYTES, l.stream, a, s.plan, router, l.w2.w,
+    EP_CUDA(ctx, ep::launch_early(first, dim3(ctx->sm_count), dim3(THREADS), TENSOR_BYTES, l.stream, a, s.plan, l.w2.w,
                                   ask ? w2_bytes : (int64_t)0));
     TensorWork b{};
     b.x = s.hidden;
@@ -928,7 +942,7 @@ int run_tensor(ep_ctx *ctx, const Layer &l, const Space &s, const Router &router
     b.slots = slots;
     auto second = experts_tensor<true, __nv_bfloat16, W>;
     EP_CUDA(ctx, cudaFuncSetAttribute(second, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)TENSOR_BYTES));
-    EP_CUDA(ctx, ep::launch_early(second, dim3(ctx->sm_count * TENSOR_BLOCKS), dim3(THREADS), TENSOR_BYTES, l.stream, b, s.plan, router, (const void *)nullptr,
+    EP_CUDA(ctx, ep::launch_early(second, dim3(ctx->sm_count), dim3(THREADS), TENSOR_BYTES, l.stream, b, s.plan, (const void *)nullptr,
                                   (int64_t)0));
     EP_CUDA(ctx, ep::launch_early(experts_sum<T>, dim3((unsigned)ep::ceil_div(l.rows * l.n_out, 256)), dim3(256), 0, l.stream, s.y, b.shares,
                                   (int)l.rows, l.n_out, l.k, s.plan, l.ids, l.weights, l.w2.scale, l.w2.bias, l.w2.bias_type,
@@ -939,7 +953,7 @@ int run_tensor(ep_ctx *ctx, const Layer &l, const Space &s, const Router &router
 bool enough_for_tensor(const ep_ctx *ctx, const Layer &l) {
     double missed = 1.0;
     for (int r = 0; r < (int)l.rows; ++r) missed *= 1.0 - (double)l.k / l.experts;
-    return l.experts * (1.0 - missed) * (l.n_hidden / 16) >= ctx->sm_count * TENSOR_BLOCKS * WARPS;
+    return l.experts * (1.0 - missed) * (l.n_hidden / 16) >= ctx->sm_count * WARPS;
 }
 
 bool sixteen(const void *p, int64_t ld, int size) { return ep::aligned(p, 16) && ld * size % 16 == 0; }
@@ -953,17 +967,36 @@ int launch_logits(ep_ctx *ctx, const Layer &l, float *logits) {
     EP_CUDA(ctx, cudaGetLastError());
     return EP_OK;
 }
+template <typename T, bool VEC>
+int launch_router(ep_ctx *ctx, const Layer &l, const Space &s, int r) {
+    auto kernel = r == 1 ? experts_router<T, VEC, 1> : r == 2 ? experts_router<T, VEC, 2> : experts_router<T, VEC, 4>;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(ROUTER_BLOCKS);
+    cfg.blockDim = dim3(THREADS);
+    cfg.stream = l.stream;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = ROUTER_BLOCKS;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    EP_CUDA(ctx, cudaLaunchKernelEx(&cfg, kernel, (const T *)l.x, l.ldx, (const T *)l.router, l.router_bias, l.router_bias_type, (int)l.rows,
+                                    l.n_in, l.experts, s.logits, l.valid, l.k, l.renormalize, l.ids, l.weights, s.plan));
+    return EP_OK;
+}
 template <typename T>
 int run_layer(ep_ctx *ctx, const Layer &l, const Space &s, int *kernels) {
     const int size = sizeof(T), w_size = ep::type_size(l.w_type);
     const bool x_ready = sixteen(l.x, l.ldx, size);
-    int rc = x_ready && sixteen(l.router, l.n_in, size) ? launch_logits<T, true>(ctx, l, s.logits) : launch_logits<T, false>(ctx, l, s.logits);
-    if (rc != EP_OK) return rc;
-    // each block for itself where a warp has a row and few logits to look at
-    const Router router{l.rows <= OWN_ROWS && l.rows * l.k <= OWN_SLOTS && l.experts <= 256, s.logits, l.valid, (int)l.rows, l.experts,
-                        l.renormalize, l.ids, l.weights};
-    *kernels = 3;
-    if (!router.here) {
+    const bool router_ready = x_ready && sixteen(l.router, l.n_in, size);
+    const int r = l.rows == 1 ? 1 : l.rows == 2 ? 2 : 4;
+    if (l.rows * l.k <= FEW_SLOTS && ep::ceil_div(l.rows, r) * l.experts <= ROUTER_JOBS) {
+        const int rc = router_ready ? launch_router<T, true>(ctx, l, s, r) : launch_router<T, false>(ctx, l, s, r);
+        if (rc != EP_OK) return rc;
+        *kernels = 3;
+    } else {
+        const int rc = router_ready ? launch_logits<T, true>(ctx, l, s.logits) : launch_logits<T, false>(ctx, l, s.logits);
+        if (rc != EP_OK) return rc;
         EP_CUDA(ctx, ep::launch_early(experts_choose, dim3(1), dim3(1024), 0, l.stream, s.logits, l.valid, (int)l.rows, l.experts, l.k,
                                       l.renormalize, l.ids, l.weights, s.plan));
         *kernels = 4;
@@ -973,16 +1006,16 @@ int run_layer(ep_ctx *ctx, const Layer &l, const Space &s, int *kernels) {
         if (vec && l.n_hidden % 8 == 0 && enough_for_tensor(ctx, l)) {
             if (l.w_type == EP_I8) {
                 ++*kernels;
-                return run_tensor<T, i8>(ctx, l, s, router);
+                return run_tensor<T, i8>(ctx, l, s);
             }
             if constexpr (std::is_same_v<T, __nv_bfloat16>) {
                 ++*kernels;
-                return run_tensor<T, T>(ctx, l, s, router);
+                return run_tensor<T, T>(ctx, l, s);
             }
         }
     }
-    if (l.w_type == EP_I8) return vec ? run_products<T, i8, true>(ctx, l, s, router) : run_products<T, i8, false>(ctx, l, s, router);
-    return vec ? run_products<T, T, true>(ctx, l, s, router) : run_products<T, T, false>(ctx, l, s, router);
+    if (l.w_type == EP_I8) return vec ? run_products<T, i8, true>(ctx, l, s) : run_products<T, i8, false>(ctx, l, s);
+    return vec ? run_products<T, T, true>(ctx, l, s) : run_products<T, T, false>(ctx, l, s);
 }
 
 bool experts_shape_ok(int64_t rows, int n_in, int n_hidden, int n_out, int experts, int k) {

@@ -47,6 +47,7 @@ struct Epilogue {
     int N;
     bool vec;                         // out, preact, residual, bias, scales: 16-byte rows of whole 8-column chunks
     bool tma;                         // out and preact can be written by TMA, the residual read by 16 bytes
+    bool params;                      // bias and w_scale, where there are any, are fp32 and start on 16 bytes
     const float *factor;              // of fp16 results: what the sums are multiplied by first (one value), or NULL
     const int *other_b;               // where this device value is not 0, B is read by the map of z (there is no z then); or NULL
     float *share;                     // where a block's share of a split sum goes: [split][M][ld_share] fp32
@@ -513,6 +514,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
 #pragma unroll
             for (int q = 0; q < SUBS; ++q) {
                 const int c = col + q * 32 + lane;
+                if (e.params && col + COLS <= e.N) break;   // (read by four where they are used)
                 bias[q] = by_tma && e.bias && c < e.N ? load_param(e.bias, e.bias_type, c) : 0.f;
                 scale[q] = by_tma && e.w_scale && c < e.N ? e.w_scale[c] : 1.f;
             }
@@ -614,6 +616,28 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
                     if (scaled) {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] *= factor;
+                    }
+                    if (e.params && col + COLS <= e.N) {
+                        // Four at a time, the same for all lanes, from the L1.  (One from each lane by shuffles, as below, costs an
+                        // instruction a column, of which an SM does one a clock: 169343 x 128 -> 512 in 8-bit integers 60 us.)
+                        const int c = col + q * 32;
+                        if (e.x_scale) {
+#pragma unroll
+                            for (int j = 0; j < 32; j += 4) {
+                                const float4 s = *reinterpret_cast<const float4 *>(e.w_scale + c + j);
+                                mul2(Pair(v[j], v[j + 1]), mul2(Pair(xs), Pair(s.x, s.y))).get(v[j], v[j + 1]);
+                                mul2(Pair(v[j + 2], v[j + 3]), mul2(Pair(xs), Pair(s.z, s.w))).get(v[j + 2], v[j + 3]);
+                            }
+                        }
+                        if (e.bias) {
+#pragma unroll
+                            for (int j = 0; j < 32; j += 4) {
+                                const float4 b = *reinterpret_cast<const float4 *>(static_cast<const float *>(e.bias) + c + j);
+                                add2(Pair(v[j], v[j + 1]), Pair(b.x, b.y)).get(v[j], v[j + 1]);
+                                add2(Pair(v[j + 2], v[j + 3]), Pair(b.z, b.w)).get(v[j + 2], v[j + 3]);
+                            }
+                        }
+                        return;
                     }
                     const float s = SUBS > 1 && q == 1 ? scale[SUBS - 1] : scale[0], b = SUBS > 1 && q == 1 ? bias[SUBS - 1] : bias[0];
                     if (e.x_scale) {
@@ -1632,6 +1656,7 @@ int ep_linear(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int64_t ld
             (!residual || ldr * type_size(out_type) % 16 == 0);
     e.tma = tma_ready(out, n_out, out_type) && tma_ready(preact, n_out, out_type) &&
             (!residual || tma_ready(residual, ldr, out_type));
+    e.params = (!bias || (bias_type == EP_F32 && aligned(bias, 16))) && aligned(w_scale, 16);
     DeviceGuard guard(ctx->device);
     Timed tm(ctx, static_cast<cudaStream_t>(cuda_stream), EP_TIMER_LINEAR);
     int kernels = 0;
