@@ -477,7 +477,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
 //
 // Rows of up to 256 elements leave room in the tensor memory for 128 rows of a gradient beside the logits, so G need not
 // leave the SM either.  One kernel serves both gradients, the roles of x and W exchanged: 128 rows P of one stay in
-// shared memory, tiles Q of BQ rows of the other go by;
+// shared memory, tiles Q of 128 rows of the other go by;
 //     S = P Q^T;   G = slopes of S, in the operands' type;   acc += G Q
 // with all three in the tensor memory and G multiplied from there (a product whose first operand is in the tensor memory
 // reads half as much of the shared memory, which otherwise could not keep up).  P = rows of x gives dx, P = classes gives dW
@@ -488,23 +488,26 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
 constexpr int FUSED_WIDTH = 256;   // the widest rows
 constexpr int P_ROWS = 128, FUSED_THREADS = 32 * (EPI_WARPS + 3);
 struct FusedShared {
-    uint64_t full[8], empty[8], p_full[2], p_empty[2], s_full[4], s_empty[4], g_full[4], g_empty[4], acc_full, acc_empty, sums_full, drain[2];
+    uint64_t full[8], empty[8], p_full[2], p_empty[2], s_full[2], s_empty[2], g_full[2], g_empty[2], acc_full, acc_empty, sums_full, drain[2];
     uint32_t tmem_base;
     int abort;
     float sums[4][P_ROWS];
 };
-// BQ = 128: rows of up to 128 elements; 64: up to 256.
-template <bool DW, int BQ>
+constexpr int Q_ROWS = 128;
+// WIDE: rows of more than 128 elements.
+template <bool DW, bool WIDE>
 struct FusedMemory {
-    static constexpr int BOXES = BQ == 128 ? 2 : 4;              // of 64 elements, of a row at most
-    static constexpr int P_BUFFERS = BQ == 128 ? 2 : 1;
+    static constexpr int BOXES = WIDE ? 4 : 2;                   // of 64 elements, of a row at most
+    static constexpr int P_BUFFERS = WIDE ? 1 : 2;
     static constexpr int P_BYTES = BOXES * P_ROWS * 128;
-    static constexpr int EXTRA = DW ? 3 * BQ * 4 : BQ * 4;       // what is known of Q's rows: shift, g, target; or the classes' bias
-    static constexpr int Q_BYTES = BOXES * BQ * 128, STAGE = Q_BYTES + 2048;
-    static constexpr int STAGES = BQ == 128 ? 4 : 4;
-    // The tensor memory: two tiles of S, a few of G (two of its numbers to a column), the sums.
-    static constexpr int LOGITS = 2, SLOPES = BQ == 128 ? 2 : 4;
-    static constexpr int G_AT = LOGITS * BQ, ACC = G_AT + SLOPES * BQ / 2;
+    static constexpr int EXTRA = (DW ? 3 : 1) * Q_ROWS * 4;      // what is known of Q's rows: shift, g, target; or the classes' bias
+    static constexpr int Q_BYTES = BOXES * Q_ROWS * 128, STAGE = Q_BYTES + 2048;
+    static constexpr int STAGES = WIDE ? 2 : 4;
+    // The tensor memory: a tile or two of S, two of G (two of its numbers to a column), the sums.  (Tiles of 64 rows of Q, so that
+    // there is room for two of S beside sums of 256 columns, need twice the instructions of S and have the shared memory read
+    // P twice as often: 4096 x 256 -> 169343 in 1340 us.)
+    static constexpr int LOGITS = WIDE ? 1 : 2, SLOPES = 2;
+    static constexpr int G_AT = LOGITS * Q_ROWS, ACC = G_AT + SLOPES * Q_ROWS / 2;
     static constexpr size_t TOTAL = 1024 + P_BUFFERS * P_BYTES + STAGES * STAGE + sizeof(FusedShared);
     static_assert(TOTAL <= 227 * 1024 && ACC + BOXES * 64 <= 512, "a block's shared and tensor memory");
 };
@@ -549,15 +552,15 @@ __device__ __forceinline__ void umma_from_tmem_elected(uint32_t d_tmem, uint32_t
                  : "memory");
 }
 
-template <bool DW, bool BIASED, int BQ, typename T>
+template <bool DW, bool BIASED, bool WIDE, typename T>
 __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q,
                                                                  const __grid_constant__ CUtensorMap map_clean, const FusedWork e, int *status) {
-    using Mem = FusedMemory<DW, BQ>;
+    using Mem = FusedMemory<DW, WIDE>;
     constexpr int STAGES = Mem::STAGES, LOGITS = Mem::LOGITS, SLOPES = Mem::SLOPES;
     // Warps to a row of S; groups of warps that take tiles in turn.  What a group waits for has barriers of its own (a barrier that
     // went on by two phases meanwhile could not be told from one that has not moved).
-    constexpr int COLUMN_WARPS = BQ / 64, GROUPS = 4 / COLUMN_WARPS;
-    static_assert(STAGES % GROUPS == 0 && SLOPES % GROUPS == 0 && GROUPS <= 4, "a group's stages and slopes are its own");
+    constexpr int BQ = Q_ROWS, COLUMN_WARPS = BQ / 64, GROUPS = 4 / COLUMN_WARPS;
+    static_assert(STAGES % GROUPS == 0 && SLOPES % GROUPS == 0 && GROUPS <= 2, "a group's stages and slopes are its own");
     extern __shared__ char smem_raw[];
     char *p_room = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     char *ring = p_room + Mem::P_BUFFERS * Mem::P_BYTES;               // [STAGES] of Q
@@ -1665,10 +1668,9 @@ int backward_run(ep_ctx *ctx, Inputs &in, const Backward &s, const Given &given,
 
 // ---- the backward of narrow rows
 bool narrow(int n_in, int type) { return type != EP_F32 && n_in <= FUSED_WIDTH; }
-int q_rows(int n_in) { return n_in <= 128 ? 128 : 64; }
-Line fused_line(const ep_ctx *ctx, int64_t p, int64_t q, int n_in) {
+Line fused_line(const ep_ctx *ctx, int64_t p, int64_t q) {
     Line l;
-    l.inner = (int)ep::ceil_div(q, q_rows(n_in));
+    l.inner = (int)ep::ceil_div(q, Q_ROWS);
     l.tiles = ep::ceil_div(p, P_ROWS) * l.inner;
     l.workers = (int)std::min<int64_t>(l.tiles, ctx->sm_count);
     return l;
@@ -1700,10 +1702,10 @@ NarrowSpace narrow_space(const ep_ctx *ctx, int64_t rows, int n_in, int classes,
     return s;
 }
 
-template <bool DW, bool BIASED, int BQ, typename T>
+template <bool DW, bool BIASED, bool WIDE, typename T>
 int launch_fused_of(ep_ctx *ctx, const CUtensorMap &p, const CUtensorMap &q, const CUtensorMap &clean, const FusedWork &e, cudaStream_t stream) {
-    auto kernel = entropy_fused<DW, BIASED, BQ, T>;
-    constexpr size_t smem = FusedMemory<DW, BQ>::TOTAL;
+    auto kernel = entropy_fused<DW, BIASED, WIDE, T>;
+    constexpr size_t smem = FusedMemory<DW, WIDE>::TOTAL;
     EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     EP_CUDA(ctx, ep::launch_early(kernel, dim3((unsigned)e.line.workers), dim3(FUSED_THREADS), smem, stream, p, q, clean, e, ctx->d_status));
     EP_CUDA(ctx, ep::launch_early(entropy_join<T>, dim3((unsigned)e.line.workers, P_ROWS / 16), dim3(256), 0, stream, e));
@@ -1718,10 +1720,10 @@ int launch_fused(ep_ctx *ctx, Inputs &in, const NarrowSpace &s, const Operand &x
     e.Q = DW ? in.rows : in.classes;
     e.width = in.n_in;
     e.boxes = (int)ep::ceil_div(in.n_in, 64);
-    e.line = fused_line(ctx, e.P, e.Q, in.n_in);
-    const int bq = q_rows(in.n_in), columns = (in.n_in + 15) & ~15;
+    e.line = fused_line(ctx, e.P, e.Q);
+    const int columns = (in.n_in + 15) & ~15;
     const uint32_t fmt = in.type == EP_BF16 ? 1u : 0u, common = (1u << 4) | (fmt << 7) | (fmt << 10) | ((uint32_t)(P_ROWS >> 4) << 24);
-    e.idesc_s = common | ((uint32_t)(bq >> 3) << 17);
+    e.idesc_s = common | ((uint32_t)(Q_ROWS >> 3) << 17);
     e.idesc_acc = common | (1u << 16) | ((uint32_t)(columns >> 3) << 17);
     e.bias = in.bias ? s.copies.bias : nullptr;
     e.rows = s.rows;
@@ -1733,16 +1735,16 @@ int launch_fused(ep_ctx *ctx, Inputs &in, const NarrowSpace &s, const Operand &x
     e.share_bias = s.share_bias;
     e.share_ld = share_width(in.n_in);
     CUtensorMap mp{}, mq{}, mc{};
-    if (!encode_operand(&mp, DW ? w : x, false, P_ROWS) || !encode_operand(&mq, DW ? x : w, false, bq) ||
-        !encode_operand(&mc, clean, false, DW ? bq : P_ROWS))
+    if (!encode_operand(&mp, DW ? w : x, false, P_ROWS) || !encode_operand(&mq, DW ? x : w, false, Q_ROWS) ||
+        !encode_operand(&mc, clean, false, DW ? Q_ROWS : P_ROWS))
         return ep::fail(ctx, EP_ERR_CUDA, "cuTensorMapEncodeTiled failed for %lld rows of %d classes", (long long)in.rows, in.classes);
     in.kernels += 2;
     // (dW of fp16 takes the power of two that G is scaled by with the bias)
     const bool biased = e.bias || (DW && in.type == EP_F16);
     auto launch = [&](auto biased, auto type) {
         using T = decltype(type);
-        return bq == 128 ? launch_fused_of<DW, decltype(biased)::value, 128, T>(ctx, mp, mq, mc, e, in.stream)
-                         : launch_fused_of<DW, decltype(biased)::value, 64, T>(ctx, mp, mq, mc, e, in.stream);
+        return in.n_in <= 128 ? launch_fused_of<DW, decltype(biased)::value, false, T>(ctx, mp, mq, mc, e, in.stream)
+                              : launch_fused_of<DW, decltype(biased)::value, true, T>(ctx, mp, mq, mc, e, in.stream);
     };
     if (in.type == EP_BF16)
         return biased ? launch(std::true_type{}, __nv_bfloat16{}) : launch(std::false_type{}, __nv_bfloat16{});
