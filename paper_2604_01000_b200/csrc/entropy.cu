@@ -491,7 +491,7 @@ struct FusedShared {
     uint64_t full[8], empty[8], p_full[2], p_empty[2], s_full[2], s_empty[2], g_full[2], g_empty[2], acc_full, acc_empty, sums_full, drain[2];
     uint32_t tmem_base;
     int abort;
-    float sums[4][P_ROWS];
+    double sums[4][P_ROWS];
 };
 constexpr int Q_ROWS = 128;
 // WIDE: rows of more than 128 elements.
@@ -523,7 +523,7 @@ struct FusedWork {
     float *dbias;             // of DW, or NULL
     bool vec;                 // out can be written by 16 bytes
     float *share;             // [2 worker + segment][P_ROWS][share_ld]: sums of part of a P tile; then its dbias [..][P_ROWS]
-    float *share_bias;
+    double *share_bias;
     int share_ld;
 };
 // Where a worker's part of P tile `tile` lies: its first segment's place, or its last one's.
@@ -729,13 +729,13 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
         float shift = 0.f, weight = 0.f, bias = 0.f;
         bool negative = false;                                 // some row's g is
         const float log_up = std::is_same_v<T, __half> ? log2f(up) : 0.f;
-        Pair total(0.f);
+        double total = 0.0;                                    // (a class's slopes, of up to 2^31 rows; fp32 within a tile)
         for (Stretch t(e.line, worker); t.more(); t.next(), ++j) {
             if (j == 0 || t.inner == 0) {
                 p = (int64_t)t.outer * P_ROWS + quad * 32 + lane;
                 if constexpr (DW) {
                     if (BIASED) bias = (e.bias ? e.bias[p] : 0.f) + log_up;   // (padded)
-                    total = Pair(0.f);
+                    total = 0.0;
                 } else {
                     shift = e.rows.shift[p] + log_up;
                     weight = e.rows.g[p] * up;
@@ -777,8 +777,9 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
                 // (what was there has long been multiplied)
                 if (!mbar_wait_warp(&sh->g_empty[gbuf], ((j / SLOPES) & 1u) ^ 1u, abort_flag)) break;
                 tc_fence_after();
+                Pair here(0.f);
                 auto half = [&](int h, auto rare) {
-                    const float *k = known + 32 * h;
+                    [[maybe_unused]] const float *k = known + 32 * h;
                     float x[32];
 #pragma unroll
                     for (int c = 0; c < 32; c += 4) {
@@ -818,7 +819,7 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
                     uint32_t out[16];
 #pragma unroll
                     for (int c = 0; c < 32; c += 2) {
-                        if (DW) total = add2(total, Pair(x[c], x[c + 1]));
+                        if (DW) here = add2(here, Pair(x[c], x[c + 1]));
                         out[c / 2] = packed<T>(x[c], x[c + 1]);
                     }
                     tmem_st16(to + 16 * h, out);
@@ -829,6 +830,11 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
                         half(h, std::true_type{});
                     else
                         half(h, std::false_type{});
+                }
+                if constexpr (DW) {
+                    float lo, hi;
+                    here.get(lo, hi);
+                    total += (double)(lo + hi);
                 }
                 tmem_st_wait();
                 tc_fence_before();
@@ -867,19 +873,17 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
             }
             if constexpr (DW) {
                 if (e.dbias) {   // a class's sums are those of its row's four warps, in order
-                    float lo, hi;
-                    total.get(lo, hi);
-                    sh->sums[column][quad * 32 + lane] = (lo + hi) * down;
+                    sh->sums[column][quad * 32 + lane] = total * (double)down;
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&sh->sums_full);
                     if (column == 0) {   // (the others write there again only after these have given the sums of products back)
                         if (!mbar_wait_warp(&sh->sums_full, (segment & 1u) ^ 1u, abort_flag)) break;
                         const int c = quad * 32 + lane;
-                        const float sum = (sh->sums[0][c] + sh->sums[1][c]) + (sh->sums[2][c] + sh->sums[3][c]);
+                        const double sum = (sh->sums[0][c] + sh->sums[1][c]) + (sh->sums[2][c] + sh->sums[3][c]);
                         if (!whole)
                             e.share_bias[place * P_ROWS + c] = sum;
                         else if (p < e.P)
-                            e.dbias[p] = sum;
+                            e.dbias[p] = (float)sum;
                     }
                 }
             }
@@ -924,19 +928,20 @@ __global__ void __launch_bounds__(256) entropy_join(const FusedWork e) {
         store_chunk(static_cast<T *>(e.out) + p * e.width, c, e.width, e.vec, sum);
     }
     if (e.dbias && threadIdx.x < 16 && tile * P_ROWS + row0 + threadIdx.x < e.P) {
-        float sum = 0.f;
+        double sum = 0.0;
         for (int w = w0; w <= w1; ++w) sum += e.share_bias[place(w) * P_ROWS + row0 + threadIdx.x];
-        e.dbias[tile * P_ROWS + row0 + threadIdx.x] = sum;
+        e.dbias[tile * P_ROWS + row0 + threadIdx.x] = (float)sum;
     }
 }
 
-// The classes' bias over log 2, padded to whole tiles.
+// The classes' bias over log 2, padded to whole tiles (a finite bias stays finite: only -infinity closes a class).
+__device__ __forceinline__ float padded_bias(const void *bias, int type, int c, int classes) {
+    const float b = c < classes ? load_param(bias, type, c) : 0.f;
+    return fabsf(b) < INFINITY ? fminf(fmaxf(b * LOG2E, -FLT_MAX), FLT_MAX) : b;
+}
 __global__ void __launch_bounds__(256) entropy_bias(const void *bias, int type, int classes, int padded, float *out) {
     const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= padded) return;
-    // (a finite bias stays finite: only -infinity closes a class)
-    const float b = c < classes ? load_param(bias, type, c) : 0.f;
-    out[c] = fabsf(b) < INFINITY ? fminf(fmaxf(b * LOG2E, -FLT_MAX), FLT_MAX) : b;
+    if (c < padded) out[c] = padded_bias(bias, type, c, classes);
 }
 
 // ---------------------------------------------------------------------------------------------- forward
@@ -1095,27 +1100,37 @@ __global__ void __launch_bounds__(256) entropy_finish(const Statistics stats, co
 // What is known of each row, and each block's largest finite |g|.  A row that takes no part counts for nothing, whatever x holds
 // there; but 0 times an infinity or a NaN is NaN, so such rows of x are looked through: a block's `unclean` is 1 where one
 // holds any (or numbers so large that a logit might overflow), and the products then read a copy of x with zeros there.
+constexpr int WEIGHT_THREADS = 512;
+__device__ __forceinline__ Scale scale_of(float top, bool scaled, int unclean) {
+    const int up = scaled && top > 0.f ? min(14 - ilogbf(top), 126) : 0;
+    return Scale{scalbnf(1.f, up), scalbnf(1.f, -up), unclean};
+}
 template <typename T>
-__global__ void __launch_bounds__(256) entropy_weights(const float *__restrict__ lse, const int32_t *__restrict__ targets, int64_t rows,
-                                                       int classes, const long long *__restrict__ counted,
-                                                       const float *__restrict__ dloss, const float *__restrict__ drow,
-                                                       const void *__restrict__ x, int64_t ldx, int n_in, RowInfo info, float *peaks,
-                                                       int *unclean, int *status) {
+__global__ void __launch_bounds__(WEIGHT_THREADS) entropy_weights(const float *__restrict__ lse, const int32_t *__restrict__ targets, int64_t rows,
+                                                                  int classes, const long long *__restrict__ counted,
+                                                                  const float *__restrict__ dloss, const float *__restrict__ drow,
+                                                                  const void *__restrict__ x, int64_t ldx, int n_in,
+                                                                  const void *__restrict__ bias, int bias_type, float *padded, RowInfo info,
+                                                                  float *peaks, int *unclean, bool scaled, Scale *scale, int *status) {
     __shared__ int bad_rows;
-    __shared__ float tops[8];
+    __shared__ float tops[WEIGHT_THREADS / 32];
     const double mean = dloss ? (double)*dloss / (double)(*counted > 0 ? *counted : 1) : 0.0;   // (the two terms may cancel)
     const int lane = threadIdx.x & 31;
+    if (bias)   // (on the way: the bias as the tile kernels read it)
+        for (int c = blockIdx.x * WEIGHT_THREADS + threadIdx.x; c < (classes + TILE - 1) / TILE * TILE; c += gridDim.x * WEIGHT_THREADS)
+            padded[c] = padded_bias(bias, bias_type, c, classes);
     if (threadIdx.x == 0) bad_rows = 0;
     __syncthreads();
     float top = 0.f;
-    for (int64_t row0 = (int64_t)blockIdx.x * 256; row0 < rows; row0 += (int64_t)gridDim.x * 256) {
+    for (int64_t row0 = (int64_t)blockIdx.x * WEIGHT_THREADS; row0 < rows; row0 += (int64_t)gridDim.x * WEIGHT_THREADS) {
         const int64_t row = row0 + threadIdx.x;
         bool dead = false;
         if (row < rows) {
             dead = target_of(targets, row, classes, status) < 0 || lse[row] == -INFINITY;
             const float g = dead ? 0.f : (float)(mean + (drow ? (double)drow[row] : 0.0));
             const float z = lse[row];
-            info.shift[row] = dead ? -INFINITY : log2f(fabsf(g)) - z * LOG2E;
+            // (rounded once: a g that all rows share would else be off by the same in all of them, and their sums with it)
+            info.shift[row] = dead ? -INFINITY : (float)(log2((double)fabsf(g)) - (double)z * 1.44269504088896340736);
             info.g[row] = z != z ? z : g;
             info.target[row] = dead ? -1 : targets[row];
             if (fabsf(g) < INFINITY) top = fmaxf(top, fabsf(g));
@@ -1144,17 +1159,21 @@ __global__ void __launch_bounds__(256) entropy_weights(const float *__restrict__
     if (lane == 0) tops[threadIdx.x >> 5] = top;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < 8; ++w) top = fmaxf(top, tops[w]);
-        peaks[blockIdx.x] = top;
-        unclean[blockIdx.x] = bad_rows;
+        for (int w = 1; w < WEIGHT_THREADS / 32; ++w) top = fmaxf(top, tops[w]);
+        if (gridDim.x == 1)   // nobody to wait for
+            *scale = scale_of(top, scaled, bad_rows);
+        else {
+            peaks[blockIdx.x] = top;
+            unclean[blockIdx.x] = bad_rows;
+        }
     }
 }
 
-__global__ void __launch_bounds__(256) entropy_scale(const float *__restrict__ peaks, const int *__restrict__ unclean, int n, bool scaled,
-                                                     Scale *out) {
+__global__ void __launch_bounds__(256) entropy_scale(const float *peaks, const int *unclean, int n, bool scaled, Scale *out) {
     __shared__ float tops[8];
     float top = 0.f;
     bool bad = false;
+    ep_wait_for_launch_before();
     for (int i = threadIdx.x; i < n; i += 256) {
         top = fmaxf(top, peaks[i]);
         bad |= unclean[i] != 0;
@@ -1165,16 +1184,16 @@ __global__ void __launch_bounds__(256) entropy_scale(const float *__restrict__ p
     const int any = __syncthreads_or(bad);
     if (threadIdx.x == 0) {
         for (int w = 1; w < 8; ++w) top = fmaxf(top, tops[w]);
-        const int up = scaled && top > 0.f ? min(14 - ilogbf(top), 126) : 0;
-        *out = Scale{scalbnf(1.f, up), scalbnf(1.f, -up), any};
+        *out = scale_of(top, scaled, any);
     }
 }
 
 // x with zeros in the rows that take no part (see entropy_weights).  from: x, copied only if a row needs it; NULL: `to` is a
 // copy of x already, of `parts` matrices.
 template <typename E>
-__global__ void __launch_bounds__(256) entropy_clean(const E *__restrict__ from, int64_t ld, int64_t rows, int cols,
-                                                     const RowInfo info, const Scale *scale, E *to, int ld_to, int parts, int64_t part_stride) {
+__global__ void __launch_bounds__(256) entropy_clean(const E *from, int64_t ld, int64_t rows, int cols, const RowInfo info, const Scale *scale,
+                                                     E *to, int ld_to, int parts, int64_t part_stride) {
+    ep_wait_for_launch_before();
     if (!scale->unclean) return;
     const int lane = threadIdx.x & 31;
     for (int64_t row = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); row < rows; row += (int64_t)gridDim.x * 8) {
@@ -1332,6 +1351,11 @@ struct Inputs {
     int kernels;
 };
 
+// Blocks of entropy_weights: one alone, for few rows, needs no other launch to join what it found.
+int weight_blocks(const ep_ctx *ctx, int64_t rows) {
+    return rows <= 2 * WEIGHT_THREADS ? 1 : (int)std::min<int64_t>(ep::ceil_div(rows, WEIGHT_THREADS), ctx->sm_count);
+}
+
 // Copies of the operands, and the bias as the tile kernel reads it.
 struct Copies {
     void *x, *w;
@@ -1353,8 +1377,8 @@ Operand rows_of(Operand o, int64_t first, int64_t rows) {
     return o;
 }
 
-int operands(ep_ctx *ctx, Inputs &in, const Copies &c, Operand *x, Operand *w) {
-    if (c.bias && in.bias) {
+int operands(ep_ctx *ctx, Inputs &in, const Copies &c, bool with_bias, Operand *x, Operand *w) {
+    if (with_bias && c.bias && in.bias) {
         const int n = (int)ep::ceil_div(in.classes, TILE) * TILE;
         entropy_bias<<<n / 256, 256, 0, in.stream>>>(in.bias, in.bias_type, in.classes, n, c.bias);
         EP_CUDA(ctx, cudaGetLastError());
@@ -1448,7 +1472,7 @@ ForwardSpace forward_space(const ep_ctx *ctx, int64_t rows, int n_in, int classe
 
 int forward_run(ep_ctx *ctx, Inputs &in, const ForwardSpace &s, float *loss, float *row_loss, float *lse, long long *counted) {
     Operand x, w;
-    int rc = operands(ctx, in, s.copies, &x, &w);
+    int rc = operands(ctx, in, s.copies, true, &x, &w);
     if (rc != EP_OK) return rc;
     Statistics stats{s.stats, in.rows, in.type != EP_F32, s.line};
     if (stats.tiled) {
@@ -1531,7 +1555,7 @@ Backward backward_space(const ep_ctx *ctx, int64_t rows, int n_in, int classes, 
     }
     const int64_t all = ep::ceil_div(rows, TILE) * TILE;
     s.rows = RowInfo{a.take<float>(all), a.take<float>(all), a.take<int>(all)};
-    s.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(rows, 256), ctx->sm_count * 2));
+    s.blocks = weight_blocks(ctx, rows);
     s.peaks = a.take<float>(s.blocks);
     s.unclean = a.take<int>(s.blocks);
     s.scale = a.take<Scale>(1);
@@ -1551,23 +1575,27 @@ struct Wanted {
 // What is known of the rows, and the operands: x, x without what rows that take no part hold, and W.
 template <typename Space>
 int prepare(ep_ctx *ctx, Inputs &in, const Space &s, const Given &g, Operand *x, Operand *clean, Operand *w) {
-    auto weights = in.type == EP_F32 ? (void (*)(const float *, const int32_t *, int64_t, int, const long long *, const float *, const float *,
-                                                 const void *, int64_t, int, RowInfo, float *, int *, int *))entropy_weights<float>
+    auto weights = in.type == EP_F32    ? entropy_weights<float>
                    : in.type == EP_BF16 ? entropy_weights<__nv_bfloat16>
                                         : entropy_weights<__half>;
-    weights<<<s.blocks, 256, 0, in.stream>>>(g.lse, in.targets, in.rows, in.classes, g.counted, g.dloss, g.drow, in.x, in.ldx, in.n_in, s.rows,
-                                             s.peaks, s.unclean, ctx->d_status);
-    entropy_scale<<<1, 256, 0, in.stream>>>(s.peaks, s.unclean, s.blocks, in.type == EP_F16, s.scale);
+    const bool scaled = in.type == EP_F16;
+    weights<<<s.blocks, WEIGHT_THREADS, 0, in.stream>>>(g.lse, in.targets, in.rows, in.classes, g.counted, g.dloss, g.drow, in.x, in.ldx, in.n_in,
+                                                        s.copies.bias ? in.bias : nullptr, in.bias_type, s.copies.bias, s.rows, s.peaks,
+                                                        s.unclean, scaled, s.scale, ctx->d_status);
+    ++in.kernels;
+    if (s.blocks > 1) {
+        EP_CUDA(ctx, ep::launch_early(entropy_scale, dim3(1), dim3(256), 0, in.stream, s.peaks, s.unclean, s.blocks, scaled, s.scale));
+        ++in.kernels;
+    }
     EP_CUDA(ctx, cudaGetLastError());
-    in.kernels += 2;
-    const int rc = operands(ctx, in, s.copies, x, w);
+    const int rc = operands(ctx, in, s.copies, false, x, w);
     if (rc != EP_OK) return rc;
     const bool direct = x->base == in.x;
     const Packed f = ep::packed_form(in.rows, in.n_in, in.type);
     const int grid = (int)std::min<int64_t>(ep::ceil_div(in.rows, 8), (int64_t)ctx->sm_count * 8);
-    entropy_clean<<<grid, 256, 0, in.stream>>>(direct ? (const uint16_t *)in.x : nullptr, in.ldx, in.rows, in.n_in, s.rows, s.scale,
-                                               (uint16_t *)s.copies.x, f.ld, f.parts, f.part_stride);
-    EP_CUDA(ctx, cudaGetLastError());
+    EP_CUDA(ctx, ep::launch_early(entropy_clean<uint16_t>, dim3((unsigned)grid), dim3(256), 0, in.stream,
+                                  direct ? (const uint16_t *)in.x : nullptr, in.ldx, in.rows, in.n_in, s.rows, s.scale, (uint16_t *)s.copies.x,
+                                  f.ld, f.parts, f.part_stride));
     ++in.kernels;
     *clean = direct ? Operand{s.copies.x, in.type, in.rows, in.n_in, f.ld, 1, 0} : *x;
     return EP_OK;
@@ -1680,7 +1708,8 @@ int share_width(int n_in) { return (n_in + 31) & ~31; }
 struct NarrowSpace {
     Copies copies;
     RowInfo rows;
-    float *peaks, *share, *share_bias;
+    float *peaks, *share;
+    double *share_bias;
     int *unclean;
     Scale *scale;
     int blocks;
@@ -1693,8 +1722,8 @@ NarrowSpace narrow_space(const ep_ctx *ctx, int64_t rows, int n_in, int classes,
     const int64_t all = ep::ceil_div(rows, TILE) * TILE;
     s.rows = RowInfo{a.take<float>(all), a.take<float>(all), a.take<int>(all)};
     s.share = a.take<float>((size_t)ctx->sm_count * 2 * P_ROWS * share_width(n_in));
-    s.share_bias = a.take<float>((size_t)ctx->sm_count * 2 * P_ROWS);
-    s.blocks = (int)std::max<int64_t>(1, std::min<int64_t>(ep::ceil_div(rows, 256), ctx->sm_count * 2));
+    s.share_bias = a.take<double>((size_t)ctx->sm_count * 2 * P_ROWS);
+    s.blocks = weight_blocks(ctx, rows);
     s.peaks = a.take<float>(s.blocks);
     s.unclean = a.take<int>(s.blocks);
     s.scale = a.take<Scale>(1);
@@ -1702,13 +1731,19 @@ NarrowSpace narrow_space(const ep_ctx *ctx, int64_t rows, int n_in, int classes,
     return s;
 }
 
+// Whether no worker begins inside a P tile.
+bool whole_tiles(const Line &l) {
+    for (int w = 1; w < l.workers; ++w)
+        if (l.begin(w) % l.inner) return false;
+    return true;
+}
 template <bool DW, bool BIASED, bool WIDE, typename T>
 int launch_fused_of(ep_ctx *ctx, const CUtensorMap &p, const CUtensorMap &q, const CUtensorMap &clean, const FusedWork &e, cudaStream_t stream) {
     auto kernel = entropy_fused<DW, BIASED, WIDE, T>;
     constexpr size_t smem = FusedMemory<DW, WIDE>::TOTAL;
     EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     EP_CUDA(ctx, ep::launch_early(kernel, dim3((unsigned)e.line.workers), dim3(FUSED_THREADS), smem, stream, p, q, clean, e, ctx->d_status));
-    EP_CUDA(ctx, ep::launch_early(entropy_join<T>, dim3((unsigned)e.line.workers, P_ROWS / 16), dim3(256), 0, stream, e));
+    if (!whole_tiles(e.line)) EP_CUDA(ctx, ep::launch_early(entropy_join<T>, dim3((unsigned)e.line.workers, P_ROWS / 16), dim3(256), 0, stream, e));
     return EP_OK;
 }
 // Gradient of x (P = x, Q = W) or of W (P = W, Q = x).
@@ -1738,7 +1773,7 @@ int launch_fused(ep_ctx *ctx, Inputs &in, const NarrowSpace &s, const Operand &x
     if (!encode_operand(&mp, DW ? w : x, false, P_ROWS) || !encode_operand(&mq, DW ? x : w, false, Q_ROWS) ||
         !encode_operand(&mc, clean, false, DW ? Q_ROWS : P_ROWS))
         return ep::fail(ctx, EP_ERR_CUDA, "cuTensorMapEncodeTiled failed for %lld rows of %d classes", (long long)in.rows, in.classes);
-    in.kernels += 2;
+    in.kernels += whole_tiles(e.line) ? 1 : 2;
     // (dW of fp16 takes the power of two that G is scaled by with the bias)
     const bool biased = e.bias || (DW && in.type == EP_F16);
     auto launch = [&](auto biased, auto type) {
