@@ -901,24 +901,24 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
 }
 
 // The sums of P tiles that several workers had a part of, in the workers' order.  The tile that worker blockIdx.x begins inside
-// of, if it is the first to do so; 16 rows a block.
+// of, if it is the first to do so; `rows` rows a block.
 template <typename T>
-__global__ void __launch_bounds__(256) entropy_join(const FusedWork e) {
+__global__ void __launch_bounds__(256) entropy_join(const FusedWork e, int rows) {
     ep_wait_for_launch_before();
     const int64_t begin = e.line.begin(blockIdx.x), tile = begin / e.line.inner;
     const int w0 = e.line.first_worker(tile), w1 = e.line.last_worker(tile);
     if (w0 == w1 || (int)blockIdx.x != (begin == tile * e.line.inner ? w0 : w0 + 1)) return;
     const float down = e.scale->down;
-    const int row0 = blockIdx.y * 16, chunks = e.share_ld / 4;
+    const int row0 = blockIdx.y * rows, chunks = e.share_ld / 4;
     // (the first worker has it as its last segment unless that is its only one, the others as their first)
     const int64_t first = share_of(e.line, w0, tile);
     auto place = [&](int w) { return w == w0 ? first : 2 * (int64_t)w; };
-    for (int i = threadIdx.x; i < 16 * chunks && e.out; i += 256) {
+    for (int i = threadIdx.x; i < rows * chunks && e.out; i += 256) {
         const int row = row0 + i / chunks, c = (i - i / chunks * chunks) * 4;
         const int64_t p = tile * P_ROWS + row;
         if (p >= e.P) break;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+#pragma unroll 8
         for (int w = w0; w <= w1; ++w) {
             const float4 v = *reinterpret_cast<const float4 *>(e.share + (place(w) * P_ROWS + row) * e.share_ld + c);
             sum[0] += v.x, sum[1] += v.y, sum[2] += v.z, sum[3] += v.w;
@@ -927,7 +927,7 @@ __global__ void __launch_bounds__(256) entropy_join(const FusedWork e) {
         for (int q = 0; q < 4; ++q) sum[q] *= down;
         store_chunk(static_cast<T *>(e.out) + p * e.width, c, e.width, e.vec, sum);
     }
-    if (e.dbias && threadIdx.x < 16 && tile * P_ROWS + row0 + threadIdx.x < e.P) {
+    if (e.dbias && threadIdx.x < rows && tile * P_ROWS + row0 + threadIdx.x < e.P) {
         double sum = 0.0;
         for (int w = w0; w <= w1; ++w) sum += e.share_bias[place(w) * P_ROWS + row0 + threadIdx.x];
         e.dbias[tile * P_ROWS + row0 + threadIdx.x] = (float)sum;
@@ -1002,8 +1002,17 @@ struct Statistics {
     int64_t M;
     bool tiled;      // [4 number + piece][M], over log 2
     Line line;
+    int lists;       // not tiled: [lists][M]
     __device__ __forceinline__ Running of(int64_t row) const {
-        if (!tiled) return Running{all[row].x, all[row].y};
+        if (!tiled) {
+            Running r{all[row].x, all[row].y};
+#pragma unroll 4
+            for (int i = 1; i < lists; ++i) {
+                const float2 v = all[(int64_t)i * M + row];
+                r = join(r, Running{v.x, v.y});
+            }
+            return r;
+        }
         const int64_t tile = row / TILE;
         const int n = 4 * (line.last_worker(tile) - line.first_worker(tile) + 1);
         float top = -FLT_MAX, sum = 0.f;
@@ -1140,6 +1149,7 @@ __global__ void __launch_bounds__(WEIGHT_THREADS) entropy_weights(const float *_
             info.g[row] = 0.f;
             info.target[row] = -1;
         }
+        if (!x) continue;
         // four rows at a time, 8 lanes to each
         for (unsigned left = __ballot_sync(FULL, dead); left;) {
             unsigned mine = left;
@@ -1280,6 +1290,228 @@ __global__ void __launch_bounds__(256) entropy_round(const float *__restrict__ s
         for (int q = 0; q < 4; ++q)
             if (i + q < n) out[i + q] = from_f32<T>(sums[i + q] * down);
     }
+}
+
+// ---------------------------------------------------------------------------------------------- small problems
+//
+// A few fp32 products cost the tile kernels mostly launches and passes (operands split in three, logits written and read back,
+// statistics or G, joins).  Then fp32 multiply-adds of tiles of 64 x 64 take the operands as they are: the forward is two
+// launches, the backward three to five.  Bound by their latency: a tile's sum is one chain of steps, each a load, a barrier and
+// the multiply-adds.  (fp32, tiles -> here, us.  Forward: 128 x 64 -> 32 11.1 -> 8.2, 50000 x 16 -> 40 30.6 -> 17.7, 200000 x 16 -> 10
+// 107 -> 48; but 16 x 160 -> 456 12.7 -> 14.4, 132 x 96 -> 7050 20 -> 52: long sums, few rows.  Backward: 128 x 64 -> 32 24.0 -> 20.3,
+// 500 x 64 -> 500 34.5 -> 26.4, 40 x 128 -> 4000 31.5 -> 27.3; but 500 x 256 -> 260 36 -> 43, 2000 x 64 -> 1000 44 -> 59.  In 16 bits, where
+// nothing is split, the tiles won at 22 of 24 sizes in each direction.)
+constexpr int ST = 64, SK = 32;   // a block's rows and columns; the step of the sum
+struct SmallTile {
+    float a[SK][ST + 4], b[SK][ST + 4];
+};
+// acc[i][j] = sum over k in [k0, k1) of A(4 ty + i, k) B(4 tx + j, k) of a tile; a_of and b_of give elements, and are asked for four of
+// one k (ALONG_ROWS: elements of one k lie next to one another) or for four k of one row.  Sums of 128 are added up (a long
+// sum of fp32 would lose bits).
+template <bool A_ALONG, bool B_ALONG, typename A, typename B, typename Step>
+__device__ __forceinline__ void small_product(SmallTile &s, int64_t k0, int64_t k1, A a_of, B b_of, Step each_step, float (&total)[4][4]) {
+    const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
+    // which elements of a step this thread brings: eight k of one row, or four rows of two k
+    constexpr int E = ST * SK / 256;
+    auto row_of = [&](bool along, int i) { return along ? (t & 15) * 4 + (i & 3) : t >> 2; };
+    auto k_of = [&](bool along, int i) { return along ? (t >> 4) + 16 * (i >> 2) : (t & 3) * E + i; };
+    float acc[4][4] = {}, pa[E], pb[E];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) total[i][j] = 0.f;
+    auto bring = [&](int64_t k) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const int64_t ka = k + k_of(A_ALONG, i), kb = k + k_of(B_ALONG, i);
+            pa[i] = ka < k1 ? a_of(row_of(A_ALONG, i), ka) : 0.f;
+            pb[i] = kb < k1 ? b_of(row_of(B_ALONG, i), kb) : 0.f;
+        }
+    };
+    bring(k0);
+    int steps = 0;
+    for (int64_t k = k0; k < k1; k += SK) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            s.a[k_of(A_ALONG, i)][row_of(A_ALONG, i)] = pa[i];
+            s.b[k_of(B_ALONG, i)][row_of(B_ALONG, i)] = pb[i];
+        }
+        __syncthreads();
+        if (k + SK < k1) bring(k + SK);
+        each_step();
+#pragma unroll
+        for (int q = 0; q < SK; ++q) {
+            const float4 x = *reinterpret_cast<const float4 *>(&s.a[q][4 * ty]), y = *reinterpret_cast<const float4 *>(&s.b[q][4 * tx]);
+            const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(xs[i], ys[j], acc[i][j]);
+        }
+        if (++steps == 128 / SK || k + SK >= k1) {
+            steps = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    total[i][j] += acc[i][j];
+                    acc[i][j] = 0.f;
+                }
+        }
+        __syncthreads();
+    }
+}
+
+struct SmallWork {
+    const float *x;
+    int64_t ldx;
+    const float *w;
+    int64_t ldw;
+    const void *bias;
+    int bias_type;
+    const int32_t *targets;
+    int64_t rows;
+    int n_in, classes, class_tiles;
+    float2 *stats;            // forward: [class tile][rows]
+    float *at_target;
+    unsigned *ticket;
+    const float *lse;         // backward
+    RowInfo info;
+    float *g;                 // [rows][ldg]
+    int ldg;
+    int dx_splits, dw_splits; // shares of the sums over classes and over rows
+    int64_t dx_blocks;
+    float *dx_part, *dw_part, *db_part;   // [share][..], or the outputs themselves are written
+    float *dx, *dweight, *dbias;
+};
+// What the tile kernels make of an infinity among fp32 operands, which split into NaN: an infinite logit is no logit.
+__device__ __forceinline__ float small_logit(float v) { return isinf(v) ? CUDART_NAN_F : v; }
+// One tile of logits: statistics of its rows (forward) or G (backward).
+template <bool GRAD>
+__global__ void __launch_bounds__(256) entropy_small_logits(const SmallWork e) {
+    __shared__ SmallTile s;
+    const int64_t row0 = (int64_t)blockIdx.y * ST;
+    const int class0 = blockIdx.x * ST, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    ep_wait_for_launch_before();
+    if (!GRAD && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *e.ticket = 0;
+    float v[4][4];
+    small_product<false, false>(
+        s, 0, e.n_in, [&](int m, int64_t k) { return row0 + m < e.rows ? e.x[(row0 + m) * e.ldx + k] : 0.f; },
+        [&](int n, int64_t k) { return class0 + n < e.classes ? e.w[(class0 + n) * e.ldw + k] : 0.f; }, [] {}, v);
+    float bias[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) bias[j] = e.bias && class0 + 4 * tx + j < e.classes ? load_param(e.bias, e.bias_type, class0 + 4 * tx + j) : 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t row = row0 + 4 * ty + i;
+        const bool there = row < e.rows;
+        if constexpr (GRAD) {
+            if (!there) continue;
+            const int target = e.info.target[row];
+            const float g = e.info.g[row], z = e.lse[row];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int c = class0 + 4 * tx + j;
+                const float p = exp_fast(small_logit(v[i][j]) + bias[j] - z) - (c == target ? 1.f : 0.f);
+                if (c < e.ldg) e.g[row * e.ldg + c] = target >= 0 && c < e.classes ? p * g : 0.f;
+            }
+        } else {
+            const int target = there ? e.targets[row] : -1;
+            Running r{-INFINITY, 0.f};
+            float l[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int c = class0 + 4 * tx + j;
+                l[j] = c < e.classes ? small_logit(v[i][j]) + bias[j] : -INFINITY;
+                if (there && c == target) e.at_target[row] = l[j];
+                r.m = fmaxf(r.m, l[j]);
+            }
+            const float shift = r.m == -INFINITY ? 0.f : r.m;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r.s += exp_fast(l[j] - shift);
+#pragma unroll
+            for (int o = 8; o >= 1; o >>= 1) r = join(r, Running{__shfl_xor_sync(FULL, r.m, o), __shfl_xor_sync(FULL, r.s, o)});
+            if (tx == 0 && there) e.stats[(int64_t)blockIdx.x * e.rows + row] = make_float2(r.m, r.s);
+        }
+    }
+}
+// dx = G W and dW = G^T x, a tile and a share of the sum to a block; dbias with the first column of tiles of dW.
+__global__ void __launch_bounds__(256) entropy_small_products(const SmallWork e) {
+    __shared__ SmallTile s;
+    const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
+    const int across = (e.n_in + ST - 1) / ST;
+    ep_wait_for_launch_before();
+    const bool is_dx = (int64_t)blockIdx.x < e.dx_blocks;
+    int64_t b = is_dx ? blockIdx.x : blockIdx.x - e.dx_blocks;
+    const int splits = is_dx ? e.dx_splits : e.dw_splits, share = (int)(b % splits);
+    b /= splits;
+    const int64_t m0 = b / across * ST, all = is_dx ? e.classes : e.rows, ms = is_dx ? e.rows : e.classes;
+    const int n0 = (int)(b % across) * ST;
+    const int64_t each = ((all + splits - 1) / splits + SK - 1) / SK * SK, k0 = min(share * each, all), k1 = min(k0 + each, all);
+    float v[4][4];
+    double column = 0.0;   // of dbias: class m0 + t
+    if (is_dx)
+        small_product<false, true>(
+            s, k0, k1, [&](int m, int64_t k) { return m0 + m < e.rows ? e.g[(m0 + m) * e.ldg + k] : 0.f; },
+            [&](int n, int64_t k) { return n0 + n < e.n_in ? e.w[k * e.ldw + n0 + n] : 0.f; }, [] {}, v);
+    else
+        small_product<true, true>(
+            s, k0, k1, [&](int m, int64_t k) { return m0 + m < e.classes ? e.g[k * e.ldg + m0 + m] : 0.f; },
+            // (a row that takes no part counts for nothing, whatever it holds)
+            [&](int n, int64_t k) { return n0 + n < e.n_in && e.info.target[k] >= 0 ? e.x[k * e.ldx + n0 + n] : 0.f; },
+            [&] {
+                if (n0 == 0 && t < ST) {
+                    float here = 0.f;
+#pragma unroll
+                    for (int q = 0; q < SK; ++q) here += s.a[q][t];
+                    column += (double)here;
+                }
+            },
+            v);
+    float *part = is_dx ? e.dx_part : e.dw_part, *out = is_dx ? e.dx : e.dweight;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t m = m0 + 4 * ty + i;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int n = n0 + 4 * tx + j;
+            if (m >= ms || n >= e.n_in) continue;
+            if (splits > 1)
+                part[((int64_t)share * ms + m) * e.n_in + n] = v[i][j];
+            else if (out)
+                out[m * e.n_in + n] = v[i][j];
+        }
+    }
+    if (!is_dx && n0 == 0 && t < ST && m0 + t < e.classes && e.dbias) {
+        if (splits > 1)
+            e.db_part[(int64_t)share * e.classes + m0 + t] = (float)column;
+        else
+            e.dbias[m0 + t] = (float)column;
+    }
+}
+// The shares: LANES lanes to an element, each every LANES-th share in order, then the lanes (in a fixed order).
+template <int LANES>
+__global__ void __launch_bounds__(256) entropy_small_fold(const float *part, int splits, int64_t n, float *out, const float *more_part,
+                                                          int64_t more, float *more_out) {
+    ep_wait_for_launch_before();
+    ep_let_next_launch_start();
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES;
+    if (at >= n + more) return;   // (a warp's lanes leave together: LANES is 1 or 32)
+    const bool rest = at >= n;
+    const int64_t i = rest ? at - n : at, all = rest ? more : n;
+    const float *from = rest ? more_part : part;
+    double sum = 0.0;
+#pragma unroll 8
+    for (int s = threadIdx.x % LANES; s < splits; s += LANES) sum += (double)from[(int64_t)s * all + i];
+    if constexpr (LANES > 1) {
+#pragma unroll
+        for (int o = LANES / 2; o >= 1; o >>= 1) sum += __shfl_xor_sync(FULL, sum, o);
+        if (threadIdx.x % LANES) return;
+    }
+    if (rest)
+        more_out[i] = (float)sum;
+    else if (out)
+        out[i] = (float)sum;
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -1474,7 +1706,7 @@ int forward_run(ep_ctx *ctx, Inputs &in, const ForwardSpace &s, float *loss, flo
     Operand x, w;
     int rc = operands(ctx, in, s.copies, true, &x, &w);
     if (rc != EP_OK) return rc;
-    Statistics stats{s.stats, in.rows, in.type != EP_F32, s.line};
+    Statistics stats{s.stats, in.rows, in.type != EP_F32, s.line, 1};
     if (stats.tiled) {
         TileWork e{};
         e.M = in.rows;
@@ -1700,7 +1932,10 @@ Line fused_line(const ep_ctx *ctx, int64_t p, int64_t q) {
     Line l;
     l.inner = (int)ep::ceil_div(q, Q_ROWS);
     l.tiles = ep::ceil_div(p, P_ROWS) * l.inner;
-    l.workers = (int)std::min<int64_t>(l.tiles, ctx->sm_count);
+    // Where there are not four tiles to each SM, workers have whole P tiles, or four tiles each: parts of a P tile have to be written and
+    // joined, which takes as long as a few tiles.
+    const int64_t outer = ep::ceil_div(p, P_ROWS), parts = ep::ceil_div(l.inner, 4);
+    l.workers = (int)std::min<int64_t>(ctx->sm_count, l.tiles <= 4 * ctx->sm_count ? outer * parts : l.tiles);
     return l;
 }
 int share_width(int n_in) { return (n_in + 31) & ~31; }
@@ -1743,7 +1978,11 @@ int launch_fused_of(ep_ctx *ctx, const CUtensorMap &p, const CUtensorMap &q, con
     constexpr size_t smem = FusedMemory<DW, WIDE>::TOTAL;
     EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     EP_CUDA(ctx, ep::launch_early(kernel, dim3((unsigned)e.line.workers), dim3(FUSED_THREADS), smem, stream, p, q, clean, e, ctx->d_status));
-    if (!whole_tiles(e.line)) EP_CUDA(ctx, ep::launch_early(entropy_join<T>, dim3((unsigned)e.line.workers, P_ROWS / 16), dim3(256), 0, stream, e));
+    // Many workers to a tile: long sums, so fewer of them to a block (rows of 29 in fp16 against 27668 classes: 8 us sooner); else few
+    // blocks, most of which have nothing to do (5322 rows against 2723 classes: 13 us sooner).
+    const int rows = e.line.workers >= 8 * (e.line.tiles / e.line.inner) ? 4 : 16;
+    if (!whole_tiles(e.line))
+        EP_CUDA(ctx, ep::launch_early(entropy_join<T>, dim3((unsigned)e.line.workers, P_ROWS / rows), dim3(256), 0, stream, e, rows));
     return EP_OK;
 }
 // Gradient of x (P = x, Q = W) or of W (P = W, Q = x).
@@ -1794,6 +2033,125 @@ int narrow_backward_run(ep_ctx *ctx, Inputs &in, const NarrowSpace &s, const Giv
     return rc;
 }
 
+// ---- small problems
+// (what was measured on both sides stands at the kernels)
+bool small_problem(bool grad, int64_t rows, int n_in, int classes, int type) {
+    const int64_t logits = rows * classes;
+    return type == EP_F32 && n_in <= 128 && (grad || classes <= 1024) && rows <= 1 << 20 && logits <= 1 << 22 && logits * n_in <= 1 << 25;
+}
+// Shares of a sum over `all` so that `tiles` tiles make about three blocks an SM, of at least 128 each.
+int small_splits(const ep_ctx *ctx, int64_t tiles, int64_t all) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>(ctx->sm_count * 3 / std::max<int64_t>(tiles, 1), ep::ceil_div(all, 2 * ST)));
+}
+struct SmallSpace {
+    float2 *stats;
+    float *at_target, *g, *dx_part, *dw_part, *db_part, *peaks;
+    Finish finish;
+    RowInfo rows;
+    int *unclean;
+    Scale *scale;
+    int ldg, dx_splits, dw_splits;
+    int64_t dx_tiles, dw_tiles;
+    size_t bytes;
+};
+SmallSpace small_space(const ep_ctx *ctx, bool grad, int64_t rows, int n_in, int classes, void *base) {
+    ep::Arena a(base);
+    SmallSpace s{};
+    if (!grad) {
+        s.stats = a.take<float2>(ep::ceil_div(classes, ST) * rows);
+        s.at_target = a.take<float>(rows);
+        s.finish.sums = a.take<double>(ep::ceil_div(rows, FINISH_ROWS));
+        s.finish.counts = a.take<long long>(ep::ceil_div(rows, FINISH_ROWS));
+        s.finish.ticket = a.take<unsigned>(1);
+    } else {
+        const int64_t all = ep::ceil_div(rows, TILE) * TILE, across = ep::ceil_div(n_in, ST);
+        s.ldg = (classes + 3) & ~3;
+        s.g = a.take<float>(rows * s.ldg);
+        s.rows = RowInfo{a.take<float>(all), a.take<float>(all), a.take<int>(all)};
+        s.peaks = a.take<float>(weight_blocks(ctx, rows));
+        s.unclean = a.take<int>(weight_blocks(ctx, rows));
+        s.scale = a.take<Scale>(1);
+        s.dx_tiles = ep::ceil_div(rows, ST) * across;
+        s.dw_tiles = ep::ceil_div(classes, ST) * across;
+        s.dx_splits = small_splits(ctx, s.dx_tiles, classes);
+        s.dw_splits = small_splits(ctx, s.dw_tiles, rows);
+        s.dx_part = a.take<float>(s.dx_splits > 1 ? (size_t)s.dx_splits * rows * n_in : 0);
+        s.dw_part = a.take<float>(s.dw_splits > 1 ? (size_t)s.dw_splits * classes * n_in : 0);
+        s.db_part = a.take<float>(s.dw_splits > 1 ? (size_t)s.dw_splits * classes : 0);
+    }
+    s.bytes = std::max<size_t>(a.used, 256);
+    return s;
+}
+SmallWork small_work(const Inputs &in) {
+    SmallWork e{};
+    e.x = static_cast<const float *>(in.x);
+    e.ldx = in.ldx;
+    e.w = static_cast<const float *>(in.w);
+    e.ldw = in.ldw;
+    e.bias = in.bias;
+    e.bias_type = in.bias_type;
+    e.targets = in.targets;
+    e.rows = in.rows;
+    e.n_in = in.n_in;
+    e.classes = in.classes;
+    e.class_tiles = (int)ep::ceil_div(in.classes, ST);
+    return e;
+}
+int small_forward(ep_ctx *ctx, Inputs &in, const SmallSpace &s, float *loss, float *row_loss, float *lse, long long *counted) {
+    SmallWork e = small_work(in);
+    e.stats = s.stats;
+    e.at_target = s.at_target;
+    e.ticket = s.finish.ticket;
+    EP_CUDA(ctx, ep::launch_early(entropy_small_logits<false>, dim3((unsigned)e.class_tiles, (unsigned)ep::ceil_div(in.rows, ST)), dim3(256), 0,
+                                  in.stream, e));
+    Finish f = s.finish;
+    f.loss = loss;
+    f.counted = counted;
+    EP_CUDA(ctx, ep::launch_early(entropy_finish, dim3((unsigned)ep::ceil_div(in.rows, FINISH_ROWS)), dim3(256), 0, in.stream,
+                                  Statistics{s.stats, in.rows, false, Line{}, e.class_tiles}, s.at_target, in.targets, in.rows, in.classes, lse,
+                                  row_loss, f, ctx->d_status));
+    in.kernels += 2;
+    return EP_OK;
+}
+int small_backward(ep_ctx *ctx, Inputs &in, const SmallSpace &s, const Given &g, const Wanted &out) {
+    const int blocks = weight_blocks(ctx, in.rows);
+    entropy_weights<float><<<blocks, WEIGHT_THREADS, 0, in.stream>>>(g.lse, in.targets, in.rows, in.classes, g.counted, g.dloss, g.drow, nullptr, 0, 0,
+                                                                 nullptr, 0, nullptr, s.rows, s.peaks, s.unclean, false, s.scale, ctx->d_status);
+    EP_CUDA(ctx, cudaGetLastError());
+    SmallWork e = small_work(in);
+    e.lse = g.lse;
+    e.info = s.rows;
+    e.g = s.g;
+    e.ldg = s.ldg;
+    e.dx_splits = out.dx ? s.dx_splits : 1;
+    e.dw_splits = out.dweight || out.dbias ? s.dw_splits : 1;
+    e.dx_blocks = out.dx ? s.dx_tiles * s.dx_splits : 0;
+    e.dx_part = s.dx_part;
+    e.dw_part = s.dw_part;
+    e.db_part = s.db_part;
+    e.dx = static_cast<float *>(out.dx);
+    e.dweight = static_cast<float *>(out.dweight);
+    e.dbias = out.dbias;
+    EP_CUDA(ctx, ep::launch_early(entropy_small_logits<true>, dim3((unsigned)e.class_tiles, (unsigned)ep::ceil_div(in.rows, ST)), dim3(256), 0,
+                                  in.stream, e));
+    const int64_t dw_blocks = out.dweight || out.dbias ? s.dw_tiles * s.dw_splits : 0;
+    EP_CUDA(ctx, ep::launch_early(entropy_small_products, dim3((unsigned)(e.dx_blocks + dw_blocks)), dim3(256), 0, in.stream, e));
+    in.kernels += 3;
+    // many shares: a warp to an element
+    auto fold = [&](const float *part, int splits, int64_t n, float *to, const float *more_part, int64_t more, float *more_to) {
+        if (splits == 1) return cudaSuccess;
+        ++in.kernels;
+        const int lanes = splits > 16 ? 32 : 1;
+        auto kernel = lanes > 1 ? entropy_small_fold<32> : entropy_small_fold<1>;
+        return ep::launch_early(kernel, dim3((unsigned)ep::ceil_div((n + more) * lanes, 256)), dim3(256), 0, in.stream, part, splits, n, to,
+                                more_part, more, more_to);
+    };
+    EP_CUDA(ctx, fold(e.dx_part, e.dx_splits, in.rows * in.n_in, e.dx, nullptr, 0, nullptr));
+    EP_CUDA(ctx, fold(e.dw_part, e.dw_splits, out.dweight ? (int64_t)in.classes * in.n_in : 0, e.dweight, e.db_part,
+                      out.dbias ? in.classes : 0, out.dbias));
+    return EP_OK;
+}
+
 }  // namespace
 
 using namespace ep;
@@ -1820,6 +2178,7 @@ extern "C" {
 size_t ep_cross_entropy_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t n_in, int32_t classes, int32_t in_type,
                                         int32_t is_aligned) {
     if (!ctx || !entropy_shape_ok(rows, n_in, classes) || !float_type(in_type)) return 0;
+    if (small_problem(false, rows, n_in, classes, in_type)) return small_space(ctx, false, rows, n_in, classes, nullptr).bytes;
     return forward_space(ctx, rows, n_in, classes, in_type, is_aligned != 0, nullptr).bytes;
 }
 
@@ -1840,11 +2199,14 @@ int ep_cross_entropy(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int
         return EP_OK;
     }
     in.aligned = can_be_read_by_tma(x, ldx, in_type) && can_be_read_by_tma(w, ldw, in_type);
-    const ForwardSpace s = forward_space(ctx, rows, n_in, classes, in_type, in.aligned, workspace);
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < s.bytes)
+    const bool small = small_problem(false, rows, n_in, classes, in_type);
+    const SmallSpace few = small ? small_space(ctx, false, rows, n_in, classes, workspace) : SmallSpace{};
+    const ForwardSpace s = small ? ForwardSpace{} : forward_space(ctx, rows, n_in, classes, in_type, in.aligned, workspace);
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < std::max(few.bytes, s.bytes))
         return fail(ctx, EP_ERR_WORKSPACE, "workspace too small or misaligned");
+    long long *count = reinterpret_cast<long long *>(counted);
     Timed tm(ctx, in.stream, EP_TIMER_ENTROPY);
-    rc = forward_run(ctx, in, s, loss, row_loss, lse, reinterpret_cast<long long *>(counted));
+    rc = small ? small_forward(ctx, in, few, loss, row_loss, lse, count) : forward_run(ctx, in, s, loss, row_loss, lse, count);
     tm.end(in.kernels);
     return rc;
 }
@@ -1852,6 +2214,7 @@ int ep_cross_entropy(ep_ctx *ctx, const void *x, int64_t ldx, const void *w, int
 size_t ep_cross_entropy_backward_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t n_in, int32_t classes, int32_t in_type,
                                                  int32_t is_aligned) {
     if (!ctx || !entropy_shape_ok(rows, n_in, classes) || !float_type(in_type)) return 0;
+    if (small_problem(true, rows, n_in, classes, in_type)) return small_space(ctx, true, rows, n_in, classes, nullptr).bytes;
     return narrow(n_in, in_type) ? narrow_space(ctx, rows, n_in, classes, in_type, is_aligned != 0, nullptr).bytes
                                  : backward_space(ctx, rows, n_in, classes, in_type, is_aligned != 0, nullptr).bytes;
 }
@@ -1875,15 +2238,18 @@ int ep_cross_entropy_backward(ep_ctx *ctx, const void *x, int64_t ldx, const voi
     }
     if (!dx && !dweight && !dbias) return EP_OK;
     in.aligned = can_be_read_by_tma(x, ldx, in_type) && can_be_read_by_tma(w, ldw, in_type);
-    const bool small = narrow(n_in, in_type);
-    const Backward s = small ? Backward{} : backward_space(ctx, rows, n_in, classes, in_type, in.aligned, workspace);
-    const NarrowSpace n = small ? narrow_space(ctx, rows, n_in, classes, in_type, in.aligned, workspace) : NarrowSpace{};
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < std::max(s.bytes, n.bytes))
+    const bool small = small_problem(true, rows, n_in, classes, in_type), in_tmem = !small && narrow(n_in, in_type);
+    const SmallSpace few = small ? small_space(ctx, true, rows, n_in, classes, workspace) : SmallSpace{};
+    const NarrowSpace n = in_tmem ? narrow_space(ctx, rows, n_in, classes, in_type, in.aligned, workspace) : NarrowSpace{};
+    const Backward s = small || in_tmem ? Backward{} : backward_space(ctx, rows, n_in, classes, in_type, in.aligned, workspace);
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < std::max({few.bytes, n.bytes, s.bytes}))
         return fail(ctx, EP_ERR_WORKSPACE, "workspace too small or misaligned");
     const Given given{lse, dloss, drow_loss, reinterpret_cast<const long long *>(counted)};
     const Wanted out{dx, dweight, dbias};
     Timed tm(ctx, in.stream, EP_TIMER_ENTROPY);
-    rc = small ? narrow_backward_run(ctx, in, n, given, out) : backward_run(ctx, in, s, given, out);
+    rc = small     ? small_backward(ctx, in, few, given, out)
+         : in_tmem ? narrow_backward_run(ctx, in, n, given, out)
+                   : backward_run(ctx, in, s, given, out);
     tm.end(in.kernels);
     return rc;
 }

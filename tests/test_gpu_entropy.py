@@ -135,8 +135,9 @@ def test_several_pieces(rows, n_in, classes, dtype):
     assert all(torch.equal(p, q) for p, q in zip(got, again))        # the same from run to run
 
 
-def test_what_is_not_wanted_is_not_made():
-    x, w, t = trained(300, 64, 100, BF16, 10)
+@pytest.mark.parametrize("rows,n_in", [(300, 64), (6000, 64), (3000, 264)])
+def test_what_is_not_wanted_is_not_made(rows, n_in):
+    x, w, t = trained(rows, n_in, 100, BF16, 10)
     r = forward(x, w, t)
     one = torch.ones(1, device="cuda")
     whole = backward(x, w, t, r, None, one)
@@ -146,15 +147,17 @@ def test_what_is_not_wanted_is_not_made():
     assert all(g is None for g in ep().ep_cross_entropy_backward(x, w, t, r, None, one, None, False, False, False))
 
 
+# (up to 2^25 products go by other kernels than more, rows of up to 256 elements by others than wider ones)
+@pytest.mark.parametrize("rows,n_in", [(500, 96), (3000, 96), (1800, 256), (700, 296)])
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
-def test_rows_without_a_class_count_for_nothing_whatever_they_hold(dtype):
-    x, w, t = trained(500, 96, 300, dtype, 11, 0.2)
+def test_rows_without_a_class_count_for_nothing_whatever_they_hold(dtype, rows, n_in):
+    x, w, t = trained(rows, n_in, 300, dtype, 11, 0.2)
     b, one = rand((300,), F32, 12), torch.ones(1, device="cuda")
     r = forward(x, w, t, b)
-    clean = backward(x, w, t, r, b, one, rand((500,), F32, 13))
+    clean = backward(x, w, t, r, b, one, rand((rows,), F32, 13))
     spoiled = x.clone()
-    spoiled[t < 0] = torch.tensor([math.nan, math.inf, -math.inf, 1.0] * 24, device="cuda").to(dtype)
-    drow = rand((500,), F32, 13)
+    spoiled[t < 0] = torch.tensor([math.nan, math.inf, -math.inf, 1.0] * (n_in // 4), device="cuda").to(dtype)
+    drow = rand((rows,), F32, 13)
     drow[t < 0] = math.nan
     q = ep().ep_cross_entropy(spoiled, w, t, b)
     assert all(torch.equal(p, s) for p, s in zip(r, q))
@@ -164,9 +167,10 @@ def test_rows_without_a_class_count_for_nothing_whatever_they_hold(dtype):
     assert all(torch.equal(p, s) for p, s in zip(got, clean))
 
 
+@pytest.mark.parametrize("rows,n_in", [(200, 64), (9000, 64), (2000, 272)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
-def test_closed_classes(dtype):
-    x, w, t = trained(200, 64, 70, dtype, 14)
+def test_closed_classes(dtype, rows, n_in):
+    x, w, t = trained(rows, n_in, 70, dtype, 14)
     b = rand((70,), F32, 15)
     b[::3] = -math.inf
     r = forward(x, w, t, b)
@@ -184,11 +188,12 @@ def test_closed_classes(dtype):
     assert all(bool((g == 0).all()) for g in got)
 
 
-def test_far_logits_and_spoiled_rows():
+@pytest.mark.parametrize("rows", [150, 14000])
+def test_far_logits_and_spoiled_rows(rows):
     # logits of hundreds: one class has all of it; masks of the type's lowest value beside it
     for dtype in (BF16, F32):
-        x, w = rand((150, 32), dtype, 16, 30.0), rand((90, 32), dtype, 17, 5.0)
-        t = some_targets(150, 90, 18)
+        x, w = rand((rows, 32), dtype, 16, 30.0), rand((90, 32), dtype, 17, 5.0)
+        t = some_targets(rows, 90, 18)
         b = torch.zeros(90, device="cuda")
         b[:40] = torch.finfo(F32).min
         r = forward(x, w, t.clamp(min=40), b)
@@ -199,9 +204,10 @@ def test_far_logits_and_spoiled_rows():
         assert bool(torch.isnan(r.row_loss[7])) and bool(torch.isnan(r.loss).all()) and int(torch.isnan(r.lse).sum()) == 1
 
 
-def test_targets_outside_the_classes_are_told_and_skipped():
+@pytest.mark.parametrize("rows,n_in", [(40, 16), (40000, 96), (14000, 264)])
+def test_targets_outside_the_classes_are_told_and_skipped(rows, n_in):
     m = ep()
-    x, w, t = trained(40, 16, 10, BF16, 19)
+    x, w, t = trained(rows, n_in, 10, BF16, 19)
     m.default_context().check()
     bad = t.clone()
     bad[3], bad[4], bad[5] = 10, -2, 2 ** 31 - 1
@@ -211,7 +217,7 @@ def test_targets_outside_the_classes_are_told_and_skipped():
     m.default_context().check()
     got = m.ep_cross_entropy(x, w, bad)
     assert m.default_context().poll_status() == 4
-    assert all(torch.equal(p, q) for p, q in zip(got, want)) and int(got.counted) == 37
+    assert all(torch.equal(p, q) for p, q in zip(got, want)) and int(got.counted) == rows - 3
     one = torch.ones(1, device="cuda")
     got = m.ep_cross_entropy_backward(x, w, bad, want, None, one)
     assert m.default_context().poll_status() == 4
@@ -233,13 +239,14 @@ def test_no_rows_and_none_that_count():
     assert not any(bool(g.any()) for g in got)
 
 
-def test_strided_rows_and_misaligned_buffers():
+@pytest.mark.parametrize("rows", [130, 7000])
+def test_strided_rows_and_misaligned_buffers(rows):
     for dtype in (BF16, F32, F16):
-        big, wide = rand((130, 200), dtype, 22), rand((70, 160), dtype, 23, 0.1)
-        t, one = some_targets(130, 70, 24), torch.ones(1, device="cuda")
+        big, wide = rand((rows, 200), dtype, 22), rand((70, 160), dtype, 23, 0.1)
+        t, one = some_targets(rows, 70, 24), torch.ones(1, device="cuda")
         for x, w in ((big[:, 8:136], wide[:, 16:144]), (big[:, 3:80], wide[:, 5:82]), (big[:, :160], wide), (big[:, 1:161], wide)):
             backward(x, w, t, forward(x, w, t), None, one)
-        half = some_targets(65, 70, 25)
+        half = some_targets(rows // 2, 70, 25)
         x = big[::2, :160]
         backward(x, wide, half, forward(x, wide, half, ref.misaligned(rand((70,), dtype, 26))), ref.misaligned(rand((70,), dtype, 26)), one)
 
@@ -266,10 +273,11 @@ def test_gradients_against_differences():
 
 def test_small_gradients_of_fp16_are_kept():
     # a mean over many rows puts whole gradients below fp16's range
-    x, w, t = trained(5000, 32, 64, F16, 30)
-    r = forward(x, w, t)
-    backward(x, w, t, r, None, torch.full((1,), 1e-4, device="cuda"))
-    backward(x, w, t, r, None, torch.full((1,), 3e4, device="cuda"))
+    for rows, n_in in ((5000, 32), (20000, 32), (3000, 264)):   # 64 classes each
+        x, w, t = trained(rows, n_in, 64, F16, 30)
+        r = forward(x, w, t)
+        backward(x, w, t, r, None, torch.full((1,), 1e-4, device="cuda"))
+        backward(x, w, t, r, None, torch.full((1,), 3e4, device="cuda"))
 
 
 def test_captured_beside_another_stream():
