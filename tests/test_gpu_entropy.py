@@ -327,3 +327,44 @@ def test_refusals():
         m.ep_cross_entropy(torch.empty(4, 70000, device="cuda", dtype=BF16), torch.empty(3, 70000, device="cuda", dtype=BF16), t[:4])
     with pytest.raises(m.EmbedPartError):
         m.ep_cross_entropy(torch.empty(4, 0, device="cuda", dtype=BF16), torch.empty(3, 0, device="cuda", dtype=BF16), t[:4])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("n_in", [17, 128, 256, 727, 1024, 4096])
+@pytest.mark.parametrize("stands_out", [0.0, 4.0])
+def test_sums_of_logits_lose_nothing_on_average(dtype, n_in, stands_out):
+    """The tensor cores cut sums off toward zero, a share of the sum that is given back.  With one class lse is the logit itself.  Of many
+    rows' logits the common share that is missing: a quarter of what was cut off, (2.5 + 1.5 steps) 1e-8 for bf16 and (5 + 1.9 steps) 1e-8 for
+    fp16 with a step of 16 products, and the roundings of the factors 1 / log 2 and log 2, 2^-24 each of themselves: 1.2e-7."""
+    rows, g = 65536, torch.Generator(device="cuda").manual_seed(n_in)
+    w = torch.randn(1, n_in, device="cuda", generator=g) / n_in ** 0.5
+    x = torch.randn(rows, n_in, device="cuda", generator=g) + stands_out * w
+    x, w = x.to(dtype), w.to(dtype)
+    lse = ep().ep_cross_entropy(x, w, torch.zeros(rows, device="cuda", dtype=torch.int32)).lse.double()
+    want = (x.double() * w.double()).sum(1)
+    steps = (n_in + 15) // 16
+    lost = (2.5 + 1.5 * steps if dtype is torch.bfloat16 else 5 + 1.9 * steps) * 1e-8
+    share = ((lse - want) * want).sum() / (want * want).sum()
+    assert abs(share.item()) <= 0.25 * lost + 1.2e-7
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows,n_in,classes", [(23406, 727, 23), (20000, 250, 5), (20000, 1000, 40)])
+def test_bias_gradient_of_many_rows_and_few_classes(dtype, rows, n_in, classes):
+    """What a logit is off in common is off in a sum over rows, too, where the slopes themselves nearly cancel: dbias is some 1e-3 and its
+    slopes up to 1.  With a quarter of what the sums lose (above) left, a row's logit l is off by less than 0.25 lost |l|, its slopes by less
+    than that and 2^-23 |l| more for the exponents' roundings, and dbias by no more than their mean."""
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    w = torch.randn(classes, n_in, device="cuda", generator=g) / n_in ** 0.5
+    t = torch.randint(0, classes, (rows,), device="cuda", generator=g)
+    x = torch.randn(rows, n_in, device="cuda", generator=g) + 4 * w[t]
+    x, w = x.to(dtype), w.to(dtype)
+    l = x.double() @ w.double().T
+    result = ep().ep_cross_entropy(x, w, t.int())._replace(lse=torch.logsumexp(l, 1).float())
+    got = ep().ep_cross_entropy_backward(x, w, t.int(), result, None, torch.ones(1, device="cuda"))
+    p = torch.exp(l - result.lse.double()[:, None])
+    p[torch.arange(rows, device="cuda"), t] -= 1.0
+    steps = (n_in + 15) // 16
+    lost = (2.5 + 1.5 * steps if dtype is torch.bfloat16 else 5 + 1.9 * steps) * 1e-8
+    most = (0.25 * lost + 2.0 ** -23) * l.abs().amax(1).mean()
+    assert (got[2].double() - p.mean(0)).abs().max() <= most
