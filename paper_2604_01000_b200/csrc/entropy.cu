@@ -1757,6 +1757,8 @@ int forward_run(ep_ctx *ctx, Inputs &in, const ForwardSpace &s, float *loss, flo
     return EP_OK;
 }
 
+// The columns' sums of this many pieces of rows are kept before they are joined to one: 2^20 rows of 2^17 classes would need 6 GB.
+constexpr int JOINED_PIECES = 16;
 struct Backward {
     Copies copies;
     void *g;
@@ -1767,6 +1769,7 @@ struct Backward {
     Pieces pieces;
     int blocks;           // of entropy_weights
     int64_t slabs;        // partial sums of a piece's columns
+    int64_t kept;         // and how many of all pieces are kept before they are joined
     size_t bytes;
 };
 Backward backward_space(const ep_ctx *ctx, int64_t rows, int n_in, int classes, int type, bool aligned, void *base) {
@@ -1796,7 +1799,8 @@ Backward backward_space(const ep_ctx *ctx, int64_t rows, int n_in, int classes, 
             s.slabs = 8 * (int64_t)most_of(p, rows, classes, [&](int64_t r, int c) {
                           return most_workers(line_of(ctx, ep::ceil_div(c, TILE), ep::ceil_div(r, TILE)));
                       });
-        s.part = a.take<float>((size_t)p.across * s.slabs * classes);
+        s.kept = p.across <= JOINED_PIECES ? p.across * s.slabs : JOINED_PIECES * s.slabs + 1;
+        s.part = a.take<float>((size_t)s.kept * classes);
     }
     const int64_t all = ep::ceil_div(rows, TILE) * TILE;
     s.rows = RowInfo{a.take<float>(all), a.take<float>(all), a.take<int>(all)};
@@ -1892,7 +1896,7 @@ int backward_run(ep_ctx *ctx, Inputs &in, const Backward &s, const Given &given,
     const size_t size = ep::type_size(in.type);
     const float *factor = in.type == EP_F16 ? &s.scale->down : nullptr;
     if (out.dbias && !f32)   // (not every piece has as many partial sums)
-        EP_CUDA(ctx, cudaMemsetAsync(s.part, 0, sizeof(float) * p.across * s.slabs * in.classes, in.stream));
+        EP_CUDA(ctx, cudaMemsetAsync(s.part, 0, sizeof(float) * s.kept * in.classes, in.stream));
     int64_t slab = 0;
     for (int64_t row0 = 0; row0 < in.rows; row0 += p.rows) {
         const int64_t rows = std::min(p.rows, in.rows - row0);
@@ -1926,6 +1930,13 @@ int backward_run(ep_ctx *ctx, Inputs &in, const Backward &s, const Given &given,
             if (rc != EP_OK) return rc;
         }
         slab += s.slabs;
+        if (out.dbias && row0 + p.rows < in.rows && slab + s.slabs > s.kept) {
+            rc = ep::sum_partials(ctx, s.part, (int)slab, in.classes, s.part, in.stream);   // (a block reads its columns before it writes them)
+            if (rc != EP_OK) return rc;
+            ++in.kernels;
+            if (!f32) EP_CUDA(ctx, cudaMemsetAsync(s.part + in.classes, 0, sizeof(float) * (s.kept - 1) * in.classes, in.stream));
+            slab = 1;
+        }
     }
     if (out.dweight && p.across > 1 && !f32) {
         rc = launch_round(ctx, in, s.dweight, (int64_t)in.classes * in.n_in, s.scale, out.dweight);

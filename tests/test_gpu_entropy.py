@@ -368,3 +368,26 @@ def test_bias_gradient_of_many_rows_and_few_classes(dtype, rows, n_in, classes):
     lost = (2.5 + 1.5 * steps if dtype is torch.bfloat16 else 5 + 1.9 * steps) * 1e-8
     most = (0.25 * lost + 2.0 ** -23) * l.abs().amax(1).mean()
     assert (got[2].double() - p.mean(0)).abs().max() <= most
+
+
+@pytest.mark.parametrize("dtype,rows", [(torch.bfloat16, 17 * 2048 + 300), (torch.float32, 34 * 1024 + 7)])
+def test_bias_gradient_over_more_pieces_of_rows_than_are_kept(dtype, rows):
+    """16384 classes by 2048 rows (16 bits) or 1024 (32) make a piece; more than 16 pieces' sums are joined on the way.  Slopes by the bounds
+    above, their sums rounded a few times: 2^-21 of the sum of magnitudes."""
+    n_in, classes = 264, 16384
+    x, w = rand((rows, n_in), dtype, 1), rand((classes, n_in), dtype, 2, 0.05)
+    t = some_targets(rows, classes, 3, dead=0.1)
+    result = ep().ep_cross_entropy(x, w, t)
+    got = ep().ep_cross_entropy_backward(x, w, t, result, None, torch.ones(1, device="cuda"), need_dx=False, need_dweight=False)[2]
+    want, off = torch.zeros(classes, device="cuda", dtype=torch.float64), torch.zeros(classes, device="cuda", dtype=torch.float64)
+    live = t >= 0
+    R = int(live.sum())
+    for i in range(0, rows, 4096):
+        l = x[i:i + 4096].double() @ w.double().T
+        lse = result.lse[i:i + 4096].double()[:, None]
+        p = torch.exp(l - lse)
+        e = logit_error(x[i:i + 4096], w, l) + 2.0 ** -19 + 2.0 ** -22 * (l.abs() + lse.abs())
+        hot = torch.nn.functional.one_hot(t[i:i + 4096].clamp(min=0).long(), classes)
+        want += ((p - hot) * live[i:i + 4096, None]).sum(0) / R
+        off += ((p * e + 2.0 ** -21 * (p + hot)) * live[i:i + 4096, None]).sum(0) / R
+    ref.within(got, want, off, "dbias")
