@@ -391,3 +391,61 @@ def test_bias_gradient_over_more_pieces_of_rows_than_are_kept(dtype, rows):
         want += ((p - hot) * live[i:i + 4096, None]).sum(0) / R
         off += ((p * e + 2.0 ** -21 * (p + hot)) * live[i:i + 4096, None]).sum(0) / R
     ref.within(got, want, off, "dbias")
+
+
+def near(got, want, what):
+    """Addresses are what is tested: values of another row would be off by as much as they are large."""
+    got, want = got.double(), want.double()
+    assert float((got - want).norm()) <= 2.0 ** -6 * float(want.norm()), what
+
+
+@pytest.mark.parametrize("n_in", [257, 256])
+def test_weights_whose_offsets_pass_32_bits(n_in):
+    classes, rows = (1 << 24) - 5, 24
+    chosen = torch.cat([torch.arange(700), torch.arange(classes // 2, classes // 2 + 700), torch.arange(classes - 700, classes)]).cuda()
+    some = rand((len(chosen), n_in), BF16, 1, n_in ** -0.5)
+    w = torch.zeros(classes, n_in, device="cuda", dtype=BF16)
+    w[chosen] = some
+    bias = torch.full((classes,), -math.inf, device="cuda")
+    bias[chosen] = 0.5
+    t = some_targets(rows, len(chosen), 2)
+    t[0], t[1] = len(chosen) - 1, 0
+    x = (rand((rows, n_in), F32, 3) + 4 * some.float()[t.long()]).to(BF16)
+    far = chosen[t.long()].int()
+    r, few = ep().ep_cross_entropy(x, w, far, bias), ep().ep_cross_entropy(x, some, t)
+    near(r.lse, few.lse + 0.5, "lse")
+    near(r.row_loss, few.row_loss, "row_loss")
+    one = torch.ones(1, device="cuda")
+    got, want = ep().ep_cross_entropy_backward(x, w, far, r, bias, one), ep().ep_cross_entropy_backward(x, some, t, few, None, one)
+    near(got.dx, want.dx, "dx")
+    near(got.dweight[chosen], want.dweight, "dweight")
+    near(got.dbias[chosen], want.dbias, "dbias")
+    got.dweight[chosen] = 0
+    got.dbias[chosen] = 0
+    assert int(torch.count_nonzero(got.dbias)) == 0
+    assert all(int(torch.count_nonzero(part)) == 0 for part in got.dweight.split(1 << 20))
+
+
+@pytest.mark.parametrize("rows,n_in", [(1 << 25, 136), ((1 << 24) - 77, 264)])
+def test_rows_whose_offsets_pass_32_bits(rows, n_in):
+    classes = 5
+    chosen = torch.cat([torch.arange(400), torch.arange(rows // 2, rows // 2 + 400), torch.arange(rows - 400, rows)]).cuda()
+    w = rand((classes, n_in), BF16, 1, n_in ** -0.5)
+    t = some_targets(len(chosen), classes, 2)
+    some = (rand((len(chosen), n_in), F32, 3) + 4 * w.float()[t.long()]).to(BF16)
+    x = torch.zeros(rows, n_in, device="cuda", dtype=BF16)
+    x[chosen] = some
+    x[rows // 4] = math.nan
+    far = torch.full((rows,), -1, device="cuda", dtype=torch.int32)
+    far[chosen] = t
+    r, few = ep().ep_cross_entropy(x, w, far), ep().ep_cross_entropy(some, w, t)
+    assert int(r.counted) == len(chosen)
+    near(r.lse[chosen], few.lse, "lse")
+    near(r.loss, few.loss, "loss")
+    one = torch.ones(1, device="cuda")
+    got, want = ep().ep_cross_entropy_backward(x, w, far, r, None, one), ep().ep_cross_entropy_backward(some, w, t, few, None, one)
+    near(got.dx[chosen], want.dx, "dx")
+    near(got.dweight, want.dweight, "dweight")
+    near(got.dbias, want.dbias, "dbias")
+    got.dx[chosen] = 0
+    assert all(int(torch.count_nonzero(part)) == 0 for part in got.dx.split(1 << 21))

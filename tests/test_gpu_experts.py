@@ -229,3 +229,25 @@ def test_refusals():
                 lambda: m.ep_experts(x.repeat(13, 1), router, w1, w2)):
         with pytest.raises(ValueError):
             bad()
+
+
+@pytest.mark.parametrize("rows", [1, 64])
+def test_parts_whose_offsets_pass_32_bits(rows):
+    """520 parts of 2048 x 4096 and 4096 x 2048 integers; the first and the last two are open, and come out as of a layer of these three."""
+    parts, n, hidden, chosen = 520, 4096, 2048, [0, 518, 519]
+    g = torch.Generator(device="cuda").manual_seed(5)
+    w1 = torch.zeros(parts, hidden, n, device="cuda", dtype=torch.int8)
+    w2 = torch.zeros(parts, n, hidden, device="cuda", dtype=torch.int8)
+    for e in chosen:
+        w1[e] = torch.randint(-127, 128, (hidden, n), generator=g, device="cuda")
+        w2[e] = torch.randint(-127, 128, (n, hidden), generator=g, device="cuda")
+    s1, s2 = (torch.rand(parts, m, generator=g, device="cuda") * 1e-4 + 1e-4 for m in (hidden, n))
+    x = torch.randn(rows, n, generator=g, device="cuda").to(BF16)
+    router = torch.randn(parts, n, generator=g, device="cuda").mul_(n ** -0.5).to(BF16)
+    closed = torch.full((parts,), -math.inf, device="cuda")
+    closed[chosen] = 0.0
+    got = ep().ep_experts(x, router, w1, w2, 2, router_bias=closed, w1_scale=s1, w2_scale=s2)
+    want = ep().ep_experts(x, router[chosen].contiguous(), w1[chosen].contiguous(), w2[chosen].contiguous(), 2, w1_scale=s1[chosen].contiguous(),
+                           w2_scale=s2[chosen].contiguous())
+    assert torch.equal(got.ids, torch.tensor(chosen, device="cuda", dtype=torch.int32)[want.ids.long()])
+    assert float((got.out.double() - want.out.double()).norm()) <= 2.0 ** -6 * float(want.out.double().norm())
