@@ -1307,70 +1307,60 @@ __global__ void __launch_bounds__(256) entropy_round(const float *__restrict__ s
 // ---------------------------------------------------------------------------------------------- small problems
 //
 // A few fp32 products cost the tile kernels mostly launches and passes (operands split in three, logits written and read back,
-// statistics or G, joins).  Then fp32 multiply-adds of tiles of 64 x 64 take the operands as they are: the forward is two
-// launches, the backward three to five.  Bound by their latency: a tile's sum is one chain of steps, each a load, a barrier and
-// the multiply-adds.  (fp32, tiles -> here, us.  Forward: 128 x 64 -> 32 11.1 -> 8.2, 50000 x 16 -> 40 30.6 -> 17.7, 200000 x 16 -> 10
-// 107 -> 48; but 16 x 160 -> 456 12.7 -> 14.4, 132 x 96 -> 7050 20 -> 52: long sums, few rows.  Backward: 128 x 64 -> 32 24.0 -> 20.3,
-// 500 x 64 -> 500 34.5 -> 26.4, 40 x 128 -> 4000 31.5 -> 27.3; but 500 x 256 -> 260 36 -> 43, 2000 x 64 -> 1000 44 -> 59.  In 16 bits, where
-// nothing is split, the tiles won at 22 of 24 sizes in each direction.)
-constexpr int ST = 64, SK = 32;   // a block's rows and columns; the step of the sum
-struct SmallTile {
-    float a[SK][ST + 4], b[SK][ST + 4];
-};
-// acc[i][j] = sum over k in [k0, k1) of A(4 ty + i, k) B(4 tx + j, k) of a tile; a_of and b_of give elements, and are asked for four of
-// one k (ALONG_ROWS: elements of one k lie next to one another) or for four k of one row.  Sums of 128 are added up (a long
-// sum of fp32 would lose bits).
-template <bool A_ALONG, bool B_ALONG, typename A, typename B, typename Step>
-__device__ __forceinline__ void small_product(SmallTile &s, int64_t k0, int64_t k1, A a_of, B b_of, Step each_step, float (&total)[4][4]) {
-    const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
-    // which elements of a step this thread brings: eight k of one row, or four rows of two k
-    constexpr int E = ST * SK / 256;
-    auto row_of = [&](bool along, int i) { return along ? (t & 15) * 4 + (i & 3) : t >> 2; };
-    auto k_of = [&](bool along, int i) { return along ? (t >> 4) + 16 * (i >> 2) : (t & 3) * E + i; };
-    float acc[4][4] = {}, pa[E], pb[E];
+// statistics or G, joins: ten launches of a backward).  Then fp32 multiply-adds of tiles of 64 x 64 take the operands as they are: the
+// forward is two launches, the backward two to four.  Bound by latency, then by what the shared memory gives the multiply-adds: a thread
+// has 4 x 4 logits (8 16-byte reads to 64 multiply-adds) or 4 rows of n_in / 16 columns of the second product.
+// fp32, tiles -> here, us.  Forward: 128 x 64 -> 32 12.2 -> 8.5, 500 x 64 -> 500 13.2 -> 9.8, 3000 x 65 -> 257 16.2 -> 13.0, 50000 x 16 -> 40
+// 30 -> 16, 200000 x 16 -> 10 109 -> 45; but 2000 x 128 -> 257 14.8 -> 18.0, 40 x 128 -> 4000 16 -> 27 (statistics of many classes).  Backward:
+// 128 x 64 -> 32 24.8 -> 11.5, 500 x 64 -> 500 34.9 -> 14.1, 40 x 128 -> 4000 31.8 -> 18.4, 3000 x 65 -> 257 41.6 -> 32.7, 18 x 42 -> 77887
+// 123 -> 77; but 2000 x 128 -> 257 37.8 -> 45.7, 64 x 128 -> 16384 45 -> 57, 2000 x 64 -> 1000 44 -> 56.  In 16 bits, where nothing is split, the
+// tiles won at nearly every size.
+constexpr int ST = 64;            // a block's rows of either operand
+constexpr int SMALL_BLOCKS = 1;   // to an SM, of either gradient's
+constexpr int SMALL_WIDTH = 128;  // elements of a row at most
+// 64 rows on their way to shared memory, LD floats apart, zero past their n_in elements and past the last row.
+template <int LD, typename Wanted>
+__device__ __forceinline__ void small_rows(float *to, const float *from, int64_t ld, int64_t row0, int64_t rows, int n_in, Wanted wanted) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int q = 0; q < ST / 8; ++q) {
+        const int r = (threadIdx.x >> 5) + 8 * q;
+        const bool there = row0 + r < rows && wanted(row0 + r);
+#pragma unroll
+        for (int c0 = 0; c0 < LD - 4; c0 += 32) {
+            const int c = c0 + lane;
+            if (c < LD - 4) {
+                const bool in = there && c < n_in;
+                const float *src = in ? from + (row0 + r) * ld + c : from;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(to + r * LD + c)), "l"(src), "r"(in ? 4 : 0) : "memory");
+            }
+        }
+    }
+}
+// s[i][j] = p_(4 ty + i) . q_(tx + 16 j); rows LD floats apart, which keeps the lanes of a 16-byte access in different banks.
+template <int LD>
+__device__ __forceinline__ void small_products(const float *p, const float *q, int n_in, int tx, int ty, float (&s)[4][4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) total[i][j] = 0.f;
-    auto bring = [&](int64_t k) {
+        for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 2
+    for (int k = 0; k < n_in; k += 4) {
+        float4 a[4], b[4];
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const int64_t ka = k + k_of(A_ALONG, i), kb = k + k_of(B_ALONG, i);
-            pa[i] = ka < k1 ? a_of(row_of(A_ALONG, i), ka) : 0.f;
-            pb[i] = kb < k1 ? b_of(row_of(B_ALONG, i), kb) : 0.f;
+        for (int i = 0; i < 4; ++i) {
+            a[i] = *reinterpret_cast<const float4 *>(p + (4 * ty + i) * LD + k);
+            b[i] = *reinterpret_cast<const float4 *>(q + (tx + 16 * i) * LD + k);
         }
-    };
-    bring(k0);
-    int steps = 0;
-    for (int64_t k = k0; k < k1; k += SK) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            s.a[k_of(A_ALONG, i)][row_of(A_ALONG, i)] = pa[i];
-            s.b[k_of(B_ALONG, i)][row_of(B_ALONG, i)] = pb[i];
-        }
-        __syncthreads();
-        if (k + SK < k1) bring(k + SK);
-        each_step();
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int q = 0; q < SK; ++q) {
-            const float4 x = *reinterpret_cast<const float4 *>(&s.a[q][4 * ty]), y = *reinterpret_cast<const float4 *>(&s.b[q][4 * tx]);
-            const float xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(xs[i], ys[j], acc[i][j]);
-        }
-        if (++steps == 128 / SK || k + SK >= k1) {
-            steps = 0;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    total[i][j] += acc[i][j];
-                    acc[i][j] = 0.f;
-                }
-        }
-        __syncthreads();
+            for (int j = 0; j < 4; ++j) {
+                s[i][j] = fmaf(a[i].x, b[j].x, s[i][j]);
+                s[i][j] = fmaf(a[i].y, b[j].y, s[i][j]);
+                s[i][j] = fmaf(a[i].z, b[j].z, s[i][j]);
+                s[i][j] = fmaf(a[i].w, b[j].w, s[i][j]);
+            }
     }
 }
 
@@ -1389,8 +1379,6 @@ struct SmallWork {
     unsigned *ticket;
     const float *lse;         // backward
     RowInfo info;
-    float *g;                 // [rows][ldg]
-    int ldg;
     int dx_splits, dw_splits; // shares of the sums over classes and over rows
     int64_t dx_blocks;
     float *dx_part, *dw_part, *db_part;   // [share][..], or the outputs themselves are written
@@ -1398,108 +1386,181 @@ struct SmallWork {
 };
 // What the tile kernels make of an infinity among fp32 operands, which split into NaN: an infinite logit is no logit.
 __device__ __forceinline__ float small_logit(float v) { return isinf(v) ? CUDART_NAN_F : v; }
-// One tile of logits: statistics of its rows (forward) or G (backward).
-template <bool GRAD>
-__global__ void __launch_bounds__(256) entropy_small_logits(const SmallWork e) {
-    __shared__ SmallTile s;
+// Statistics of a tile's rows.  J = ceil(n_in / 16).
+template <int J>
+__global__ void __launch_bounds__(256) entropy_small_forward(const SmallWork e) {
+    constexpr int LD = 16 * J + 4;
+    extern __shared__ float4 small_memory[];
+    float *const p = reinterpret_cast<float *>(small_memory), *const q = p + ST * LD;
     const int64_t row0 = (int64_t)blockIdx.y * ST;
     const int class0 = blockIdx.x * ST, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    auto all = [](int64_t) { return true; };
     ep_wait_for_launch_before();
-    if (!GRAD && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *e.ticket = 0;
-    float v[4][4];
-    small_product<false, false>(
-        s, 0, e.n_in, [&](int m, int64_t k) { return row0 + m < e.rows ? e.x[(row0 + m) * e.ldx + k] : 0.f; },
-        [&](int n, int64_t k) { return class0 + n < e.classes ? e.w[(class0 + n) * e.ldw + k] : 0.f; }, [] {}, v);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *e.ticket = 0;
+    small_rows<LD>(p, e.x, e.ldx, row0, e.rows, e.n_in, all);
+    small_rows<LD>(q, e.w, e.ldw, class0, e.classes, e.n_in, all);
+    copies_end_group();
     float bias[4];
+    int target[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) bias[j] = e.bias && class0 + 4 * tx + j < e.classes ? load_param(e.bias, e.bias_type, class0 + 4 * tx + j) : 0.f;
+    for (int j = 0; j < 4; ++j) {
+        const int c = class0 + tx + 16 * j;
+        bias[j] = e.bias && c < e.classes ? load_param(e.bias, e.bias_type, c) : 0.f;
+        target[j] = row0 + 4 * ty + j < e.rows ? e.targets[row0 + 4 * ty + j] : -1;
+    }
+    copies_wait<0>();
+    __syncthreads();
+    float s[4][4];
+    small_products<LD>(p, q, e.n_in, tx, ty, s);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int64_t row = row0 + 4 * ty + i;
-        const bool there = row < e.rows;
-        if constexpr (GRAD) {
-            if (!there) continue;
-            const int target = e.info.target[row];
-            const float g = e.info.g[row], z = e.lse[row];
+        Running r{-INFINITY, 0.f};
+        float l[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int c = class0 + tx + 16 * j;
+            l[j] = c < e.classes ? small_logit(s[i][j]) + bias[j] : -INFINITY;
+            if (c == target[i] && c < e.classes) e.at_target[row] = l[j];
+            r.m = fmaxf(r.m, l[j]);
+        }
+        const float shift = r.m == -INFINITY ? 0.f : r.m;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r.s += exp_fast(l[j] - shift);
+#pragma unroll
+        for (int o = 8; o >= 1; o >>= 1) r = join(r, Running{__shfl_xor_sync(FULL, r.m, o), __shfl_xor_sync(FULL, r.s, o)});
+        if (tx == 0 && row < e.rows) e.stats[(int64_t)blockIdx.x * e.rows + row] = make_float2(r.m, r.s);
+    }
+}
+// Gradient of 64 rows of x (P = x, Q = W), or of W (P = W, Q = x): over its share of Q, 64 rows at a time, the logits, G of them, G Q.
+// (Either makes all logits: it needs a third more multiply-adds than G written and read back, and two launches less.)
+template <bool DW, int J>
+__device__ __forceinline__ void small_gradient(const SmallWork &e, int64_t block, float *memory) {
+    constexpr int LD = 16 * J + 4, LDG = ST + 4;
+    float *const p = memory, *const q = p + ST * LD, *const g = q + 2 * ST * LD;   // q: two tiles; g[row of Q][row of P]
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const int splits = DW ? e.dw_splits : e.dx_splits, share = (int)(block % splits);
+    const int64_t P = DW ? e.classes : e.rows, Q = DW ? e.rows : e.classes, p0 = block / splits * ST, tiles = (Q + ST - 1) / ST;
+    const int64_t t0 = tiles * share / splits, t1 = tiles * (share + 1) / splits;
+    auto bring = [&](int64_t tile) {
+        // (a row that takes no part counts for nothing, whatever it holds)
+        small_rows<LD>(q + (tile & 1) * ST * LD, DW ? e.x : e.w, DW ? e.ldx : e.ldw, tile * ST, Q, e.n_in,
+                       [&](int64_t r) { return !DW || e.info.target[r] >= 0; });
+    };
+    small_rows<LD>(p, DW ? e.w : e.x, DW ? e.ldw : e.ldx, p0, P, e.n_in, [](int64_t) { return true; });
+    if (t0 < t1) bring(t0);
+    copies_end_group();
+    // what is known of rows of x (target, g, lse) and of classes (bias), of either operand
+    struct Known {
+        int target[4];
+        float g[4], z[4], bias[4];
+    };
+    auto known = [&](bool rows, int64_t first, int step, Known &k) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t at = first + i * step;
+            if (rows) {
+                k.target[i] = at < e.rows ? e.info.target[at] : -1;
+                k.g[i] = k.target[i] >= 0 ? e.info.g[at] : 0.f;
+                k.z[i] = k.target[i] >= 0 ? e.lse[at] : 0.f;
+            } else
+                k.bias[i] = e.bias && at < e.classes ? load_param(e.bias, e.bias_type, at) : 0.f;
+        }
+    };
+    Known k;
+    known(!DW, p0 + 4 * ty, 1, k);
+    float total[4][J];
+    double column[4] = {};   // of dbias
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < J; ++j) total[i][j] = 0.f;
+    for (int64_t tile = t0; tile < t1; ++tile) {
+        const int64_t q0 = tile * ST;
+        const float *const mine = q + (tile & 1) * ST * LD;
+        known(DW, q0 + tx, 16, k);
+        copies_wait<0>();
+        __syncthreads();
+        if (tile + 1 < t1) {
+            bring(tile + 1);
+            copies_end_group();
+        }
+        float s[4][4];
+        small_products<LD>(p, mine, e.n_in, tx, ty, s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int c = class0 + 4 * tx + j;
-                const float p = exp_fast(small_logit(v[i][j]) + bias[j] - z) - (c == target ? 1.f : 0.f);
-                if (c < e.ldg) e.g[row * e.ldg + c] = target >= 0 && c < e.classes ? p * g : 0.f;
+                const int r = DW ? j : i, c = DW ? i : j;
+                const int64_t one_class = DW ? p0 + 4 * ty + i : q0 + tx + 16 * j;
+                const float share_of_class = exp_fast(small_logit(s[i][j]) + k.bias[c] - k.z[r]) - (one_class == k.target[r] ? 1.f : 0.f);
+                s[i][j] = k.target[r] >= 0 && one_class < e.classes ? share_of_class * k.g[r] : 0.f;
             }
-        } else {
-            const int target = there ? e.targets[row] : -1;
-            Running r{-INFINITY, 0.f};
-            float l[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int c = class0 + 4 * tx + j;
-                l[j] = c < e.classes ? small_logit(v[i][j]) + bias[j] : -INFINITY;
-                if (there && c == target) e.at_target[row] = l[j];
-                r.m = fmaxf(r.m, l[j]);
+        for (int j = 0; j < 4; ++j)
+            *reinterpret_cast<float4 *>(g + (tx + 16 * j) * LDG + 4 * ty) = make_float4(s[0][j], s[1][j], s[2][j], s[3][j]);
+        if (DW)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) column[i] += (double)((s[i][0] + s[i][1]) + (s[i][2] + s[i][3]));
+        __syncthreads();
+        float acc[4][J];   // of this tile: a long sum of fp32 would lose bits
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < J; ++j) acc[i][j] = 0.f;
+#pragma unroll 4
+        for (int r = 0; r < ST; ++r) {
+            const float4 a = *reinterpret_cast<const float4 *>(g + r * LDG + 4 * ty);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const float b = mine[r * LD + tx + 16 * j];
+                acc[0][j] = fmaf(a.x, b, acc[0][j]);
+                acc[1][j] = fmaf(a.y, b, acc[1][j]);
+                acc[2][j] = fmaf(a.z, b, acc[2][j]);
+                acc[3][j] = fmaf(a.w, b, acc[3][j]);
             }
-            const float shift = r.m == -INFINITY ? 0.f : r.m;
+        }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) r.s += exp_fast(l[j] - shift);
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int o = 8; o >= 1; o >>= 1) r = join(r, Running{__shfl_xor_sync(FULL, r.m, o), __shfl_xor_sync(FULL, r.s, o)});
-            if (tx == 0 && there) e.stats[(int64_t)blockIdx.x * e.rows + row] = make_float2(r.m, r.s);
+            for (int j = 0; j < J; ++j) total[i][j] += acc[i][j];
+    }
+    copies_wait<0>();
+    float *const part = DW ? e.dw_part : e.dx_part, *const out = DW ? e.dweight : e.dx;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t m = p0 + 4 * ty + i;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int n = tx + 16 * j;
+            if (m >= P || n >= e.n_in) continue;
+            if (splits > 1)
+                part[((int64_t)share * P + m) * e.n_in + n] = total[i][j];
+            else if (out)
+                out[m * e.n_in + n] = total[i][j];
+        }
+        if (DW && e.dbias) {
+#pragma unroll
+            for (int o = 8; o >= 1; o >>= 1) column[i] += __shfl_xor_sync(FULL, column[i], o);
+            if (tx == 0 && m < P) {
+                if (splits > 1)
+                    e.db_part[(int64_t)share * P + m] = (float)column[i];
+                else
+                    e.dbias[m] = (float)column[i];
+            }
         }
     }
 }
-// dx = G W and dW = G^T x, a tile and a share of the sum to a block; dbias with the first column of tiles of dW.
-__global__ void __launch_bounds__(256) entropy_small_products(const SmallWork e) {
-    __shared__ SmallTile s;
-    const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
-    const int across = (e.n_in + ST - 1) / ST;
+template <int J>
+__global__ void __launch_bounds__(256, 2) entropy_small_backward(const SmallWork e) {
+    extern __shared__ float4 small_memory[];
+    float *const memory = reinterpret_cast<float *>(small_memory);
     ep_wait_for_launch_before();
-    const bool is_dx = (int64_t)blockIdx.x < e.dx_blocks;
-    int64_t b = is_dx ? blockIdx.x : blockIdx.x - e.dx_blocks;
-    const int splits = is_dx ? e.dx_splits : e.dw_splits, share = (int)(b % splits);
-    b /= splits;
-    const int64_t m0 = b / across * ST, all = is_dx ? e.classes : e.rows, ms = is_dx ? e.rows : e.classes;
-    const int n0 = (int)(b % across) * ST;
-    const int64_t each = ((all + splits - 1) / splits + SK - 1) / SK * SK, k0 = min(share * each, all), k1 = min(k0 + each, all);
-    float v[4][4];
-    double column = 0.0;   // of dbias: class m0 + t
-    if (is_dx)
-        small_product<false, true>(
-            s, k0, k1, [&](int m, int64_t k) { return m0 + m < e.rows ? e.g[(m0 + m) * e.ldg + k] : 0.f; },
-            [&](int n, int64_t k) { return n0 + n < e.n_in ? e.w[k * e.ldw + n0 + n] : 0.f; }, [] {}, v);
+    ep_let_next_launch_start();
+    if ((int64_t)blockIdx.x < e.dx_blocks)
+        small_gradient<false, J>(e, blockIdx.x, memory);
     else
-        small_product<true, true>(
-            s, k0, k1, [&](int m, int64_t k) { return m0 + m < e.classes ? e.g[k * e.ldg + m0 + m] : 0.f; },
-            // (a row that takes no part counts for nothing, whatever it holds)
-            [&](int n, int64_t k) { return n0 + n < e.n_in && e.info.target[k] >= 0 ? e.x[k * e.ldx + n0 + n] : 0.f; },
-            [&] {
-                if (n0 == 0 && t < ST) {
-                    float here = 0.f;
-#pragma unroll
-                    for (int q = 0; q < SK; ++q) here += s.a[q][t];
-                    column += (double)here;
-                }
-            },
-            v);
-    float *part = is_dx ? e.dx_part : e.dw_part, *out = is_dx ? e.dx : e.dweight;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t m = m0 + 4 * ty + i;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int n = n0 + 4 * tx + j;
-            if (m >= ms || n >= e.n_in) continue;
-            if (splits > 1)
-                part[((int64_t)share * ms + m) * e.n_in + n] = v[i][j];
-            else if (out)
-                out[m * e.n_in + n] = v[i][j];
-        }
-    }
-    if (!is_dx && n0 == 0 && t < ST && m0 + t < e.classes && e.dbias) {
-        if (splits > 1)
-            e.db_part[(int64_t)share * e.classes + m0 + t] = (float)column;
-        else
-            e.dbias[m0 + t] = (float)column;
-    }
+        small_gradient<true, J>(e, blockIdx.x - e.dx_blocks, memory);
 }
 // The shares: LANES lanes to an element, each every LANES-th share in order, then the lanes (in a fixed order).
 template <int LANES>
@@ -2059,23 +2120,31 @@ int narrow_backward_run(ep_ctx *ctx, Inputs &in, const NarrowSpace &s, const Giv
 }
 
 // ---- small problems
-// (what was measured on both sides stands at the kernels)
+// (What was measured on both sides stands at the kernels.)  Tiles of 64 x 64 cost the same however little of them there is, and the tile
+// kernels' k-blocks of 64 elements as much for fewer.
 bool small_problem(bool grad, int64_t rows, int n_in, int classes, int type) {
-    const int64_t logits = rows * classes;
-    return type == EP_F32 && n_in <= 128 && (grad || classes <= 1024) && rows <= 1 << 20 && logits <= 1 << 22 && logits * n_in <= 1 << 25;
+    if (type != EP_F32 || n_in > SMALL_WIDTH || rows > 1 << 20 || (!grad && classes > 512)) return false;
+    return ep::ceil_div(rows, ST) * ST * (ep::ceil_div(classes, ST) * ST) * n_in <= (n_in <= 48 ? 1 << 28 : 1 << 26);
 }
-// Shares of a sum over `all` so that `tiles` tiles make about three blocks an SM, of at least 128 each.
+// f(J) with J = ceil(n_in / 16).
+template <int J = 1, typename F>
+int small_width(int n_in, F f) {
+    if constexpr (J < SMALL_WIDTH / 16)
+        if (n_in > 16 * J) return small_width<J + 1>(n_in, f);
+    return f(std::integral_constant<int, J>{});
+}
+// Shares of a sum over `all` rows of the other operand, so that `tiles` tiles make about two blocks an SM.
 int small_splits(const ep_ctx *ctx, int64_t tiles, int64_t all) {
-    return (int)std::max<int64_t>(1, std::min<int64_t>(ctx->sm_count * 3 / std::max<int64_t>(tiles, 1), ep::ceil_div(all, 2 * ST)));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(ctx->sm_count * SMALL_BLOCKS / std::max<int64_t>(tiles, 1), ep::ceil_div(all, ST)));
 }
 struct SmallSpace {
     float2 *stats;
-    float *at_target, *g, *dx_part, *dw_part, *db_part, *peaks;
+    float *at_target, *dx_part, *dw_part, *db_part, *peaks;
     Finish finish;
     RowInfo rows;
     int *unclean;
     Scale *scale;
-    int ldg, dx_splits, dw_splits;
+    int dx_splits, dw_splits;
     int64_t dx_tiles, dw_tiles;
     size_t bytes;
 };
@@ -2089,15 +2158,13 @@ SmallSpace small_space(const ep_ctx *ctx, bool grad, int64_t rows, int n_in, int
         s.finish.counts = a.take<long long>(ep::ceil_div(rows, FINISH_ROWS));
         s.finish.ticket = a.take<unsigned>(1);
     } else {
-        const int64_t all = ep::ceil_div(rows, TILE) * TILE, across = ep::ceil_div(n_in, ST);
-        s.ldg = (classes + 3) & ~3;
-        s.g = a.take<float>(rows * s.ldg);
+        const int64_t all = ep::ceil_div(rows, TILE) * TILE;
         s.rows = RowInfo{a.take<float>(all), a.take<float>(all), a.take<int>(all)};
         s.peaks = a.take<float>(weight_blocks(ctx, rows));
         s.unclean = a.take<int>(weight_blocks(ctx, rows));
         s.scale = a.take<Scale>(1);
-        s.dx_tiles = ep::ceil_div(rows, ST) * across;
-        s.dw_tiles = ep::ceil_div(classes, ST) * across;
+        s.dx_tiles = ep::ceil_div(rows, ST);
+        s.dw_tiles = ep::ceil_div(classes, ST);
         s.dx_splits = small_splits(ctx, s.dx_tiles, classes);
         s.dw_splits = small_splits(ctx, s.dw_tiles, rows);
         s.dx_part = a.take<float>(s.dx_splits > 1 ? (size_t)s.dx_splits * rows * n_in : 0);
@@ -2127,8 +2194,15 @@ int small_forward(ep_ctx *ctx, Inputs &in, const SmallSpace &s, float *loss, flo
     e.stats = s.stats;
     e.at_target = s.at_target;
     e.ticket = s.finish.ticket;
-    EP_CUDA(ctx, ep::launch_early(entropy_small_logits<false>, dim3((unsigned)e.class_tiles, (unsigned)ep::ceil_div(in.rows, ST)), dim3(256), 0,
-                                  in.stream, e));
+    const int rc = small_width(in.n_in, [&](auto j) {
+        constexpr int J = decltype(j)::value;
+        constexpr size_t smem = sizeof(float) * 2 * ST * (16 * J + 4);
+        EP_CUDA(ctx, cudaFuncSetAttribute(entropy_small_forward<J>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        EP_CUDA(ctx, ep::launch_early(entropy_small_forward<J>, dim3((unsigned)e.class_tiles, (unsigned)ep::ceil_div(in.rows, ST)), dim3(256), smem,
+                                      in.stream, e));
+        return (int)EP_OK;
+    });
+    if (rc != EP_OK) return rc;
     Finish f = s.finish;
     f.loss = loss;
     f.counted = counted;
@@ -2140,16 +2214,16 @@ int small_forward(ep_ctx *ctx, Inputs &in, const SmallSpace &s, float *loss, flo
 }
 int small_backward(ep_ctx *ctx, Inputs &in, const SmallSpace &s, const Given &g, const Wanted &out) {
     const int blocks = weight_blocks(ctx, in.rows);
-    entropy_weights<float><<<blocks, WEIGHT_THREADS, 0, in.stream>>>(g.lse, in.targets, in.rows, in.classes, g.counted, g.dloss, g.drow, nullptr, 0, 0,
-                                                                 nullptr, 0, nullptr, s.rows, s.peaks, s.unclean, false, s.scale, ctx->d_status);
+    entropy_weights<float><<<blocks, WEIGHT_THREADS, 0, in.stream>>>(g.lse, in.targets, in.rows, in.classes, g.counted, g.dloss, g.drow, nullptr, 0,
+                                                                     0, nullptr, 0, nullptr, s.rows, s.peaks, s.unclean, false, s.scale,
+                                                                     ctx->d_status);
     EP_CUDA(ctx, cudaGetLastError());
+    const bool over_rows = out.dweight || out.dbias;
     SmallWork e = small_work(in);
     e.lse = g.lse;
     e.info = s.rows;
-    e.g = s.g;
-    e.ldg = s.ldg;
-    e.dx_splits = out.dx ? s.dx_splits : 1;
-    e.dw_splits = out.dweight || out.dbias ? s.dw_splits : 1;
+    e.dx_splits = s.dx_splits;
+    e.dw_splits = s.dw_splits;
     e.dx_blocks = out.dx ? s.dx_tiles * s.dx_splits : 0;
     e.dx_part = s.dx_part;
     e.dw_part = s.dw_part;
@@ -2157,23 +2231,28 @@ int small_backward(ep_ctx *ctx, Inputs &in, const SmallSpace &s, const Given &g,
     e.dx = static_cast<float *>(out.dx);
     e.dweight = static_cast<float *>(out.dweight);
     e.dbias = out.dbias;
-    EP_CUDA(ctx, ep::launch_early(entropy_small_logits<true>, dim3((unsigned)e.class_tiles, (unsigned)ep::ceil_div(in.rows, ST)), dim3(256), 0,
-                                  in.stream, e));
-    const int64_t dw_blocks = out.dweight || out.dbias ? s.dw_tiles * s.dw_splits : 0;
-    EP_CUDA(ctx, ep::launch_early(entropy_small_products, dim3((unsigned)(e.dx_blocks + dw_blocks)), dim3(256), 0, in.stream, e));
-    in.kernels += 3;
+    const int64_t grid = e.dx_blocks + (over_rows ? s.dw_tiles * s.dw_splits : 0);
+    const int rc = small_width(in.n_in, [&](auto j) {
+        constexpr int J = decltype(j)::value;
+        constexpr size_t smem = sizeof(float) * (3 * ST * (16 * J + 4) + ST * (ST + 4));
+        EP_CUDA(ctx, cudaFuncSetAttribute(entropy_small_backward<J>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        EP_CUDA(ctx, ep::launch_early(entropy_small_backward<J>, dim3((unsigned)grid), dim3(256), smem, in.stream, e));
+        return (int)EP_OK;
+    });
+    if (rc != EP_OK) return rc;
+    in.kernels += 2;
     // many shares: a warp to an element
     auto fold = [&](const float *part, int splits, int64_t n, float *to, const float *more_part, int64_t more, float *more_to) {
-        if (splits == 1) return cudaSuccess;
+        if (splits == 1 || n + more == 0) return cudaSuccess;
         ++in.kernels;
         const int lanes = splits > 16 ? 32 : 1;
         auto kernel = lanes > 1 ? entropy_small_fold<32> : entropy_small_fold<1>;
         return ep::launch_early(kernel, dim3((unsigned)ep::ceil_div((n + more) * lanes, 256)), dim3(256), 0, in.stream, part, splits, n, to,
                                 more_part, more, more_to);
     };
-    EP_CUDA(ctx, fold(e.dx_part, e.dx_splits, in.rows * in.n_in, e.dx, nullptr, 0, nullptr));
-    EP_CUDA(ctx, fold(e.dw_part, e.dw_splits, out.dweight ? (int64_t)in.classes * in.n_in : 0, e.dweight, e.db_part,
-                      out.dbias ? in.classes : 0, out.dbias));
+    EP_CUDA(ctx, fold(e.dx_part, e.dx_splits, out.dx ? in.rows * in.n_in : 0, e.dx, nullptr, 0, nullptr));
+    EP_CUDA(ctx, fold(e.dw_part, e.dw_splits, out.dweight ? (int64_t)in.classes * in.n_in : 0, e.dweight, e.db_part, out.dbias ? in.classes : 0,
+                      out.dbias));
     return EP_OK;
 }
 
