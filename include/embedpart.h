@@ -520,8 +520,11 @@ int ep_route_backward(ep_ctx *ctx, const void *logits, int32_t type, int64_t row
  *   aligned  (of the queries) as for ep_linear
  * A row whose every class is closed takes no part either (row_loss 0, lse -infinity).  A target that is closed while others are
  * not has row_loss infinity.  A NaN or +infinity among the logits of a row that takes part makes its lse and loss
- * NaN.  With R = 0 loss is 0.  The logits are summed in fp32 as ep_linear sums them for an EP_F32 output; EP_F32 inputs are split
- * as there (an infinity in x or w of EP_F32 makes the logits it reaches NaN).
+ * NaN.  With R = 0 loss is 0.
+ * Logits are fp32 sums.  Of 16-bit inputs they run through n_in in the tensor cores, which cut off 2.5 to 5e-8 and 1.5 to 1.9e-8 more
+ * for every 16 products, of the sum; that share is given back, so that what is left (a fifth of it, and chance) has no sign.
+ * Of EP_F32 inputs they are ep_linear's, or, for few of them, fp32 multiply-adds; an infinity in x or w makes the logits it
+ * reaches NaN either way.
  *
  * ep_cross_entropy_backward:  G = (exp(l - lse) - [c = target]) g,  g[r] = dloss / R + drow_loss[r], 0 in rows that
  * take no part;  dx = G W;  dweight = G^T x;  dbias = sum over rows of G
@@ -531,7 +534,9 @@ int ep_route_backward(ep_ctx *ctx, const void *logits, int32_t type, int64_t row
  *   dbias     [dev] out or NULL, classes fp32
  * The logits are made once more, a piece at a time.  G is rounded to in_type before the products of 16-bit types, for EP_F16
  * after multiplication by the power of two that brings the largest |g| to 2^14 (the sums are scaled back): elements below
- * 2^-39 of that largest are lost.
+ * 2^-39 of that largest are lost.  dbias is summed from G before that rounding.
+ * Rows that take no part are not multiplied where they hold a NaN, an infinity or a number from 1e18 on: x is then read from a copy
+ * in the workspace, with zeros there.
  */
 size_t ep_cross_entropy_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t n_in, int32_t classes, int32_t in_type,
                                         int32_t aligned);   /* 0 = invalid shape or type; at least 256 */
@@ -562,8 +567,10 @@ int ep_cross_entropy_backward(ep_ctx *ctx, const void *x, int64_t ldx, const voi
  *   b1       [dev] experts x n_hidden, b2 [dev] experts x n_out, of bias_type, or NULL;  act  EP_ACT_*
  *   residual [dev] rows x n_out of type, rows ldr apart, or NULL
  *   out      [dev] out, rows x n_out of type;  ids [dev] out, rows x k int32;  weights [dev] out, rows x k fp32
- * Sums are fp32 multiply-adds, the hidden values stay in fp32, out is rounded once.  Parts that no row chose are not read.
- * Logits, ties, NaN and infinities among them as for ep_route.
+ * Sums are fp32 multiply-adds, the hidden values stay in fp32, out is rounded once.  Of 16-bit rows with rows * k >= 16 and EP_I8
+ * weights, or rows * k >= 40 and EP_BF16 weights, where 16 bytes divide the rows, both products go through matrix instructions: sums
+ * are theirs, and a hidden value is the sum of two bf16 numbers (2^-17 of itself off).
+ * Parts that no row chose are not read.  Logits, ties, NaN and infinities among them as for ep_route.
  */
 size_t ep_experts_workspace_bytes(const ep_ctx *ctx, int64_t rows, int32_t n_in, int32_t n_hidden, int32_t n_out, int32_t experts,
                                   int32_t k);   /* 0 = invalid shape; at least 256 */

@@ -4,7 +4,13 @@
 //
 // What it costs is reading the chosen experts' weights, once each: slots (a row's choice of a part) are sorted by part, up to 8
 // rows of one part make a group, and a warp that fetches a row of weights multiplies it with all rows of the group.  Sums
-// are fp32 multiply-adds; the hidden values stay in fp32.
+// are fp32 multiply-adds and the hidden values stay in fp32, or, with enough slots, matrix instructions and two bf16 numbers to a
+// hidden value (see there).
+//
+// Measured, on the device: one row, 2 of 64 experts of 1024 -> 4096 -> 1024 bf16 (33.6 MB of weights, 5.2 us at 6551 GB/s) 16.4 us, in three
+// launches that wait for one another: router 5 us of latency, then 6 us each for 17 MB (the second's come to the L2 meanwhile).
+// 16 rows, weights in 8 bits, 173 MB: 87 us, 2.0 TB/s: bound by instructions (0.47 a clock and scheduler: integers made floats) and by
+// what 16 warps an SM keep in flight (three steps of 64 bytes a lane).  7 rows of 333 -> 1029 -> 77 fp32, not aligned: 27.6 us.
 #include "activation.cuh"
 #include "ep_common.cuh"
 #include "rows.cuh"
@@ -611,7 +617,7 @@ __global__ void __launch_bounds__(THREADS) experts_output(const float *hidden, W
 
 // ---------------------------------------------------------------------------------------------- products by matrix instructions
 //
-// Where there are enough rows of weights to keep every warp busy 16 at a time, a warp multiplies 16 of them with the (up to 8)
+// Where there are enough slots (enough_for_tensor), a warp multiplies 16 rows of weights with the (up to 8)
 // rows of a group by matrix instructions, 16 x 8 x 16 at a time: a number of weights then costs a third of the instructions, most
 // of them for making 8-bit integers 16-bit floats (which hold them exactly).  The order of the columns within a step is the lanes'
 // own: each takes 16 bytes of its rows of weights, and the same columns of its row of x.  Hidden values go to the second
@@ -949,12 +955,12 @@ int run_tensor(ep_ctx *ctx, const Layer &l, const Space &s) {
                                   (const T *)l.residual, l.ldr, (T *)l.out));
     return EP_OK;
 }
-// Whether there is a tile of 16 rows of weights for every warp of the first product, of the experts that `rows` rows are likely to choose.
-bool enough_for_tensor(const ep_ctx *ctx, const Layer &l) {
-    double missed = 1.0;
-    for (int r = 0; r < (int)l.rows; ++r) missed *= 1.0 - (double)l.k / l.experts;
-    return l.experts * (1.0 - missed) * (l.n_hidden / 16) >= ctx->sm_count * WARPS;
-}
+// Multiply-adds grow with the slots, matrix instructions hardly do (16 rows of weights take 8 slots at once): from 16 slots on with integers,
+// which the multiply-adds have to convert, from 40 with bf16.  Measured, multiply-adds -> matrix instructions, us, k = 2, 1024 -> 4096 -> 1024:
+// integers, 4 rows of 64 parts 38 -> 38, 8 of 32 56 -> 55, 16 of 32 91 -> 88, 64 of 32 293 -> 118, 64 of 8 219 -> 78, 8 of 2 38 -> 30;
+// bf16, 8 of 32 66 -> 82, 16 of 32 100 -> 119, 32 of 32 169 -> 157, 64 of 32 267 -> 172, 64 of 8 225 -> 106; and 64 rows of 2 parts of
+// 256 -> 64 -> 64, integers 23 -> 18, bf16 21 -> 18.
+bool enough_for_tensor(const Layer &l) { return l.rows * l.k >= (l.w_type == EP_I8 ? 16 : 40); }
 
 bool sixteen(const void *p, int64_t ld, int size) { return ep::aligned(p, 16) && ld * size % 16 == 0; }
 
@@ -1003,7 +1009,7 @@ int run_layer(ep_ctx *ctx, const Layer &l, const Space &s, int *kernels) {
     }
     const bool vec = x_ready && sixteen(l.w1.w, l.n_in, w_size) && sixteen(l.w2.w, l.n_hidden, w_size);
     if constexpr (!std::is_same_v<T, float>) {
-        if (vec && l.n_hidden % 8 == 0 && enough_for_tensor(ctx, l)) {
+        if (vec && l.n_hidden % 8 == 0 && enough_for_tensor(l)) {
             if (l.w_type == EP_I8) {
                 ++*kernels;
                 return run_tensor<T, i8>(ctx, l, s);
