@@ -14,7 +14,10 @@
 // 2000 x 4096 x 4096 in 8 bits 31 us, 2150 TFLOP/s (1.7 waves of tiles, so 2); 169343 x 128 -> 512 bf16 41 us, 5.3 TB/s of
 // 6.5, with z kept 76 us, 5.2 TB/s; backward of 232965 x 256 x 256 bf16 through GELU 155 us: dz 62, dx 44, dW 46 and its
 // join 7, against 74 us for reading and writing everything once; one row of 1024 x 1024 3 us.  fp32 by six bf16 products:
-// 8192 x 4096 x 4096 1266 us, 217 TFLOP/s of 278 (a sixth of bf16's); 169343 x 128 -> 512 219 us.
+// 8192 x 4096 x 4096 1266 us, 217 TFLOP/s of 278 (a sixth of bf16's); 169343 x 128 -> 512 219 us.  8-bit integers (kind::i8, exact sums
+// of 32 bits): 8192 x 4096 x 4096 86 us, 3190 Top/s (tensor pipe 81 % busy); 169343 x 128 -> 512 to bf16 55 us, 3.6 TB/s (bound by the
+// epilogue's instructions: conversion, two scales, bias for every sum); one row of 1024 x 1024 2.8 us (dp4a); 301 x 515 -> 257 12 us
+// (operands copied first, results that TMA cannot write).
 #include "activation.cuh"
 #include "ep_common.cuh"
 #include "rows.cuh"
