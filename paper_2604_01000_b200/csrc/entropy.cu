@@ -7,7 +7,7 @@
 // and sum for each row (forward), or make a tile of G of it (backward), in the operands' type, for two more products.  G exists a
 // piece at a time (some rows by some classes, small enough to stay in the L2 until both products have read it).
 // fp32 inputs are split into three bf16 numbers as in linear.cu; a piece of their logits is made by the products' own tile
-// kernel, and row kernels go over it to the same ends; few of them go without either (small problems, below).
+// kernel, and row kernels go over it to the same ends; few of them, and few 16-bit ones' gradients, go without either (small problems, below).
 //
 // Measured, on the device.  Forward of 169343 x 128 -> 4096 bf16: 231 us; the product alone would need 109 us at 1625 TFLOP/s, its 694
 // million exponentials 154 us at 16 a clock and SM: bound by the issue of what is around them (0.44 a clock and scheduler; the tensor pipe
@@ -1312,33 +1312,56 @@ __global__ void __launch_bounds__(256) entropy_round(const float *__restrict__ s
 
 // ---------------------------------------------------------------------------------------------- small problems
 //
-// A few fp32 products cost the tile kernels mostly launches and passes (operands split in three, logits written and read back,
+// A few products cost the tile kernels mostly launches and passes (fp32 operands split in three, logits written and read back,
 // statistics or G, joins: ten launches of a backward).  Then fp32 multiply-adds of tiles of 64 x 64 take the operands as they are: the
 // forward is two launches, the backward two to four.  Bound by latency, then by what the shared memory gives the multiply-adds: a thread
 // has 4 x 4 logits (8 16-byte reads to 64 multiply-adds) or 4 rows of n_in / 16 columns of the second product.
 // fp32, tiles -> here, us.  Forward: 128 x 64 -> 32 12.2 -> 8.5, 500 x 64 -> 500 13.2 -> 9.8, 3000 x 65 -> 257 16.2 -> 13.0, 50000 x 16 -> 40
 // 30 -> 16, 200000 x 16 -> 10 109 -> 45; but 2000 x 128 -> 257 14.8 -> 18.0, 40 x 128 -> 4000 16 -> 27 (statistics of many classes).  Backward:
 // 128 x 64 -> 32 24.8 -> 11.5, 500 x 64 -> 500 34.9 -> 14.1, 40 x 128 -> 4000 31.8 -> 18.4, 3000 x 65 -> 257 41.6 -> 32.7, 18 x 42 -> 77887
-// 123 -> 77; but 2000 x 128 -> 257 37.8 -> 45.7, 64 x 128 -> 16384 45 -> 57, 2000 x 64 -> 1000 44 -> 56.  In 16 bits, where nothing is split, the
-// tiles won at nearly every size.
+// 123 -> 77; but 2000 x 128 -> 257 37.8 -> 45.7, 64 x 128 -> 16384 45 -> 57, 2000 x 64 -> 1000 44 -> 56.  
+// In 16 bits, where nothing is split, the tiles' forward is as quick or quicker everywhere.  Backward, bf16: 128 x 64 -> 32 15.8 -> 11.5,
+// 16 x 100 -> 456 35.5 -> 15.1, 500 x 64 -> 500 23.3 -> 14.3, 3000 x 65 -> 257 46 -> 32, 1000 x 64 -> 1000 31.8 -> 29.1; but 2000 x 64 -> 1000 33,
+// fp32 here 56.  G stays fp32 here, in all types.
 constexpr int ST = 64;            // a block's rows of either operand
 constexpr int SMALL_BLOCKS = 1;   // to an SM, of either gradient's
 constexpr int SMALL_WIDTH = 128;  // elements of a row at most
 // 64 rows on their way to shared memory, LD floats apart, zero past their n_in elements and past the last row.
-template <int LD, typename Wanted>
-__device__ __forceinline__ void small_rows(float *to, const float *from, int64_t ld, int64_t row0, int64_t rows, int n_in, Wanted wanted) {
+// (Asynchronously of fp32; 16-bit elements become fp32 on the way.)
+template <int LD, typename T, typename Wanted>
+__device__ __forceinline__ void small_rows(float *to, const T *from, int64_t ld, int64_t row0, int64_t rows, int n_in, Wanted wanted) {
     const int lane = threadIdx.x & 31;
+    if constexpr (sizeof(T) == 2) {
+        constexpr int COLUMNS = (LD - 4 + 31) / 32;
 #pragma unroll
-    for (int q = 0; q < ST / 8; ++q) {
-        const int r = (threadIdx.x >> 5) + 8 * q;
-        const bool there = row0 + r < rows && wanted(row0 + r);
+        for (int q0 = 0; q0 < ST / 8; q0 += 4) {
+            T v[4][COLUMNS];
 #pragma unroll
-        for (int c0 = 0; c0 < LD - 4; c0 += 32) {
-            const int c = c0 + lane;
-            if (c < LD - 4) {
-                const bool in = there && c < n_in;
-                const float *src = in ? from + (row0 + r) * ld + c : from;
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(to + r * LD + c)), "l"(src), "r"(in ? 4 : 0) : "memory");
+            for (int q = 0; q < 4; ++q) {
+                const int64_t row = row0 + (threadIdx.x >> 5) + 8 * (q0 + q);
+                const bool there = row < rows && wanted(row);
+#pragma unroll
+                for (int i = 0; i < COLUMNS; ++i) v[q][i] = there && 32 * i + lane < n_in ? from[row * ld + 32 * i + lane] : from_f32<T>(0.f);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+#pragma unroll
+                for (int i = 0; i < COLUMNS; ++i)
+                    if (32 * i + lane < LD - 4) to[((threadIdx.x >> 5) + 8 * (q0 + q)) * LD + 32 * i + lane] = to_f32(v[q][i]);
+        }
+    } else {
+#pragma unroll
+        for (int q = 0; q < ST / 8; ++q) {
+            const int r = (threadIdx.x >> 5) + 8 * q;
+            const bool there = row0 + r < rows && wanted(row0 + r);
+#pragma unroll
+            for (int c0 = 0; c0 < LD - 4; c0 += 32) {
+                const int c = c0 + lane;
+                if (c < LD - 4) {
+                    const bool in = there && c < n_in;
+                    const float *src = in ? from + (row0 + r) * ld + c : from;
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(to + r * LD + c)), "l"(src), "r"(in ? 4 : 0) : "memory");
+                }
             }
         }
     }
@@ -1371,9 +1394,9 @@ __device__ __forceinline__ void small_products(const float *p, const float *q, i
 }
 
 struct SmallWork {
-    const float *x;
+    const void *x;
     int64_t ldx;
-    const float *w;
+    const void *w;
     int64_t ldw;
     const void *bias;
     int bias_type;
@@ -1388,10 +1411,12 @@ struct SmallWork {
     int dx_splits, dw_splits; // shares of the sums over classes and over rows
     int64_t dx_blocks;
     float *dx_part, *dw_part, *db_part;   // [share][..], or the outputs themselves are written
-    float *dx, *dweight, *dbias;
+    void *dx, *dweight;
+    float *dbias;
 };
 // What the tile kernels make of an infinity among fp32 operands, which split into NaN: an infinite logit is no logit.
-__device__ __forceinline__ float small_logit(float v) { return isinf(v) ? CUDART_NAN_F : v; }
+template <typename T>
+__device__ __forceinline__ float small_logit(float v) { return sizeof(T) == 4 && isinf(v) ? CUDART_NAN_F : v; }
 // Statistics of a tile's rows.  J = ceil(n_in / 16).
 template <int J>
 __global__ void __launch_bounds__(256) entropy_small_forward(const SmallWork e) {
@@ -1403,8 +1428,8 @@ __global__ void __launch_bounds__(256) entropy_small_forward(const SmallWork e) 
     auto all = [](int64_t) { return true; };
     ep_wait_for_launch_before();
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *e.ticket = 0;
-    small_rows<LD>(p, e.x, e.ldx, row0, e.rows, e.n_in, all);
-    small_rows<LD>(q, e.w, e.ldw, class0, e.classes, e.n_in, all);
+    small_rows<LD>(p, static_cast<const float *>(e.x), e.ldx, row0, e.rows, e.n_in, all);
+    small_rows<LD>(q, static_cast<const float *>(e.w), e.ldw, class0, e.classes, e.n_in, all);
     copies_end_group();
     float bias[4];
     int target[4];
@@ -1426,7 +1451,7 @@ __global__ void __launch_bounds__(256) entropy_small_forward(const SmallWork e) 
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int c = class0 + tx + 16 * j;
-            l[j] = c < e.classes ? small_logit(s[i][j]) + bias[j] : -INFINITY;
+            l[j] = c < e.classes ? small_logit<float>(s[i][j]) + bias[j] : -INFINITY;
             if (c == target[i] && c < e.classes) e.at_target[row] = l[j];
             r.m = fmaxf(r.m, l[j]);
         }
@@ -1440,7 +1465,7 @@ __global__ void __launch_bounds__(256) entropy_small_forward(const SmallWork e) 
 }
 // Gradient of 64 rows of x (P = x, Q = W), or of W (P = W, Q = x): over its share of Q, 64 rows at a time, the logits, G of them, G Q.
 // (Either makes all logits: it needs a third more multiply-adds than G written and read back, and two launches less.)
-template <bool DW, int J>
+template <typename T, bool DW, int J>
 __device__ __forceinline__ void small_gradient(const SmallWork &e, int64_t block, float *memory) {
     constexpr int LD = 16 * J + 4, LDG = ST + 4;
     float *const p = memory, *const q = p + ST * LD, *const g = q + 2 * ST * LD;   // q: two tiles; g[row of Q][row of P]
@@ -1450,10 +1475,10 @@ __device__ __forceinline__ void small_gradient(const SmallWork &e, int64_t block
     const int64_t t0 = tiles * share / splits, t1 = tiles * (share + 1) / splits;
     auto bring = [&](int64_t tile) {
         // (a row that takes no part counts for nothing, whatever it holds)
-        small_rows<LD>(q + (tile & 1) * ST * LD, DW ? e.x : e.w, DW ? e.ldx : e.ldw, tile * ST, Q, e.n_in,
+        small_rows<LD>(q + (tile & 1) * ST * LD, static_cast<const T *>(DW ? e.x : e.w), DW ? e.ldx : e.ldw, tile * ST, Q, e.n_in,
                        [&](int64_t r) { return !DW || e.info.target[r] >= 0; });
     };
-    small_rows<LD>(p, DW ? e.w : e.x, DW ? e.ldw : e.ldx, p0, P, e.n_in, [](int64_t) { return true; });
+    small_rows<LD>(p, static_cast<const T *>(DW ? e.w : e.x), DW ? e.ldw : e.ldx, p0, P, e.n_in, [](int64_t) { return true; });
     if (t0 < t1) bring(t0);
     copies_end_group();
     // what is known of rows of x (target, g, lse) and of classes (bias), of either operand
@@ -1499,7 +1524,7 @@ __device__ __forceinline__ void small_gradient(const SmallWork &e, int64_t block
             for (int j = 0; j < 4; ++j) {
                 const int r = DW ? j : i, c = DW ? i : j;
                 const int64_t one_class = DW ? p0 + 4 * ty + i : q0 + tx + 16 * j;
-                const float share_of_class = exp_fast(small_logit(s[i][j]) + k.bias[c] - k.z[r]) - (one_class == k.target[r] ? 1.f : 0.f);
+                const float share_of_class = exp_fast(small_logit<T>(s[i][j]) + k.bias[c] - k.z[r]) - (one_class == k.target[r] ? 1.f : 0.f);
                 s[i][j] = k.target[r] >= 0 && one_class < e.classes ? share_of_class * k.g[r] : 0.f;
             }
 #pragma unroll
@@ -1532,7 +1557,8 @@ __device__ __forceinline__ void small_gradient(const SmallWork &e, int64_t block
             for (int j = 0; j < J; ++j) total[i][j] += acc[i][j];
     }
     copies_wait<0>();
-    float *const part = DW ? e.dw_part : e.dx_part, *const out = DW ? e.dweight : e.dx;
+    float *const part = DW ? e.dw_part : e.dx_part;
+    T *const out = static_cast<T *>(DW ? e.dweight : e.dx);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int64_t m = p0 + 4 * ty + i;
@@ -1543,7 +1569,7 @@ __device__ __forceinline__ void small_gradient(const SmallWork &e, int64_t block
             if (splits > 1)
                 part[((int64_t)share * P + m) * e.n_in + n] = total[i][j];
             else if (out)
-                out[m * e.n_in + n] = total[i][j];
+                out[m * e.n_in + n] = from_f32<T>(total[i][j]);
         }
         if (DW && e.dbias) {
 #pragma unroll
@@ -1557,20 +1583,20 @@ __device__ __forceinline__ void small_gradient(const SmallWork &e, int64_t block
         }
     }
 }
-template <int J>
+template <typename T, int J>
 __global__ void __launch_bounds__(256, 2) entropy_small_backward(const SmallWork e) {
     extern __shared__ float4 small_memory[];
     float *const memory = reinterpret_cast<float *>(small_memory);
     ep_wait_for_launch_before();
     ep_let_next_launch_start();
     if ((int64_t)blockIdx.x < e.dx_blocks)
-        small_gradient<false, J>(e, blockIdx.x, memory);
+        small_gradient<T, false, J>(e, blockIdx.x, memory);
     else
-        small_gradient<true, J>(e, blockIdx.x - e.dx_blocks, memory);
+        small_gradient<T, true, J>(e, blockIdx.x - e.dx_blocks, memory);
 }
 // The shares: LANES lanes to an element, each every LANES-th share in order, then the lanes (in a fixed order).
-template <int LANES>
-__global__ void __launch_bounds__(256) entropy_small_fold(const float *part, int splits, int64_t n, float *out, const float *more_part,
+template <typename T, int LANES>
+__global__ void __launch_bounds__(256) entropy_small_fold(const float *part, int splits, int64_t n, T *out, const float *more_part,
                                                           int64_t more, float *more_out) {
     ep_wait_for_launch_before();
     ep_let_next_launch_start();
@@ -1590,7 +1616,7 @@ __global__ void __launch_bounds__(256) entropy_small_fold(const float *part, int
     if (rest)
         more_out[i] = (float)sum;
     else if (out)
-        out[i] = (float)sum;
+        out[i] = from_f32<T>((float)sum);
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -2129,8 +2155,8 @@ int narrow_backward_run(ep_ctx *ctx, Inputs &in, const NarrowSpace &s, const Giv
 // (What was measured on both sides stands at the kernels.)  Tiles of 64 x 64 cost the same however little of them there is, and the tile
 // kernels' k-blocks of 64 elements as much for fewer.
 bool small_problem(bool grad, int64_t rows, int n_in, int classes, int type) {
-    if (type != EP_F32 || n_in > SMALL_WIDTH || rows > 1 << 20 || (!grad && classes > 512)) return false;
-    return ep::ceil_div(rows, ST) * ST * (ep::ceil_div(classes, ST) * ST) * n_in <= (n_in <= 48 ? 1 << 28 : 1 << 26);
+    if ((type != EP_F32 && !grad) || n_in > SMALL_WIDTH || rows > 1 << 20 || (!grad && classes > 512)) return false;
+    return ep::ceil_div(rows, ST) * ST * (ep::ceil_div(classes, ST) * ST) * n_in <= (type == EP_F32 && n_in <= 48 ? 1 << 28 : 1 << 26);
 }
 // f(J) with J = ceil(n_in / 16).
 template <int J = 1, typename F>
@@ -2182,9 +2208,9 @@ SmallSpace small_space(const ep_ctx *ctx, bool grad, int64_t rows, int n_in, int
 }
 SmallWork small_work(const Inputs &in) {
     SmallWork e{};
-    e.x = static_cast<const float *>(in.x);
+    e.x = in.x;
     e.ldx = in.ldx;
-    e.w = static_cast<const float *>(in.w);
+    e.w = in.w;
     e.ldw = in.ldw;
     e.bias = in.bias;
     e.bias_type = in.bias_type;
@@ -2218,6 +2244,7 @@ int small_forward(ep_ctx *ctx, Inputs &in, const SmallSpace &s, float *loss, flo
     in.kernels += 2;
     return EP_OK;
 }
+template <typename T>
 int small_backward(ep_ctx *ctx, Inputs &in, const SmallSpace &s, const Given &g, const Wanted &out) {
     const int blocks = weight_blocks(ctx, in.rows);
     entropy_weights<float><<<blocks, WEIGHT_THREADS, 0, in.stream>>>(g.lse, in.targets, in.rows, in.classes, g.counted, g.dloss, g.drow, nullptr, 0,
@@ -2234,27 +2261,27 @@ int small_backward(ep_ctx *ctx, Inputs &in, const SmallSpace &s, const Given &g,
     e.dx_part = s.dx_part;
     e.dw_part = s.dw_part;
     e.db_part = s.db_part;
-    e.dx = static_cast<float *>(out.dx);
-    e.dweight = static_cast<float *>(out.dweight);
+    e.dx = out.dx;
+    e.dweight = out.dweight;
     e.dbias = out.dbias;
     const int64_t grid = e.dx_blocks + (over_rows ? s.dw_tiles * s.dw_splits : 0);
     const int rc = small_width(in.n_in, [&](auto j) {
         constexpr int J = decltype(j)::value;
         constexpr size_t smem = sizeof(float) * (3 * ST * (16 * J + 4) + ST * (ST + 4));
-        EP_CUDA(ctx, cudaFuncSetAttribute(entropy_small_backward<J>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-        EP_CUDA(ctx, ep::launch_early(entropy_small_backward<J>, dim3((unsigned)grid), dim3(256), smem, in.stream, e));
+        EP_CUDA(ctx, cudaFuncSetAttribute(entropy_small_backward<T, J>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+        EP_CUDA(ctx, ep::launch_early(entropy_small_backward<T, J>, dim3((unsigned)grid), dim3(256), smem, in.stream, e));
         return (int)EP_OK;
     });
     if (rc != EP_OK) return rc;
     in.kernels += 2;
     // many shares: a warp to an element
-    auto fold = [&](const float *part, int splits, int64_t n, float *to, const float *more_part, int64_t more, float *more_to) {
+    auto fold = [&](const float *part, int splits, int64_t n, void *to, const float *more_part, int64_t more, float *more_to) {
         if (splits == 1 || n + more == 0) return cudaSuccess;
         ++in.kernels;
         const int lanes = splits > 16 ? 32 : 1;
-        auto kernel = lanes > 1 ? entropy_small_fold<32> : entropy_small_fold<1>;
-        return ep::launch_early(kernel, dim3((unsigned)ep::ceil_div((n + more) * lanes, 256)), dim3(256), 0, in.stream, part, splits, n, to,
-                                more_part, more, more_to);
+        auto kernel = lanes > 1 ? entropy_small_fold<T, 32> : entropy_small_fold<T, 1>;
+        return ep::launch_early(kernel, dim3((unsigned)ep::ceil_div((n + more) * lanes, 256)), dim3(256), 0, in.stream, part, splits, n,
+                                static_cast<T *>(to), more_part, more, more_to);
     };
     EP_CUDA(ctx, fold(e.dx_part, e.dx_splits, out.dx ? in.rows * in.n_in : 0, e.dx, nullptr, 0, nullptr));
     EP_CUDA(ctx, fold(e.dw_part, e.dw_splits, out.dweight ? (int64_t)in.classes * in.n_in : 0, e.dweight, e.db_part, out.dbias ? in.classes : 0,
@@ -2357,7 +2384,9 @@ int ep_cross_entropy_backward(ep_ctx *ctx, const void *x, int64_t ldx, const voi
     const Given given{lse, dloss, drow_loss, reinterpret_cast<const long long *>(counted)};
     const Wanted out{dx, dweight, dbias};
     Timed tm(ctx, in.stream, EP_TIMER_ENTROPY);
-    rc = small     ? small_backward(ctx, in, few, given, out)
+    rc = small     ? (in_type == EP_F32    ? small_backward<float>(ctx, in, few, given, out)
+                      : in_type == EP_BF16 ? small_backward<__nv_bfloat16>(ctx, in, few, given, out)
+                                           : small_backward<__half>(ctx, in, few, given, out))
          : in_tmem ? narrow_backward_run(ctx, in, n, given, out)
                    : backward_run(ctx, in, s, given, out);
     tm.end(in.kernels);
