@@ -1319,7 +1319,7 @@ __global__ void __launch_bounds__(256) entropy_round(const float *__restrict__ s
 // fp32, tiles -> here, us.  Forward: 128 x 64 -> 32 12.2 -> 8.5, 500 x 64 -> 500 13.2 -> 9.8, 3000 x 65 -> 257 16.2 -> 13.0, 50000 x 16 -> 40
 // 30 -> 16, 200000 x 16 -> 10 109 -> 45; but 2000 x 128 -> 257 14.8 -> 18.0, 40 x 128 -> 4000 16 -> 27 (statistics of many classes).  Backward:
 // 128 x 64 -> 32 24.8 -> 11.5, 500 x 64 -> 500 34.9 -> 14.1, 40 x 128 -> 4000 31.8 -> 18.4, 3000 x 65 -> 257 41.6 -> 32.7, 18 x 42 -> 77887
-// 123 -> 77; but 2000 x 128 -> 257 37.8 -> 45.7, 64 x 128 -> 16384 45 -> 57, 2000 x 64 -> 1000 44 -> 56.  
+// 123 -> 77; but 2000 x 128 -> 257 37.8 -> 45.7, 64 x 128 -> 16384 45 -> 57, 2000 x 64 -> 1000 44 -> 56.
 // In 16 bits, where nothing is split, the tiles' forward is as quick or quicker everywhere.  Backward, bf16: 128 x 64 -> 32 15.8 -> 11.5,
 // 16 x 100 -> 456 35.5 -> 15.1, 500 x 64 -> 500 23.3 -> 14.3, 3000 x 65 -> 257 46 -> 32, 1000 x 64 -> 1000 31.8 -> 29.1; but 2000 x 64 -> 1000 33,
 // fp32 here 56.  G stays fp32 here, in all types.
@@ -2153,10 +2153,12 @@ int narrow_backward_run(ep_ctx *ctx, Inputs &in, const NarrowSpace &s, const Giv
 
 // ---- small problems
 // (What was measured on both sides stands at the kernels.)  Tiles of 64 x 64 cost the same however little of them there is, and the tile
-// kernels' k-blocks of 64 elements as much for fewer.
+// kernels' k-blocks of 64 elements and tiles of 128 or 256 rows as much for fewer.
 bool small_problem(bool grad, int64_t rows, int n_in, int classes, int type) {
     if ((type != EP_F32 && !grad) || n_in > SMALL_WIDTH || rows > 1 << 20 || (!grad && classes > 512)) return false;
-    return ep::ceil_div(rows, ST) * ST * (ep::ceil_div(classes, ST) * ST) * n_in <= (type == EP_F32 && n_in <= 48 ? 1 << 28 : 1 << 26);
+    // (backward, fp32, tiles -> here: 200000 x 16 -> 10 212 -> 183, 18 x 42 -> 77887 121 -> 77; but 39224 x 24 -> 237 101 -> 154)
+    const bool empty_tiles = n_in <= 48 && (!grad || std::min<int64_t>(rows, classes) <= ST);
+    return ep::ceil_div(rows, ST) * ST * (ep::ceil_div(classes, ST) * ST) * n_in <= (type == EP_F32 && empty_tiles ? 1 << 28 : 1 << 26);
 }
 // f(J) with J = ceil(n_in / 16).
 template <int J = 1, typename F>
