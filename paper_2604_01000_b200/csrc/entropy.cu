@@ -772,9 +772,10 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
                 uint32_t a[2][32];
                 tmem_ld32_issue(at, a[0]);
                 tmem_ld32_issue(at + 32, a[1]);
-                // Where a row's class is among these columns, its slope is its share less all of g; and slopes may be negative.
-                // Both are rare and out of the way of what is not.
-                int mine = -1;
+                // Where a row's class is among these columns, its slope is its share less all of g; slopes may be negative; and columns past
+                // the last class, which fill the last tile up, have none (their logit of 0 may be far above the others: 2^shift then
+                // passes the operands' type, and infinity times the zeros of W there is NaN).  All are rare and out of the way of what is not.
+                int mine = -1, classes = 64;
                 bool special[2];
                 if constexpr (DW) {
                     const int class0 = (int)p - lane;
@@ -784,8 +785,9 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
                                                           known[BQ + 32 * h + lane] < 0.f);
                 } else {
                     mine = target >= 0 ? target - t.inner * BQ - piece * 64 : -1;
-                    special[0] = negative || __any_sync(FULL, (unsigned)mine < 32u);
-                    special[1] = negative || __any_sync(FULL, (unsigned)(mine - 32) < 32u);
+                    classes = (int)e.Q - t.inner * BQ - piece * 64;
+                    special[0] = negative || classes < 32 || __any_sync(FULL, (unsigned)mine < 32u);
+                    special[1] = negative || classes < 64 || __any_sync(FULL, (unsigned)(mine - 32) < 32u);
                 }
                 tmem_ld_wait(a[0]);
                 tmem_ld_wait(a[1]);
@@ -831,7 +833,7 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
                                 const float g = k[BQ + c];
                                 x[c] = copysignf(1.f, g) * x[c] - (reinterpret_cast<const int *>(k)[2 * BQ + c] == (int)p ? g * up : 0.f);
                             } else
-                                x[c] = copysignf(1.f, weight) * x[c] - (32 * h + c == mine ? weight : 0.f);
+                                x[c] = 32 * h + c < classes ? copysignf(1.f, weight) * x[c] - (32 * h + c == mine ? weight : 0.f) : 0.f;
                         }
                     }
                     uint32_t out[16];
