@@ -530,6 +530,7 @@ struct FusedMemory {
 };
 struct FusedWork {
     int64_t P, Q;             // rows of either
+    int ragged;               // the tile of Q that has classes past the last, or -1
     int width, boxes;         // of a row, and its boxes
     Line line;
     uint32_t idesc_s, idesc_acc;
@@ -772,10 +773,9 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
                 uint32_t a[2][32];
                 tmem_ld32_issue(at, a[0]);
                 tmem_ld32_issue(at + 32, a[1]);
-                // Where a row's class is among these columns, its slope is its share less all of g; slopes may be negative; and columns past
-                // the last class, which fill the last tile up, have none (their logit of 0 may be far above the others: 2^shift then
-                // passes the operands' type, and infinity times the zeros of W there is NaN).  All are rare and out of the way of what is not.
-                int mine = -1, classes = 64;
+                // Where a row's class is among these columns, its slope is its share less all of g; and slopes may be negative.
+                // Both are rare and out of the way of what is not.
+                int mine = -1;
                 bool special[2];
                 if constexpr (DW) {
                     const int class0 = (int)p - lane;
@@ -785,15 +785,23 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
                                                           known[BQ + 32 * h + lane] < 0.f);
                 } else {
                     mine = target >= 0 ? target - t.inner * BQ - piece * 64 : -1;
-                    classes = (int)e.Q - t.inner * BQ - piece * 64;
-                    special[0] = negative || classes < 32 || __any_sync(FULL, (unsigned)mine < 32u);
-                    special[1] = negative || classes < 64 || __any_sync(FULL, (unsigned)(mine - 32) < 32u);
+                    special[0] = negative || __any_sync(FULL, (unsigned)mine < 32u);
+                    special[1] = negative || __any_sync(FULL, (unsigned)(mine - 32) < 32u);
                 }
                 tmem_ld_wait(a[0]);
                 tmem_ld_wait(a[1]);
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh->s_empty[group]);
+                // Columns past the last class, which fill the last tile up, have no slope.  (Their logit of 0 may be far above all others:
+                // 2^shift then passes the operands' type, and infinity times the zeros of W there is NaN.  Done here, not with the slopes
+                // below, it costs the other tiles nothing: gradient of 169343 x 128 against 4096 classes 328 us, there 362.)
+                if (!DW && t.inner == e.ragged) {
+                    const int classes = (int)e.Q - t.inner * BQ - piece * 64;
+#pragma unroll
+                    for (int c = 0; c < 64; ++c)
+                        if (c >= classes) a[c / 32][c % 32] = __float_as_uint(-INFINITY);
+                }
                 // (what was there has long been multiplied)
                 if (!mbar_wait_warp(&sh->g_empty[gbuf], ((j / SLOPES) & 1u) ^ 1u, abort_flag)) break;
                 tc_fence_after();
@@ -833,7 +841,7 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
                                 const float g = k[BQ + c];
                                 x[c] = copysignf(1.f, g) * x[c] - (reinterpret_cast<const int *>(k)[2 * BQ + c] == (int)p ? g * up : 0.f);
                             } else
-                                x[c] = 32 * h + c < classes ? copysignf(1.f, weight) * x[c] - (32 * h + c == mine ? weight : 0.f) : 0.f;
+                                x[c] = copysignf(1.f, weight) * x[c] - (32 * h + c == mine ? weight : 0.f);
                         }
                     }
                     uint32_t out[16];
@@ -2111,6 +2119,7 @@ int launch_fused(ep_ctx *ctx, Inputs &in, const NarrowSpace &s, const Operand &x
     FusedWork e{};
     e.P = DW ? in.classes : in.rows;
     e.Q = DW ? in.rows : in.classes;
+    e.ragged = DW || e.Q % Q_ROWS == 0 ? -1 : (int)(e.Q / Q_ROWS);
     e.width = in.n_in;
     e.boxes = (int)ep::ceil_div(in.n_in, 64);
     e.line = fused_line(ctx, e.P, e.Q);
