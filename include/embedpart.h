@@ -521,8 +521,10 @@ int ep_route_backward(ep_ctx *ctx, const void *logits, int32_t type, int64_t row
  * A row whose every class is closed takes no part either (row_loss 0, lse -infinity).  A target that is closed while others are
  * not has row_loss infinity.  A NaN or +infinity among the logits of a row that takes part makes its lse and loss
  * NaN.  With R = 0 loss is 0.
- * Logits are fp32 sums.  Of 16-bit inputs they run through n_in in the tensor cores, which cut off 2.5 to 5e-8 and 1.5 to 1.9e-8 more
- * for every 16 products, of the sum; that share is given back, so that what is left (a fifth of it, and chance) has no sign.
+ * Logits are fp32 sums.  Of 16-bit inputs the tensor cores make them, which cut a sum off toward zero after every 16 products: nothing of
+ * a sum that fits fp32, 1e-7 of one of one sign, on average 1.5e-8 (EP_BF16) to 1.9e-8 of dense ones.  More than 256 elements are summed 128
+ * at a time and added up to nearest, so that a logit loses no more than 8 such steps do; up to 256 are summed at once, and what dense
+ * rows lose of them on average, up to 3.6e-7 of the logit, is added again, whatever they hold.
  * Of EP_F32 inputs they are ep_linear's, or, for few of them, fp32 multiply-adds; an infinity in x or w makes the logits it
  * reaches NaN either way.
  *

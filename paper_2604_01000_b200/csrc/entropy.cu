@@ -118,13 +118,19 @@ struct RowInfo {
     int *target;
     __host__ __device__ RowInfo from(int64_t row) const { return RowInfo{shift + row, g + row, target + row}; }
 };
-// 1 / log 2, and what a sum of n_in products in the tensor memory has lost: the tensor cores cut a sum off after every 16 products, toward
-// zero, they do not round it.  Measured, such a sum of 16-bit products comes out smaller by a share of itself that grows with its steps and
-// hardly depends on what is summed: 16 to 4096 products of bf16 lose (2.5 + 1.5 steps) 1e-8 of the sum, of fp16 (5 + 1.9 steps) 1e-8, within a fifth.
-// Given back on average with the factor that every logit is multiplied by anyway (1024 products of bf16: off by 9e-7 instead of 4.6e-6 at
-// logits of 4), so that what many rows add up to (dbias) does not keep it.
+// The tensor cores cut a sum off after every 16 products, toward zero, they do not round it.  What that costs depends on what is summed:
+// nothing where the sum fits fp32 (rows of one element, or of few bits), 1e-7 of the sum a step where all products have one sign, and
+// of dense rows of either sign, on average and within a fifth, (2.5 + 1.5 steps) 1e-8 of the sum in bf16, (5 + 1.9 steps) 1e-8 in fp16.
+// So a logit of more than 256 elements is summed in runs of 8 such steps, which are added up to nearest in registers: however long it is,
+// it loses what one run does.  (Forward and backward, us, in one run -> in such: 169343 x 512 -> 4096 bf16 451 -> 620 and 2163 -> 2793, 20000 x
+// 1024 -> 4096 108 -> 138 and 474 -> 554, 8192 x 4096 -> 4096 203 -> 233 and 595 -> 639: two accumulators in the tensor memory are one tile's, not
+// two.  Runs of 16 steps take 506, 120 and 218 in the forward and lose 3.5e-7.)
+// Up to 256 elements a logit is one run, of up to 16 steps.  Many rows' sums (dbias) would keep the part of its loss that has always the same
+// sign (100000 x 256 -> 10 in bf16: dbias off by 1.4e-5 of itself, so by 1.1e-6); what dense rows lose on average is therefore given back there
+// with the factor 1 / log 2: at most 3.6e-7 of the logit, three units of fp32's last place, by which a sum that lost nothing is too large.
+constexpr int ONE_RUN = 256, RUN_KB = 2;   // elements; k-blocks of a run of longer sums
 float sums_log2e(int n_in, int type) {
-    const double steps = (n_in + 15) / 16, lost = type == EP_BF16 ? 2.5 + 1.5 * steps : 5.0 + 1.9 * steps;
+    const double steps = (n_in + 15) / 16, lost = n_in > ONE_RUN ? 0.0 : type == EP_BF16 ? 2.5 + 1.5 * steps : 5.0 + 1.9 * steps;
     return (float)(1.4426950408889634 * (1.0 + 1e-8 * lost));
 }
 struct TileWork {
@@ -155,17 +161,15 @@ __device__ __forceinline__ float tmem_ld_column(uint32_t taddr) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\ntcgen05.wait::ld.sync.aligned;" : "=r"(v) : "r"(taddr) : "memory");
     return __uint_as_float(v);
 }
-// 16 lanes of 64 accumulator columns: lane l holds rows l / 4 and l / 4 + 8, of each 8 columns two from 2 (l % 4) on:
-// v[4 c + 2 r + i] is column 8 c + 2 (l % 4) + i of row l / 4 + 8 r.
-__device__ __forceinline__ void tmem_ld_rows16(uint32_t taddr, uint32_t (&v)[32]) {
+// 16 lanes of 32 accumulator columns, waited for in the same statement: lane l holds rows l / 4 and l / 4 + 8, of each 8 columns two
+// from 2 (l % 4) on: v[4 c + 2 r + i] is column 8 c + 2 (l % 4) + i of row l / 4 + 8 r.
+__device__ __forceinline__ void tmem_ld_rows16(uint32_t taddr, uint32_t (&v)[16]) {
     asm volatile(
-        "tcgen05.ld.sync.aligned.16x256b.x8.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n"
+        "tcgen05.wait::ld.sync.aligned;"
         : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
-          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
-          "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
-          "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+          "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
         : "r"(taddr)
         : "memory");
 }
@@ -185,13 +189,14 @@ __device__ __forceinline__ uint32_t packed(float lo, float hi) {
     }
 }
 
-// (BIASED: of the forward alone)
-template <bool GRAD, bool BIASED, typename T>
+// RUNS: rows of more than ONE_RUN elements, which those of the backward always are.  (BIASED: of the forward alone)
+template <bool GRAD, bool BIASED, bool RUNS, typename T>
 __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                                                                  const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_clean,
                                                                  const TileWork e, int *status) {
     using Mem = TileMemory<GRAD>;
     constexpr int STAGES = Mem::STAGES;
+    static_assert(RUNS || !GRAD, "the backward of shorter rows is entropy_fused");
     extern __shared__ char smem_raw[];
     char *ring = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     char *staging = ring + Mem::RING;
@@ -260,24 +265,29 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
         uint32_t acc = 0, s = 0, ph = 0;
         bool ok = true;
         const uint32_t ring_base = smem_u32(ring);
-        for (Stretch t(e.line, worker); rank == 0 && ok && t.more(); t.next(), ++acc) {
+        for (Stretch t(e.line, worker); rank == 0 && ok && t.more(); t.next()) {
             const uint32_t idesc = e.idesc | (uint32_t)(columns(class_tile(t)) >> 3) << 17;
-            const uint32_t buf = acc & 1u;
-            if (!(ok = mbar_wait_warp(&sh->t_empty[buf], ((acc >> 1) & 1u) ^ 1u, abort_flag))) break;
-            tc_fence_after();
-            for (int kb = 0; kb < e.kb; ++kb) {
-                if (!(ok = mbar_wait_warp(&sh->full[s], ph, abort_flag))) break;
+            int kb = 0;
+            do {
+                const uint32_t buf = acc & 1u;
+                if (!(ok = mbar_wait_warp(&sh->t_empty[buf], ((acc >> 1) & 1u) ^ 1u, abort_flag))) break;
                 tc_fence_after();
-                const uint32_t a = ring_base + s * (uint32_t)STAGE_BYTES;
-                umma_kblock_elected<HALF, true>(tmem_base + buf * TILE, operand_desc(a, false), operand_desc(a + BLOCK_ROWS * 128, false), 2,
-                                                2, idesc, kb > 0);
-                commit_elected<true>(&sh->empty[s]);
-                if (++s == (uint32_t)STAGES) {
-                    s = 0;
-                    ph ^= 1u;
+                const int first = kb, end = RUNS ? min(kb + RUN_KB, e.kb) : e.kb;
+                for (; kb < end; ++kb) {
+                    if (!(ok = mbar_wait_warp(&sh->full[s], ph, abort_flag))) break;
+                    tc_fence_after();
+                    const uint32_t a = ring_base + s * (uint32_t)STAGE_BYTES;
+                    umma_kblock_elected<HALF, true>(tmem_base + buf * TILE, operand_desc(a, false), operand_desc(a + BLOCK_ROWS * 128, false), 2,
+                                                    2, idesc, kb > first);
+                    commit_elected<true>(&sh->empty[s]);
+                    if (++s == (uint32_t)STAGES) {
+                        s = 0;
+                        ph ^= 1u;
+                    }
                 }
-            }
-            if (ok) commit_elected<true>(&sh->t_full[buf]);
+                if (ok) commit_elected<true>(&sh->t_full[buf]);
+                ++acc;
+            } while (RUNS && ok && kb < e.kb);
         }
         if (rank == 0 && __any_sync(FULL, !ok || *abort_flag)) {
             commit_elected<true>(&sh->drain);
@@ -292,43 +302,27 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
             __syncwarp();
             if (lane == 0) arrive_at(t_empty + buf * 8);
         };
-        uint32_t acc = 0;
+        uint32_t acc = 0;   // accumulators so far, a run's each
         const float log2e = e.log2e;
+        // take(buffer) of each run of a tile's sums, if there is any of it that is wanted; false after an abort
+        auto each_run = [&](bool wanted, auto take) {
+            for (int run = 0; run < e.kb; run += RUN_KB, ++acc) {
+                if (!mbar_wait_warp(&sh->t_full[acc & 1u], (acc >> 1) & 1u, abort_flag)) return false;
+                tc_fence_after();
+                if (wanted) take(from + (acc & 1u) * TILE);
+                give_back(acc & 1u);
+            }
+            return true;
+        };
         if constexpr (!GRAD) {
             float top = -FLT_MAX, sum = 0.f;   // (finite from the start: what is closed is below it)
             int target = -1;
-            for (Stretch t(e.line, worker); t.more(); t.next(), ++acc) {
+            for (Stretch t(e.line, worker); t.more(); t.next()) {
                 const int64_t row = (int64_t)t.outer * TILE + rank * BLOCK_ROWS + quad * 32 + lane;
                 const int col = t.inner * TILE + piece * PIECE_COLS;
                 if (acc == 0 || t.inner == 0) target = row < e.M ? e.targets[row] : -1;
-                const uint32_t buf = acc & 1u;
-                if (!mbar_wait_warp(&sh->t_full[buf], (acc >> 1) & 1u, abort_flag)) break;
-                tc_fence_after();
-                if (col < e.N && row - lane < e.M) {
-                    const uint32_t at = from + buf * TILE;
-                    uint32_t a[64];
-                    tmem_ld32_issue(at, reinterpret_cast<uint32_t(&)[32]>(a[0]));
-                    tmem_ld32_issue(at + 32, reinterpret_cast<uint32_t(&)[32]>(a[32]));
-                    // The logits of targets among these columns: a column to each, read once more.
-                    const int mine = target >= 0 ? target - col : -1;
-                    unsigned hits = __ballot_sync(FULL, (unsigned)mine < 64u);
-                    const bool few = __popc(hits) <= 4;
-                    float found = 0.f;
-                    for (; few && hits; hits &= hits - 1) {
-                        const int who = __ffs(hits) - 1;
-                        const float v = tmem_ld_column(at + __shfl_sync(FULL, mine, who));
-                        if (lane == who) found = v;
-                    }
-                    tmem_ld_wait(reinterpret_cast<uint32_t(&)[32]>(a[0]));
-                    tmem_ld_wait(reinterpret_cast<uint32_t(&)[32]>(a[32]));
-                    give_back(buf);
-                    float f[64];
-#pragma unroll
-                    for (int j = 0; j < 64; ++j) f[j] = __uint_as_float(a[j]);
-                    if (!few) {
-#pragma unroll
-                        for (int j = 0; j < 64; ++j) found = j == mine ? f[j] : found;
-                    }
+                // these logits into the row's statistics; mine: the target's column, if it is one of these, found: its logit
+                auto count = [&](float (&f)[64], int mine, float found) {
                     if ((unsigned)mine < 64u) e.at_target[row] = BIASED ? fmaf(found, log2e, e.bias[target]) : found * log2e;
                     if (BIASED) {
 #pragma unroll
@@ -371,8 +365,66 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
                         more = sum_below(top);
                     }
                     sum += more;
-                } else
-                    give_back(buf);
+                };
+                if constexpr (RUNS) {
+                    const bool wanted = col < e.N && row - lane < e.M;
+                    float f[64], found = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 64; ++j) f[j] = 0.f;
+                    if (!each_run(wanted, [&](uint32_t at) {
+#pragma unroll
+                            for (int q = 0; q < 64; q += 16) {
+                                uint32_t a[16];
+                                tmem_ld16(at + q, a);
+#pragma unroll
+                                for (int j = 0; j < 16; j += 2)
+                                    add2(Pair(f[q + j], f[q + j + 1]), Pair(__uint_as_float(a[j]), __uint_as_float(a[j + 1])))
+                                        .get(f[q + j], f[q + j + 1]);
+                            }
+                        }))
+                        break;
+                    if (wanted) {
+                        const int mine = target >= 0 ? target - col : -1;
+                        if (__any_sync(FULL, (unsigned)mine < 64u)) {
+#pragma unroll
+                            for (int j = 0; j < 64; ++j) found = j == mine ? f[j] : found;
+                        }
+                        count(f, mine, found);
+                    }
+                } else {
+                    const uint32_t buf = acc & 1u;
+                    if (!mbar_wait_warp(&sh->t_full[buf], (acc >> 1) & 1u, abort_flag)) break;
+                    tc_fence_after();
+                    if (col < e.N && row - lane < e.M) {
+                        const uint32_t at = from + buf * TILE;
+                        uint32_t a[64];
+                        tmem_ld32_issue(at, reinterpret_cast<uint32_t(&)[32]>(a[0]));
+                        tmem_ld32_issue(at + 32, reinterpret_cast<uint32_t(&)[32]>(a[32]));
+                        // The logits of targets among these columns: a column to each, read once more.
+                        const int mine = target >= 0 ? target - col : -1;
+                        unsigned hits = __ballot_sync(FULL, (unsigned)mine < 64u);
+                        const bool few = __popc(hits) <= 4;
+                        float found = 0.f;
+                        for (; few && hits; hits &= hits - 1) {
+                            const int who = __ffs(hits) - 1;
+                            const float v = tmem_ld_column(at + __shfl_sync(FULL, mine, who));
+                            if (lane == who) found = v;
+                        }
+                        tmem_ld_wait(reinterpret_cast<uint32_t(&)[32]>(a[0]));
+                        tmem_ld_wait(reinterpret_cast<uint32_t(&)[32]>(a[32]));
+                        give_back(buf);
+                        float f[64];
+#pragma unroll
+                        for (int j = 0; j < 64; ++j) f[j] = __uint_as_float(a[j]);
+                        if (!few) {
+#pragma unroll
+                            for (int j = 0; j < 64; ++j) found = j == mine ? f[j] : found;
+                        }
+                        count(f, mine, found);
+                    } else
+                        give_back(buf);
+                    ++acc;
+                }
                 if (t.left == 1 || t.inner + 1 == t.inners) {
                     if (row < e.M) e.partial[((int64_t)(worker - e.line.first_worker(t.outer)) * 4 + piece) * e.M + row] = make_float2(top, sum);
                     top = -FLT_MAX;
@@ -385,58 +437,65 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
             Pair sums[8];
 #pragma unroll
             for (int c = 0; c < 8; ++c) sums[c] = Pair(0.f);
-            Pair bias[8];
-            for (Stretch t(e.line, worker); t.more(); t.next(), ++acc) {
+            for (Stretch t(e.line, worker); t.more(); t.next()) {
                 const int64_t row0 = (int64_t)t.inner * TILE + rank * BLOCK_ROWS + quad * 32;
                 const int col = t.outer * TILE + piece * PIECE_COLS;
-                if (e.bias && (acc == 0 || t.inner == 0)) {
+                const bool wanted = col < e.N && row0 < e.M;
+                float v[2][32];   // 16 rows each, as tmem_ld_rows16 has them
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        const float2 b = *reinterpret_cast<const float2 *>(e.bias + e.class0 + col + 8 * c + 2 * (lane & 3));
-                        bias[c] = Pair(b.x, b.y);
-                    }
-                }
-                float shift[4], weight[4], sign[4];
-                int target[4];
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int64_t row = row0 + 8 * i + (lane >> 2);
-                    shift[i] = e.rows.shift[row];
-                    weight[i] = fabsf(e.rows.g[row]);
-                    sign[i] = e.rows.g[row] < 0.f ? -up : up;
-                    target[i] = e.rows.target[row];
-                }
-                const uint32_t buf = acc & 1u;
-                if (!mbar_wait_warp(&sh->t_full[buf], (acc >> 1) & 1u, abort_flag)) break;
-                tc_fence_after();
-                if (col < e.N && row0 < e.M) {
+                    for (int q = 0; q < 32; ++q) v[h][q] = 0.f;
+                if (!each_run(wanted, [&](uint32_t at) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int q = 0; q < 32; q += 16) {
+                                uint32_t a[16];
+                                tmem_ld_rows16(at + ((uint32_t)(16 * h) << 16) + 2 * q, a);
+#pragma unroll
+                                for (int j = 0; j < 16; j += 2)
+                                    add2(Pair(v[h][q + j], v[h][q + j + 1]), Pair(__uint_as_float(a[j]), __uint_as_float(a[j + 1])))
+                                        .get(v[h][q + j], v[h][q + j + 1]);
+                            }
+                    }))
+                    break;
+                if (wanted) {
                     stores_read<0>();
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        uint32_t a[32];
-                        tmem_ld_rows16(from + buf * TILE + ((uint32_t)(16 * h) << 16), a);
-                        tmem_ld_wait(a);
-                        if (h == 1) give_back(buf);
-                        float f[32];
+                        float shift[2], weight[2], sign[2];
+                        int target[2];
 #pragma unroll
-                        for (int c = 0; c < 8; ++c)
+                        for (int r = 0; r < 2; ++r) {
+                            const int64_t row = row0 + 16 * h + 8 * r + (lane >> 2);
+                            const float g = e.rows.g[row];
+                            shift[r] = e.rows.shift[row];
+                            weight[r] = fabsf(g);
+                            sign[r] = g < 0.f ? -up : up;
+                            target[r] = e.rows.target[row];
+                        }
+                        float(&f)[32] = v[h];
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            const float2 b = e.bias ? *reinterpret_cast<const float2 *>(e.bias + e.class0 + col + 8 * c + 2 * (lane & 3)) : float2{};
 #pragma unroll
                             for (int r = 0; r < 2; ++r) {
-                                Pair v = fma2(Pair(__uint_as_float(a[4 * c + 2 * r]), __uint_as_float(a[4 * c + 2 * r + 1])), Pair(log2e),
-                                              Pair(shift[2 * h + r]));
-                                if (e.bias) v = add2(v, bias[c]);
-                                v.get(f[4 * c + 2 * r], f[4 * c + 2 * r + 1]);
+                                Pair l = fma2(Pair(f[4 * c + 2 * r], f[4 * c + 2 * r + 1]), Pair(log2e), Pair(shift[r]));
+                                if (e.bias) l = add2(l, Pair(b.x, b.y));
+                                l.get(f[4 * c + 2 * r], f[4 * c + 2 * r + 1]);
                             }
+                        }
 #pragma unroll
                         for (int q = 0; q < 32; ++q) f[q] = exp2_fast(f[q]);
 #pragma unroll
                         for (int r = 0; r < 2; ++r) {
-                            const int at = target[2 * h + r] - e.class0 - col;
-                            const bool mine = target[2 * h + r] >= 0 && (unsigned)at < 64u && ((at >> 1) & 3) == (lane & 3);
+                            const int at = target[r] - e.class0 - col;
+                            const bool mine = target[r] >= 0 && (unsigned)at < 64u && ((at >> 1) & 3) == (lane & 3);
                             const int index = mine ? (at >> 3) * 2 + (at & 1) : -1;
                             if (__any_sync(FULL, mine)) {
 #pragma unroll
-                                for (int q = 0; q < 16; ++q) f[4 * (q >> 1) + 2 * r + (q & 1)] -= q == index ? weight[2 * h + r] : 0.f;
+                                for (int q = 0; q < 16; ++q) f[4 * (q >> 1) + 2 * r + (q & 1)] -= q == index ? weight[r] : 0.f;
                             }
                         }
                         uint32_t out[16];
@@ -444,7 +503,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
                         for (int c = 0; c < 8; ++c)
 #pragma unroll
                             for (int r = 0; r < 2; ++r) {
-                                const Pair g = mul2(Pair(f[4 * c + 2 * r], f[4 * c + 2 * r + 1]), Pair(sign[2 * h + r]));
+                                const Pair g = mul2(Pair(f[4 * c + 2 * r], f[4 * c + 2 * r + 1]), Pair(sign[r]));
                                 if (e.sums) sums[c] = add2(sums[c], g);
                                 float lo, hi;
                                 g.get(lo, hi);
@@ -458,8 +517,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
                     }
                     before_stores();
                     tma_store_3d_elected(&map_g, slot, col, (int)row0, 0);
-                } else
-                    give_back(buf);
+                }
                 if (e.sums && (t.left == 1 || t.inner + 1 == t.inners)) {
                     float *to = e.sums + ((int64_t)(worker - e.line.first_worker(t.outer)) * 8 + rank * 4 + quad) * e.stride + col;
 #pragma unroll
@@ -502,7 +560,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
 // once and read twice) is not moved (169343 x 128 -> 4096 bf16: 1548 us with G written and read, 684 so).  Of 19 warps one loads, one makes S, one adds up, 16 make G: groups of
 // them take tiles in turn, a thread a row of S and 64 columns.
 // Workers (SMs) share out the tiles as in entropy_tiles; who has only a part of a P tile leaves its sums for entropy_join.
-constexpr int FUSED_WIDTH = 256;   // the widest rows
+constexpr int FUSED_WIDTH = ONE_RUN;   // the widest rows
 constexpr int P_ROWS = 128, FUSED_THREADS = 32 * (EPI_WARPS + 3);
 struct FusedShared {
     uint64_t full[8], empty[8], p_full[2], p_empty[2], s_full[2], s_empty[2], g_full[2], g_empty[2], acc_full, acc_empty, sums_full, drain[2];
@@ -1744,10 +1802,10 @@ int logits_of(ep_ctx *ctx, Inputs &in, const Operand &x, const Operand &w, int64
                        EP_F32, false, nullptr, share, in.stream, &in.kernels);
 }
 
-template <bool GRAD, bool BIASED, typename T>
+template <bool GRAD, bool BIASED, bool RUNS, typename T>
 int launch_tiles_of(ep_ctx *ctx, const CUtensorMap &x, const CUtensorMap &w, const CUtensorMap &g, const CUtensorMap &clean,
                     const TileWork &e, cudaStream_t stream) {
-    auto kernel = entropy_tiles<GRAD, BIASED, T>;
+    auto kernel = entropy_tiles<GRAD, BIASED, RUNS, T>;
     constexpr size_t smem = TileMemory<GRAD>::TOTAL;
     EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     cudaLaunchConfig_t cfg{};
@@ -1779,13 +1837,20 @@ int launch_tiles(ep_ctx *ctx, const Operand &x, const Operand &w, void *g, int64
         (GRAD && !(encode_result(&mg, g, x.type, 1, e.M, e.N, ld, TILE) && encode_operand(&mc, clean, false, BLOCK_ROWS))))
         return ep::fail(ctx, EP_ERR_CUDA, "cuTensorMapEncodeTiled failed for %lld rows of %d classes", (long long)e.M, e.N);
     ++*kernels;
-    if constexpr (!GRAD) {
-        if (e.bias)
-            return x.type == EP_BF16 ? launch_tiles_of<GRAD, true, __nv_bfloat16>(ctx, mx, mw, mg, mc, e, stream)
-                                     : launch_tiles_of<GRAD, true, __half>(ctx, mx, mw, mg, mc, e, stream);
-    }
-    return x.type == EP_BF16 ? launch_tiles_of<GRAD, false, __nv_bfloat16>(ctx, mx, mw, mg, mc, e, stream)
-                             : launch_tiles_of<GRAD, false, __half>(ctx, mx, mw, mg, mc, e, stream);
+    auto launch = [&](auto biased, auto runs, auto type) {
+        return launch_tiles_of<GRAD, decltype(biased)::value, decltype(runs)::value, decltype(type)>(ctx, mx, mw, mg, mc, e, stream);
+    };
+    auto of_type = [&](auto biased, auto runs) {
+        return x.type == EP_BF16 ? launch(biased, runs, __nv_bfloat16{}) : launch(biased, runs, __half{});
+    };
+    const std::true_type yes;
+    const std::false_type no;
+    if constexpr (GRAD)
+        return of_type(no, yes);
+    else if (x.cols > ONE_RUN)
+        return e.bias ? of_type(yes, yes) : of_type(no, yes);
+    else
+        return e.bias ? of_type(yes, no) : of_type(no, no);
 }
 
 struct ForwardSpace {

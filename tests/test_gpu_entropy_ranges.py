@@ -41,3 +41,53 @@ def test_a_common_shift_of_the_logits(dtype, classes, rows, n_in, by):
         r = forward(x, w, t, b)
         got = backward(x, w, t, r, b, one(), rand((rows,), F32, 5, 1.0 / rows))
         assert all(bool(torch.isfinite(g).all()) for g in got)
+
+
+# ---------------------------------------------------------------------------------------------- sums of logits
+def one_class(x, w):
+    """The logits themselves, as lse of a single class."""
+    return ep().ep_cross_entropy(x, w, torch.zeros(x.shape[0], device="cuda", dtype=torch.int32)).lse.double()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n_in", [60, 256, 264, 1024, 4096, 65536])
+def test_logits_of_one_element_are_exact(dtype, n_in):
+    """One product of 8 by 8 or 11 by 11 bits fits fp32: what is off is 1 / log 2 and log 2 and the products with them, 2^-24 of the logit
+    each.  Up to 256 elements a sum is given back what dense ones lose of it on average: (5 + 1.9 * 16) 1e-8 of itself at most."""
+    rows = 200
+    w, at = rand((1, n_in), dtype, 1), torch.arange(rows, device="cuda") * 37 % n_in
+    x = torch.zeros(rows, n_in, device="cuda", dtype=dtype)
+    x[torch.arange(rows, device="cuda"), at] = rand((rows,), dtype, 2, 16.0)
+    want = (x.double() * w.double()).sum(1)
+    most = 2.0 ** -22 + (3.54e-7 if n_in <= 256 else 0.0)
+    ref.within(one_class(x, w), want, most * want.abs(), "lse")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n_in", [300, 1024, 4096, 65536])
+def test_logits_of_one_sign(dtype, n_in):
+    """Sums of one sign lose the most: with every step of 16 products up to 2^-23 of the sum so far, and as much where the products are
+    brought to one exponent.  After 8 steps they are added up to nearest, which costs 2^-24 of the sum each time."""
+    x, w = rand((64, n_in), dtype, 1).abs(), rand((1, n_in), dtype, 2).abs()
+    want = (x.double() * w.double()).sum(1)
+    ref.within(one_class(x, w), want, (16 * 2.0 ** -23 + -(-n_in // 128) * 2.0 ** -24 + 2.0 ** -22) * want, "lse")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n_in", [264, 1024, 4096, 65536])
+def test_slopes_of_exact_logits(dtype, n_in):
+    """dbias of a single row is that row of G, not rounded to the operands' type: p is off by 2^-20 of itself beside what the exponent's two
+    roundings cost, 2^-22 (|l| + |lse|)."""
+    classes = 40
+    x, w = torch.zeros(1, n_in, device="cuda", dtype=dtype), rand((classes, n_in), dtype, 1)
+    x[0, n_in // 2] = 1.0
+    w[:, n_in // 2] = torch.linspace(56, 64, classes, device="cuda").to(dtype)
+    t = torch.zeros(1, device="cuda", dtype=torch.int32)
+    l = w[:, n_in // 2].double()
+    lse = torch.logsumexp(l, 0)
+    r = ep().ep_cross_entropy(x, w, t)._replace(lse=lse.float()[None])
+    got = ep().ep_cross_entropy_backward(x, w, t, r, None, one()).dbias
+    p = torch.exp(l - r.lse.double())
+    want = p.clone()
+    want[0] -= 1.0
+    ref.within(got, want, p * (2.0 ** -20 + 2.0 ** -22 * (l.abs() + lse.abs())) + 2.0 ** -24 * want.abs(), "dbias")
