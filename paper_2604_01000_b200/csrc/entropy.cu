@@ -987,13 +987,13 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
 }
 
 // The sums of P tiles that several workers had a part of, in the workers' order.  The tile that worker blockIdx.x begins inside
-// of, if it is the first to do so; `rows` rows a block.
+// of, if it is the first to do so (the second of those that share it); `rows` rows a block.
 template <typename T>
 __global__ void __launch_bounds__(256) entropy_join(const FusedWork e, int rows) {
     ep_wait_for_launch_before();
-    const int64_t begin = e.line.begin(blockIdx.x), tile = begin / e.line.inner;
+    const int64_t tile = e.line.begin(blockIdx.x) / e.line.inner;
     const int w0 = e.line.first_worker(tile), w1 = e.line.last_worker(tile);
-    if (w0 == w1 || (int)blockIdx.x != (begin == tile * e.line.inner ? w0 : w0 + 1)) return;
+    if (w0 == w1 || (int)blockIdx.x != w0 + 1) return;
     const float down = e.scale->down;
     const int row0 = blockIdx.y * rows, chunks = e.share_ld / 4;
     // (the first worker has it as its last segment unless that is its only one, the others as their first)
