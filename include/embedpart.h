@@ -520,7 +520,8 @@ int ep_route_backward(ep_ctx *ctx, const void *logits, int32_t type, int64_t row
  *   aligned  (of the queries) as for ep_linear
  * A row whose every class is closed takes no part either (row_loss 0, lse -infinity).  A target that is closed while others are
  * not has row_loss infinity.  A NaN or +infinity among the logits of a row that takes part makes its lse and loss
- * NaN.  With R = 0 loss is 0.
+ * NaN.  With R = 0 loss is 0.  (A bias of the type's lowest value closes no class: beside others its loss is that large.  lse is fp32: where all
+ * logits of a row are so far from zero that it has no bits for their differences, the backward has none either.)
  * Logits are fp32 sums.  Of 16-bit inputs the tensor cores make them, which cut a sum off toward zero after every 16 products: nothing of
  * a sum that fits fp32, 1e-7 of one of one sign, on average 1.5e-8 (EP_BF16) to 1.9e-8 of dense ones.  More than 256 elements are summed 128
  * at a time and added up to nearest, so that a logit loses no more than 8 such steps do; up to 256 are summed at once, and what dense

@@ -1020,7 +1020,7 @@ __global__ void __launch_bounds__(256) entropy_join(const FusedWork e, int rows)
     }
 }
 
-// The classes' bias over log 2, padded to whole tiles (a finite bias stays finite: only -infinity closes a class).
+// The classes' bias over log 2, padded to whole tiles (a finite bias stays finite: only -infinity closes a class; see entropy_finish).
 __device__ __forceinline__ float padded_bias(const void *bias, int type, int c, int classes) {
     const float b = c < classes ? load_param(bias, type, c) : 0.f;
     return fabsf(b) < INFINITY ? fminf(fmaxf(b * LOG2E, -FLT_MAX), FLT_MAX) : b;
@@ -1144,7 +1144,8 @@ __device__ __forceinline__ void sum_block(double &total, long long &live, double
         }
 }
 __global__ void __launch_bounds__(256) entropy_finish(const Statistics stats, const float *at_target, const int32_t *targets, int64_t rows,
-                                                      int classes, float *lse, float *row_loss, const Finish f, int *status) {
+                                                      int classes, const void *bias, int bias_type, float *lse, float *row_loss, const Finish f,
+                                                      int *status) {
     __shared__ double sum[8];
     __shared__ long long count[8];
     __shared__ bool last;
@@ -1160,7 +1161,10 @@ __global__ void __launch_bounds__(256) entropy_finish(const Statistics stats, co
             if (r.m == -INFINITY && r.s == 0.f)   // every class is closed: the row takes no part
                 z = -INFINITY;
             else {
-                loss = z - at_target[row] * (stats.tiled ? LN2 : 1.f);
+                float at = at_target[row] * (stats.tiled ? LN2 : 1.f);
+                // (over log 2 a bias near fp32's lowest value was cut off at that value: beside other classes the logit is the bias)
+                if (stats.tiled && bias && at_target[row] == -FLT_MAX && z > at) at = load_param(bias, bias_type, targets[row]);
+                loss = z - at;
                 live = 1;
             }
         }
@@ -1920,7 +1924,7 @@ int forward_run(ep_ctx *ctx, Inputs &in, const ForwardSpace &s, float *loss, flo
     f.loss = loss;
     f.counted = counted;
     EP_CUDA(ctx, ep::launch_early(entropy_finish, dim3((unsigned)ep::ceil_div(in.rows, FINISH_ROWS)), dim3(256), 0, in.stream, stats, s.at_target,
-                                  in.targets, in.rows, in.classes, lse, row_loss, f, ctx->d_status));
+                                  in.targets, in.rows, in.classes, in.bias, in.bias_type, lse, row_loss, f, ctx->d_status));
     ++in.kernels;
     return EP_OK;
 }
@@ -2317,8 +2321,8 @@ int small_forward(ep_ctx *ctx, Inputs &in, const SmallSpace &s, float *loss, flo
     f.loss = loss;
     f.counted = counted;
     EP_CUDA(ctx, ep::launch_early(entropy_finish, dim3((unsigned)ep::ceil_div(in.rows, FINISH_ROWS)), dim3(256), 0, in.stream,
-                                  Statistics{s.stats, in.rows, false, Line{}, e.class_tiles}, s.at_target, in.targets, in.rows, in.classes, lse,
-                                  row_loss, f, ctx->d_status));
+                                  Statistics{s.stats, in.rows, false, Line{}, e.class_tiles}, s.at_target, in.targets, in.rows, in.classes, in.bias,
+                                  in.bias_type, lse, row_loss, f, ctx->d_status));
     in.kernels += 2;
     return EP_OK;
 }

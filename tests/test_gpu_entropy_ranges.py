@@ -91,3 +91,16 @@ def test_slopes_of_exact_logits(dtype, n_in):
     want = p.clone()
     want[0] -= 1.0
     ref.within(got, want, p * (2.0 ** -20 + 2.0 ** -22 * (l.abs() + lse.abs())) + 2.0 ** -24 * want.abs(), "dbias")
+
+
+# ---------------------------------------------------------------------------------------------- a class closed by the type's lowest value
+@pytest.mark.parametrize("dtype,bias_dtype", [(BF16, F32), (BF16, BF16), (F16, F32), (F32, F32), (F32, BF16)])
+@pytest.mark.parametrize("rows,n_in", [(50, 24), (400, 264)])
+def test_loss_against_a_class_of_the_lowest_bias(dtype, bias_dtype, rows, n_in):
+    x, w, t = trained(rows, n_in, 90, dtype, 1)
+    b = rand((90,), bias_dtype, 2)
+    b[30:60] = torch.finfo(bias_dtype).min
+    r = forward(x, w, t, b)
+    assert bool(((t >= 30) & (t < 60)).any())
+    got = backward(x, w, t, r, b, one())
+    assert bool((got.dbias[30:60] <= 0).all())
