@@ -104,3 +104,101 @@ def test_loss_against_a_class_of_the_lowest_bias(dtype, bias_dtype, rows, n_in):
     assert bool(((t >= 30) & (t < 60)).any())
     got = backward(x, w, t, r, b, one())
     assert bool((got.dbias[30:60] <= 0).all())
+
+
+# ---------------------------------------------------------------------------------------------- each kernel of the backward
+NARROW = [(30000, 64, 100), (17000, 96, 100), (1800, 200, 100)]
+WIDE = [(1200, 264, 300)]
+
+
+@pytest.mark.parametrize("rows,n_in,classes", NARROW + WIDE)
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_only_what_is_wanted(dtype, rows, n_in, classes):
+    assert goes_by_tiles(rows, n_in, classes)
+    x, w, t = trained(rows, n_in, classes, dtype, 10, 0.1)
+    b = rand((classes,), F32, 11)
+    r = forward(x, w, t, b)
+    whole = backward(x, w, t, r, b, one())
+    for wanted in ((0,), (1,), (2,), (0, 1), (0, 2), (1, 2)):
+        got = backward(x, w, t, r, b, one(), **{n: i in wanted for i, n in enumerate(("need_dx", "need_dweight", "need_dbias"))})
+        assert all(torch.equal(got[i], whole[i]) if i in wanted else got[i] is None for i in range(3)), wanted
+
+
+@pytest.mark.parametrize("rows,n_in", [(40000, 32), (2000, 160), (1000, 272)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_far_logits_of_each_kernel(dtype, rows, n_in):
+    # logits of hundreds: one class has all of it; masks of the type's lowest value beside it
+    assert goes_by_tiles(rows, n_in, 90)
+    x, w = rand((rows, n_in), dtype, 16, 30.0), rand((90, n_in), dtype, 17, 5.0)
+    t = some_targets(rows, 90, 18).clamp(min=40)
+    b = torch.zeros(90, device="cuda")
+    b[:40] = torch.finfo(F32).min
+    r = forward(x, w, t, b)
+    backward(x, w, t, r, b, one())
+    bad = x.clone()
+    bad[7, 3] = math.nan
+    r = ep().ep_cross_entropy(bad, w, t, b)
+    got = ep().ep_cross_entropy_backward(bad, w, t, r, b, one())
+    spoiled = torch.isnan(got.dx).any(1)
+    assert bool(spoiled[7]) and int(spoiled.sum()) == 1
+
+
+@pytest.mark.parametrize("rows,n_in", [(40000, 32), (2000, 160), (1000, 272)])
+def test_fp16_gradients_of_any_size(rows, n_in):
+    # a mean over many rows puts whole gradients below fp16's range
+    assert goes_by_tiles(rows, n_in, 64)
+    x, w, t = trained(rows, n_in, 64, F16, 30)
+    r = forward(x, w, t)
+    for g in (1e-4, 3e4, -1e-30, 1e-40):
+        backward(x, w, t, r, None, torch.full((1,), g, device="cuda"))
+    drow = rand((rows,), F32, 31) * torch.logspace(-6, 2, rows, device="cuda")
+    drow[::5] = 0
+    backward(x, w, t, r, None, None, drow)
+
+
+@pytest.mark.parametrize("sizes", [((2500, 64, 900), (900, 200, 300)), ((3000, 128, 200), (900, 264, 300))])
+def test_graphs_of_each_kernel_on_two_streams(sizes):
+    m = ep()
+    cases = [trained(rows, n_in, classes, dtype, 31 + i, 0.1) for i, ((rows, n_in, classes), dtype) in enumerate(zip(sizes, (BF16, F16)))]
+    assert all(goes_by_tiles(*s) for s in sizes)
+    ones = one()
+
+    def both(a, b, c):
+        r = m.ep_cross_entropy(a, b, c)
+        return [*r, *m.ep_cross_entropy_backward(a, b, c, r, None, ones)]
+    want = [both(*c) for c in cases]
+    torch.cuda.synchronize()
+    graphs, outs, streams = [], [], []
+    for c in cases:
+        s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            outs.append(both(*c))
+        graphs.append(g)
+        streams.append(s)
+    for _ in range(5):
+        for o in outs:
+            for p in o:
+                p.zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for o, w in zip(outs, want) for a, b in zip(o, w))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n_in", [64, 130, 256, 264])
+def test_rows_without_a_class_and_spoiled_ones_of_each_kernel(dtype, n_in):
+    rows, classes = (20000, 70) if n_in <= 128 else (1500, 70)
+    assert goes_by_tiles(rows, n_in, classes)
+    x, w, t = trained(rows, n_in, classes, dtype, 40, 0.3)
+    b, drow = rand((classes,), F32, 41) - 30, rand((rows,), F32, 42)
+    r = forward(x, w, t, b)
+    clean = backward(x, w, t, r, b, one(), drow)
+    bad = x.clone()
+    bad[t < 0] = torch.tensor([math.nan, math.inf], device="cuda").repeat(n_in // 2).to(dtype)
+    q = ep().ep_cross_entropy(bad, w, t, b)
+    assert all(torch.equal(p, s) for p, s in zip(r, q))
+    got = ep().ep_cross_entropy_backward(bad, w, t, q, b, one(), drow.masked_fill(t < 0, math.nan))
+    assert all(torch.equal(p, s) for p, s in zip(got, clean))
