@@ -523,8 +523,8 @@ int ep_route_backward(ep_ctx *ctx, const void *logits, int32_t type, int64_t row
  * NaN.  With R = 0 loss is 0.  (A bias of the type's lowest value closes no class: beside others its loss is that large.  lse is fp32: where all
  * logits of a row are so far from zero that it has no bits for their differences, the backward has none either.)
  * Logits are fp32 sums.  Of 16-bit inputs the tensor cores make them, which cut a sum off toward zero after every 16 products: nothing of
- * a sum that fits fp32, 1e-7 of one of one sign, on average 1.5e-8 (EP_BF16) to 1.9e-8 of dense ones.  More than 256 elements are summed 128
- * at a time and added up to nearest, so that a logit loses no more than 8 such steps do; up to 256 are summed at once, and what dense
+ * a sum that fits fp32, 1e-7 of one of one sign, on average 1.5e-8 (EP_BF16) to 1.9e-8 of dense ones.  More than 256 elements are summed 256
+ * at a time and added up to nearest, so that a logit loses no more than 16 such steps do; up to 256 are summed at once, and what dense
  * rows lose of them on average, up to 3.6e-7 of the logit, is added again, whatever they hold.
  * Of EP_F32 inputs they are ep_linear's, or, for few of them, fp32 multiply-adds; an infinity in x or w makes the logits it
  * reaches NaN either way.

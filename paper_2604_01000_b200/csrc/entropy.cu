@@ -8,6 +8,7 @@
 // piece at a time (some rows by some classes, small enough to stay in the L2 until both products have read it).
 // fp32 inputs are split into three bf16 numbers as in linear.cu; a piece of their logits is made by the products' own tile
 // kernel, and row kernels go over it to the same ends; few of them, and few 16-bit ones' gradients, go without either (small problems, below).
+// Logits of more than 256 16-bit elements are summed in runs (sums_log2e, below).
 //
 // Measured, on the device.  Forward of 169343 x 128 -> 4096 bf16: 231 us; the product alone would need 109 us at 1625 TFLOP/s, its 694
 // million exponentials 154 us at 16 a clock and SM: bound by the issue of what is around them (0.44 a clock and scheduler; the tensor pipe
@@ -52,7 +53,7 @@ __device__ __forceinline__ int target_of(const int32_t *targets, int64_t row, in
 // ---------------------------------------------------------------------------------------------- logits by tiles
 //
 // A pair of blocks works on 256 rows x 256 classes at a time (see linear.cu, whose pipeline this is: one warp loads, one of
-// the first block multiplies, 16 finish a tile while the next one is being summed).  Workers share out the tiles evenly, in
+// the first block multiplies, 16 finish a tile, or take a run's sums, while the next is being summed).  Workers share out the tiles evenly, in
 // one long line: row tile after row tile in the forward (a thread keeps its row's statistics from tile to tile), class tile after
 // class tile in the backward (a thread keeps its classes' sums), each worker a stretch of it.  What a worker has when its
 // stretch or its row (class) tile ends is a partial result, number `worker - first worker of that tile`.
@@ -121,14 +122,14 @@ struct RowInfo {
 // The tensor cores cut a sum off after every 16 products, toward zero, they do not round it.  What that costs depends on what is summed:
 // nothing where the sum fits fp32 (rows of one element, or of few bits), 1e-7 of the sum a step where all products have one sign, and
 // of dense rows of either sign, on average and within a fifth, (2.5 + 1.5 steps) 1e-8 of the sum in bf16, (5 + 1.9 steps) 1e-8 in fp16.
-// So a logit of more than 256 elements is summed in runs of 8 such steps, which are added up to nearest in registers: however long it is,
-// it loses what one run does.  (Forward and backward, us, in one run -> in such: 169343 x 512 -> 4096 bf16 451 -> 620 and 2163 -> 2793, 20000 x
-// 1024 -> 4096 108 -> 138 and 474 -> 554, 8192 x 4096 -> 4096 203 -> 233 and 595 -> 639: two accumulators in the tensor memory are one tile's, not
-// two.  Runs of 16 steps take 506, 120 and 218 in the forward and lose 3.5e-7.)
+// So a logit of more than 256 elements is summed in runs of 16 such steps, as fp32 products are in linear.cu, which are added up to nearest
+// in registers: however long it is, it loses what one run does.  (Forward and backward, us, in one run -> in such: 169343 x 512 -> 4096 bf16
+// 440 -> 501 and 2162 -> 2503, 20000 x 1024 -> 4096 107 -> 119 and 472 -> 532, 8192 x 4096 -> 4096 197 -> 213 and 581 -> 626: a run is handed
+// over while there is room for one more.  Runs of 8 steps would lose half as much and take 612, 138 and 223; 2794, 549 and 628.)
 // Up to 256 elements a logit is one run, of up to 16 steps.  Many rows' sums (dbias) would keep the part of its loss that has always the same
 // sign (100000 x 256 -> 10 in bf16: dbias off by 1.4e-5 of itself, so by 1.1e-6); what dense rows lose on average is therefore given back there
 // with the factor 1 / log 2: at most 3.6e-7 of the logit, three units of fp32's last place, by which a sum that lost nothing is too large.
-constexpr int ONE_RUN = 256, RUN_KB = 2;   // elements; k-blocks of a run of longer sums
+constexpr int ONE_RUN = 256, RUN_KB = ONE_RUN / 64;   // elements of a run, and its k-blocks
 float sums_log2e(int n_in, int type) {
     const double steps = (n_in + 15) / 16, lost = n_in > ONE_RUN ? 0.0 : type == EP_BF16 ? 2.5 + 1.5 * steps : 5.0 + 1.9 * steps;
     return (float)(1.4426950408889634 * (1.0 + 1e-8 * lost));
@@ -578,9 +579,9 @@ struct FusedMemory {
     static constexpr int EXTRA = (DW ? 3 : 1) * Q_ROWS * 4;      // what is known of Q's rows: shift, g, target; or the classes' bias
     static constexpr int Q_BYTES = BOXES * Q_ROWS * 128, STAGE = Q_BYTES + 2048;
     static constexpr int STAGES = WIDE ? 2 : 4;
-    // The tensor memory: a tile or two of S, two of G (two of its numbers to a column), the sums.  (Tiles of 64 rows of Q, so that
-    // there is room for two of S beside sums of 256 columns, need twice the instructions of S and have the shared memory read
-    // P twice as often: 4096 x 256 -> 169343 in 1340 us.)
+    // The tensor memory: a tile or two of S, two of G (two of its numbers to a column), the sums.  (G has columns of its own, so that
+    // beside sums of 256 columns there is room for one S.  Tiles of 64 rows of Q, two of which fit, need twice the instructions of S
+    // and have the shared memory read P twice as often: 4096 x 256 -> 169343 in 1340 us.)
     static constexpr int LOGITS = WIDE ? 1 : 2, SLOPES = 2;
     static constexpr int G_AT = LOGITS * Q_ROWS, ACC = G_AT + SLOPES * Q_ROWS / 2;
     static constexpr size_t TOTAL = 1024 + P_BUFFERS * P_BYTES + STAGES * STAGE + sizeof(FusedShared);

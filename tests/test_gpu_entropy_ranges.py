@@ -66,8 +66,8 @@ def test_logits_of_one_element_are_exact(dtype, n_in):
 @pytest.mark.parametrize("dtype", [BF16, F16])
 @pytest.mark.parametrize("n_in", [300, 1024, 4096, 65536])
 def test_logits_of_one_sign(dtype, n_in):
-    """Sums of one sign lose the most: with every step of 16 products up to 2^-23 of the sum so far, and as much where the products are
-    brought to one exponent.  After 8 steps they are added up to nearest, which costs 2^-24 of the sum each time."""
+    """Sums of one sign lose the most, with every step of 16 products 1e-7 of the result, which is below 2^-23.  After 16 steps at most they are
+    added up to nearest, which costs 2^-24 of the sum each time (twice as many of them are allowed for)."""
     x, w = rand((64, n_in), dtype, 1).abs(), rand((1, n_in), dtype, 2).abs()
     want = (x.double() * w.double()).sum(1)
     ref.within(one_class(x, w), want, (16 * 2.0 ** -23 + -(-n_in // 128) * 2.0 ** -24 + 2.0 ** -22) * want, "lse")
