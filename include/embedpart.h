@@ -536,9 +536,10 @@ int ep_route_backward(ep_ctx *ctx, const void *logits, int32_t type, int64_t row
  *   dx        [dev] out or NULL, rows x n_in of in_type;  dweight [dev] out or NULL, classes x n_in of in_type
  *   dbias     [dev] out or NULL, classes fp32
  * The logits are made once more, a piece at a time.  G is rounded to in_type before the products of 16-bit types (not of few,
- * rows * classes * n_in up to 2^26, rows and classes rounded up to 64s, with n_in <= 128: it stays fp32 there), for EP_F16
- * after multiplication by the power of two that brings the largest |g| to 2^14 (the sums are scaled back): elements below
- * 2^-39 of that largest are lost.  dbias is summed from G before that rounding.
+ * rows * classes * n_in up to 2^26, rows and classes rounded up to 64s, with n_in <= 128: it stays fp32 there).  Without drow_loss
+ * it is measured in |g|, which all rows share, so that the target's -g is exact and what is rounded are chances (1 is 2^14 of
+ * EP_F16); with it G of EP_F16 is multiplied by the power of two that brings the largest |g| to 2^14.  The sums are scaled
+ * back.  In EP_F16 elements below 2^-39 of the largest are lost.  dbias is summed from G before that rounding.
  * Rows that take no part are not multiplied where they hold a NaN, an infinity or a number from 1e18 on: x is then read from a copy
  * in the workspace, with zeros there.
  */

@@ -106,9 +106,14 @@ struct Stretch {
     }
 };
 
-// What the blocks of entropy_weights have found, together.  fp16 holds nothing below 2^-25, where a mean over many rows puts
-// whole gradients: G is multiplied by the power of two that brings the largest |g| to [2^14, 2^15) (|p - 1| is at most 1), and
-// the products' sums by its inverse.
+// What the blocks of entropy_weights have found, together.  G is rounded to 16 bits, so what it is measured in matters.
+// The gradient of a mean (no weights of the rows' own) has the same g in every row, and -g where the target is unlikely: rounded, all of
+// a gradient would be off by the same up to 2^-8 in bf16.  There G is measured in |g|, 2^14 of which are 1 in fp16, and the products' sums are
+// multiplied by |g|: -1 is exact, and what is rounded are chances (of a target less likely than 2^-9, p is lost beside 1).  255 x 64 rows of 3000
+// classes, bf16: gradients were off by 3.6e-3 in common, now by p = 3.3e-4; in all by 0.0017 of themselves, as their own rounding leaves.
+// Otherwise fp16, which holds nothing below 2^-25, takes the power of two that brings the largest |g| to [2^14, 2^15) (|p - 1| is at
+// most 1), and the sums its inverse.
+// up: what g and the slopes still have to be multiplied by.
 struct Scale {
     float up, down;
     int unclean;
@@ -116,7 +121,7 @@ struct Scale {
 // What the backward knows of each row, padded by a tile.  Rows that take no part, and those past the end: -infinity, 0, -1.
 struct RowInfo {
     float *shift;   // -lse / log 2 + log2 |g|: the slope of a class that is not the target is 2^(l / log 2 + shift), or minus that
-    float *g;
+    float *g;       // in what G is measured in
     int *target;
     __host__ __device__ RowInfo from(int64_t row) const { return RowInfo{shift + row, g + row, target + row}; }
 };
@@ -1198,24 +1203,41 @@ __global__ void __launch_bounds__(256) entropy_finish(const Statistics stats, co
 }
 
 // ---------------------------------------------------------------------------------------------- backward
-// What is known of each row, and each block's largest finite |g|.  A row that takes no part counts for nothing, whatever x holds
+// What is known of each row, and each block's largest finite |g|, in what G is measured in.  A row that takes no part counts for nothing, whatever x holds
 // there; but 0 times an infinity or a NaN is NaN, so such rows of x are looked through: a block's `unclean` is 1 where one
 // holds any (or numbers so large that a logit might overflow), and the products then read a copy of x with zeros there.
 constexpr int WEIGHT_THREADS = 512;
-__device__ __forceinline__ Scale scale_of(float top, bool scaled, int unclean) {
-    const int up = scaled && top > 0.f ? min(14 - ilogbf(top), 126) : 0;
+// How G of 16 bits is measured: in |g| of all rows, or, with weights of their own, by a power of two; `log2_unit`: what 1 becomes.
+struct Measure {
+    const float *dloss;
+    const long long *counted;
+    bool mean;        // no row has a weight of its own
+    bool scaled;      // by a power of two, where not by |g|
+    int log2_unit;
+};
+__device__ __forceinline__ double mean_weight(const Measure &m) {
+    return m.dloss ? (double)*m.dloss / (double)(*m.counted > 0 ? *m.counted : 1) : 0.0;
+}
+// |g| of all rows, or 0 (which leaves what is measured in it and its inverse far from the ends of fp32).
+__device__ __forceinline__ float common_weight(const Measure &m, double mean) {
+    const float g = fabsf((float)mean);
+    return m.mean && g >= 7.9e-31f && g <= 1.2e30f ? g : 0.f;
+}
+__device__ __forceinline__ Scale scale_of(float common, float top, const Measure &m, int unclean) {
+    if (common > 0.f) return Scale{1.f, scalbnf(common, -m.log2_unit), unclean};
+    const int up = m.scaled && top > 0.f ? min(14 - ilogbf(top), 126) : 0;
     return Scale{scalbnf(1.f, up), scalbnf(1.f, -up), unclean};
 }
 template <typename T>
 __global__ void __launch_bounds__(WEIGHT_THREADS) entropy_weights(const float *__restrict__ lse, const int32_t *__restrict__ targets, int64_t rows,
-                                                                  int classes, const long long *__restrict__ counted,
-                                                                  const float *__restrict__ dloss, const float *__restrict__ drow,
+                                                                  int classes, const Measure measure, const float *__restrict__ drow,
                                                                   const void *__restrict__ x, int64_t ldx, int n_in,
                                                                   const void *__restrict__ bias, int bias_type, float *padded, RowInfo info,
-                                                                  float *peaks, int *unclean, bool scaled, Scale *scale, int *status) {
+                                                                  float *peaks, int *unclean, Scale *scale, int *status) {
     __shared__ int bad_rows;
     __shared__ float tops[WEIGHT_THREADS / 32];
-    const double mean = dloss ? (double)*dloss / (double)(*counted > 0 ? *counted : 1) : 0.0;   // (the two terms may cancel)
+    const double mean = mean_weight(measure);   // (it and a row's own may cancel)
+    const float common = common_weight(measure, mean), unit = scalbnf(1.f, measure.log2_unit);
     const int lane = threadIdx.x & 31;
     if (bias)   // (on the way: the bias as the tile kernels read it)
         for (int c = blockIdx.x * WEIGHT_THREADS + threadIdx.x; c < (classes + TILE - 1) / TILE * TILE; c += gridDim.x * WEIGHT_THREADS)
@@ -1228,7 +1250,7 @@ __global__ void __launch_bounds__(WEIGHT_THREADS) entropy_weights(const float *_
         bool dead = false;
         if (row < rows) {
             dead = target_of(targets, row, classes, status) < 0 || lse[row] == -INFINITY;
-            const float g = dead ? 0.f : (float)(mean + (drow ? (double)drow[row] : 0.0));
+            const float g = dead ? 0.f : common > 0.f ? copysignf(unit, (float)mean) : (float)(mean + (drow ? (double)drow[row] : 0.0));
             const float z = lse[row];
             // (rounded once: a g that all rows share would else be off by the same in all of them, and their sums with it)
             info.shift[row] = dead ? -INFINITY : (float)(log2((double)fabsf(g)) - (double)z * 1.44269504088896340736);
@@ -1263,7 +1285,7 @@ __global__ void __launch_bounds__(WEIGHT_THREADS) entropy_weights(const float *_
     if (threadIdx.x == 0) {
         for (int w = 1; w < WEIGHT_THREADS / 32; ++w) top = fmaxf(top, tops[w]);
         if (gridDim.x == 1)   // nobody to wait for
-            *scale = scale_of(top, scaled, bad_rows);
+            *scale = scale_of(common, top, measure, bad_rows);
         else {
             peaks[blockIdx.x] = top;
             unclean[blockIdx.x] = bad_rows;
@@ -1271,7 +1293,7 @@ __global__ void __launch_bounds__(WEIGHT_THREADS) entropy_weights(const float *_
     }
 }
 
-__global__ void __launch_bounds__(256) entropy_scale(const float *peaks, const int *unclean, int n, bool scaled, Scale *out) {
+__global__ void __launch_bounds__(256) entropy_scale(const float *peaks, const int *unclean, int n, const Measure measure, Scale *out) {
     __shared__ float tops[8];
     float top = 0.f;
     bool bad = false;
@@ -1286,7 +1308,7 @@ __global__ void __launch_bounds__(256) entropy_scale(const float *peaks, const i
     const int any = __syncthreads_or(bad);
     if (threadIdx.x == 0) {
         for (int w = 1; w < 8; ++w) top = fmaxf(top, tops[w]);
-        *out = scale_of(top, scaled, any);
+        *out = scale_of(common_weight(measure, mean_weight(measure)), top, measure, any);
     }
 }
 
@@ -2001,13 +2023,13 @@ int prepare(ep_ctx *ctx, Inputs &in, const Space &s, const Given &g, Operand *x,
     auto weights = in.type == EP_F32    ? entropy_weights<float>
                    : in.type == EP_BF16 ? entropy_weights<__nv_bfloat16>
                                         : entropy_weights<__half>;
-    const bool scaled = in.type == EP_F16;
-    weights<<<s.blocks, WEIGHT_THREADS, 0, in.stream>>>(g.lse, in.targets, in.rows, in.classes, g.counted, g.dloss, g.drow, in.x, in.ldx, in.n_in,
+    const Measure measure{g.dloss, g.counted, in.type != EP_F32 && !g.drow, in.type == EP_F16, in.type == EP_F16 ? 14 : 0};
+    weights<<<s.blocks, WEIGHT_THREADS, 0, in.stream>>>(g.lse, in.targets, in.rows, in.classes, measure, g.drow, in.x, in.ldx, in.n_in,
                                                         s.copies.bias ? in.bias : nullptr, in.bias_type, s.copies.bias, s.rows, s.peaks,
-                                                        s.unclean, scaled, s.scale, ctx->d_status);
+                                                        s.unclean, s.scale, ctx->d_status);
     ++in.kernels;
     if (s.blocks > 1) {
-        EP_CUDA(ctx, ep::launch_early(entropy_scale, dim3(1), dim3(256), 0, in.stream, s.peaks, s.unclean, s.blocks, scaled, s.scale));
+        EP_CUDA(ctx, ep::launch_early(entropy_scale, dim3(1), dim3(256), 0, in.stream, s.peaks, s.unclean, s.blocks, measure, s.scale));
         ++in.kernels;
     }
     EP_CUDA(ctx, cudaGetLastError());
@@ -2068,7 +2090,7 @@ int backward_run(ep_ctx *ctx, Inputs &in, const Backward &s, const Given &given,
     const Pieces &p = s.pieces;
     const bool f32 = in.type == EP_F32;
     const size_t size = ep::type_size(in.type);
-    const float *factor = in.type == EP_F16 ? &s.scale->down : nullptr;
+    const float *factor = f32 ? nullptr : &s.scale->down;
     if (out.dbias && !f32)   // (not every piece has as many partial sums)
         EP_CUDA(ctx, cudaMemsetAsync(s.part, 0, sizeof(float) * s.kept * in.classes, in.stream));
     int64_t slab = 0;
@@ -2331,9 +2353,8 @@ int small_forward(ep_ctx *ctx, Inputs &in, const SmallSpace &s, float *loss, flo
 template <typename T>
 int small_backward(ep_ctx *ctx, Inputs &in, const SmallSpace &s, const Given &g, const Wanted &out) {
     const int blocks = weight_blocks(ctx, in.rows);
-    entropy_weights<float><<<blocks, WEIGHT_THREADS, 0, in.stream>>>(g.lse, in.targets, in.rows, in.classes, g.counted, g.dloss, g.drow, nullptr, 0,
-                                                                     0, nullptr, 0, nullptr, s.rows, s.peaks, s.unclean, false, s.scale,
-                                                                     ctx->d_status);
+    entropy_weights<float><<<blocks, WEIGHT_THREADS, 0, in.stream>>>(g.lse, in.targets, in.rows, in.classes, Measure{g.dloss, g.counted}, g.drow, nullptr,
+                                                                     0, 0, nullptr, 0, nullptr, s.rows, s.peaks, s.unclean, s.scale, ctx->d_status);
     EP_CUDA(ctx, cudaGetLastError());
     const bool over_rows = out.dweight || out.dbias;
     SmallWork e = small_work(in);

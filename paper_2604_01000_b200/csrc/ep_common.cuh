@@ -224,7 +224,7 @@ struct Matrix {
 int make_operands(ep_ctx *ctx, const Matrix &first, const Matrix &second, int type, cudaStream_t stream, Operand *a, Operand *b,
                   int *kernels);
 // out[M][N] = A B^T (+ what out holds, if accumulate) for the other files; *_mn: the operand is stored along its own rows, K of
-// them.  An operand with fewer than M or N rows counts as zero there.  factor: of fp16 results, a device value that the sums
+// them.  An operand with fewer than M or N rows counts as zero there.  factor: of 16-bit results, a device value that the sums
 // are multiplied by, or NULL.  type: the operands' (EP_F32 where they have three parts).
 size_t product_bytes(const ep_ctx *ctx, int64_t M, int N, int64_t K, int type, int out_type);
 int product(ep_ctx *ctx, const Operand &a, bool a_mn, const Operand &b, bool b_mn, int64_t M, int N, int64_t K, void *out, int out_type,

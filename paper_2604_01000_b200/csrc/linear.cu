@@ -51,7 +51,7 @@ struct Epilogue {
     bool vec;                         // out, preact, residual, bias, scales: 16-byte rows of whole 8-column chunks
     bool tma;                         // out and preact can be written by TMA, the residual read by 16 bytes
     bool params;                      // bias and w_scale, where there are any, are fp32 and start on 16 bytes
-    const float *factor;              // of fp16 results: what the sums are multiplied by first (one value), or NULL
+    const float *factor;              // of 16-bit results: what the sums are multiplied by first (one value), or NULL
     const int *other_b;               // where this device value is not 0, B is read by the map of z (there is no z then); or NULL
     float *share;                     // where a block's share of a split sum goes: [split][M][ld_share] fp32
     int ld_share;
@@ -84,7 +84,7 @@ struct Columns {
 template <typename O, int n>
 __device__ __forceinline__ void finish(const Epilogue &e, int64_t row, int col, const Columns<n> &c, float (&v)[n],
                                        const float (&r)[n]) {
-    if constexpr (std::is_same_v<O, __half>) {
+    if constexpr (sizeof(O) == 2) {
         if (e.factor) {
             const float f = *e.factor;
 #pragma unroll
@@ -490,7 +490,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
         uint32_t acc = 0;
         bool ok = true;
         const bool by_tma = e.tma && !e.share, with_z = e.preact != nullptr;
-        const bool scaled = std::is_same_v<O, __half> && e.factor && !e.share;   // (shares are joined first)
+        const bool scaled = sizeof(O) == 2 && e.factor && !e.share;   // (shares are joined first)
         const float factor = scaled ? *e.factor : 1.f;
         // The residual is copied into the slot that the result will leave from, and added in place.
         auto fetch_residual = [&](int64_t row0, int col) {

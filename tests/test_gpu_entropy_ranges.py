@@ -202,3 +202,32 @@ def test_rows_without_a_class_and_spoiled_ones_of_each_kernel(dtype, n_in):
     assert all(torch.equal(p, s) for p, s in zip(r, q))
     got = ep().ep_cross_entropy_backward(bad, w, t, q, b, one(), drow.masked_fill(t < 0, math.nan))
     assert all(torch.equal(p, s) for p, s in zip(got, clean))
+
+
+# ---------------------------------------------------------------------------------------------- what all elements of a gradient have in common
+def common_share(got, want):
+    """How much of `want` is missing in all of got: roundings by chance add up to nothing."""
+    got, want = got.double(), want.double()
+    return float(((got - want) * want).sum() / (want * want).sum())
+
+
+@pytest.mark.parametrize("dtype,rows,n_in,classes", [(BF16, 255 * 64, 64, 3000), (BF16, 255 * 8, 200, 3000), (BF16, 255 * 8, 272, 3000),
+                                                     (BF16, 255 * 8, 272, 40000), (F16, 2047 * 8, 64, 3000), (F16, 2047, 200, 3000), (F16, 2047, 272, 3000)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_a_mean_loss_scales_no_gradient(dtype, rows, n_in, classes, sign):
+    """1 / rows lies half-way between two numbers of 8 (11) bits: as such in every row's target, a gradient would be off by 2^-8 (2^-11) throughout.
+    Roundings by chance of n elements leave about UNIT / sqrt(n); sums in the tensor cores lose 1e-7 a step, some of it of one sign.  What may stay
+    in common: 1 - p is rounded to 1 where the target's p is below half the spacing there (2^-9, 2^-12), so that it is off by p; the mean of p bounds
+    that.  The result's own rounding is left out by rounding what is wanted, too (a single row's x times 1 / rows is rounded alike throughout)."""
+    x, w = rand((rows, n_in), dtype, 1, 0.3), rand((classes, n_in), dtype, 2, n_in ** -0.5)
+    t = some_targets(rows, classes, 3)
+    r = forward(x, w, t)
+    got = backward(x, w, t, r, None, sign * one())
+    l = x.double() @ w.double().T
+    G = ref.entropy_slopes(l, r.lse, t, sign * one(), None, rows)[0]
+    p = torch.exp(l.gather(1, t.long()[:, None])[:, 0] - r.lse.double())
+    for g, want in ((got.dx, G @ w.double()), (got.dweight, G.T @ x.double())):
+        most = ref.UNIT[dtype] * 8 / math.sqrt(want.numel()) + 1e-7 * max(rows, classes) / 16 * 0.1 + 1e-6 + float(p.mean())
+        if dtype == F16:      # below fp16's smallest normal number roundings are larger
+            most = most + 2.0 ** -25 / float(want.abs().mean()) * 8 / math.sqrt(want.numel())
+        assert abs(common_share(g, want.to(dtype))) <= most
