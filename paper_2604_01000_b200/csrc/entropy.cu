@@ -573,7 +573,7 @@ struct FusedShared {
     uint64_t full[8], empty[8], p_full[2], p_empty[2], s_full[2], s_empty[2], g_full[2], g_empty[2], acc_full, acc_empty, sums_full, drain[2];
     uint32_t tmem_base;
     int abort;
-    double sums[4][P_ROWS];
+    double sums[2][4][P_ROWS];   // of a class's slopes, by each of its row's four warps; of P tiles in turn
 };
 constexpr int Q_ROWS = 128;
 // WIDE: rows of more than 128 elements.
@@ -608,7 +608,7 @@ struct FusedWork {
     bool vec;                 // out can be written by 16 bytes
     float *share;             // [2 worker + segment][P_ROWS][share_ld]: sums of part of a P tile; then its dbias [..][P_ROWS]
     double *share_bias;
-    int share_ld;
+    int share_ld;             // (behind share, too: [worker][share_ld / 4][P_ROWS][4], the runs so far of a worker's P tile)
 };
 // Where a worker's part of P tile `tile` lies: its first segment's place, or its last one's.
 __host__ __device__ __forceinline__ int64_t share_of(const Line &l, int worker, int64_t tile) {
@@ -636,15 +636,88 @@ __device__ __forceinline__ void umma_from_tmem_elected(uint32_t d_tmem, uint32_t
                  : "memory");
 }
 
+// The sums of a run, or of the last one of a P tile or of this worker's part of it (over): put away, or with the earlier runs' to the gradient or this
+// worker's share.  By the 16 warps that make G, 32 columns of 32 rows each at a time.  false after an abort.  (What is put away lies so that a warp's
+// rows are side by side: 4096 x 256 -> 169343 in fp16, whose sums are put away after each 64 tiles, 1290 us; in rows as they are shared 1335; never 1290.)
+template <bool DW, bool WIDE, typename T>
+__device__ __forceinline__ bool put_away(const FusedWork &e, FusedShared *sh, int worker, int outer, int inner, bool over, int run) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, quad = warp & 3, column = warp >> 2;
+    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+    const int64_t p = (int64_t)outer * P_ROWS + quad * 32 + lane;
+    const float down = e.scale->down;
+    tc_fence_after();
+    const bool whole = e.line.first_worker(outer) == e.line.last_worker(outer);
+    const int64_t place = share_of(e.line, worker, outer), begin = e.line.begin(worker);
+    const int before = (int)(begin / e.line.inner);   // the P tile that this worker begins in
+    const bool kept = inner / run > (outer == before ? (int)(begin - (int64_t)before * e.line.inner) : 0) / run;   // earlier runs' sums
+    // (this thread's own: four columns of its row at a time, those of a warp's rows side by side)
+    float4 *const away = reinterpret_cast<float4 *>(e.share + (int64_t)(2 * e.line.workers + worker) * P_ROWS * e.share_ld) + quad * 32 + lane;
+#pragma unroll 1
+    for (int c0 = column * 32; c0 < e.width && e.out; c0 += 128) {
+        uint32_t a[32];
+        tmem_ld32_issue(lanes + FusedMemory<DW, WIDE>::ACC + c0, a);
+        tmem_ld_wait(a);
+        float v[32];
+#pragma unroll
+        for (int c = 0; c < 32; ++c) v[c] = __uint_as_float(a[c]);
+        if (kept) {
+#pragma unroll
+            for (int c = 0; c < 32; c += 4) {
+                const float4 k = away[(c0 + c) / 4 * P_ROWS];
+                v[c] += k.x, v[c + 1] += k.y, v[c + 2] += k.z, v[c + 3] += k.w;
+            }
+        }
+        if (!over) {
+#pragma unroll
+            for (int c = 0; c < 32; c += 4) away[(c0 + c) / 4 * P_ROWS] = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+        } else if (!whole) {
+            float *to = e.share + (place * P_ROWS + quad * 32 + lane) * e.share_ld + c0;
+#pragma unroll
+            for (int c = 0; c < 32; c += 4) *reinterpret_cast<float4 *>(to + c) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
+        } else if (p < e.P) {
+            T *to = static_cast<T *>(e.out) + p * e.width;
+#pragma unroll
+            for (int c = 0; c < 32; c += 8) {
+                float w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) w[i] = v[c + i] * down;
+                store_chunk(to, c0 + c, e.width, e.vec, w);
+            }
+        }
+    }
+    if constexpr (DW) {
+        if (e.dbias && over) {   // a class's sums are those of its row's four warps, in order
+            const uint32_t turn = (uint32_t)(outer - before) & 1u;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh->sums_full);
+            if (column == 0) {   // (the others write there again only after these have given the sums of products back)
+                if (!mbar_wait_warp(&sh->sums_full, turn, &sh->abort)) return false;
+                const int c = quad * 32 + lane;
+                const double(&part)[4][P_ROWS] = sh->sums[turn];
+                const double sum = ((part[0][c] + part[1][c]) + (part[2][c] + part[3][c])) * (double)down;
+                if (!whole)
+                    e.share_bias[place * P_ROWS + c] = sum;
+                else if (p < e.P)
+                    e.dbias[p] = (float)sum;
+            }
+        }
+    }
+    return true;
+}
+
 template <bool DW, bool BIASED, bool WIDE, typename T>
 __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_constant__ CUtensorMap map_p, const __grid_constant__ CUtensorMap map_q,
-                                                                 const __grid_constant__ CUtensorMap map_clean, const FusedWork e, int *status) {
+                                                                 const __grid_constant__ CUtensorMap map_clean, const __grid_constant__ FusedWork e, int *status) {
     using Mem = FusedMemory<DW, WIDE>;
     constexpr int STAGES = Mem::STAGES, LOGITS = Mem::LOGITS, SLOPES = Mem::SLOPES;
     // Warps to a row of S; groups of warps that take tiles in turn.  What a group waits for has barriers of its own (a barrier that
     // went on by two phases meanwhile could not be told from one that has not moved).
     constexpr int BQ = Q_ROWS, COLUMN_WARPS = BQ / 64, GROUPS = 4 / COLUMN_WARPS;
     static_assert(STAGES % GROUPS == 0 && SLOPES % GROUPS == 0 && GROUPS <= 2, "a group's stages and slopes are its own");
+    // Long sums are put away after 512 steps of 16 products (fp16) or 4096 (bf16), as in linear.cu: at tiles of Q whose number RUN divides.
+    // (In one go of 10584 steps a column of fp16 gradients that should be 0 came out as 3.8e-4 of its terms.)
+    constexpr int RUN = (std::is_same_v<T, __half> ? 512 : 4096) / (BQ / 16);
+    auto ends_run = [](const Stretch &t) { return t.left == 1 || t.inner + 1 == t.inners || (t.inner + 1) % RUN == 0; };
     extern __shared__ char smem_raw[];
     char *p_room = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     char *ring = p_room + Mem::P_BUFFERS * Mem::P_BYTES;               // [STAGES] of Q
@@ -774,7 +847,7 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
         const uint32_t q_base = smem_u32(ring);
         uint32_t j = 0, s = 0, buf = 0, lap = 0, segment = 0;
         for (Stretch t(e.line, worker); t.more(); t.next(), ++j) {
-            const bool first = j == 0 || t.inner == 0;
+            const bool first = j == 0 || t.inner % RUN == 0;
             if (!(ok = mbar_wait_warp(&sh->g_full[buf], lap, abort_flag))) break;
             if (first && !(ok = mbar_wait_warp(&sh->acc_empty, (segment & 1u) ^ 1u, abort_flag))) break;
             tc_fence_after();
@@ -787,7 +860,7 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
                                        !first || k > 0);
             commit_elected<false>(&sh->empty[s]);
             commit_elected<false>(&sh->g_empty[buf]);
-            if (t.left == 1 || t.inner + 1 == t.inners) {
+            if (ends_run(t)) {
                 commit_elected<false>(&sh->acc_full);
                 ++segment;
             }
@@ -805,7 +878,7 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
         const int quad = warp & 3, column = warp >> 2;   // TMEM lanes 32 quad.., and which of the warps that share them
         const int piece = column % COLUMN_WARPS, group = column / COLUMN_WARPS;
         const uint32_t lanes = tmem_base + ((uint32_t)(quad * 32) << 16);
-        const float up = e.scale->up, down = e.scale->down;
+        const float up = e.scale->up;
         uint32_t j = 0, segment = 0;
         int64_t p = 0;
         // of dx: what is known of this thread's row; of dW: its class's bias, and the scale of fp16
@@ -813,13 +886,15 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
         float shift = 0.f, weight = 0.f, bias = 0.f;
         bool negative = false;                                 // some row's g is
         const float log_up = std::is_same_v<T, __half> ? log2f(up) : 0.f, log2e = e.log2e;
-        double total = 0.0;                                    // (a class's slopes, of up to 2^31 rows; fp32 within a tile)
+        double *total = nullptr;                               // (a class's slopes, of up to 2^31 rows; fp32 within a tile)
+        uint32_t tiles = 0;
         for (Stretch t(e.line, worker); t.more(); t.next(), ++j) {
             if (j == 0 || t.inner == 0) {
                 p = (int64_t)t.outer * P_ROWS + quad * 32 + lane;
                 if constexpr (DW) {
                     if (BIASED) bias = (e.bias ? e.bias[p] : 0.f) + log_up;   // (padded)
-                    total = 0.0;
+                    total = &sh->sums[tiles++ & 1u][column][quad * 32 + lane];
+                    *total = 0.0;
                 } else {
                     shift = e.rows.shift[p] + log_up;
                     weight = e.rows.g[p] * up;
@@ -927,59 +1002,18 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
                 if constexpr (DW) {
                     float lo, hi;
                     here.get(lo, hi);
-                    total += (double)(lo + hi);
+                    *total += (double)(lo + hi);
                 }
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sh->g_full[gbuf]);
             }
-            if (t.left > 1 && t.inner + 1 < t.inners) continue;
-            // the end of a P tile, or of this worker's part of it
+            if (!ends_run(t)) continue;
+            // the end of a run; of a P tile, or of this worker's part of it
             if (!mbar_wait_warp(&sh->acc_full, segment & 1u, abort_flag)) break;
             ++segment;
-            tc_fence_after();
-            const bool whole = e.line.first_worker(t.outer) == e.line.last_worker(t.outer);
-            const int64_t place = share_of(e.line, worker, t.outer);
-#pragma unroll 1
-            for (int c0 = column * 32; c0 < e.width && e.out; c0 += 128) {
-                uint32_t a[32];
-                tmem_ld32_issue(lanes + Mem::ACC + c0, a);
-                tmem_ld_wait(a);
-                float v[32];
-#pragma unroll
-                for (int c = 0; c < 32; ++c) v[c] = __uint_as_float(a[c]);
-                if (!whole) {
-                    float *to = e.share + (place * P_ROWS + quad * 32 + lane) * e.share_ld + c0;
-#pragma unroll
-                    for (int c = 0; c < 32; c += 4) *reinterpret_cast<float4 *>(to + c) = make_float4(v[c], v[c + 1], v[c + 2], v[c + 3]);
-                } else if (p < e.P) {
-                    T *to = static_cast<T *>(e.out) + p * e.width;
-#pragma unroll
-                    for (int c = 0; c < 32; c += 8) {
-                        float w[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) w[i] = v[c + i] * down;
-                        store_chunk(to, c0 + c, e.width, e.vec, w);
-                    }
-                }
-            }
-            if constexpr (DW) {
-                if (e.dbias) {   // a class's sums are those of its row's four warps, in order
-                    sh->sums[column][quad * 32 + lane] = total * (double)down;
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh->sums_full);
-                    if (column == 0) {   // (the others write there again only after these have given the sums of products back)
-                        if (!mbar_wait_warp(&sh->sums_full, (segment & 1u) ^ 1u, abort_flag)) break;
-                        const int c = quad * 32 + lane;
-                        const double sum = (sh->sums[0][c] + sh->sums[1][c]) + (sh->sums[2][c] + sh->sums[3][c]);
-                        if (!whole)
-                            e.share_bias[place * P_ROWS + c] = sum;
-                        else if (p < e.P)
-                            e.dbias[p] = (float)sum;
-                    }
-                }
-            }
+            if (!put_away<DW, WIDE, T>(e, sh, worker, t.outer, t.inner, t.left == 1 || t.inner + 1 == t.inners, RUN)) break;
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh->acc_empty);
@@ -2176,7 +2210,7 @@ NarrowSpace narrow_space(const ep_ctx *ctx, int64_t rows, int n_in, int classes,
     s.copies = copies_space(a, rows, n_in, classes, type, aligned, true);
     const int64_t all = ep::ceil_div(rows, TILE) * TILE;
     s.rows = RowInfo{a.take<float>(all), a.take<float>(all), a.take<int>(all)};
-    s.share = a.take<float>((size_t)ctx->sm_count * 2 * P_ROWS * share_width(n_in));
+    s.share = a.take<float>((size_t)ctx->sm_count * 3 * P_ROWS * share_width(n_in));
     s.share_bias = a.take<double>((size_t)ctx->sm_count * 2 * P_ROWS);
     s.blocks = weight_blocks(ctx, rows);
     s.peaks = a.take<float>(s.blocks);

@@ -231,3 +231,44 @@ def test_a_mean_loss_scales_no_gradient(dtype, rows, n_in, classes, sign):
         if dtype == F16:      # below fp16's smallest normal number roundings are larger
             most = most + 2.0 ** -25 / float(want.abs().mean()) * 8 / math.sqrt(want.numel())
         assert abs(common_share(g, want.to(dtype))) <= most
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("n_in", [64, 200])
+def test_long_sums_over_classes_and_over_rows(dtype, n_in):
+    """A column of W (of x) that is 1 throughout: its gradient dx is g (sum of p - 1) = 0, and that of W is dbias.  The tensor cores cut off 1e-7 of a sum of
+    one sign with every 16 products; after 512 steps (fp16; bf16 4096) a sum is put away: 2^-23 512 of it, instead of all 10584.  G's roundings: the
+    target's 1 - p by half the spacing below 1, UNIT / 2; by chance UNIT p a class, less than UNIT / 64 in all; exponentials and lse 2^-19."""
+    steps = 512 if dtype == F16 else 4096
+    rows, classes = 128 * 148 + 50, 169343
+    x, w = rand((rows, n_in), dtype, 1), rand((classes, n_in), dtype, 2, n_in ** -0.5)
+    w[:, 0], x[:, 1] = 1.0, 1.0
+    t = some_targets(rows, classes, 3)
+    r = ep().ep_cross_entropy(x, w, t)
+    got = ep().ep_cross_entropy_backward(x, w, t, r, None, one() * rows, need_dweight=False, need_dbias=False)
+    off = steps * 2.0 ** -23 + ref.UNIT[dtype] / 2 + ref.UNIT[dtype] / 64 + 2.0 ** -19
+    ref.within(got.dx[:, 0], torch.zeros(rows), torch.full((rows,), off), "dx")
+    # on average what rounding leaves is the mean of p where 1 - p is rounded to 1
+    p = torch.exp(-r.row_loss.double())
+    assert abs(float(got.dx[:, 0].double().mean())) <= steps * 2.0 ** -23 + float(p.clamp(max=ref.UNIT[dtype] / 2).mean()) + 2.0 ** -19
+    # and over rows: the parts of dbias of one sign are the probabilities' sum and the targets'
+    rows, classes = 169343, 128 * 148 + 50
+    x, w, t = rand((rows, n_in), dtype, 4), w[:classes], some_targets(rows, classes, 5)
+    x[:, 1] = 1.0
+    r = ep().ep_cross_entropy(x, w, t)
+    got = ep().ep_cross_entropy_backward(x, w, t, r, None, one() * rows, need_dx=False)
+    sizes = 2 * torch.bincount(t.long(), minlength=classes).double() + got.dbias.double()
+    off = (steps * 2.0 ** -23 + ref.UNIT[dtype] / 64) * sizes + ref.UNIT[dtype] * got.dbias.double().abs() + ref.UNIT[dtype] * sizes.sqrt()
+    ref.within(got.dweight[:, 1], got.dbias, off, "dweight")
+
+
+@pytest.mark.parametrize("n_in", [64, 200])
+def test_sums_that_are_put_away_on_the_way(n_in):
+    # a block's stretch is more than the 64 tiles of 128 rows after which fp16 sums are put away, and neither begins nor ends with a row tile
+    rows, classes = 128 * 148 + 50, 9000
+    x, w, t = trained(rows, n_in, classes, F16, 50, 0.1)
+    b = rand((classes,), F32, 51)
+    r = forward(x, w, t, b)
+    whole = backward(x, w, t, r, b, one() * 1000)
+    again = ep().ep_cross_entropy_backward(x, w, t, r, b, one() * 1000, need_dx=False)
+    assert torch.equal(again.dweight, whole.dweight) and torch.equal(again.dbias, whole.dbias)
