@@ -321,7 +321,8 @@ struct Items {
     __device__ __forceinline__ int kbn() const { return (g.kb - split + g.splits - 1) / g.splits; }
 };
 
-template <int BN, Kind KIND, int PARTS, bool RUNS, bool PAIR, typename O>
+// FACTOR: bf16 results that are multiplied by e.factor (apart from those that are not, which the question cost 4 % where the epilogue is the bound).
+template <int BN, Kind KIND, int PARTS, bool RUNS, bool PAIR, typename O, bool FACTOR>
 __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linear_tiles(const __grid_constant__ CUtensorMap map_a,
                                                                 const __grid_constant__ CUtensorMap map_b,
                                                                 const __grid_constant__ CUtensorMap map_out,
@@ -490,7 +491,7 @@ __global__ void __launch_bounds__(TileMemory<BN, PARTS, PAIR>::THREADS, 1) linea
         uint32_t acc = 0;
         bool ok = true;
         const bool by_tma = e.tma && !e.share, with_z = e.preact != nullptr;
-        const bool scaled = sizeof(O) == 2 && e.factor && !e.share;   // (shares are joined first)
+        const bool scaled = (FACTOR || std::is_same_v<O, __half>) && e.factor && !e.share;   // (shares are joined first)
         const float factor = scaled ? *e.factor : 1.f;
         // The residual is copied into the slot that the result will leave from, and added in place.
         auto fetch_residual = [&](int64_t row0, int col) {
@@ -1230,7 +1231,9 @@ struct Maps {
 
 template <int BN, Kind KIND, int PARTS, bool RUNS, bool PAIR, typename O>
 int launch_tiles(ep_ctx *ctx, const GemmPlan &p, const Maps &m, const Epilogue &e, cudaStream_t stream) {
-    auto kernel = linear_tiles<BN, KIND, PARTS, RUNS, PAIR, O>;
+    auto kernel = linear_tiles<BN, KIND, PARTS, RUNS, PAIR, O, false>;
+    if constexpr (KIND == HALF && std::is_same_v<O, __nv_bfloat16>)
+        if (e.factor && !e.share) kernel = linear_tiles<BN, KIND, PARTS, RUNS, PAIR, O, true>;
     constexpr size_t smem = TileMemory<BN, PARTS, PAIR>::TOTAL;
     EP_CUDA(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     cudaLaunchConfig_t cfg{};
