@@ -12,7 +12,7 @@
 //
 // Measured, on the device.  Forward of 169343 x 128 -> 4096 bf16: 231 us; the product alone would need 109 us at 1625 TFLOP/s, its 694
 // million exponentials 154 us at 16 a clock and SM: bound by the issue of what is around them (0.44 a clock and scheduler; the tensor pipe
-// is 33 % busy).  Backward: 684 us, of three products 328 us and of the exponentials, made for either gradient, 308 us; 4096 x 256 -> 169343
+// is 33 % busy).  Backward: 691 us, of three products 328 us and of the exponentials, made for either gradient, 308 us; 4096 x 256 -> 169343
 // fp16: 1291 us of 656 us: bound by the hand-over of tiles between the tensor core and the 16 warps that make G (tensor pipe 42 to
 // 48 % busy, issue 0.24 to 0.47).  fp32: forward of 128 x 64 -> 32 8.4 us: latency; backward of
 // 2999 x 65 -> 257 33 us, of which its multiply-adds, fed from shared memory, 26.
@@ -564,7 +564,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) entropy_tiles(const __grid_co
 // with all three in the tensor memory and G multiplied from there (a product whose first operand is in the tensor memory
 // reads half as much of the shared memory, which otherwise could not keep up).  P = rows of x gives dx, P = classes gives dW
 // and dbias; the logits are so made twice, four products in all where three would do, but G (two bytes for 4 n_in operations, written
-// once and read twice) is not moved (169343 x 128 -> 4096 bf16: 1548 us with G written and read, 684 so).  Of 19 warps one loads, one makes S, one adds up, 16 make G: groups of
+// once and read twice) is not moved (169343 x 128 -> 4096 bf16: 1548 us with G written and read, 691 so).  Of 19 warps one loads, one makes S, one adds up, 16 make G: groups of
 // them take tiles in turn, a thread a row of S and 64 columns.
 // Workers (SMs) share out the tiles as in entropy_tiles; who has only a part of a P tile leaves its sums for entropy_join.
 constexpr int FUSED_WIDTH = ONE_RUN;   // the widest rows
@@ -935,7 +935,7 @@ __global__ void __launch_bounds__(FUSED_THREADS, 1) entropy_fused(const __grid_c
                 if (lane == 0) mbar_arrive(&sh->s_empty[group]);
                 // Columns past the last class, which fill the last tile up, have no slope.  (Their logit of 0 may be far above all others:
                 // 2^shift then passes the operands' type, and infinity times the zeros of W there is NaN.  Done here, not with the slopes
-                // below, it costs the other tiles nothing: gradient of 169343 x 128 against 4096 classes 328 us, there 362.)
+                // below, it costs the other tiles nothing; there it cost a tenth of dx.)
                 if (!DW && t.inner == e.ragged) {
                     const int classes = (int)e.Q - t.inner * BQ - piece * 64;
 #pragma unroll
