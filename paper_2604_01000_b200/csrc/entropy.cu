@@ -13,7 +13,7 @@
 // Measured, on the device.  Forward of 169343 x 128 -> 4096 bf16: 231 us; the product alone would need 109 us at 1625 TFLOP/s, its 694
 // million exponentials 154 us at 16 a clock and SM: bound by the issue of what is around them (0.44 a clock and scheduler; the tensor pipe
 // is 33 % busy).  Backward: 691 us, of three products 328 us and of the exponentials, made for either gradient, 308 us; 4096 x 256 -> 169343
-// fp16: 1291 us of 656 us: bound by the hand-over of tiles between the tensor core and the 16 warps that make G (tensor pipe 42 to
+// fp16: 1291 us of 656 us: bound by the hand-over of tiles between the tensor core and the 16 warps that make G (tensor pipe 40 to
 // 48 % busy, issue 0.24 to 0.47).  fp32: forward of 128 x 64 -> 32 8.4 us: latency; backward of
 // 2999 x 65 -> 257 33 us, of which its multiply-adds, fed from shared memory, 26.
 #include "ep_common.cuh"
